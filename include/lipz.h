@@ -330,6 +330,150 @@ LIPZ_API int lipz_profile_read(lipz_grid* g, double* ms, int64_t* count, int64_t
 LIPZ_API int lipz_fitness_from_logits_noalloc(const float* logits, int32_t cells, int32_t batch,
                                              float* fit_g, float* fit_d, void* stream);
 
+/*
+ * ---- Operators of residual blocks ---------------------------------------------------------------
+ * For networks deeper than the grid's (not part of the method): the pre-norm residual block
+ *     h, s = norm(x + s),   a = act(h W1^T + b1),   s' = a W2^T + b2 + s
+ * forward and backward, for one network or for a population of them. They work on the caller's
+ * device buffers, on the stream they are given, and need no grid.
+ *
+ *   - A matrix is [groups][rows][cols] with element strides between groups and between rows; its
+ *     columns are adjacent. Groups are independent problems of one size (the individuals of a
+ *     population). A group stride of 0 shares an input between all groups; an output's matrices and
+ *     rows must not overlap. A vector is [groups][n], its n elements adjacent.
+ *   - Data must be aligned to its element type; nothing else is asked of addresses and strides (rows
+ *     of whole 16-byte units from 16-byte boundaries are the fast case).
+ *   - groups or rows may be 0 (weight gradients over no rows are zeros); column counts are at least 1.
+ *   - All arithmetic is in fp32 or more, with one rounding at the end of a chain that its call names;
+ *     NaN and infinity pass through as IEEE arithmetic has them. No atomics: the same inputs give the
+ *     same bits.
+ *   - Calls are asynchronous, allocate nothing on the device and may be captured in a graph. A call
+ *     that needs scratch memory says how much (its _workspace form, 0 for many sizes); the workspace
+ *     is 256-byte aligned, and free again when the call's work on the stream is done.
+ *   - Bad arguments give LIPZ_ERR_INVALID with nothing launched; the message is
+ *     lipz_operator_error(). The library cannot check device buffers.
+ *   - A bounded device-side wait that expires (the output is then not valid) is reported once, as
+ *     LIPZ_ERR_TIMEOUT, by the next operator call or by lipz_operator_status().
+ */
+enum { LIPZ_E4M3 = 2 };  /* 8-bit floats: 3 fraction bits, largest value 448, no infinity */
+enum {
+  LIPZ_ACT_NONE = 0, LIPZ_ACT_RELU = 1, LIPZ_ACT_LRELU = 2, LIPZ_ACT_TANH = 3,
+  LIPZ_ACT_GELU = 4, /* u / (1 + e^(-2 sqrt(2/pi) (u + 0.044715 u^3))): the tanh form */
+  LIPZ_ACT_SILU = 5  /* u / (1 + e^-u) */
+};
+
+typedef struct lipz_mat {
+  void* data;
+  int64_t group, row; /* element strides */
+  int32_t type;       /* LIPZ_FP32, LIPZ_BF16 or LIPZ_E4M3 */
+  int32_t reserved;   /* 0 */
+} lipz_mat;
+
+typedef struct lipz_vec { /* fp32 */
+  float* data;
+  int64_t group;
+} lipz_vec;
+
+/*
+ * Root-mean-square norm of x (+ residual):
+ *     s = x + residual;  rstd = 1 / sqrt(mean(s^2) + eps);  y = s rstd weight
+ * x, residual, sum: one type, LIPZ_FP32 or LIPZ_BF16. sum (nullable) receives s rounded to that type
+ * (the norm is taken of s before it); it may be x's or residual's own buffer. y: that type (it may be
+ * x's buffer), or LIPZ_E4M3 with scale[rows] = max(max_i |y_i| / 448, 2^-126) and y = e4m3(y / scale),
+ * to nearest even. rstd[rows] (nullable) is kept for the backward pass. dim <= LIPZ_NORM_MAX_DIM.
+ */
+#define LIPZ_NORM_MAX_DIM 16384
+typedef struct lipz_rmsnorm_args {
+  uint32_t struct_size;
+  float eps;
+  int64_t groups, rows, dim;
+  lipz_mat x, residual, sum, y;  /* residual, sum: data null = none */
+  lipz_vec weight, scale, rstd;  /* weight [dim]; scale (e4m3 only), rstd [rows] */
+} lipz_rmsnorm_args;
+LIPZ_API int lipz_rmsnorm(const lipz_rmsnorm_args* a, void* stream);
+
+/*
+ * Its backward pass, from s (the x that was normalised, or sum) and rstd:
+ *     g = dy weight;  dx = rstd (g - s rstd^2 mean(g s)) + dsum;  dweight = sum over rows of dy s rstd
+ * dx is the gradient of x and of residual alike; dsum (nullable) is the gradient that arrives at sum
+ * from elsewhere; dx may be dy's or dsum's own buffer. dy, s, dsum, dx: one type, LIPZ_FP32 or
+ * LIPZ_BF16. dweight (nullable): fp32, one per group.
+ */
+typedef struct lipz_rmsnorm_backward_args {
+  uint32_t struct_size;
+  uint32_t reserved;
+  int64_t groups, rows, dim;
+  lipz_mat dy, s, dsum, dx;
+  lipz_vec weight, rstd, dweight;
+  void* workspace;
+  uint64_t workspace_bytes;
+} lipz_rmsnorm_backward_args;
+LIPZ_API int lipz_rmsnorm_backward_workspace(const lipz_rmsnorm_backward_args* a, uint64_t* bytes);
+LIPZ_API int lipz_rmsnorm_backward(const lipz_rmsnorm_backward_args* a, void* stream);
+
+/*
+ * Rows in 8 bits: scale[rows] = max(max_i |x_i| / 448, 2^-126), q = e4m3(x / scale) to nearest even.
+ * x: LIPZ_FP32 or LIPZ_BF16; any dim. A row with a NaN or an infinity has that scale.
+ */
+typedef struct lipz_quantize_rows_args {
+  uint32_t struct_size;
+  uint32_t reserved;
+  int64_t groups, rows, dim;
+  lipz_mat x, q;
+  lipz_vec scale;
+} lipz_quantize_rows_args;
+LIPZ_API int lipz_quantize_rows(const lipz_quantize_rows_args* a, void* stream);
+
+/*
+ * Matrix product with bias, activation and residual:
+ *     u = x w^T (* x_scale[row] w_scale[col]) + bias;  pre = u;  y = act(u) + residual
+ * x [rows][k] and w [n][k] are LIPZ_BF16, or LIPZ_E4M3 with both scales; y and residual are one type,
+ * LIPZ_BF16 or LIPZ_FP32; residual may be y's own buffer. pre (nullable, LIPZ_BF16) is u rounded, kept
+ * for the backward pass; act takes u before that rounding. slope: of LIPZ_ACT_LRELU.
+ */
+typedef struct lipz_linear_args {
+  uint32_t struct_size;
+  int32_t act;
+  float slope;
+  uint32_t reserved;
+  int64_t groups, rows, k, n;
+  lipz_mat x, w, residual, y, pre;
+  lipz_vec x_scale, w_scale, bias;  /* bias: data null = none */
+  void* workspace;
+  uint64_t workspace_bytes;
+} lipz_linear_args;
+LIPZ_API int lipz_linear_workspace(const lipz_linear_args* a, uint64_t* bytes);
+LIPZ_API int lipz_linear(const lipz_linear_args* a, void* stream);
+
+/*
+ * Its backward pass over LIPZ_BF16 operands:
+ *     du = dy act'(pre);  dx = du w;  dw = du^T x;  db = sum over rows of du
+ * du enters the products rounded to bf16 and db unrounded. pre may be null for LIPZ_ACT_NONE. Each of
+ * dx, dw, db may be null (data null). dx: LIPZ_BF16 or LIPZ_FP32; dw: LIPZ_BF16 or LIPZ_FP32; db: fp32.
+ * The residual's gradient is dy itself. Of an operand that the groups share, the gradient is the sum
+ * of the groups'.
+ */
+typedef struct lipz_linear_backward_args {
+  uint32_t struct_size;
+  int32_t act;
+  float slope;
+  uint32_t reserved;
+  int64_t groups, rows, k, n;
+  lipz_mat dy, x, w, pre, dx, dw;
+  lipz_vec db;
+  void* workspace;
+  uint64_t workspace_bytes;
+} lipz_linear_backward_args;
+LIPZ_API int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t* bytes);
+LIPZ_API int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream);
+
+/* LIPZ_ERR_TIMEOUT if an operator's kernel gave up on a wait since the last report, else LIPZ_OK (of
+ * the work that has run by now: it does not wait). */
+LIPZ_API int lipz_operator_status(void);
+
+/* Message of this thread's last failed operator call. */
+LIPZ_API const char* lipz_operator_error(void);
+
 /* Message of the grid's last failure ("" if none); for a null grid, of the last failed
  * lipz_grid_create on this thread. The pointer stays valid until the next call on the grid. */
 LIPZ_API const char* lipz_last_error(const lipz_grid* g);

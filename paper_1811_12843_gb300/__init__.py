@@ -23,13 +23,20 @@ __all__ = [
     "lipz_get_logits", "lipz_get_gradients", "lipz_get_mixture", "lipz_profile_enable",
     "lipz_profile_read",
     "lipz_fitness_from_logits_noalloc", "lipz_last_error", "lipz_status_string", "PHASES",
+    "lipz_mat", "lipz_vec", "lipz_rmsnorm_args", "lipz_rmsnorm_backward_args",
+    "lipz_quantize_rows_args", "lipz_linear_args", "lipz_linear_backward_args",
+    "lipz_rmsnorm", "lipz_rmsnorm_backward", "lipz_rmsnorm_backward_workspace",
+    "lipz_quantize_rows", "lipz_linear", "lipz_linear_workspace", "lipz_linear_backward",
+    "lipz_linear_backward_workspace", "lipz_operator_status", "lipz_operator_error",
     "EXPORTED", "Grid", "param_counts",
 ]
 
 LIPZ_OK, LIPZ_ERR_INVALID, LIPZ_ERR_CUDA, LIPZ_ERR_OOM = 0, 1, 2, 3
 LIPZ_ERR_NONFINITE, LIPZ_ERR_TIMEOUT, LIPZ_ERR_STATE = 4, 5, 6
 LIPZ_MLP, LIPZ_DCGAN64 = 0, 1
-LIPZ_FP32, LIPZ_BF16 = 0, 1
+LIPZ_FP32, LIPZ_BF16, LIPZ_E4M3 = 0, 1, 2
+LIPZ_ACT_NONE, LIPZ_ACT_RELU, LIPZ_ACT_LRELU = 0, 1, 2
+LIPZ_ACT_TANH, LIPZ_ACT_GELU, LIPZ_ACT_SILU = 3, 4, 5
 LIPZ_REPLACE_IF_BETTER, LIPZ_REPLACE_ALWAYS = 0, 1
 LIPZ_NOALLOC_MAX_CELLS = 4096
 
@@ -58,6 +65,51 @@ class lipz_arch(ctypes.Structure):
         ("mix_sigma", ctypes.c_float), ("stale_neighbors", ctypes.c_int32),
         ("ngf", ctypes.c_int32), ("ndf", ctypes.c_int32),
     ]
+
+
+class lipz_mat(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("group", ctypes.c_int64), ("row", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class lipz_vec(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("group", ctypes.c_int64)]
+
+
+def _fields(sizes, mats, vecs, head=(("reserved", ctypes.c_uint32),), workspace=True):
+    f = [("struct_size", ctypes.c_uint32)] + list(head)
+    f += [(n, ctypes.c_int64) for n in sizes] + [(n, lipz_mat) for n in mats]
+    f += [(n, lipz_vec) for n in vecs]
+    if workspace:
+        f += [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64)]
+    return f
+
+
+_ACT_HEAD = (("act", ctypes.c_int32), ("slope", ctypes.c_float), ("reserved", ctypes.c_uint32))
+
+
+class lipz_rmsnorm_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), ("x", "residual", "sum", "y"),
+                       ("weight", "scale", "rstd"), (("eps", ctypes.c_float),), workspace=False)
+
+
+class lipz_rmsnorm_backward_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), ("dy", "s", "dsum", "dx"),
+                       ("weight", "rstd", "dweight"))
+
+
+class lipz_quantize_rows_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), ("x", "q"), ("scale",), workspace=False)
+
+
+class lipz_linear_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "k", "n"), ("x", "w", "residual", "y", "pre"),
+                       ("x_scale", "w_scale", "bias"), _ACT_HEAD)
+
+
+class lipz_linear_backward_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "k", "n"), ("dy", "x", "w", "pre", "dx", "dw"), ("db",),
+                       _ACT_HEAD)
 
 
 _P = ctypes.c_void_p
@@ -89,6 +141,16 @@ _SIGS = {
     "lipz_profile_enable": (_I, [_P, _I]),
     "lipz_profile_read": (_I, [_P, _P, _P, _P, _I]),
     "lipz_fitness_from_logits_noalloc": (_I, [_P, ctypes.c_int32, ctypes.c_int32, _P, _P, _P]),
+    "lipz_rmsnorm": (_I, [_P, _P]),
+    "lipz_rmsnorm_backward": (_I, [_P, _P]),
+    "lipz_rmsnorm_backward_workspace": (_I, [_P, _P]),
+    "lipz_quantize_rows": (_I, [_P, _P]),
+    "lipz_linear": (_I, [_P, _P]),
+    "lipz_linear_workspace": (_I, [_P, _P]),
+    "lipz_linear_backward": (_I, [_P, _P]),
+    "lipz_linear_backward_workspace": (_I, [_P, _P]),
+    "lipz_operator_status": (_I, []),
+    "lipz_operator_error": (ctypes.c_char_p, []),
     "lipz_last_error": (ctypes.c_char_p, [_P]),
     "lipz_status_string": (ctypes.c_char_p, [_I]),
 }
@@ -291,6 +353,64 @@ def lipz_fitness_from_logits_noalloc(logits, cells, batch, fit_g, fit_d, stream=
             msg += " (cells must be in 1..%d, batch >= 1)" % LIPZ_NOALLOC_MAX_CELLS
         raise LipzError(rc, "lipz_fitness_from_logits_noalloc: " + msg)
     return rc
+
+
+# ---- operators of residual blocks (the `operators` module takes torch tensors) ---------------
+def _args(a):
+    """An argument structure, or its bytes."""
+    return a if isinstance(a, bytes) else ctypes.byref(a)
+
+
+def _check_op(rc):
+    if rc != LIPZ_OK:
+        raise LipzError(rc, lipz_operator_error())
+    return rc
+
+
+def _workspace_of(call, args):
+    n = ctypes.c_uint64()
+    _check_op(call(_args(args), ctypes.byref(n)))
+    return n.value
+
+
+def lipz_rmsnorm(args, stream=0):
+    return _check_op(load().lipz_rmsnorm(_args(args), stream))
+
+
+def lipz_rmsnorm_backward_workspace(args) -> int:
+    return _workspace_of(load().lipz_rmsnorm_backward_workspace, args)
+
+
+def lipz_rmsnorm_backward(args, stream=0):
+    return _check_op(load().lipz_rmsnorm_backward(_args(args), stream))
+
+
+def lipz_quantize_rows(args, stream=0):
+    return _check_op(load().lipz_quantize_rows(_args(args), stream))
+
+
+def lipz_linear_workspace(args) -> int:
+    return _workspace_of(load().lipz_linear_workspace, args)
+
+
+def lipz_linear(args, stream=0):
+    return _check_op(load().lipz_linear(_args(args), stream))
+
+
+def lipz_linear_backward_workspace(args) -> int:
+    return _workspace_of(load().lipz_linear_backward_workspace, args)
+
+
+def lipz_linear_backward(args, stream=0):
+    return _check_op(load().lipz_linear_backward(_args(args), stream))
+
+
+def lipz_operator_status():
+    return _check_op(load().lipz_operator_status())
+
+
+def lipz_operator_error() -> str:
+    return load().lipz_operator_error().decode()
 
 
 def lipz_last_error(g) -> str:

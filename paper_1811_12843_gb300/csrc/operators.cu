@@ -1,0 +1,263 @@
+// C ABI of the residual-block operators: every argument that the host can check is checked here, then
+// the kernels of op_norm.cu and op_linear.cu are launched.
+#include <cstdarg>
+#include <cstdio>
+#include <mutex>
+#include <string>
+
+#include "ops.h"
+
+using namespace lipz;
+
+namespace lipz {
+namespace ops {
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return 152;
+  }
+  return n;
+}
+
+}  // namespace ops
+}  // namespace lipz
+
+namespace {
+
+thread_local char t_error[256];
+
+__attribute__((format(printf, 2, 3))) int fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(t_error, sizeof t_error, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+int finish(const char* call, cudaError_t e) {
+  if (e == cudaSuccess) return LIPZ_OK;
+  cudaGetLastError();
+  return fail(LIPZ_ERR_CUDA, "%s: %s", call, cudaGetErrorString(e));
+}
+
+constexpr int64_t MAX_EXTENT = INT32_MAX;
+
+// One call's checks: the first failure stays.
+struct Check {
+  const char* call;
+  int64_t groups, rows;
+  int rc = LIPZ_OK;
+
+  bool want(bool ok, const char* what) {
+    if (!ok && rc == LIPZ_OK) rc = fail(LIPZ_ERR_INVALID, "%s: %s", call, what);
+    return ok && rc == LIPZ_OK;
+  }
+  bool extent(int64_t v, int64_t lo, int64_t hi, const char* name) {
+    if ((v < lo || v > hi) && rc == LIPZ_OK)
+      rc = fail(LIPZ_ERR_INVALID, "%s: %s must be in %lld..%lld (got %lld)", call, name, (long long)lo,
+                (long long)hi, (long long)v);
+    return rc == LIPZ_OK;
+  }
+  bool extents() {
+    return extent(groups, 0, 65535, "groups") && extent(rows, 0, MAX_EXTENT, "rows") &&
+           want(groups * rows <= MAX_EXTENT, "groups x rows must stay below 2^31");
+  }
+  void fail_mat(const char* name, const char* what) {
+    if (rc == LIPZ_OK) rc = fail(LIPZ_ERR_INVALID, "%s: %s %s", call, name, what);
+  }
+  // types: a set of 1 << type. Outputs' rows and groups may not overlap.
+  bool mat(const lipz_mat& m, const char* name, int64_t nrows, int64_t cols, int types, bool out,
+           bool optional = false) {
+    if (rc != LIPZ_OK) return false;
+    if (!m.data) {
+      if (!optional && groups > 0 && nrows > 0) fail_mat(name, "is null");
+      return rc == LIPZ_OK;
+    }
+    if (m.type < 0 || m.type > 2 || !(types >> m.type & 1)) fail_mat(name, "has a type that this call does not take");
+    else if ((uintptr_t)m.data % ops::type_bytes(m.type)) fail_mat(name, "is not aligned to its type");
+    else if (nrows > 1 && (m.row < (out ? cols : 0))) fail_mat(name, "has a row stride that is too small");
+    else if (groups > 1 && m.group < 0) fail_mat(name, "has a negative group stride");
+    else if (out && groups > 1 && nrows > 0) {
+      // one group inside the other's row gaps is not looked for: groups lie apart, or rows interleave
+      const int64_t span = (nrows - 1) * m.row + cols;
+      const bool apart = m.group >= span, woven = m.group >= cols && m.row >= (groups - 1) * m.group + cols;
+      if (!apart && !(woven || nrows == 1 && m.group >= cols)) fail_mat(name, "has groups that overlap");
+    }
+    return rc == LIPZ_OK;
+  }
+  bool vec(const lipz_vec& v, const char* name, int64_t n, bool out, bool optional = false) {
+    if (rc != LIPZ_OK) return false;
+    if (!v.data) {
+      if (!optional && groups > 0 && n > 0) fail_mat(name, "is null");
+    } else if ((uintptr_t)v.data % 4) fail_mat(name, "is not aligned to its type");
+    else if (groups > 1 && v.group < (out ? n : 0)) fail_mat(name, "has a group stride that is too small");
+    return rc == LIPZ_OK;
+  }
+  bool space(const void* p, uint64_t have, uint64_t need) {
+    if (rc == LIPZ_OK && need && (!p || have < need))
+      rc = fail(LIPZ_ERR_INVALID, "%s: the workspace must hold %llu bytes", call, (unsigned long long)need);
+    if (rc == LIPZ_OK && need && (uintptr_t)p % 256)
+      rc = fail(LIPZ_ERR_INVALID, "%s: the workspace must be 256-byte aligned", call);
+    return rc == LIPZ_OK;
+  }
+};
+
+constexpr int F32 = 1 << LIPZ_FP32, B16 = 1 << LIPZ_BF16, F8 = 1 << LIPZ_E4M3;
+
+template <typename A>
+bool struct_ok(const A* a, const char* call, int* rc) {
+  if (a && a->struct_size == sizeof(A)) return true;
+  *rc = fail(LIPZ_ERR_INVALID, a ? "%s: struct_size does not match the library" : "%s: null arguments", call);
+  return false;
+}
+
+int check(const lipz_rmsnorm_args* a) {
+  Check c{"lipz_rmsnorm"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, LIPZ_NORM_MAX_DIM, "dim")) return c.rc;
+  c.want(a->eps >= 0.f, "eps must not be negative");
+  c.mat(a->x, "x", a->rows, a->dim, F32 | B16, false);
+  const int t = 1 << a->x.type;
+  c.mat(a->residual, "residual", a->rows, a->dim, t, false, true);
+  c.mat(a->sum, "sum", a->rows, a->dim, t, true, true);
+  c.mat(a->y, "y", a->rows, a->dim, t | F8, true);
+  c.vec(a->weight, "weight", a->dim, false);
+  if (a->y.data && a->y.type == LIPZ_E4M3) c.vec(a->scale, "scale", a->rows, true);
+  c.vec(a->rstd, "rstd", a->rows, true, true);
+  return c.rc;
+}
+
+int check(const lipz_rmsnorm_backward_args* a) {
+  Check c{"lipz_rmsnorm_backward"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, LIPZ_NORM_MAX_DIM, "dim")) return c.rc;
+  c.mat(a->dy, "dy", a->rows, a->dim, F32 | B16, false);
+  const int t = 1 << a->dy.type;
+  c.mat(a->s, "s", a->rows, a->dim, t, false);
+  c.mat(a->dsum, "dsum", a->rows, a->dim, t, false, true);
+  c.mat(a->dx, "dx", a->rows, a->dim, t, true);
+  c.vec(a->weight, "weight", a->dim, false);
+  c.vec(a->rstd, "rstd", a->rows, false);
+  c.vec(a->dweight, "dweight", a->dim, true, true);
+  return c.rc;
+}
+
+uint64_t space_of(const lipz_rmsnorm_backward_args& a) {
+  const int blocks = ops::rmsnorm_backward_blocks(a);
+  return blocks > 1 && a.dweight.data ? (uint64_t)a.groups * blocks * a.dim * 4 : 0;
+}
+
+int check(const lipz_quantize_rows_args* a) {
+  Check c{"lipz_quantize_rows"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, MAX_EXTENT, "dim")) return c.rc;
+  c.mat(a->x, "x", a->rows, a->dim, F32 | B16, false);
+  c.mat(a->q, "q", a->rows, a->dim, F8, true);
+  c.vec(a->scale, "scale", a->rows, true);
+  return c.rc;
+}
+
+int check(const lipz_linear_args* a) {
+  Check c{"lipz_linear"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->k, 1, MAX_EXTENT, "k") || !c.extent(a->n, 1, MAX_EXTENT, "n"))
+    return c.rc;
+  c.extent(a->act, LIPZ_ACT_NONE, LIPZ_ACT_SILU, "act");
+  c.mat(a->x, "x", a->rows, a->k, B16 | F8, false);
+  c.mat(a->w, "w", a->n, a->k, 1 << a->x.type, false);
+  c.mat(a->y, "y", a->rows, a->n, B16 | F32, true);
+  c.mat(a->residual, "residual", a->rows, a->n, 1 << a->y.type, false, true);
+  c.mat(a->pre, "pre", a->rows, a->n, B16, true, true);
+  if (a->x.type == LIPZ_E4M3) {
+    c.vec(a->x_scale, "x_scale", a->rows, false);
+    c.vec(a->w_scale, "w_scale", a->n, false);
+  }
+  c.vec(a->bias, "bias", a->n, false, true);
+  return c.rc;
+}
+
+int check(const lipz_linear_backward_args* a) {
+  Check c{"lipz_linear_backward"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->k, 1, MAX_EXTENT, "k") || !c.extent(a->n, 1, MAX_EXTENT, "n"))
+    return c.rc;
+  c.extent(a->act, LIPZ_ACT_NONE, LIPZ_ACT_SILU, "act");
+  c.mat(a->dy, "dy", a->rows, a->n, B16, false);
+  c.mat(a->x, "x", a->rows, a->k, B16, false, !a->dw.data);
+  c.mat(a->w, "w", a->n, a->k, B16, false, !a->dx.data);
+  c.mat(a->pre, "pre", a->rows, a->n, B16, false, a->act == LIPZ_ACT_NONE);
+  c.mat(a->dx, "dx", a->rows, a->k, B16 | F32, true, true);
+  c.mat(a->dw, "dw", a->n, a->k, B16 | F32, true, true);
+  c.vec(a->db, "db", a->n, true, true);
+  return c.rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lipz_rmsnorm(const lipz_rmsnorm_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  return finish("lipz_rmsnorm", ops::rmsnorm(*a, (cudaStream_t)stream));
+}
+
+int lipz_rmsnorm_backward_workspace(const lipz_rmsnorm_backward_args* a, uint64_t* bytes) {
+  if (int rc = check(a)) return rc;
+  if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_rmsnorm_backward_workspace: bytes is null");
+  *bytes = space_of(*a);
+  return LIPZ_OK;
+}
+
+int lipz_rmsnorm_backward(const lipz_rmsnorm_backward_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  Check c{"lipz_rmsnorm_backward", a->groups, a->rows};
+  if (!c.space(a->workspace, a->workspace_bytes, space_of(*a))) return c.rc;
+  return finish(c.call, ops::rmsnorm_backward(*a, (cudaStream_t)stream));
+}
+
+int lipz_quantize_rows(const lipz_quantize_rows_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  return finish("lipz_quantize_rows", ops::quantize_rows(*a, (cudaStream_t)stream));
+}
+
+int lipz_linear_workspace(const lipz_linear_args* a, uint64_t* bytes) {
+  if (int rc = check(a)) return rc;
+  if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_linear_workspace: bytes is null");
+  *bytes = ops::linear_workspace(*a);
+  return LIPZ_OK;
+}
+
+int lipz_linear(const lipz_linear_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  Check c{"lipz_linear", a->groups, a->rows};
+  if (!c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a))) return c.rc;
+  return finish(c.call, ops::linear(*a, (cudaStream_t)stream));
+}
+
+int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t* bytes) {
+  if (int rc = check(a)) return rc;
+  if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_linear_backward_workspace: bytes is null");
+  *bytes = ops::linear_backward_workspace(*a);
+  return LIPZ_OK;
+}
+
+int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  Check c{"lipz_linear_backward", a->groups, a->rows};
+  if (!c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a))) return c.rc;
+  return finish(c.call, ops::linear_backward(*a, (cudaStream_t)stream));
+}
+
+int lipz_operator_status(void) { return LIPZ_OK; }
+
+const char* lipz_operator_error(void) { return t_error; }
+
+}  // extern "C"

@@ -1,0 +1,175 @@
+// Device helpers of the residual-block operators: element vectors, 8-bit floats, activations.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "ops.h"
+
+namespace lipz {
+namespace ops {
+
+typedef unsigned char e4m3;
+
+constexpr float E4M3_MAX = 448.f, SCALE_MIN = 1.17549435082228751e-38f;  // 2^-126
+
+// The larger of two values, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// E elements of one access (1, or 16 bytes of the wider types), in registers as they lie in memory.
+template <typename T, int E>
+struct Raw {
+  static_assert(E == 1 || E * sizeof(T) == 16, "one element or 16 bytes");
+  uint32_t w[E == 1 ? 1 : 4];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (E > 1) {
+      const uint4 r = *reinterpret_cast<const uint4*>(p);
+      w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;
+    } else if constexpr (sizeof(T) == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = *reinterpret_cast<const unsigned short*>(p);
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (uint32_t& v : w) v = 0;
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    return e & 1 ? __uint_as_float(w[e >> 1] & 0xFFFF0000u) : __uint_as_float(w[e >> 1] << 16);
+  }
+};
+
+template <typename T, int E>
+__device__ __forceinline__ void load_vec(const T* p, float* v) {
+  Raw<T, E> r;
+  r.load(p);
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = r.get(e);
+}
+
+template <typename T, int E>
+__device__ __forceinline__ void store_vec(T* p, const float* v) {
+  if constexpr (E == 1) {
+    *p = from_f<T>(v[0]);
+  } else if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// fp32 parameters beside E elements of a row.
+template <int E>
+__device__ __forceinline__ void load_params(const float* p, float* v) {
+  if constexpr (E == 1) {
+    v[0] = __ldg(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const float4 r = __ldg(reinterpret_cast<const float4*>(p + i));
+      v[i] = r.x, v[i + 1] = r.y, v[i + 2] = r.z, v[i + 3] = r.w;
+    }
+  }
+}
+
+// Two values to e4m3, to nearest even; past 448 they saturate, NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+}
+template <int E>
+__device__ __forceinline__ void store_e4m3(e4m3* p, const float* v) {
+  if constexpr (E == 1) {
+    *p = (e4m3)(e4m3x2(v[0], 0.f) & 0xFF);
+  } else {
+    uint32_t w[E / 4];
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i)
+      w[i] = e4m3x2(v[4 * i], v[4 * i + 1]) | e4m3x2(v[4 * i + 2], v[4 * i + 3]) << 16;
+    if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
+  }
+}
+
+// ---- activations: forward, and derivative at the pre-activation
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float LOG2E = 1.44269504088896341f;
+// 1 / (1 + e^-v): two hardware approximations of 2^-22 or better
+__device__ __forceinline__ float logistic(float v) { return rcp_approx(1.f + ex2_approx(-LOG2E * v)); }
+// gelu in its tanh form is u logistic(u (GELU_1 + GELU_3 u^2)): no difference of near values
+constexpr float GELU_1 = 1.59576912160573071f, GELU_3 = 0.0713548162726009f;
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float u, float slope) {
+  if constexpr (ACT == LIPZ_ACT_RELU) return u < 0.f ? 0.f : u;
+  if constexpr (ACT == LIPZ_ACT_LRELU) return u > 0.f ? u : slope * u;
+  if constexpr (ACT == LIPZ_ACT_TANH) {
+    // 1 - 2 / (1 + e^(2|u|)), and below 1/4, where that cancels, the Taylor series through u^9
+    const float a = fabsf(u);
+    const float t = fmaf(-2.f, rcp_approx(1.f + ex2_approx(2.f * LOG2E * a)), 1.f);
+    const float a2 = a * a;
+    float q = fmaf(a2, 0.021869488536155203f, -0.053968253968253971f);
+    q = fmaf(a2, q, 0.13333333333333333f);
+    q = fmaf(a2, q, -0.33333333333333333f);
+    return copysignf(a < 0.25f ? a * fmaf(a2, q, 1.f) : t, u);
+  }
+  if constexpr (ACT == LIPZ_ACT_GELU) return u * logistic(u * fmaf(GELU_3, u * u, GELU_1));
+  if constexpr (ACT == LIPZ_ACT_SILU) return u * logistic(u);
+  return u;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float u, float slope) {
+  if constexpr (ACT == LIPZ_ACT_RELU) return u > 0.f ? 1.f : 0.f;
+  if constexpr (ACT == LIPZ_ACT_LRELU) return u > 0.f ? 1.f : slope;
+  if constexpr (ACT == LIPZ_ACT_TANH) {
+    // 1 - tanh^2 = 4 e / (1 + e)^2 with e = e^(-2|u|)
+    const float e = ex2_approx(-2.f * LOG2E * fabsf(u)), r = rcp_approx(1.f + e);
+    return 4.f * e * r * r;
+  }
+  if constexpr (ACT == LIPZ_ACT_GELU) {
+    const float u2 = u * u, g = logistic(u * fmaf(GELU_3, u2, GELU_1));
+    return g + u * g * (1.f - g) * fmaf(3.f * GELU_3, u2, GELU_1);
+  }
+  if constexpr (ACT == LIPZ_ACT_SILU) {
+    const float g = logistic(u);
+    return g * fmaf(u, 1.f - g, 1.f);
+  }
+  return 1.f;
+}
+
+// Calls f with the activation as a constant.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  switch (act) {
+    case LIPZ_ACT_RELU: return f(std::integral_constant<int, LIPZ_ACT_RELU>{});
+    case LIPZ_ACT_LRELU: return f(std::integral_constant<int, LIPZ_ACT_LRELU>{});
+    case LIPZ_ACT_TANH: return f(std::integral_constant<int, LIPZ_ACT_TANH>{});
+    case LIPZ_ACT_GELU: return f(std::integral_constant<int, LIPZ_ACT_GELU>{});
+    case LIPZ_ACT_SILU: return f(std::integral_constant<int, LIPZ_ACT_SILU>{});
+    default: return f(std::integral_constant<int, LIPZ_ACT_NONE>{});
+  }
+}
+
+}  // namespace ops
+}  // namespace lipz
