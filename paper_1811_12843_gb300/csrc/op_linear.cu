@@ -1,6 +1,8 @@
-// Matrix product with bias, activation and residual, and its backward pass.
+// Matrix product with bias, activation and residual, and its backward pass: a few rows in a kernel of
+// their own, else by the tensor-core product of op_gemm.cu.
 #include <type_traits>
 
+#include "op_gemm.h"
 #include "ops.cuh"
 
 namespace lipz {
@@ -8,82 +10,152 @@ namespace ops {
 
 namespace {
 
-// C[m][n] = sum_k A(m, k) B(n, k), one problem per group, with the forward's epilogue. Strides in
-// elements along m or n and along k.
-struct Product {
-  const void *a, *b;
-  int64_t ag, am, ak, bg, bn, bk;
-  int64_t m, n, k;
-  int ab_type;
-  lipz_mat y, residual, pre;
-  lipz_vec x_scale, w_scale, bias;
-  int act;
-  float slope;
+// y for a few rows: w's rows stream through the warps of a block, W_ROWS at a time, each warp over its part
+// of k (parts > 1: few columns), and meet the rows of x, which stay in L1. Bound: HBM (w is read once).
+constexpr int W_ROWS = 2, VEC_WARPS = 4;
+
+template <int TYPE>
+struct Elem;
+template <>
+struct Elem<LIPZ_BF16> {
+  typedef bf16 T;
+  static constexpr int E = 8;
+  static __device__ __forceinline__ void decode(const uint4& r, float* v) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ float one(T v) { return __bfloat162float(v); }
+};
+template <>
+struct Elem<LIPZ_E4M3> {
+  typedef e4m3 T;
+  static constexpr int E = 16;
+  static __device__ __forceinline__ void decode(const uint4& r, float* v) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const __half2_raw h =
+          __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (i & 1) * 16), __NV_E4M3);
+      const float2 f = __half22float2(__half2(h));
+      v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ float one(T v) {
+    __nv_fp8_e4m3 f;
+    f.__x = v;
+    return (float)f;
+  }
 };
 
-__device__ __forceinline__ float element(const void* p, int64_t i, int type) {
-  if (type == LIPZ_BF16) return __bfloat162float(reinterpret_cast<const bf16*>(p)[i]);
-  __nv_fp8_e4m3 v;
-  v.__x = reinterpret_cast<const e4m3*>(p)[i];
-  return (float)v;
-}
+struct VecParams {
+  lipz_mat x, w;
+  Epilogue e;
+  int64_t n, k;
+  int rows, parts;  // warps that share an output
+};
 
-__global__ void __launch_bounds__(256) k_product(const Product p) {
-  constexpr int BT = 64, BK = 16;
-  __shared__ float sa[BK][BT + 1], sb[BK][BT + 1];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int64_t m0 = (int64_t)blockIdx.y * BT, n0 = (int64_t)blockIdx.x * BT, g = blockIdx.z;
+template <int TYPE, int R, bool VEC>
+__global__ void __launch_bounds__(32 * VEC_WARPS) k_linear_rows(const VecParams p) {
+  using L = Elem<TYPE>;
+  using T = typename L::T;
+  constexpr int E = VEC ? L::E : 1;
+  __shared__ float s[VEC_WARPS][R * W_ROWS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % p.parts;
+  const int per_block = VEC_WARPS / p.parts * W_ROWS;
+  const int64_t g = blockIdx.y, n0 = (int64_t)blockIdx.x * per_block + warp / p.parts * W_ROWS;
+  const T* x = (const T*)p.x.data + g * p.x.group;
+  const T* w = (const T*)p.w.data + g * p.w.group;
   pdl_wait();
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < p.k; k0 += BK) {
-    for (int i = threadIdx.x; i < BT * BK; i += 256) {
-      const int ra = p.ak == 1 ? i / BK : i % BT, ka = p.ak == 1 ? i % BK : i / BT;
-      const int rb = p.bk == 1 ? i / BK : i % BT, kb = p.bk == 1 ? i % BK : i / BT;
-      sa[ka][ra] = m0 + ra < p.m && k0 + ka < p.k
-                       ? element(p.a, g * p.ag + (m0 + ra) * p.am + (k0 + ka) * p.ak, p.ab_type) : 0.f;
-      sb[kb][rb] = n0 + rb < p.n && k0 + kb < p.k
-                       ? element(p.b, g * p.bg + (n0 + rb) * p.bn + (k0 + kb) * p.bk, p.ab_type) : 0.f;
-    }
-    __syncthreads();
+  float acc[W_ROWS][R];
 #pragma unroll
-    for (int kk = 0; kk < BK; ++kk)
+  for (int j = 0; j < W_ROWS; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int r = 0; r < R; ++r) acc[j][r] = 0.f;
+  const int64_t units = p.k / E, step = 32 * p.parts;
+  int64_t wo[W_ROWS], xo[R];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[i][j] = fmaf(sa[kk][ty + 16 * i], sb[kk][tx + 16 * j], acc[i][j]);
-    __syncthreads();
-  }
-  with_act(p.act, [&](auto act) {
+  for (int j = 0; j < W_ROWS; ++j) wo[j] = min(n0 + j, p.n - 1) * p.w.row;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int r = 0; r < R; ++r) xo[r] = (int64_t)min(r, p.rows - 1) * p.x.row;
+  if (n0 < p.n) {
+#pragma unroll 4
+    for (int64_t u = part * 32 + lane; u < units; u += step) {
+      float wv[W_ROWS][E];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-        if (m >= p.m || n >= p.n) continue;
-        float u = acc[i][j];
-        if (p.x_scale.data)
-          u *= p.x_scale.data[g * p.x_scale.group + m] * p.w_scale.data[g * p.w_scale.group + n];
-        if (p.bias.data) u += p.bias.data[g * p.bias.group + n];
-        if (p.pre.data)
-          reinterpret_cast<bf16*>(p.pre.data)[g * p.pre.group + m * p.pre.row + n] =
-              __float2bfloat16_rn(u);
-        float y = act_value<decltype(act)::value>(u, p.slope);
-        const int64_t ro = g * p.residual.group + m * p.residual.row + n;
-        const int64_t yo = g * p.y.group + m * p.y.row + n;
-        if (p.residual.data)
-          y += p.y.type == LIPZ_FP32 ? reinterpret_cast<const float*>(p.residual.data)[ro]
-                                     : __bfloat162float(reinterpret_cast<const bf16*>(p.residual.data)[ro]);
-        if (p.y.type == LIPZ_FP32) reinterpret_cast<float*>(p.y.data)[yo] = y;
-        else reinterpret_cast<bf16*>(p.y.data)[yo] = __float2bfloat16_rn(y);
+      for (int j = 0; j < W_ROWS; ++j) {
+        if constexpr (VEC) L::decode(__ldg((const uint4*)(w + wo[j] + u * E)), wv[j]);
+        else wv[j][0] = L::one(w[wo[j] + u]);
       }
-  });
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float xv[E];
+        if constexpr (VEC) L::decode(__ldg((const uint4*)(x + xo[r] + u * E)), xv);
+        else xv[0] = L::one(x[xo[r] + u]);
+#pragma unroll
+        for (int j = 0; j < W_ROWS; ++j)
+#pragma unroll
+          for (int i = 0; i < E; ++i) acc[j][r] = fmaf(wv[j][i], xv[i], acc[j][r]);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < W_ROWS; ++j)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) acc[j][r] += __shfl_xor_sync(0xffffffffu, acc[j][r], o);
+      if (lane == 0) s[warp][r * W_ROWS + j] = acc[j][r];
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < per_block * p.rows; i += 32 * VEC_WARPS) {
+    const int c = i % per_block, r = i / per_block;
+    const int64_t n = (int64_t)blockIdx.x * per_block + c;
+    if (n >= p.n) continue;
+    float u = 0.f;
+    for (int q = 0; q < p.parts; ++q) u += s[c / W_ROWS * p.parts + q][r * W_ROWS + c % W_ROWS];
+    finish(p.e, g, r, n, u);
+  }
 }
 
-cudaError_t product(const Product& p, int64_t groups, cudaStream_t st) {
-  return launch_pdl(k_product,
-                    dim3((unsigned)ceil_div(p.n, 64), (unsigned)ceil_div(p.m, 64), (unsigned)groups),
-                    dim3(256), 0, st, p);
+// A few rows go to k_linear_rows.
+constexpr int FEW_ROWS = 4;
+
+template <int TYPE, bool VEC>
+cudaError_t launch_rows(const VecParams& p, dim3 grid, cudaStream_t st) {
+  const dim3 block(32 * VEC_WARPS);
+  if (p.rows == 1) return launch_pdl(k_linear_rows<TYPE, 1, VEC>, grid, block, 0, st, p);
+  if (p.rows == 2) return launch_pdl(k_linear_rows<TYPE, 2, VEC>, grid, block, 0, st, p);
+  return launch_pdl(k_linear_rows<TYPE, 4, VEC>, grid, block, 0, st, p);
+}
+
+cudaError_t linear_rows(const lipz_linear_args& a, const Epilogue& e, cudaStream_t st) {
+  const int per = 16 / type_bytes(a.x.type);
+  const bool vec = a.k % per == 0 && rows_aligned(a.x, a.groups, a.rows, 16) &&
+                   rows_aligned(a.w, a.groups, a.n, 16);
+  // warps share an output where whole rows would leave the SMs with fewer than eight warps each
+  int parts = 1;
+  while (parts < VEC_WARPS && a.groups * ceil_div(a.n, W_ROWS) * parts < 8 * sm_count() &&
+         a.k >= (vec ? per : 1) * 64 * parts)
+    parts *= 2;
+  const VecParams p{a.x, a.w, e, a.n, a.k, (int)a.rows, parts};
+  const dim3 grid((unsigned)ceil_div(a.n, VEC_WARPS / parts * W_ROWS), (unsigned)a.groups);
+  if (a.x.type == LIPZ_E4M3)
+    return vec ? launch_rows<LIPZ_E4M3, true>(p, grid, st) : launch_rows<LIPZ_E4M3, false>(p, grid, st);
+  return vec ? launch_rows<LIPZ_BF16, true>(p, grid, st) : launch_rows<LIPZ_BF16, false>(p, grid, st);
+}
+
+Epilogue epilogue_of(const lipz_linear_args& a) {
+  Epilogue e{a.y, a.residual, a.pre, a.x_scale, a.w_scale, a.bias, a.act, a.slope};
+  if (a.x.type != LIPZ_E4M3) e.x_scale.data = e.w_scale.data = nullptr;
+  return e;
+}
+Gemm gemm_of(const lipz_linear_args& a) {
+  return {{a.x.data, a.x.group, a.x.row, true}, {a.w.data, a.w.group, a.w.row, true}, a.x.type,
+          a.groups, a.rows, a.n, a.k, epilogue_of(a)};
 }
 
 // du = dy act'(pre), in bf16 rows of ldu elements, and the sums of its columns over the block's rows:
@@ -140,11 +212,12 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p) {
   }
 }
 
-// The workspace of a backward call: du, then the parts of db.
+// The workspace of a backward call: du, the parts of db, then the larger of the two products' own.
 struct BackPlan {
   bool vec, need_du;
   int64_t ldu, blocks, rows_per_block;
-  uint64_t du_bytes, bytes;
+  uint64_t du_bytes, db_bytes, bytes;
+  Gemm dx, dw;
 };
 BackPlan back_plan(const lipz_linear_backward_args& a) {
   BackPlan b;
@@ -157,21 +230,32 @@ BackPlan back_plan(const lipz_linear_backward_args& a) {
   const int64_t want = ceil_div(fill, cols * (a.groups > 0 ? a.groups : 1));
   b.rows_per_block = ceil_div(ceil_div(a.rows > 0 ? a.rows : 1, want), 8) * 8;
   b.blocks = ceil_div(a.rows, b.rows_per_block);
-  b.du_bytes = b.need_du ? ceil_div(a.groups * a.rows * b.ldu * 2, 256) * 256 : 0;
-  b.bytes = b.du_bytes + (a.db.data ? (uint64_t)(a.groups * b.blocks * a.n * 4) : 0);
+  auto round256 = [](int64_t v) { return (uint64_t)ceil_div(v, 256) * 256; };
+  b.du_bytes = b.need_du ? round256(a.groups * a.rows * b.ldu * 2) : 0;
+  b.db_bytes = a.db.data ? round256(a.groups * b.blocks * a.n * 4) : 0;
+  const void* d = b.need_du ? a.workspace : a.dy.data;
+  const int64_t dg = b.need_du ? a.rows * b.ldu : a.dy.group, dr = b.need_du ? b.ldu : a.dy.row;
+  b.dx = {{d, dg, dr, true}, {a.w.data, a.w.group, a.w.row, false}, LIPZ_BF16, a.groups, a.rows, a.k,
+          a.n, {a.dx}};
+  b.dw = {{d, dg, dr, false}, {a.x.data, a.x.group, a.x.row, false}, LIPZ_BF16, a.groups, a.n, a.k,
+          a.rows, {a.dw}};
+  const bool none = a.groups == 0 || a.rows == 0;
+  const uint64_t x = a.dx.data && !none ? gemm_workspace(b.dx) : 0;
+  const uint64_t w = a.dw.data && !none ? gemm_workspace(b.dw) : 0;
+  b.bytes = b.du_bytes + b.db_bytes + (x > w ? x : w);
   return b;
 }
 
 }  // namespace
 
-uint64_t linear_workspace(const lipz_linear_args&) { return 0; }
+uint64_t linear_workspace(const lipz_linear_args& a) {
+  return a.groups == 0 || a.rows <= FEW_ROWS ? 0 : gemm_workspace(gemm_of(a));
+}
 
 cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {
   if (a.groups == 0 || a.rows == 0) return cudaSuccess;
-  Product p{a.x.data, a.w.data, a.x.group, a.x.row, 1, a.w.group, a.w.row, 1, a.rows, a.n, a.k,
-            a.x.type, a.y, a.residual, a.pre, a.x_scale, a.w_scale, a.bias, a.act, a.slope};
-  if (a.x.type != LIPZ_E4M3) p.x_scale.data = nullptr;
-  return product(p, a.groups, st);
+  if (a.rows <= FEW_ROWS) return linear_rows(a, epilogue_of(a), st);
+  return gemm(gemm_of(a), a.workspace, st);
 }
 
 uint64_t linear_backward_workspace(const lipz_linear_backward_args& a) { return back_plan(a).bytes; }
@@ -194,6 +278,7 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st)
   const BackPlan b = back_plan(a);
   bf16* du = b.need_du ? (bf16*)a.workspace : nullptr;
   float* part = a.db.data ? (float*)((char*)a.workspace + b.du_bytes) : nullptr;
+  void* rest = (char*)a.workspace + b.du_bytes + b.db_bytes;
   cudaError_t e = cudaSuccess;
   if (du || part) {
     const DuArgs p{a.dy, a.pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope};
@@ -202,16 +287,8 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st)
               : launch_pdl(k_du<1>, grid, dim3(256), 0, st, p);
     if (e == cudaSuccess && part) e = sum_parts(part, a.groups, (int)b.blocks, a.n, a.db, st);
   }
-  const void* d = du ? du : a.dy.data;
-  const int64_t dg = du ? a.rows * b.ldu : a.dy.group, dr = du ? b.ldu : a.dy.row;
-  if (e == cudaSuccess && a.dx.data) {
-    Product p{d, a.w.data, dg, dr, 1, a.w.group, 1, a.w.row, a.rows, a.k, a.n, LIPZ_BF16, a.dx};
-    e = product(p, a.groups, st);
-  }
-  if (e == cudaSuccess && a.dw.data) {
-    Product p{d, a.x.data, dg, 1, dr, a.x.group, 1, a.x.row, a.n, a.k, a.rows, LIPZ_BF16, a.dw};
-    e = product(p, a.groups, st);
-  }
+  if (e == cudaSuccess && a.dx.data) e = gemm(b.dx, rest, st);
+  if (e == cudaSuccess && a.dw.data) e = gemm(b.dw, rest, st);
   return e;
 }
 

@@ -1,11 +1,10 @@
 // C ABI of the residual-block operators: every argument that the host can check is checked here, then
-// the kernels of op_norm.cu and op_linear.cu are launched.
+// the kernels of op_norm.cu, op_linear.cu and op_gemm.cu are launched.
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
-#include <mutex>
-#include <string>
 
-#include "ops.h"
+#include "op_gemm.h"
 
 using namespace lipz;
 
@@ -20,6 +19,26 @@ int sm_count() {
     return 152;
   }
   return n;
+}
+
+// One word of pinned memory, which every device reaches: kernels store to it, the host reads it without
+// waiting for them.
+int* timeout_word() {
+  static int* const word = [] {
+    int* p = nullptr;
+    // (allocating host memory is not part of a graph that another thread's stream may be capturing)
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (cudaHostAlloc((void**)&p, sizeof(int), cudaHostAllocPortable | cudaHostAllocMapped) != cudaSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    } else {
+      *p = 0;
+    }
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    return p;
+  }();
+  return word;
 }
 
 }  // namespace ops
@@ -41,6 +60,17 @@ int finish(const char* call, cudaError_t e) {
   if (e == cudaSuccess) return LIPZ_OK;
   cudaGetLastError();
   return fail(LIPZ_ERR_CUDA, "%s: %s", call, cudaGetErrorString(e));
+}
+
+// Whether a kernel gave up on a wait since the last report (products take the word before they launch).
+std::atomic<bool> g_word_in_use{false};
+int take_timeout(const char* call) {
+  if (!g_word_in_use.load()) return LIPZ_OK;
+  int* word = ops::timeout_word();
+  const int code = word ? __atomic_exchange_n(word, 0, __ATOMIC_ACQ_REL) : 0;
+  if (!code) return LIPZ_OK;
+  return fail(LIPZ_ERR_TIMEOUT, "%s: an earlier product gave up on a wait (%d): its results are not valid",
+              call, code);
 }
 
 constexpr int64_t MAX_EXTENT = INT32_MAX;
@@ -206,6 +236,7 @@ extern "C" {
 
 int lipz_rmsnorm(const lipz_rmsnorm_args* a, void* stream) {
   if (int rc = check(a)) return rc;
+  if (int rc = take_timeout("lipz_rmsnorm")) return rc;
   return finish("lipz_rmsnorm", ops::rmsnorm(*a, (cudaStream_t)stream));
 }
 
@@ -220,11 +251,13 @@ int lipz_rmsnorm_backward(const lipz_rmsnorm_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_rmsnorm_backward", a->groups, a->rows};
   if (!c.space(a->workspace, a->workspace_bytes, space_of(*a))) return c.rc;
+  if (int rc = take_timeout(c.call)) return rc;
   return finish(c.call, ops::rmsnorm_backward(*a, (cudaStream_t)stream));
 }
 
 int lipz_quantize_rows(const lipz_quantize_rows_args* a, void* stream) {
   if (int rc = check(a)) return rc;
+  if (int rc = take_timeout("lipz_quantize_rows")) return rc;
   return finish("lipz_quantize_rows", ops::quantize_rows(*a, (cudaStream_t)stream));
 }
 
@@ -239,6 +272,8 @@ int lipz_linear(const lipz_linear_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear", a->groups, a->rows};
   if (!c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a))) return c.rc;
+  if (int rc = take_timeout(c.call)) return rc;
+  g_word_in_use.store(true);
   return finish(c.call, ops::linear(*a, (cudaStream_t)stream));
 }
 
@@ -253,10 +288,12 @@ int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear_backward", a->groups, a->rows};
   if (!c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a))) return c.rc;
+  if (int rc = take_timeout(c.call)) return rc;
+  g_word_in_use.store(true);
   return finish(c.call, ops::linear_backward(*a, (cudaStream_t)stream));
 }
 
-int lipz_operator_status(void) { return LIPZ_OK; }
+int lipz_operator_status(void) { return take_timeout("lipz_operator_status"); }
 
 const char* lipz_operator_error(void) { return t_error; }
 

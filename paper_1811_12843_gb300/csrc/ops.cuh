@@ -3,8 +3,10 @@
 
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "common.cuh"
-#include "ops.h"
+#include "op_gemm.h"
 
 namespace lipz {
 namespace ops {
@@ -168,6 +170,25 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
     case LIPZ_ACT_GELU: return f(std::integral_constant<int, LIPZ_ACT_GELU>{});
     case LIPZ_ACT_SILU: return f(std::integral_constant<int, LIPZ_ACT_SILU>{});
     default: return f(std::integral_constant<int, LIPZ_ACT_NONE>{});
+  }
+}
+
+// The epilogue of element (m, n) of group g, from its sum u.
+__device__ __forceinline__ void finish(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
+  if (e.w_scale.data)
+    u *= e.x_scale.data[g * e.x_scale.group + m] * e.w_scale.data[g * e.w_scale.group + n];
+  if (e.bias.data) u += e.bias.data[g * e.bias.group + n];
+  if (e.pre.data)
+    ((bf16*)e.pre.data)[g * e.pre.group + m * e.pre.row + n] = __float2bfloat16_rn(u);
+  with_act(e.act, [&](auto act) { u = act_value<decltype(act)::value>(u, e.slope); });
+  const int64_t ro = g * e.residual.group + m * e.residual.row + n;
+  const int64_t yo = g * e.y.group + m * e.y.row + n;
+  if (e.y.type == LIPZ_FP32) {
+    if (e.residual.data) u += ((const float*)e.residual.data)[ro];
+    ((float*)e.y.data)[yo] = u;
+  } else {
+    if (e.residual.data) u += __bfloat162float(((const bf16*)e.residual.data)[ro]);
+    ((bf16*)e.y.data)[yo] = __float2bfloat16_rn(u);
   }
 }
 

@@ -1,5 +1,5 @@
 // Internal interface of the residual-block operators (include/lipz.h): operators.cu checks a call's
-// arguments and launches the kernels of op_norm.cu, op_linear.cu.
+// arguments and launches the kernels of op_norm.cu, op_linear.cu and op_gemm.cu.
 #pragma once
 
 #include <cuda_runtime.h>
