@@ -1,9 +1,11 @@
 // Root-mean-square norm with the residual's addition (forward and backward) and the row quantiser.
 //
 // A row's elements are read once and stay in the registers of its threads (multiples of 32 of them, NV
-// vectors of E elements each) between the row's sums and its results.
+// vectors of E elements each) between the row's sums and its results. Few rows are loaded by their threads;
+// many stream through a ring of shared-memory stages.
 // Bound: HBM; a launch and two memory latencies for a few rows.
 #include "ops.cuh"
+#include "tc_ptx.cuh"
 
 namespace lipz {
 namespace ops {
@@ -15,31 +17,36 @@ struct RowArgs {
   lipz_vec weight, scale, rstd;
   int64_t rows, total;  // of a group, of all
   int dim, tpr, rpb;    // threads per row, rows per block
-  float eps;
+  float eps, inv_dim;
 };
 
-// Sum of a and NaN-propagating maximum of b over the tpr threads of this thread's row. Every thread of
-// the block calls it.
-__device__ __forceinline__ float2 row_reduce(float a, float b, int tpr, float2* s) {
+// A row's sums: of squares, and the largest magnitude's bits (as integers, magnitudes keep their order, with
+// infinity above every number and NaN above that).
+struct Sums {
+  float ss;
+  uint32_t top;
+};
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+template <bool SUM, bool MAX>
+__device__ __forceinline__ Sums warp_reduce(Sums v) {
+  if constexpr (SUM) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, o);
-    b = max_nan(b, __shfl_xor_sync(0xffffffffu, b, o));
+    for (int o = 16; o; o >>= 1) v.ss += __shfl_xor_sync(0xffffffffu, v.ss, o);
   }
-  if (tpr > 32) {
-    const int warp = threadIdx.x >> 5, w = tpr >> 5, first = threadIdx.x / tpr * w;
-    if ((threadIdx.x & 31) == 0) s[warp] = make_float2(a, b);
-    __syncthreads();
-    float2 r = s[first];
-    for (int i = 1; i < w; ++i) {
-      const float2 q = s[first + i];
-      r.x += q.x;
-      r.y = max_nan(r.y, q.y);
-    }
-    __syncthreads();
-    return r;
+  if constexpr (MAX) v.top = __reduce_max_sync(0xffffffffu, v.top);
+  return v;
+}
+// Over the `warps` warps of a row from `first` on, after a barrier; s[i]: warp i's.
+template <bool SUM, bool MAX>
+__device__ __forceinline__ Sums join(const Sums* s, int first, int warps) {
+  Sums r = s[first];
+  for (int i = 1; i < warps; ++i) {
+    const Sums q = s[first + i];
+    if constexpr (SUM) r.ss += q.ss;
+    if constexpr (MAX) r.top = max(r.top, q.top);
   }
-  return make_float2(a, b);
+  return r;
 }
 
 template <typename T>
@@ -47,14 +54,53 @@ __device__ __forceinline__ T* row_of(const lipz_mat& m, int64_t g, int64_t r) {
   return reinterpret_cast<T*>(m.data) + g * m.group + r * m.row;
 }
 
+// (rows of all groups stay below 2^31)
+__device__ __forceinline__ int64_t group_of(const RowArgs& p, int64_t r) {
+  return p.total == p.rows ? 0 : (uint32_t)r / (uint32_t)p.rows;
+}
+
+// A row's results from its sums {sum of squares, largest magnitude} and its elements (times the weights).
+template <typename T, int E, int NV, bool QUANT>
+__device__ __forceinline__ void row_results(const RowArgs& p, int64_t g, int64_t gr, Sums red,
+                                            float (&v)[NV][E], int t, int tpr, int nvec) {
+  float f = 1.f;
+  if (!QUANT) {
+    f = rsqrtf(fmaf(red.ss, p.inv_dim, p.eps));
+    if (t == 0 && p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = f;
+  }
+  if (QUANT || p.scale.data) {
+    const float top = __uint_as_float(red.top) * f;
+    if (t == 0) p.scale.data[g * p.scale.group + gr] = max_nan(top / E4M3_MAX, SCALE_MIN);
+    const float inv = min_nan(E4M3_MAX * rcp_approx(top), 1.f / SCALE_MIN);
+    // (f and inv one after the other: their product may be infinite)
+    e4m3* y = row_of<e4m3>(p.y, g, gr);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (t + i * tpr < nvec) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f * inv;
+        store_e4m3<E>(y + (t + i * tpr) * E, v[i]);
+      }
+  } else {
+    T* y = row_of<T>(p.y, g, gr);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (t + i * tpr < nvec) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[i][e] *= f;
+        store_vec<T, E>(y + (t + i * tpr) * E, v[i]);
+      }
+  }
+}
+
 // The norm, or with QUANT only the rows' values to 8 bits.
 template <typename T, int E, int NV, bool QUANT>
 __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs p) {
-  __shared__ float2 s_red[32];
+  __shared__ Sums s_red[32];
   const int sub = threadIdx.x / p.tpr, t = threadIdx.x - sub * p.tpr;
   const int64_t r = (int64_t)blockIdx.x * p.rpb + sub;
   const bool live = r < p.total;
-  const int64_t g = live ? r / p.rows : 0, gr = live ? r - g * p.rows : 0;
+  const int64_t g = live ? group_of(p, r) : 0, gr = live ? r - g * p.rows : 0;
   const int nvec = live ? p.dim / E : 0;
   pdl_wait();
   float v[NV][E];
@@ -69,9 +115,8 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
       for (int e = 0; e < E; ++e) v[i][e] = 0.f;
     }
   }
-  const bool q8 = QUANT || p.scale.data;
   const float* weight = QUANT ? nullptr : p.weight.data + g * p.weight.group;
-  float ss = 0.f, top = 0.f;
+  Sums red{0.f, 0u};
   if (!QUANT) {
     if (p.residual.data) {
       const T* res = row_of<const T>(p.residual, g, gr);
@@ -94,63 +139,215 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
+    if constexpr (!QUANT) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-    if (!QUANT && t + i * p.tpr < nvec) {
-      float w[E];
-      load_params<E>(weight + (t + i * p.tpr) * E, w);
+      for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
+      if (t + i * p.tpr < nvec) {
+        float w[E];
+        load_params<E>(weight + (t + i * p.tpr) * E, w);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[i][e] *= w[e];
+        for (int e = 0; e < E; ++e) v[i][e] *= w[e];
+      }
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
+    for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
   }
-  const float2 red = row_reduce(ss, top, p.tpr, s_red);
-  float f = 1.f;
-  if (!QUANT) {
-    f = 1.f / sqrtf(red.x / (float)p.dim + p.eps);
-    if (live && t == 0 && p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = f;
+  red = warp_reduce<!QUANT, true>(red);
+  if (p.tpr > 32) {
+    if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = red;
+    __syncthreads();
+    red = join<!QUANT, true>(s_red, sub * (p.tpr >> 5), p.tpr >> 5);
   }
-  if (q8) {
-    const float scale = max_nan(red.y * f / E4M3_MAX, SCALE_MIN);
-    if (live && t == 0) p.scale.data[g * p.scale.group + gr] = scale;
-    const float inv = 1.f / scale;  // (two factors: their product may be infinite)
-    e4m3* y = row_of<e4m3>(p.y, g, gr);
+  if (live) row_results<T, E, NV, QUANT>(p, g, gr, red, v, t, p.tpr, nvec);
+}
+
+// ---- many rows: a block of one row's threads walks over rows that arrive in a ring of shared-memory
+// stages by bulk copies, so that loads stay in flight while rows are summed and written. Whole 16-byte
+// units are copied, from the one that holds a row's first byte to the one that holds its last.
+constexpr int RING_MAX = 8, RING_BARS = 128;  // stages; bytes before the first
+
+struct Ring {
+  uint32_t bars, data;
+  int stages, slot, arrays;  // slot: bytes of one array's row in a stage
+  volatile int* abort_flag;
+  int* code;
+};
+
+__device__ __forceinline__ Ring ring_init(uint8_t* smem, int stages, int slot, int arrays) {
+  Ring q;
+  q.bars = tc::smem_u32(smem);
+  q.data = q.bars + RING_BARS;
+  q.stages = stages, q.slot = slot, q.arrays = arrays;
+  q.abort_flag = reinterpret_cast<volatile int*>(smem + 8 * RING_MAX);
+  q.code = reinterpret_cast<int*>(smem + 8 * RING_MAX + 4);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) tc::mbar_init(q.bars + 8 * s, 1);
+    *q.abort_flag = 0;
+    *q.code = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+  return q;
+}
+// One thread: the rows at `src` (n of them used) into a stage.
+__device__ __forceinline__ void ring_load(const Ring& q, int stage, const char* const* src, int bytes) {
+  uint32_t size[3], total = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (t + i * p.tpr < nvec) {
+  for (int i = 0; i < 3; ++i)
+    if (i < q.arrays) {
+      const uint64_t a = (uint64_t)src[i];
+      size[i] = (uint32_t)(((a + bytes + 15) & ~15ull) - (a & ~15ull));
+      total += size[i];
+    }
+  const uint32_t bar = q.bars + 8 * stage;
+  tc::mbar_expect_tx(bar, total);
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f * inv;
-        store_e4m3<E>(y + (t + i * p.tpr) * E, v[i]);
+  for (int i = 0; i < 3; ++i)
+    if (i < q.arrays)
+      asm volatile(
+          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+              q.data + (stage * q.arrays + i) * q.slot),
+          "l"((uint64_t)src[i] & ~15ull), "r"(size[i]), "r"(bar)
+          : "memory");
+}
+// A wait that expires leaves what is in the stage as it is; the block runs on without waiting and reports.
+__device__ __forceinline__ void ring_wait(const Ring& q, int stage, uint32_t parity) {
+  if (!*q.abort_flag) tc::mbar_wait(q.bars + 8 * stage, parity, q.abort_flag, q.code, 1);
+}
+// Where the row of array i begins in a stage.
+__device__ __forceinline__ const char* ring_row(const uint8_t* smem, const Ring& q, int stage, int i,
+                                                const void* src) {
+  return reinterpret_cast<const char*>(smem) + RING_BARS + (stage * q.arrays + i) * q.slot +
+         ((uint64_t)src & 15);
+}
+__device__ __forceinline__ void ring_done(const Ring& q, int* err) {
+  __syncthreads();
+  if (*q.abort_flag) {  // copies in flight land before the block leaves
+    const unsigned long long t0 = tc::globaltimer();
+    while (tc::globaltimer() - t0 < 200000ull) {
+    }
+    if (threadIdx.x == 0 && err) *reinterpret_cast<volatile int*>(err) = *q.code;
+  }
+}
+
+// The block's sums, with one barrier; s: [2][16], by turns.
+template <bool SUM, bool MAX>
+__device__ __forceinline__ Sums block_reduce(Sums v, Sums* s) {
+  v = warp_reduce<SUM, MAX>(v);
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (warps == 1) {
+    __syncwarp();
+    return v;
+  }
+  if ((threadIdx.x & 31) == 0) s[warp] = v;
+  __syncthreads();
+  return join<SUM, MAX>(s, 0, warps);
+}
+
+template <typename T, int E, int NV, bool QUANT>
+__global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages, int slot, int* err) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Sums s_red[2][16];
+  const bool has_res = !QUANT && p.residual.data;
+  const Ring q = ring_init(smem, stages, slot, has_res ? 2 : 1);
+  const int t = threadIdx.x, tpr = blockDim.x, nvec = p.dim / E, bytes = p.dim * (int)sizeof(T);
+  pdl_wait();
+  auto load = [&](int64_t r, int stage) {
+    const int64_t g = group_of(p, r), gr = r - g * p.rows;
+    const char* src[3] = {(const char*)row_of<const T>(p.x, g, gr),
+                          has_res ? (const char*)row_of<const T>(p.residual, g, gr) : nullptr, nullptr};
+    ring_load(q, stage, src, bytes);
+  };
+  if (t == 0)
+    for (int s = 0; s < stages; ++s) {
+      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
+      if (r < p.total) load(r, s);
+    }
+  int stage = 0;
+  uint32_t turn = 0;
+  for (int64_t r = blockIdx.x; r < p.total; r += gridDim.x) {
+    const int64_t g = group_of(p, r), gr = r - g * p.rows;
+    const float* weight = QUANT ? nullptr : p.weight.data + g * p.weight.group;
+    const T* gx = row_of<const T>(p.x, g, gr);
+    const T* x = reinterpret_cast<const T*>(ring_row(smem, q, stage, 0, gx));
+    const T* res = has_res ? reinterpret_cast<const T*>(
+                                 ring_row(smem, q, stage, 1, row_of<const T>(p.residual, g, gr)))
+                           : nullptr;
+    ring_wait(q, stage, turn & 1);
+    float v[NV][E];
+    Sums red{0.f, 0u};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + i * tpr;
+      if (c < nvec) {
+        load_vec<T, E>(x + c * E, v[i]);
+        if (has_res) {
+          float w[E];
+          load_vec<T, E>(res + c * E, w);
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[i][e] += w[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[i][e] = 0.f;
       }
-  } else {
-    T* y = row_of<T>(p.y, g, gr);
+    }
+    if (!QUANT && p.sum.data) {
+      T* s = row_of<T>(p.sum, g, gr);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (t + i * p.tpr < nvec) {
+      for (int i = 0; i < NV; ++i)
+        if (t + i * tpr < nvec) store_vec<T, E>(s + (t + i * tpr) * E, v[i]);
+    }
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] *= f;
-        store_vec<T, E>(y + (t + i * p.tpr) * E, v[i]);
+    for (int i = 0; i < NV; ++i) {
+      if constexpr (!QUANT) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
+        if (t + i * tpr < nvec) {
+          float w[E];
+          load_params<E>(weight + (t + i * tpr) * E, w);
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[i][e] *= w[e];
+        }
       }
+#pragma unroll
+      for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+    }
+    red = block_reduce<!QUANT, true>(red, s_red[turn >> 1 & 1]);
+    // (the row is in registers everywhere: its stage takes the row that comes `stages` later)
+    if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
+    row_results<T, E, NV, QUANT>(p, g, gr, red, v, t, tpr, nvec);
+    turn ^= 2;
+    if (++stage == stages) {
+      stage = 0;
+      turn ^= 1;
+    }
   }
+  ring_done(q, err);
 }
 
 // Rows too long for the registers of 1024 threads are read twice, one block per row.
 template <typename T, int E>
 __global__ void __launch_bounds__(1024) k_quantize_long(const RowArgs p, int64_t dim) {
-  __shared__ float2 s_red[32];
-  const int64_t r = blockIdx.x, g = r / p.rows, gr = r - g * p.rows;
+  __shared__ Sums s_red[32];
+  const int64_t r = blockIdx.x, g = group_of(p, r), gr = r - g * p.rows;
   const T* x = row_of<const T>(p.x, g, gr);
   e4m3* y = row_of<e4m3>(p.y, g, gr);
   pdl_wait();
-  float top = 0.f, v[E];
+  Sums red{0.f, 0u};
+  float v[E];
 #pragma unroll 4
   for (int64_t c = threadIdx.x; c < dim / E; c += 1024) {
     load_vec<T, E>(x + c * E, v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[e]));
+    for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[e]));
   }
-  const float scale = max_nan(row_reduce(0.f, top, 1024, s_red).y / E4M3_MAX, SCALE_MIN);
+  red = warp_reduce<false, true>(red);
+  if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = red;
+  __syncthreads();
+  red = join<false, true>(s_red, 0, 32);
+  const float scale = max_nan(__uint_as_float(red.top) / E4M3_MAX, SCALE_MIN);
   if (threadIdx.x == 0) p.scale.data[g * p.scale.group + gr] = scale;
   const float f = 1.f / scale;
 #pragma unroll 4
@@ -167,101 +364,105 @@ struct BackArgs {
   lipz_vec weight, rstd, dweight;
   float* part;  // [groups][gridDim.x][dim], or null: the block's sums are the group's
   int64_t rows;
-  int dim, tpr, rpb;
+  int dim;
+  float inv_dim;
 };
 
-// A block walks over rows of one group (blockIdx.y); its sums for dweight stay in registers, then those
-// of its row threads are added in shared memory.
+// A block of one row's threads walks over rows of one group (blockIdx.y), which arrive in a ring; its sums
+// for dweight stay in registers.
 template <typename T, int E, int NV>
-__global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p) {
-  extern __shared__ float s_dw[];  // [rpb][dim] where rpb > 1
-  __shared__ float2 s_red[32];
-  const int sub = threadIdx.x / p.tpr, t = threadIdx.x - sub * p.tpr;
+__global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p, int stages, int slot, int* err) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Sums s_red[2][16];
+  const bool has_dsum = p.dsum.data;
+  const Ring q = ring_init(smem, stages, slot, has_dsum ? 3 : 2);
   const int64_t g = blockIdx.y;
-  const int nvec = p.dim / E;
+  const int t = threadIdx.x, tpr = blockDim.x, nvec = p.dim / E, bytes = p.dim * (int)sizeof(T);
   pdl_wait();
+  auto load = [&](int64_t r, int stage) {
+    const char* src[3] = {(const char*)row_of<const T>(p.dy, g, r), (const char*)row_of<const T>(p.s, g, r),
+                          has_dsum ? (const char*)row_of<const T>(p.dsum, g, r) : nullptr};
+    ring_load(q, stage, src, bytes);
+  };
+  if (t == 0)
+    for (int s = 0; s < stages; ++s) {
+      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
+      if (r < p.rows) load(r, s);
+    }
   const float* weight = p.weight.data + g * p.weight.group;
   float dw[NV][E];
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < E; ++e) dw[i][e] = 0.f;
-  for (int64_t r0 = (int64_t)blockIdx.x * p.rpb; r0 < p.rows; r0 += (int64_t)gridDim.x * p.rpb) {
-    const int64_t r = r0 + sub;
-    const bool live = r < p.rows;
-    Raw<T, E> dy[NV], s[NV];
-    const float rstd = live ? p.rstd.data[g * p.rstd.group + r] : 0.f;
+  int stage = 0;
+  uint32_t turn = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+    const float rstd = p.rstd.data[g * p.rstd.group + r];
+    const T* sdy = reinterpret_cast<const T*>(ring_row(smem, q, stage, 0, row_of<const T>(p.dy, g, r)));
+    const T* ss = reinterpret_cast<const T*>(ring_row(smem, q, stage, 1, row_of<const T>(p.s, g, r)));
+    const T* sds = has_dsum ? reinterpret_cast<const T*>(
+                                  ring_row(smem, q, stage, 2, row_of<const T>(p.dsum, g, r)))
+                            : nullptr;
+    ring_wait(q, stage, turn & 1);
+    Raw<T, E> dy[NV], s[NV], ds[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = t + i * p.tpr;
-      if (live && c < nvec) {
-        dy[i].load(row_of<const T>(p.dy, g, r) + c * E);
-        s[i].load(row_of<const T>(p.s, g, r) + c * E);
-      } else {
-        dy[i].zero();
-        s[i].zero();
+      const int c = t + i * tpr;
+      dy[i].zero(), s[i].zero(), ds[i].zero();
+      if (c < nvec) {
+        dy[i].load(sdy + c * E);
+        s[i].load(ss + c * E);
+        if (has_dsum) ds[i].load(sds + c * E);
       }
     }
     float along = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = t + i * p.tpr;
+      const int c = t + i * tpr;
       if (c < nvec) {
         float w[E];
         load_params<E>(weight + c * E, w);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float ds = dy[i].get(e) * s[i].get(e);
-          dw[i][e] = fmaf(ds, rstd, dw[i][e]);
-          along = fmaf(ds, w[e], along);
+          const float m = dy[i].get(e) * s[i].get(e);
+          dw[i][e] = fmaf(m, rstd, dw[i][e]);
+          along = fmaf(m, w[e], along);
         }
       }
     }
-    along = row_reduce(along, 0.f, p.tpr, s_red).x;
-    const float c2 = rstd * rstd * (along / (float)p.dim);
-    if (live) {
-      T* dx = row_of<T>(p.dx, g, r);
+    along = block_reduce<true, false>(Sums{along, 0u}, s_red[turn >> 1 & 1]).ss;
+    if (t == 0 && r + (int64_t)stages * gridDim.x < p.rows) load(r + (int64_t)stages * gridDim.x, stage);
+    const float c2 = rstd * rstd * (along * p.inv_dim);
+    T* dx = row_of<T>(p.dx, g, r);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = t + i * p.tpr;
-        if (c < nvec) {
-          float v[E], w[E];
-          load_params<E>(weight + c * E, w);
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + i * tpr;
+      if (c < nvec) {
+        float v[E], w[E];
+        load_params<E>(weight + c * E, w);
 #pragma unroll
-          for (int e = 0; e < E; ++e) v[e] = rstd * fmaf(-s[i].get(e), c2, dy[i].get(e) * w[e]);
-          if (p.dsum.data) {
-            float d[E];
-            load_vec<T, E>(row_of<const T>(p.dsum, g, r) + c * E, d);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] += d[e];
-          }
-          store_vec<T, E>(dx + c * E, v);
-        }
+        for (int e = 0; e < E; ++e)
+          v[e] = fmaf(rstd, fmaf(-s[i].get(e), c2, dy[i].get(e) * w[e]), ds[i].get(e));
+        store_vec<T, E>(dx + c * E, v);
       }
+    }
+    turn ^= 2;
+    if (++stage == stages) {
+      stage = 0;
+      turn ^= 1;
     }
   }
-  if (!p.dweight.data) return;
-  float* out = p.part ? p.part + (g * gridDim.x + blockIdx.x) * (int64_t)p.dim
-                      : p.dweight.data + g * p.dweight.group;
-  if (p.rpb == 1) {
+  if (p.dweight.data) {
+    float* out = p.part ? p.part + (g * gridDim.x + blockIdx.x) * (int64_t)p.dim
+                        : p.dweight.data + g * p.dweight.group;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      if (t + i * p.tpr < nvec)
+      if (t + i * tpr < nvec)
 #pragma unroll
-        for (int e = 0; e < E; ++e) out[(t + i * p.tpr) * E + e] = dw[i][e];
-    return;
+        for (int e = 0; e < E; ++e) out[(t + i * tpr) * E + e] = dw[i][e];
   }
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (t + i * p.tpr < nvec)
-#pragma unroll
-      for (int e = 0; e < E; ++e) s_dw[sub * p.dim + (t + i * p.tpr) * E + e] = dw[i][e];
-  __syncthreads();
-  for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
-    float v = 0.f;
-    for (int q = 0; q < p.rpb; ++q) v += s_dw[q * p.dim + c];
-    out[c] = v;
-  }
+  ring_done(q, err);
 }
 
 // 32 columns by 32 parts per block: each thread adds every 32nd part, then the 32 sums are added.
@@ -286,32 +487,69 @@ __global__ void __launch_bounds__(1024)
   if (tx == 0 && co < cols) out.data[g * out.group + co] = v;
 }
 
-// Threads per row and vectors per thread: 32 elements per thread reach LIPZ_NORM_MAX_DIM with 512
-// threads.
-struct RowShape {
-  int tpr, nv;
-};
 int row_threads(int nvec, int nv) { return (int)(ceil_div(ceil_div(nvec, nv), 32) * 32); }
-// Few rows: as many threads as vectors (of 4 single elements), so that a row takes one load latency;
-// else two vectors per thread, and more where 512 threads of two do not reach the row's end.
-template <int E>
-RowShape row_shape(int64_t total, int nvec) {
-  constexpr int few = E == 1 ? 4 : 1, mid = E == 1 ? 8 : 2;
-  if (total <= 2 * sm_count() && row_threads(nvec, few) <= 1024) return {row_threads(nvec, few), few};
-  if (row_threads(nvec, mid) <= 512) return {row_threads(nvec, mid), mid};
-  return {row_threads(nvec, 32 / E), 32 / E};
+
+// A streaming kernel's block: 16 elements per thread, 32 where 512 threads of 16 do not reach the row's
+// end (at LIPZ_NORM_MAX_DIM they do), and as many blocks per SM as its registers allow (`threads` of 16
+// elements, half of them of 32) and as leave each two stages or more. Measured, 2048 threads and two
+// stages against 1024 and three: norm of 16384 x 8192 with residual to 8 bits 153 and 162 us, backward of
+// 16384 x 8192 163 and 210 us, quantiser of 16384 x 8192 77 and 82 us.
+struct StreamShape {
+  bool wide;
+  int tpr, per_sm, stages, slot, smem;
+};
+StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads) {
+  StreamShape s;
+  const int nvec = dim / e;
+  s.wide = row_threads(nvec, 16 / e) > 512;
+  s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
+  s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;
+  const int budget = 216 * 1024, row = s.slot * arrays;
+  if (s.wide) threads /= 2;
+  s.per_sm = threads / s.tpr < 24 ? threads / s.tpr : 24;
+  if (s.per_sm < 1) s.per_sm = 1;
+  auto stages = [&] { return (budget / s.per_sm - 1024 - RING_BARS) / row; };
+  while (s.per_sm > 1 && stages() < 2) --s.per_sm;
+  s.stages = stages() > RING_MAX ? RING_MAX : stages();
+  s.smem = RING_BARS + s.stages * row;
+  return s;
+}
+
+template <typename K>
+cudaError_t allow_smem(K kernel, int smem) {
+  return smem <= 48 * 1024
+             ? cudaSuccess
+             : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+}
+
+// From this many rows per SM on, rows stream through rings; fewer are loaded by the threads that use them.
+constexpr int STREAM_ROWS = 4;
+
+template <typename T, int E, int NV, bool QUANT>
+cudaError_t launch_stream(const RowArgs& p, const StreamShape& s, cudaStream_t st) {
+  auto kernel = k_rows_stream<T, E, NV, QUANT>;
+  const cudaError_t e = allow_smem(kernel, s.smem);
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = (int64_t)s.per_sm * sm_count();
+  return launch_pdl(kernel, dim3((unsigned)(blocks < p.total ? blocks : p.total)), dim3(s.tpr), s.smem,
+                    st, p, s.stages, s.slot, timeout_word());
 }
 
 template <typename T, int E, bool QUANT>
 cudaError_t launch_rows(RowArgs& p, cudaStream_t st) {
-  constexpr int few = E == 1 ? 4 : 1, mid = E == 1 ? 8 : 2;
-  const RowShape s = row_shape<E>(p.total, p.dim / E);
-  p.tpr = s.tpr;
-  p.rpb = s.tpr >= 256 ? 1 : 256 / s.tpr;
+  if (p.total > STREAM_ROWS * sm_count()) {
+    const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 2048);
+    return s.wide ? launch_stream<T, E, 32 / E, QUANT>(p, s, st)
+                  : launch_stream<T, E, 16 / E, QUANT>(p, s, st);
+  }
+  // as many threads as vectors (of 4 single elements), so that a row takes one load latency
+  constexpr int few = E == 1 ? 4 : 1;
+  const int nvec = p.dim / E, nv = row_threads(nvec, few) <= 1024 ? few : 32 / E;
+  p.tpr = row_threads(nvec, nv);
+  p.rpb = p.tpr >= 256 ? 1 : 256 / p.tpr;
   const dim3 grid((unsigned)ceil_div(p.total, p.rpb)), block(p.tpr * p.rpb);
-  if (s.nv == few) return launch_pdl(k_rows<T, E, few, QUANT>, grid, block, 0, st, p);
-  if (s.nv == mid) return launch_pdl(k_rows<T, E, mid, QUANT>, grid, block, 0, st, p);
-  return launch_pdl(k_rows<T, E, 32 / E, QUANT>, grid, block, 0, st, p);
+  return nv == few ? launch_pdl(k_rows<T, E, few, QUANT>, grid, block, 0, st, p)
+                   : launch_pdl(k_rows<T, E, 32 / E, QUANT>, grid, block, 0, st, p);
 }
 
 // Vector elements of a backward call: 16 bytes where every row allows it.
@@ -322,50 +560,28 @@ bool backward_vec(const lipz_rmsnorm_backward_args& a) {
          rows_aligned(a.weight, a.groups, 16);
 }
 
-struct BackShape {
-  RowShape s;
-  int rpb, blocks;
-};
-BackShape backward_shape(const lipz_rmsnorm_backward_args& a) {
-  const int e = backward_vec(a) ? 16 / type_bytes(a.dy.type) : 1;
-  const int nvec = (int)(a.dim / e);
-  const int mid = e == 1 ? 8 : 2;
-  BackShape b;
-  b.s = row_threads(nvec, mid) <= 256 ? RowShape{row_threads(nvec, mid), mid}
-                                      : RowShape{row_threads(nvec, 32 / e), 32 / e};
-  b.rpb = b.s.tpr >= 256 ? 1 : 256 / b.s.tpr;
-  while (b.rpb > 1 && (int64_t)b.rpb * a.dim * 4 > 48 * 1024) --b.rpb;
-  const int64_t fill = 4 * sm_count() * 256 / (b.s.tpr * b.rpb > 256 ? b.s.tpr * b.rpb : 256);
-  const int64_t want = fill / (a.groups > 0 ? a.groups : 1);
-  const int64_t most = ceil_div(a.rows, b.rpb);
-  b.blocks = (int)(want < 1 ? 1 : want > most ? most : want);
-  if (b.blocks < 1) b.blocks = 1;
-  return b;
+StreamShape backward_shape(const lipz_rmsnorm_backward_args& a) {
+  const int eb = type_bytes(a.dy.type);
+  return stream_shape((int)a.dim, backward_vec(a) ? 16 / eb : 1, eb, a.dsum.data ? 3 : 2, 1024);
 }
 
-template <typename T, int E, int NV>
-cudaError_t launch_back(const BackArgs& p, int64_t groups, int blocks, cudaStream_t st) {
-  return launch_pdl(k_rmsnorm_backward<T, E, NV>, dim3(blocks, (unsigned)groups),
-                    dim3(p.tpr * p.rpb), p.rpb > 1 ? (size_t)p.rpb * p.dim * 4 : 0, st, p);
-}
-
-template <typename T>
-cudaError_t back_type(const BackArgs& p, bool vec, int nv, int64_t groups, int blocks,
-                      cudaStream_t st) {
-  constexpr int E = 16 / sizeof(T);
-  if (vec) {
-    if (nv == 2) return launch_back<T, E, 2>(p, groups, blocks, st);
-    return launch_back<T, E, 32 / E>(p, groups, blocks, st);
-  }
-  if (nv == 8) return launch_back<T, 1, 8>(p, groups, blocks, st);
-  return launch_back<T, 1, 32>(p, groups, blocks, st);
+template <typename T, int E>
+cudaError_t launch_back(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
+                        cudaStream_t st) {
+  auto go = [&](auto kernel) {
+    const cudaError_t e = allow_smem(kernel, s.smem);
+    return e != cudaSuccess ? e
+                            : launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(s.tpr), s.smem, st,
+                                         p, s.stages, s.slot, timeout_word());
+  };
+  return s.wide ? go(k_rmsnorm_backward<T, E, 32 / E>) : go(k_rmsnorm_backward<T, E, 16 / E>);
 }
 
 }  // namespace
 
 cudaError_t rmsnorm(const lipz_rmsnorm_args& a, cudaStream_t st) {
   RowArgs p{a.x, a.residual, a.sum, a.y, a.weight, a.scale, a.rstd, a.rows, a.groups * a.rows,
-            (int)a.dim, 0, 0, a.eps};
+            (int)a.dim, 0, 0, a.eps, 1.f / (float)a.dim};
   if (a.y.type != LIPZ_E4M3) p.scale.data = nullptr;
   if (p.total == 0) return cudaSuccess;
   const int e = 16 / type_bytes(a.x.type);
@@ -411,19 +627,30 @@ cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols
                     st, part, parts, cols, out);
 }
 
-int rmsnorm_backward_blocks(const lipz_rmsnorm_backward_args& a) { return backward_shape(a).blocks; }
+// Every block's sums are written and read once more: four rows or more per block.
+int rmsnorm_backward_blocks(const lipz_rmsnorm_backward_args& a) {
+  const int64_t fill = (int64_t)backward_shape(a).per_sm * sm_count() / (a.groups > 0 ? a.groups : 1);
+  const int64_t most = ceil_div(a.rows, 4), b = fill < most ? fill : most;
+  return b < 1 ? 1 : (int)b;
+}
 
 cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t st) {
   if (a.groups == 0) return cudaSuccess;
-  const BackShape b = backward_shape(a);
-  BackArgs p{a.dy, a.s, a.dsum, a.dx, a.weight, a.rstd, a.dweight, nullptr, a.rows, (int)a.dim,
-             b.s.tpr, b.rpb};
-  if (b.blocks > 1) p.part = (float*)a.workspace;
+  const StreamShape s = backward_shape(a);
+  const int blocks = rmsnorm_backward_blocks(a);
+  const BackArgs p{a.dy, a.s, a.dsum, a.dx, a.weight, a.rstd, a.dweight,
+                   blocks > 1 ? (float*)a.workspace : nullptr, a.rows, (int)a.dim,
+                   1.f / (float)a.dim};
   const bool vec = backward_vec(a);
-  cudaError_t e = a.dy.type == LIPZ_FP32 ? back_type<float>(p, vec, b.s.nv, a.groups, b.blocks, st)
-                                         : back_type<bf16>(p, vec, b.s.nv, a.groups, b.blocks, st);
-  if (e != cudaSuccess || b.blocks == 1 || !a.dweight.data) return e;
-  return sum_parts(p.part, a.groups, b.blocks, a.dim, a.dweight, st);
+  cudaError_t e;
+  if (a.dy.type == LIPZ_FP32)
+    e = vec ? launch_back<float, 4>(p, s, a.groups, blocks, st)
+            : launch_back<float, 1>(p, s, a.groups, blocks, st);
+  else
+    e = vec ? launch_back<bf16, 8>(p, s, a.groups, blocks, st)
+            : launch_back<bf16, 1>(p, s, a.groups, blocks, st);
+  if (e != cudaSuccess || blocks == 1 || !a.dweight.data) return e;
+  return sum_parts(p.part, a.groups, blocks, a.dim, a.dweight, st);
 }
 
 }  // namespace ops

@@ -56,20 +56,23 @@ __attribute__((format(printf, 2, 3))) int fail(int code, const char* fmt, ...) {
   return code;
 }
 
+// Set once a kernel may have been launched that stores to the timeout word.
+std::atomic<bool> g_word_in_use{false};
+
 int finish(const char* call, cudaError_t e) {
+  g_word_in_use.store(true, std::memory_order_relaxed);
   if (e == cudaSuccess) return LIPZ_OK;
   cudaGetLastError();
   return fail(LIPZ_ERR_CUDA, "%s: %s", call, cudaGetErrorString(e));
 }
 
-// Whether a kernel gave up on a wait since the last report (products take the word before they launch).
-std::atomic<bool> g_word_in_use{false};
+// Whether a kernel gave up on a wait since the last report.
 int take_timeout(const char* call) {
   if (!g_word_in_use.load()) return LIPZ_OK;
   int* word = ops::timeout_word();
   const int code = word ? __atomic_exchange_n(word, 0, __ATOMIC_ACQ_REL) : 0;
   if (!code) return LIPZ_OK;
-  return fail(LIPZ_ERR_TIMEOUT, "%s: an earlier product gave up on a wait (%d): its results are not valid",
+  return fail(LIPZ_ERR_TIMEOUT, "%s: an earlier call's kernel gave up on a wait (%d): its results are not valid",
               call, code);
 }
 
@@ -273,7 +276,6 @@ int lipz_linear(const lipz_linear_args* a, void* stream) {
   Check c{"lipz_linear", a->groups, a->rows};
   if (!c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a))) return c.rc;
   if (int rc = take_timeout(c.call)) return rc;
-  g_word_in_use.store(true);
   return finish(c.call, ops::linear(*a, (cudaStream_t)stream));
 }
 
@@ -289,7 +291,6 @@ int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream) {
   Check c{"lipz_linear_backward", a->groups, a->rows};
   if (!c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a))) return c.rc;
   if (int rc = take_timeout(c.call)) return rc;
-  g_word_in_use.store(true);
   return finish(c.call, ops::linear_backward(*a, (cudaStream_t)stream));
 }
 

@@ -11,15 +11,14 @@ CUDA graph. What the library does not take raises ``LipzError`` with nothing lau
 records an autograd graph: the backward passes are calls of their own.
 """
 
+import ctypes
 import struct
 from typing import NamedTuple, Optional
 
 import torch
 
-from . import (LIPZ_BF16, LIPZ_E4M3, LIPZ_ERR_INVALID, LIPZ_FP32, LipzError, lipz_linear,
-               lipz_linear_backward, lipz_linear_backward_workspace, lipz_linear_workspace,
-               lipz_quantize_rows, lipz_rmsnorm, lipz_rmsnorm_backward,
-               lipz_rmsnorm_backward_workspace)
+from . import (LIPZ_BF16, LIPZ_E4M3, LIPZ_ERR_INVALID, LIPZ_FP32, LIPZ_OK, LipzError, load,
+               lipz_operator_error)
 
 __all__ = ["Norm", "rmsnorm", "rmsnorm_backward", "quantize_rows", "linear", "linear_backward",
            "ACTIVATIONS"]
@@ -43,43 +42,50 @@ def _refuse(call, what):
     raise LipzError(LIPZ_ERR_INVALID, "%s: %s" % (call, what))
 
 
-def _mat(call, name, t, shape, dtypes, device):
-    """(address, group stride, row stride, type, 0) of a checked matrix."""
-    if t is None:
-        return _NO_MAT
-    if not isinstance(t, torch.Tensor) or t.device != device or not t.is_cuda:
+def _refuse_tensor(call, name, t, shape, dtypes, device):
+    """Says why a tensor is refused."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
         _refuse(call, "%s must be a CUDA tensor on the same device as the others" % name)
     if t.dtype not in dtypes:
         _refuse(call, "%s has dtype %s, taken are %s" % (name, t.dtype, ", ".join(map(str, dtypes))))
     if t.shape != shape:
         _refuse(call, "%s has shape %s, not %s" % (name, list(t.shape), list(shape)))
-    st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1 and t.numel():
-        _refuse(call, "%s: columns must be adjacent" % name)
-    return t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2], _TYPE[t.dtype], 0
+    _refuse(call, "%s: columns must be adjacent" % name)
+
+
+# (These run for every tensor of every call, next to kernels of a few microseconds.)
+def _mat(call, name, t, shape, dtypes, device):
+    """(address, group stride, row stride, type, 0) of a checked matrix."""
+    if t is None:
+        return _NO_MAT
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == device:
+        st = t.stride()
+        if st[-1] == 1 or shape[-1] <= 1 or not t.numel():
+            return t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2], _TYPE[t.dtype], 0
+    _refuse_tensor(call, name, t, shape, dtypes, device)
 
 
 def _vec(call, name, t, shape, device):
     """(address, group stride) of a checked fp32 vector."""
     if t is None:
         return _NO_VEC
-    if not isinstance(t, torch.Tensor) or t.device != device or not t.is_cuda:
-        _refuse(call, "%s must be a CUDA tensor on the same device as the others" % name)
-    if t.dtype is not _F32 or t.shape != shape:
-        _refuse(call, "%s must be float32 of shape %s, not %s of %s"
-                % (name, list(shape), t.dtype, list(t.shape)))
-    st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1 and t.numel():
-        _refuse(call, "%s: elements must be adjacent" % name)
-    return t.data_ptr(), st[0] if len(st) == 2 else 0
+    if isinstance(t, torch.Tensor) and t.dtype is _F32 and t.shape == shape and t.get_device() == device:
+        st = t.stride()
+        if st[-1] == 1 or shape[-1] <= 1 or not t.numel():
+            return t.data_ptr(), st[0] if len(st) == 2 else 0
+    _refuse_tensor(call, name, t, shape, (_F32,), device)
 
 
 def _first(call, name, t):
-    """(leading dimensions, groups, rows, columns, device) that a call's other tensors go by."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() not in (2, 3):
-        _refuse(call, "%s must be a CUDA tensor [rows, columns] or [groups, rows, columns]" % name)
+    """(shape, groups, rows, columns, device, its index) that a call's other tensors go by."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(call, "%s must be a CUDA tensor" % name)
     s = t.shape
-    return s[:-2], (s[0] if len(s) == 3 else 1), s[-2], s[-1], t.device
+    if len(s) == 2:
+        return s, 1, s[0], s[1], t.device, t.get_device()
+    if len(s) != 3:
+        _refuse(call, "%s must be [rows, columns] or [groups, rows, columns]" % name)
+    return s, s[0], s[1], s[2], t.device, t.get_device()
 
 
 def _act(call, act):
@@ -89,27 +95,35 @@ def _act(call, act):
     return code
 
 
-def _run(f, args, device):
-    """The call on the device's current stream."""
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        return f(args, stream)
-    with torch.cuda.device(device):
-        return f(args, stream)
+# the handle of the device's current stream, without the object around it
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _run_with_space(f, space, pack, fields, device):
-    """The call with the workspace that it asks for."""
-    args = pack(*fields, 0, 0)
-    if device.index == torch.cuda.current_device():
-        need = space(args)
-    else:
+def _run(name, args, device):
+    """The library's call on the device's current stream."""
+    if device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            need = space(args)
-    if need:
-        work = torch.empty(need, dtype=torch.uint8, device=device)
-        args = pack(*fields, work.data_ptr(), need)
-    return _run(f, args, device)
+            return _run(name, args, device)
+    rc = getattr(load(), name)(args, _stream(device))
+    if rc != LIPZ_OK:
+        raise LipzError(rc, lipz_operator_error())
+
+
+def _run_with_space(name, struct_, fields, dev, device):
+    """The call with the workspace that it asks for."""
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _run_with_space(name, struct_, fields, dev, device)
+    need = ctypes.c_uint64()
+    args = struct_.pack(*fields, 0, 0)
+    rc = getattr(load(), name + "_workspace")(args, ctypes.byref(need))
+    if rc != LIPZ_OK:
+        raise LipzError(rc, lipz_operator_error())
+    if need.value:
+        work = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        args = struct_.pack(*fields, work.data_ptr(), need.value)
+    _run(name, args, device)
 
 
 class Norm(NamedTuple):
@@ -128,26 +142,27 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, e4m3=False, keep=False, sum_out=
     residual stream updated in place). y has x's type; with ``e4m3`` it is float8_e4m3fn and
     y scale[row] the values. ``keep``: return rstd, which the backward pass reads."""
     call = "rmsnorm"
-    lead, groups, rows, dim, dev = _first(call, "x", x)
-    shape, dt = x.shape, (x.dtype,)
-    mx = _mat(call, "x", x, shape, (_BF16, _F32), dev)
-    mr = _mat(call, "residual", residual, shape, dt, dev)
-    vw = _vec(call, "weight", weight, lead + (dim,), dev)
+    shape, groups, rows, dim, dev, device = _first(call, "x", x)
+    dt = (x.dtype,)
+    mx = _mat(call, "x", x, shape, (_BF16, _F32), device)
+    vw = _vec(call, "weight", weight, (dim,) if len(shape) == 2 else (groups, dim), device)
+    if weight is None:
+        _refuse(call, "weight must be given")
     if residual is None:
         if sum_out is not None:
             _refuse(call, "sum_out needs a residual")
-        total, ms = x, _NO_MAT
+        total, mr, ms = x, _NO_MAT, _NO_MAT
     else:
+        mr = _mat(call, "residual", residual, shape, dt, device)
         total = torch.empty(shape, dtype=x.dtype, device=dev) if sum_out is None else sum_out
-        ms = _mat(call, "sum_out", total, shape, dt, dev)
+        ms = _mat(call, "sum_out", total, shape, dt, device)
     y = torch.empty(shape, dtype=_E4M3 if e4m3 else x.dtype, device=dev)
-    scale = torch.empty(lead + (rows,), dtype=_F32, device=dev) if e4m3 else None
-    rstd = torch.empty(lead + (rows,), dtype=_F32, device=dev) if keep else None
-    args = _S_RMSNORM.pack(
+    scale = torch.empty(shape[:-1], dtype=_F32, device=dev) if e4m3 else None
+    rstd = torch.empty(shape[:-1], dtype=_F32, device=dev) if keep else None
+    _run("lipz_rmsnorm", _S_RMSNORM.pack(
         _S_RMSNORM.size, eps, groups, rows, dim, *mx, *mr, *ms,
-        y.data_ptr(), rows * dim, dim, LIPZ_E4M3 if e4m3 else _TYPE[x.dtype], 0, *vw,
-        scale.data_ptr() if e4m3 else 0, rows, rstd.data_ptr() if keep else 0, rows)
-    _run(lipz_rmsnorm, args, dev)
+        y.data_ptr(), rows * dim, dim, LIPZ_E4M3 if e4m3 else mx[3], 0, *vw,
+        scale.data_ptr() if e4m3 else 0, rows, rstd.data_ptr() if keep else 0, rows), device)
     return Norm(y, total, scale, rstd)
 
 
@@ -155,20 +170,21 @@ def rmsnorm_backward(dy, s, rstd, weight, dsum=None, want_dweight=True):
     """(dx, dweight) of rmsnorm: from its ``sum`` and ``rstd``, y's gradient, and dsum, the gradient
     that reaches the sum from elsewhere. dx is the gradient of x and of residual; dweight is fp32."""
     call = "rmsnorm_backward"
-    lead, groups, rows, dim, dev = _first(call, "s", s)
-    shape, dt = s.shape, (s.dtype,)
-    mats = (_mat(call, "dy", dy, shape, dt, dev) + _mat(call, "s", s, shape, (_BF16, _F32), dev)
-            + _mat(call, "dsum", dsum, shape, dt, dev))
-    if dy is None:
-        _refuse(call, "dy must be given")
-    vecs = (_vec(call, "weight", weight, lead + (dim,), dev)
-            + _vec(call, "rstd", rstd, lead + (rows,), dev))
+    shape, groups, rows, dim, dev, device = _first(call, "s", s)
+    lead, dt = shape[:-2], (s.dtype,)
+    if dy is None or weight is None or rstd is None:
+        _refuse(call, "dy, rstd and weight must be given")
+    mats = (_mat(call, "dy", dy, shape, dt, device)
+            + _mat(call, "s", s, shape, (_BF16, _F32), device)
+            + _mat(call, "dsum", dsum, shape, dt, device))
+    vecs = (_vec(call, "weight", weight, lead + (dim,), device)
+            + _vec(call, "rstd", rstd, shape[:-1], device))
     dx = torch.empty(shape, dtype=s.dtype, device=dev)
     dweight = torch.empty(lead + (dim,), dtype=_F32, device=dev) if want_dweight else None
-    fields = (_S_RMSNORM_BACKWARD.size, 0, groups, rows, dim, *mats, dx.data_ptr(), rows * dim, dim,
-              _TYPE[s.dtype], 0, *vecs, dweight.data_ptr() if want_dweight else 0, dim)
-    _run_with_space(lipz_rmsnorm_backward, lipz_rmsnorm_backward_workspace, _S_RMSNORM_BACKWARD.pack,
-                    fields, dev)
+    _run_with_space("lipz_rmsnorm_backward", _S_RMSNORM_BACKWARD,
+                    (_S_RMSNORM_BACKWARD.size, 0, groups, rows, dim, *mats, dx.data_ptr(), rows * dim,
+                     dim, _TYPE[s.dtype], 0, *vecs, dweight.data_ptr() if want_dweight else 0, dim),
+                    dev, device)
     return dx, dweight
 
 
@@ -176,13 +192,13 @@ def quantize_rows(x):
     """(q, scale): x [.., rows, columns] (bf16 or fp32) in float8_e4m3fn with an fp32 scale per row,
     q scale the values."""
     call = "quantize_rows"
-    lead, groups, rows, dim, dev = _first(call, "x", x)
-    mx = _mat(call, "x", x, x.shape, (_BF16, _F32), dev)
-    q = torch.empty(x.shape, dtype=_E4M3, device=dev)
-    scale = torch.empty(lead + (rows,), dtype=_F32, device=dev)
-    _run(lipz_quantize_rows,
+    shape, groups, rows, dim, dev, device = _first(call, "x", x)
+    mx = _mat(call, "x", x, shape, (_BF16, _F32), device)
+    q = torch.empty(shape, dtype=_E4M3, device=dev)
+    scale = torch.empty(shape[:-1], dtype=_F32, device=dev)
+    _run("lipz_quantize_rows",
          _S_QUANTIZE.pack(_S_QUANTIZE.size, 0, groups, rows, dim, *mx, q.data_ptr(), rows * dim, dim,
-                          LIPZ_E4M3, 0, scale.data_ptr(), rows), dev)
+                          LIPZ_E4M3, 0, scale.data_ptr(), rows), device)
     return q, scale
 
 
@@ -194,28 +210,30 @@ def linear(x, w, bias=None, act="none", slope=0.2, residual=None, x_scale=None, 
     y: out_dtype (bf16 or fp32). y is written to ``out`` if given (it may be the residual). ``keep``:
     pre is u in bf16, which the backward pass reads (else None)."""
     call = "linear"
-    lead, groups, rows, k, dev = _first(call, "x", x)
-    if not isinstance(w, torch.Tensor) or w.dim() != x.dim():
+    x_shape, groups, rows, k, dev, device = _first(call, "x", x)
+    if not isinstance(w, torch.Tensor) or w.dim() != len(x_shape):
         _refuse(call, "w must be a CUDA tensor with x's number of dimensions")
-    n = w.shape[-2]
-    shape = lead + (rows, n)
-    code = _act(call, act)
-    if out_dtype not in (_BF16, _F32):
+    lead, n = x_shape[:-2], w.shape[-2]
+    shape, row, code = lead + (rows, n), lead + (n,), _act(call, act)
+    mx = _mat(call, "x", x, x_shape, (_BF16, _E4M3), device)
+    mw = _mat(call, "w", w, lead + (n, k), (x.dtype,), device)
+    if out_dtype is not _BF16 and out_dtype is not _F32:
         _refuse(call, "out_dtype must be bfloat16 or float32")
-    mx = _mat(call, "x", x, x.shape, (_BF16, _E4M3), dev)
-    mw = _mat(call, "w", w, lead + (n, k), (x.dtype,), dev)
-    mr = _mat(call, "residual", residual, shape, (out_dtype,), dev)
-    if (x_scale is None) != (x.dtype is not _E4M3) or (w_scale is None) != (x.dtype is not _E4M3):
+    if (x_scale is None) != (mx[3] != LIPZ_E4M3) or (w_scale is None) != (mx[3] != LIPZ_E4M3):
         _refuse(call, "x_scale and w_scale go with 8-bit operands, and with them alone")
-    vecs = (_vec(call, "x_scale", x_scale, lead + (rows,), dev)
-            + _vec(call, "w_scale", w_scale, lead + (n,), dev)
-            + _vec(call, "bias", bias, lead + (n,), dev))
-    y = torch.empty(shape, dtype=out_dtype, device=dev) if out is None else out
-    my = _mat(call, "out", y, shape, (out_dtype,), dev)
+    mr = _mat(call, "residual", residual, shape, (out_dtype,), device)
+    vecs = (_vec(call, "x_scale", x_scale, x_shape[:-1], device)
+            + _vec(call, "w_scale", w_scale, row, device) + _vec(call, "bias", bias, row, device))
+    if out is None:
+        y = torch.empty(shape, dtype=out_dtype, device=dev)
+        my = (y.data_ptr(), rows * n, n, _TYPE[out_dtype], 0)
+    else:
+        y, my = out, _mat(call, "out", out, shape, (out_dtype,), device)
     pre = torch.empty(shape, dtype=_BF16, device=dev) if keep else None
     mp = (pre.data_ptr(), rows * n, n, LIPZ_BF16, 0) if keep else _NO_MAT
-    fields = (_S_LINEAR.size, code, slope, 0, groups, rows, k, n, *mx, *mw, *mr, *my, *mp, *vecs)
-    _run_with_space(lipz_linear, lipz_linear_workspace, _S_LINEAR.pack, fields, dev)
+    _run_with_space("lipz_linear", _S_LINEAR,
+                    (_S_LINEAR.size, code, slope, 0, groups, rows, k, n, *mx, *mw, *mr, *my, *mp, *vecs),
+                    dev, device)
     return y, pre
 
 
@@ -224,28 +242,26 @@ def linear_backward(dy, x, w, act="none", slope=0.2, pre=None, want_dx=True, wan
     """(dx, dw, db) of linear over bf16 operands: du = dy act'(pre), dx = du w, dw = du^T x, db the
     sums of du over the rows; None for what is not wanted. The residual's gradient is dy."""
     call = "linear_backward"
-    lead, groups, rows, n, dev = _first(call, "dy", dy)
-    if not isinstance(x, torch.Tensor) or x.dim() != dy.dim():
+    shape, groups, rows, n, dev, device = _first(call, "dy", dy)
+    if not isinstance(x, torch.Tensor) or x.dim() != len(shape):
         _refuse(call, "x must be a CUDA tensor with dy's number of dimensions")
-    k = x.shape[-1]
-    code = _act(call, act)
-    if code and pre is None:
-        _refuse(call, "act %r needs pre" % act)
-    if dw_dtype not in (_BF16, _F32):
-        _refuse(call, "dw_dtype must be bfloat16 or float32")
-    bf = (_BF16,)
-    mats = (_mat(call, "dy", dy, dy.shape, bf, dev) + _mat(call, "x", x, lead + (rows, k), bf, dev)
-            + _mat(call, "w", w, lead + (n, k), bf, dev)
-            + _mat(call, "pre", pre if code else None, dy.shape, bf, dev))
     if w is None:
         _refuse(call, "w must be given")
+    lead, k, bf, code = shape[:-2], x.shape[-1], (_BF16,), _act(call, act)
+    if code and pre is None:
+        _refuse(call, "act %r needs pre" % act)
+    if dw_dtype is not _BF16 and dw_dtype is not _F32:
+        _refuse(call, "dw_dtype must be bfloat16 or float32")
+    mats = (_mat(call, "dy", dy, shape, bf, device)
+            + _mat(call, "x", x, lead + (rows, k), bf, device)
+            + _mat(call, "w", w, lead + (n, k), bf, device)
+            + _mat(call, "pre", pre if code else None, shape, bf, device))
     dx = torch.empty(lead + (rows, k), dtype=_BF16, device=dev) if want_dx else None
     dw = torch.empty(lead + (n, k), dtype=dw_dtype, device=dev) if want_dw else None
     db = torch.empty(lead + (n,), dtype=_F32, device=dev) if want_db else None
-    fields = (_S_LINEAR_BACKWARD.size, code, slope, 0, groups, rows, k, n, *mats,
-              *((dx.data_ptr(), rows * k, k, LIPZ_BF16, 0) if want_dx else _NO_MAT),
-              *((dw.data_ptr(), n * k, k, _TYPE[dw_dtype], 0) if want_dw else _NO_MAT),
-              db.data_ptr() if want_db else 0, n)
-    _run_with_space(lipz_linear_backward, lipz_linear_backward_workspace, _S_LINEAR_BACKWARD.pack,
-                    fields, dev)
+    mx = (dx.data_ptr(), rows * k, k, LIPZ_BF16, 0) if want_dx else _NO_MAT
+    mw = (dw.data_ptr(), n * k, k, _TYPE[dw_dtype], 0) if want_dw else _NO_MAT
+    _run_with_space("lipz_linear_backward", _S_LINEAR_BACKWARD,
+                    (_S_LINEAR_BACKWARD.size, code, slope, 0, groups, rows, k, n, *mats, *mx, *mw,
+                     db.data_ptr() if want_db else 0, n), dev, device)
     return dx, dw, db
