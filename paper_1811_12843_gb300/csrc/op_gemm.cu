@@ -9,6 +9,9 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <stdlib.h>
+#include <string.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -22,30 +25,46 @@ namespace ops {
 namespace {
 
 constexpr int ROW = 128;                  // bytes of a swizzled row: 64 bf16 or 128 e4m3 of k
-constexpr int EPI_WARPS = 8, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
+constexpr int EPI_WARPS = 16, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 constexpr int TURN = 32 * 17 * 4;         // a warp's block for turning rows into columns
 constexpr int MN_BOX = 64 * ROW;          // 64 k by 64 m (or n) of an operand whose rows run along m (n)
 constexpr int SUM_CHUNKS = 8;             // chunks of k whose sum stands in tensor memory, for fp32 results
-constexpr int SMEM_MAX = 232448;
+constexpr int SMEM_MAX = 232448, STAGES_MAX = 8;
 
 template <int CG, int BN>
 struct Shape {
   static constexpr int A_BYTES = 128 * ROW, B_BYTES = BN / CG * ROW, STAGE = A_BYTES + B_BYTES;
-  static constexpr int EXTRA = 1024 + EPI_WARPS * TURN + 2 * BN * 8 + 256;
-  static constexpr int STAGES = (SMEM_MAX - EXTRA) / STAGE < 8 ? (SMEM_MAX - EXTRA) / STAGE : 8;
-  static constexpr int SMEM = EXTRA + STAGES * STAGE;
+  // after the stages: a tile's column parameters (two tiles'), partial sums' block, barriers
+  static constexpr int COLS = 2 * BN * 8, SUMS = EPI_WARPS * 32 * 4, BARS = 256;
+  static constexpr int smem(int stages, bool turn) {
+    return 1024 + stages * STAGE + COLS + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
+  }
+  static constexpr int stages(bool turn) {
+    int n = STAGES_MAX;
+    while (smem(n, turn) > SMEM_MAX) --n;
+    return n;
+  }
 };
 
-struct GemmParams {
+// One product's part of a launch.
+struct Problem {
   Epilogue e;
   float* part;  // partial sums [splits][groups][m][ldp] instead of results, or null
-  int* err;
   int64_t ldp;
   int groups, m, n, tiles_m, tiles_n, units, splits, chunks, chunks_per_split;
-  int a_bytes;           // of A's box per CTA and stage
-  int az, bz;            // 0: one matrix for every group
+  int a_bytes;               // of A's box per CTA and stage
+  int az, bz;                // 0: one matrix for every group
+  int a_mn, b_mn;            // rows run along m (n) instead of k
   int a_blocked, b_blocked;  // a 4-D map brings the 64-wide boxes of a stage together
   int y_align, res_align, pre_align;  // 32, 16, or 0: bytes that divide every row's start
+};
+template <int NP>
+struct GemmParams {
+  CUtensorMap a[NP], b[NP];
+  Problem p[NP];
+  PartSums sums;
+  int units, stages;
+  int* err;
 };
 
 template <int CG>
@@ -88,7 +107,7 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
 }
 // fp32 accumulators; bf16 (format 1) or e4m3 (format 0) operands
 template <int TYPE>
-__host__ __device__ constexpr uint32_t idesc(int m, int n, bool a_mn, bool b_mn) {
+__device__ __forceinline__ uint32_t idesc(int m, int n, int a_mn, int b_mn) {
   return (1u << 4) | (TYPE == LIPZ_BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)a_mn << 15) |
          ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
@@ -105,16 +124,18 @@ __device__ __forceinline__ void ld_v8(const void* p, uint32_t* r) {
                : "memory");
 }
 
-// 32 elements of this lane's row, from column c of a warp's 32 rows: 32- or 16-byte accesses where the
-// rows' starts allow, else turned in shared memory so that the lanes run along a row. (rows, cols: what
-// there is of the 32.) Words: two bf16, or one fp32.
+// 16 elements of this lane's row, from a column of a warp's 32 rows on: 32- or 16-byte accesses where the
+// rows' starts allow, else turned in shared memory so that the lanes run along a row. rows, cols: what there
+// is of the 32 and the 16.
 template <typename T>
 __device__ __forceinline__ void load_row(const T* base, int64_t ld, int rows, int cols, int align,
-                                         float* turn, float (&v)[32]) {
+                                         float* turn, float* v) {
   const int lane = threadIdx.x & 31;
-  constexpr int W = sizeof(T) * 8;  // words of 32 elements
-  if (align && cols >= 32) {
+  constexpr int W = sizeof(T) * 4;  // words of 16 elements: two bf16, or one fp32
+  if (align && cols >= 16) {
     uint32_t w[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0;
     if (lane < rows) {
       const char* p = reinterpret_cast<const char*>(base + lane * ld);
       if (align == 32) {
@@ -127,35 +148,29 @@ __device__ __forceinline__ void load_row(const T* base, int64_t ld, int rows, in
           w[i] = r.x, w[i + 1] = r.y, w[i + 2] = r.z, w[i + 3] = r.w;
         }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < W; ++i) w[i] = 0;
     }
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
+    for (int e = 0; e < 16; ++e) {
       if constexpr (sizeof(T) == 4) v[e] = __uint_as_float(w[e]);
       else v[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
     }
     return;
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = h * 16 + (lane & 15);
-    __syncwarp();
+  const int col = lane & 15;
+  __syncwarp();
 #pragma unroll 8
-    for (int r = lane >> 4; r < 32; r += 2)
-      turn[r * 17 + (lane & 15)] = r < rows && col < cols ? to_f<T>(base[r * ld + col]) : 0.f;
-    __syncwarp();
+  for (int r = lane >> 4; r < 32; r += 2)
+    turn[r * 17 + col] = r < rows && col < cols ? to_f<T>(base[r * ld + col]) : 0.f;
+  __syncwarp();
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[h * 16 + e] = turn[lane * 17 + e];
-  }
+  for (int e = 0; e < 16; ++e) v[e] = turn[lane * 17 + e];
 }
 template <typename T>
 __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int cols, int align,
-                                          float* turn, const float (&v)[32]) {
+                                          float* turn, const float* v) {
   const int lane = threadIdx.x & 31;
-  constexpr int W = sizeof(T) * 8;
-  if (align && cols >= 32) {
+  constexpr int W = sizeof(T) * 4;
+  if (align && cols >= 16) {
     if (lane >= rows) return;
     uint32_t w[W];
 #pragma unroll
@@ -176,18 +191,17 @@ __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int col
     }
     return;
   }
+  const int col = lane & 15;
+  __syncwarp();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int col = h * 16 + (lane & 15);
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < 16; ++e) turn[lane * 17 + e] = v[h * 16 + e];
-    __syncwarp();
+  for (int e = 0; e < 16; ++e) turn[lane * 17 + e] = v[e];
+  __syncwarp();
 #pragma unroll 8
-    for (int r = lane >> 4; r < 32; r += 2)
-      if (r < rows && col < cols) base[r * ld + col] = from_f<T>(turn[r * 17 + (lane & 15)]);
-  }
+  for (int r = lane >> 4; r < 32; r += 2)
+    if (r < rows && col < cols) base[r * ld + col] = from_f<T>(turn[r * 17 + col]);
 }
+
+__device__ __forceinline__ int64_t ceil_div_d(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // A tile's place: groups outermost, then panels of 8 tile rows, along which neighbouring CTAs share
 // operands in L2.
@@ -201,34 +215,36 @@ __device__ __forceinline__ Place place(int t, int tiles_m, int tiles_n) {
   return {g, first + q % w, q / w};
 }
 
-// T: the results' type; fp32 results (SUMS) are sums, in fp32 registers, of sums over SUM_CHUNKS chunks,
-// because the tensor cores' additions truncate. FORWARD: K-major operands and the forward's epilogue, else
-// a plain product.
-template <int TYPE, int CG, int BN, bool AMN, bool BMN, typename T>
+// T: the results' type; fp32 results are sums, in fp32 registers, of sums over SUM_CHUNKS chunks of k,
+// because the tensor cores' additions truncate. FORWARD: K-major operands and the forward's epilogue, one
+// product; else up to two plain products.
+template <int TYPE, int CG, int BN, bool FORWARD, typename T>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_gemm_op(const __grid_constant__ CUtensorMap mA, const __grid_constant__ CUtensorMap mB,
-              const __grid_constant__ GemmParams p) {
+    k_gemm_op(const __grid_constant__ GemmParams<FORWARD ? 1 : 2> prm) {
   using S = Shape<CG, BN>;
-  constexpr int STAGES = S::STAGES, BM = 128 * CG, HALF = BN / 2;
-  constexpr bool SUMS = sizeof(T) == 4, FORWARD = !AMN && !BMN;
+  constexpr bool SUMS = sizeof(T) == 4;
+  constexpr int BM = 128 * CG, QUART = BN / 4;      // columns of a result warp
+  constexpr int CW = QUART < 32 ? QUART : 32;       // columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
   extern __shared__ uint8_t smem_raw[];
+  const int stages = prm.stages;
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* after = smem_raw + (base - raw) + STAGES * S::STAGE;
-  float* s_turn = reinterpret_cast<float*>(after);
-  float2* s_col = reinterpret_cast<float2*>(after + EPI_WARPS * TURN);  // [2][BN] {w_scale, bias}
-  uint64_t* bars = reinterpret_cast<uint64_t*>(after + EPI_WARPS * TURN + 2 * BN * 8);
-  const uint32_t bFull = tc::smem_u32(bars), bEmpty = bFull + 8 * STAGES;
-  const uint32_t bAcc = bEmpty + 8 * STAGES, bFree = bAcc + 16;
+  uint8_t* after = smem_raw + (base - raw) + stages * S::STAGE;
+  float2* s_col = reinterpret_cast<float2*>(after);  // [2][BN] {w_scale, bias}
+  float* s_sum = reinterpret_cast<float*>(after + S::COLS);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(after + S::COLS + S::SUMS);
+  float* s_turn = reinterpret_cast<float*>(after + S::COLS + S::SUMS + S::BARS);
+  const uint32_t bFull = tc::smem_u32(bars), bEmpty = bFull + 8 * STAGES_MAX;
+  const uint32_t bAcc = bEmpty + 8 * STAGES_MAX, bFree = bAcc + 16;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + 24);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 25);
   int* code = reinterpret_cast<int*>(bars + 26);
-  static_assert(2 * STAGES + 4 <= 24, "barriers");
+  static_assert(2 * STAGES_MAX + 4 <= 24, "barriers");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? tc::cluster_ctarank() : 0;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < stages; ++s) {
       tc::mbar_init(bFull + 8 * s, 2);  // A's and B's issuers
       tc::mbar_init(bEmpty + 8 * s, 1);
     }
@@ -263,8 +279,13 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t lFree = CG == 2 ? tc::mapa_shared(bFree, 0) : bFree;
   const int first = CG == 2 ? (int)tc::cluster_id_x() : (int)blockIdx.x;
   const int step = CG == 2 ? (int)tc::nclusters_x() : (int)gridDim.x;
-  // a unit's chunks of k
-  auto chunk_range = [&](int unit, int& c0, int& c1) {
+  // a unit's product, its number there, and its chunks of k
+  auto problem_of = [&](int& unit) -> int {
+    if (FORWARD || unit < prm.p[0].units) return 0;
+    unit -= prm.p[0].units;
+    return FORWARD ? 0 : 1;
+  };
+  auto chunk_range = [&](const Problem& p, int unit, int& c0, int& c1) {
     c0 = unit % p.splits * p.chunks_per_split;
     c1 = min(p.chunks, c0 + p.chunks_per_split);
   };
@@ -273,19 +294,22 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (warp < 2) {
     // ============ TMA: warp 0 loads A, warp 1 loads B (both CTAs of a pair) ============
     const bool elected = tc::elect_one(), is_a = warp == 0;
-    const CUtensorMap* map = is_a ? &mA : &mB;
-    const bool mn = is_a ? AMN : BMN, blocked = is_a ? p.a_blocked : p.b_blocked;
-    const int rows = is_a ? 128 : BN / CG, zmul = is_a ? p.az : p.bz;
-    const uint32_t bytes = is_a && !AMN ? (uint32_t)p.a_bytes : (uint32_t)(rows * ROW);
+    const int rows = is_a ? 128 : BN / CG;
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int unit = first; unit < p.units && ok; unit += step) {
+    for (int all = first; all < prm.units && ok; all += step) {
+      int unit = all;
+      const int which = problem_of(unit);
+      const Problem& p = prm.p[which];
+      const CUtensorMap* map = is_a ? &prm.a[which] : &prm.b[which];
+      const bool mn = !FORWARD && (is_a ? p.a_mn : p.b_mn), blocked = is_a ? p.a_blocked : p.b_blocked;
+      const uint32_t bytes = is_a && !mn ? (uint32_t)p.a_bytes : (uint32_t)(rows * ROW);
       const Place pl = place(unit / p.splits, p.tiles_m, p.tiles_n);
       const int at = is_a ? pl.mt * BM + (int)rank * 128 : pl.nt * BN + (int)rank * (BN / CG);
-      const int z = pl.g * zmul;
+      const int z = pl.g * (is_a ? p.az : p.bz);
       int c0, c1;
-      chunk_range(unit, c0, c1);
+      chunk_range(p, unit, c0, c1);
       for (int kc = c0; kc < c1; ++kc) {
         if (!tc::mbar_wait(bEmpty + 8 * stage, phase ^ 1u, abort_flag, code, 1)) {
           ok = false;
@@ -305,7 +329,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               load3<CG>(dst + i * MN_BOX, map, full, at + 64 * i, kc * KE, z);
           }
         }
-        if (++stage == STAGES) {
+        if (++stage == stages) {
           stage = 0;
           phase ^= 1u;
         }
@@ -320,15 +344,18 @@ __global__ void __launch_bounds__(THREADS, 1)
     // ============ MMAs (rank 0) ============
     if (rank == 0) {
       const bool elected = tc::elect_one();
-      constexpr uint32_t ID = idesc<TYPE>(BM, BN, AMN, BMN);
-      // a step further along k, in 16-byte units: 32 bytes of a row, or 16 rows of 128 bytes
-      constexpr uint32_t IA = AMN ? 128 : 2, IB = BMN ? 128 : 2;
       int stage = 0, sums = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int unit = first; unit < p.units && ok; unit += step) {
+      for (int all = first; all < prm.units && ok; all += step) {
+        int unit = all;
+        const Problem& p = prm.p[problem_of(unit)];
+        const int a_mn = FORWARD ? 0 : p.a_mn, b_mn = FORWARD ? 0 : p.b_mn;
+        const uint32_t id = idesc<TYPE>(BM, BN, a_mn, b_mn);
+        // a step further along k, in 16-byte units: 32 bytes of a row, or 16 rows of 128 bytes
+        const uint32_t ia = a_mn ? 128 : 2, ib = b_mn ? 128 : 2;
         int c0, c1;
-        chunk_range(unit, c0, c1);
+        chunk_range(p, unit, c0, c1);
         for (int kc = c0; kc < c1 && ok;) {
           const int end = SUMS ? min(c1, kc + SUM_CHUNKS) : c1, r = sums & 1;
           if (sums >= 2 && !tc::mbar_wait(bFree + 8 * r, (uint32_t)(sums / 2 - 1) & 1, abort_flag, code, 2)) {
@@ -344,15 +371,15 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             tc::tc_fence_after();
             const uint32_t sA = base + stage * S::STAGE, sB = sA + S::A_BYTES;
-            const uint64_t dA = AMN ? tc::sw128_mn_desc(sA, MN_BOX) : tc::sw128_desc(sA);
-            const uint64_t dB = BMN ? tc::sw128_mn_desc(sB, MN_BOX) : tc::sw128_desc(sB);
+            const uint64_t dA = a_mn ? tc::sw128_mn_desc(sA, MN_BOX) : tc::sw128_desc(sA);
+            const uint64_t dB = b_mn ? tc::sw128_mn_desc(sB, MN_BOX) : tc::sw128_desc(sB);
             if (elected) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) mma<TYPE, CG>(d, dA + i * IA, dB + i * IB, ID, acc | (uint32_t)i);
+              for (int i = 0; i < 4; ++i) mma<TYPE, CG>(d, dA + i * ia, dB + i * ib, id, acc | (uint32_t)i);
               commit<CG>(bEmpty + 8 * stage);
             }
             acc = 1;
-            if (++stage == STAGES) {
+            if (++stage == stages) {
               stage = 0;
               phase ^= 1u;
             }
@@ -364,16 +391,39 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   } else if (warp >= FIRST_EPI) {
-    // ============ results ============
-    const int ew = warp - FIRST_EPI, q = warp & 3, half = ew >> 2, et = threadIdx.x - 32 * FIRST_EPI;
+    // ============ results: a warp has 32 rows and a quarter of the tile's columns ============
+    const int ew = warp - FIRST_EPI, q = warp & 3, quarter = ew >> 2, et = threadIdx.x - 32 * FIRST_EPI;
     float* turn = s_turn + ew * (TURN / 4);
-    const Epilogue& e = p.e;
+    auto barrier = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory"); };
+    if (!FORWARD && prm.sums.part) {
+      // 32 columns of partial sums at a time, beside the first MMAs: every warp adds a 16th of the parts
+      const PartSums& ps = prm.sums;
+      const int64_t per = ceil_div_d(ps.cols, 32), blocks = per * ps.groups;
+      for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+        const int64_t g = b / per, c = (b - g * per) * 32 + lane;
+        float v = 0.f;
+        if (c < ps.cols) {
+          const float* src = ps.part + g * ps.parts * ps.cols + c;
+#pragma unroll 8
+          for (int i = ew; i < ps.parts; i += EPI_WARPS) v += src[i * ps.cols];
+        }
+        s_sum[ew * 32 + lane] = v;
+        barrier();
+        if (ew == 0 && c < ps.cols) {
+          v = 0.f;
+#pragma unroll
+          for (int i = 0; i < EPI_WARPS; ++i) v += s_sum[i * 32 + lane];
+          ps.out.data[g * ps.out.group + c] = v;
+        }
+        barrier();
+      }
+    }
     int sums = 0, tile = 0;
     bool ok = true;
     auto wait_sum = [&]() {
       ok = tc::mbar_wait_warp(bAcc + 8 * (sums & 1), (uint32_t)(sums >> 1) & 1, abort_flag, code, 4);
       tc::tc_fence_after();
-      return tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)((sums & 1) * BN + half * HALF);
+      return tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)((sums & 1) * BN + quarter * QUART);
     };
     auto free_sum = [&]() {
       tc::tc_fence_before();
@@ -384,98 +434,130 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       ++sums;
     };
-    for (int unit = first; unit < p.units; unit += step, ++tile) {
+    // the next tile's column parameters (thread et: column et) and this lane's x_scale, loaded a tile ahead
+    float2 next_col = make_float2(1.f, 0.f);
+    float next_xs = 1.f;
+    auto prefetch = [&](int unit) {
+      if (!FORWARD || unit >= prm.units) return;
+      const Problem& p = prm.p[0];
+      const Place pl = place(unit / p.splits, p.tiles_m, p.tiles_n);
+      const int n = pl.nt * BN + et, m = pl.mt * BM + (int)rank * 128 + q * 32 + lane;
+      const int64_t g = pl.g;
+      if (et < BN && n < p.n) {
+        if (TYPE == LIPZ_E4M3) next_col.x = __ldg(p.e.w_scale.data + g * p.e.w_scale.group + n);
+        if (p.e.bias.data) next_col.y = __ldg(p.e.bias.data + g * p.e.bias.group + n);
+      }
+      if (TYPE == LIPZ_E4M3 && m < p.m) next_xs = __ldg(p.e.x_scale.data + g * p.e.x_scale.group + m);
+    };
+    if (FORWARD && !prm.p[0].part) prefetch(first);
+    for (int all = first; all < prm.units; all += step, ++tile) {
+      int unit = all;
+      const Problem& p = prm.p[problem_of(unit)];
+      const Epilogue& e = p.e;
       const Place pl = place(unit / p.splits, p.tiles_m, p.tiles_n);
       const int row0 = pl.mt * BM + (int)rank * 128 + q * 32, rows = p.m - row0;
-      const int64_t g = pl.g, row = row0 + lane;
+      const int64_t g = pl.g;
       int c0, c1;
-      chunk_range(unit, c0, c1);
+      chunk_range(p, unit, c0, c1);
       float2* col = s_col + (tile & 1) * BN;
       float xs = 1.f;
       if (FORWARD && !p.part) {
-        for (int i = et; i < BN; i += 32 * EPI_WARPS) {
-          const int n = pl.nt * BN + i;
-          float2 v = make_float2(1.f, 0.f);
-          if (n < p.n && e.w_scale.data) v.x = __ldg(e.w_scale.data + g * e.w_scale.group + n);
-          if (n < p.n && e.bias.data) v.y = __ldg(e.bias.data + g * e.bias.group + n);
-          col[i] = v;
-        }
-        if (e.x_scale.data && lane < rows) xs = __ldg(e.x_scale.data + g * e.x_scale.group + row);
-        asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
+        xs = next_xs;
+        if (et < BN) col[et] = next_col;
+        barrier();
+        prefetch(all + step);
       }
       if (!ok) continue;  // (a warp that gave up still comes to the others' barrier)
-      // 32 results of this lane's row, from column c of the warp's half
-      auto results = [&](float (&u)[32], int c) {
-        const int n0 = pl.nt * BN + half * HALF + c, cols = p.n - n0;
-        if (rows <= 0 || cols <= 0) return;
+      // CW results of this lane's row, from column c of the warp's quarter; v: the residual
+      auto columns_left = [&](int c) { return p.n - (pl.nt * BN + quarter * QUART + c); };
+      auto residual = [&](float (&v)[CW], int c) {
+        if (!FORWARD || p.part || !e.residual.data || rows <= 0) return;
+        const int64_t o = g * e.residual.group + (int64_t)row0 * e.residual.row + pl.nt * BN + quarter * QUART + c;
+#pragma unroll
+        for (int h = 0; h < CW; h += 16)
+          if (columns_left(c + h) > 0)
+            load_row<T>((const T*)e.residual.data + o + h, e.residual.row, rows, columns_left(c + h),
+                        p.res_align, turn, v + h);
+      };
+      auto results = [&](float (&u)[CW], const float (&v)[CW], int c) {
+        if (rows <= 0 || columns_left(c) <= 0) return;
+        const int n0 = pl.nt * BN + quarter * QUART + c;
         if (p.part) {
           const int64_t o = ((int64_t)(unit % p.splits) * p.groups + g) * p.m + row0;
-          store_row<float>(p.part + o * p.ldp + n0, p.ldp, rows, cols, 32, turn, u);
+#pragma unroll
+          for (int h = 0; h < CW; h += 16)
+            if (columns_left(c + h) > 0)
+              // (ldp is a multiple of 16: whole vectors)
+              store_row<float>(p.part + o * p.ldp + n0 + h, p.ldp, rows, 16, 32, turn, u + h);
           return;
         }
         if constexpr (FORWARD) {
+          const float2* cc = col + quarter * QUART + c;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float2 v = col[half * HALF + c + i];
-            u[i] = fmaf(u[i], xs * v.x, v.y);
+          for (int i = 0; i < CW; ++i) {
+            if (TYPE == LIPZ_E4M3) u[i] = fmaf(u[i], xs * cc[i].x, cc[i].y);
+            else u[i] += cc[i].y;
           }
-          if (e.pre.data)
-            store_row<bf16>((bf16*)e.pre.data + g * e.pre.group + (int64_t)row0 * e.pre.row + n0,
-                            e.pre.row, rows, cols, p.pre_align, turn, u);
+          if (e.pre.data) {
+            const int64_t o = g * e.pre.group + (int64_t)row0 * e.pre.row + n0;
+#pragma unroll
+            for (int h = 0; h < CW; h += 16)
+              if (columns_left(c + h) > 0)
+                store_row<bf16>((bf16*)e.pre.data + o + h, e.pre.row, rows, columns_left(c + h),
+                                p.pre_align, turn, u + h);
+          }
           with_act(e.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) u[i] = act_value<decltype(act)::value>(u[i], e.slope);
+            for (int i = 0; i < CW; i += 2) act_pair<decltype(act)::value>(u[i], u[i + 1], e.slope);
           });
           if (e.residual.data) {
-            float v[32];
-            load_row<T>((const T*)e.residual.data + g * e.residual.group +
-                            (int64_t)row0 * e.residual.row + n0,
-                        e.residual.row, rows, cols, p.res_align, turn, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) u[i] += v[i];
+            for (int i = 0; i < CW; ++i) u[i] += v[i];
           }
         }
-        store_row<T>((T*)e.y.data + g * e.y.group + (int64_t)row0 * e.y.row + n0, e.y.row, rows, cols,
-                     p.y_align, turn, u);
+        const int64_t o = g * e.y.group + (int64_t)row0 * e.y.row + n0;
+#pragma unroll
+        for (int h = 0; h < CW; h += 16)
+          if (columns_left(c + h) > 0)
+            store_row<T>((T*)e.y.data + o + h, e.y.row, rows, columns_left(c + h), p.y_align, turn, u + h);
+      };
+      auto tmem_load = [&](uint32_t t, float (&u)[CW]) {
+        uint32_t r[CW];
+        if constexpr (CW == 32) LIPZ_TMEM_LD32(t, r);
+        else LIPZ_TMEM_LD16(t, r);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < CW; ++i) u[i] = __uint_as_float(r[i]);
       };
       if constexpr (SUMS) {
-        float acc[HALF];
+        static_assert(QUART == CW, "the sums of a warp's columns stand in registers");
+        float acc[CW], v[CW];
 #pragma unroll
-        for (int i = 0; i < HALF; ++i) acc[i] = 0.f;
+        for (int i = 0; i < CW; ++i) acc[i] = 0.f;
         for (int kc = c0; kc < c1; kc += SUM_CHUNKS) {
           const uint32_t t = wait_sum();
           if (!ok) break;
-#pragma unroll
-          for (int c = 0; c < HALF; c += 32) {
-            uint32_t r[32];
-            LIPZ_TMEM_LD32(t + c, r);
-            tc::tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[c + i] += __uint_as_float(r[i]);
-          }
+          float u[CW];
+          tmem_load(t, u);
           free_sum();
+#pragma unroll
+          for (int i = 0; i < CW; ++i) acc[i] += u[i];
         }
         if (!ok) continue;
-#pragma unroll
-        for (int c = 0; c < HALF; c += 32) {
-          float u[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) u[i] = acc[c + i];
-          results(u, c);
-        }
+        residual(v, 0);
+        results(acc, v, 0);
       } else {
+        float v[CW];
+        residual(v, 0);
         const uint32_t t = wait_sum();
         if (!ok) continue;
 #pragma unroll 1
-        for (int c = 0; c < HALF; c += 32) {
-          uint32_t r[32];
-          float u[32];
-          LIPZ_TMEM_LD32(t + c, r);
-          tc::tmem_wait_ld();
-          if (c + 32 == HALF) free_sum();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) u[i] = __uint_as_float(r[i]);
-          results(u, c);
+        for (int c = 0; c < QUART; c += CW) {
+          float u[CW];
+          if (c) residual(v, c);
+          tmem_load(t + c, u);
+          if (c + CW == QUART) free_sum();
+          results(u, v, c);
         }
       }
     }
@@ -490,7 +572,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     else
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * BN));
   }
-  if (threadIdx.x == 0 && *code && p.err) *reinterpret_cast<volatile int*>(p.err) = *code;
+  if (threadIdx.x == 0 && *code && prm.err) *reinterpret_cast<volatile int*>(prm.err) = *code;
 }
 
 // Sum of the parts of k, in order, and the epilogue. E columns per thread.
@@ -500,8 +582,12 @@ struct FinishParams {
   int64_t ldp, split_stride, total;  // rows of all groups
   int splits, m, n;
 };
+struct FinishPair {
+  FinishParams f[2];
+};
 template <int E>
-__global__ void __launch_bounds__(256) k_finish(const FinishParams p) {
+__global__ void __launch_bounds__(256) k_finish(const __grid_constant__ FinishPair both_p) {
+  const FinishParams& p = both_p.f[blockIdx.z];
   const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   pdl_wait();
   if (r >= p.total) return;
@@ -555,29 +641,40 @@ __global__ void __launch_bounds__(256) k_finish(const FinishParams p) {
   }
 }
 
-// Rows copied to rows of whole 16-byte units (the bytes past a row's last are zero). A thread forms 16
-// bytes of one row.
+// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a
+// warp; a thread forms 16 bytes at a time.
 template <typename U>
-__global__ void __launch_bounds__(256)
-    k_align_rows(const U* __restrict__ src, int64_t group, int64_t ld, uint4* __restrict__ dst,
-                 int64_t rows, int64_t total, int cols, int units) {
+__device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
   constexpr int E = 16 / sizeof(U);
-  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  pdl_wait();
-  if (r >= total) return;
-  const int64_t g = r / rows;
-  const U* s = src + g * group + (r - g * rows) * ld;
-  for (int u = blockIdx.y * 32 + (threadIdx.x & 31); u < units; u += gridDim.y * 32) {
+  const int64_t g = r / p.rows;
+  const U* s = (const U*)p.src + g * p.group + (r - g * p.rows) * p.ld;
+  for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) {
     union {
       uint4 v;
       U e[E];
     } w;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const int64_t c = (int64_t)u * E + i;
-      w.e[i] = c < cols ? s[c] : U(0);
+    for (int i = 0; i < E; ++i) w.e[i] = u * E + i < p.cols ? s[u * E + i] : U(0);
+    ((uint4*)p.dst)[r * p.units + u] = w.v;
+  }
+}
+struct CopyJobs {
+  RowCopy c[4];
+  int n;
+};
+// 8 rows per block, of one copy after the other.
+template <typename U>
+__global__ void __launch_bounds__(256) k_copy_rows(const __grid_constant__ CopyJobs jobs) {
+  pdl_wait();
+  int64_t b = blockIdx.x;
+  for (int j = 0; j < jobs.n; ++j) {
+    const int64_t blocks = ceil_div_d(jobs.c[j].total, 8);
+    if (b < blocks) {
+      const int64_t r = b * 8 + (threadIdx.x >> 5);
+      if (r < jobs.c[j].total) copy_row<U>(jobs.c[j], r);
+      return;
     }
-    dst[r * units + u] = w.v;
+    b -= blocks;
   }
 }
 
@@ -651,109 +748,70 @@ bool encode(CUtensorMap* map, const Operand& o, const Extent& x, int64_t groups,
   return r == CUDA_SUCCESS;
 }
 
-struct Plan {
-  int cg, bn, splits;
-  bool sums;
-  int64_t tiles_m, tiles_n, chunks, chunks_per_split, ldp;
-  bool copy_a, copy_b;
-  int64_t lda, ldb;  // of the copies
-  uint64_t a_bytes, b_bytes, part_bytes;
-};
-
-Plan make_plan(const Gemm& g) {
-  Plan p{};
-  const int eb = type_bytes(g.type), unit = 16 / eb;
-  const Extent xa = extent(g.a, g.m, g.k), xb = extent(g.b, g.n, g.k);
-  p.copy_a = !tma_takes(g.a, xa, g.groups, eb);
-  p.copy_b = !tma_takes(g.b, xb, g.groups, eb);
-  auto round256 = [](int64_t v) { return (uint64_t)ceil_div(v, 256) * 256; };
-  p.lda = ceil_div(xa.cols, unit) * unit;
-  p.ldb = ceil_div(xb.cols, unit) * unit;
-  p.a_bytes = p.copy_a ? round256(g.groups * xa.rows * p.lda * eb) : 0;
-  p.b_bytes = p.copy_b ? round256(g.groups * xb.rows * p.ldb * eb) : 0;
-  p.chunks = ceil_div(g.k * eb, ROW);
-  p.sums = g.e.y.type == LIPZ_FP32;
-  // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its
-  // MMA steps (pairs of 256 x 256 run at the tensor cores' rate, narrower ones are bound by shared memory)
-  // or its epilogue, whichever is longer, and once the ring's and the epilogue's latency; parts of k cost
-  // another launch and their way through L2.
-  const int sms = sm_count();
-  struct Config { int cg, bn; double step, epi; };
-  static const Config configs[] = {{2, 256, 128, 5000}, {2, 128, 86, 2600}, {1, 128, 86, 2600}, {1, 64, 60, 1400}};
-  double best = 0;
-  for (const Config& c : configs) {
-    if (p.sums && c.bn > 128) continue;
-    const int64_t tm = ceil_div(g.m, 128 * c.cg), tn = ceil_div(g.n, c.bn), tiles = tm * tn * g.groups;
-    const int64_t slots = sms / c.cg;
-    for (int64_t s = 1; s <= 64 && s <= p.chunks; s *= 2) {
-      const int64_t per = ceil_div(p.chunks, s), parts = ceil_div(p.chunks, per);
-      if (parts != s && s > 1) continue;
-      if (s > 1 && tiles * s > 2 * slots) continue;
-      const double mma = per * 4 * c.step, waves = (double)ceil_div(tiles * s, slots);
-      double t = waves * (mma > c.epi ? mma : c.epi) + (mma > c.epi ? c.epi : mma) + 2000;
-      if (s > 1) t += 5000 + (double)g.groups * g.m * g.n * 4 * s * 2 / 4000;
-      if (tiles * s > INT32_MAX) continue;
-      if (best == 0 || t < best) {
-        best = t;
-        p.cg = c.cg, p.bn = c.bn, p.splits = (int)s;
-        p.tiles_m = tm, p.tiles_n = tn, p.chunks_per_split = per;
-      }
-    }
-  }
-  p.ldp = ceil_div(g.n, 8) * 8;
-  p.part_bytes = p.splits > 1 ? round256((int64_t)p.splits * g.groups * g.m * p.ldp * 4) : 0;
-  return p;
-}
+uint64_t round256(int64_t v) { return (uint64_t)ceil_div(v, 256) * 256; }
 
 // Sets the kernel's shared memory once per device.
 template <typename K>
-cudaError_t prepare_kernel(K kernel, int smem, std::atomic<uint64_t>& done) {
+cudaError_t prepare_kernel(K kernel, std::atomic<uint64_t>& done) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 64 && done.load() >> dev & 1) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
   if (e == cudaSuccess && dev < 64) done.fetch_or((uint64_t)1 << dev);
   return e;
 }
 
-template <int TYPE, int CG, int BN, bool AMN, bool BMN, typename T>
-cudaError_t launch(const Gemm& g, const Plan& p, void* part, cudaStream_t st) {
+template <int TYPE, int CG, int BN, bool FORWARD, typename T>
+cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
+                   cudaStream_t st) {
   using S = Shape<CG, BN>;
-  CUtensorMap ma, mb;
-  GemmParams k{};
-  const Extent xa = extent(g.a, g.m, g.k), xb = extent(g.b, g.n, g.k);
-  k.a_blocked = AMN && g.m % 64 == 0;
-  k.b_blocked = BMN && g.n % 64 == 0;
-  const int arows = AMN ? 64 : (int)(g.m >= 128 ? 128 : ceil_div(g.m, 8) * 8);
-  const int brows = BMN ? 64 : BN / CG;
-  if (!encode(&ma, g.a, xa, g.groups, TYPE, arows, k.a_blocked ? 2 : 0) ||
-      !encode(&mb, g.b, xb, g.groups, TYPE, brows, k.b_blocked ? BN / CG / 64 : 0))
-    return cudaErrorInvalidValue;
-  k.e = g.e;
-  k.part = (float*)part;
+  GemmParams<FORWARD ? 1 : 2> k;
+  memset(&k, 0, sizeof k);
+  bool turn = false;
+  for (int i = 0; i < q.n; ++i) {
+    const Gemm& g = q.g[i];
+    const GemmPlan::One& o = plan.p[i];
+    Problem& p = k.p[i];
+    const Extent xa = extent(g.a, g.m, g.k), xb = extent(g.b, g.n, g.k);
+    p.a_mn = !g.a.k_major, p.b_mn = !g.b.k_major;
+    p.a_blocked = p.a_mn && g.m % 64 == 0;
+    p.b_blocked = p.b_mn && g.n % 64 == 0;
+    const int arows = p.a_mn ? 64 : (int)(g.m >= 128 ? 128 : ceil_div(g.m, 8) * 8);
+    const int brows = p.b_mn ? 64 : BN / CG;
+    if (!encode(&k.a[i], g.a, xa, g.groups, TYPE, arows, p.a_blocked ? 2 : 0) ||
+        !encode(&k.b[i], g.b, xb, g.groups, TYPE, brows, p.b_blocked ? BN / CG / 64 : 0))
+      return cudaErrorInvalidValue;
+    p.e = g.e;
+    p.part = parts[i];
+    p.ldp = o.ldp;
+    p.groups = (int)g.groups, p.m = (int)g.m, p.n = (int)g.n;
+    p.tiles_m = (int)o.tiles_m, p.tiles_n = (int)o.tiles_n;
+    p.splits = o.splits;
+    p.units = (int)(o.tiles_m * o.tiles_n * g.groups * o.splits);
+    p.chunks = (int)o.chunks, p.chunks_per_split = (int)o.chunks_per_split;
+    p.a_bytes = arows * ROW;
+    p.az = g.groups > 1 && g.a.group != 0, p.bz = g.groups > 1 && g.b.group != 0;
+    auto align = [&](const lipz_mat& m) {
+      const int a = !m.data ? 32 : rows_aligned(m, g.groups, g.m, 32) ? 32 : rows_aligned(m, g.groups, g.m, 16) ? 16 : 0;
+      turn = turn || (m.data && !p.part && (!a || g.n % 16));
+      return a;
+    };
+    p.y_align = align(g.e.y), p.res_align = align(g.e.residual), p.pre_align = align(g.e.pre);
+    k.units += p.units;
+  }
+  if (sums) k.sums = *sums;
   k.err = timeout_word();
-  k.ldp = p.ldp;
-  k.groups = (int)g.groups, k.m = (int)g.m, k.n = (int)g.n;
-  k.tiles_m = (int)p.tiles_m, k.tiles_n = (int)p.tiles_n;
-  k.splits = p.splits;
-  k.units = (int)(p.tiles_m * p.tiles_n * g.groups * p.splits);
-  k.chunks = (int)p.chunks, k.chunks_per_split = (int)p.chunks_per_split;
-  k.a_bytes = arows * ROW;
-  k.az = g.groups > 1 && g.a.group != 0, k.bz = g.groups > 1 && g.b.group != 0;
-  auto align = [&](const lipz_mat& m) {
-    return !m.data ? 0 : rows_aligned(m, g.groups, g.m, 32) ? 32 : rows_aligned(m, g.groups, g.m, 16) ? 16 : 0;
-  };
-  k.y_align = align(g.e.y), k.res_align = align(g.e.residual), k.pre_align = align(g.e.pre);
+  k.stages = S::stages(turn);
   static std::atomic<uint64_t> done{0};
-  auto kernel = k_gemm_op<TYPE, CG, BN, AMN, BMN, T>;
-  cudaError_t e = prepare_kernel(kernel, S::SMEM, done);
+  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T>;
+  cudaError_t e = prepare_kernel(kernel, done);
   if (e != cudaSuccess) return e;
   const int slots = sm_count() / CG, ctas = (k.units < slots ? k.units : slots) * CG;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = S::SMEM;
+  cfg.dynamicSmemBytes = S::smem(k.stages, turn);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -764,70 +822,159 @@ cudaError_t launch(const Gemm& g, const Plan& p, void* part, cudaStream_t st) {
   const bool shared = st == nullptr || st == cudaStreamLegacy || st == cudaStreamPerThread;
   cfg.attrs = attr;
   cfg.numAttrs = shared ? 1 : 2;
-  return cudaLaunchKernelEx(&cfg, kernel, ma, mb, k);
+  return cudaLaunchKernelEx(&cfg, kernel, k);
 }
 
-template <int TYPE, bool AMN, bool BMN>
-cudaError_t launch_shape(const Gemm& g, const Plan& p, void* part, cudaStream_t st) {
-  if (p.sums) {
-    if (p.cg == 2) return launch<TYPE, 2, 128, AMN, BMN, float>(g, p, part, st);
-    if (p.bn == 128) return launch<TYPE, 1, 128, AMN, BMN, float>(g, p, part, st);
-    return launch<TYPE, 1, 64, AMN, BMN, float>(g, p, part, st);
+template <int TYPE, bool FORWARD>
+cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* parts, const PartSums* sums,
+                         cudaStream_t st) {
+  if (q.g[0].e.y.type == LIPZ_FP32) {
+    if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, float>(q, p, parts, sums, st);
+    if (p.bn == 128) return launch<TYPE, 1, 128, FORWARD, float>(q, p, parts, sums, st);
+    return launch<TYPE, 1, 64, FORWARD, float>(q, p, parts, sums, st);
   }
-  if (p.cg == 2 && p.bn == 256) return launch<TYPE, 2, 256, AMN, BMN, bf16>(g, p, part, st);
-  if (p.cg == 2) return launch<TYPE, 2, 128, AMN, BMN, bf16>(g, p, part, st);
-  if (p.bn == 128) return launch<TYPE, 1, 128, AMN, BMN, bf16>(g, p, part, st);
-  return launch<TYPE, 1, 64, AMN, BMN, bf16>(g, p, part, st);
-}
-
-cudaError_t align_rows(Operand* o, const Extent& x, int64_t groups, int eb, int64_t ld, void* dst,
-                       cudaStream_t st) {
-  const int units = (int)(ld * eb / 16);
-  const int64_t total = groups * x.rows;
-  const dim3 grid = rows_by_columns(total, units);
-  cudaError_t e =
-      eb == 2 ? launch_pdl(k_align_rows<unsigned short>, grid, dim3(256), 0, st,
-                           (const unsigned short*)o->data, o->group, o->ld, (uint4*)dst, x.rows, total,
-                           (int)x.cols, units)
-              : launch_pdl(k_align_rows<unsigned char>, grid, dim3(256), 0, st,
-                           (const unsigned char*)o->data, o->group, o->ld, (uint4*)dst, x.rows, total,
-                           (int)x.cols, units);
-  o->data = dst;
-  o->ld = ld;
-  o->group = x.rows * ld;
-  return e;
+  if (p.cg == 2 && p.bn == 256) return launch<TYPE, 2, 256, FORWARD, bf16>(q, p, parts, sums, st);
+  if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, bf16>(q, p, parts, sums, st);
+  if (p.bn == 128) return launch<TYPE, 1, 128, FORWARD, bf16>(q, p, parts, sums, st);
+  return launch<TYPE, 1, 64, FORWARD, bf16>(q, p, parts, sums, st);
 }
 
 }  // namespace
 
-uint64_t gemm_workspace(const Gemm& g) {
-  const Plan p = make_plan(g);
-  return p.a_bytes + p.b_bytes + p.part_bytes;
+GemmPlan plan_products(const Products& q) {
+  GemmPlan plan{};
+  const int eb = type_bytes(q.g[0].type);
+  const bool sums = q.g[0].e.y.type == LIPZ_FP32;
+  // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its
+  // MMA steps (pairs of 256 x 256 run at the tensor cores' rate, narrower ones are bound by shared memory)
+  // or its epilogue, whichever is longer, and once the ring's and the epilogue's latency; parts of k cost
+  // another launch and their way through L2.
+  const int sms = sm_count();
+  struct Config { int cg, bn; double step, epi; };
+  static const Config configs[] = {{2, 256, 128, 5000}, {2, 128, 86, 2600}, {1, 128, 86, 2600}, {1, 64, 60, 1400}};
+  double best = -1;
+  static const int force_cg = getenv("OPCG") ? atoi(getenv("OPCG")) : 0, force_bn = getenv("OPBN") ? atoi(getenv("OPBN")) : 0, force_s = getenv("OPS") ? atoi(getenv("OPS")) : 0;
+  for (const Config& c : configs) {
+    if (sums && c.bn > 128) continue;
+    if (force_cg && (c.cg != force_cg || c.bn != force_bn)) continue;
+    const int64_t slots = sms / c.cg;
+    for (int s0 = 1; s0 <= 64; s0 *= 2) {
+      if (force_s && s0 != force_s) continue;
+      GemmPlan t{};
+      t.cg = c.cg, t.bn = c.bn;
+      double work = 0, top = 0, extra = 0;
+      bool fits = true, split = false;
+      for (int i = 0; i < q.n; ++i) {
+        const Gemm& g = q.g[i];
+        GemmPlan::One& o = t.p[i];
+        o.tiles_m = ceil_div(g.m, 128 * c.cg), o.tiles_n = ceil_div(g.n, c.bn);
+        o.chunks = ceil_div(g.k * eb, ROW);
+        const int64_t want = s0 < o.chunks ? s0 : o.chunks, tiles = o.tiles_m * o.tiles_n * g.groups;
+        o.chunks_per_split = ceil_div(o.chunks, want);
+        o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);
+        fits = fits && tiles * o.splits <= INT32_MAX / 2 && (o.splits == 1 || tiles * o.splits <= 2 * slots);
+        const double mma = o.chunks_per_split * 4 * c.step, unit_t = mma > c.epi ? mma : c.epi;
+        work += unit_t * tiles * o.splits;
+        top = unit_t > top ? unit_t : top;
+        if (o.splits > 1) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 4000, split = true;
+      }
+      if (!fits || (s0 > 1 && !split)) continue;
+      double waves = work / (slots * top);
+      waves = waves < 1 ? 1 : (double)(int64_t)(waves + 0.999);
+      const double time = waves * top + c.epi + 2000 + extra + (split ? 5000 : 0);
+      if (best < 0 || time < best) best = time, plan = t;
+    }
+  }
+  plan_space(q, &plan);
+  return plan;
 }
 
-cudaError_t gemm(const Gemm& args, void* workspace, cudaStream_t st) {
-  Gemm g = args;
-  const Plan p = make_plan(g);
-  const int eb = type_bytes(g.type);
+void plan_space(const Products& q, GemmPlan* plan) {
+  const int eb = type_bytes(q.g[0].type), unit = 16 / eb;
+  plan->bytes = 0;
+  for (int i = 0; i < q.n; ++i) {
+    const Gemm& g = q.g[i];
+    GemmPlan::One& o = plan->p[i];
+    const Extent xa = extent(g.a, g.m, g.k), xb = extent(g.b, g.n, g.k);
+    o.copy_a = !tma_takes(g.a, xa, g.groups, eb);
+    o.copy_b = !tma_takes(g.b, xb, g.groups, eb);
+    o.lda = ceil_div(xa.cols, unit) * unit;
+    o.ldb = ceil_div(xb.cols, unit) * unit;
+    o.a_bytes = o.copy_a ? round256(g.groups * xa.rows * o.lda * eb) : 0;
+    o.b_bytes = o.copy_b ? round256(g.groups * xb.rows * o.ldb * eb) : 0;
+    o.ldp = ceil_div(g.n, 16) * 16;
+    o.part_bytes = o.splits > 1 ? round256((int64_t)o.splits * g.groups * g.m * o.ldp * 4) : 0;
+    plan->bytes += o.a_bytes + o.b_bytes + o.part_bytes;
+  }
+}
+
+int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* copies) {
   char* w = (char*)workspace;
-  cudaError_t e = cudaSuccess;
-  if (p.copy_a) e = align_rows(&g.a, extent(g.a, g.m, g.k), g.groups, eb, p.lda, w, st);
-  if (e == cudaSuccess && p.copy_b)
-    e = align_rows(&g.b, extent(g.b, g.n, g.k), g.groups, eb, p.ldb, w + p.a_bytes, st);
-  if (e != cudaSuccess) return e;
-  void* part = p.splits > 1 ? w + p.a_bytes + p.b_bytes : nullptr;
-  if (g.type == LIPZ_E4M3) e = launch_shape<LIPZ_E4M3, false, false>(g, p, part, st);
-  else if (g.a.k_major && g.b.k_major) e = launch_shape<LIPZ_BF16, false, false>(g, p, part, st);
-  else if (g.a.k_major) e = launch_shape<LIPZ_BF16, false, true>(g, p, part, st);
-  else e = launch_shape<LIPZ_BF16, true, true>(g, p, part, st);
-  if (e != cudaSuccess || !part) return e;
-  FinishParams f{g.e, (const float*)part, p.ldp, g.groups * g.m * p.ldp, g.groups * g.m, p.splits,
-                 (int)g.m, (int)g.n};
-  auto four = [&](const lipz_mat& m) {
-    return !m.data || rows_aligned(m, g.groups, g.m, 4 * type_bytes(m.type));
-  };
-  const bool vec = g.n % 4 == 0 && four(g.e.y) && four(g.e.pre);
-  const dim3 grid = rows_by_columns(f.total, vec ? g.n / 4 : g.n);
+  int n = 0;
+  for (int i = 0; i < q->n; ++i) {
+    Gemm& g = q->g[i];
+    const GemmPlan::One& o = plan.p[i];
+    const int eb = type_bytes(g.type);
+    auto add = [&](Operand& t, const Extent& x, int64_t ld, uint64_t bytes) {
+      copies[n++] = {t.data, w, t.group, t.ld, x.rows, g.groups * x.rows, x.cols, ld * eb / 16};
+      t.data = w, t.ld = ld, t.group = x.rows * ld;
+      w += bytes;
+    };
+    if (o.copy_a) add(g.a, extent(g.a, g.m, g.k), o.lda, o.a_bytes);
+    if (o.copy_b) add(g.b, extent(g.b, g.n, g.k), o.ldb, o.b_bytes);
+  }
+  return n;
+}
+
+cudaError_t run_copies(const RowCopy* c, int n, int type, cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  CopyJobs jobs{};
+  jobs.n = n;
+  int64_t blocks = 0;
+  for (int i = 0; i < n; ++i) {
+    jobs.c[i] = c[i];
+    blocks += ceil_div(c[i].total, 8);
+  }
+  return type == LIPZ_BF16
+             ? launch_pdl(k_copy_rows<unsigned short>, dim3((unsigned)blocks), dim3(256), 0, st, jobs)
+             : launch_pdl(k_copy_rows<unsigned char>, dim3((unsigned)blocks), dim3(256), 0, st, jobs);
+}
+
+cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
+                         cudaStream_t st) {
+  char* w = (char*)workspace;
+  float* parts[2] = {nullptr, nullptr};
+  for (int i = 0; i < q.n; ++i) w += plan.p[i].a_bytes + plan.p[i].b_bytes;
+  for (int i = 0; i < q.n; ++i)
+    if (plan.p[i].part_bytes) {
+      parts[i] = (float*)w;
+      w += plan.p[i].part_bytes;
+    }
+  const Gemm& g0 = q.g[0];
+  cudaError_t e;
+  if (g0.type == LIPZ_E4M3) e = launch_shape<LIPZ_E4M3, true>(q, plan, parts, sums, st);
+  else if (g0.a.k_major && g0.b.k_major) e = launch_shape<LIPZ_BF16, true>(q, plan, parts, sums, st);
+  else e = launch_shape<LIPZ_BF16, false>(q, plan, parts, sums, st);
+  if (e != cudaSuccess || (!parts[0] && !parts[1])) return e;
+  FinishPair f{};
+  int n = 0;
+  bool vec = true;
+  int64_t rows = 0, cols = 0;
+  for (int i = 0; i < q.n; ++i) {
+    if (!parts[i]) continue;
+    const Gemm& g = q.g[i];
+    const int64_t ldp = plan.p[i].ldp;
+    f.f[n++] = {g.e, parts[i], ldp, g.groups * g.m * ldp, g.groups * g.m, plan.p[i].splits, (int)g.m,
+                (int)g.n};
+    auto four = [&](const lipz_mat& m) {
+      return !m.data || rows_aligned(m, g.groups, g.m, 4 * type_bytes(m.type));
+    };
+    vec = vec && g.n % 4 == 0 && four(g.e.y) && four(g.e.pre);
+    rows = rows > g.groups * g.m ? rows : g.groups * g.m;
+    cols = cols > g.n ? cols : g.n;
+  }
+  dim3 grid = rows_by_columns(rows, vec ? cols / 4 : cols);
+  grid.z = n;
   return vec ? launch_pdl(k_finish<4>, grid, dim3(256), 0, st, f)
              : launch_pdl(k_finish<1>, grid, dim3(256), 0, st, f);
 }

@@ -30,9 +30,49 @@ struct Gemm {
   Epilogue e;
 };
 
-// Scratch bytes of a product: copies of operands whose rows TMA does not take, partial sums.
-uint64_t gemm_workspace(const Gemm& g);
-cudaError_t gemm(const Gemm& g, void* workspace, cudaStream_t st);
+// Sums that a launch forms beside its products: out[g][c] = sum over p < parts of part[g][p][c].
+struct PartSums {
+  const float* part;
+  int64_t cols;
+  int groups, parts;
+  lipz_vec out;
+};
+
+// One product, or two independent ones (the backward's: products with a plain epilogue and the same type
+// of results), which then share a launch.
+struct Products {
+  Gemm g[2];
+  int n;
+};
+
+// Copies of operands whose rows TMA does not take, to rows of whole 16-byte units.
+struct RowCopy {
+  const void* src;  // null: none
+  void* dst;
+  int64_t group, ld, rows, total, cols, units;
+};
+
+// How products will run: their scratch memory, and the copies that have to be made before them.
+struct GemmPlan {
+  struct One {
+    int splits;
+    bool copy_a, copy_b;
+    int64_t tiles_m, tiles_n, chunks, chunks_per_split, lda, ldb, ldp;
+    uint64_t a_bytes, b_bytes, part_bytes;
+  } p[2];
+  int cg, bn;
+  uint64_t bytes;
+};
+GemmPlan plan_products(const Products& q);
+// The scratch memory of a plan (already part of plan_products' own).
+void plan_space(const Products& q, GemmPlan* plan);
+// The copies that the products of a plan need, into its workspace (copies[4]), and the operands that the
+// products then have.
+int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* copies);
+cudaError_t run_copies(const RowCopy* c, int n, int type, cudaStream_t st);
+// The products themselves; sums: null, or formed beside them.
+cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
+                         cudaStream_t st);
 
 // The device word that a kernel sets when one of its waits expires (null: none can be had).
 int* timeout_word();

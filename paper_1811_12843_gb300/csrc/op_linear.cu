@@ -14,41 +14,45 @@ namespace {
 // of k (parts > 1: few columns), and meet the rows of x, which stay in L1. Bound: HBM (w is read once).
 constexpr int W_ROWS = 2, VEC_WARPS = 4;
 
+// 16 bytes of a row (VEC), or one element.
 template <int TYPE>
-struct Elem;
-template <>
-struct Elem<LIPZ_BF16> {
-  typedef bf16 T;
-  static constexpr int E = 8;
-  static __device__ __forceinline__ void decode(const uint4& r, float* v) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+struct Elem {
+  typedef typename std::conditional<TYPE == LIPZ_BF16, bf16, e4m3>::type T;
+  static constexpr int E = 16 / sizeof(T);
+  template <bool VEC>
+  struct Vec {
+    uint32_t w[VEC ? 4 : 1];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      for (uint32_t& v : w) v = 0;
     }
-  }
-  static __device__ __forceinline__ float one(T v) { return __bfloat162float(v); }
-};
-template <>
-struct Elem<LIPZ_E4M3> {
-  typedef e4m3 T;
-  static constexpr int E = 16;
-  static __device__ __forceinline__ void decode(const uint4& r, float* v) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    __device__ __forceinline__ void load(const T* p) {
+      if constexpr (VEC) {
+        const uint4 r = __ldg(reinterpret_cast<const uint4*>(p));
+        w[0] = r.x, w[1] = r.y, w[2] = r.z, w[3] = r.w;
+      } else if constexpr (TYPE == LIPZ_BF16) {
+        w[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
+      } else {
+        w[0] = __ldg(p);
+      }
+    }
+    __device__ __forceinline__ void decode(float* v) const {
+      if constexpr (TYPE == LIPZ_BF16) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const __half2_raw h =
-          __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (i & 1) * 16), __NV_E4M3);
-      const float2 f = __half22float2(__half2(h));
-      v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        for (int i = 0; i < (VEC ? 8 : 1); ++i)
+          v[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < (VEC ? 8 : 1); ++i) {
+          const __half2_raw h =
+              __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (i & 1) * 16), __NV_E4M3);
+          const float2 f = __half22float2(__half2(h));
+          v[2 * i] = f.x;
+          if constexpr (VEC) v[2 * i + 1] = f.y;
+        }
+      }
     }
-  }
-  static __device__ __forceinline__ float one(T v) {
-    __nv_fp8_e4m3 f;
-    f.__x = v;
-    return (float)f;
-  }
+  };
 };
 
 struct VecParams {
@@ -81,24 +85,37 @@ __global__ void __launch_bounds__(32 * VEC_WARPS) k_linear_rows(const VecParams 
   for (int j = 0; j < W_ROWS; ++j) wo[j] = min(n0 + j, p.n - 1) * p.w.row;
 #pragma unroll
   for (int r = 0; r < R; ++r) xo[r] = (int64_t)min(r, p.rows - 1) * p.x.row;
+  // AHEAD vectors of each of w's rows are in flight while those before them are multiplied
+  constexpr int AHEAD = 4;
   if (n0 < p.n) {
-#pragma unroll 4
-    for (int64_t u = part * 32 + lane; u < units; u += step) {
-      float wv[W_ROWS][E];
+    for (int64_t u0 = part * 32 + lane; u0 < units; u0 += AHEAD * step) {
+      typename L::template Vec<VEC> wv[AHEAD][W_ROWS];
 #pragma unroll
-      for (int j = 0; j < W_ROWS; ++j) {
-        if constexpr (VEC) L::decode(__ldg((const uint4*)(w + wo[j] + u * E)), wv[j]);
-        else wv[j][0] = L::one(w[wo[j] + u]);
-      }
+      for (int a = 0; a < AHEAD; ++a)
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float xv[E];
-        if constexpr (VEC) L::decode(__ldg((const uint4*)(x + xo[r] + u * E)), xv);
-        else xv[0] = L::one(x[xo[r] + u]);
+        for (int j = 0; j < W_ROWS; ++j) {
+          const int64_t u = u0 + a * step;
+          wv[a][j].zero();
+          if (u < units) wv[a][j].load(w + wo[j] + u * E);
+        }
 #pragma unroll
-        for (int j = 0; j < W_ROWS; ++j)
+      for (int a = 0; a < AHEAD; ++a) {
+        const int64_t u = u0 + a * step;
+        if (u >= units) break;
+        float wf[W_ROWS][E];
 #pragma unroll
-          for (int i = 0; i < E; ++i) acc[j][r] = fmaf(wv[j][i], xv[i], acc[j][r]);
+        for (int j = 0; j < W_ROWS; ++j) wv[a][j].decode(wf[j]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          typename L::template Vec<VEC> xv;
+          float xf[E];
+          xv.load(x + xo[r] + u * E);
+          xv.decode(xf);
+#pragma unroll
+          for (int j = 0; j < W_ROWS; ++j)
+#pragma unroll
+            for (int i = 0; i < E; ++i) acc[j][r] = fmaf(wf[j][i], xf[i], acc[j][r]);
+        }
       }
     }
   }
@@ -153,9 +170,10 @@ Epilogue epilogue_of(const lipz_linear_args& a) {
   if (a.x.type != LIPZ_E4M3) e.x_scale.data = e.w_scale.data = nullptr;
   return e;
 }
-Gemm gemm_of(const lipz_linear_args& a) {
-  return {{a.x.data, a.x.group, a.x.row, true}, {a.w.data, a.w.group, a.w.row, true}, a.x.type,
-          a.groups, a.rows, a.n, a.k, epilogue_of(a)};
+Products product_of(const lipz_linear_args& a) {
+  return {{{{a.x.data, a.x.group, a.x.row, true}, {a.w.data, a.w.group, a.w.row, true}, a.x.type,
+            a.groups, a.rows, a.n, a.k, epilogue_of(a)}},
+          1};
 }
 
 // du = dy act'(pre), in bf16 rows of ldu elements, and the sums of its columns over the block's rows:
@@ -212,50 +230,81 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p) {
   }
 }
 
-// The workspace of a backward call: du, the parts of db, then the larger of the two products' own.
+// The workspace of a backward call: du, the parts of db, then the products' own. dx and dw share a launch
+// where their results have one type.
 struct BackPlan {
   bool vec, need_du;
   int64_t ldu, blocks, rows_per_block;
   uint64_t du_bytes, db_bytes, bytes;
-  Gemm dx, dw;
+  int launches;
+  Products q[2];
+  GemmPlan plan[2];
 };
 BackPlan back_plan(const lipz_linear_backward_args& a) {
-  BackPlan b;
+  BackPlan b{};
   b.vec = a.n % 8 == 0 && rows_aligned(a.dy, a.groups, a.rows, 16) &&
           (!a.pre.data || rows_aligned(a.pre, a.groups, a.rows, 16));
   b.need_du = a.act != LIPZ_ACT_NONE && (a.dx.data || a.dw.data);
   b.ldu = ceil_div(a.n, 8) * 8;
+  if (a.groups == 0 || a.rows == 0) return b;
   // enough blocks to fill the device, of 8 rows or more
   const int64_t cols = ceil_div(a.n, b.vec ? 256 : 32), fill = 8 * sm_count();
-  const int64_t want = ceil_div(fill, cols * (a.groups > 0 ? a.groups : 1));
-  b.rows_per_block = ceil_div(ceil_div(a.rows > 0 ? a.rows : 1, want), 8) * 8;
+  const int64_t want = ceil_div(fill, cols * a.groups);
+  b.rows_per_block = ceil_div(ceil_div(a.rows, want), 8) * 8;
   b.blocks = ceil_div(a.rows, b.rows_per_block);
   auto round256 = [](int64_t v) { return (uint64_t)ceil_div(v, 256) * 256; };
   b.du_bytes = b.need_du ? round256(a.groups * a.rows * b.ldu * 2) : 0;
   b.db_bytes = a.db.data ? round256(a.groups * b.blocks * a.n * 4) : 0;
+  b.bytes = b.du_bytes + b.db_bytes;
   const void* d = b.need_du ? a.workspace : a.dy.data;
   const int64_t dg = b.need_du ? a.rows * b.ldu : a.dy.group, dr = b.need_du ? b.ldu : a.dy.row;
-  b.dx = {{d, dg, dr, true}, {a.w.data, a.w.group, a.w.row, false}, LIPZ_BF16, a.groups, a.rows, a.k,
-          a.n, {a.dx}};
-  b.dw = {{d, dg, dr, false}, {a.x.data, a.x.group, a.x.row, false}, LIPZ_BF16, a.groups, a.n, a.k,
-          a.rows, {a.dw}};
-  const bool none = a.groups == 0 || a.rows == 0;
-  const uint64_t x = a.dx.data && !none ? gemm_workspace(b.dx) : 0;
-  const uint64_t w = a.dw.data && !none ? gemm_workspace(b.dw) : 0;
-  b.bytes = b.du_bytes + b.db_bytes + (x > w ? x : w);
+  const Gemm dx{{d, dg, dr, true}, {a.w.data, a.w.group, a.w.row, false}, LIPZ_BF16, a.groups, a.rows,
+                a.k, a.n, {a.dx}};
+  const Gemm dw{{d, dg, dr, false}, {a.x.data, a.x.group, a.x.row, false}, LIPZ_BF16, a.groups, a.n,
+                a.k, a.rows, {a.dw}};
+  // bf16 results run as planned for both, whether or not both are asked for, so that one's values do not
+  // depend on the other; fp32 results are planned by themselves
+  Products both{{dx, dw}, 2};
+  both.g[0].e.y.type = both.g[1].e.y.type = LIPZ_BF16;
+  const GemmPlan joint = plan_products(both);
+  auto add = [&](const Gemm& g, int i) {
+    if (!g.e.y.data) return;
+    if (g.e.y.type == LIPZ_FP32) {
+      b.q[b.launches] = {{g}, 1};
+      b.plan[b.launches] = plan_products(b.q[b.launches]);
+      ++b.launches;
+      return;
+    }
+    if (!b.launches || b.q[b.launches - 1].g[0].e.y.type == LIPZ_FP32) {
+      b.plan[b.launches] = joint;
+      b.q[b.launches++].n = 0;
+    }
+    Products& q = b.q[b.launches - 1];
+    b.plan[b.launches - 1].p[q.n] = joint.p[i];
+    q.g[q.n++] = g;
+    plan_space(q, &b.plan[b.launches - 1]);
+  };
+  add(dx, 0);
+  add(dw, 1);
+  for (int i = 0; i < b.launches; ++i) b.bytes += b.plan[i].bytes;
   return b;
 }
 
 }  // namespace
 
 uint64_t linear_workspace(const lipz_linear_args& a) {
-  return a.groups == 0 || a.rows <= FEW_ROWS ? 0 : gemm_workspace(gemm_of(a));
+  return a.groups == 0 || a.rows <= FEW_ROWS ? 0 : plan_products(product_of(a)).bytes;
 }
 
 cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {
   if (a.groups == 0 || a.rows == 0) return cudaSuccess;
   if (a.rows <= FEW_ROWS) return linear_rows(a, epilogue_of(a), st);
-  return gemm(gemm_of(a), a.workspace, st);
+  Products q = product_of(a);
+  const GemmPlan plan = plan_products(q);
+  RowCopy copies[4];
+  const int n = plan_copies(plan, &q, a.workspace, copies);
+  const cudaError_t e = run_copies(copies, n, a.x.type, st);
+  return e != cudaSuccess ? e : run_products(plan, q, a.workspace, nullptr, st);
 }
 
 uint64_t linear_backward_workspace(const lipz_linear_backward_args& a) { return back_plan(a).bytes; }
@@ -275,20 +324,26 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st)
     }
     return e;
   }
-  const BackPlan b = back_plan(a);
+  BackPlan b = back_plan(a);
   bf16* du = b.need_du ? (bf16*)a.workspace : nullptr;
   float* part = a.db.data ? (float*)((char*)a.workspace + b.du_bytes) : nullptr;
-  void* rest = (char*)a.workspace + b.du_bytes + b.db_bytes;
-  cudaError_t e = cudaSuccess;
-  if (du || part) {
+  char* rest = (char*)a.workspace + b.du_bytes + b.db_bytes;
+  RowCopy copies[4];
+  int n = 0;
+  char* at[2] = {rest, rest + b.plan[0].bytes};
+  for (int i = 0; i < b.launches; ++i) n += plan_copies(b.plan[i], &b.q[i], at[i], copies + n);
+  cudaError_t e = run_copies(copies, n, LIPZ_BF16, st);
+  if (e == cudaSuccess && (du || part)) {
     const DuArgs p{a.dy, a.pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope};
     const dim3 grid((unsigned)ceil_div(a.n, b.vec ? 256 : 32), (unsigned)b.blocks, (unsigned)a.groups);
     e = b.vec ? launch_pdl(k_du<8>, grid, dim3(256), 0, st, p)
               : launch_pdl(k_du<1>, grid, dim3(256), 0, st, p);
-    if (e == cudaSuccess && part) e = sum_parts(part, a.groups, (int)b.blocks, a.n, a.db, st);
   }
-  if (e == cudaSuccess && a.dx.data) e = gemm(b.dx, rest, st);
-  if (e == cudaSuccess && a.dw.data) e = gemm(b.dw, rest, st);
+  const PartSums sums{part, a.n, (int)a.groups, (int)b.blocks, a.db};
+  if (e == cudaSuccess && part && !b.launches)
+    e = sum_parts(part, a.groups, (int)b.blocks, a.n, a.db, st);
+  for (int i = 0; i < b.launches && e == cudaSuccess; ++i)
+    e = run_products(b.plan[i], b.q[i], at[i], i == 0 && part ? &sums : nullptr, st);
   return e;
 }
 

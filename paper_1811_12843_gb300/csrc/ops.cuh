@@ -165,6 +165,65 @@ __device__ __forceinline__ float act_slope(float u, float slope) {
   return 1.f;
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t both(float a) { return pack2(a, a); }
+
+// act_value of two values, in place: the same operations in the same order.
+template <int ACT>
+__device__ __forceinline__ void act_pair(float& a, float& b, float slope) {
+  if constexpr (ACT == LIPZ_ACT_TANH || ACT == LIPZ_ACT_GELU || ACT == LIPZ_ACT_SILU) {
+    const uint64_t u = pack2(a, b), one = both(1.f);
+    if constexpr (ACT == LIPZ_ACT_TANH) {
+      const float aa = fabsf(a), ab = fabsf(b);
+      const uint64_t m = pack2(aa, ab), m2 = mul2(m, m);
+      const float2 arg = unpack2(mul2(m, both(2.f * LOG2E)));
+      const float2 y = unpack2(add2(pack2(ex2_approx(arg.x), ex2_approx(arg.y)), one));
+      const float2 t = unpack2(fma2(both(-2.f), pack2(rcp_approx(y.x), rcp_approx(y.y)), one));
+      uint64_t q = fma2(m2, both(0.021869488536155203f), both(-0.053968253968253971f));
+      q = fma2(m2, q, both(0.13333333333333333f));
+      q = fma2(m2, q, both(-0.33333333333333333f));
+      const float2 s = unpack2(mul2(m, fma2(m2, q, one)));
+      a = copysignf(aa < 0.25f ? s.x : t.x, a);
+      b = copysignf(ab < 0.25f ? s.y : t.y, b);
+    } else {
+      uint64_t v = u;
+      if constexpr (ACT == LIPZ_ACT_GELU) v = mul2(u, fma2(both(GELU_3), mul2(u, u), both(GELU_1)));
+      const float2 arg = unpack2(mul2(v, both(-LOG2E)));
+      const float2 y = unpack2(add2(pack2(ex2_approx(arg.x), ex2_approx(arg.y)), one));
+      const float2 r = unpack2(mul2(u, pack2(rcp_approx(y.x), rcp_approx(y.y))));
+      a = r.x, b = r.y;
+    }
+  } else {
+    a = act_value<ACT>(a, slope);
+    b = act_value<ACT>(b, slope);
+  }
+}
+
 // Calls f with the activation as a constant.
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F&& f) {
