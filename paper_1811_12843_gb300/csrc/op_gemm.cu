@@ -31,13 +31,24 @@ constexpr int MN_BOX = 64 * ROW;          // 64 k by 64 m (or n) of an operand w
 constexpr int SUM_CHUNKS = 8;             // chunks of k whose sum stands in tensor memory, for fp32 results
 constexpr int SMEM_MAX = 232448, STAGES_MAX = 8;
 
+// A tile's parameters for the result warps.
+struct Slot {
+  int64_t y, residual, pre, part;  // element offsets of the CTA's first row and the tile's first column
+  int rows, cols;                  // of the operand from there on
+  int which, c0, c1, pad[3];       // product; chunks of k
+};
+
 template <int CG, int BN>
 struct Shape {
+  static constexpr int COLSW = BN / 4;            // columns of a result warp
+  static constexpr int ACCS = BN == 256 ? 2 : 4;  // accumulators in tensor memory
+  static constexpr int SLOTS = 4;                 // tiles whose parameters are at hand
   static constexpr int A_BYTES = 128 * ROW, B_BYTES = BN / CG * ROW, STAGE = A_BYTES + B_BYTES;
-  // after the stages: a tile's column parameters (two tiles'), partial sums' block, barriers
-  static constexpr int COLS = 2 * BN * 8, SUMS = EPI_WARPS * 32 * 4, BARS = 256;
+  // after the stages: the slots, each with {bias, w_scale}[BN] and x_scale[128]; partial sums; barriers
+  static constexpr int SLOT = sizeof(Slot) + (2 * BN + 128) * 4;
+  static constexpr int SUMS = EPI_WARPS * 32 * 4, BARS = 320;
   static constexpr int smem(int stages, bool turn) {
-    return 1024 + stages * STAGE + COLS + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
+    return 1024 + stages * STAGE + SLOTS * SLOT + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
   }
   static constexpr int stages(bool turn) {
     int n = STAGES_MAX;
@@ -46,12 +57,26 @@ struct Shape {
   }
 };
 
+// n / d for 0 <= n < 2^31 as a multiplication: with s = ceil(log2 d) and m = ceil(2^(31 + s) / d), n m /
+// 2^(31 + s) is above n / d by less than n / (d 2^31) < 1 / d.
+struct Divisor {
+  uint32_t mul;
+  int shift;
+  __device__ __forceinline__ int operator()(int n) const { return (int)((uint64_t)(uint32_t)n * mul >> shift); }
+};
+Divisor divisor(int64_t d) {
+  int s = 0;
+  while (((int64_t)1 << s) < d) ++s;
+  return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
+}
+
 // One product's part of a launch.
 struct Problem {
   Epilogue e;
   float* part;  // partial sums [splits][groups][m][ldp] instead of results, or null
   int64_t ldp;
-  int groups, m, n, tiles_m, tiles_n, units, splits, chunks, chunks_per_split;
+  int groups, m, n, tiles_m, tiles_n, tiles, units, splits, chunks, chunks_per_split;
+  Divisor by_split, by_group, by_panel, by_rest;  // splits, tiles, 8 tiles_n, rows of the last panel
   int a_bytes;               // of A's box per CTA and stage
   int az, bz;                // 0: one matrix for every group
   int a_mn, b_mn;            // rows run along m (n) instead of k
@@ -66,6 +91,32 @@ struct GemmParams {
   int units, stages;
   int* err;
 };
+
+// Bounded wait for a barrier's phase, as tc::mbar_wait, that leaves the issue slots to the result warps: a
+// try suspends the thread for up to 20 us.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* code,
+                                     int what) {
+  const auto attempt = [&] {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(20000u)
+        : "memory");
+    return ok != 0;
+  };
+  if (attempt()) return true;
+  for (const unsigned long long t0 = tc::globaltimer(); !attempt();) {
+    if (*abort_flag) return false;
+    if (tc::globaltimer() - t0 > tc::WAIT_NS) {
+      *abort_flag = 1;
+      *code = what;
+      return false;
+    }
+  }
+  return true;
+}
 
 template <int CG>
 __device__ __forceinline__ void load3(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y,
@@ -124,18 +175,22 @@ __device__ __forceinline__ void ld_v8(const void* p, uint32_t* r) {
                : "memory");
 }
 
-// 16 elements of this lane's row, from a column of a warp's 32 rows on: 32- or 16-byte accesses where the
-// rows' starts allow, else turned in shared memory so that the lanes run along a row. rows, cols: what there
-// is of the 32 and the 16.
+// 16 elements of this lane's row (two bf16 or one fp32 per word), from a column of a warp's 32 rows on: 32-
+// or 16-byte accesses where the rows' starts allow, else turned in shared memory so that the lanes run along
+// a row. rows, cols: what there is of the 32 and the 16.
+template <typename T>
+constexpr int WORDS = sizeof(T) * 4;
+template <typename T>
+__device__ __forceinline__ float element(const uint32_t* w, int e) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+  return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+}
 template <typename T>
 __device__ __forceinline__ void load_row(const T* base, int64_t ld, int rows, int cols, int align,
-                                         float* turn, float* v) {
+                                         float* turn, uint32_t* w) {
   const int lane = threadIdx.x & 31;
-  constexpr int W = sizeof(T) * 4;  // words of 16 elements: two bf16, or one fp32
+  constexpr int W = WORDS<T>;
   if (align && cols >= 16) {
-    uint32_t w[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = 0;
     if (lane < rows) {
       const char* p = reinterpret_cast<const char*>(base + lane * ld);
       if (align == 32) {
@@ -149,11 +204,6 @@ __device__ __forceinline__ void load_row(const T* base, int64_t ld, int rows, in
         }
       }
     }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      if constexpr (sizeof(T) == 4) v[e] = __uint_as_float(w[e]);
-      else v[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
-    }
     return;
   }
   const int col = lane & 15;
@@ -163,13 +213,16 @@ __device__ __forceinline__ void load_row(const T* base, int64_t ld, int rows, in
     turn[r * 17 + col] = r < rows && col < cols ? to_f<T>(base[r * ld + col]) : 0.f;
   __syncwarp();
 #pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] = turn[lane * 17 + e];
+  for (int i = 0; i < W; ++i) {
+    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(turn[lane * 17 + i]);
+    else w[i] = tc::pack_bf16(turn[lane * 17 + 2 * i], turn[lane * 17 + 2 * i + 1]);
+  }
 }
 template <typename T>
 __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int cols, int align,
                                           float* turn, const float* v) {
   const int lane = threadIdx.x & 31;
-  constexpr int W = sizeof(T) * 4;
+  constexpr int W = WORDS<T>;
   if (align && cols >= 16) {
     if (lane >= rows) return;
     uint32_t w[W];
@@ -203,16 +256,17 @@ __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int col
 
 __device__ __forceinline__ int64_t ceil_div_d(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// A tile's place: groups outermost, then panels of 8 tile rows, along which neighbouring CTAs share
-// operands in L2.
+// A unit's place: which part of k of which tile; groups outermost, then panels of 8 tile rows, along which
+// neighbouring CTAs share operands in L2.
 struct Place {
-  int g, mt, nt;
+  int g, mt, nt, split;
 };
-__device__ __forceinline__ Place place(int t, int tiles_m, int tiles_n) {
-  const int per = tiles_m * tiles_n, g = t / per, r = t - g * per;
-  const int panel = r / (8 * tiles_n), first = panel * 8, w = min(8, tiles_m - first);
-  const int q = r - panel * 8 * tiles_n;
-  return {g, first + q % w, q / w};
+__device__ __forceinline__ Place place(const Problem& p, int unit) {
+  const int t = p.by_split(unit), g = p.by_group(t), r = t - g * p.tiles;
+  const int panel = p.by_panel(r), first = panel * 8, q = r - panel * 8 * p.tiles_n;
+  const bool whole = first + 8 <= p.tiles_m;
+  const int nt = whole ? q >> 3 : p.by_rest(q);
+  return {g, first + q - nt * (whole ? 8 : p.tiles_m - first), nt, unit - t * p.splits};
 }
 
 // T: the results' type; fp32 results are sums, in fp32 registers, of sums over SUM_CHUNKS chunks of k,
@@ -223,23 +277,23 @@ __global__ void __launch_bounds__(THREADS, 1)
     k_gemm_op(const __grid_constant__ GemmParams<FORWARD ? 1 : 2> prm) {
   using S = Shape<CG, BN>;
   constexpr bool SUMS = sizeof(T) == 4;
-  constexpr int BM = 128 * CG, QUART = BN / 4;      // columns of a result warp
-  constexpr int CW = QUART < 32 ? QUART : 32;       // columns at a time
+  constexpr int BM = 128 * CG, COLSW = S::COLSW, ACCS = S::ACCS, SLOTS = S::SLOTS;
+  constexpr int CW = COLSW < 32 ? COLSW : 32;       // a result warp's columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
   extern __shared__ uint8_t smem_raw[];
   const int stages = prm.stages;
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* after = smem_raw + (base - raw) + stages * S::STAGE;
-  float2* s_col = reinterpret_cast<float2*>(after);  // [2][BN] {w_scale, bias}
-  float* s_sum = reinterpret_cast<float*>(after + S::COLS);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(after + S::COLS + S::SUMS);
-  float* s_turn = reinterpret_cast<float*>(after + S::COLS + S::SUMS + S::BARS);
+  uint8_t* slots = smem_raw + (base - raw) + stages * S::STAGE;
+  float* s_sum = reinterpret_cast<float*>(slots + SLOTS * S::SLOT);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(slots + SLOTS * S::SLOT + S::SUMS);
+  float* s_turn = reinterpret_cast<float*>(slots + SLOTS * S::SLOT + S::SUMS + S::BARS);
   const uint32_t bFull = tc::smem_u32(bars), bEmpty = bFull + 8 * STAGES_MAX;
-  const uint32_t bAcc = bEmpty + 8 * STAGES_MAX, bFree = bAcc + 16;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + 24);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 25);
-  int* code = reinterpret_cast<int*>(bars + 26);
-  static_assert(2 * STAGES_MAX + 4 <= 24, "barriers");
+  const uint32_t bAcc = bEmpty + 8 * STAGES_MAX, bFree = bAcc + 8 * ACCS;
+  const uint32_t bSlot = bFree + 8 * ACCS, bRead = bSlot + 8 * SLOTS;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + 33);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 34);
+  int* code = reinterpret_cast<int*>(bars + 35);
+  static_assert(2 * STAGES_MAX + 2 * ACCS + 2 * SLOTS <= 33, "barriers");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? tc::cluster_ctarank() : 0;
@@ -248,9 +302,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       tc::mbar_init(bFull + 8 * s, 2);  // A's and B's issuers
       tc::mbar_init(bEmpty + 8 * s, 1);
     }
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < ACCS; ++r) {
       tc::mbar_init(bAcc + 8 * r, 1);
       tc::mbar_init(bFree + 8 * r, EPI_WARPS * CG);
+    }
+    for (int r = 0; r < SLOTS; ++r) {
+      tc::mbar_init(bSlot + 8 * r, 1);
+      tc::mbar_init(bRead + 8 * r, EPI_WARPS);
     }
     *abort_flag = 0;
     *code = 0;
@@ -261,12 +319,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     if constexpr (CG == 2) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                        tc::smem_u32((const void*)tmem_slot)),
-                   "n"(2 * BN));
+                   "n"(ACCS * BN));
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     } else {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                        tc::smem_u32((const void*)tmem_slot)),
-                   "n"(2 * BN));
+                   "n"(ACCS * BN));
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
   }
@@ -279,14 +337,27 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t lFree = CG == 2 ? tc::mapa_shared(bFree, 0) : bFree;
   const int first = CG == 2 ? (int)tc::cluster_id_x() : (int)blockIdx.x;
   const int step = CG == 2 ? (int)tc::nclusters_x() : (int)gridDim.x;
-  // a unit's product, its number there, and its chunks of k
-  auto problem_of = [&](int& unit) -> int {
-    if (FORWARD || unit < prm.p[0].units) return 0;
-    unit -= prm.p[0].units;
-    return FORWARD ? 0 : 1;
+  // The place of the warp's i-th unit: its lanes work out 32 units' places at a time.
+  Place ahead{};
+  auto unit_place = [&](int i) {
+    if ((i & 31) == 0) {
+      int unit = min(first + (i + lane) * step, prm.units - 1);
+      const int which = !FORWARD && unit >= prm.p[0].units;
+      if (which) unit -= prm.p[0].units;
+      ahead = place(prm.p[which], unit);
+      ahead.g |= which << 30;
+    }
+    const int from = i & 31;
+    Place r{__shfl_sync(0xffffffffu, ahead.g, from), __shfl_sync(0xffffffffu, ahead.mt, from),
+            __shfl_sync(0xffffffffu, ahead.nt, from), __shfl_sync(0xffffffffu, ahead.split, from)};
+    return r;
   };
-  auto chunk_range = [&](const Problem& p, int unit, int& c0, int& c1) {
-    c0 = unit % p.splits * p.chunks_per_split;
+  auto problem_of = [&](const Place& pl) -> const Problem& {
+    return prm.p[FORWARD ? 0 : pl.g >> 30];
+  };
+  const int my_units = first < prm.units ? (prm.units - first + step - 1) / step : 0;
+  auto chunk_range = [&](const Problem& p, int split, int& c0, int& c1) {
+    c0 = split * p.chunks_per_split;
     c1 = min(p.chunks, c0 + p.chunks_per_split);
   };
   pdl_wait();
@@ -298,20 +369,19 @@ __global__ void __launch_bounds__(THREADS, 1)
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int all = first; all < prm.units && ok; all += step) {
-      int unit = all;
-      const int which = problem_of(unit);
-      const Problem& p = prm.p[which];
+    for (int i = 0; i < my_units && ok; ++i) {
+      const Place pl = unit_place(i);
+      const Problem& p = problem_of(pl);
+      const int which = FORWARD ? 0 : pl.g >> 30;
       const CUtensorMap* map = is_a ? &prm.a[which] : &prm.b[which];
       const bool mn = !FORWARD && (is_a ? p.a_mn : p.b_mn), blocked = is_a ? p.a_blocked : p.b_blocked;
       const uint32_t bytes = is_a && !mn ? (uint32_t)p.a_bytes : (uint32_t)(rows * ROW);
-      const Place pl = place(unit / p.splits, p.tiles_m, p.tiles_n);
       const int at = is_a ? pl.mt * BM + (int)rank * 128 : pl.nt * BN + (int)rank * (BN / CG);
-      const int z = pl.g * (is_a ? p.az : p.bz);
+      const int z = (pl.g & 0x3FFFFFFF) * (is_a ? p.az : p.bz);
       int c0, c1;
-      chunk_range(p, unit, c0, c1);
+      chunk_range(p, pl.split, c0, c1);
       for (int kc = c0; kc < c1; ++kc) {
-        if (!tc::mbar_wait(bEmpty + 8 * stage, phase ^ 1u, abort_flag, code, 1)) {
+        if (!wait(bEmpty + 8 * stage, phase ^ 1u, abort_flag, code, 1)) {
           ok = false;
           break;
         }
@@ -325,8 +395,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           } else if (blocked) {
             load4<CG>(dst, map, full, 0, kc * KE, at >> 6, z);
           } else {
-            for (int i = 0; i < rows / 64; ++i)
-              load3<CG>(dst + i * MN_BOX, map, full, at + 64 * i, kc * KE, z);
+            for (int h = 0; h < rows / 64; ++h)
+              load3<CG>(dst + h * MN_BOX, map, full, at + 64 * h, kc * KE, z);
           }
         }
         if (++stage == stages) {
@@ -347,25 +417,26 @@ __global__ void __launch_bounds__(THREADS, 1)
       int stage = 0, sums = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int all = first; all < prm.units && ok; all += step) {
-        int unit = all;
-        const Problem& p = prm.p[problem_of(unit)];
+      for (int i = 0; i < my_units && ok; ++i) {
+        const Place pl = unit_place(i);
+        const Problem& p = problem_of(pl);
         const int a_mn = FORWARD ? 0 : p.a_mn, b_mn = FORWARD ? 0 : p.b_mn;
         const uint32_t id = idesc<TYPE>(BM, BN, a_mn, b_mn);
         // a step further along k, in 16-byte units: 32 bytes of a row, or 16 rows of 128 bytes
         const uint32_t ia = a_mn ? 128 : 2, ib = b_mn ? 128 : 2;
         int c0, c1;
-        chunk_range(p, unit, c0, c1);
+        chunk_range(p, pl.split, c0, c1);
         for (int kc = c0; kc < c1 && ok;) {
-          const int end = SUMS ? min(c1, kc + SUM_CHUNKS) : c1, r = sums & 1;
-          if (sums >= 2 && !tc::mbar_wait(bFree + 8 * r, (uint32_t)(sums / 2 - 1) & 1, abort_flag, code, 2)) {
+          const int end = SUMS ? min(c1, kc + SUM_CHUNKS) : c1, r = sums % ACCS;
+          if (sums >= ACCS &&
+              !wait(bFree + 8 * r, (uint32_t)(sums / ACCS - 1) & 1, abort_flag, code, 2)) {
             ok = false;
             break;
           }
           tc::tc_fence_after();
           const uint32_t d = tmem + (uint32_t)(r * BN);
           for (uint32_t acc = 0; kc < end; ++kc) {
-            if (!tc::mbar_wait(bFull + 8 * stage, phase, abort_flag, code, 3)) {
+            if (!wait(bFull + 8 * stage, phase, abort_flag, code, 3)) {
               ok = false;
               break;
             }
@@ -375,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             const uint64_t dB = b_mn ? tc::sw128_mn_desc(sB, MN_BOX) : tc::sw128_desc(sB);
             if (elected) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) mma<TYPE, CG>(d, dA + i * ia, dB + i * ib, id, acc | (uint32_t)i);
+              for (int j = 0; j < 4; ++j) mma<TYPE, CG>(d, dA + j * ia, dB + j * ib, id, acc | (uint32_t)j);
               commit<CG>(bEmpty + 8 * stage);
             }
             acc = 1;
@@ -390,9 +461,64 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
       }
     }
-  } else if (warp >= FIRST_EPI) {
+  } else if (warp == 3) {
+    // ============ the tiles' parameters, as far ahead as there are slots ============
+    bool ok = true;
+    for (int i = 0; i < my_units && ok; ++i) {
+      const Place pl = unit_place(i);
+      const Problem& p = problem_of(pl);
+      const Epilogue& e = p.e;
+      const int64_t g = pl.g & 0x3FFFFFFF;
+      const int row0 = pl.mt * BM + (int)rank * 128, n0 = pl.nt * BN;
+      int c0, c1;
+      chunk_range(p, pl.split, c0, c1);
+      float bias[BN / 32], ws[BN / 32], xs[4];
+      if (FORWARD && !p.part) {
+#pragma unroll
+        for (int j = 0; j < BN / 32; ++j) {
+          const int n = n0 + j * 32 + lane;
+          bias[j] = e.bias.data && n < p.n ? __ldg(e.bias.data + g * e.bias.group + n) : 0.f;
+          if (TYPE == LIPZ_E4M3) ws[j] = n < p.n ? __ldg(e.w_scale.data + g * e.w_scale.group + n) : 1.f;
+        }
+        if (TYPE == LIPZ_E4M3) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int m = row0 + j * 32 + lane;
+            xs[j] = m < p.m ? __ldg(e.x_scale.data + g * e.x_scale.group + m) : 1.f;
+          }
+        }
+      }
+      const int r = i % SLOTS;
+      if (i >= SLOTS && !wait(bRead + 8 * r, (uint32_t)(i / SLOTS - 1) & 1, abort_flag, code, 5)) {
+        ok = false;
+        break;
+      }
+      uint8_t* slot = slots + r * S::SLOT;
+      if (lane == 0)
+        *reinterpret_cast<Slot*>(slot) =
+            Slot{g * e.y.group + (int64_t)row0 * e.y.row + n0,
+                 g * e.residual.group + (int64_t)row0 * e.residual.row + n0,
+                 g * e.pre.group + (int64_t)row0 * e.pre.row + n0,
+                 (((int64_t)pl.split * p.groups + g) * p.m + row0) * p.ldp + n0, p.m - row0, p.n - n0,
+                 FORWARD ? 0 : pl.g >> 30, c0, c1};
+      if (FORWARD && !p.part) {
+        float* f = reinterpret_cast<float*>(slot + sizeof(Slot));
+#pragma unroll
+        for (int j = 0; j < BN / 32; ++j) {
+          f[j * 32 + lane] = bias[j];
+          if (TYPE == LIPZ_E4M3) f[BN + j * 32 + lane] = ws[j];
+        }
+        if (TYPE == LIPZ_E4M3) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[2 * BN + j * 32 + lane] = xs[j];
+        }
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bSlot + 8 * r);
+    }
+  } else {
     // ============ results: a warp has 32 rows and a quarter of the tile's columns ============
-    const int ew = warp - FIRST_EPI, q = warp & 3, quarter = ew >> 2, et = threadIdx.x - 32 * FIRST_EPI;
+    const int ew = warp - FIRST_EPI, q = warp & 3, col0 = (ew >> 2) * COLSW;
     float* turn = s_turn + ew * (TURN / 4);
     auto barrier = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory"); };
     if (!FORWARD && prm.sums.part) {
@@ -418,108 +544,94 @@ __global__ void __launch_bounds__(THREADS, 1)
         barrier();
       }
     }
-    int sums = 0, tile = 0;
+    int sums = 0;
     bool ok = true;
     auto wait_sum = [&]() {
-      ok = tc::mbar_wait_warp(bAcc + 8 * (sums & 1), (uint32_t)(sums >> 1) & 1, abort_flag, code, 4);
+      ok = __all_sync(0xffffffffu, wait(bAcc + 8 * (sums % ACCS), (uint32_t)(sums / ACCS) & 1, abort_flag, code, 4));
       tc::tc_fence_after();
-      return tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)((sums & 1) * BN + quarter * QUART);
+      return tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(sums % ACCS * BN + col0);
     };
     auto free_sum = [&]() {
       tc::tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        if constexpr (CG == 2) tc::mbar_arrive_remote(lFree + 8 * (sums & 1));
-        else tc::mbar_arrive(bFree + 8 * (sums & 1));
+        if constexpr (CG == 2) tc::mbar_arrive_remote(lFree + 8 * (sums % ACCS));
+        else tc::mbar_arrive(bFree + 8 * (sums % ACCS));
       }
       ++sums;
     };
-    // the next tile's column parameters (thread et: column et) and this lane's x_scale, loaded a tile ahead
-    float2 next_col = make_float2(1.f, 0.f);
-    float next_xs = 1.f;
-    auto prefetch = [&](int unit) {
-      if (!FORWARD || unit >= prm.units) return;
-      const Problem& p = prm.p[0];
-      const Place pl = place(unit / p.splits, p.tiles_m, p.tiles_n);
-      const int n = pl.nt * BN + et, m = pl.mt * BM + (int)rank * 128 + q * 32 + lane;
-      const int64_t g = pl.g;
-      if (et < BN && n < p.n) {
-        if (TYPE == LIPZ_E4M3) next_col.x = __ldg(p.e.w_scale.data + g * p.e.w_scale.group + n);
-        if (p.e.bias.data) next_col.y = __ldg(p.e.bias.data + g * p.e.bias.group + n);
-      }
-      if (TYPE == LIPZ_E4M3 && m < p.m) next_xs = __ldg(p.e.x_scale.data + g * p.e.x_scale.group + m);
-    };
-    if (FORWARD && !prm.p[0].part) prefetch(first);
-    for (int all = first; all < prm.units; all += step, ++tile) {
-      int unit = all;
-      const Problem& p = prm.p[problem_of(unit)];
+    for (int i = 0; i < my_units; ++i) {
+      const int r = i % SLOTS;
+      ok = __all_sync(0xffffffffu, wait(bSlot + 8 * r, (uint32_t)(i / SLOTS) & 1, abort_flag, code, 6));
+      if (!ok) break;
+      const uint8_t* slot = slots + r * S::SLOT;
+      const Slot sl = *reinterpret_cast<const Slot*>(slot);
+      const float* col = reinterpret_cast<const float*>(slot + sizeof(Slot)) + col0;
+      const Problem& p = prm.p[FORWARD ? 0 : sl.which];
       const Epilogue& e = p.e;
-      const Place pl = place(unit / p.splits, p.tiles_m, p.tiles_n);
-      const int row0 = pl.mt * BM + (int)rank * 128 + q * 32, rows = p.m - row0;
-      const int64_t g = pl.g;
-      int c0, c1;
-      chunk_range(p, unit, c0, c1);
-      float2* col = s_col + (tile & 1) * BN;
-      float xs = 1.f;
-      if (FORWARD && !p.part) {
-        xs = next_xs;
-        if (et < BN) col[et] = next_col;
-        barrier();
-        prefetch(all + step);
-      }
-      if (!ok) continue;  // (a warp that gave up still comes to the others' barrier)
-      // CW results of this lane's row, from column c of the warp's quarter; v: the residual
-      auto columns_left = [&](int c) { return p.n - (pl.nt * BN + quarter * QUART + c); };
-      auto residual = [&](float (&v)[CW], int c) {
-        if (!FORWARD || p.part || !e.residual.data || rows <= 0) return;
-        const int64_t o = g * e.residual.group + (int64_t)row0 * e.residual.row + pl.nt * BN + quarter * QUART + c;
+      const int rows = sl.rows - q * 32;
+      const float xs = TYPE == LIPZ_E4M3 && FORWARD && !p.part ? col[2 * BN - col0 + q * 32 + lane] : 1.f;
+      // CW results of this lane's row, from column c of the warp's; v: the residual
+      auto columns_left = [&](int c) { return sl.cols - (col0 + c); };
+      constexpr int VW = CW / 16 * WORDS<T>;
+      const bool has_res = FORWARD && !p.part && e.residual.data && rows > 0;
+      auto residual = [&](uint32_t (&v)[VW], int c) {
+        if (!has_res) return;
+        const T* src = (const T*)e.residual.data + sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
 #pragma unroll
         for (int h = 0; h < CW; h += 16)
           if (columns_left(c + h) > 0)
-            load_row<T>((const T*)e.residual.data + o + h, e.residual.row, rows, columns_left(c + h),
-                        p.res_align, turn, v + h);
+            load_row<T>(src + h, e.residual.row, rows, columns_left(c + h), p.res_align, turn,
+                        v + h / 16 * WORDS<T>);
       };
-      auto results = [&](float (&u)[CW], const float (&v)[CW], int c) {
+      auto results = [&](float (&u)[CW], const uint32_t (&v)[VW], int c) {
         if (rows <= 0 || columns_left(c) <= 0) return;
-        const int n0 = pl.nt * BN + quarter * QUART + c;
         if (p.part) {
-          const int64_t o = ((int64_t)(unit % p.splits) * p.groups + g) * p.m + row0;
+          float* dst = p.part + sl.part + (int64_t)(q * 32) * p.ldp + col0 + c;
 #pragma unroll
           for (int h = 0; h < CW; h += 16)
             if (columns_left(c + h) > 0)
               // (ldp is a multiple of 16: whole vectors)
-              store_row<float>(p.part + o * p.ldp + n0 + h, p.ldp, rows, 16, 32, turn, u + h);
+              store_row<float>(dst + h, p.ldp, rows, 16, 32, turn, u + h);
           return;
         }
         if constexpr (FORWARD) {
-          const float2* cc = col + quarter * QUART + c;
 #pragma unroll
-          for (int i = 0; i < CW; ++i) {
-            if (TYPE == LIPZ_E4M3) u[i] = fmaf(u[i], xs * cc[i].x, cc[i].y);
-            else u[i] += cc[i].y;
+          for (int i = 0; i < CW; i += 4) {
+            const float4 b4 = *reinterpret_cast<const float4*>(col + c + i);
+            uint64_t lo = pack2(u[i], u[i + 1]), hi = pack2(u[i + 2], u[i + 3]);
+            if (TYPE == LIPZ_E4M3) {
+              const float4 w4 = *reinterpret_cast<const float4*>(col + BN + c + i);
+              lo = fma2(mul2(lo, both(xs)), pack2(w4.x, w4.y), pack2(b4.x, b4.y));
+              hi = fma2(mul2(hi, both(xs)), pack2(w4.z, w4.w), pack2(b4.z, b4.w));
+            } else {
+              lo = add2(lo, pack2(b4.x, b4.y));
+              hi = add2(hi, pack2(b4.z, b4.w));
+            }
+            const float2 l = unpack2(lo), h = unpack2(hi);
+            u[i] = l.x, u[i + 1] = l.y, u[i + 2] = h.x, u[i + 3] = h.y;
           }
           if (e.pre.data) {
-            const int64_t o = g * e.pre.group + (int64_t)row0 * e.pre.row + n0;
+            bf16* dst = (bf16*)e.pre.data + sl.pre + (int64_t)(q * 32) * e.pre.row + col0 + c;
 #pragma unroll
             for (int h = 0; h < CW; h += 16)
               if (columns_left(c + h) > 0)
-                store_row<bf16>((bf16*)e.pre.data + o + h, e.pre.row, rows, columns_left(c + h),
-                                p.pre_align, turn, u + h);
+                store_row<bf16>(dst + h, e.pre.row, rows, columns_left(c + h), p.pre_align, turn, u + h);
           }
           with_act(e.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < CW; i += 2) act_pair<decltype(act)::value>(u[i], u[i + 1], e.slope);
+            for (int i = 0; i < CW; i += 2) act_pair<decltype(act)::value, SUMS>(u[i], u[i + 1], e.slope);
           });
-          if (e.residual.data) {
+          if (has_res) {
 #pragma unroll
-            for (int i = 0; i < CW; ++i) u[i] += v[i];
+            for (int i = 0; i < CW; ++i) u[i] += element<T>(v + i / 16 * WORDS<T>, i % 16);
           }
         }
-        const int64_t o = g * e.y.group + (int64_t)row0 * e.y.row + n0;
+        T* dst = (T*)e.y.data + sl.y + (int64_t)(q * 32) * e.y.row + col0 + c;
 #pragma unroll
         for (int h = 0; h < CW; h += 16)
           if (columns_left(c + h) > 0)
-            store_row<T>((T*)e.y.data + o + h, e.y.row, rows, columns_left(c + h), p.y_align, turn, u + h);
+            store_row<T>(dst + h, e.y.row, rows, columns_left(c + h), p.y_align, turn, u + h);
       };
       auto tmem_load = [&](uint32_t t, float (&u)[CW]) {
         uint32_t r[CW];
@@ -529,12 +641,13 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
         for (int i = 0; i < CW; ++i) u[i] = __uint_as_float(r[i]);
       };
+      uint32_t v[VW];
       if constexpr (SUMS) {
-        static_assert(QUART == CW, "the sums of a warp's columns stand in registers");
-        float acc[CW], v[CW];
+        static_assert(COLSW == CW, "the sums of a warp's columns stand in registers");
+        float acc[CW];
 #pragma unroll
         for (int i = 0; i < CW; ++i) acc[i] = 0.f;
-        for (int kc = c0; kc < c1; kc += SUM_CHUNKS) {
+        for (int kc = sl.c0; kc < sl.c1; kc += SUM_CHUNKS) {
           const uint32_t t = wait_sum();
           if (!ok) break;
           float u[CW];
@@ -543,23 +656,27 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int i = 0; i < CW; ++i) acc[i] += u[i];
         }
-        if (!ok) continue;
+        if (!ok) break;
         residual(v, 0);
         results(acc, v, 0);
       } else {
-        float v[CW];
         residual(v, 0);
         const uint32_t t = wait_sum();
-        if (!ok) continue;
+        if (!ok) break;
 #pragma unroll 1
-        for (int c = 0; c < QUART; c += CW) {
+        for (int c = 0; c < COLSW; c += CW) {
           float u[CW];
-          if (c) residual(v, c);
           tmem_load(t + c, u);
-          if (c + CW == QUART) free_sum();
-          results(u, v, c);
+          if (c + CW == COLSW) free_sum();
+          uint32_t cur[VW];
+#pragma unroll
+          for (int i = 0; i < VW; ++i) cur[i] = v[i];
+          if (c + CW < COLSW) residual(v, c + CW);
+          results(u, cur, c);
         }
       }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bRead + 8 * r);
     }
   }
   tc::tc_fence_before();
@@ -568,9 +685,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   tc::tc_fence_after();
   if (warp == 2) {
     if constexpr (CG == 2)
-      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * BN));
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(ACCS * BN));
     else
-      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * BN));
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(ACCS * BN));
   }
   if (threadIdx.x == 0 && *code && prm.err) *reinterpret_cast<volatile int*>(prm.err) = *code;
 }
@@ -788,7 +905,10 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
     p.groups = (int)g.groups, p.m = (int)g.m, p.n = (int)g.n;
     p.tiles_m = (int)o.tiles_m, p.tiles_n = (int)o.tiles_n;
     p.splits = o.splits;
-    p.units = (int)(o.tiles_m * o.tiles_n * g.groups * o.splits);
+    p.tiles = (int)(o.tiles_m * o.tiles_n);
+    p.units = (int)(p.tiles * g.groups * o.splits);
+    p.by_split = divisor(o.splits), p.by_group = divisor(p.tiles);
+    p.by_panel = divisor(8 * o.tiles_n), p.by_rest = divisor(o.tiles_m % 8 ? o.tiles_m % 8 : 8);
     p.chunks = (int)o.chunks, p.chunks_per_split = (int)o.chunks_per_split;
     p.a_bytes = arows * ROW;
     p.az = g.groups > 1 && g.a.group != 0, p.bz = g.groups > 1 && g.b.group != 0;
@@ -878,7 +998,7 @@ GemmPlan plan_products(const Products& q) {
         top = unit_t > top ? unit_t : top;
         if (o.splits > 1) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 4000, split = true;
       }
-      if (!fits || (s0 > 1 && !split)) continue;
+      if ((!fits && !force_cg) || (s0 > 1 && !split)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 1 : (double)(int64_t)(waves + 0.999);
       const double time = waves * top + c.epi + 2000 + extra + (split ? 5000 : 0);

@@ -193,8 +193,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 __device__ __forceinline__ uint64_t both(float a) { return pack2(a, a); }
 
-// act_value of two values, in place: the same operations in the same order.
-template <int ACT>
+// act_value of two values, in place. Without EXACT the result is good to 2^-16, for results that are then
+// rounded to bf16: tanh takes x - x^3/3 below 1/64, where its other form has lost 2^-17.
+template <int ACT, bool EXACT>
 __device__ __forceinline__ void act_pair(float& a, float& b, float slope) {
   if constexpr (ACT == LIPZ_ACT_TANH || ACT == LIPZ_ACT_GELU || ACT == LIPZ_ACT_SILU) {
     const uint64_t u = pack2(a, b), one = both(1.f);
@@ -204,12 +205,16 @@ __device__ __forceinline__ void act_pair(float& a, float& b, float slope) {
       const float2 arg = unpack2(mul2(m, both(2.f * LOG2E)));
       const float2 y = unpack2(add2(pack2(ex2_approx(arg.x), ex2_approx(arg.y)), one));
       const float2 t = unpack2(fma2(both(-2.f), pack2(rcp_approx(y.x), rcp_approx(y.y)), one));
-      uint64_t q = fma2(m2, both(0.021869488536155203f), both(-0.053968253968253971f));
-      q = fma2(m2, q, both(0.13333333333333333f));
-      q = fma2(m2, q, both(-0.33333333333333333f));
+      uint64_t q = both(-0.33333333333333333f);
+      if constexpr (EXACT) {
+        q = fma2(m2, both(0.021869488536155203f), both(-0.053968253968253971f));
+        q = fma2(m2, q, both(0.13333333333333333f));
+        q = fma2(m2, q, both(-0.33333333333333333f));
+      }
       const float2 s = unpack2(mul2(m, fma2(m2, q, one)));
-      a = copysignf(aa < 0.25f ? s.x : t.x, a);
-      b = copysignf(ab < 0.25f ? s.y : t.y, b);
+      constexpr float small = EXACT ? 0.25f : 0.015625f;
+      a = copysignf(aa < small ? s.x : t.x, a);
+      b = copysignf(ab < small ? s.y : t.y, b);
     } else {
       uint64_t v = u;
       if constexpr (ACT == LIPZ_ACT_GELU) v = mul2(u, fma2(both(GELU_3), mul2(u, u), both(GELU_1)));
