@@ -35,20 +35,23 @@ constexpr int SMEM_MAX = 232448, STAGES_MAX = 8;
 struct Slot {
   int64_t y, residual, pre, part;  // element offsets of the CTA's first row and the tile's first column
   int rows, cols;                  // of the operand from there on
-  int which, c0, c1, pad[3];       // product; chunks of k
+  int which, c0, c1;               // product; chunks of k
+  int g, m, n;                     // group, first row and column
 };
 
-template <int CG, int BN>
+// VIA: a tile's residual and results pass through shared memory, by TMA.
+template <int CG, int BN, bool VIA>
 struct Shape {
   static constexpr int COLSW = BN / 4;            // columns of a result warp
   static constexpr int ACCS = BN == 256 ? 2 : 4;  // accumulators in tensor memory
-  static constexpr int SLOTS = 4;                 // tiles whose parameters are at hand
+  static constexpr int SLOTS = VIA ? 3 : 4;  // tiles whose parameters (and residual) are at hand
+  static constexpr int TILE = VIA ? 128 * BN * 2 : 0;
   static constexpr int A_BYTES = 128 * ROW, B_BYTES = BN / CG * ROW, STAGE = A_BYTES + B_BYTES;
   // after the stages: the slots, each with {bias, w_scale}[BN] and x_scale[128]; partial sums; barriers
   static constexpr int SLOT = sizeof(Slot) + (2 * BN + 128) * 4;
   static constexpr int SUMS = EPI_WARPS * 32 * 4, BARS = 320;
   static constexpr int smem(int stages, bool turn) {
-    return 1024 + stages * STAGE + SLOTS * SLOT + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
+    return 1024 + stages * STAGE + SLOTS * (TILE + SLOT) + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
   }
   static constexpr int stages(bool turn) {
     int n = STAGES_MAX;
@@ -81,11 +84,13 @@ struct Problem {
   int az, bz;                // 0: one matrix for every group
   int a_mn, b_mn;            // rows run along m (n) instead of k
   int a_blocked, b_blocked;  // a 4-D map brings the 64-wide boxes of a stage together
+  int rz;                    // VIA: 0: one residual for every group
   int y_align, res_align, pre_align;  // 32, 16, or 0: bytes that divide every row's start
 };
 template <int NP>
 struct GemmParams {
   CUtensorMap a[NP], b[NP];
+  CUtensorMap residual, y;  // VIA: boxes of 32 columns by 128 and 32 rows
   Problem p[NP];
   PartSums sums;
   int units, stages;
@@ -272,18 +277,22 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
 // T: the results' type; fp32 results are sums, in fp32 registers, of sums over SUM_CHUNKS chunks of k,
 // because the tensor cores' additions truncate. FORWARD: K-major operands and the forward's epilogue, one
 // product; else up to two plain products.
-template <int TYPE, int CG, int BN, bool FORWARD, typename T>
+// VIA: with row-per-lane accesses a tile's results cost 12 us and its residual 25 to 39 us at 144 x 512 x 256
+// -> 768 (of 47 and 88 us in all).
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA>
 __global__ void __launch_bounds__(THREADS, 1)
     k_gemm_op(const __grid_constant__ GemmParams<FORWARD ? 1 : 2> prm) {
-  using S = Shape<CG, BN>;
+  using S = Shape<CG, BN, VIA>;
   constexpr bool SUMS = sizeof(T) == 4;
+  static_assert(!VIA || (FORWARD && !SUMS && S::COLSW == 32), "boxes of 32 bf16 columns");
   constexpr int BM = 128 * CG, COLSW = S::COLSW, ACCS = S::ACCS, SLOTS = S::SLOTS;
   constexpr int CW = COLSW < 32 ? COLSW : 32;       // a result warp's columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
   extern __shared__ uint8_t smem_raw[];
   const int stages = prm.stages;
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* slots = smem_raw + (base - raw) + stages * S::STAGE;
+  uint8_t* tiles = smem_raw + (base - raw) + stages * S::STAGE;  // [SLOTS][BN / 32][128 rows][64 bytes]
+  uint8_t* slots = tiles + SLOTS * S::TILE;
   float* s_sum = reinterpret_cast<float*>(slots + SLOTS * S::SLOT);
   uint64_t* bars = reinterpret_cast<uint64_t*>(slots + SLOTS * S::SLOT + S::SUMS);
   float* s_turn = reinterpret_cast<float*>(slots + SLOTS * S::SLOT + S::SUMS + S::BARS);
@@ -500,7 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                  g * e.residual.group + (int64_t)row0 * e.residual.row + n0,
                  g * e.pre.group + (int64_t)row0 * e.pre.row + n0,
                  (((int64_t)pl.split * p.groups + g) * p.m + row0) * p.ldp + n0, p.m - row0, p.n - n0,
-                 FORWARD ? 0 : pl.g >> 30, c0, c1};
+                 FORWARD ? 0 : pl.g >> 30, c0, c1, (int)g, row0, n0};
       if (FORWARD && !p.part) {
         float* f = reinterpret_cast<float*>(slot + sizeof(Slot));
 #pragma unroll
@@ -514,7 +523,23 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
       }
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bSlot + 8 * r);
+      if (VIA && e.residual.data) {
+        if (lane == 0) {
+          const uint32_t bar = bSlot + 8 * r, dst = tc::smem_u32(tiles + r * S::TILE);
+          tc::mbar_expect_tx(bar, S::TILE);
+#pragma unroll
+          for (int j = 0; j < BN / 32; ++j)
+            tc::tma_load_3d(dst + j * (S::TILE / (BN / 32)), &prm.residual, bar, n0 + j * 32, row0,
+                            (int)g * p.rz);
+        }
+      } else if (lane == 0) {
+        tc::mbar_arrive(bSlot + 8 * r);
+      }
+    }
+    if (!ok) {  // loads in flight land before the CTA leaves
+      const unsigned long long t0 = tc::globaltimer();
+      while (tc::globaltimer() - t0 < 200000ull) {
+      }
     }
   } else {
     // ============ results: a warp has 32 rows and a quarter of the tile's columns ============
@@ -575,8 +600,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       auto columns_left = [&](int c) { return sl.cols - (col0 + c); };
       constexpr int VW = CW / 16 * WORDS<T>;
       const bool has_res = FORWARD && !p.part && e.residual.data && rows > 0;
+      // VIA: this lane's 64 bytes of the warp's 32 rows, 16-byte units in the 64-byte swizzle
+      uint8_t* mine = tiles + r * S::TILE + (ew >> 2) * (S::TILE / (BN / 32)) + q * 2048 + lane * 64;
+      const int swizzle = lane >> 1 & 3;
       auto residual = [&](uint32_t (&v)[VW], int c) {
-        if (!has_res) return;
+        if (VIA || !has_res) return;
         const T* src = (const T*)e.residual.data + sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
 #pragma unroll
         for (int h = 0; h < CW; h += 16)
@@ -622,10 +650,31 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int i = 0; i < CW; i += 2) act_pair<decltype(act)::value, SUMS>(u[i], u[i + 1], e.slope);
           });
-          if (has_res) {
+          if (VIA && has_res) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint4 w = *reinterpret_cast<const uint4*>(mine + ((j ^ swizzle) << 4));
+              const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+              for (int i = 0; i < 8; ++i) u[j * 8 + i] += element<T>(ww, i);
+            }
+          } else if (has_res) {
 #pragma unroll
             for (int i = 0; i < CW; ++i) u[i] += element<T>(v + i / 16 * WORDS<T>, i % 16);
           }
+        }
+        if constexpr (VIA) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<uint4*>(mine + ((j ^ swizzle) << 4)) =
+                make_uint4(tc::pack_bf16(u[j * 8], u[j * 8 + 1]), tc::pack_bf16(u[j * 8 + 2], u[j * 8 + 3]),
+                           tc::pack_bf16(u[j * 8 + 4], u[j * 8 + 5]),
+                           tc::pack_bf16(u[j * 8 + 6], u[j * 8 + 7]));
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0)
+            tc::tma_store_3d(&prm.y, tc::smem_u32(mine), sl.n + col0, sl.m + q * 32, sl.g);
+          return;
         }
         T* dst = (T*)e.y.data + sl.y + (int64_t)(q * 32) * e.y.row + col0 + c;
 #pragma unroll
@@ -675,9 +724,20 @@ __global__ void __launch_bounds__(THREADS, 1)
           results(u, cur, c);
         }
       }
+      if (VIA) {
+        // a slot is free again when the stores of the warp's tile before this one have read it
+        if (lane == 0) {
+          tc::bulk_commit();
+          tc::bulk_wait_read<1>();
+          if (i) tc::mbar_arrive(bRead + 8 * ((i - 1) % SLOTS));
+        }
+        __syncwarp();
+        continue;
+      }
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bRead + 8 * r);
     }
+    if (VIA && lane == 0) tc::bulk_wait_all();
   }
   tc::tc_fence_before();
   if constexpr (CG == 2) tc::cluster_sync_all();
@@ -832,6 +892,21 @@ bool tma_takes(const Operand& o, const Extent& x, int64_t groups, int eb) {
   return groups == 1 || (o.group * eb % 16 == 0 && o.group * eb < (int64_t)1 << 40);
 }
 
+// The map of results or a residual, {n, m, groups}, in boxes of 32 bf16 columns.
+bool encode_tile(CUtensorMap* map, const lipz_mat& m, int64_t rows, int64_t cols, int64_t groups,
+                 int box_rows) {
+  const auto f = encoder();
+  if (!f) return false;
+  const cuuint64_t row = rows > 1 ? (cuuint64_t)m.row * 2 : (cuuint64_t)ceil_div(cols, 8) * 16;
+  const cuuint64_t depth = groups > 1 && m.group ? (cuuint64_t)groups : 1;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, depth};
+  const cuuint64_t strides[2] = {row, depth > 1 ? (cuuint64_t)m.group * 2 : row};
+  const cuuint32_t box[3] = {32, (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
+  return f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, m.data, dims, strides, box, es,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The map of an operand: {cols, rows, groups} in boxes of one 128-byte unit by box_rows rows; blocked:
 // {64, rows, cols / 64, groups} in boxes of 64 x 64 x blocks.
 bool encode(CUtensorMap* map, const Operand& o, const Extent& x, int64_t groups, int type, int box_rows,
@@ -879,10 +954,10 @@ cudaError_t prepare_kernel(K kernel, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <int TYPE, int CG, int BN, bool FORWARD, typename T>
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false>
 cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
                    cudaStream_t st) {
-  using S = Shape<CG, BN>;
+  using S = Shape<CG, BN, VIA>;
   GemmParams<FORWARD ? 1 : 2> k;
   memset(&k, 0, sizeof k);
   bool turn = false;
@@ -914,17 +989,23 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
     p.az = g.groups > 1 && g.a.group != 0, p.bz = g.groups > 1 && g.b.group != 0;
     auto align = [&](const lipz_mat& m) {
       const int a = !m.data ? 32 : rows_aligned(m, g.groups, g.m, 32) ? 32 : rows_aligned(m, g.groups, g.m, 16) ? 16 : 0;
-      turn = turn || (m.data && !p.part && (!a || g.n % 16));
+      turn = turn || (m.data && !p.part && (!a || g.n % 16) && (!VIA || m.data == g.e.pre.data));
       return a;
     };
     p.y_align = align(g.e.y), p.res_align = align(g.e.residual), p.pre_align = align(g.e.pre);
     k.units += p.units;
+    if (VIA) {
+      p.rz = g.groups > 1 && g.e.residual.group != 0;
+      if (!encode_tile(&k.y, g.e.y, g.m, g.n, g.groups, 32) ||
+          (g.e.residual.data && !encode_tile(&k.residual, g.e.residual, g.m, g.n, g.groups, 128)))
+        return cudaErrorInvalidValue;
+    }
   }
   if (sums) k.sums = *sums;
   k.err = timeout_word();
   k.stages = S::stages(turn);
   static std::atomic<uint64_t> done{0};
-  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T>;
+  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T, VIA>;
   cudaError_t e = prepare_kernel(kernel, done);
   if (e != cudaSuccess) return e;
   const int slots = sm_count() / CG, ctas = (k.units < slots ? k.units : slots) * CG;
@@ -945,6 +1026,14 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   return cudaLaunchKernelEx(&cfg, kernel, k);
 }
 
+// Whether TMA takes a forward's bf16 results and residual as they lie.
+bool results_by_tma(const Gemm& g) {
+  auto takes = [&](const lipz_mat& m) {
+    return !m.data || tma_takes({m.data, m.group, m.row, true}, {g.m, g.n}, g.groups, 2);
+  };
+  return g.e.y.type == LIPZ_BF16 && g.a.k_major && g.b.k_major && takes(g.e.y) && takes(g.e.residual);
+}
+
 template <int TYPE, bool FORWARD>
 cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* parts, const PartSums* sums,
                          cudaStream_t st) {
@@ -954,6 +1043,10 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
     return launch<TYPE, 1, 64, FORWARD, float>(q, p, parts, sums, st);
   }
   if (p.cg == 2 && p.bn == 256) return launch<TYPE, 2, 256, FORWARD, bf16>(q, p, parts, sums, st);
+  if constexpr (FORWARD) {
+    if (p.cg == 2 && !parts[0] && results_by_tma(q.g[0]))
+      return launch<TYPE, 2, 128, true, bf16, true>(q, p, parts, sums, st);
+  }
   if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, bf16>(q, p, parts, sums, st);
   if (p.bn == 128) return launch<TYPE, 1, 128, FORWARD, bf16>(q, p, parts, sums, st);
   return launch<TYPE, 1, 64, FORWARD, bf16>(q, p, parts, sums, st);
@@ -963,26 +1056,34 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
 
 GemmPlan plan_products(const Products& q) {
   GemmPlan plan{};
-  const int eb = type_bytes(q.g[0].type);
-  const bool sums = q.g[0].e.y.type == LIPZ_FP32;
-  // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its
-  // MMA steps (pairs of 256 x 256 run at the tensor cores' rate, narrower ones are bound by shared memory)
-  // or its epilogue, whichever is longer, and once the ring's and the epilogue's latency; parts of k cost
-  // another launch and their way through L2.
+  const Gemm& g0 = q.g[0];
+  const int eb = type_bytes(g0.type);
+  const bool sums = g0.e.y.type == LIPZ_FP32, res = g0.e.residual.data, heavy = g0.e.act >= LIPZ_ACT_TANH;
+  // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its MMA
+  // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost another launch and their
+  // way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 x 8192 in bf16 (8 bits: 184 instead
+  // of 158), epilogues at 144 x 512 x 256 -> 768 without an activation, what tanh adds, what a residual adds.
+  struct Shape {
+    int cg, bn;
+    double step, epi, act, residual;
+  };
+  static const Shape shapes[] = {{2, 256, 158, 9000, 2500, 5500}, {2, 128, 88, 3900, 800, 2600},
+                                 {1, 128, 108, 3900, 800, 2600}, {1, 64, 82, 2350, 250, 900}};
+  const Shape via{2, 128, 100, 3500, 400, 1000};  // shape 1 with its results through shared memory
+  const bool by_tma = results_by_tma(g0);
   const int sms = sm_count();
-  struct Config { int cg, bn; double step, epi; };
-  static const Config configs[] = {{2, 256, 128, 5000}, {2, 128, 86, 2600}, {1, 128, 86, 2600}, {1, 64, 60, 1400}};
   double best = -1;
   static const int force_cg = getenv("OPCG") ? atoi(getenv("OPCG")) : 0, force_bn = getenv("OPBN") ? atoi(getenv("OPBN")) : 0, force_s = getenv("OPS") ? atoi(getenv("OPS")) : 0;
-  for (const Config& c : configs) {
-    if (sums && c.bn > 128) continue;
-    if (force_cg && (c.cg != force_cg || c.bn != force_bn)) continue;
-    const int64_t slots = sms / c.cg;
+  for (const Shape& shape : shapes) {
+    if (sums && shape.bn > 128) continue;
+    if (force_cg && (shape.cg != force_cg || shape.bn != force_bn)) continue;
     for (int s0 = 1; s0 <= 64; s0 *= 2) {
       if (force_s && s0 != force_s) continue;
+      const Shape& c = by_tma && s0 == 1 && shape.cg == 2 && shape.bn == 128 ? via : shape;
+      const int64_t slots = sms / c.cg;
       GemmPlan t{};
       t.cg = c.cg, t.bn = c.bn;
-      double work = 0, top = 0, extra = 0;
+      double work = 0, top = 0, last = 0, extra = 0;
       bool fits = true, split = false;
       for (int i = 0; i < q.n; ++i) {
         const Gemm& g = q.g[i];
@@ -993,15 +1094,17 @@ GemmPlan plan_products(const Products& q) {
         o.chunks_per_split = ceil_div(o.chunks, want);
         o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);
         fits = fits && tiles * o.splits <= INT32_MAX / 2 && (o.splits == 1 || tiles * o.splits <= 2 * slots);
-        const double mma = o.chunks_per_split * 4 * c.step, unit_t = mma > c.epi ? mma : c.epi;
-        work += unit_t * tiles * o.splits;
-        top = unit_t > top ? unit_t : top;
-        if (o.splits > 1) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 4000, split = true;
+        const double mma = o.chunks_per_split * 4 * c.step * (eb == 1 ? 1.16 : 1);
+        const double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0), unit = mma > epi ? mma : epi;
+        work += unit * tiles * o.splits;
+        if (unit > top) top = unit;
+        if (mma + epi > last) last = mma + epi;
+        if (o.splits > 1) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000, split = true;
       }
       if ((!fits && !force_cg) || (s0 > 1 && !split)) continue;
       double waves = work / (slots * top);
-      waves = waves < 1 ? 1 : (double)(int64_t)(waves + 0.999);
-      const double time = waves * top + c.epi + 2000 + extra + (split ? 5000 : 0);
+      waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
+      const double time = waves * top + last + extra + (split ? 9500 : 0);
       if (best < 0 || time < best) best = time, plan = t;
     }
   }
