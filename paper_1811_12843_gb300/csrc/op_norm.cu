@@ -59,38 +59,39 @@ __device__ __forceinline__ int64_t group_of(const RowArgs& p, int64_t r) {
   return p.total == p.rows ? 0 : (uint32_t)r / (uint32_t)p.rows;
 }
 
-// A row's results from its sums {sum of squares, largest magnitude} and its elements (times the weights).
+// What a row's elements (times the weights) are multiplied by: f, and for 8 bits then by inv (one after the
+// other: their product may be infinite); else inv is 1. `first`: this thread writes rstd and scale.
+struct RowScale {
+  float f, inv;
+};
+template <bool QUANT>
+__device__ __forceinline__ RowScale row_scale(const RowArgs& p, int64_t g, int64_t gr, Sums red, bool first) {
+  RowScale s{1.f, 1.f};
+  if (!QUANT) {
+    s.f = rsqrtf(fmaf(red.ss, p.inv_dim, p.eps));
+    if (first && p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = s.f;
+  }
+  if (QUANT || p.scale.data) {
+    const float top = __uint_as_float(red.top) * s.f;
+    if (first) p.scale.data[g * p.scale.group + gr] = max_nan(top / E4M3_MAX, SCALE_MIN);
+    s.inv = min_nan(E4M3_MAX * rcp_approx(top), 1.f / SCALE_MIN);
+  }
+  return s;
+}
+
+// A row's results from its sums and its elements (times the weights).
 template <typename T, int E, int NV, bool QUANT>
 __device__ __forceinline__ void row_results(const RowArgs& p, int64_t g, int64_t gr, Sums red,
                                             float (&v)[NV][E], int t, int tpr, int nvec) {
-  float f = 1.f;
-  if (!QUANT) {
-    f = rsqrtf(fmaf(red.ss, p.inv_dim, p.eps));
-    if (t == 0 && p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = f;
-  }
-  if (QUANT || p.scale.data) {
-    const float top = __uint_as_float(red.top) * f;
-    if (t == 0) p.scale.data[g * p.scale.group + gr] = max_nan(top / E4M3_MAX, SCALE_MIN);
-    const float inv = min_nan(E4M3_MAX * rcp_approx(top), 1.f / SCALE_MIN);
-    // (f and inv one after the other: their product may be infinite)
-    e4m3* y = row_of<e4m3>(p.y, g, gr);
+  const RowScale f = row_scale<QUANT>(p, g, gr, red, t == 0);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (t + i * tpr < nvec) {
+  for (int i = 0; i < NV; ++i)
+    if (t + i * tpr < nvec) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f * inv;
-        store_e4m3<E>(y + (t + i * tpr) * E, v[i]);
-      }
-  } else {
-    T* y = row_of<T>(p.y, g, gr);
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (t + i * tpr < nvec) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] *= f;
-        store_vec<T, E>(y + (t + i * tpr) * E, v[i]);
-      }
-  }
+      for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f.f * f.inv;
+      if (QUANT || p.scale.data) store_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
+      else store_vec<T, E>(row_of<T>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
+    }
 }
 
 // The norm, or with QUANT only the rows' values to 8 bits.
@@ -327,6 +328,135 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
   ring_done(q, err);
 }
 
+// ---- rows that start off the 16-byte grid (odd widths), all of a call's matrices at the same place of a
+// 16-byte unit in each row: threads take the whole units that a row touches, and the first and the last of
+// them in part. Parameters stand in shared memory, one word in 33 left out, so that lanes E columns apart
+// meet different banks. (Element by element, 16385 x 4097 with residual to 8 bits took 262 us, and 332
+// backward.)
+__device__ __forceinline__ int padded(int c) { return c + (c >> 5); }
+
+// Element e of unit c is column c E - m + e; `whole`: all of the unit lies in the row.
+template <int E>
+struct Unit {
+  int col;
+  bool live, whole;
+  __device__ __forceinline__ Unit(int c, int m, int dim)
+      : col(c * E - m), live(c * E - m < dim), whole(c * E >= m && c * E - m + E <= dim) {}
+  __device__ __forceinline__ bool in(int e, int dim) const { return whole || (col + e >= 0 && col + e < dim); }
+};
+template <typename T, int E>
+__device__ __forceinline__ void store_unit(T* row, const Unit<E>& u, int dim, const float* v) {
+  if (u.whole) {
+    store_vec<T, E>(row + u.col, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (u.in(e, dim)) row[u.col + e] = from_f<T>(v[e]);
+  }
+}
+template <int E>
+__device__ __forceinline__ void store_unit_e4m3(e4m3* row, const Unit<E>& u, int dim, const float* v) {
+  if (u.whole) {
+    store_e4m3<E>(row + u.col, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (u.in(e, dim)) store_e4m3<1>(row + u.col + e, v + e);
+  }
+}
+
+template <typename T, int E, int NV, bool QUANT>
+__global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages, int slot, int* err) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Sums s_red[2][16];
+  const bool has_res = !QUANT && p.residual.data, one = p.total == p.rows || p.weight.group == 0;
+  const Ring q = ring_init(smem, stages, slot, has_res ? 2 : 1);
+  float* s_w = reinterpret_cast<float*>(smem + RING_BARS + stages * q.arrays * slot);
+  const int t = threadIdx.x, tpr = blockDim.x, dim = p.dim, bytes = dim * (int)sizeof(T);
+  pdl_wait();
+  auto load = [&](int64_t r, int stage) {
+    const int64_t g = group_of(p, r), gr = r - g * p.rows;
+    const char* src[3] = {(const char*)row_of<const T>(p.x, g, gr),
+                          has_res ? (const char*)row_of<const T>(p.residual, g, gr) : nullptr, nullptr};
+    ring_load(q, stage, src, bytes);
+  };
+  if (t == 0)
+    for (int s = 0; s < stages; ++s) {
+      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
+      if (r < p.total) load(r, s);
+    }
+  if (!QUANT && one) {
+    for (int c = t; c < dim; c += tpr) s_w[padded(c)] = p.weight.data[c];
+    __syncthreads();
+  }
+  int stage = 0;
+  uint32_t turn = 0;
+  for (int64_t r = blockIdx.x; r < p.total; r += gridDim.x) {
+    const int64_t g = group_of(p, r), gr = r - g * p.rows;
+    const float* weight = QUANT ? nullptr : p.weight.data + g * p.weight.group;
+    const int m = (int)((uint64_t)row_of<const T>(p.x, g, gr) & 15) / (int)sizeof(T);
+    const uint8_t* x = smem + RING_BARS + stage * q.arrays * slot;
+    ring_wait(q, stage, turn & 1);
+    float v[NV][E];
+    Sums red{0.f, 0u};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + i * tpr;
+      const Unit<E> u(c, m, dim);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[i][e] = 0.f;
+      if (u.live) {
+        load_vec<T, E>(reinterpret_cast<const T*>(x) + c * E, v[i]);
+        if (has_res) {
+          float w[E];
+          load_vec<T, E>(reinterpret_cast<const T*>(x + slot) + c * E, w);
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[i][e] += w[e];
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (!u.in(e, dim)) v[i][e] = 0.f;
+        if (!QUANT && p.sum.data) store_unit<T, E>(row_of<T>(p.sum, g, gr), u, dim, v[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Unit<E> u(t + i * tpr, m, dim);
+      if constexpr (!QUANT) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
+        if (u.live) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int c = min(max(u.col + e, 0), dim - 1);
+            v[i][e] *= u.in(e, dim) ? (one ? s_w[padded(c)] : __ldg(weight + c)) : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+    }
+    red = block_reduce<!QUANT, true>(red, s_red[turn >> 1 & 1]);
+    if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
+    const RowScale f = row_scale<QUANT>(p, g, gr, red, t == 0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Unit<E> u(t + i * tpr, m, dim);
+      if (!u.live) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f.f * f.inv;
+      if (QUANT || p.scale.data) store_unit_e4m3<E>(row_of<e4m3>(p.y, g, gr), u, dim, v[i]);
+      else store_unit<T, E>(row_of<T>(p.y, g, gr), u, dim, v[i]);
+    }
+    turn ^= 2;
+    if (++stage == stages) {
+      stage = 0;
+      turn ^= 1;
+    }
+  }
+  ring_done(q, err);
+}
+
 // Rows too long for the registers of 1024 threads are read twice, one block per row.
 template <typename T, int E>
 __global__ void __launch_bounds__(1024) k_quantize_long(const RowArgs p, int64_t dim) {
@@ -465,6 +595,92 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p, int 
   ring_done(q, err);
 }
 
+// The same for rows off the 16-byte grid (k_rows_shift's units): a column is another thread's in every row,
+// so the sums for dweight stand in shared memory, beside the weights.
+template <typename T, int E, int NV>
+__global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p, int stages, int slot,
+                                                                int* err) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Sums s_red[2][16];
+  const bool has_dsum = p.dsum.data;
+  const Ring q = ring_init(smem, stages, slot, has_dsum ? 3 : 2);
+  const int64_t g = blockIdx.y;
+  const int t = threadIdx.x, tpr = blockDim.x, dim = p.dim, bytes = dim * (int)sizeof(T);
+  float* s_w = reinterpret_cast<float*>(smem + RING_BARS + stages * q.arrays * slot);
+  float* s_dw = s_w + padded(dim) + 1;
+  pdl_wait();
+  auto load = [&](int64_t r, int stage) {
+    const char* src[3] = {(const char*)row_of<const T>(p.dy, g, r), (const char*)row_of<const T>(p.s, g, r),
+                          has_dsum ? (const char*)row_of<const T>(p.dsum, g, r) : nullptr};
+    ring_load(q, stage, src, bytes);
+  };
+  if (t == 0)
+    for (int s = 0; s < stages; ++s) {
+      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
+      if (r < p.rows) load(r, s);
+    }
+  const float* weight = p.weight.data + g * p.weight.group;
+  for (int c = t; c < dim; c += tpr) s_w[padded(c)] = weight[c], s_dw[padded(c)] = 0.f;
+  __syncthreads();
+  int stage = 0;
+  uint32_t turn = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+    const float rstd = p.rstd.data[g * p.rstd.group + r];
+    const int m = (int)((uint64_t)row_of<const T>(p.s, g, r) & 15) / (int)sizeof(T);
+    const uint8_t* rows = smem + RING_BARS + stage * q.arrays * slot;
+    ring_wait(q, stage, turn & 1);
+    Raw<T, E> dy[NV], s[NV], ds[NV];
+    float along = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + i * tpr;
+      const Unit<E> u(c, m, dim);
+      dy[i].zero(), s[i].zero(), ds[i].zero();
+      if (!u.live) continue;
+      dy[i].load(reinterpret_cast<const T*>(rows) + c * E);
+      s[i].load(reinterpret_cast<const T*>(rows + slot) + c * E);
+      if (has_dsum) ds[i].load(reinterpret_cast<const T*>(rows + 2 * slot) + c * E);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (u.in(e, dim)) {
+          const float d = dy[i].get(e) * s[i].get(e);
+          const int at = padded(u.col + e);
+          s_dw[at] = fmaf(d, rstd, s_dw[at]);
+          along = fmaf(d, s_w[at], along);
+        }
+    }
+    // (the next row's sums for a column follow after this barrier)
+    along = block_reduce<true, false>(Sums{along, 0u}, s_red[turn >> 1 & 1]).ss;
+    if (t == 0 && r + (int64_t)stages * gridDim.x < p.rows) load(r + (int64_t)stages * gridDim.x, stage);
+    const float c2 = rstd * rstd * (along * p.inv_dim);
+    T* dx = row_of<T>(p.dx, g, r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Unit<E> u(t + i * tpr, m, dim);
+      if (!u.live) continue;
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float w = u.in(e, dim) ? s_w[padded(u.col + e)] : 0.f;
+        v[e] = fmaf(rstd, fmaf(-s[i].get(e), c2, dy[i].get(e) * w), ds[i].get(e));
+      }
+      store_unit<T, E>(dx, u, dim, v);
+    }
+    turn ^= 2;
+    if (++stage == stages) {
+      stage = 0;
+      turn ^= 1;
+    }
+  }
+  __syncthreads();
+  if (p.dweight.data) {
+    float* out = p.part ? p.part + (g * gridDim.x + blockIdx.x) * (int64_t)dim
+                        : p.dweight.data + g * p.dweight.group;
+    for (int c = t; c < dim; c += tpr) out[c] = s_dw[padded(c)];
+  }
+  ring_done(q, err);
+}
+
 // Short rows: a warp per row, loaded into registers one row ahead; a block of BACK_WARPS walks over rows of
 // one group, and its warps' sums for dweight are added in shared memory. (With a ring and a block per row,
 // 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks' own set-up.)
@@ -562,7 +778,7 @@ __global__ void __launch_bounds__(1024)
   float v = 0.f;
   if (c < cols) {
     const float* p = part + g * parts * cols + c;
-#pragma unroll 4
+#pragma unroll 16
     for (int i = threadIdx.y; i < parts; i += blockDim.y) v += p[i * cols];
   }
   s[threadIdx.y][threadIdx.x] = v;
@@ -583,9 +799,12 @@ struct StreamShape {
   bool wide;
   int tpr, per_sm, stages, slot, smem;
 };
-StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads) {
+// `params`: fp32 parameters of a column that stand in shared memory (k_rows_shift and its backward, whose
+// rows touch up to two units more).
+StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int params = 0) {
   StreamShape s;
-  const int nvec = dim / e;
+  const int nvec = params ? (int)ceil_div(dim + 2 * e - 2, e) : dim / e;
+  const int fixed = params * (dim + dim / 32 + 2) * 4;
   s.wide = row_threads(nvec, 16 / e) > 512;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
   s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;
@@ -593,10 +812,10 @@ StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads) {
   if (s.wide) threads /= 2;
   s.per_sm = threads / s.tpr < 24 ? threads / s.tpr : 24;
   if (s.per_sm < 1) s.per_sm = 1;
-  auto stages = [&] { return (budget / s.per_sm - 1024 - RING_BARS) / row; };
+  auto stages = [&] { return (budget / s.per_sm - 1024 - RING_BARS - fixed) / row; };
   while (s.per_sm > 1 && stages() < 2) --s.per_sm;
   s.stages = stages() > RING_MAX ? RING_MAX : stages();
-  s.smem = RING_BARS + s.stages * row;
+  s.smem = RING_BARS + s.stages * row + fixed;
   return s;
 }
 
@@ -606,6 +825,11 @@ cudaError_t allow_smem(K kernel, int smem) {
              ? cudaSuccess
              : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
 }
+
+// (512 threads of 32 elements, less the two units more)
+constexpr int SHIFT_MAX_DIM = 16384 - 16;
+// (two parameters and one stage of three fp32 rows in shared memory)
+constexpr int SHIFT_BACK_MAX_DIM = 8192;
 
 // From this many rows per SM on, rows stream through rings; fewer are loaded by the threads that use them.
 constexpr int STREAM_ROWS = 4;
@@ -620,9 +844,36 @@ cudaError_t launch_stream(const RowArgs& p, const StreamShape& s, cudaStream_t s
                     st, p, s.stages, s.slot, timeout_word());
 }
 
+// Whether, in every row, two matrices begin at the same element of a unit of e elements.
+bool same_shift(const lipz_mat& a, const lipz_mat& b, int64_t groups, int64_t rows, int e) {
+  if (!b.data) return true;
+  auto first = [](const lipz_mat& m) { return (int64_t)((uintptr_t)m.data / type_bytes(m.type)); };
+  return (first(a) - first(b)) % e == 0 && (rows == 1 || (a.row - b.row) % e == 0) &&
+         (groups == 1 || (a.group - b.group) % e == 0);
+}
+
+template <typename T, bool QUANT>
+cudaError_t launch_shift(const RowArgs& p, cudaStream_t st) {
+  constexpr int E = 16 / sizeof(T);
+  const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 1024, 1);
+  auto go = [&](auto kernel) {
+    const cudaError_t e = allow_smem(kernel, s.smem);
+    const int64_t blocks = (int64_t)s.per_sm * sm_count();
+    return e != cudaSuccess ? e
+                            : launch_pdl(kernel, dim3((unsigned)(blocks < p.total ? blocks : p.total)),
+                                         dim3(s.tpr), s.smem, st, p, s.stages, s.slot, timeout_word());
+  };
+  return s.wide ? go(k_rows_shift<T, E, 32 / E, QUANT>) : go(k_rows_shift<T, E, 16 / E, QUANT>);
+}
+
 template <typename T, int E, bool QUANT>
 cudaError_t launch_rows(RowArgs& p, cudaStream_t st) {
   if (p.total > STREAM_ROWS * sm_count()) {
+    constexpr int U = 16 / sizeof(T);
+    const int64_t groups = p.total / p.rows;
+    if (E == 1 && p.dim <= SHIFT_MAX_DIM && same_shift(p.x, p.y, groups, p.rows, U) &&
+        same_shift(p.x, p.residual, groups, p.rows, U) && same_shift(p.x, p.sum, groups, p.rows, U))
+      return launch_shift<T, QUANT>(p, st);
     const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 2048);
     return s.wide ? launch_stream<T, E, 32 / E, QUANT>(p, s, st)
                   : launch_stream<T, E, 16 / E, QUANT>(p, s, st);
@@ -651,9 +902,29 @@ int backward_row_vectors(const lipz_rmsnorm_backward_args& a) {
   return !backward_vec(a) || per > 4 ? 0 : per <= 1 ? 1 : per <= 2 ? 2 : 4;
 }
 
+bool backward_shift(const lipz_rmsnorm_backward_args& a) {
+  const int e = 16 / type_bytes(a.dy.type);
+  return !backward_vec(a) && a.dim <= SHIFT_BACK_MAX_DIM && same_shift(a.s, a.dy, a.groups, a.rows, e) &&
+         same_shift(a.s, a.dsum, a.groups, a.rows, e) && same_shift(a.s, a.dx, a.groups, a.rows, e);
+}
+
 StreamShape backward_shape(const lipz_rmsnorm_backward_args& a) {
   const int eb = type_bytes(a.dy.type);
+  if (backward_shift(a)) return stream_shape((int)a.dim, 16 / eb, eb, a.dsum.data ? 3 : 2, 1024, 2);
   return stream_shape((int)a.dim, backward_vec(a) ? 16 / eb : 1, eb, a.dsum.data ? 3 : 2, 1024);
+}
+
+template <typename T>
+cudaError_t launch_back_shift(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
+                              cudaStream_t st) {
+  constexpr int E = 16 / sizeof(T);
+  auto go = [&](auto kernel) {
+    const cudaError_t e = allow_smem(kernel, s.smem);
+    return e != cudaSuccess ? e
+                            : launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(s.tpr), s.smem, st,
+                                         p, s.stages, s.slot, timeout_word());
+  };
+  return s.wide ? go(k_rmsnorm_backward_shift<T, E, 32 / E>) : go(k_rmsnorm_backward_shift<T, E, 16 / E>);
 }
 
 template <typename T>
@@ -757,6 +1028,9 @@ cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t s
   if (nv)
     e = a.dy.type == LIPZ_FP32 ? launch_back_rows<float>(p, nv, a.groups, blocks, st)
                                : launch_back_rows<bf16>(p, nv, a.groups, blocks, st);
+  else if (backward_shift(a))
+    e = a.dy.type == LIPZ_FP32 ? launch_back_shift<float>(p, s, a.groups, blocks, st)
+                               : launch_back_shift<bf16>(p, s, a.groups, blocks, st);
   else if (a.dy.type == LIPZ_FP32)
     e = vec ? launch_back<float, 4>(p, s, a.groups, blocks, st)
             : launch_back<float, 1>(p, s, a.groups, blocks, st);

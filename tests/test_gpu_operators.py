@@ -232,6 +232,59 @@ def test_rmsnorm_gradients_are_those_of_the_forward():
             assert abs(got - diff / (2 * h)) < 1e-4
 
 
+# rows that start anywhere in a 16-byte unit, enough of them to stream; a dimension past the kernels' widest
+OFF_GRID = [(1, 1300, 257), (3, 300, 1001), (1, 650, 8191), (2, 700, 7), (1, 640, 1), (1, 700, 16383),
+            (5, 200, 12), (1, 900, 4100), (1, 1000, 16378)]
+
+
+@pytest.mark.parametrize("groups,rows,dim", OFF_GRID)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("residual,e4m3", [(False, False), (True, True), (True, False)])
+def test_many_rows_off_the_grid(groups, rows, dim, dtype, residual, e4m3):
+    x = randn(121, norm_shape(groups, rows, dim), 2.0, dtype)
+    res = randn(122, norm_shape(groups, rows, dim), 3.0, dtype) if residual else None
+    w = 1 + randn(123, norm_shape(groups, dim), 0.2, F32)
+    r = ops.rmsnorm(x, w, residual=res, eps=1e-5, e4m3=e4m3, keep=True)
+    check_norm(r, x, res, w, 1e-5, e4m3, True)
+    q, scale = ops.quantize_rows(x)
+    ref = (d(x).abs().amax(dim=-1) / 448).clamp(min=2.0 ** -126)
+    within(scale, ref, 2.0 ** -23 * ref, "scale")
+    v = d(x) / ref[..., None]
+    within(q, v, 2.0 ** -4 * v.abs() * (1 + 2.0 ** -20) + 2.0 ** -10, "q")
+
+
+@pytest.mark.parametrize("groups,rows,dim", OFF_GRID)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("with_dsum", [False, True])
+def test_many_rows_off_the_grid_backward(groups, rows, dim, dtype, with_dsum):
+    test_rmsnorm_backward(groups, rows, dim, dtype, with_dsum)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("wide,cut,res_cut", [(264, 3, 3), (261, 0, 0), (264, 3, 2), (257, 1, 1)])
+def test_many_strided_rows(dtype, wide, cut, res_cut):
+    """Rows cut from wider ones, the residual at the same place in them or at another; the stream updated
+    in place, and nothing beside it."""
+    rows, groups, dim = 400, 3, 253
+    x = randn(124, (rows, groups, wide), 1.0, dtype)[:, :, cut:cut + dim].permute(1, 0, 2)
+    whole = randn(125, (rows, groups, wide), 1.0, dtype)
+    res = whole[:, :, res_cut:res_cut + dim].permute(1, 0, 2)
+    w = (1 + randn(126, (1, dim), 0.1, F32)).expand(groups, dim)
+    before, beside = res.clone(), whole.clone()
+    r = ops.rmsnorm(x, w, residual=res, sum_out=res, keep=True)
+    check_norm(r, x, before, w, 1e-6, False, True)
+    beside[:, :, res_cut:res_cut + dim] = whole[:, :, res_cut:res_cut + dim]
+    assert torch.equal(beside, whole)
+    dy = randn(127, (rows, groups, wide), 0.1, dtype)[:, :, cut:cut + dim].permute(1, 0, 2)
+    dx, dw = ops.rmsnorm_backward(dy, res, r.rstd, w, dsum=x)
+    ref_dx, ref_dw = norm_backward_ref(dy, res, r.rstd, w, x)
+    g, rs = d(dy).abs() * d(w).abs()[..., None, :], d(r.rstd)[..., None]
+    size = rs * (g + d(res).abs() * rs * rs * (g * d(res).abs()).mean(dim=-1, keepdim=True)) + d(x).abs()
+    within(dx, ref_dx, ROUND[dtype] * ref_dx.abs() + ((dim + 16) * 2.0 ** -24 + 2.0 ** -20) * size, "dx")
+    mag = (d(dy) * d(res) * rs).abs().sum(dim=-2)
+    within(dw, ref_dw, (rows + 16) * 2.0 ** -23 * mag, "dweight")
+
+
 # ---- quantize_rows --------------------------------------------------------------------------------
 @pytest.mark.parametrize("groups,rows,dim", NORM_SHAPES + [(1, 3, 20000), (2, 2, 33333), (1, 2, 65536)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
