@@ -79,6 +79,7 @@ struct Problem {
   float* part;  // partial sums [splits][groups][m][ldp] instead of results, or null
   int64_t ldp;
   int groups, m, n, tiles_m, tiles_n, tiles, units, splits, chunks, chunks_per_split;
+  int parts;             // SPLIT: CTAs of a cluster (and splits is 1)
   Divisor by_split, by_group, by_panel, by_rest;  // splits, tiles, 8 tiles_n, rows of the last panel
   int a_bytes;               // of A's box per CTA and stage
   int az, bz;                // 0: one matrix for every group
@@ -279,12 +280,15 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
 // product; else up to two plain products.
 // VIA: with row-per-lane accesses a tile's results cost 12 us and its residual 25 to 39 us at 144 x 512 x 256
 // -> 768 (of 47 and 88 us in all).
-template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA>
+// SPLIT: a cluster of CTAs shares a tile, each with a part of k; their sums are added over the cluster's
+// shared memory, each CTA finishing a part of the columns. One tile per cluster.
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
     k_gemm_op(const __grid_constant__ GemmParams<FORWARD ? 1 : 2> prm) {
   using S = Shape<CG, BN, VIA>;
   constexpr bool SUMS = sizeof(T) == 4;
   static_assert(!VIA || (FORWARD && !SUMS && S::COLSW == 32), "boxes of 32 bf16 columns");
+  static_assert(!SPLIT || (FORWARD && CG == 1 && !VIA && 128 * (BN + 1) * 4 <= 2 * S::STAGE), "sums of a tile");
   constexpr int BM = 128 * CG, COLSW = S::COLSW, ACCS = S::ACCS, SLOTS = S::SLOTS;
   constexpr int CW = COLSW < 32 ? COLSW : 32;       // a result warp's columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
@@ -344,8 +348,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem = *tmem_slot;
   const uint32_t lFull = CG == 2 ? tc::mapa_shared(bFull, 0) : bFull;
   const uint32_t lFree = CG == 2 ? tc::mapa_shared(bFree, 0) : bFree;
-  const int first = CG == 2 ? (int)tc::cluster_id_x() : (int)blockIdx.x;
-  const int step = CG == 2 ? (int)tc::nclusters_x() : (int)gridDim.x;
+  const int first = CG == 2 || SPLIT ? (int)tc::cluster_id_x() : (int)blockIdx.x;
+  const int step = CG == 2 || SPLIT ? (int)tc::nclusters_x() : (int)gridDim.x;
+  float* s_part = reinterpret_cast<float*>(smem_raw + (base - raw));  // SPLIT: [128][BN + 1], over the stages
   // The place of the warp's i-th unit: its lanes work out 32 units' places at a time.
   Place ahead{};
   auto unit_place = [&](int i) {
@@ -359,6 +364,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int from = i & 31;
     Place r{__shfl_sync(0xffffffffu, ahead.g, from), __shfl_sync(0xffffffffu, ahead.mt, from),
             __shfl_sync(0xffffffffu, ahead.nt, from), __shfl_sync(0xffffffffu, ahead.split, from)};
+    if (SPLIT) r.split = (int)tc::cluster_ctarank();
     return r;
   };
   auto problem_of = [&](const Place& pl) -> const Problem& {
@@ -482,7 +488,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       int c0, c1;
       chunk_range(p, pl.split, c0, c1);
       float bias[BN / 32], ws[BN / 32], xs[4];
-      if (FORWARD && !p.part) {
+      if (FORWARD && !SPLIT) {
 #pragma unroll
         for (int j = 0; j < BN / 32; ++j) {
           const int n = n0 + j * 32 + lane;
@@ -510,7 +516,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                  g * e.pre.group + (int64_t)row0 * e.pre.row + n0,
                  (((int64_t)pl.split * p.groups + g) * p.m + row0) * p.ldp + n0, p.m - row0, p.n - n0,
                  FORWARD ? 0 : pl.g >> 30, c0, c1, (int)g, row0, n0};
-      if (FORWARD && !p.part) {
+      if (FORWARD && !SPLIT) {
         float* f = reinterpret_cast<float*>(slot + sizeof(Slot));
 #pragma unroll
         for (int j = 0; j < BN / 32; ++j) {
@@ -595,11 +601,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       const Problem& p = prm.p[FORWARD ? 0 : sl.which];
       const Epilogue& e = p.e;
       const int rows = sl.rows - q * 32;
-      const float xs = TYPE == LIPZ_E4M3 && FORWARD && !p.part ? col[2 * BN - col0 + q * 32 + lane] : 1.f;
+      const float xs = TYPE == LIPZ_E4M3 && FORWARD && !SPLIT ? col[2 * BN - col0 + q * 32 + lane] : 1.f;
       // CW results of this lane's row, from column c of the warp's; v: the residual
       auto columns_left = [&](int c) { return sl.cols - (col0 + c); };
       constexpr int VW = CW / 16 * WORDS<T>;
-      const bool has_res = FORWARD && !p.part && e.residual.data && rows > 0;
+      const bool has_res = FORWARD && !SPLIT && e.residual.data && rows > 0;
       // VIA: this lane's 64 bytes of the warp's 32 rows, 16-byte units in the 64-byte swizzle
       uint8_t* mine = tiles + r * S::TILE + (ew >> 2) * (S::TILE / (BN / 32)) + q * 2048 + lane * 64;
       const int swizzle = lane >> 1 & 3;
@@ -614,7 +620,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       };
       auto results = [&](float (&u)[CW], const uint32_t (&v)[VW], int c) {
         if (rows <= 0 || columns_left(c) <= 0) return;
-        if (p.part) {
+        if constexpr (SPLIT) {
+          float* dst = s_part + (q * 32 + lane) * (BN + 1) + col0 + c;
+#pragma unroll
+          for (int j = 0; j < CW; ++j) dst[j] = u[j];
+          return;
+        }
+        if (!FORWARD && p.part) {
           float* dst = p.part + sl.part + (int64_t)(q * 32) * p.ldp + col0 + c;
 #pragma unroll
           for (int h = 0; h < CW; h += 16)
@@ -739,8 +751,29 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     if (VIA && lane == 0) tc::bulk_wait_all();
   }
+  if constexpr (SPLIT) {
+    __syncwarp();
+    tc::cluster_sync_all();  // every CTA's sums stand in its shared memory
+    const Problem& p = prm.p[0];
+    const Place pl = place(p, first);
+    const int parts = p.parts, rows = min(128, p.m - pl.mt * 128), width = BN / parts;
+    const int c0 = (int)tc::cluster_ctarank() * width;
+    for (int i = threadIdx.x; i < rows * width; i += THREADS) {
+      const int r = i / width, c = c0 + i - r * width, n = pl.nt * BN + c;
+      if (n >= p.n) continue;
+      const uint32_t at = tc::smem_u32(s_part + r * (BN + 1) + c);
+      float u = 0.f;
+      for (int j = 0; j < parts; ++j) {
+        float v;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_shared(at, j)) : "memory");
+        u += v;
+      }
+      finish(p.e, pl.g, pl.mt * 128 + r, n, u);
+    }
+  }
   tc::tc_fence_before();
-  if constexpr (CG == 2) tc::cluster_sync_all();
+  __syncwarp();
+  if constexpr (CG == 2 || SPLIT) tc::cluster_sync_all();  // (SPLIT: no CTA leaves while its sums are read)
   else __syncthreads();
   tc::tc_fence_after();
   if (warp == 2) {
@@ -752,9 +785,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (threadIdx.x == 0 && *code && prm.err) *reinterpret_cast<volatile int*>(prm.err) = *code;
 }
 
-// Sum of the parts of k, in order, and the epilogue. E columns per thread.
+// Sum of the parts of k, in order. E columns per thread.
 struct FinishParams {
-  Epilogue e;
+  lipz_mat y;
   const float* part;
   int64_t ldp, split_stride, total;  // rows of all groups
   int splits, m, n;
@@ -768,13 +801,13 @@ __global__ void __launch_bounds__(256) k_finish(const __grid_constant__ FinishPa
   const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   pdl_wait();
   if (r >= p.total) return;
-  const Epilogue& e = p.e;
+  const int64_t g = r / p.m, o = g * p.y.group + (r - g * p.m) * p.y.row;
   for (int64_t c = ((int64_t)blockIdx.y * 32 + (threadIdx.x & 31)) * E; c < p.n;
        c += (int64_t)gridDim.y * 32 * E) {
-    const int64_t g = r / p.m, m = r - g * p.m;
     float u[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) u[i] = 0.f;
+#pragma unroll 4
     for (int s = 0; s < p.splits; ++s) {
       const float* q = p.part + s * p.split_stride + r * p.ldp + c;
       if constexpr (E == 4) {
@@ -784,75 +817,22 @@ __global__ void __launch_bounds__(256) k_finish(const __grid_constant__ FinishPa
         u[0] += *q;
       }
     }
-    const float xs = e.x_scale.data ? e.x_scale.data[g * e.x_scale.group + m] : 1.f;
+    if (p.y.type == LIPZ_FP32) {
+      float* y = (float*)p.y.data + o + c;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      if (e.w_scale.data) u[i] *= xs * e.w_scale.data[g * e.w_scale.group + c + i];
-      if (e.bias.data) u[i] += e.bias.data[g * e.bias.group + c + i];
+      for (int i = 0; i < E; ++i) y[i] = u[i];
+    } else {
+      bf16* y = (bf16*)p.y.data + o + c;
+#pragma unroll
+      for (int i = 0; i < E; ++i) y[i] = __float2bfloat16_rn(u[i]);
     }
-    auto put = [&](auto t, const lipz_mat& d) {
-      using T = decltype(t);
-      T* o = (T*)d.data + g * d.group + m * d.row + c;
-      if constexpr (E == 1) {
-        *o = from_f<T>(u[0]);
-      } else if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(o) = make_float4(u[0], u[1], u[2], u[3]);
-      } else {
-        *reinterpret_cast<uint2*>(o) = make_uint2(tc::pack_bf16(u[0], u[1]), tc::pack_bf16(u[2], u[3]));
-      }
-    };
-    if (e.pre.data) put(bf16{}, e.pre);
-    with_act(e.act, [&](auto act) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) u[i] = act_value<decltype(act)::value>(u[i], e.slope);
-    });
-    if (e.residual.data) {
-      const int64_t o = g * e.residual.group + m * e.residual.row + c;
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        u[i] += e.y.type == LIPZ_FP32 ? ((const float*)e.residual.data)[o + i]
-                                      : __bfloat162float(((const bf16*)e.residual.data)[o + i]);
-    }
-    if (e.y.type == LIPZ_FP32) put(float{}, e.y);
-    else put(bf16{}, e.y);
   }
 }
 
-// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a
-// warp; a thread forms 16 bytes at a time.
-template <typename U>
-__device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
-  constexpr int E = 16 / sizeof(U);
-  const int64_t g = r / p.rows;
-  const U* s = (const U*)p.src + g * p.group + (r - g * p.rows) * p.ld;
-  for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) {
-    union {
-      uint4 v;
-      U e[E];
-    } w;
-#pragma unroll
-    for (int i = 0; i < E; ++i) w.e[i] = u * E + i < p.cols ? s[u * E + i] : U(0);
-    ((uint4*)p.dst)[r * p.units + u] = w.v;
-  }
-}
-struct CopyJobs {
-  RowCopy c[4];
-  int n;
-};
-// 8 rows per block, of one copy after the other.
 template <typename U>
 __global__ void __launch_bounds__(256) k_copy_rows(const __grid_constant__ CopyJobs jobs) {
   pdl_wait();
-  int64_t b = blockIdx.x;
-  for (int j = 0; j < jobs.n; ++j) {
-    const int64_t blocks = ceil_div_d(jobs.c[j].total, 8);
-    if (b < blocks) {
-      const int64_t r = b * 8 + (threadIdx.x >> 5);
-      if (r < jobs.c[j].total) copy_row<U>(jobs.c[j], r);
-      return;
-    }
-    b -= blocks;
-  }
+  copy_rows<U>(jobs, blockIdx.x);
 }
 
 // Blocks of 8 rows by 32 columns' threads; columns past 65535 blocks are looped over.
@@ -954,7 +934,7 @@ cudaError_t prepare_kernel(K kernel, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false>
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false>
 cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
                    cudaStream_t st) {
   using S = Shape<CG, BN, VIA>;
@@ -979,10 +959,11 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
     p.ldp = o.ldp;
     p.groups = (int)g.groups, p.m = (int)g.m, p.n = (int)g.n;
     p.tiles_m = (int)o.tiles_m, p.tiles_n = (int)o.tiles_n;
-    p.splits = o.splits;
+    p.splits = SPLIT ? 1 : o.splits;
+    p.parts = o.splits;
     p.tiles = (int)(o.tiles_m * o.tiles_n);
-    p.units = (int)(p.tiles * g.groups * o.splits);
-    p.by_split = divisor(o.splits), p.by_group = divisor(p.tiles);
+    p.units = (int)(p.tiles * g.groups * p.splits);
+    p.by_split = divisor(p.splits), p.by_group = divisor(p.tiles);
     p.by_panel = divisor(8 * o.tiles_n), p.by_rest = divisor(o.tiles_m % 8 ? o.tiles_m % 8 : 8);
     p.chunks = (int)o.chunks, p.chunks_per_split = (int)o.chunks_per_split;
     p.a_bytes = arows * ROW;
@@ -1005,10 +986,11 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   k.err = timeout_word();
   k.stages = S::stages(turn);
   static std::atomic<uint64_t> done{0};
-  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T, VIA>;
+  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T, VIA, SPLIT>;
   cudaError_t e = prepare_kernel(kernel, done);
   if (e != cudaSuccess) return e;
-  const int slots = sm_count() / CG, ctas = (k.units < slots ? k.units : slots) * CG;
+  const int cluster = SPLIT ? k.p[0].parts : CG, slots = SPLIT ? k.units : sm_count() / CG;
+  const int ctas = (k.units < slots ? k.units : slots) * cluster;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(THREADS);
@@ -1016,7 +998,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CG;
+  attr[0].val.clusterDim.x = cluster;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
@@ -1037,6 +1019,11 @@ bool results_by_tma(const Gemm& g) {
 template <int TYPE, bool FORWARD>
 cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* parts, const PartSums* sums,
                          cudaStream_t st) {
+  if constexpr (FORWARD) {
+    if (p.p[0].splits > 1)
+      return q.g[0].e.y.type == LIPZ_FP32 ? launch<TYPE, 1, 64, true, float, false, true>(q, p, parts, sums, st)
+                                          : launch<TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
+  }
   if (q.g[0].e.y.type == LIPZ_FP32) {
     if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, float>(q, p, parts, sums, st);
     if (p.bn == 128) return launch<TYPE, 1, 128, FORWARD, float>(q, p, parts, sums, st);
@@ -1044,7 +1031,7 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
   }
   if (p.cg == 2 && p.bn == 256) return launch<TYPE, 2, 256, FORWARD, bf16>(q, p, parts, sums, st);
   if constexpr (FORWARD) {
-    if (p.cg == 2 && !parts[0] && results_by_tma(q.g[0]))
+    if (p.cg == 2 && results_by_tma(q.g[0]))
       return launch<TYPE, 2, 128, true, bf16, true>(q, p, parts, sums, st);
   }
   if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, bf16>(q, p, parts, sums, st);
@@ -1060,8 +1047,8 @@ GemmPlan plan_products(const Products& q) {
   const int eb = type_bytes(g0.type);
   const bool sums = g0.e.y.type == LIPZ_FP32, res = g0.e.residual.data, heavy = g0.e.act >= LIPZ_ACT_TANH;
   // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its MMA
-  // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost another launch and their
-  // way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 x 8192 in bf16 (8 bits: 184 instead
+  // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost a cluster's exchange, or
+  // another launch and their way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 x 8192 in bf16 (8 bits: 184 instead
   // of 158), epilogues at 144 x 512 x 256 -> 768 without an activation, what tanh adds, what a residual adds.
   struct Shape {
     int cg, bn;
@@ -1070,15 +1057,17 @@ GemmPlan plan_products(const Products& q) {
   static const Shape shapes[] = {{2, 256, 158, 9000, 2500, 5500}, {2, 128, 88, 3900, 800, 2600},
                                  {1, 128, 108, 3900, 800, 2600}, {1, 64, 82, 2350, 250, 900}};
   const Shape via{2, 128, 100, 3500, 400, 1000};  // shape 1 with its results through shared memory
-  const bool by_tma = results_by_tma(g0);
+  const bool by_tma = results_by_tma(g0), forward = g0.a.k_major && g0.b.k_major;
   const int sms = sm_count();
   double best = -1;
   static const int force_cg = getenv("OPCG") ? atoi(getenv("OPCG")) : 0, force_bn = getenv("OPBN") ? atoi(getenv("OPBN")) : 0, force_s = getenv("OPS") ? atoi(getenv("OPS")) : 0;
   for (const Shape& shape : shapes) {
     if (sums && shape.bn > 128) continue;
     if (force_cg && (shape.cg != force_cg || shape.bn != force_bn)) continue;
-    for (int s0 = 1; s0 <= 64; s0 *= 2) {
+    // a forward's parts of k are a cluster's CTAs, all clusters resident at once
+    for (int s0 = 1; s0 <= (forward ? 8 : 64); s0 *= 2) {
       if (force_s && s0 != force_s) continue;
+      if (forward && s0 > 1 && shape.bn != 64) continue;
       const Shape& c = by_tma && s0 == 1 && shape.cg == 2 && shape.bn == 128 ? via : shape;
       const int64_t slots = sms / c.cg;
       GemmPlan t{};
@@ -1093,18 +1082,21 @@ GemmPlan plan_products(const Products& q) {
         const int64_t want = s0 < o.chunks ? s0 : o.chunks, tiles = o.tiles_m * o.tiles_n * g.groups;
         o.chunks_per_split = ceil_div(o.chunks, want);
         o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);
-        fits = fits && tiles * o.splits <= INT32_MAX / 2 && (o.splits == 1 || tiles * o.splits <= 2 * slots);
+        fits = fits && tiles * o.splits <= INT32_MAX / 2 &&
+               (o.splits == 1 || tiles * o.splits <= (forward ? 1 : 2) * slots) &&
+               (!forward || o.splits == s0);
         const double mma = o.chunks_per_split * 4 * c.step * (eb == 1 ? 1.16 : 1);
         const double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0), unit = mma > epi ? mma : epi;
         work += unit * tiles * o.splits;
         if (unit > top) top = unit;
         if (mma + epi > last) last = mma + epi;
-        if (o.splits > 1) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000, split = true;
+        if (o.splits > 1 && !forward) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000;
+        split = split || o.splits > 1;
       }
-      if ((!fits && !force_cg) || (s0 > 1 && !split)) continue;
+      if ((!fits && (!force_cg || forward)) || (s0 > 1 && !split)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
-      const double time = waves * top + last + extra + (split ? 9500 : 0);
+      const double time = waves * top + last + extra + (!split ? 0 : forward ? 2000 : 9500);
       if (best < 0 || time < best) best = time, plan = t;
     }
   }
@@ -1126,7 +1118,7 @@ void plan_space(const Products& q, GemmPlan* plan) {
     o.a_bytes = o.copy_a ? round256(g.groups * xa.rows * o.lda * eb) : 0;
     o.b_bytes = o.copy_b ? round256(g.groups * xb.rows * o.ldb * eb) : 0;
     o.ldp = ceil_div(g.n, 16) * 16;
-    o.part_bytes = o.splits > 1 ? round256((int64_t)o.splits * g.groups * g.m * o.ldp * 4) : 0;
+    o.part_bytes = o.splits > 1 && !(g.a.k_major && g.b.k_major) ? round256((int64_t)o.splits * g.groups * g.m * o.ldp * 4) : 0;
     plan->bytes += o.a_bytes + o.b_bytes + o.part_bytes;
   }
 }
@@ -1149,18 +1141,21 @@ int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* cop
   return n;
 }
 
-cudaError_t run_copies(const RowCopy* c, int n, int type, cudaStream_t st) {
-  if (n == 0) return cudaSuccess;
+CopyJobs copy_jobs(const RowCopy* c, int n) {
   CopyJobs jobs{};
   jobs.n = n;
-  int64_t blocks = 0;
   for (int i = 0; i < n; ++i) {
     jobs.c[i] = c[i];
-    blocks += ceil_div(c[i].total, 8);
+    jobs.blocks += ceil_div(c[i].total, COPY_ROWS);
   }
-  return type == LIPZ_BF16
-             ? launch_pdl(k_copy_rows<unsigned short>, dim3((unsigned)blocks), dim3(256), 0, st, jobs)
-             : launch_pdl(k_copy_rows<unsigned char>, dim3((unsigned)blocks), dim3(256), 0, st, jobs);
+  return jobs;
+}
+
+cudaError_t run_copies(const CopyJobs& jobs, int type, cudaStream_t st) {
+  if (jobs.blocks == 0) return cudaSuccess;
+  const dim3 grid((unsigned)jobs.blocks), block(256);
+  return type == LIPZ_BF16 ? launch_pdl(k_copy_rows<unsigned short>, grid, block, 0, st, jobs)
+                           : launch_pdl(k_copy_rows<unsigned char>, grid, block, 0, st, jobs);
 }
 
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
@@ -1187,12 +1182,9 @@ cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspac
     if (!parts[i]) continue;
     const Gemm& g = q.g[i];
     const int64_t ldp = plan.p[i].ldp;
-    f.f[n++] = {g.e, parts[i], ldp, g.groups * g.m * ldp, g.groups * g.m, plan.p[i].splits, (int)g.m,
+    f.f[n++] = {g.e.y, parts[i], ldp, g.groups * g.m * ldp, g.groups * g.m, plan.p[i].splits, (int)g.m,
                 (int)g.n};
-    auto four = [&](const lipz_mat& m) {
-      return !m.data || rows_aligned(m, g.groups, g.m, 4 * type_bytes(m.type));
-    };
-    vec = vec && g.n % 4 == 0 && four(g.e.y) && four(g.e.pre);
+    vec = vec && g.n % 4 == 0;
     rows = rows > g.groups * g.m ? rows : g.groups * g.m;
     cols = cols > g.n ? cols : g.n;
   }

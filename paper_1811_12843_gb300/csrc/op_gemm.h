@@ -69,7 +69,14 @@ void plan_space(const Products& q, GemmPlan* plan);
 // The copies that the products of a plan need, into its workspace (copies[4]), and the operands that the
 // products then have.
 int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* copies);
-cudaError_t run_copies(const RowCopy* c, int n, int type, cudaStream_t st);
+constexpr int COPY_ROWS = 8;  // rows of a block
+struct CopyJobs {
+  RowCopy c[4];
+  int n;
+  int64_t blocks;
+};
+CopyJobs copy_jobs(const RowCopy* c, int n);
+cudaError_t run_copies(const CopyJobs& jobs, int type, cudaStream_t st);
 // The products themselves; sums: null, or formed beside them.
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
                          cudaStream_t st);

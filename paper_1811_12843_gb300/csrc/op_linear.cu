@@ -177,7 +177,7 @@ Products product_of(const lipz_linear_args& a) {
 }
 
 // du = dy act'(pre), in bf16 rows of ldu elements, and the sums of its columns over the block's rows:
-// 32 vectors of columns by 8 rows at a time. Bound: HBM.
+// 32 vectors of columns by 8 rows at a time; the blocks after those copy operands' rows. Bound: HBM.
 struct DuArgs {
   lipz_mat dy, pre;
   bf16* du;     // [groups][rows][ldu], or null: the sums only
@@ -185,16 +185,20 @@ struct DuArgs {
   int64_t rows, n, ldu, rows_per_block;
   int act;
   float slope;
+  int col_blocks, row_blocks, blocks;  // of a group; of all groups
 };
 
 template <int E>
-__global__ void __launch_bounds__(256) k_du(const DuArgs p) {
+__global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
   __shared__ float s[8][32 * E + 1];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int64_t c = ((int64_t)blockIdx.x * 32 + tx) * E, g = blockIdx.z;
-  const int64_t r0 = blockIdx.y * p.rows_per_block;
-  const int64_t r1 = min(p.rows, r0 + p.rows_per_block);
   pdl_wait();
+  if ((int)blockIdx.x >= p.blocks) return copy_rows<unsigned short>(jobs, (int)blockIdx.x - p.blocks);
+  const int per = p.col_blocks * p.row_blocks, in_group = blockIdx.x % per;
+  const int row_block = in_group / p.col_blocks, col_block = in_group - row_block * p.col_blocks;
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int64_t c = ((int64_t)col_block * 32 + tx) * E, g = blockIdx.x / per;
+  const int64_t r0 = row_block * p.rows_per_block;
+  const int64_t r1 = min(p.rows, r0 + p.rows_per_block);
   float sum[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] = 0.f;
@@ -222,11 +226,11 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p) {
   for (int e = 0; e < E; ++e) s[ty][tx * E + e] = sum[e];
   __syncthreads();
   for (int i = threadIdx.x; i < 32 * E; i += 256) {
-    const int64_t col = (int64_t)blockIdx.x * 32 * E + i;
+    const int64_t col = (int64_t)col_block * 32 * E + i;
     float v = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) v += s[q][i];
-    if (col < p.n) p.part[(g * gridDim.y + blockIdx.y) * p.n + col] = v;
+    if (col < p.n) p.part[(g * p.row_blocks + row_block) * p.n + col] = v;
   }
 }
 
@@ -303,7 +307,7 @@ cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {
   const GemmPlan plan = plan_products(q);
   RowCopy copies[4];
   const int n = plan_copies(plan, &q, a.workspace, copies);
-  const cudaError_t e = run_copies(copies, n, a.x.type, st);
+  const cudaError_t e = run_copies(copy_jobs(copies, n), a.x.type, st);
   return e != cudaSuccess ? e : run_products(plan, q, a.workspace, nullptr, st);
 }
 
@@ -332,12 +336,17 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st)
   int n = 0;
   char* at[2] = {rest, rest + b.plan[0].bytes};
   for (int i = 0; i < b.launches; ++i) n += plan_copies(b.plan[i], &b.q[i], at[i], copies + n);
-  cudaError_t e = run_copies(copies, n, LIPZ_BF16, st);
-  if (e == cudaSuccess && (du || part)) {
-    const DuArgs p{a.dy, a.pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope};
-    const dim3 grid((unsigned)ceil_div(a.n, b.vec ? 256 : 32), (unsigned)b.blocks, (unsigned)a.groups);
-    e = b.vec ? launch_pdl(k_du<8>, grid, dim3(256), 0, st, p)
-              : launch_pdl(k_du<1>, grid, dim3(256), 0, st, p);
+  const CopyJobs jobs = copy_jobs(copies, n);
+  cudaError_t e;
+  if (du || part) {
+    const int64_t cols = ceil_div(a.n, b.vec ? 256 : 32), blocks = cols * b.blocks * a.groups;
+    const DuArgs p{a.dy, a.pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope,
+                   (int)cols, (int)b.blocks, (int)blocks};
+    const dim3 grid((unsigned)(blocks + jobs.blocks));
+    e = b.vec ? launch_pdl(k_du<8>, grid, dim3(256), 0, st, p, jobs)
+              : launch_pdl(k_du<1>, grid, dim3(256), 0, st, p, jobs);
+  } else {
+    e = run_copies(jobs, LIPZ_BF16, st);
   }
   const PartSums sums{part, a.n, (int)a.groups, (int)b.blocks, a.db};
   if (e == cudaSuccess && part && !b.launches)

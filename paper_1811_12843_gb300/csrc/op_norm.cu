@@ -681,16 +681,18 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
   ring_done(q, err);
 }
 
-// Short rows: a warp per row, loaded into registers one row ahead; a block of BACK_WARPS walks over rows of
-// one group, and its warps' sums for dweight are added in shared memory. (With a ring and a block per row,
+// Short rows: a warp per row, loaded into registers one row ahead; a block of WARPS walks over rows of one
+// group, and its warps' sums for dweight are added in shared memory. (With a ring and a block per row,
 // 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks' own set-up.)
-constexpr int BACK_WARPS = 8;
+template <int NV>
+constexpr int BACK_WARPS = NV == 1 ? 16 : 8;  // (registers)
 
 template <typename T, int E, int NV>
-__global__ void __launch_bounds__(32 * BACK_WARPS) k_rmsnorm_backward_rows(const BackArgs p) {
-  extern __shared__ float s_dw[];  // [BACK_WARPS][dim]
+__global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(const BackArgs p) {
+  constexpr int WARPS = BACK_WARPS<NV>;
+  extern __shared__ float s_dw[];  // [WARPS][dim]
   const int warp = threadIdx.x >> 5, t = threadIdx.x & 31, nvec = p.dim / E;
-  const int64_t g = blockIdx.y, step = (int64_t)gridDim.x * BACK_WARPS;
+  const int64_t g = blockIdx.y, step = (int64_t)gridDim.x * WARPS;
   pdl_wait();
   float w[NV][E], dw[NV][E];
   const float* weight = p.weight.data + g * p.weight.group;
@@ -719,7 +721,7 @@ __global__ void __launch_bounds__(32 * BACK_WARPS) k_rmsnorm_backward_rows(const
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) dy[i].zero(), s[i].zero(), ds[i].zero();
-  int64_t r = (int64_t)blockIdx.x * BACK_WARPS + warp;
+  int64_t r = (int64_t)blockIdx.x * WARPS + warp;
   load(r);
   for (; r < p.rows; r += step) {
     Raw<T, E> a[NV], b[NV], c3[NV];
@@ -763,7 +765,7 @@ __global__ void __launch_bounds__(32 * BACK_WARPS) k_rmsnorm_backward_rows(const
   for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
     float v = 0.f;
 #pragma unroll
-    for (int q = 0; q < BACK_WARPS; ++q) v += s_dw[q * p.dim + c];
+    for (int q = 0; q < WARPS; ++q) v += s_dw[q * p.dim + c];
     out[c] = v;
   }
 }
@@ -930,13 +932,13 @@ cudaError_t launch_back_shift(const BackArgs& p, const StreamShape& s, int64_t g
 template <typename T>
 cudaError_t launch_back_rows(const BackArgs& p, int nv, int64_t groups, int blocks, cudaStream_t st) {
   constexpr int E = 16 / sizeof(T);
-  auto go = [&](auto kernel) {
-    return launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(32 * BACK_WARPS),
-                      (size_t)BACK_WARPS * p.dim * 4, st, p);
+  auto go = [&](auto kernel, int warps) {
+    return launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(32 * warps),
+                      (size_t)warps * p.dim * 4, st, p);
   };
-  if (nv == 1) return go(k_rmsnorm_backward_rows<T, E, 1>);
-  if (nv == 2) return go(k_rmsnorm_backward_rows<T, E, 2>);
-  return go(k_rmsnorm_backward_rows<T, E, 4>);
+  if (nv == 1) return go(k_rmsnorm_backward_rows<T, E, 1>, BACK_WARPS<1>);
+  if (nv == 2) return go(k_rmsnorm_backward_rows<T, E, 2>, BACK_WARPS<2>);
+  return go(k_rmsnorm_backward_rows<T, E, 4>, BACK_WARPS<4>);
 }
 
 template <typename T, int E>
@@ -1004,9 +1006,10 @@ cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols
 // Every block's sums are written and read once more: four rows or more per block.
 int rmsnorm_backward_blocks(const lipz_rmsnorm_backward_args& a) {
   const int64_t groups = a.groups > 0 ? a.groups : 1;
-  if (backward_row_vectors(a)) {
+  if (const int nv = backward_row_vectors(a)) {
     // two blocks per SM; one block per group, which needs no second launch, from half that many groups on
-    const int64_t fill = 2 * sm_count() / groups, most = ceil_div(a.rows, 2 * BACK_WARPS);
+    const int warps = nv == 1 ? BACK_WARPS<1> : BACK_WARPS<2>;
+    const int64_t fill = 2 * sm_count() / groups, most = ceil_div(a.rows, 2 * warps);
     const int64_t b = fill < 4 ? 1 : fill < most ? fill : most;
     return b < 1 ? 1 : (int)b;
   }

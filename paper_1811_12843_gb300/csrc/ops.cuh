@@ -242,6 +242,36 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
   }
 }
 
+// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a
+// warp; a thread forms 16 bytes at a time.
+template <typename U>
+__device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
+  constexpr int E = 16 / sizeof(U);
+  const int64_t g = r / p.rows;
+  const U* s = (const U*)p.src + g * p.group + (r - g * p.rows) * p.ld;
+  for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) {
+    union {
+      uint4 v;
+      U e[E];
+    } w;
+#pragma unroll
+    for (int i = 0; i < E; ++i) w.e[i] = u * E + i < p.cols ? s[u * E + i] : U(0);
+    ((uint4*)p.dst)[r * p.units + u] = w.v;
+  }
+}
+// Block `b` of 256 threads: 8 rows, of one copy after the other.
+template <typename U>
+__device__ __forceinline__ void copy_rows(const CopyJobs& jobs, int64_t b) {
+  for (int j = 0; j < jobs.n; ++j) {
+    const int64_t blocks = (jobs.c[j].total + COPY_ROWS - 1) / COPY_ROWS;
+    if (b < blocks) {
+      const int64_t r = b * COPY_ROWS + (threadIdx.x >> 5);
+      if (r < jobs.c[j].total) copy_row<U>(jobs.c[j], r);
+      return;
+    }
+    b -= blocks;
+  }
+}
 // The epilogue of element (m, n) of group g, from its sum u.
 __device__ __forceinline__ void finish(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
   if (e.w_scale.data)

@@ -36,6 +36,7 @@ _S_QUANTIZE = struct.Struct("=II3q" + 2 * _MAT + _VEC)
 _S_LINEAR = struct.Struct("=IifI4q" + 5 * _MAT + 3 * _VEC + "QQ")
 _S_LINEAR_BACKWARD = struct.Struct("=IifI4q" + 6 * _MAT + _VEC + "QQ")
 _NO_MAT, _NO_VEC = (0, 0, 0, 0, 0), (0, 0)
+_WIDE = (_BF16, _F32)
 
 
 def _refuse(call, what):
@@ -76,16 +77,18 @@ def _vec(call, name, t, shape, device):
     _refuse_tensor(call, name, t, shape, (_F32,), device)
 
 
-def _first(call, name, t):
-    """(shape, groups, rows, columns, device, its index) that a call's other tensors go by."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+def _first(call, name, t, dtypes):
+    """(shape, groups, rows, columns, device index, matrix) of the tensor that a call's others go by."""
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
         _refuse(call, "%s must be a CUDA tensor" % name)
-    s = t.shape
-    if len(s) == 2:
-        return s, 1, s[0], s[1], t.device, t.get_device()
-    if len(s) != 3:
+    s, st, dtype = t.shape, t.stride(), t.dtype
+    if len(s) != 2 and len(s) != 3:
         _refuse(call, "%s must be [rows, columns] or [groups, rows, columns]" % name)
-    return s, s[0], s[1], s[2], t.device, t.get_device()
+    if dtype not in dtypes or (st[-1] != 1 and s[-1] > 1 and t.numel()):
+        _refuse_tensor(call, name, t, s, dtypes, t.get_device())
+    if len(s) == 2:
+        return s, 1, s[0], s[1], t.get_device(), (t.data_ptr(), 0, st[0], _TYPE[dtype], 0)
+    return s, s[0], s[1], s[2], t.get_device(), (t.data_ptr(), st[0], st[1], _TYPE[dtype], 0)
 
 
 def _act(call, act):
@@ -142,9 +145,9 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, e4m3=False, keep=False, sum_out=
     residual stream updated in place). y has x's type; with ``e4m3`` it is float8_e4m3fn and
     y scale[row] the values. ``keep``: return rstd, which the backward pass reads."""
     call = "rmsnorm"
-    shape, groups, rows, dim, dev, device = _first(call, "x", x)
-    dt = (x.dtype,)
-    mx = _mat(call, "x", x, shape, (_BF16, _F32), device)
+    shape, groups, rows, dim, device, mx = _first(call, "x", x, _WIDE)
+    dev, dtype = x.device, x.dtype
+    dt = (dtype,)
     vw = _vec(call, "weight", weight, (dim,) if len(shape) == 2 else (groups, dim), device)
     if weight is None:
         _refuse(call, "weight must be given")
@@ -154,9 +157,12 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, e4m3=False, keep=False, sum_out=
         total, mr, ms = x, _NO_MAT, _NO_MAT
     else:
         mr = _mat(call, "residual", residual, shape, dt, device)
-        total = torch.empty(shape, dtype=x.dtype, device=dev) if sum_out is None else sum_out
-        ms = _mat(call, "sum_out", total, shape, dt, device)
-    y = torch.empty(shape, dtype=_E4M3 if e4m3 else x.dtype, device=dev)
+        if sum_out is None:
+            total = torch.empty(shape, dtype=dtype, device=dev)
+            ms = (total.data_ptr(), rows * dim, dim, mx[3], 0)
+        else:
+            total, ms = sum_out, _mat(call, "sum_out", sum_out, shape, dt, device)
+    y = torch.empty(shape, dtype=_E4M3 if e4m3 else dtype, device=dev)
     scale = torch.empty(shape[:-1], dtype=_F32, device=dev) if e4m3 else None
     rstd = torch.empty(shape[:-1], dtype=_F32, device=dev) if keep else None
     _run("lipz_rmsnorm", _S_RMSNORM.pack(
@@ -170,20 +176,18 @@ def rmsnorm_backward(dy, s, rstd, weight, dsum=None, want_dweight=True):
     """(dx, dweight) of rmsnorm: from its ``sum`` and ``rstd``, y's gradient, and dsum, the gradient
     that reaches the sum from elsewhere. dx is the gradient of x and of residual; dweight is fp32."""
     call = "rmsnorm_backward"
-    shape, groups, rows, dim, dev, device = _first(call, "s", s)
-    lead, dt = shape[:-2], (s.dtype,)
+    shape, groups, rows, dim, device, ms = _first(call, "s", s, _WIDE)
+    dev, lead, dt = s.device, shape[:-2], (s.dtype,)
     if dy is None or weight is None or rstd is None:
         _refuse(call, "dy, rstd and weight must be given")
-    mats = (_mat(call, "dy", dy, shape, dt, device)
-            + _mat(call, "s", s, shape, (_BF16, _F32), device)
-            + _mat(call, "dsum", dsum, shape, dt, device))
+    mats = _mat(call, "dy", dy, shape, dt, device) + ms + _mat(call, "dsum", dsum, shape, dt, device)
     vecs = (_vec(call, "weight", weight, lead + (dim,), device)
             + _vec(call, "rstd", rstd, shape[:-1], device))
     dx = torch.empty(shape, dtype=s.dtype, device=dev)
     dweight = torch.empty(lead + (dim,), dtype=_F32, device=dev) if want_dweight else None
     _run_with_space("lipz_rmsnorm_backward", _S_RMSNORM_BACKWARD,
                     (_S_RMSNORM_BACKWARD.size, 0, groups, rows, dim, *mats, dx.data_ptr(), rows * dim,
-                     dim, _TYPE[s.dtype], 0, *vecs, dweight.data_ptr() if want_dweight else 0, dim),
+                     dim, ms[3], 0, *vecs, dweight.data_ptr() if want_dweight else 0, dim),
                     dev, device)
     return dx, dweight
 
@@ -192,8 +196,8 @@ def quantize_rows(x):
     """(q, scale): x [.., rows, columns] (bf16 or fp32) in float8_e4m3fn with an fp32 scale per row,
     q scale the values."""
     call = "quantize_rows"
-    shape, groups, rows, dim, dev, device = _first(call, "x", x)
-    mx = _mat(call, "x", x, shape, (_BF16, _F32), device)
+    shape, groups, rows, dim, device, mx = _first(call, "x", x, _WIDE)
+    dev = x.device
     q = torch.empty(shape, dtype=_E4M3, device=dev)
     scale = torch.empty(shape[:-1], dtype=_F32, device=dev)
     _run("lipz_quantize_rows",
@@ -210,12 +214,12 @@ def linear(x, w, bias=None, act="none", slope=0.2, residual=None, x_scale=None, 
     y: out_dtype (bf16 or fp32). y is written to ``out`` if given (it may be the residual). ``keep``:
     pre is u in bf16, which the backward pass reads (else None)."""
     call = "linear"
-    x_shape, groups, rows, k, dev, device = _first(call, "x", x)
+    x_shape, groups, rows, k, device, mx = _first(call, "x", x, (_BF16, _E4M3))
+    dev = x.device
     if not isinstance(w, torch.Tensor) or w.dim() != len(x_shape):
         _refuse(call, "w must be a CUDA tensor with x's number of dimensions")
     lead, n = x_shape[:-2], w.shape[-2]
     shape, row, code = lead + (rows, n), lead + (n,), _act(call, act)
-    mx = _mat(call, "x", x, x_shape, (_BF16, _E4M3), device)
     mw = _mat(call, "w", w, lead + (n, k), (x.dtype,), device)
     if out_dtype is not _BF16 and out_dtype is not _F32:
         _refuse(call, "out_dtype must be bfloat16 or float32")
@@ -242,18 +246,19 @@ def linear_backward(dy, x, w, act="none", slope=0.2, pre=None, want_dx=True, wan
     """(dx, dw, db) of linear over bf16 operands: du = dy act'(pre), dx = du w, dw = du^T x, db the
     sums of du over the rows; None for what is not wanted. The residual's gradient is dy."""
     call = "linear_backward"
-    shape, groups, rows, n, dev, device = _first(call, "dy", dy)
+    bf = (_BF16,)
+    shape, groups, rows, n, device, mdy = _first(call, "dy", dy, bf)
+    dev = dy.device
     if not isinstance(x, torch.Tensor) or x.dim() != len(shape):
         _refuse(call, "x must be a CUDA tensor with dy's number of dimensions")
     if w is None:
         _refuse(call, "w must be given")
-    lead, k, bf, code = shape[:-2], x.shape[-1], (_BF16,), _act(call, act)
+    lead, k, code = shape[:-2], x.shape[-1], _act(call, act)
     if code and pre is None:
         _refuse(call, "act %r needs pre" % act)
     if dw_dtype is not _BF16 and dw_dtype is not _F32:
         _refuse(call, "dw_dtype must be bfloat16 or float32")
-    mats = (_mat(call, "dy", dy, shape, bf, device)
-            + _mat(call, "x", x, lead + (rows, k), bf, device)
+    mats = (mdy + _mat(call, "x", x, lead + (rows, k), bf, device)
             + _mat(call, "w", w, lead + (n, k), bf, device)
             + _mat(call, "pre", pre if code else None, shape, bf, device))
     dx = torch.empty(lead + (rows, k), dtype=_BF16, device=dev) if want_dx else None
