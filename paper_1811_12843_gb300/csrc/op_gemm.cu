@@ -29,7 +29,8 @@ constexpr int EPI_WARPS = 16, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WAR
 constexpr int TURN = 32 * 17 * 4;         // a warp's block for turning rows into columns
 constexpr int MN_BOX = 64 * ROW;          // 64 k by 64 m (or n) of an operand whose rows run along m (n)
 constexpr int SUM_CHUNKS = 8;             // chunks of k whose sum stands in tensor memory, for fp32 results
-constexpr int SMEM_MAX = 232448, STAGES_MAX = 8;
+constexpr int SMEM_MAX = 232448, STAGES_MAX = 20;
+constexpr int DIRECT_CHUNKS = 4;          // most chunks of k per CTA whose operands the result warps bring
 
 // A tile's parameters for the result warps.
 struct Slot {
@@ -49,13 +50,16 @@ struct Shape {
   static constexpr int A_BYTES = 128 * ROW, B_BYTES = BN / CG * ROW, STAGE = A_BYTES + B_BYTES;
   // after the stages: the slots, each with {bias, w_scale}[BN] and x_scale[128]; partial sums; barriers
   static constexpr int SLOT = sizeof(Slot) + (2 * BN + 128) * 4;
-  static constexpr int SUMS = EPI_WARPS * 32 * 4, BARS = 320;
-  static constexpr int smem(int stages, bool turn) {
-    return 1024 + stages * STAGE + SLOTS * (TILE + SLOT) + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
+  static constexpr int SUMS = EPI_WARPS * 32 * 4, BARS = 512;
+  // a_rows: of A's box, fewer than 128 where m has fewer (the MMAs then read past them, into what follows:
+  // rows of the sums that nobody reads)
+  static constexpr int stage(int a_rows) { return a_rows * ROW + B_BYTES; }
+  static constexpr int smem(int stages, int a_rows, bool turn) {
+    return 1024 + stages * stage(a_rows) + (128 - a_rows) * ROW + SLOTS * (TILE + SLOT) + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
   }
-  static constexpr int stages(bool turn) {
-    int n = STAGES_MAX;
-    while (smem(n, turn) > SMEM_MAX) --n;
+  static constexpr int stages(int a_rows, bool turn) {
+    int n = a_rows < 128 ? STAGES_MAX : 8;
+    while (smem(n, a_rows, turn) > SMEM_MAX) --n;
     return n;
   }
 };
@@ -80,6 +84,8 @@ struct Problem {
   int64_t ldp;
   int groups, m, n, tiles_m, tiles_n, tiles, units, splits, chunks, chunks_per_split;
   int parts;             // SPLIT: CTAs of a cluster (and splits is 1)
+  const uint8_t *a_rows, *b_rows;            // DIRECT: the operands, and their strides and k in bytes
+  int64_t a_group, a_ld, b_group, b_ld, k_bytes;
   Divisor by_split, by_group, by_panel, by_rest;  // splits, tiles, 8 tiles_n, rows of the last panel
   int a_bytes;               // of A's box per CTA and stage
   int az, bz;                // 0: one matrix for every group
@@ -94,7 +100,7 @@ struct GemmParams {
   CUtensorMap residual, y;  // VIA: boxes of 32 columns by 128 and 32 rows
   Problem p[NP];
   PartSums sums;
-  int units, stages;
+  int units, stages, stage_bytes, a_rows;  // a_rows: of A in a stage
   int* err;
 };
 
@@ -260,6 +266,23 @@ __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int col
     if (r < rows && col < cols) base[r * ld + col] = from_f<T>(turn[r * 17 + col]);
 }
 
+// 16 bytes from any address, the first n of them, then zeros: the aligned words that hold them, shifted.
+__device__ __forceinline__ uint4 bytes16(const uint8_t* p, int64_t n) {
+  if (n <= 0) return make_uint4(0, 0, 0, 0);
+  const int off = (int)((uint64_t)p & 3), left = n < 16 ? (int)n : 16;
+  const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
+  uint32_t w[5], r[4];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = 4 * i < off + left ? __ldg(q + i) : 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = __funnelshift_r(w[i], w[i + 1], off * 8);
+    const int keep = left - 4 * i;  // bytes of this word
+    if (keep < 4) r[i] = keep <= 0 ? 0u : r[i] & ((1u << 8 * keep) - 1u);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
 __device__ __forceinline__ int64_t ceil_div_d(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // A unit's place: which part of k of which tile; groups outermost, then panels of 8 tile rows, along which
@@ -282,20 +305,22 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
 // -> 768 (of 47 and 88 us in all).
 // SPLIT: a cluster of CTAs shares a tile, each with a part of k; their sums are added over the cluster's
 // shared memory, each CTA finishing a part of the columns. One tile per cluster.
-template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA, bool SPLIT>
+// DIRECT: the result warps bring the operands first, from rows that TMA does not take.
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA, bool SPLIT, bool DIRECT>
 __global__ void __launch_bounds__(THREADS, 1)
     k_gemm_op(const __grid_constant__ GemmParams<FORWARD ? 1 : 2> prm) {
   using S = Shape<CG, BN, VIA>;
   constexpr bool SUMS = sizeof(T) == 4;
   static_assert(!VIA || (FORWARD && !SUMS && S::COLSW == 32), "boxes of 32 bf16 columns");
-  static_assert(!SPLIT || (FORWARD && CG == 1 && !VIA && 128 * (BN + 1) * 4 <= 2 * S::STAGE), "sums of a tile");
+  static_assert(!SPLIT || (FORWARD && CG == 1 && !VIA && 128 * (BN + 1) * 4 <= 5 * S::B_BYTES), "sums of a tile");
   constexpr int BM = 128 * CG, COLSW = S::COLSW, ACCS = S::ACCS, SLOTS = S::SLOTS;
   constexpr int CW = COLSW < 32 ? COLSW : 32;       // a result warp's columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
   extern __shared__ uint8_t smem_raw[];
-  const int stages = prm.stages;
+  const int stages = prm.stages, stage_bytes = FORWARD ? prm.stage_bytes : S::STAGE;
+  const int a_stage = FORWARD ? prm.a_rows * ROW : S::A_BYTES;
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* tiles = smem_raw + (base - raw) + stages * S::STAGE;  // [SLOTS][BN / 32][128 rows][64 bytes]
+  uint8_t* tiles = smem_raw + (base - raw) + stages * stage_bytes + (S::A_BYTES - a_stage);  // [SLOTS][BN / 32][128 rows][64 bytes]
   uint8_t* slots = tiles + SLOTS * S::TILE;
   float* s_sum = reinterpret_cast<float*>(slots + SLOTS * S::SLOT);
   uint64_t* bars = reinterpret_cast<uint64_t*>(slots + SLOTS * S::SLOT + S::SUMS);
@@ -303,16 +328,16 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t bFull = tc::smem_u32(bars), bEmpty = bFull + 8 * STAGES_MAX;
   const uint32_t bAcc = bEmpty + 8 * STAGES_MAX, bFree = bAcc + 8 * ACCS;
   const uint32_t bSlot = bFree + 8 * ACCS, bRead = bSlot + 8 * SLOTS;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + 33);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 34);
-  int* code = reinterpret_cast<int*>(bars + 35);
-  static_assert(2 * STAGES_MAX + 2 * ACCS + 2 * SLOTS <= 33, "barriers");
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + 60);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 61);
+  int* code = reinterpret_cast<int*>(bars + 62);
+  static_assert(2 * STAGES_MAX + 2 * ACCS + 2 * SLOTS <= 60, "barriers");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? tc::cluster_ctarank() : 0;
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
-      tc::mbar_init(bFull + 8 * s, 2);  // A's and B's issuers
+      tc::mbar_init(bFull + 8 * s, DIRECT ? EPI_WARPS : 2);  // who brings: all, or A's and B's issuers
       tc::mbar_init(bEmpty + 8 * s, 1);
     }
     for (int r = 0; r < ACCS; ++r) {
@@ -377,7 +402,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   };
   pdl_wait();
 
-  if (warp < 2) {
+  if (DIRECT && warp < 2) {
+  } else if (warp < 2) {
     // ============ TMA: warp 0 loads A, warp 1 loads B (both CTAs of a pair) ============
     const bool elected = tc::elect_one(), is_a = warp == 0;
     const int rows = is_a ? 128 : BN / CG;
@@ -400,7 +426,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           ok = false;
           break;
         }
-        const uint32_t dst = base + stage * S::STAGE + (is_a ? 0 : S::A_BYTES);
+        const uint32_t dst = base + stage * stage_bytes + (is_a ? 0 : a_stage);
         const uint32_t full = lFull + 8 * stage;
         if (elected) {
           // the leader expects both CTAs' bytes; the peer's may land first
@@ -456,7 +482,7 @@ __global__ void __launch_bounds__(THREADS, 1)
               break;
             }
             tc::tc_fence_after();
-            const uint32_t sA = base + stage * S::STAGE, sB = sA + S::A_BYTES;
+            const uint32_t sA = base + stage * stage_bytes, sB = sA + a_stage;
             const uint64_t dA = a_mn ? tc::sw128_mn_desc(sA, MN_BOX) : tc::sw128_desc(sA);
             const uint64_t dB = b_mn ? tc::sw128_mn_desc(sB, MN_BOX) : tc::sw128_desc(sB);
             if (elected) {
@@ -577,6 +603,35 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     int sums = 0;
     bool ok = true;
+    if constexpr (DIRECT) {
+      static_assert(SPLIT, "one unit");
+      const Problem& p = prm.p[0];
+      const Place pl = unit_place(0);
+      const int rows_a = min(prm.a_rows, p.m - pl.mt * BM), units = (rows_a + min(BN, p.n - pl.nt * BN)) * 8;
+      const uint8_t* a = p.a_rows + pl.g * p.a_group + (int64_t)(pl.mt * BM) * p.a_ld;
+      const uint8_t* b = p.b_rows + pl.g * p.b_group + (int64_t)(pl.nt * BN) * p.b_ld;
+      int c0, c1;
+      chunk_range(p, pl.split, c0, c1);
+      for (int kc = c0; kc < c1 && ok; ++kc) {
+        const int stage = (kc - c0) % stages;
+        ok = wait(bEmpty + 8 * stage, (uint32_t)((kc - c0) / stages & 1) ^ 1u, abort_flag, code, 1);
+        const uint32_t dst = base + stage * stage_bytes;
+#pragma unroll 2
+        for (int i = ew * 32 + lane; i < units; i += 32 * EPI_WARPS) {
+          const int r = i >> 3, u = i & 7, rb = r - rows_a;
+          const int64_t at = (int64_t)kc * ROW + u * 16;
+          const uint4 v = bytes16(rb < 0 ? a + r * p.a_ld + at : b + rb * p.b_ld + at, p.k_bytes - at);
+          const int row = rb < 0 ? r : rb;
+          const uint32_t to = dst + (rb < 0 ? 0 : a_stage) + row * ROW + ((u ^ (row & 7)) << 4);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z),
+                       "r"(v.w)
+                       : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bFull + 8 * stage);
+      }
+    }
     auto wait_sum = [&]() {
       ok = __all_sync(0xffffffffu, wait(bAcc + 8 * (sums % ACCS), (uint32_t)(sums / ACCS) & 1, abort_flag, code, 4));
       tc::tc_fence_after();
@@ -934,7 +989,7 @@ cudaError_t prepare_kernel(K kernel, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false>
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false, bool DIRECT = false>
 cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
                    cudaStream_t st) {
   using S = Shape<CG, BN, VIA>;
@@ -951,8 +1006,13 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
     p.b_blocked = p.b_mn && g.n % 64 == 0;
     const int arows = p.a_mn ? 64 : (int)(g.m >= 128 ? 128 : ceil_div(g.m, 8) * 8);
     const int brows = p.b_mn ? 64 : BN / CG;
-    if (!encode(&k.a[i], g.a, xa, g.groups, TYPE, arows, p.a_blocked ? 2 : 0) ||
-        !encode(&k.b[i], g.b, xb, g.groups, TYPE, brows, p.b_blocked ? BN / CG / 64 : 0))
+    if (DIRECT) {
+      const int eb = type_bytes(TYPE);
+      p.a_rows = (const uint8_t*)g.a.data, p.b_rows = (const uint8_t*)g.b.data;
+      p.a_group = g.a.group * eb, p.a_ld = g.a.ld * eb, p.b_group = g.b.group * eb, p.b_ld = g.b.ld * eb;
+      p.k_bytes = g.k * eb;
+    } else if (!encode(&k.a[i], g.a, xa, g.groups, TYPE, arows, p.a_blocked ? 2 : 0) ||
+               !encode(&k.b[i], g.b, xb, g.groups, TYPE, brows, p.b_blocked ? BN / CG / 64 : 0))
       return cudaErrorInvalidValue;
     p.e = g.e;
     p.part = parts[i];
@@ -984,9 +1044,12 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   }
   if (sums) k.sums = *sums;
   k.err = timeout_word();
-  k.stages = S::stages(turn);
+  const Gemm& first = q.g[0];
+  k.a_rows = FORWARD && CG == 1 && first.m < 128 ? (int)ceil_div(first.m, 8) * 8 : 128;
+  k.stage_bytes = S::stage(k.a_rows);
+  k.stages = S::stages(k.a_rows, turn);
   static std::atomic<uint64_t> done{0};
-  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T, VIA, SPLIT>;
+  auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T, VIA, SPLIT, DIRECT>;
   cudaError_t e = prepare_kernel(kernel, done);
   if (e != cudaSuccess) return e;
   const int cluster = SPLIT ? k.p[0].parts : CG, slots = SPLIT ? k.units : sm_count() / CG;
@@ -994,7 +1057,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = S::smem(k.stages, turn);
+  cfg.dynamicSmemBytes = S::smem(k.stages, k.a_rows, turn);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1020,6 +1083,10 @@ template <int TYPE, bool FORWARD>
 cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* parts, const PartSums* sums,
                          cudaStream_t st) {
   if constexpr (FORWARD) {
+    if (p.direct)
+      return q.g[0].e.y.type == LIPZ_FP32
+                 ? launch<TYPE, 1, 64, true, float, false, true, true>(q, p, parts, sums, st)
+                 : launch<TYPE, 1, 64, true, bf16, false, true, true>(q, p, parts, sums, st);
     if (p.p[0].splits > 1)
       return q.g[0].e.y.type == LIPZ_FP32 ? launch<TYPE, 1, 64, true, float, false, true>(q, p, parts, sums, st)
                                           : launch<TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
@@ -1100,6 +1167,25 @@ GemmPlan plan_products(const Products& q) {
       if (best < 0 || time < best) best = time, plan = t;
     }
   }
+  if (forward) {
+    // Rows that TMA does not take: brought by the result warps where one wave of small tiles is all, so that
+    // no copies have to be made first (37 x 1000 -> 500 over 8-bit operands: 12 us with the copies' launch,
+    // 8 without). As many parts of k as there are CTAs for.
+    const Extent xa = extent(g0.a, g0.m, g0.k), xb = extent(g0.b, g0.n, g0.k);
+    GemmPlan t{};
+    GemmPlan::One& o = t.p[0];
+    o.tiles_m = ceil_div(g0.m, 128), o.tiles_n = ceil_div(g0.n, 64), o.chunks = ceil_div(g0.k * eb, ROW);
+    const int64_t tiles = o.tiles_m * o.tiles_n * g0.groups;
+    if ((!tma_takes(g0.a, xa, g0.groups, eb) || !tma_takes(g0.b, xb, g0.groups, eb)) && tiles <= sms) {
+      t.direct = true, t.cg = 1, t.bn = 64;
+      for (int s0 = 8; s0 >= 1; s0 /= 2) {
+        o.chunks_per_split = ceil_div(o.chunks, s0 < o.chunks ? s0 : o.chunks);
+        o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);
+        if (o.splits == s0 && tiles * s0 <= sms) break;
+      }
+      if (o.chunks_per_split <= DIRECT_CHUNKS) plan = t;
+    }
+  }
   plan_space(q, &plan);
   return plan;
 }
@@ -1111,8 +1197,8 @@ void plan_space(const Products& q, GemmPlan* plan) {
     const Gemm& g = q.g[i];
     GemmPlan::One& o = plan->p[i];
     const Extent xa = extent(g.a, g.m, g.k), xb = extent(g.b, g.n, g.k);
-    o.copy_a = !tma_takes(g.a, xa, g.groups, eb);
-    o.copy_b = !tma_takes(g.b, xb, g.groups, eb);
+    o.copy_a = !plan->direct && !tma_takes(g.a, xa, g.groups, eb);
+    o.copy_b = !plan->direct && !tma_takes(g.b, xb, g.groups, eb);
     o.lda = ceil_div(xa.cols, unit) * unit;
     o.ldb = ceil_div(xb.cols, unit) * unit;
     o.a_bytes = o.copy_a ? round256(g.groups * xa.rows * o.lda * eb) : 0;

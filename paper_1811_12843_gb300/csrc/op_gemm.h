@@ -61,6 +61,7 @@ struct GemmPlan {
     uint64_t a_bytes, b_bytes, part_bytes;
   } p[2];
   int cg, bn;
+  bool direct;  // operands from rows that TMA does not take, without copies
   uint64_t bytes;
 };
 GemmPlan plan_products(const Products& q);
