@@ -779,9 +779,18 @@ __global__ void __launch_bounds__(1024)
   pdl_wait();
   float v = 0.f;
   if (c < cols) {
+    // (sixteen loads in flight: 608 parts of 4096 columns took 13 us with as many as the compiler chose)
     const float* p = part + g * parts * cols + c;
-#pragma unroll 16
-    for (int i = threadIdx.y; i < parts; i += blockDim.y) v += p[i * cols];
+    for (int i0 = threadIdx.y; i0 < parts; i0 += 16 * blockDim.y) {
+      float w[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int i = i0 + j * blockDim.y;
+        w[j] = i < parts ? __ldg(p + i * cols) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v += w[j];
+    }
   }
   s[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
