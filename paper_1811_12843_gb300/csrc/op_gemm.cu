@@ -9,7 +9,6 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
-#include <stdlib.h>
 #include <string.h>
 
 #include <atomic>
@@ -1127,13 +1126,10 @@ GemmPlan plan_products(const Products& q) {
   const bool by_tma = results_by_tma(g0), forward = g0.a.k_major && g0.b.k_major;
   const int sms = sm_count();
   double best = -1;
-  static const int force_cg = getenv("OPCG") ? atoi(getenv("OPCG")) : 0, force_bn = getenv("OPBN") ? atoi(getenv("OPBN")) : 0, force_s = getenv("OPS") ? atoi(getenv("OPS")) : 0;
   for (const Shape& shape : shapes) {
     if (sums && shape.bn > 128) continue;
-    if (force_cg && (shape.cg != force_cg || shape.bn != force_bn)) continue;
     // a forward's parts of k are a cluster's CTAs, all clusters resident at once
     for (int s0 = 1; s0 <= (forward ? 8 : 64); s0 *= 2) {
-      if (force_s && s0 != force_s) continue;
       if (forward && s0 > 1 && shape.bn != 64) continue;
       const Shape& c = by_tma && s0 == 1 && shape.cg == 2 && shape.bn == 128 ? via : shape;
       const int64_t slots = sms / c.cg;
@@ -1160,10 +1156,12 @@ GemmPlan plan_products(const Products& q) {
         if (o.splits > 1 && !forward) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000;
         split = split || o.splits > 1;
       }
-      if ((!fits && (!force_cg || forward)) || (s0 > 1 && !split)) continue;
+      if (!fits || (s0 > 1 && !split)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
-      const double time = waves * top + last + extra + (!split ? 0 : forward ? 2000 : 9500);
+      // (a cluster's CTA finishes 64 / s0 columns of up to 128 rows, an element per thread and turn)
+      const double join = 4500 + 70.0 / s0 * (g0.m < 128 ? g0.m : 128);
+      const double time = waves * top + last + extra + (!split ? 0 : forward ? join : 9500);
       if (best < 0 || time < best) best = time, plan = t;
     }
   }
