@@ -340,7 +340,7 @@ LIPZ_API int lipz_fitness_from_logits_noalloc(const float* logits, int32_t cells
  *   - A matrix is [groups][rows][cols] with element strides between groups and between rows; its
  *     columns are adjacent. Groups are independent problems of one size (the individuals of a
  *     population). A group stride of 0 shares an input between all groups; an output's matrices and
- *     rows must not overlap. A vector is [groups][n], its n elements adjacent.
+ *     rows must not overlap, nor an output an input unless its call says so. A vector is [groups][n], its n elements adjacent.
  *   - Data must be aligned to its element type; nothing else is asked of addresses and strides (rows
  *     of whole 16-byte units from 16-byte boundaries are the fast case).
  *   - groups or rows may be 0 (weight gradients over no rows are zeros); column counts are at least 1.

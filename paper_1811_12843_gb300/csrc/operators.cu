@@ -200,7 +200,8 @@ int check(const lipz_linear_args* a) {
   Check c{"lipz_linear"};
   if (!struct_ok(a, c.call, &c.rc)) return c.rc;
   c.groups = a->groups, c.rows = a->rows;
-  if (!c.extents() || !c.extent(a->k, 1, MAX_EXTENT, "k") || !c.extent(a->n, 1, MAX_EXTENT, "n"))
+  if (!c.extents() || !c.extent(a->k, 1, MAX_EXTENT, "k") || !c.extent(a->n, 1, MAX_EXTENT, "n") ||
+      !c.want(a->groups * a->n <= MAX_EXTENT, "groups x n must stay below 2^31"))
     return c.rc;
   c.extent(a->act, LIPZ_ACT_NONE, LIPZ_ACT_SILU, "act");
   c.mat(a->x, "x", a->rows, a->k, B16 | F8, false);
@@ -220,7 +221,8 @@ int check(const lipz_linear_backward_args* a) {
   Check c{"lipz_linear_backward"};
   if (!struct_ok(a, c.call, &c.rc)) return c.rc;
   c.groups = a->groups, c.rows = a->rows;
-  if (!c.extents() || !c.extent(a->k, 1, MAX_EXTENT, "k") || !c.extent(a->n, 1, MAX_EXTENT, "n"))
+  if (!c.extents() || !c.extent(a->k, 1, MAX_EXTENT, "k") || !c.extent(a->n, 1, MAX_EXTENT, "n") ||
+      !c.want(a->groups * a->n <= MAX_EXTENT, "groups x n must stay below 2^31"))
     return c.rc;
   c.extent(a->act, LIPZ_ACT_NONE, LIPZ_ACT_SILU, "act");
   c.mat(a->dy, "dy", a->rows, a->n, B16, false);

@@ -5,7 +5,7 @@
 forward and backward in bf16, and forward over 8-bit operands, for one network or for a population
 of them: tensors are [rows, columns], or [groups, rows, columns] with weights per group. Columns
 must be adjacent; rows and groups may be strided, and a group stride of 0 (``expand``) shares an
-input between the groups. Every call runs the library's CUDA kernels on the current stream of the
+input between the groups. An output may not overlap an input unless its call says so. Every call runs the library's CUDA kernels on the current stream of the
 tensors' device, allocates its outputs as torch does, waits for nothing, and may be captured in a
 CUDA graph. What the library does not take raises ``LipzError`` with nothing launched. Nothing here
 records an autograd graph: the backward passes are calls of their own.
@@ -242,9 +242,10 @@ def linear(x, w, bias=None, act="none", slope=0.2, residual=None, x_scale=None, 
 
 
 def linear_backward(dy, x, w, act="none", slope=0.2, pre=None, want_dx=True, want_dw=True,
-                    want_db=True, dw_dtype=torch.bfloat16):
+                    want_db=True, dx_dtype=torch.bfloat16, dw_dtype=torch.bfloat16):
     """(dx, dw, db) of linear over bf16 operands: du = dy act'(pre), dx = du w, dw = du^T x, db the
-    sums of du over the rows; None for what is not wanted. The residual's gradient is dy."""
+    sums of du over the rows (fp32); None for what is not wanted. dx and dw: bf16 or fp32. The
+    residual's gradient is dy."""
     call = "linear_backward"
     bf = (_BF16,)
     shape, groups, rows, n, device, mdy = _first(call, "dy", dy, bf)
@@ -256,15 +257,15 @@ def linear_backward(dy, x, w, act="none", slope=0.2, pre=None, want_dx=True, wan
     lead, k, code = shape[:-2], x.shape[-1], _act(call, act)
     if code and pre is None:
         _refuse(call, "act %r needs pre" % act)
-    if dw_dtype is not _BF16 and dw_dtype is not _F32:
-        _refuse(call, "dw_dtype must be bfloat16 or float32")
+    if dx_dtype not in _WIDE or dw_dtype not in _WIDE:
+        _refuse(call, "dx_dtype and dw_dtype must be bfloat16 or float32")
     mats = (mdy + _mat(call, "x", x, lead + (rows, k), bf, device)
             + _mat(call, "w", w, lead + (n, k), bf, device)
             + _mat(call, "pre", pre if code else None, shape, bf, device))
-    dx = torch.empty(lead + (rows, k), dtype=_BF16, device=dev) if want_dx else None
+    dx = torch.empty(lead + (rows, k), dtype=dx_dtype, device=dev) if want_dx else None
     dw = torch.empty(lead + (n, k), dtype=dw_dtype, device=dev) if want_dw else None
     db = torch.empty(lead + (n,), dtype=_F32, device=dev) if want_db else None
-    mx = (dx.data_ptr(), rows * k, k, LIPZ_BF16, 0) if want_dx else _NO_MAT
+    mx = (dx.data_ptr(), rows * k, k, _TYPE[dx_dtype], 0) if want_dx else _NO_MAT
     mw = (dw.data_ptr(), n * k, k, _TYPE[dw_dtype], 0) if want_dw else _NO_MAT
     _run_with_space("lipz_linear_backward", _S_LINEAR_BACKWARD,
                     (_S_LINEAR_BACKWARD.size, code, slope, 0, groups, rows, k, n, *mats, *mx, *mw,

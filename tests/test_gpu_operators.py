@@ -520,6 +520,37 @@ def test_linear_gradients_are_those_of_the_forward(act):
             assert abs((d(got) * v).sum() - diff) <= 2.0 ** -7 * size + 1e-6
 
 
+@pytest.mark.parametrize("groups,rows,k,n", [(1, 4, 64, 16), (2, 300, 500, 333), (1, 777, 784, 256),
+                                             (1, 5000, 96, 64)])
+@pytest.mark.parametrize("dx_dtype,dw_dtype", [(F32, F32), (F32, BF16), (BF16, F32)])
+def test_linear_backward_result_types(groups, rows, k, n, dx_dtype, dw_dtype):
+    """Without an activation the deltas are exact, and fp32 gradients as near as fp32 sums; a gradient's
+    values do not depend on whether the other is asked for."""
+    dy, x = randn(111, norm_shape(groups, rows, n), 0.1), randn(112, norm_shape(groups, rows, k))
+    w = randn(113, norm_shape(groups, n, k), k ** -0.5)
+    kw = dict(dx_dtype=dx_dtype, dw_dtype=dw_dtype)
+    dx, dw, db = ops.linear_backward(dy, x, w, **kw)
+    assert dx.dtype == dx_dtype and dw.dtype == dw_dtype
+    _, rx, rw, rb = backward_ref(dy, x, w, "none", None)
+    within(dx, rx, ROUND[dx_dtype] * rx.abs() + sum_error(n) * (d(dy).abs() @ d(w).abs()), "dx")
+    within(dw, rw, ROUND[dw_dtype] * rw.abs()
+           + sum_error(rows) * (d(dy).abs().transpose(-1, -2) @ d(x).abs()), "dw")
+    within(db, rb, (rows + 16) * 2.0 ** -24 * d(dy).abs().sum(dim=-2), "db")
+    assert torch.equal(ops.linear_backward(dy, x, w, want_dw=False, **kw)[0], dx)
+    assert torch.equal(ops.linear_backward(dy, x, w, want_dx=False, **kw)[1], dw)
+
+
+@pytest.mark.parametrize("k", [1024, 8192])
+def test_linear_sums_in_fp32_stay_near_64_bits(k):
+    """The tensor cores truncate; fp32 results add their sums over 512 k in registers. Relative error in
+    the 2-norm: below 2^-20, whatever k."""
+    x, w = randn(114, (300, k)), randn(115, (200, k), k ** -0.5)
+    u = d(x) @ d(w).T
+    for rows in (300, 20):
+        y, _ = ops.linear(x[:rows], w, out_dtype=F32)
+        assert (d(y) - u[:rows]).norm() < 2.0 ** -20 * u[:rows].norm()
+
+
 # ---- streams, graphs, refusals ------------------------------------------------------------------------
 def _block(x, stream, w):
     r = ops.rmsnorm(x, w["g"], residual=stream, e4m3=True)
