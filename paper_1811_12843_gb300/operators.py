@@ -98,35 +98,41 @@ def _act(call, act):
     return code
 
 
-# the handle of the device's current stream, without the object around it
+# the handle of the device's current stream, and the current device, without the objects around them
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _raise(rc):
+    raise LipzError(rc, lipz_operator_error())
 
 
 def _run(name, args, device):
     """The library's call on the device's current stream."""
-    if device != torch.cuda.current_device():
+    if device != _current():
         with torch.cuda.device(device):
             return _run(name, args, device)
     rc = getattr(load(), name)(args, _stream(device))
-    if rc != LIPZ_OK:
-        raise LipzError(rc, lipz_operator_error())
+    if rc:
+        _raise(rc)
 
 
-def _run_with_space(name, struct_, fields, dev, device):
+def _run_with_space(name, query, struct_, fields, dev, device):
     """The call with the workspace that it asks for."""
-    if device != torch.cuda.current_device():
+    if device != _current():
         with torch.cuda.device(device):
-            return _run_with_space(name, struct_, fields, dev, device)
-    need = ctypes.c_uint64()
-    args = struct_.pack(*fields, 0, 0)
-    rc = getattr(load(), name + "_workspace")(args, ctypes.byref(need))
-    if rc != LIPZ_OK:
-        raise LipzError(rc, lipz_operator_error())
+            return _run_with_space(name, query, struct_, fields, dev, device)
+    lib, need, args = load(), ctypes.c_uint64(), struct_.pack(*fields, 0, 0)
+    rc = getattr(lib, query)(args, ctypes.byref(need))
+    if rc:
+        _raise(rc)
     if need.value:
         work = torch.empty(need.value, dtype=torch.uint8, device=dev)
         args = struct_.pack(*fields, work.data_ptr(), need.value)
-    _run(name, args, device)
+    rc = getattr(lib, name)(args, _stream(device))
+    if rc:
+        _raise(rc)
 
 
 class Norm(NamedTuple):
@@ -148,7 +154,9 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, e4m3=False, keep=False, sum_out=
     shape, groups, rows, dim, device, mx = _first(call, "x", x, _WIDE)
     dev, dtype = x.device, x.dtype
     dt = (dtype,)
-    vw = _vec(call, "weight", weight, (dim,) if len(shape) == 2 else (groups, dim), device)
+    two = len(shape) == 2
+    per_row, per_col = ((rows,), (dim,)) if two else ((groups, rows), (groups, dim))
+    vw = _vec(call, "weight", weight, per_col, device)
     if weight is None:
         _refuse(call, "weight must be given")
     if residual is None:
@@ -163,8 +171,8 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, e4m3=False, keep=False, sum_out=
         else:
             total, ms = sum_out, _mat(call, "sum_out", sum_out, shape, dt, device)
     y = torch.empty(shape, dtype=_E4M3 if e4m3 else dtype, device=dev)
-    scale = torch.empty(shape[:-1], dtype=_F32, device=dev) if e4m3 else None
-    rstd = torch.empty(shape[:-1], dtype=_F32, device=dev) if keep else None
+    scale = torch.empty(per_row, dtype=_F32, device=dev) if e4m3 else None
+    rstd = torch.empty(per_row, dtype=_F32, device=dev) if keep else None
     _run("lipz_rmsnorm", _S_RMSNORM.pack(
         _S_RMSNORM.size, eps, groups, rows, dim, *mx, *mr, *ms,
         y.data_ptr(), rows * dim, dim, LIPZ_E4M3 if e4m3 else mx[3], 0, *vw,
@@ -177,15 +185,15 @@ def rmsnorm_backward(dy, s, rstd, weight, dsum=None, want_dweight=True):
     that reaches the sum from elsewhere. dx is the gradient of x and of residual; dweight is fp32."""
     call = "rmsnorm_backward"
     shape, groups, rows, dim, device, ms = _first(call, "s", s, _WIDE)
-    dev, lead, dt = s.device, shape[:-2], (s.dtype,)
+    dev, dt = s.device, (s.dtype,)
+    per_row, per_col = ((rows,), (dim,)) if len(shape) == 2 else ((groups, rows), (groups, dim))
     if dy is None or weight is None or rstd is None:
         _refuse(call, "dy, rstd and weight must be given")
     mats = _mat(call, "dy", dy, shape, dt, device) + ms + _mat(call, "dsum", dsum, shape, dt, device)
-    vecs = (_vec(call, "weight", weight, lead + (dim,), device)
-            + _vec(call, "rstd", rstd, shape[:-1], device))
+    vecs = _vec(call, "weight", weight, per_col, device) + _vec(call, "rstd", rstd, per_row, device)
     dx = torch.empty(shape, dtype=s.dtype, device=dev)
-    dweight = torch.empty(lead + (dim,), dtype=_F32, device=dev) if want_dweight else None
-    _run_with_space("lipz_rmsnorm_backward", _S_RMSNORM_BACKWARD,
+    dweight = torch.empty(per_col, dtype=_F32, device=dev) if want_dweight else None
+    _run_with_space("lipz_rmsnorm_backward", "lipz_rmsnorm_backward_workspace", _S_RMSNORM_BACKWARD,
                     (_S_RMSNORM_BACKWARD.size, 0, groups, rows, dim, *mats, dx.data_ptr(), rows * dim,
                      dim, ms[3], 0, *vecs, dweight.data_ptr() if want_dweight else 0, dim),
                     dev, device)
@@ -199,7 +207,7 @@ def quantize_rows(x):
     shape, groups, rows, dim, device, mx = _first(call, "x", x, _WIDE)
     dev = x.device
     q = torch.empty(shape, dtype=_E4M3, device=dev)
-    scale = torch.empty(shape[:-1], dtype=_F32, device=dev)
+    scale = torch.empty((rows,) if len(shape) == 2 else (groups, rows), dtype=_F32, device=dev)
     _run("lipz_quantize_rows",
          _S_QUANTIZE.pack(_S_QUANTIZE.size, 0, groups, rows, dim, *mx, q.data_ptr(), rows * dim, dim,
                           LIPZ_E4M3, 0, scale.data_ptr(), rows), device)
@@ -218,16 +226,20 @@ def linear(x, w, bias=None, act="none", slope=0.2, residual=None, x_scale=None, 
     dev = x.device
     if not isinstance(w, torch.Tensor) or w.dim() != len(x_shape):
         _refuse(call, "w must be a CUDA tensor with x's number of dimensions")
-    lead, n = x_shape[:-2], w.shape[-2]
-    shape, row, code = lead + (rows, n), lead + (n,), _act(call, act)
-    mw = _mat(call, "w", w, lead + (n, k), (x.dtype,), device)
+    n, code = w.shape[-2], _act(call, act)
+    if len(x_shape) == 2:
+        shape, w_shape, per_row, per_col = (rows, n), (n, k), (rows,), (n,)
+    else:
+        shape, w_shape, per_row, per_col = (groups, rows, n), (groups, n, k), (groups, rows), (groups, n)
+    mw = _mat(call, "w", w, w_shape, (x.dtype,), device)
     if out_dtype is not _BF16 and out_dtype is not _F32:
         _refuse(call, "out_dtype must be bfloat16 or float32")
     if (x_scale is None) != (mx[3] != LIPZ_E4M3) or (w_scale is None) != (mx[3] != LIPZ_E4M3):
         _refuse(call, "x_scale and w_scale go with 8-bit operands, and with them alone")
     mr = _mat(call, "residual", residual, shape, (out_dtype,), device)
-    vecs = (_vec(call, "x_scale", x_scale, x_shape[:-1], device)
-            + _vec(call, "w_scale", w_scale, row, device) + _vec(call, "bias", bias, row, device))
+    vecs = (_vec(call, "x_scale", x_scale, per_row, device)
+            + _vec(call, "w_scale", w_scale, per_col, device)
+            + _vec(call, "bias", bias, per_col, device))
     if out is None:
         y = torch.empty(shape, dtype=out_dtype, device=dev)
         my = (y.data_ptr(), rows * n, n, _TYPE[out_dtype], 0)
@@ -235,7 +247,7 @@ def linear(x, w, bias=None, act="none", slope=0.2, residual=None, x_scale=None, 
         y, my = out, _mat(call, "out", out, shape, (out_dtype,), device)
     pre = torch.empty(shape, dtype=_BF16, device=dev) if keep else None
     mp = (pre.data_ptr(), rows * n, n, LIPZ_BF16, 0) if keep else _NO_MAT
-    _run_with_space("lipz_linear", _S_LINEAR,
+    _run_with_space("lipz_linear", "lipz_linear_workspace", _S_LINEAR,
                     (_S_LINEAR.size, code, slope, 0, groups, rows, k, n, *mx, *mw, *mr, *my, *mp, *vecs),
                     dev, device)
     return y, pre
@@ -254,20 +266,23 @@ def linear_backward(dy, x, w, act="none", slope=0.2, pre=None, want_dx=True, wan
         _refuse(call, "x must be a CUDA tensor with dy's number of dimensions")
     if w is None:
         _refuse(call, "w must be given")
-    lead, k, code = shape[:-2], x.shape[-1], _act(call, act)
+    k, code = x.shape[-1], _act(call, act)
+    if len(shape) == 2:
+        x_shape, w_shape, per_col = (rows, k), (n, k), (n,)
+    else:
+        x_shape, w_shape, per_col = (groups, rows, k), (groups, n, k), (groups, n)
     if code and pre is None:
         _refuse(call, "act %r needs pre" % act)
     if dx_dtype not in _WIDE or dw_dtype not in _WIDE:
         _refuse(call, "dx_dtype and dw_dtype must be bfloat16 or float32")
-    mats = (mdy + _mat(call, "x", x, lead + (rows, k), bf, device)
-            + _mat(call, "w", w, lead + (n, k), bf, device)
+    mats = (mdy + _mat(call, "x", x, x_shape, bf, device) + _mat(call, "w", w, w_shape, bf, device)
             + _mat(call, "pre", pre if code else None, shape, bf, device))
-    dx = torch.empty(lead + (rows, k), dtype=dx_dtype, device=dev) if want_dx else None
-    dw = torch.empty(lead + (n, k), dtype=dw_dtype, device=dev) if want_dw else None
-    db = torch.empty(lead + (n,), dtype=_F32, device=dev) if want_db else None
+    dx = torch.empty(x_shape, dtype=dx_dtype, device=dev) if want_dx else None
+    dw = torch.empty(w_shape, dtype=dw_dtype, device=dev) if want_dw else None
+    db = torch.empty(per_col, dtype=_F32, device=dev) if want_db else None
     mx = (dx.data_ptr(), rows * k, k, _TYPE[dx_dtype], 0) if want_dx else _NO_MAT
     mw = (dw.data_ptr(), n * k, k, _TYPE[dw_dtype], 0) if want_dw else _NO_MAT
-    _run_with_space("lipz_linear_backward", _S_LINEAR_BACKWARD,
+    _run_with_space("lipz_linear_backward", "lipz_linear_backward_workspace", _S_LINEAR_BACKWARD,
                     (_S_LINEAR_BACKWARD.size, code, slope, 0, groups, rows, k, n, *mats, *mx, *mw,
                      db.data_ptr() if want_db else 0, n), dev, device)
     return dx, dw, db
