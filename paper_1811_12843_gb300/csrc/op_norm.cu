@@ -229,6 +229,7 @@ __device__ __forceinline__ void ring_done(const Ring& q, int* err) {
     while (tc::globaltimer() - t0 < 200000ull) {
     }
     if (threadIdx.x == 0 && err) *reinterpret_cast<volatile int*>(err) = *q.code;
+    __syncthreads();
   }
 }
 
@@ -492,14 +493,38 @@ __global__ void __launch_bounds__(1024) k_quantize_long(const RowArgs p, int64_t
 struct BackArgs {
   lipz_mat dy, s, dsum, dx;
   lipz_vec weight, rstd, dweight;
-  float* part;  // [groups][gridDim.x][dim], or null: the block's sums are the group's
+  float* part;  // [groups][clusters, or blocks][dim], or null: those of one are the group's
   int64_t rows;
   int dim;
   float inv_dim;
 };
 
+// The sums for dweight of a cluster's blocks (place(c): column c's in shared memory), added by the blocks,
+// each for a share of the columns. Every thread of the cluster calls it.
+template <typename Place>
+__device__ __forceinline__ void join_cluster(const BackArgs& p, int64_t g, const float* s_dw, Place place) {
+  __syncwarp();
+  tc::cluster_sync_all();
+  uint32_t size;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+  const int64_t part = blockIdx.x / size, parts = gridDim.x / size;
+  float* out = p.part ? p.part + (g * parts + part) * (int64_t)p.dim : p.dweight.data + g * p.dweight.group;
+  for (int c = (int)tc::cluster_ctarank() * (int)blockDim.x + threadIdx.x; c < p.dim; c += size * blockDim.x) {
+    const uint32_t at = tc::smem_u32(s_dw + place(c));
+    float v = 0.f;
+    for (uint32_t i = 0; i < size; ++i) {
+      float w;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(tc::mapa_shared(at, i)) : "memory");
+      v += w;
+    }
+    out[c] = v;
+  }
+  __syncwarp();
+  tc::cluster_sync_all();  // no block leaves while its sums are read
+}
+
 // A block of one row's threads walks over rows of one group (blockIdx.y), which arrive in a ring; its sums
-// for dweight stay in registers.
+// for dweight stay in registers, and are added over a cluster of blocks in shared memory.
 template <typename T, int E, int NV>
 __global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p, int stages, int slot, int* err) {
   extern __shared__ __align__(128) uint8_t smem[];
@@ -583,16 +608,15 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p, int 
       turn ^= 1;
     }
   }
-  if (p.dweight.data) {
-    float* out = p.part ? p.part + (g * gridDim.x + blockIdx.x) * (int64_t)p.dim
-                        : p.dweight.data + g * p.dweight.group;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (t + i * tpr < nvec)
-#pragma unroll
-        for (int e = 0; e < E; ++e) out[(t + i * tpr) * E + e] = dw[i][e];
-  }
   ring_done(q, err);
+  if (!p.dweight.data) return;
+  float* s_dw = reinterpret_cast<float*>(smem + RING_BARS);  // over the ring
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (t + i * tpr < nvec)
+#pragma unroll
+      for (int e = 0; e < E; ++e) s_dw[(t + i * tpr) * E + e] = dw[i][e];
+  join_cluster(p, g, s_dw, [](int c) { return c; });
 }
 
 // The same for rows off the 16-byte grid (k_rows_shift's units): a column is another thread's in every row,
@@ -672,13 +696,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
       turn ^= 1;
     }
   }
-  __syncthreads();
-  if (p.dweight.data) {
-    float* out = p.part ? p.part + (g * gridDim.x + blockIdx.x) * (int64_t)dim
-                        : p.dweight.data + g * p.dweight.group;
-    for (int c = t; c < dim; c += tpr) out[c] = s_dw[padded(c)];
-  }
   ring_done(q, err);
+  if (p.dweight.data) join_cluster(p, g, s_dw, [](int c) { return padded(c); });
 }
 
 // Short rows: a warp per row, loaded into registers one row ahead; a block of WARPS walks over rows of one
@@ -925,16 +944,46 @@ StreamShape backward_shape(const lipz_rmsnorm_backward_args& a) {
   return stream_shape((int)a.dim, backward_vec(a) ? 16 / eb : 1, eb, a.dsum.data ? 3 : 2, 1024);
 }
 
+// A cluster's blocks: two where bf16 rows lie on the grid (8192 x 4096 59 -> 56 us). In clusters of 4 or 8,
+// four of them per SM, some blocks found no place in their GPC and ran after the others (72 us instead of 53
+// without the parts' sum), and so did blocks of k_rmsnorm_backward_shift in clusters of two (bf16 16385 x 777
+// 51 -> 71 us); fp32 gains nothing.
+int back_cluster(const lipz_rmsnorm_backward_args& a, const StreamShape& s) {
+  return a.dy.type == LIPZ_BF16 && backward_vec(a) && !s.wide && s.per_sm % 2 == 0 ? 2 : 1;
+}
+
+// Launch in clusters of `cluster` blocks.
+template <typename K>
+cudaError_t launch_clusters(K kernel, const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
+                            int cluster, cudaStream_t st) {
+  const cudaError_t e = allow_smem(kernel, s.smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks, (unsigned)groups);
+  cfg.blockDim = dim3(s.tpr);
+  cfg.dynamicSmemBytes = s.smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  cfg.attrs = attr;
+  if (cluster > 1) {
+    cudaLaunchAttribute& c = attr[cfg.numAttrs++];
+    c.id = cudaLaunchAttributeClusterDimension;
+    c.val.clusterDim.x = cluster;
+    c.val.clusterDim.y = c.val.clusterDim.z = 1;
+  }
+  if (st != nullptr && st != cudaStreamLegacy && st != cudaStreamPerThread) {
+    cudaLaunchAttribute& c = attr[cfg.numAttrs++];
+    c.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    c.val.programmaticStreamSerializationAllowed = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, p, s.stages, s.slot, timeout_word());
+}
+
 template <typename T>
 cudaError_t launch_back_shift(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
                               cudaStream_t st) {
   constexpr int E = 16 / sizeof(T);
-  auto go = [&](auto kernel) {
-    const cudaError_t e = allow_smem(kernel, s.smem);
-    return e != cudaSuccess ? e
-                            : launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(s.tpr), s.smem, st,
-                                         p, s.stages, s.slot, timeout_word());
-  };
+  auto go = [&](auto kernel) { return launch_clusters(kernel, p, s, groups, blocks, 1, st); };
   return s.wide ? go(k_rmsnorm_backward_shift<T, E, 32 / E>) : go(k_rmsnorm_backward_shift<T, E, 16 / E>);
 }
 
@@ -951,14 +1000,9 @@ cudaError_t launch_back_rows(const BackArgs& p, int nv, int64_t groups, int bloc
 }
 
 template <typename T, int E>
-cudaError_t launch_back(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
+cudaError_t launch_back(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks, int parts,
                         cudaStream_t st) {
-  auto go = [&](auto kernel) {
-    const cudaError_t e = allow_smem(kernel, s.smem);
-    return e != cudaSuccess ? e
-                            : launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(s.tpr), s.smem, st,
-                                         p, s.stages, s.slot, timeout_word());
-  };
+  auto go = [&](auto kernel) { return launch_clusters(kernel, p, s, groups, blocks, blocks / parts, st); };
   return s.wide ? go(k_rmsnorm_backward<T, E, 32 / E>) : go(k_rmsnorm_backward<T, E, 16 / E>);
 }
 
@@ -1012,27 +1056,40 @@ cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols
                     dim3(32, parts >= 128 ? 32 : parts >= 16 ? 8 : 1), 0, st, part, parts, cols, out);
 }
 
-// Every block's sums are written and read once more: four rows or more per block.
-int rmsnorm_backward_blocks(const lipz_rmsnorm_backward_args& a) {
+namespace {
+// Blocks per group, and the parts in which their sums come.
+struct BackBlocks {
+  int blocks, parts;
+};
+BackBlocks backward_blocks(const lipz_rmsnorm_backward_args& a) {
   const int64_t groups = a.groups > 0 ? a.groups : 1;
   if (const int nv = backward_row_vectors(a)) {
     // two blocks per SM; one block per group, which needs no second launch, from half that many groups on
     const int warps = nv == 1 ? BACK_WARPS<1> : BACK_WARPS<2>;
     const int64_t fill = 2 * sm_count() / groups, most = ceil_div(a.rows, 2 * warps);
     const int64_t b = fill < 4 ? 1 : fill < most ? fill : most;
-    return b < 1 ? 1 : (int)b;
+    return {b < 1 ? 1 : (int)b, b < 1 ? 1 : (int)b};
   }
-  const int64_t fill = (int64_t)backward_shape(a).per_sm * sm_count() / groups;
-  const int64_t most = ceil_div(a.rows, 4), b = fill < most ? fill : most;
-  return b < 1 ? 1 : (int)b;
+  // four rows or more per block, whole clusters where there are that many
+  const StreamShape s = backward_shape(a);
+  const int cluster = back_cluster(a, s);
+  const int64_t fill = (int64_t)s.per_sm * sm_count() / groups, most = ceil_div(a.rows, 4);
+  int64_t b = fill < most ? fill : most;
+  if (b < 1) b = 1;
+  if (b < cluster) return {(int)b, (int)b};
+  b -= b % cluster;
+  return {(int)b, (int)b / cluster};
 }
+}  // namespace
+
+int rmsnorm_backward_parts(const lipz_rmsnorm_backward_args& a) { return backward_blocks(a).parts; }
 
 cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t st) {
   if (a.groups == 0) return cudaSuccess;
   const StreamShape s = backward_shape(a);
-  const int blocks = rmsnorm_backward_blocks(a);
+  const auto [blocks, parts] = backward_blocks(a);
   const BackArgs p{a.dy, a.s, a.dsum, a.dx, a.weight, a.rstd, a.dweight,
-                   blocks > 1 ? (float*)a.workspace : nullptr, a.rows, (int)a.dim,
+                   parts > 1 ? (float*)a.workspace : nullptr, a.rows, (int)a.dim,
                    1.f / (float)a.dim};
   const bool vec = backward_vec(a);
   const int nv = backward_row_vectors(a);
@@ -1044,13 +1101,13 @@ cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t s
     e = a.dy.type == LIPZ_FP32 ? launch_back_shift<float>(p, s, a.groups, blocks, st)
                                : launch_back_shift<bf16>(p, s, a.groups, blocks, st);
   else if (a.dy.type == LIPZ_FP32)
-    e = vec ? launch_back<float, 4>(p, s, a.groups, blocks, st)
-            : launch_back<float, 1>(p, s, a.groups, blocks, st);
+    e = vec ? launch_back<float, 4>(p, s, a.groups, blocks, parts, st)
+            : launch_back<float, 1>(p, s, a.groups, blocks, parts, st);
   else
-    e = vec ? launch_back<bf16, 8>(p, s, a.groups, blocks, st)
-            : launch_back<bf16, 1>(p, s, a.groups, blocks, st);
-  if (e != cudaSuccess || blocks == 1 || !a.dweight.data) return e;
-  return sum_parts(p.part, a.groups, blocks, a.dim, a.dweight, st);
+    e = vec ? launch_back<bf16, 8>(p, s, a.groups, blocks, parts, st)
+            : launch_back<bf16, 1>(p, s, a.groups, blocks, parts, st);
+  if (e != cudaSuccess || parts == 1 || !a.dweight.data) return e;
+  return sum_parts(p.part, a.groups, parts, a.dim, a.dweight, st);
 }
 
 }  // namespace ops

@@ -181,8 +181,8 @@ int check(const lipz_rmsnorm_backward_args* a) {
 }
 
 uint64_t space_of(const lipz_rmsnorm_backward_args& a) {
-  const int blocks = ops::rmsnorm_backward_blocks(a);
-  return blocks > 1 && a.dweight.data ? (uint64_t)a.groups * blocks * a.dim * 4 : 0;
+  const int parts = ops::rmsnorm_backward_parts(a);
+  return parts > 1 && a.dweight.data ? (uint64_t)a.groups * parts * a.dim * 4 : 0;
 }
 
 int check(const lipz_quantize_rows_args* a) {

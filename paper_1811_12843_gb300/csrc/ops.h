@@ -32,9 +32,9 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int sm_count();
 
 cudaError_t rmsnorm(const lipz_rmsnorm_args& a, cudaStream_t st);
-// Blocks per group of the backward kernel; with more than one, their weight-gradient sums go through
-// the workspace, [groups][blocks][dim] fp32.
-int rmsnorm_backward_blocks(const lipz_rmsnorm_backward_args& a);
+// Parts per group in which the backward kernel's weight-gradient sums come; more than one go through the
+// workspace, [groups][parts][dim] fp32.
+int rmsnorm_backward_parts(const lipz_rmsnorm_backward_args& a);
 cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t st);
 cudaError_t quantize_rows(const lipz_quantize_rows_args& a, cudaStream_t st);
 
