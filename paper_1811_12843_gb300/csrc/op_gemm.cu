@@ -1,11 +1,18 @@
-// Tensor-core product of the residual-block operators (tcgen05, sm_103a).
+// Tensor-core product of the residual-block operators (tcgen05, sm_103a):
+//     u = (A B^T) x_scale w_scale + bias,   y = act(u) + residual
 //
 // A tile of C is BM x BN: 128 rows on one CTA, or 256 on a pair of CTAs whose MMAs take A's rows from both
 // and half of B's rows from each (so that a byte of B that is brought from L2 serves 256 rows). Persistent
-// CTAs walk over tiles (and parts of k); two warps issue the TMA loads of A and of B into a ring of
-// 128-byte-swizzled stages, one issues the MMAs into one of two accumulators in tensor memory, and eight
-// turn the other accumulator into results.
-// Bound: the tensor cores for large sizes, the epilogue for k of a few hundred, HBM for few rows.
+// CTAs walk over tiles and parts of k. Two warps issue the TMA loads of A and of B into a ring of
+// 128-byte-swizzled stages, one issues the MMAs into two or four accumulators in tensor memory, one brings
+// the tiles' parameters (and residuals) ahead, and sixteen turn accumulators into results.
+//
+// Bound, and measured (a copy runs at 6.79 TB/s, cuBLAS at 1.94 PFLOP/s in bf16):
+//   large k   the tensor cores: backward products of 8192 x 4096 -> 4096 300 us, 1.83 PFLOP/s (0.95);
+//             8192 x 4096 -> 8192 over 8-bit operands 174 us by itself (3.2 PFLOP/s), 203 in a row, where the
+//             power limit lowers the clock.
+//   small k   the way of operands and results through L2: 144 x 500 x 256 -> 784 47 us (208 MB: 31 us).
+//   few rows  HBM and latency: 16 x 8192 -> 8192 37 us (134 MB: 20 us), 37 x 1000 -> 500 7.5 us.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -300,8 +307,9 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
 // T: the results' type; fp32 results are sums, in fp32 registers, of sums over SUM_CHUNKS chunks of k,
 // because the tensor cores' additions truncate. FORWARD: K-major operands and the forward's epilogue, one
 // product; else up to two plain products.
-// VIA: with row-per-lane accesses a tile's results cost 12 us and its residual 25 to 39 us at 144 x 512 x 256
-// -> 768 (of 47 and 88 us in all).
+// VIA: the residual comes and the results leave by TMA, through shared memory. With row-per-lane accesses,
+// whose 64-byte pieces reach memory one by one, results cost 12 us and a residual 25 more at 144 x 512 x 256
+// -> 768 (tanh with residual 88 us in all; by TMA 62).
 // SPLIT: a cluster of CTAs shares a tile, each with a part of k; their sums are added over the cluster's
 // shared memory, each CTA finishing a part of the columns. One tile per cluster.
 // DIRECT: the result warps bring the operands first, from rows that TMA does not take.
