@@ -272,23 +272,6 @@ __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int col
     if (r < rows && col < cols) base[r * ld + col] = from_f<T>(turn[r * 17 + col]);
 }
 
-// 16 bytes from any address, the first n of them, then zeros: the aligned words that hold them, shifted.
-__device__ __forceinline__ uint4 bytes16(const uint8_t* p, int64_t n) {
-  if (n <= 0) return make_uint4(0, 0, 0, 0);
-  const int off = (int)((uint64_t)p & 3), left = n < 16 ? (int)n : 16;
-  const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
-  uint32_t w[5], r[4];
-#pragma unroll
-  for (int i = 0; i < 5; ++i) w[i] = 4 * i < off + left ? __ldg(q + i) : 0u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[i] = __funnelshift_r(w[i], w[i + 1], off * 8);
-    const int keep = left - 4 * i;  // bytes of this word
-    if (keep < 4) r[i] = keep <= 0 ? 0u : r[i] & ((1u << 8 * keep) - 1u);
-  }
-  return make_uint4(r[0], r[1], r[2], r[3]);
-}
-
 __device__ __forceinline__ int64_t ceil_div_d(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // A unit's place: which part of k of which tile; groups outermost, then panels of 8 tile rows, along which
@@ -891,10 +874,9 @@ __global__ void __launch_bounds__(256) k_finish(const __grid_constant__ FinishPa
   }
 }
 
-template <typename U>
 __global__ void __launch_bounds__(256) k_copy_rows(const __grid_constant__ CopyJobs jobs) {
   pdl_wait();
-  copy_rows<U>(jobs, blockIdx.x);
+  copy_rows(jobs, blockIdx.x);
 }
 
 // Blocks of 8 rows by 32 columns' threads; columns past 65535 blocks are looped over.
@@ -1223,7 +1205,8 @@ int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* cop
     const GemmPlan::One& o = plan.p[i];
     const int eb = type_bytes(g.type);
     auto add = [&](Operand& t, const Extent& x, int64_t ld, uint64_t bytes) {
-      copies[n++] = {t.data, w, t.group, t.ld, x.rows, g.groups * x.rows, x.cols, ld * eb / 16};
+      copies[n++] = {(const uint8_t*)t.data, w, t.group * eb, t.ld * eb, x.rows, g.groups * x.rows, x.cols * eb,
+                     ld * eb / 16};
       t.data = w, t.ld = ld, t.group = x.rows * ld;
       w += bytes;
     };
@@ -1243,11 +1226,9 @@ CopyJobs copy_jobs(const RowCopy* c, int n) {
   return jobs;
 }
 
-cudaError_t run_copies(const CopyJobs& jobs, int type, cudaStream_t st) {
+cudaError_t run_copies(const CopyJobs& jobs, cudaStream_t st) {
   if (jobs.blocks == 0) return cudaSuccess;
-  const dim3 grid((unsigned)jobs.blocks), block(256);
-  return type == LIPZ_BF16 ? launch_pdl(k_copy_rows<unsigned short>, grid, block, 0, st, jobs)
-                           : launch_pdl(k_copy_rows<unsigned char>, grid, block, 0, st, jobs);
+  return launch_pdl(k_copy_rows, dim3((unsigned)jobs.blocks), dim3(256), 0, st, jobs);
 }
 
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,

@@ -47,9 +47,10 @@ struct Products {
 
 // Copies of operands whose rows TMA does not take, to rows of whole 16-byte units.
 struct RowCopy {
-  const void* src;  // null: none
+  const uint8_t* src;
   void* dst;
-  int64_t group, ld, rows, total, cols, units;
+  int64_t group, ld, rows, total;  // strides in bytes; rows of a group, of all
+  int64_t bytes, units;            // of a row: to copy; 16-byte units there
 };
 
 // How products will run: their scratch memory, and the copies that have to be made before them.
@@ -77,7 +78,7 @@ struct CopyJobs {
   int64_t blocks;
 };
 CopyJobs copy_jobs(const RowCopy* c, int n);
-cudaError_t run_copies(const CopyJobs& jobs, int type, cudaStream_t st);
+cudaError_t run_copies(const CopyJobs& jobs, cudaStream_t st);
 // The products themselves; sums: null, or formed beside them.
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
                          cudaStream_t st);

@@ -201,17 +201,31 @@ struct DuArgs {
   int col_blocks, row_blocks, blocks;  // of a group; of all groups
 };
 
-template <int E>
+// ALIGNED: rows of whole 16-byte units; else 8 columns are brought from the aligned words that hold them
+// (777 x 1001 with the copies beside it: one at a time 8.6 us, so 7.9, most of it latency).
+template <bool ALIGNED>
 __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
+  constexpr int E = 8;
   __shared__ float s[8][32 * E + 1];
   pdl_wait();
-  if ((int)blockIdx.x >= p.blocks) return copy_rows<unsigned short>(jobs, (int)blockIdx.x - p.blocks);
+  if ((int)blockIdx.x >= p.blocks) return copy_rows(jobs, (int)blockIdx.x - p.blocks);
   const int per = p.col_blocks * p.row_blocks, in_group = blockIdx.x % per;
   const int row_block = in_group / p.col_blocks, col_block = in_group - row_block * p.col_blocks;
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int64_t c = ((int64_t)col_block * 32 + tx) * E, g = blockIdx.x / per;
   const int64_t r0 = row_block * p.rows_per_block;
   const int64_t r1 = min(p.rows, r0 + p.rows_per_block);
+  auto load = [&](const lipz_mat& m, int64_t r, float* v) {
+    const bf16* src = (const bf16*)m.data + g * m.group + r * m.row + c;
+    if constexpr (ALIGNED) {
+      load_vec<bf16, E>(src, v);
+    } else {
+      const uint4 w = bytes16((const uint8_t*)src, (p.n - c) * 2);  // (columns past the last are zero)
+      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = __uint_as_float(e & 1 ? ww[e >> 1] & 0xFFFF0000u : ww[e >> 1] << 16);
+    }
+  };
   float sum[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] = 0.f;
@@ -221,10 +235,10 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constan
 #pragma unroll 4
       for (int64_t r = r0 + ty; r < r1; r += 8) {
         float d[E];
-        load_vec<bf16, E>((const bf16*)p.dy.data + g * p.dy.group + r * p.dy.row + c, d);
+        load(p.dy, r, d);
         if constexpr (ACT != LIPZ_ACT_NONE) {
           float u[E];
-          load_vec<bf16, E>((const bf16*)p.pre.data + g * p.pre.group + r * p.pre.row + c, u);
+          load(p.pre, r, u);
 #pragma unroll
           for (int e = 0; e < E; ++e) d[e] *= act_slope<ACT>(u[e], p.slope);
         }
@@ -265,7 +279,7 @@ BackPlan back_plan(const lipz_linear_backward_args& a) {
   b.ldu = ceil_div(a.n, 8) * 8;
   if (a.groups == 0 || a.rows == 0) return b;
   // enough blocks to fill the device, of 8 rows or more
-  const int64_t cols = ceil_div(a.n, b.vec ? 256 : 32), fill = 8 * sm_count();
+  const int64_t cols = ceil_div(a.n, 256), fill = 8 * sm_count();
   const int64_t want = ceil_div(fill, cols * a.groups);
   b.rows_per_block = ceil_div(ceil_div(a.rows, want), 8) * 8;
   b.blocks = ceil_div(a.rows, b.rows_per_block);
@@ -320,7 +334,7 @@ cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {
   const GemmPlan plan = plan_products(q);
   RowCopy copies[4];
   const int n = plan_copies(plan, &q, a.workspace, copies);
-  const cudaError_t e = run_copies(copy_jobs(copies, n), a.x.type, st);
+  const cudaError_t e = run_copies(copy_jobs(copies, n), st);
   return e != cudaSuccess ? e : run_products(plan, q, a.workspace, nullptr, st);
 }
 
@@ -352,14 +366,14 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st)
   const CopyJobs jobs = copy_jobs(copies, n);
   cudaError_t e;
   if (du || part) {
-    const int64_t cols = ceil_div(a.n, b.vec ? 256 : 32), blocks = cols * b.blocks * a.groups;
+    const int64_t cols = ceil_div(a.n, 256), blocks = cols * b.blocks * a.groups;
     const DuArgs p{a.dy, a.pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope,
                    (int)cols, (int)b.blocks, (int)blocks};
     const dim3 grid((unsigned)(blocks + jobs.blocks));
-    e = b.vec ? launch_pdl(k_du<8>, grid, dim3(256), 0, st, p, jobs)
-              : launch_pdl(k_du<1>, grid, dim3(256), 0, st, p, jobs);
+    e = b.vec ? launch_pdl(k_du<true>, grid, dim3(256), 0, st, p, jobs)
+              : launch_pdl(k_du<false>, grid, dim3(256), 0, st, p, jobs);
   } else {
-    e = run_copies(jobs, LIPZ_BF16, st);
+    e = run_copies(jobs, st);
   }
   const PartSums sums{part, a.n, (int)a.groups, (int)b.blocks, a.db};
   if (e == cudaSuccess && part && !b.launches)

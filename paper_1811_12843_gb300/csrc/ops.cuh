@@ -242,31 +242,38 @@ __device__ __forceinline__ void with_act(int act, F&& f) {
   }
 }
 
-// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a
-// warp; a thread forms 16 bytes at a time.
-template <typename U>
-__device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
-  constexpr int E = 16 / sizeof(U);
-  const int64_t g = r / p.rows;
-  const U* s = (const U*)p.src + g * p.group + (r - g * p.rows) * p.ld;
-  for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) {
-    union {
-      uint4 v;
-      U e[E];
-    } w;
+// 16 bytes from any address, the first n of them, then zeros: the aligned words that hold them, shifted.
+__device__ __forceinline__ uint4 bytes16(const uint8_t* p, int64_t n) {
+  if (n <= 0) return make_uint4(0, 0, 0, 0);
+  const int off = (int)((uint64_t)p & 3), left = n < 16 ? (int)n : 16;
+  const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
+  uint32_t w[5], r[4];
 #pragma unroll
-    for (int i = 0; i < E; ++i) w.e[i] = u * E + i < p.cols ? s[u * E + i] : U(0);
-    ((uint4*)p.dst)[r * p.units + u] = w.v;
+  for (int i = 0; i < 5; ++i) w[i] = 4 * i < off + left ? __ldg(q + i) : 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = __funnelshift_r(w[i], w[i + 1], off * 8);
+    const int keep = left - 4 * i;  // bytes of this word
+    if (keep < 4) r[i] = keep <= 0 ? 0u : r[i] & ((1u << 8 * keep) - 1u);
   }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a warp.
+__device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
+  const int64_t g = r / p.rows;
+  const uint8_t* s = p.src + g * p.group + (r - g * p.rows) * p.ld;
+  uint4* d = (uint4*)p.dst + r * p.units;
+#pragma unroll 2
+  for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) d[u] = bytes16(s + u * 16, p.bytes - u * 16);
 }
 // Block `b` of 256 threads: 8 rows, of one copy after the other.
-template <typename U>
 __device__ __forceinline__ void copy_rows(const CopyJobs& jobs, int64_t b) {
   for (int j = 0; j < jobs.n; ++j) {
     const int64_t blocks = (jobs.c[j].total + COPY_ROWS - 1) / COPY_ROWS;
     if (b < blocks) {
       const int64_t r = b * COPY_ROWS + (threadIdx.x >> 5);
-      if (r < jobs.c[j].total) copy_row<U>(jobs.c[j], r);
+      if (r < jobs.c[j].total) copy_row(jobs.c[j], r);
       return;
     }
     b -= blocks;
