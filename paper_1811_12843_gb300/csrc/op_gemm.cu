@@ -61,7 +61,8 @@ struct Shape {
   // rows of the sums that nobody reads)
   static constexpr int stage(int a_rows) { return a_rows * ROW + B_BYTES; }
   static constexpr int smem(int stages, int a_rows, bool turn) {
-    return 1024 + stages * stage(a_rows) + (128 - a_rows) * ROW + SLOTS * (TILE + SLOT) + SUMS + BARS + (turn ? EPI_WARPS * TURN : 0);
+    return 1024 + stages * stage(a_rows) + (128 - a_rows) * ROW + SLOTS * (TILE + SLOT) + SUMS + BARS +
+           (turn ? EPI_WARPS * TURN : 0);
   }
   static constexpr int stages(int a_rows, bool turn) {
     int n = a_rows < 128 ? STAGES_MAX : 8;
@@ -110,8 +111,8 @@ struct GemmParams {
   int* err;
 };
 
-// Bounded wait for a barrier's phase, as tc::mbar_wait, that leaves the issue slots to the result warps: a
-// try suspends the thread for up to 20 us.
+// Bounded wait of a warp for a barrier's phase, as tc::mbar_wait, that leaves the issue slots to the result
+// warps: a try suspends the thread for up to 20 us.
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* code,
                                      int what) {
   const auto attempt = [&] {
@@ -124,16 +125,16 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
         : "memory");
     return ok != 0;
   };
-  if (attempt()) return true;
-  for (const unsigned long long t0 = tc::globaltimer(); !attempt();) {
-    if (*abort_flag) return false;
-    if (tc::globaltimer() - t0 > tc::WAIT_NS) {
-      *abort_flag = 1;
-      *code = what;
-      return false;
-    }
+  bool ok = attempt();
+  if (!ok) {
+    const unsigned long long t0 = tc::globaltimer();
+    while (!(ok = attempt()) && !*abort_flag)
+      if (tc::globaltimer() - t0 > tc::WAIT_NS) {
+        *abort_flag = 1;
+        *code = what;
+      }
   }
-  return true;
+  return __all_sync(0xffffffffu, ok);  // (its lanes leave the same way: they go on to warp-wide operations)
 }
 
 template <int CG>
@@ -310,7 +311,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int stages = prm.stages, stage_bytes = FORWARD ? prm.stage_bytes : S::STAGE;
   const int a_stage = FORWARD ? prm.a_rows * ROW : S::A_BYTES;
   const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* tiles = smem_raw + (base - raw) + stages * stage_bytes + (S::A_BYTES - a_stage);  // [SLOTS][BN / 32][128 rows][64 bytes]
+  // [SLOTS][BN / 32][128 rows][64 bytes]
+  uint8_t* tiles = smem_raw + (base - raw) + stages * stage_bytes + (S::A_BYTES - a_stage);
   uint8_t* slots = tiles + SLOTS * S::TILE;
   float* s_sum = reinterpret_cast<float*>(slots + SLOTS * S::SLOT);
   uint64_t* bars = reinterpret_cast<uint64_t*>(slots + SLOTS * S::SLOT + S::SUMS);
@@ -623,7 +625,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
     auto wait_sum = [&]() {
-      ok = __all_sync(0xffffffffu, wait(bAcc + 8 * (sums % ACCS), (uint32_t)(sums / ACCS) & 1, abort_flag, code, 4));
+      ok = wait(bAcc + 8 * (sums % ACCS), (uint32_t)(sums / ACCS) & 1, abort_flag, code, 4);
       tc::tc_fence_after();
       return tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(sums % ACCS * BN + col0);
     };
@@ -638,7 +640,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     };
     for (int i = 0; i < my_units; ++i) {
       const int r = i % SLOTS;
-      ok = __all_sync(0xffffffffu, wait(bSlot + 8 * r, (uint32_t)(i / SLOTS) & 1, abort_flag, code, 6));
+      ok = wait(bSlot + 8 * r, (uint32_t)(i / SLOTS) & 1, abort_flag, code, 6);
       if (!ok) break;
       const uint8_t* slot = slots + r * S::SLOT;
       const Slot sl = *reinterpret_cast<const Slot*>(slot);

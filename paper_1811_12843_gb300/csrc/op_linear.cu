@@ -194,7 +194,7 @@ Products product_of(const lipz_linear_args& a) {
 struct DuArgs {
   lipz_mat dy, pre;
   bf16* du;     // [groups][rows][ldu], or null: the sums only
-  float* part;  // [groups][gridDim.y][n], or null: no sums
+  float* part;  // [groups][row_blocks][n], or null: no sums
   int64_t rows, n, ldu, rows_per_block;
   int act;
   float slope;
