@@ -76,7 +76,9 @@ struct Shape {
 struct Divisor {
   uint32_t mul;
   int shift;
-  __device__ __forceinline__ int operator()(int n) const { return (int)((uint64_t)(uint32_t)n * mul >> shift); }
+  __device__ __forceinline__ int operator()(int n) const {
+    return (int)((uint64_t)(uint32_t)n * mul >> shift);
+  }
 };
 Divisor divisor(int64_t d) {
   int s = 0;
@@ -303,7 +305,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   using S = Shape<CG, BN, VIA>;
   constexpr bool SUMS = sizeof(T) == 4;
   static_assert(!VIA || (FORWARD && !SUMS && S::COLSW == 32), "boxes of 32 bf16 columns");
-  static_assert(!SPLIT || (FORWARD && CG == 1 && !VIA && 128 * (BN + 1) * 4 <= 5 * S::B_BYTES), "sums of a tile");
+  static_assert(!SPLIT || (FORWARD && CG == 1 && !VIA && 128 * (BN + 1) * 4 <= 5 * S::B_BYTES),
+                "sums of a tile");
   constexpr int BM = 128 * CG, COLSW = S::COLSW, ACCS = S::ACCS, SLOTS = S::SLOTS;
   constexpr int CW = COLSW < 32 ? COLSW : 32;       // a result warp's columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
@@ -599,7 +602,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       static_assert(SPLIT, "one unit");
       const Problem& p = prm.p[0];
       const Place pl = unit_place(0);
-      const int rows_a = min(prm.a_rows, p.m - pl.mt * BM), units = (rows_a + min(BN, p.n - pl.nt * BN)) * 8;
+      const int rows_a = min(prm.a_rows, p.m - pl.mt * BM);
+      const int units = (rows_a + min(BN, p.n - pl.nt * BN)) * 8;
       const uint8_t* a = p.a_rows + pl.g * p.a_group + (int64_t)(pl.mt * BM) * p.a_ld;
       const uint8_t* b = p.b_rows + pl.g * p.b_group + (int64_t)(pl.nt * BN) * p.b_ld;
       int c0, c1;
@@ -658,7 +662,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int swizzle = lane >> 1 & 3;
       auto residual = [&](uint32_t (&v)[VW], int c) {
         if (VIA || !has_res) return;
-        const T* src = (const T*)e.residual.data + sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
+        const T* src =
+            (const T*)e.residual.data + sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
 #pragma unroll
         for (int h = 0; h < CW; h += 16)
           if (columns_left(c + h) > 0)
@@ -1020,7 +1025,9 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
     p.a_bytes = arows * ROW;
     p.az = g.groups > 1 && g.a.group != 0, p.bz = g.groups > 1 && g.b.group != 0;
     auto align = [&](const lipz_mat& m) {
-      const int a = !m.data ? 32 : rows_aligned(m, g.groups, g.m, 32) ? 32 : rows_aligned(m, g.groups, g.m, 16) ? 16 : 0;
+      const int a = !m.data || rows_aligned(m, g.groups, g.m, 32) ? 32
+                    : rows_aligned(m, g.groups, g.m, 16)          ? 16
+                                                                  : 0;
       turn = turn || (m.data && !p.part && (!a || g.n % 16) && (!VIA || m.data == g.e.pre.data));
       return a;
     };
@@ -1079,8 +1086,9 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
                  ? launch<TYPE, 1, 64, true, float, false, true, true>(q, p, parts, sums, st)
                  : launch<TYPE, 1, 64, true, bf16, false, true, true>(q, p, parts, sums, st);
     if (p.p[0].splits > 1)
-      return q.g[0].e.y.type == LIPZ_FP32 ? launch<TYPE, 1, 64, true, float, false, true>(q, p, parts, sums, st)
-                                          : launch<TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
+      return q.g[0].e.y.type == LIPZ_FP32
+                 ? launch<TYPE, 1, 64, true, float, false, true>(q, p, parts, sums, st)
+                 : launch<TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
   }
   if (q.g[0].e.y.type == LIPZ_FP32) {
     if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, float>(q, p, parts, sums, st);
@@ -1106,8 +1114,9 @@ GemmPlan plan_products(const Products& q) {
   const bool sums = g0.e.y.type == LIPZ_FP32, res = g0.e.residual.data, heavy = g0.e.act >= LIPZ_ACT_TANH;
   // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its MMA
   // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost a cluster's exchange, or
-  // another launch and their way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 x 8192 in bf16 (8 bits: 184 instead
-  // of 158), epilogues at 144 x 512 x 256 -> 768 without an activation, what tanh adds, what a residual adds.
+  // another launch and their way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 -> 8192 in bf16
+  // (8 bits: 184 instead of 158), epilogues at 144 x 512 x 256 -> 768 without an activation, what tanh adds, what
+  // a residual adds.
   struct Shape {
     int cg, bn;
     double step, epi, act, residual;
@@ -1141,7 +1150,8 @@ GemmPlan plan_products(const Products& q) {
                (o.splits == 1 || tiles * o.splits <= (forward ? 1 : 2) * slots) &&
                (!forward || o.splits == s0);
         const double mma = o.chunks_per_split * 4 * c.step * (eb == 1 ? 1.16 : 1);
-        const double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0), unit = mma > epi ? mma : epi;
+        const double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0);
+        const double unit = mma > epi ? mma : epi;
         work += unit * tiles * o.splits;
         if (unit > top) top = unit;
         if (mma + epi > last) last = mma + epi;
@@ -1194,7 +1204,8 @@ void plan_space(const Products& q, GemmPlan* plan) {
     o.a_bytes = o.copy_a ? round256(g.groups * xa.rows * o.lda * eb) : 0;
     o.b_bytes = o.copy_b ? round256(g.groups * xb.rows * o.ldb * eb) : 0;
     o.ldp = ceil_div(g.n, 16) * 16;
-    o.part_bytes = o.splits > 1 && !(g.a.k_major && g.b.k_major) ? round256((int64_t)o.splits * g.groups * g.m * o.ldp * 4) : 0;
+    const bool through_memory = o.splits > 1 && !(g.a.k_major && g.b.k_major);
+    o.part_bytes = through_memory ? round256((int64_t)o.splits * g.groups * g.m * o.ldp * 4) : 0;
     plan->bytes += o.a_bytes + o.b_bytes + o.part_bytes;
   }
 }

@@ -72,8 +72,8 @@ int take_timeout(const char* call) {
   int* word = ops::timeout_word();
   const int code = word ? __atomic_exchange_n(word, 0, __ATOMIC_ACQ_REL) : 0;
   if (!code) return LIPZ_OK;
-  return fail(LIPZ_ERR_TIMEOUT, "%s: an earlier call's kernel gave up on a wait (%d): its results are not valid",
-              call, code);
+  return fail(LIPZ_ERR_TIMEOUT,
+              "%s: an earlier call's kernel gave up on a wait (%d): its results are not valid", call, code);
 }
 
 constexpr int64_t MAX_EXTENT = INT32_MAX;
@@ -109,7 +109,8 @@ struct Check {
       if (!optional && groups > 0 && nrows > 0) fail_mat(name, "is null");
       return rc == LIPZ_OK;
     }
-    if (m.type < 0 || m.type > 2 || !(types >> m.type & 1)) fail_mat(name, "has a type that this call does not take");
+    if (m.type < 0 || m.type > 2 || !(types >> m.type & 1))
+      fail_mat(name, "has a type that this call does not take");
     else if ((uintptr_t)m.data % ops::type_bytes(m.type)) fail_mat(name, "is not aligned to its type");
     else if (nrows > 1 && (m.row < (out ? cols : 0))) fail_mat(name, "has a row stride that is too small");
     else if (groups > 1 && m.group < 0) fail_mat(name, "has a negative group stride");

@@ -424,6 +424,30 @@ def test_linear_strides_and_places(kind, rows, k, n, cut):
     assert torch.equal(rest, wide)  # nothing outside the output was written
 
 
+@pytest.mark.parametrize("groups,rows,k,n", [(40, 300, 256, 520), (160, 100, 208, 264), (1, 20000, 256, 392),
+                                             (24, 513, 64, 640), (1, 9000, 784, 512), (3, 7000, 240, 136)])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("act,with_residual,keep", [("tanh", False, False), ("gelu", True, False),
+                                                    ("none", True, True)])
+def test_linear_short_sums(groups, rows, k, n, kind, act, with_residual, keep):
+    """Many tiles of a few hundred k, one residual for every group, the stream updated in place."""
+    x, xs = operand(161, norm_shape(groups, rows, k), 1.0, kind)
+    w, ws = operand(162, norm_shape(groups, n, k), k ** -0.5, kind)
+    bias = randn(163, norm_shape(groups, n), 0.5, F32)
+    residual = None
+    if with_residual:
+        residual = randn(164, norm_shape(groups, rows, n))
+        if groups > 1 and not keep:
+            residual = residual[:1].expand(groups, rows, n)
+    before = residual if residual is None or not keep else residual.clone()
+    y, pre = ops.linear(x, w, bias, act=act, residual=residual, x_scale=xs, w_scale=ws, keep=keep,
+                        out=residual if keep else None)
+    check_linear(y, pre, x, w, xs, ws, bias, act, before)
+    if not keep:
+        again, _ = ops.linear(x, w, bias, act=act, residual=residual, x_scale=xs, w_scale=ws)
+        assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("rows", [1, 20, 300])
 def test_linear_nan_and_infinity_stay_in_their_row_and_column(kind, rows):
