@@ -985,7 +985,8 @@ cudaError_t prepare_kernel(K kernel, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false, bool DIRECT = false>
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false,
+          bool DIRECT = false>
 cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
                    cudaStream_t st) {
   using S = Shape<CG, BN, VIA>;

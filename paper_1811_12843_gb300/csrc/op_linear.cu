@@ -148,10 +148,25 @@ __global__ void __launch_bounds__(32 * VEC_WARPS) k_linear_rows(const VecParams 
   }
 }
 
-// One row or two go to k_linear_rows, and up to four with small weights (4 x 4096 -> 4096 takes 20 us there
-// and 18 on the tensor cores, over 8-bit operands 18 and 14; 3 x 777 -> 1001 10 and 15).
+// Whether rows of x and w are whole 16-byte units.
+bool in_units(const lipz_linear_args& a) {
+  return a.k % (16 / type_bytes(a.x.type)) == 0 && rows_aligned(a.x, a.groups, a.rows, 16) &&
+         rows_aligned(a.w, a.groups, a.n, 16);
+}
+
+// Few rows go to k_linear_rows while it is the faster. Beside w's bytes it pays for each row of x that meets
+// them, so the weights that it takes fall with the square of the rows, and for each block, so the outputs of
+// all groups are bounded; element by element (rows off the 16-byte grid) its rate is bounded by the loads,
+// and the tensor cores' product has such rows copied first. There and on the tensor cores, us, bf16:
+//   rows   1 x 4096 -> 4096 12.3, 16.5   2 x 4096 -> 4096 14.5, 16.5   4 x 4096 -> 4096 18.7, 16.4
+//          1 x 8192 -> 8192 29.0, 34.3   2 x 8192 -> 8192 41.5, 34.6   4 x 1024 -> 1024  8.3, 14.5
+//   blocks 1 x 512 -> 16384 11.1, 11.9   1 x 512 -> 32768 15.3, 14.3   1 x 256 -> 512, 256 groups 34.8, 18.5
+//   odd    2 x 1001 -> 8001 18.4, 22.7   2 x 4001 -> 8001 59.2, 52.4   1 x 777 -> 500, 16 groups 14.3, 19.4
 bool few_rows(const lipz_linear_args& a) {
-  return a.rows <= 2 || (a.rows <= 4 && a.groups * a.n * a.k <= 4 << 20);
+  if (a.rows > 4) return false;
+  const double work = (double)a.rows * a.rows * a.groups * a.n * a.k;
+  if (!in_units(a)) return work <= 32 << 20;
+  return (a.rows == 1 || work <= 64 << 20) && a.groups * a.n <= 12 << 10;
 }
 
 template <int TYPE, bool VEC>
@@ -164,8 +179,7 @@ cudaError_t launch_rows(const VecParams& p, dim3 grid, cudaStream_t st) {
 
 cudaError_t linear_rows(const lipz_linear_args& a, const Epilogue& e, cudaStream_t st) {
   const int per = 16 / type_bytes(a.x.type);
-  const bool vec = a.k % per == 0 && rows_aligned(a.x, a.groups, a.rows, 16) &&
-                   rows_aligned(a.w, a.groups, a.n, 16);
+  const bool vec = in_units(a);
   // warps share an output where whole rows would leave the SMs with fewer than eight warps each
   int parts = 1;
   while (parts < VEC_WARPS && a.groups * ceil_div(a.n, W_ROWS) * parts < 8 * sm_count() &&
@@ -324,7 +338,7 @@ BackPlan back_plan(const lipz_linear_backward_args& a) {
 }  // namespace
 
 uint64_t linear_workspace(const lipz_linear_args& a) {
-  return a.groups == 0 || few_rows(a) ? 0 : plan_products(product_of(a)).bytes;
+  return a.groups == 0 || a.rows == 0 || few_rows(a) ? 0 : plan_products(product_of(a)).bytes;
 }
 
 cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {

@@ -448,6 +448,26 @@ def test_linear_short_sums(groups, rows, k, n, kind, act, with_residual, keep):
         assert torch.equal(y, again)
 
 
+# One to four rows on both sides of the sizes at which another kernel takes them.
+@pytest.mark.parametrize("groups,rows,k,n", [(1, 1, 64, 12352), (1, 2, 72, 12304), (1, 2, 72, 12280),
+                                             (300, 1, 64, 48), (200, 2, 128, 72), (1, 2, 4112, 4096),
+                                             (1, 3, 4112, 2048), (1, 4, 2050, 1023), (1, 4, 2050, 1029),
+                                             (1, 2, 4099, 2053), (97, 4, 200, 33)])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("apart", [0, 5])
+def test_linear_few_rows(groups, rows, k, n, kind, apart):
+    """Rows of x as they lie and with a gap that takes them off the 16-byte grid."""
+    x, xs = operand(171, norm_shape(groups, rows, k + apart), 1.0, kind)
+    x = x[..., :k]
+    w, ws = operand(172, norm_shape(groups, n, k), k ** -0.5, kind)
+    bias = randn(173, norm_shape(groups, n), 0.5, F32)
+    residual = randn(174, norm_shape(groups, rows, n))
+    y, pre = ops.linear(x, w, bias, act="gelu", residual=residual, x_scale=xs, w_scale=ws, keep=True)
+    check_linear(y, pre, x, w, xs, ws, bias, "gelu", residual)
+    again, _ = ops.linear(x, w, bias, act="gelu", residual=residual, x_scale=xs, w_scale=ws)
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("rows", [1, 20, 300])
 def test_linear_nan_and_infinity_stay_in_their_row_and_column(kind, rows):
