@@ -34,6 +34,7 @@ constexpr int ROW = 128;                  // bytes of a swizzled row: 64 bf16 or
 constexpr int EPI_WARPS = 16, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 constexpr int TURN = 32 * 17 * 4;         // a warp's block for turning rows into columns
 constexpr int MN_BOX = 64 * ROW;          // 64 k by 64 m (or n) of an operand whose rows run along m (n)
+static_assert(EPI_WARPS == SUM_WAYS, "a result warp per way");
 constexpr int SUM_CHUNKS = 8;             // chunks of k whose sum stands in tensor memory, for fp32 results
 constexpr int SMEM_MAX = 232448, STAGES_MAX = 20;
 constexpr int DIRECT_CHUNKS = 4;          // most chunks of k per CTA whose operands the result warps bring
@@ -923,6 +924,9 @@ bool tma_takes(const Operand& o, const Extent& x, int64_t groups, int eb) {
   return groups == 1 || (o.group * eb % 16 == 0 && o.group * eb < (int64_t)1 << 40);
 }
 
+// An operand that the groups share is copied once (144 groups of 100 x 777 -> 501: 76 -> 38 us).
+int64_t copied_groups(const Operand& o, int64_t groups) { return o.group ? groups : 1; }
+
 // The map of results or a residual, {n, m, groups}, in boxes of 32 bf16 columns.
 bool encode_tile(CUtensorMap* map, const lipz_mat& m, int64_t rows, int64_t cols, int64_t groups,
                  int box_rows) {
@@ -1202,8 +1206,8 @@ void plan_space(const Products& q, GemmPlan* plan) {
     o.copy_b = !plan->direct && !tma_takes(g.b, xb, g.groups, eb);
     o.lda = ceil_div(xa.cols, unit) * unit;
     o.ldb = ceil_div(xb.cols, unit) * unit;
-    o.a_bytes = o.copy_a ? round256(g.groups * xa.rows * o.lda * eb) : 0;
-    o.b_bytes = o.copy_b ? round256(g.groups * xb.rows * o.ldb * eb) : 0;
+    o.a_bytes = o.copy_a ? round256(copied_groups(g.a, g.groups) * xa.rows * o.lda * eb) : 0;
+    o.b_bytes = o.copy_b ? round256(copied_groups(g.b, g.groups) * xb.rows * o.ldb * eb) : 0;
     o.ldp = ceil_div(g.n, 16) * 16;
     const bool through_memory = o.splits > 1 && !(g.a.k_major && g.b.k_major);
     o.part_bytes = through_memory ? round256((int64_t)o.splits * g.groups * g.m * o.ldp * 4) : 0;
@@ -1219,9 +1223,10 @@ int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* cop
     const GemmPlan::One& o = plan.p[i];
     const int eb = type_bytes(g.type);
     auto add = [&](Operand& t, const Extent& x, int64_t ld, uint64_t bytes) {
-      copies[n++] = {(const uint8_t*)t.data, w, t.group * eb, t.ld * eb, x.rows, g.groups * x.rows, x.cols * eb,
+      const int64_t groups = copied_groups(t, g.groups);
+      copies[n++] = {(const uint8_t*)t.data, w, t.group * eb, t.ld * eb, x.rows, groups * x.rows, x.cols * eb,
                      ld * eb / 16};
-      t.data = w, t.ld = ld, t.group = x.rows * ld;
+      t.data = w, t.ld = ld, t.group = groups > 1 ? x.rows * ld : 0;
       w += bytes;
     };
     if (o.copy_a) add(g.a, extent(g.a, g.m, g.k), o.lda, o.a_bytes);

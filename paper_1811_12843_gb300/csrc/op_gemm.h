@@ -30,7 +30,9 @@ struct Gemm {
   Epilogue e;
 };
 
-// Sums that a launch forms beside its products: out[g][c] = sum over p < parts of part[g][p][c].
+// Sums that a launch forms beside its products: out[g][c] = sum over p < parts of part[g][p][c], SUM_WAYS
+// parts at a time.
+constexpr int SUM_WAYS = 16;
 struct PartSums {
   const float* part;
   int64_t cols;

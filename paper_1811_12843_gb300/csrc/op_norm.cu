@@ -1051,9 +1051,9 @@ cudaError_t quantize_rows(const lipz_quantize_rows_args& a, cudaStream_t st) {
 }
 
 cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols, lipz_vec out,
-                      cudaStream_t st) {
-  return launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(cols, 32), (unsigned)groups),
-                    dim3(32, parts >= 128 ? 32 : parts >= 16 ? 8 : 1), 0, st, part, parts, cols, out);
+                      int ways, cudaStream_t st) {
+  return launch_pdl(k_sum_parts, dim3((unsigned)ceil_div(cols, 32), (unsigned)groups), dim3(32, ways), 0, st,
+                    part, parts, cols, out);
 }
 
 namespace {
@@ -1107,7 +1107,7 @@ cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t s
     e = vec ? launch_back<bf16, 8>(p, s, a.groups, blocks, parts, st)
             : launch_back<bf16, 1>(p, s, a.groups, blocks, parts, st);
   if (e != cudaSuccess || parts == 1 || !a.dweight.data) return e;
-  return sum_parts(p.part, a.groups, parts, a.dim, a.dweight, st);
+  return sum_parts(p.part, a.groups, parts, a.dim, a.dweight, parts >= 128 ? 32 : parts >= 16 ? 8 : 1, st);
 }
 
 }  // namespace ops

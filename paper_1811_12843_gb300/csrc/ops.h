@@ -38,8 +38,9 @@ int rmsnorm_backward_parts(const lipz_rmsnorm_backward_args& a);
 cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t st);
 cudaError_t quantize_rows(const lipz_quantize_rows_args& a, cudaStream_t st);
 
-// out[g][c] = sum over p < parts of part[g][p][c], in a fixed order.
-cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols, lipz_vec out,
+// out[g][c] = sum over p < parts of part[g][p][c], in a fixed order: `ways` (at most 32) sums of every
+// ways-th part, then theirs.
+cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols, lipz_vec out, int ways,
                       cudaStream_t st);
 
 uint64_t linear_workspace(const lipz_linear_args& a);

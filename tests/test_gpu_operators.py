@@ -535,6 +535,26 @@ def test_linear_backward_strides(rows, k, n, cut):
     within(db, rb, (2.0 ** -17 + (rows + 16) * 2.0 ** -24) * size.sum(dim=-2), "db")
 
 
+@pytest.mark.parametrize("rows,k,n,cut", [(150, 256, 320, 3), (40, 130, 77, 0), (700, 129, 250, 1), (1, 33, 9, 1),
+                                          (3, 100, 100, 0)])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_linear_backward_without_activation(rows, k, n, cut, groups):
+    """dy off the 16-byte grid, operands that the groups share, and every choice of results: the same bits."""
+    dy = randn(181, (groups, rows, n + 5), 0.1)[:, :, cut:cut + n]
+    x = randn(182, (1, rows, k + 3))[:, :, cut:cut + k].expand(groups, rows, k)
+    w = randn(183, (1, n, k + 3), k ** -0.5)[:, :, :k].expand(groups, n, k)
+    dx, dw, db = ops.linear_backward(dy, x, w)
+    _, rx, rw, rb = backward_ref(dy, x, w, "none", None)
+    within(dx, rx, 2.0 ** -8 * rx.abs() + sum_error(n) * (d(dy).abs() @ d(w).abs()), "dx")
+    within(dw, rw, 2.0 ** -8 * rw.abs() + sum_error(rows) * (d(dy).abs().transpose(-1, -2) @ d(x).abs()), "dw")
+    within(db, rb, (rows + 16) * 2.0 ** -24 * d(dy).abs().sum(dim=-2), "db")
+    for i in range(1, 7):
+        want = [bool(i & 1), bool(i & 2), bool(i & 4)]
+        got = ops.linear_backward(dy, x, w, want_dx=want[0], want_dw=want[1], want_db=want[2])
+        for on, a, b in zip(want, got, (dx, dw, db)):
+            assert (a is None) if not on else torch.equal(a, b)
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_linear_gradients_are_those_of_the_forward(act):
     """Against central differences of the definition in 64 bits along random directions: within the
