@@ -1,15 +1,18 @@
-"""Builds the engine's shared library (liblipz.so) for sm_103a with nvcc, in-tree.
+"""Builds the engine's shared library (liblipz.so) for sm_103a with nvcc, in-tree, and the binding of
+its operators to torch tensors (torch_operators.so) with the host compiler.
 
-Each translation unit compiles in parallel; the link is skipped when a stamp of the sources
-and flags is unchanged. The library goes to ``paper_1811_12843_gb300/_lib/liblipz.so``.
+Each translation unit compiles in parallel; the work is skipped when a stamp of the sources
+and flags is unchanged. Both go to ``paper_1811_12843_gb300/_lib/``.
 """
 
 import concurrent.futures
 import hashlib
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -17,6 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT_DIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(OUT_DIR, "liblipz.so")
+BINDING = os.path.join(OUT_DIR, "torch_operators.so")
 
 SOURCES = ["api.cu", "simt_kernels.cu", "gemm_tc.cu", "fwd_tc.cu", "bwd_tc.cu", "noalloc.cu",
            "conv_kernels.cu", "dcgan.cu", "conv_tc.cu", "operators.cu", "op_linear.cu", "op_gemm.cu",
@@ -33,8 +37,35 @@ def _nvcc():
     raise RuntimeError("nvcc not found")
 
 
+def _torch_dir():
+    """torch's installation, found without importing it."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None or not spec.origin:
+        raise RuntimeError("torch not found")
+    return os.path.dirname(spec.origin)
+
+
+def _cxx():
+    for cand in (os.environ.get("CXX"), "g++", "c++"):
+        if cand and shutil.which(cand):
+            return cand
+    raise RuntimeError("no host C++ compiler found")
+
+
+def _run(cmd, what, verbose=False):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("%s failed:\n%s\n%s" % (what, " ".join(cmd), r.stderr))
+    if verbose and r.stderr:
+        sys.stderr.write(r.stderr)
+
+
 def _stamp():
     h = hashlib.sha256()
+    # (the binding goes by torch's headers and Python's)
+    with open(os.path.join(_torch_dir(), "version.py"), "rb") as f:
+        h.update(f.read())
+    h.update(sys.version.encode())
     for d in (CSRC, INCLUDE):
         for name in sorted(os.listdir(d)):
             p = os.path.join(d, name)
@@ -52,7 +83,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     os.makedirs(OUT_DIR, exist_ok=True)
     stamp_file = os.path.join(OUT_DIR, "stamp")
     stamp = _stamp() + "|" + " ".join(extra_flags)
-    if not force and os.path.exists(LIB) and os.path.exists(stamp_file):
+    if not force and os.path.exists(LIB) and os.path.exists(BINDING) and os.path.exists(stamp_file):
         with open(stamp_file) as f:
             if f.read() == stamp:
                 return LIB
@@ -63,21 +94,32 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     def compile_one(src):
         obj = os.path.join(obj_dir, src.replace(".cu", ".o"))
         cmd = [nvcc] + ARCH + FLAGS + list(extra_flags) + ["-c", os.path.join(CSRC, src), "-o", obj]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError("nvcc failed for %s:\n%s\n%s" % (src, " ".join(cmd), r.stderr))
-        if verbose and r.stderr:
-            sys.stderr.write(r.stderr)
+        _run(cmd, "nvcc of " + src, verbose)
         return obj
 
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    torch_dir = _torch_dir()
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+    binding_obj = os.path.join(obj_dir, "torch_operators.o")
+    binding_cmd = [_cxx(), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I" + INCLUDE]
+    for d in (os.path.join(torch_dir, "include"),
+              os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+              sysconfig.get_paths()["include"], os.path.join(cuda, "include")):
+        binding_cmd += ["-isystem", d]
+    binding_cmd += ["-c", os.path.join(CSRC, "torch_operators.cpp"), "-o", binding_obj]
+
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(_run, binding_cmd, "the binding's compilation", verbose)
         objs = list(ex.map(compile_one, SOURCES))
+        binding.result()
     tmp = LIB + ".tmp"
-    cmd = [nvcc] + ARCH + ["-shared", "-o", tmp] + objs
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("link failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
+    _run([nvcc] + ARCH + ["-shared", "-o", tmp] + objs, "link")
     os.replace(tmp, LIB)
+    # (torch's libraries are loaded by then: the binding is imported after torch)
+    tmp = BINDING + ".tmp"
+    _run([_cxx(), "-shared", "-o", tmp, binding_obj, "-L" + OUT_DIR, "-llipz", "-Wl,-rpath,$ORIGIN",
+          "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
+          "-lc10_cuda", "-lc10"], "the binding's link")
+    os.replace(tmp, BINDING)
     with open(stamp_file, "w") as f:
         f.write(stamp)
     return LIB
