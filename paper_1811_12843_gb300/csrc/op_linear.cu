@@ -346,11 +346,14 @@ uint64_t linear_workspace(const lipz_linear_args& a) {
   return a.groups == 0 || a.rows == 0 || few_rows(a) ? 0 : plan_products(product_of(a)).bytes;
 }
 
-cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {
+cudaError_t linear(const lipz_linear_args& a, cudaStream_t st, uint64_t* need) {
+  *need = 0;
   if (a.groups == 0 || a.rows == 0) return cudaSuccess;
   if (few_rows(a)) return linear_rows(a, epilogue_of(a), st);
   Products q = product_of(a);
   const GemmPlan plan = plan_products(q);
+  *need = plan.bytes;
+  if (!space_given(a.workspace, a.workspace_bytes, *need)) return cudaSuccess;
   RowCopy copies[4];
   const int n = plan_copies(plan, &q, a.workspace, copies);
   const cudaError_t e = run_copies(copy_jobs(copies, n), st);
@@ -359,7 +362,8 @@ cudaError_t linear(const lipz_linear_args& a, cudaStream_t st) {
 
 uint64_t linear_backward_workspace(const lipz_linear_backward_args& a) { return back_plan(a).bytes; }
 
-cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st) {
+cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st, uint64_t* need) {
+  *need = 0;
   if (a.groups == 0) return cudaSuccess;
   if (a.rows == 0) {  // sums over no rows
     cudaError_t e = cudaSuccess;
@@ -375,6 +379,8 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st)
     return e;
   }
   BackPlan b = back_plan(a);
+  *need = b.bytes;
+  if (!space_given(a.workspace, a.workspace_bytes, *need)) return cudaSuccess;
   bf16* du = b.need_du ? (bf16*)a.workspace : nullptr;
   float* part = a.db.data ? (float*)((char*)a.workspace + b.du_bytes) : nullptr;
   char* rest = (char*)a.workspace + b.du_bytes + b.db_bytes;

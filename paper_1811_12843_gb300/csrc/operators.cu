@@ -131,9 +131,10 @@ struct Check {
     return rc == LIPZ_OK;
   }
   bool space(const void* p, uint64_t have, uint64_t need) {
-    if (rc == LIPZ_OK && need && (!p || have < need))
+    if (rc != LIPZ_OK || ops::space_given(p, have, need)) return rc == LIPZ_OK;
+    if (!p || have < need)
       rc = fail(LIPZ_ERR_INVALID, "%s: the workspace must hold %llu bytes", call, (unsigned long long)need);
-    if (rc == LIPZ_OK && need && (uintptr_t)p % 256)
+    else
       rc = fail(LIPZ_ERR_INVALID, "%s: the workspace must be 256-byte aligned", call);
     return rc == LIPZ_OK;
   }
@@ -277,9 +278,11 @@ int lipz_linear_workspace(const lipz_linear_args* a, uint64_t* bytes) {
 int lipz_linear(const lipz_linear_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear", a->groups, a->rows};
-  if (!c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a))) return c.rc;
   if (int rc = take_timeout(c.call)) return rc;
-  return finish(c.call, ops::linear(*a, (cudaStream_t)stream));
+  uint64_t need;
+  const cudaError_t e = ops::linear(*a, (cudaStream_t)stream, &need);
+  if (!c.space(a->workspace, a->workspace_bytes, need)) return c.rc;
+  return finish(c.call, e);
 }
 
 int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t* bytes) {
@@ -292,9 +295,11 @@ int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t*
 int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear_backward", a->groups, a->rows};
-  if (!c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a))) return c.rc;
   if (int rc = take_timeout(c.call)) return rc;
-  return finish(c.call, ops::linear_backward(*a, (cudaStream_t)stream));
+  uint64_t need;
+  const cudaError_t e = ops::linear_backward(*a, (cudaStream_t)stream, &need);
+  if (!c.space(a->workspace, a->workspace_bytes, need)) return c.rc;
+  return finish(c.call, e);
 }
 
 int lipz_operator_status(void) { return take_timeout("lipz_operator_status"); }

@@ -43,10 +43,16 @@ cudaError_t quantize_rows(const lipz_quantize_rows_args& a, cudaStream_t st);
 cudaError_t sum_parts(const float* part, int64_t groups, int parts, int64_t cols, lipz_vec out, int ways,
                       cudaStream_t st);
 
+// Whether a call has the scratch memory that it needs.
+inline bool space_given(const void* p, uint64_t have, uint64_t need) {
+  return !need || (p && have >= need && (uintptr_t)p % 256 == 0);
+}
+// *need: the scratch memory; nothing is launched where the call does not have it. (The plan that tells is the
+// launch's own: a call plans once.)
 uint64_t linear_workspace(const lipz_linear_args& a);
-cudaError_t linear(const lipz_linear_args& a, cudaStream_t st);
+cudaError_t linear(const lipz_linear_args& a, cudaStream_t st, uint64_t* need);
 uint64_t linear_backward_workspace(const lipz_linear_backward_args& a);
-cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st);
+cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st, uint64_t* need);
 
 }  // namespace ops
 }  // namespace lipz
