@@ -1,8 +1,9 @@
 // Root-mean-square norm with the residual's addition (forward and backward) and the row quantiser.
 //
 // A row's elements are read once and stay in the registers of its threads (multiples of 32 of them, NV
-// vectors of E elements each) between the row's sums and its results. Few rows are loaded by their threads;
-// many stream through a ring of shared-memory stages.
+// vectors of E elements each, or a part of a warp) between the row's sums and its results. Few rows are loaded
+// by their threads; many short ones by warps that take several at a time; many longer ones stream through a ring
+// of shared-memory stages.
 // Bound: HBM; a launch and two memory latencies for a few rows.
 #include "ops.cuh"
 #include "tc_ptx.cuh"
@@ -160,6 +161,87 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
     red = join<!QUANT, true>(s_red, sub * (p.tpr >> 5), p.tpr >> 5);
   }
   if (live) row_results<T, E, NV, QUANT>(p, g, gr, red, v, t, p.tpr, nvec);
+}
+
+// ---- many short rows: a warp walks over sets of 32 / L rows, L lanes to a row of 32 elements each. The next
+// set's loads are in flight while this one is summed and written, and a lane's weights stay in its registers.
+// No barrier; and a row's fixed work (sums over lanes, places, scales) is shared by 32 / L rows. Bound: HBM.
+// Measured against a block and a ring per row, as in k_rows_stream: bf16 131072 x 256 norm 61 -> 27 us (134 MB,
+// 0.74 of the copy rate), with residual to 8 bits 78 -> 38 (0.92), quantiser 41 -> 19; 262144 x 64 113 -> 17;
+// 65536 x 784 68 -> 48; fp32 131072 x 256 68 -> 44. With 32 lanes to each row 131072 x 256 took 45 us.
+constexpr int SHORT_WARPS = 4, SHORT_BLOCKS = 8;  // warps of a block; blocks per SM at most
+
+template <typename T, int E, int L, bool QUANT>
+__global__ void __launch_bounds__(32 * SHORT_WARPS) k_rows_short(const RowArgs p) {
+  constexpr int NV = 32 / E, R = 32 / L;
+  const int lane = threadIdx.x & 31, t = lane % L, sub = lane / L, nvec = p.dim / E;
+  const int64_t step = (int64_t)gridDim.x * SHORT_WARPS * R;
+  const bool has_res = !QUANT && p.residual.data, want_top = QUANT || p.scale.data;
+  pdl_wait();
+  Raw<T, E> x[NV], res[NV];
+  auto bring = [&](int64_t r) {
+    const bool live = r < p.total;
+    const int64_t g = live ? group_of(p, r) : 0, gr = r - g * p.rows;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = t + i * L;
+      x[i].zero();
+      if (!QUANT) res[i].zero();
+      if (live && c < nvec) {
+        x[i].load(row_of<const T>(p.x, g, gr) + c * E);
+        if (has_res) res[i].load(row_of<const T>(p.residual, g, gr) + c * E);
+      }
+    }
+  };
+  float w[NV][E];
+  int64_t w_at = -1;  // where in p.weight w is from
+  int64_t r = ((int64_t)blockIdx.x * SHORT_WARPS + (threadIdx.x >> 5)) * R + sub;
+  bring(r);
+  for (; r - sub < p.total; r += step) {  // (the same turns for all lanes of a warp)
+    float v[NV][E];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[i][e] = x[i].get(e);
+        if (has_res) v[i][e] += res[i].get(e);
+      }
+    bring(r + step);
+    const bool live = r < p.total;
+    const int64_t g = live ? group_of(p, r) : 0, gr = r - g * p.rows;
+    Sums red{0.f, 0u};
+    if constexpr (!QUANT) {
+      if (live && p.sum.data)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (t + i * L < nvec) store_vec<T, E>(row_of<T>(p.sum, g, gr) + (t + i * L) * E, v[i]);
+      if (g * p.weight.group != w_at) {
+        w_at = g * p.weight.group;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (t + i * L < nvec) load_params<E>(p.weight.data + w_at + (t + i * L) * E, w[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (t + i * L < nvec)
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            red.ss = fmaf(v[i][e], v[i][e], red.ss);
+            v[i][e] *= w[i][e];
+          }
+    }
+    if (want_top)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) {
+      if (!QUANT) red.ss += __shfl_xor_sync(0xffffffffu, red.ss, o);
+      if (want_top) red.top = max(red.top, __shfl_xor_sync(0xffffffffu, red.top, o));
+    }
+    if (live) row_results<T, E, NV, QUANT>(p, g, gr, red, v, t, L, nvec);
+  }
 }
 
 // ---- many rows: a block of one row's threads walks over rows that arrive in a ring of shared-memory
@@ -831,11 +913,12 @@ struct StreamShape {
 };
 // `params`: fp32 parameters of a column that stand in shared memory (k_rows_shift and its backward, whose
 // rows touch up to two units more).
-StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int params = 0) {
+// wide: 32 elements per thread wherever the row is.
+StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int params = 0, bool wide = false) {
   StreamShape s;
   const int nvec = params ? (int)ceil_div(dim + 2 * e - 2, e) : dim / e;
   const int fixed = params * (dim + dim / 32 + 2) * 4;
-  s.wide = row_threads(nvec, 16 / e) > 512;
+  s.wide = row_threads(nvec, 16 / e) > 512 || wide;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
   s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;
   const int budget = 216 * 1024, row = s.slot * arrays;
@@ -896,15 +979,34 @@ cudaError_t launch_shift(const RowArgs& p, cudaStream_t st) {
   return s.wide ? go(k_rows_shift<T, E, 32 / E, QUANT>) : go(k_rows_shift<T, E, 16 / E, QUANT>);
 }
 
+template <typename T, int E, int L, bool QUANT>
+cudaError_t launch_short(const RowArgs& p, cudaStream_t st) {
+  const int64_t most = (int64_t)sm_count() * SHORT_BLOCKS, want = ceil_div(p.total, SHORT_WARPS * (32 / L));
+  return launch_pdl(k_rows_short<T, E, L, QUANT>, dim3((unsigned)(want < most ? want : most)),
+                    dim3(32 * SHORT_WARPS), 0, st, p);
+}
+
 template <typename T, int E, bool QUANT>
 cudaError_t launch_rows(RowArgs& p, cudaStream_t st) {
+  if constexpr (E > 1) {
+    const int lanes = (int)ceil_div(p.dim, 32);
+    if (p.total > STREAM_ROWS * sm_count() && lanes <= 32) {
+      if (lanes <= 2) return launch_short<T, E, 2, QUANT>(p, st);
+      if (lanes <= 4) return launch_short<T, E, 4, QUANT>(p, st);
+      if (lanes <= 8) return launch_short<T, E, 8, QUANT>(p, st);
+      if (lanes <= 16) return launch_short<T, E, 16, QUANT>(p, st);
+      return launch_short<T, E, 32, QUANT>(p, st);
+    }
+  }
   if (p.total > STREAM_ROWS * sm_count()) {
     constexpr int U = 16 / sizeof(T);
     const int64_t groups = p.total / p.rows;
     if (E == 1 && p.dim <= SHIFT_MAX_DIM && same_shift(p.x, p.y, groups, p.rows, U) &&
         same_shift(p.x, p.residual, groups, p.rows, U) && same_shift(p.x, p.sum, groups, p.rows, U))
       return launch_shift<T, QUANT>(p, st);
-    const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 2048);
+    // bf16 rows in 32 elements per thread, since a row's fixed work is each thread's: 16384 x 4096 norm 58 -> 52
+    // us, with residual to 8 bits 77 -> 73, quantiser 39 -> 35; fp32 rows lose (85 -> 135 us: registers).
+    const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 2048, 0, E == 8);
     return s.wide ? launch_stream<T, E, 32 / E, QUANT>(p, s, st)
                   : launch_stream<T, E, 16 / E, QUANT>(p, s, st);
   }

@@ -213,6 +213,49 @@ def test_rmsnorm_backward(groups, rows, dim, dtype, with_dsum):
     assert torch.equal(dx, dx3) and torch.equal(dw, dw3)
 
 
+# widths on both sides of the lanes that take a row, many rows, and counts that leave a last set in part
+@pytest.mark.parametrize("groups,rows,dim", [(1, 1237, 8), (1, 700, 64), (3, 301, 72), (1, 2001, 128), (2, 777, 136),
+                                             (144, 10, 256), (1, 650, 264), (1, 621, 512), (1, 613, 520),
+                                             (5, 131, 784), (1, 609, 1024), (1, 615, 1032), (1, 640, 2048)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("residual,e4m3", [(False, False), (True, False), (True, True)])
+def test_many_short_rows(groups, rows, dim, dtype, residual, e4m3):
+    test_rmsnorm(groups, rows, dim, dtype, residual, e4m3, not e4m3)
+    if not residual:
+        test_quantize_rows(groups, rows, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 256, 784])
+def test_many_short_rows_with_extremes_and_strides(dtype, dim):
+    """Rows cut from wider ones, groups woven row by row, a shared weight, the stream updated in place; rows
+    of zeros, of NaN and infinity and of the type's ends among them, each of which stays in its row."""
+    rows, groups = 300, 4
+    wide = randn(131, (rows, groups, dim + 16), 1.0, dtype)
+    x = wide[:, :, 8:8 + dim].permute(1, 0, 2)
+    w = (1 + randn(132, (1, dim), 0.1, F32)).expand(groups, dim)
+    own = randn(133, (groups, rows, dim), 1.0, dtype)
+    before, rest = own.clone(), wide.clone()
+    r = ops.rmsnorm(x, w, residual=own, sum_out=own)
+    check_norm(r, x, before, w, 1e-6, False, False)
+    assert torch.equal(rest, wide)
+    x = x.clone()
+    x[0, 5], x[1, 6, 3], x[2, 7, 0] = 0.0, float("nan"), float("inf")
+    x[3, 8] *= 1e-38
+    x[0, 9] = torch.finfo(dtype).max
+    q, s = ops.quantize_rows(x)
+    y = ops.rmsnorm(x, w, e4m3=True)
+    bad = torch.zeros(groups, rows, dtype=torch.bool, device="cuda")
+    bad[1, 6] = bad[2, 7] = True
+    for scale in (s, y.scale):
+        assert torch.equal(~torch.isfinite(scale[bad]), torch.ones(2, dtype=torch.bool, device="cuda"))
+    assert torch.isfinite(s[~bad]).all() and torch.isfinite(q.float()[~bad]).all()
+    few_q, few_s = ops.quantize_rows(x[:, 4:10].contiguous())  # the same rows by the kernel for a few
+    assert torch.equal(few_s.isnan(), s[:, 4:10].isnan())
+    assert torch.equal(torch.nan_to_num(few_s), torch.nan_to_num(s[:, 4:10]))
+    assert torch.equal(torch.nan_to_num(few_q.float()), torch.nan_to_num(q.float()[:, 4:10]))
+
+
 def test_rmsnorm_gradients_are_those_of_the_forward():
     """Against central differences of the definition in 64 bits, along random directions."""
     rows, dim, eps = 5, 48, 1e-3
