@@ -782,24 +782,25 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
   if (p.dweight.data) join_cluster(p, g, s_dw, [](int c) { return padded(c); });
 }
 
-// Short rows: a warp per row, loaded into registers one row ahead; a block of WARPS walks over rows of one
-// group, and its warps' sums for dweight are added in shared memory. (With a ring and a block per row,
-// 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks' own set-up.)
+// Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of WARPS
+// walks over rows of one group, and its warps' sums for dweight are added in shared memory. (With a ring and a
+// block per row, 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks' own set-up; 10 so.
+// With 32 lanes to every row bf16 131072 x 256 took 54 us instead of 39, 262144 x 64 77 instead of 23.)
 template <int NV>
-constexpr int BACK_WARPS = NV == 1 ? 16 : 8;  // (registers)
+constexpr int BACK_WARPS = NV <= 2 ? 16 : 8;  // (registers)
 
-template <typename T, int E, int NV>
+template <typename T, int E, int NV, int L>
 __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(const BackArgs p) {
-  constexpr int WARPS = BACK_WARPS<NV>;
+  constexpr int WARPS = BACK_WARPS<NV>, R = 32 / L;
   extern __shared__ float s_dw[];  // [WARPS][dim]
-  const int warp = threadIdx.x >> 5, t = threadIdx.x & 31, nvec = p.dim / E;
-  const int64_t g = blockIdx.y, step = (int64_t)gridDim.x * WARPS;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane % L, sub = lane / L, nvec = p.dim / E;
+  const int64_t g = blockIdx.y, step = (int64_t)gridDim.x * WARPS * R;
   pdl_wait();
   float w[NV][E], dw[NV][E];
   const float* weight = p.weight.data + g * p.weight.group;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = t + i * 32;
+    const int c = t + i * L;
 #pragma unroll
     for (int e = 0; e < E; ++e) w[i][e] = dw[i][e] = 0.f;
     if (c < nvec) load_params<E>(weight + c * E, w[i]);
@@ -808,11 +809,16 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(c
   Raw<T, E> dy[NV], s[NV], ds[NV];
   float rstd = 0.f;
   auto load = [&](int64_t r) {
-    if (r >= p.rows) return;
+    if (r >= p.rows) {  // (a row of zeros adds nothing to the sums)
+      rstd = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) dy[i].zero(), s[i].zero();
+      return;
+    }
     rstd = p.rstd.data[g * p.rstd.group + r];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = t + i * 32;
+      const int c = t + i * L;
       if (c < nvec) {
         dy[i].load(row_of<const T>(p.dy, g, r) + c * E);
         s[i].load(row_of<const T>(p.s, g, r) + c * E);
@@ -822,9 +828,9 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(c
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) dy[i].zero(), s[i].zero(), ds[i].zero();
-  int64_t r = (int64_t)blockIdx.x * WARPS + warp;
+  int64_t r = ((int64_t)blockIdx.x * WARPS + warp) * R + sub;
   load(r);
-  for (; r < p.rows; r += step) {
+  for (; r - sub < p.rows; r += step) {  // (the same turns for all lanes of a warp)
     Raw<T, E> a[NV], b[NV], c3[NV];
     const float f = rstd;
 #pragma unroll
@@ -839,12 +845,14 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(c
         dw[i][e] = fmaf(m, f, dw[i][e]);
         along = fmaf(m, w[i][e], along);
       }
-    along = warp_reduce<true, false>(Sums{along, 0u}).ss;
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) along += __shfl_xor_sync(0xffffffffu, along, o);
+    if (r >= p.rows) continue;
     const float c2 = f * f * (along * p.inv_dim);
     T* dx = row_of<T>(p.dx, g, r);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = t + i * 32;
+      const int c = t + i * L;
       if (c < nvec) {
         float v[E];
 #pragma unroll
@@ -857,9 +865,12 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(c
   if (!p.dweight.data) return;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (t + i * 32 < nvec)
 #pragma unroll
-      for (int e = 0; e < E; ++e) s_dw[warp * p.dim + (t + i * 32) * E + e] = dw[i][e];
+    for (int e = 0; e < E; ++e) {
+#pragma unroll
+      for (int o = L; o < 32; o <<= 1) dw[i][e] += __shfl_xor_sync(0xffffffffu, dw[i][e], o);
+      if (sub == 0 && t + i * L < nvec) s_dw[warp * p.dim + (t + i * L) * E + e] = dw[i][e];
+    }
   __syncthreads();
   float* out = p.part ? p.part + (g * gridDim.x + blockIdx.x) * (int64_t)p.dim
                       : p.dweight.data + g * p.dweight.group;
@@ -1028,10 +1039,16 @@ bool backward_vec(const lipz_rmsnorm_backward_args& a) {
          rows_aligned(a.weight, a.groups, 16);
 }
 
-// Rows of up to 1024 elements in whole vectors go to the warp-per-row kernel: 0, or its vectors per thread.
-int backward_row_vectors(const lipz_rmsnorm_backward_args& a) {
-  const int64_t per = ceil_div(a.dim, 32 * (16 / type_bytes(a.dy.type)));
-  return !backward_vec(a) || per > 4 ? 0 : per <= 1 ? 1 : per <= 2 ? 2 : 4;
+// Lanes of a row in k_rmsnorm_backward_rows, two vectors to each (past 32: four to each of 32).
+int back_lanes(int64_t nvec) {
+  int lanes = 4;
+  while (lanes < 64 && lanes * 2 < nvec) lanes *= 2;
+  return lanes;
+}
+
+// Whether rows go there: up to 128 whole vectors.
+bool backward_short(const lipz_rmsnorm_backward_args& a) {
+  return backward_vec(a) && ceil_div(a.dim, 16 / type_bytes(a.dy.type)) <= 128;
 }
 
 bool backward_shift(const lipz_rmsnorm_backward_args& a) {
@@ -1090,15 +1107,18 @@ cudaError_t launch_back_shift(const BackArgs& p, const StreamShape& s, int64_t g
 }
 
 template <typename T>
-cudaError_t launch_back_rows(const BackArgs& p, int nv, int64_t groups, int blocks, cudaStream_t st) {
+cudaError_t launch_back_rows(const BackArgs& p, int64_t groups, int blocks, cudaStream_t st) {
   constexpr int E = 16 / sizeof(T);
   auto go = [&](auto kernel, int warps) {
     return launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(32 * warps),
                       (size_t)warps * p.dim * 4, st, p);
   };
-  if (nv == 1) return go(k_rmsnorm_backward_rows<T, E, 1>, BACK_WARPS<1>);
-  if (nv == 2) return go(k_rmsnorm_backward_rows<T, E, 2>, BACK_WARPS<2>);
-  return go(k_rmsnorm_backward_rows<T, E, 4>, BACK_WARPS<4>);
+  const int lanes = back_lanes(p.dim / E);
+  if (lanes > 32) return go(k_rmsnorm_backward_rows<T, E, 4, 32>, BACK_WARPS<4>);
+  if (lanes == 32) return go(k_rmsnorm_backward_rows<T, E, 2, 32>, BACK_WARPS<2>);
+  if (lanes == 16) return go(k_rmsnorm_backward_rows<T, E, 2, 16>, BACK_WARPS<2>);
+  if (lanes == 8) return go(k_rmsnorm_backward_rows<T, E, 2, 8>, BACK_WARPS<2>);
+  return go(k_rmsnorm_backward_rows<T, E, 2, 4>, BACK_WARPS<2>);
 }
 
 template <typename T, int E>
@@ -1165,10 +1185,11 @@ struct BackBlocks {
 };
 BackBlocks backward_blocks(const lipz_rmsnorm_backward_args& a) {
   const int64_t groups = a.groups > 0 ? a.groups : 1;
-  if (const int nv = backward_row_vectors(a)) {
-    // two blocks per SM; one block per group, which needs no second launch, from half that many groups on
-    const int warps = nv == 1 ? BACK_WARPS<1> : BACK_WARPS<2>;
-    const int64_t fill = 2 * sm_count() / groups, most = ceil_div(a.rows, 2 * warps);
+  if (backward_short(a)) {
+    // sixteen warps per SM; one block per group, which needs no second launch, from half that many groups on
+    const int lanes = back_lanes(ceil_div(a.dim, 16 / type_bytes(a.dy.type)));
+    const int warps = lanes > 32 ? BACK_WARPS<4> : BACK_WARPS<2>, set = warps * (lanes > 32 ? 1 : 32 / lanes);
+    const int64_t fill = (int64_t)(16 / warps) * sm_count() / groups, most = ceil_div(a.rows, 2 * set);
     const int64_t b = fill < 4 ? 1 : fill < most ? fill : most;
     return {b < 1 ? 1 : (int)b, b < 1 ? 1 : (int)b};
   }
@@ -1194,11 +1215,10 @@ cudaError_t rmsnorm_backward(const lipz_rmsnorm_backward_args& a, cudaStream_t s
                    parts > 1 ? (float*)a.workspace : nullptr, a.rows, (int)a.dim,
                    1.f / (float)a.dim};
   const bool vec = backward_vec(a);
-  const int nv = backward_row_vectors(a);
   cudaError_t e;
-  if (nv)
-    e = a.dy.type == LIPZ_FP32 ? launch_back_rows<float>(p, nv, a.groups, blocks, st)
-                               : launch_back_rows<bf16>(p, nv, a.groups, blocks, st);
+  if (backward_short(a))
+    e = a.dy.type == LIPZ_FP32 ? launch_back_rows<float>(p, a.groups, blocks, st)
+                               : launch_back_rows<bf16>(p, a.groups, blocks, st);
   else if (backward_shift(a))
     e = a.dy.type == LIPZ_FP32 ? launch_back_shift<float>(p, s, a.groups, blocks, st)
                                : launch_back_shift<bf16>(p, s, a.groups, blocks, st);

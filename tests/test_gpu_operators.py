@@ -225,6 +225,15 @@ def test_many_short_rows(groups, rows, dim, dtype, residual, e4m3):
         test_quantize_rows(groups, rows, dim, dtype)
 
 
+@pytest.mark.parametrize("groups,rows,dim", [(1, 1237, 8), (1, 700, 32), (3, 301, 72), (1, 2001, 128), (2, 777, 136),
+                                             (7, 33, 256), (1, 650, 264), (1, 621, 512), (1, 613, 520),
+                                             (5, 131, 784), (1, 609, 1024), (80, 3, 64), (1, 3000, 264)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("with_dsum", [False, True])
+def test_many_short_rows_backward(groups, rows, dim, dtype, with_dsum):
+    test_rmsnorm_backward(groups, rows, dim, dtype, with_dsum)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("dim", [64, 256, 784])
 def test_many_short_rows_with_extremes_and_strides(dtype, dim):
