@@ -167,12 +167,13 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
 // set's loads are in flight while this one is summed and written, and a lane's weights stay in its registers.
 // No barrier; and a row's fixed work (sums over lanes, places, scales) is shared by 32 / L rows. Bound: HBM.
 // Measured against a block and a ring per row, as in k_rows_stream: bf16 131072 x 256 norm 61 -> 27 us (134 MB,
-// 0.74 of the copy rate), with residual to 8 bits 78 -> 38 (0.92), quantiser 41 -> 19; 262144 x 64 113 -> 17;
-// 65536 x 784 68 -> 48; fp32 131072 x 256 68 -> 44. With 32 lanes to each row 131072 x 256 took 45 us.
-constexpr int SHORT_WARPS = 4, SHORT_BLOCKS = 8;  // warps of a block; blocks per SM at most
+// 0.74 of the copy rate), with residual to 8 bits 78 -> 39 (0.89), quantiser 41 -> 18; 262144 x 64 113 -> 17;
+// 65536 x 784 68 -> 48; fp32 131072 x 256 68 -> 43 (0.92). With 32 lanes to each row 131072 x 256 took 45 us.
+constexpr int SHORT_WARPS = 4;  // of a block
 
+// (bf16 in at most 128 registers, for four blocks per SM: three take 31 us)
 template <typename T, int E, int L, bool QUANT>
-__global__ void __launch_bounds__(32 * SHORT_WARPS) k_rows_short(const RowArgs p) {
+__global__ void __launch_bounds__(32 * SHORT_WARPS, E == 8 ? 4 : 3) k_rows_short(const RowArgs p) {
   constexpr int NV = 32 / E, R = 32 / L;
   const int lane = threadIdx.x & 31, t = lane % L, sub = lane / L, nvec = p.dim / E;
   const int64_t step = (int64_t)gridDim.x * SHORT_WARPS * R;
@@ -333,7 +334,7 @@ template <typename T, int E, int NV, bool QUANT>
 __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages, int slot, int* err) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Sums s_red[2][16];
-  const bool has_res = !QUANT && p.residual.data;
+  const bool has_res = !QUANT && p.residual.data, want_top = QUANT || p.scale.data;
   const Ring q = ring_init(smem, stages, slot, has_res ? 2 : 1);
   const int t = threadIdx.x, tpr = blockDim.x, nvec = p.dim / E, bytes = p.dim * (int)sizeof(T);
   pdl_wait();
@@ -395,8 +396,9 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
           for (int e = 0; e < E; ++e) v[i][e] *= w[e];
         }
       }
+      if (want_top)
 #pragma unroll
-      for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+        for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
     }
     red = block_reduce<!QUANT, true>(red, s_red[turn >> 1 & 1]);
     // (the row is in registers everywhere: its stage takes the row that comes `stages` later)
@@ -413,8 +415,8 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
 
 // ---- rows that start off the 16-byte grid (odd widths), all of a call's matrices at the same place of a
 // 16-byte unit in each row: threads take the whole units that a row touches, and the first and the last of
-// them in part. Parameters stand in shared memory, one word in 33 left out, so that lanes E columns apart
-// meet different banks. (Element by element, 16385 x 4097 with residual to 8 bits took 262 us, and 332
+// them in part. Parameters stand in shared memory, one word in E + 1 (in the backward pass one in 33) left out,
+// so that lanes E columns apart meet different banks. (Element by element, 16385 x 4097 with residual to 8 bits took 262 us, and 332
 // backward.)
 __device__ __forceinline__ int padded(int c) { return c + (c >> 5); }
 
@@ -453,6 +455,7 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Sums s_red[2][16];
   const bool has_res = !QUANT && p.residual.data, one = p.total == p.rows || p.weight.group == 0;
+  const bool want_top = QUANT || p.scale.data;
   const Ring q = ring_init(smem, stages, slot, has_res ? 2 : 1);
   float* s_w = reinterpret_cast<float*>(smem + RING_BARS + stages * q.arrays * slot);
   const int t = threadIdx.x, tpr = blockDim.x, dim = p.dim, bytes = dim * (int)sizeof(T);
@@ -469,7 +472,9 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
       if (r < p.total) load(r, s);
     }
   if (!QUANT && one) {
-    for (int c = t; c < dim; c += tpr) s_w[padded(c)] = p.weight.data[c];
+    // (zeros on either side; one word in E + 1 is left out: lanes E columns apart meet different banks)
+    for (int c = t - E; c < dim + E; c += tpr)
+      s_w[c + E + (c + E) / E] = c >= 0 && c < dim ? p.weight.data[c] : 0.f;
     __syncthreads();
   }
   int stage = 0;
@@ -496,9 +501,10 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
 #pragma unroll
           for (int e = 0; e < E; ++e) v[i][e] += w[e];
         }
+        if (!u.whole)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (!u.in(e, dim)) v[i][e] = 0.f;
+          for (int e = 0; e < E; ++e)
+            if (!u.in(e, dim)) v[i][e] = 0.f;
         if (!QUANT && p.sum.data) store_unit<T, E>(row_of<T>(p.sum, g, gr), u, dim, v[i]);
       }
     }
@@ -509,15 +515,15 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
 #pragma unroll
         for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
         if (u.live) {
+          const float* w = s_w + (t + i * tpr) * (E + 1) + E - m;
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int c = min(max(u.col + e, 0), dim - 1);
-            v[i][e] *= u.in(e, dim) ? (one ? s_w[padded(c)] : __ldg(weight + c)) : 0.f;
-          }
+          for (int e = 0; e < E; ++e)
+            v[i][e] *= one ? w[e + (e >= m)] : u.in(e, dim) ? __ldg(weight + u.col + e) : 0.f;
         }
       }
+      if (want_top)
 #pragma unroll
-      for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+        for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
     }
     red = block_reduce<!QUANT, true>(red, s_red[turn >> 1 & 1]);
     if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
@@ -928,7 +934,8 @@ struct StreamShape {
 StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int params = 0, bool wide = false) {
   StreamShape s;
   const int nvec = params ? (int)ceil_div(dim + 2 * e - 2, e) : dim / e;
-  const int fixed = params * (dim + dim / 32 + 2) * 4;
+  // (k_rows_shift: columns and E more on either side, one word in E + 1 left out)
+  const int fixed = params == 1 ? ((dim + 2 * e) / e + 1) * (e + 1) * 4 : params * (dim + dim / 32 + 2) * 4;
   s.wide = row_threads(nvec, 16 / e) > 512 || wide;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
   s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;
@@ -990,9 +997,17 @@ cudaError_t launch_shift(const RowArgs& p, cudaStream_t st) {
   return s.wide ? go(k_rows_shift<T, E, 32 / E, QUANT>) : go(k_rows_shift<T, E, 16 / E, QUANT>);
 }
 
+// (one wave of blocks: with a wave and a half 131072 x 256 took 33 us instead of 27)
 template <typename T, int E, int L, bool QUANT>
 cudaError_t launch_short(const RowArgs& p, cudaStream_t st) {
-  const int64_t most = (int64_t)sm_count() * SHORT_BLOCKS, want = ceil_div(p.total, SHORT_WARPS * (32 / L));
+  static const int resident = [] {
+    int n = 0;
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_rows_short<T, E, L, QUANT>,
+                                                                        32 * SHORT_WARPS, 0);
+    if (e != cudaSuccess) cudaGetLastError();
+    return e == cudaSuccess && n > 0 ? n : 4;
+  }();
+  const int64_t most = (int64_t)sm_count() * resident, want = ceil_div(p.total, SHORT_WARPS * (32 / L));
   return launch_pdl(k_rows_short<T, E, L, QUANT>, dim3((unsigned)(want < most ? want : most)),
                     dim3(32 * SHORT_WARPS), 0, st, p);
 }
