@@ -38,11 +38,9 @@ def _nvcc():
 
 
 def _torch_dir():
-    """torch's installation, found without importing it."""
+    """torch's installation, found without importing it; None without one (and then no binding)."""
     spec = importlib.util.find_spec("torch")
-    if spec is None or not spec.origin:
-        raise RuntimeError("torch not found")
-    return os.path.dirname(spec.origin)
+    return os.path.dirname(spec.origin) if spec is not None and spec.origin else None
 
 
 def _cxx():
@@ -63,8 +61,10 @@ def _run(cmd, what, verbose=False):
 def _stamp():
     h = hashlib.sha256()
     # (the binding goes by torch's headers and Python's)
-    with open(os.path.join(_torch_dir(), "version.py"), "rb") as f:
-        h.update(f.read())
+    torch_dir = _torch_dir()
+    if torch_dir:
+        with open(os.path.join(torch_dir, "version.py"), "rb") as f:
+            h.update(f.read())
     h.update(sys.version.encode())
     for d in (CSRC, INCLUDE):
         for name in sorted(os.listdir(d)):
@@ -83,7 +83,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     os.makedirs(OUT_DIR, exist_ok=True)
     stamp_file = os.path.join(OUT_DIR, "stamp")
     stamp = _stamp() + "|" + " ".join(extra_flags)
-    if not force and os.path.exists(LIB) and os.path.exists(BINDING) and os.path.exists(stamp_file):
+    built = os.path.exists(LIB) and (os.path.exists(BINDING) or not _torch_dir())
+    if not force and built and os.path.exists(stamp_file):
         with open(stamp_file) as f:
             if f.read() == stamp:
                 return LIB
@@ -98,28 +99,33 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     torch_dir = _torch_dir()
-    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
     binding_obj = os.path.join(obj_dir, "torch_operators.o")
-    binding_cmd = [_cxx(), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I" + INCLUDE]
-    for d in (os.path.join(torch_dir, "include"),
-              os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
-              sysconfig.get_paths()["include"], os.path.join(cuda, "include")):
-        binding_cmd += ["-isystem", d]
-    binding_cmd += ["-c", os.path.join(CSRC, "torch_operators.cpp"), "-o", binding_obj]
+
+    def compile_binding():
+        cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+        cmd = [_cxx(), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I" + INCLUDE]
+        for d in (os.path.join(torch_dir, "include"),
+                  os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+                  sysconfig.get_paths()["include"], os.path.join(cuda, "include")):
+            cmd += ["-isystem", d]
+        cmd += ["-c", os.path.join(CSRC, "torch_operators.cpp"), "-o", binding_obj]
+        _run(cmd, "the binding's compilation", verbose)
 
     with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        binding = ex.submit(_run, binding_cmd, "the binding's compilation", verbose)
+        binding = ex.submit(compile_binding) if torch_dir else None
         objs = list(ex.map(compile_one, SOURCES))
-        binding.result()
+        if binding:
+            binding.result()
     tmp = LIB + ".tmp"
     _run([nvcc] + ARCH + ["-shared", "-o", tmp] + objs, "link")
     os.replace(tmp, LIB)
-    # (torch's libraries are loaded by then: the binding is imported after torch)
-    tmp = BINDING + ".tmp"
-    _run([_cxx(), "-shared", "-o", tmp, binding_obj, "-L" + OUT_DIR, "-llipz", "-Wl,-rpath,$ORIGIN",
-          "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
-          "-lc10_cuda", "-lc10"], "the binding's link")
-    os.replace(tmp, BINDING)
+    if torch_dir:
+        # (torch's libraries are loaded by then: the binding is imported after torch)
+        tmp = BINDING + ".tmp"
+        _run([_cxx(), "-shared", "-o", tmp, binding_obj, "-L" + OUT_DIR, "-llipz", "-Wl,-rpath,$ORIGIN",
+              "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
+              "-lc10_cuda", "-lc10"], "the binding's link")
+        os.replace(tmp, BINDING)
     with open(stamp_file, "w") as f:
         f.write(stamp)
     return LIB

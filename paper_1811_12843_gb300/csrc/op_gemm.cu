@@ -1118,10 +1118,10 @@ GemmPlan plan_products(const Products& q) {
   const int eb = type_bytes(g0.type);
   const bool sums = g0.e.y.type == LIPZ_FP32, res = g0.e.residual.data, heavy = g0.e.act >= LIPZ_ACT_TANH;
   // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its MMA
-  // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost a cluster's exchange, or
-  // another launch and their way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 -> 8192 in bf16
-  // (8 bits: 184 instead of 158), epilogues at 144 x 512 x 256 -> 768 without an activation, what tanh adds, what
-  // a residual adds.
+  // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost a cluster's exchange,
+  // or another launch and their way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 -> 8192
+  // in bf16 (8 bits: 184 instead of 158), epilogues at 144 x 512 x 256 -> 768 without an activation, what
+  // tanh adds, what a residual adds.
   struct Shape {
     int cg, bn;
     double step, epi, act, residual;

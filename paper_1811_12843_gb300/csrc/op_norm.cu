@@ -1,10 +1,9 @@
 // Root-mean-square norm with the residual's addition (forward and backward) and the row quantiser.
 //
 // A row's elements are read once and stay in the registers of its threads (multiples of 32 of them, NV
-// vectors of E elements each, or a part of a warp) between the row's sums and its results. Few rows are loaded
-// by their threads; many short ones by warps that take several at a time; many longer ones stream through a ring
-// of shared-memory stages.
-// Bound: HBM; a launch and two memory latencies for a few rows.
+// vectors of E elements each, or a part of a warp) between the row's sums and its results. Few rows are
+// loaded by their threads; many short ones by warps that take several at a time; many longer ones stream
+// through a ring of shared-memory stages. Bound: HBM; a launch and two memory latencies for a few rows.
 #include "ops.cuh"
 #include "tc_ptx.cuh"
 
@@ -164,11 +163,12 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
 }
 
 // ---- many short rows: a warp walks over sets of 32 / L rows, L lanes to a row of 32 elements each. The next
-// set's loads are in flight while this one is summed and written, and a lane's weights stay in its registers.
-// No barrier; and a row's fixed work (sums over lanes, places, scales) is shared by 32 / L rows. Bound: HBM.
-// Measured against a block and a ring per row, as in k_rows_stream: bf16 131072 x 256 norm 61 -> 27 us (134 MB,
-// 0.74 of the copy rate), with residual to 8 bits 78 -> 39 (0.89), quantiser 41 -> 18; 262144 x 64 113 -> 17;
-// 65536 x 784 68 -> 48; fp32 131072 x 256 68 -> 43 (0.92). With 32 lanes to each row 131072 x 256 took 45 us.
+// set's loads are in flight while this one is summed and written, and a lane's weights stay in its
+// registers. No barrier; and a row's fixed work (sums over lanes, places, scales) is shared by 32 / L rows.
+// Bound: HBM. Measured against a block and a ring per row, as in k_rows_stream: bf16 131072 x 256 norm 61
+// -> 27 us (134 MB, 0.74 of the copy rate), with residual to 8 bits 78 -> 39 (0.89), quantiser 41 -> 18;
+// 262144 x 64 113 -> 17; 65536 x 784 68 -> 48; fp32 131072 x 256 68 -> 43 (0.92). With 32 lanes to each row
+// 131072 x 256 took 45 us.
 constexpr int SHORT_WARPS = 4;  // of a block
 
 // (bf16 in at most 128 registers, for four blocks per SM: three take 31 us)
@@ -415,9 +415,9 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
 
 // ---- rows that start off the 16-byte grid (odd widths), all of a call's matrices at the same place of a
 // 16-byte unit in each row: threads take the whole units that a row touches, and the first and the last of
-// them in part. Parameters stand in shared memory, one word in E + 1 (in the backward pass one in 33) left out,
-// so that lanes E columns apart meet different banks. (Element by element, 16385 x 4097 with residual to 8 bits took 262 us, and 332
-// backward.)
+// them in part. Parameters stand in shared memory, one word in E + 1 (in the backward pass one in 33) left
+// out, so that lanes E columns apart meet different banks. (Element by element, 16385 x 4097 with residual
+// to 8 bits took 262 us, and 332 backward.)
 __device__ __forceinline__ int padded(int c) { return c + (c >> 5); }
 
 // Element e of unit c is column c E - m + e; `whole`: all of the unit lies in the row.
@@ -788,10 +788,11 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
   if (p.dweight.data) join_cluster(p, g, s_dw, [](int c) { return padded(c); });
 }
 
-// Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of WARPS
-// walks over rows of one group, and its warps' sums for dweight are added in shared memory. (With a ring and a
-// block per row, 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks' own set-up; 10 so.
-// With 32 lanes to every row bf16 131072 x 256 took 54 us instead of 39, 262144 x 64 77 instead of 23.)
+// Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of
+// WARPS walks over rows of one group, and its warps' sums for dweight are added in shared memory. (With a
+// ring and a block per row, 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks'
+// own set-up; 10 so. With 32 lanes to every row bf16 131072 x 256 took 54 us instead of 39, 262144 x 64 77
+// instead of 23.)
 template <int NV>
 constexpr int BACK_WARPS = NV <= 2 ? 16 : 8;  // (registers)
 
@@ -962,7 +963,8 @@ constexpr int SHIFT_MAX_DIM = 16384 - 16;
 // (two parameters and one stage of three fp32 rows in shared memory)
 constexpr int SHIFT_BACK_MAX_DIM = 8192;
 
-// From this many rows per SM on, rows stream through rings; fewer are loaded by the threads that use them.
+// From this many rows per SM on, rows stream through rings or are taken by warps, several to each; fewer are
+// loaded by the threads that use them.
 constexpr int STREAM_ROWS = 4;
 
 template <typename T, int E, int NV, bool QUANT>
@@ -1030,8 +1032,9 @@ cudaError_t launch_rows(RowArgs& p, cudaStream_t st) {
     if (E == 1 && p.dim <= SHIFT_MAX_DIM && same_shift(p.x, p.y, groups, p.rows, U) &&
         same_shift(p.x, p.residual, groups, p.rows, U) && same_shift(p.x, p.sum, groups, p.rows, U))
       return launch_shift<T, QUANT>(p, st);
-    // bf16 rows in 32 elements per thread, since a row's fixed work is each thread's: 16384 x 4096 norm 58 -> 52
-    // us, with residual to 8 bits 77 -> 73, quantiser 39 -> 35; fp32 rows lose (85 -> 135 us: registers).
+    // bf16 rows in 32 elements per thread, since a row's fixed work is each thread's: 16384 x 4096 norm 58
+    // -> 52 us, with residual to 8 bits 77 -> 73, quantiser 39 -> 35; fp32 rows lose (85 -> 135 us:
+    // registers).
     const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 2048, 0, E == 8);
     return s.wide ? launch_stream<T, E, 32 / E, QUANT>(p, s, st)
                   : launch_stream<T, E, 16 / E, QUANT>(p, s, st);
