@@ -79,6 +79,48 @@ __device__ __forceinline__ RowScale row_scale(const RowArgs& p, int64_t g, int64
   return s;
 }
 
+// Element by element: v f, v w, and the sums of squares; in bf16 rows, whose instructions bound them, two at a
+// time (16384 x 4096 quantiser 35 -> 32 us, norm 54 -> 51; fp32 rows lose by the registers that pairs need).
+template <int E>
+__device__ __forceinline__ void scale_by(float* v, float f) {
+#pragma unroll
+  for (int e = 0; e < E; e += E == 8 ? 2 : 1) {
+    if constexpr (E == 8) {
+      const float2 r = unpack2(mul2(pack2(v[e], v[e + 1]), both(f)));
+      v[e] = r.x, v[e + 1] = r.y;
+    } else {
+      v[e] *= f;
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void times(float* v, const float* w) {
+#pragma unroll
+  for (int e = 0; e < E; e += E == 8 ? 2 : 1) {
+    if constexpr (E == 8) {
+      const float2 r = unpack2(mul2(pack2(v[e], v[e + 1]), pack2(w[e], w[e + 1])));
+      v[e] = r.x, v[e + 1] = r.y;
+    } else {
+      v[e] *= w[e];
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void add_squares(const float* v, float2& ss) {
+  if constexpr (E == 8) {
+    uint64_t a = pack2(ss.x, ss.y);
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const uint64_t q = pack2(v[e], v[e + 1]);
+      a = fma2(q, q, a);
+    }
+    ss = unpack2(a);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) ss.x = fmaf(v[e], v[e], ss.x);
+  }
+}
+
 // A row's results from its sums and its elements (times the weights).
 template <typename T, int E, int NV, bool QUANT>
 __device__ __forceinline__ void row_results(const RowArgs& p, int64_t g, int64_t gr, Sums red,
@@ -87,10 +129,13 @@ __device__ __forceinline__ void row_results(const RowArgs& p, int64_t g, int64_t
 #pragma unroll
   for (int i = 0; i < NV; ++i)
     if (t + i * tpr < nvec) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f.f * f.inv;
-      if (QUANT || p.scale.data) store_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
-      else store_vec<T, E>(row_of<T>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
+      if (!QUANT) scale_by<E>(v[i], f.f);
+      if (QUANT || p.scale.data) {
+        scale_by<E>(v[i], f.inv);
+        store_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
+      } else {
+        store_vec<T, E>(row_of<T>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
+      }
     }
 }
 
@@ -117,7 +162,8 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
     }
   }
   const float* weight = QUANT ? nullptr : p.weight.data + g * p.weight.group;
-  Sums red{0.f, 0u};
+  float2 ss = make_float2(0.f, 0.f);
+  float top = 0.f;
   if (!QUANT) {
     if (p.residual.data) {
       const T* res = row_of<const T>(p.residual, g, gr);
@@ -141,18 +187,17 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_rows(const RowArgs
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     if constexpr (!QUANT) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
+      add_squares<E>(v[i], ss);
       if (t + i * p.tpr < nvec) {
         float w[E];
         load_params<E>(weight + (t + i * p.tpr) * E, w);
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] *= w[e];
+        times<E>(v[i], w);
       }
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+    for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
   }
+  Sums red{ss.x + ss.y, __float_as_uint(top)};
   red = warp_reduce<!QUANT, true>(red);
   if (p.tpr > 32) {
     if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = red;
@@ -210,7 +255,8 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 8 ? 4 : 3) k_rows_short
     bring(r + step);
     const bool live = r < p.total;
     const int64_t g = live ? group_of(p, r) : 0, gr = r - g * p.rows;
-    Sums red{0.f, 0u};
+    float2 ss = make_float2(0.f, 0.f);
+    float top = 0.f;
     if constexpr (!QUANT) {
       if (live && p.sum.data)
 #pragma unroll
@@ -224,18 +270,17 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 8 ? 4 : 3) k_rows_short
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (t + i * L < nvec)
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            red.ss = fmaf(v[i][e], v[i][e], red.ss);
-            v[i][e] *= w[i][e];
-          }
+        if (t + i * L < nvec) {
+          add_squares<E>(v[i], ss);
+          times<E>(v[i], w[i]);
+        }
     }
     if (want_top)
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+        for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
+    Sums red{ss.x + ss.y, __float_as_uint(top)};
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) {
       if (!QUANT) red.ss += __shfl_xor_sync(0xffffffffu, red.ss, o);
@@ -361,7 +406,8 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
                            : nullptr;
     ring_wait(q, stage, turn & 1);
     float v[NV][E];
-    Sums red{0.f, 0u};
+    float2 ss = make_float2(0.f, 0.f);
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = t + i * tpr;
@@ -387,19 +433,18 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if constexpr (!QUANT) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
+        add_squares<E>(v[i], ss);
         if (t + i * tpr < nvec) {
           float w[E];
           load_params<E>(weight + (t + i * tpr) * E, w);
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[i][e] *= w[e];
+          times<E>(v[i], w);
         }
       }
       if (want_top)
 #pragma unroll
-        for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+        for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
     }
+    Sums red{ss.x + ss.y, __float_as_uint(top)};
     red = block_reduce<!QUANT, true>(red, s_red[turn >> 1 & 1]);
     // (the row is in registers everywhere: its stage takes the row that comes `stages` later)
     if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
@@ -486,7 +531,7 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
     const uint8_t* x = smem + RING_BARS + stage * q.arrays * slot;
     ring_wait(q, stage, turn & 1);
     float v[NV][E];
-    Sums red{0.f, 0u};
+    float ss = 0.f, top = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = t + i * tpr;
@@ -513,7 +558,7 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
       const Unit<E> u(t + i * tpr, m, dim);
       if constexpr (!QUANT) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) red.ss = fmaf(v[i][e], v[i][e], red.ss);
+        for (int e = 0; e < E; ++e) ss = fmaf(v[i][e], v[i][e], ss);
         if (u.live) {
           const float* w = s_w + (t + i * tpr) * (E + 1) + E - m;
 #pragma unroll
@@ -523,8 +568,9 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
       }
       if (want_top)
 #pragma unroll
-        for (int e = 0; e < E; ++e) red.top = max(red.top, magnitude(v[i][e]));
+        for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
     }
+    Sums red{ss, __float_as_uint(top)};
     red = block_reduce<!QUANT, true>(red, s_red[turn >> 1 & 1]);
     if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
     const RowScale f = row_scale<QUANT>(p, g, gr, red, t == 0);
