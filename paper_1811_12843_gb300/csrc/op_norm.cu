@@ -559,11 +559,13 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
       if constexpr (!QUANT) {
 #pragma unroll
         for (int e = 0; e < E; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-        if (u.live) {
+        if (u.live && one) {
           const float* w = s_w + (t + i * tpr) * (E + 1) + E - m;
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            v[i][e] *= one ? w[e + (e >= m)] : u.in(e, dim) ? __ldg(weight + u.col + e) : 0.f;
+          for (int e = 0; e < E; ++e) v[i][e] *= w[e + (e >= m)];
+        } else if (u.live) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[i][e] *= u.in(e, dim) ? __ldg(weight + u.col + e) : 0.f;
         }
       }
       if (want_top)
@@ -1013,12 +1015,26 @@ constexpr int SHIFT_BACK_MAX_DIM = 8192;
 // loaded by the threads that use them.
 constexpr int STREAM_ROWS = 4;
 
+// A kernel's registers per thread, and the blocks of tpr threads that an SM then holds, at most `most`: a grid
+// of more has its last blocks run alone (k_rows_shift, fp32 8192 x 4097 51 us instead of 63).
+int registers_of(const void* kernel) {
+  cudaFuncAttributes f;
+  if (cudaFuncGetAttributes(&f, kernel) == cudaSuccess) return f.numRegs;
+  cudaGetLastError();
+  return 64;
+}
+int blocks_resident(int registers, int tpr, int most) {
+  const int held = 65536 / (((registers * 32 + 255) / 256 * 256) * (tpr / 32));
+  return held < 1 ? 1 : held < most ? held : most;
+}
+
 template <typename T, int E, int NV, bool QUANT>
 cudaError_t launch_stream(const RowArgs& p, const StreamShape& s, cudaStream_t st) {
   auto kernel = k_rows_stream<T, E, NV, QUANT>;
   const cudaError_t e = allow_smem(kernel, s.smem);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = (int64_t)s.per_sm * sm_count();
+  static const int registers = registers_of((const void*)kernel);
+  const int64_t blocks = (int64_t)blocks_resident(registers, s.tpr, s.per_sm) * sm_count();
   return launch_pdl(kernel, dim3((unsigned)(blocks < p.total ? blocks : p.total)), dim3(s.tpr), s.smem,
                     st, p, s.stages, s.slot, timeout_word());
 }
@@ -1031,18 +1047,25 @@ bool same_shift(const lipz_mat& a, const lipz_mat& b, int64_t groups, int64_t ro
          (groups == 1 || (a.group - b.group) % e == 0);
 }
 
+template <typename T, int E, int NV, bool QUANT>
+cudaError_t launch_shift_of(const RowArgs& p, const StreamShape& s, cudaStream_t st) {
+  const auto kernel = k_rows_shift<T, E, NV, QUANT>;
+  static const int registers = registers_of((const void*)kernel);
+  const cudaError_t e = allow_smem(kernel, s.smem);
+  const int64_t blocks = (int64_t)blocks_resident(registers, s.tpr, s.per_sm) * sm_count();
+  return e != cudaSuccess ? e
+                          : launch_pdl(kernel, dim3((unsigned)(blocks < p.total ? blocks : p.total)),
+                                       dim3(s.tpr), s.smem, st, p, s.stages, s.slot, timeout_word());
+}
+
 template <typename T, bool QUANT>
 cudaError_t launch_shift(const RowArgs& p, cudaStream_t st) {
   constexpr int E = 16 / sizeof(T);
-  const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 1024, 1);
-  auto go = [&](auto kernel) {
-    const cudaError_t e = allow_smem(kernel, s.smem);
-    const int64_t blocks = (int64_t)s.per_sm * sm_count();
-    return e != cudaSuccess ? e
-                            : launch_pdl(kernel, dim3((unsigned)(blocks < p.total ? blocks : p.total)),
-                                         dim3(s.tpr), s.smem, st, p, s.stages, s.slot, timeout_word());
-  };
-  return s.wide ? go(k_rows_shift<T, E, 32 / E, QUANT>) : go(k_rows_shift<T, E, 16 / E, QUANT>);
+  // bf16 rows in 32 elements per thread where two matrices or one of them in 8 bits keep the loads going: 8192 x
+  // 4097 with residual to 8 bits 54 -> 50 us, without (norm) 45 -> 54.
+  const bool wide = E == 8 && p.dim > 512 && (QUANT || p.residual.data);
+  const StreamShape s = stream_shape(p.dim, E, sizeof(T), !QUANT && p.residual.data ? 2 : 1, 2048, 1, wide);
+  return s.wide ? launch_shift_of<T, E, 32 / E, QUANT>(p, s, st) : launch_shift_of<T, E, 16 / E, QUANT>(p, s, st);
 }
 
 // (one wave of blocks: with a wave and a half 131072 x 256 took 33 us instead of 27)
