@@ -460,10 +460,13 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
 
 // ---- rows that start off the 16-byte grid (odd widths), all of a call's matrices at the same place of a
 // 16-byte unit in each row: threads take the whole units that a row touches, and the first and the last of
-// them in part. Parameters stand in shared memory, one word in E + 1 (in the backward pass one in 33) left
-// out, so that lanes E columns apart meet different banks. (Element by element, 16385 x 4097 with residual
+// them in part. Parameters stand in shared memory, one word in E + 1 left out, so that lanes E columns apart meet different banks. (Element by element, 16385 x 4097 with residual
 // to 8 bits took 262 us, and 332 backward.)
-__device__ __forceinline__ int padded(int c) { return c + (c >> 5); }
+// Where a column's parameter stands, E columns of zeros on either side.
+template <int E>
+__device__ __forceinline__ int padded(int c) {
+  return c + E + (c + E) / E;
+}
 
 // Element e of unit c is column c E - m + e; `whole`: all of the unit lies in the row.
 template <int E>
@@ -517,9 +520,8 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
       if (r < p.total) load(r, s);
     }
   if (!QUANT && one) {
-    // (zeros on either side; one word in E + 1 is left out: lanes E columns apart meet different banks)
     for (int c = t - E; c < dim + E; c += tpr)
-      s_w[c + E + (c + E) / E] = c >= 0 && c < dim ? p.weight.data[c] : 0.f;
+      s_w[padded<E>(c)] = c >= 0 && c < dim ? p.weight.data[c] : 0.f;
     __syncthreads();
   }
   int stage = 0;
@@ -756,7 +758,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p, int 
 }
 
 // The same for rows off the 16-byte grid (k_rows_shift's units): a column is another thread's in every row,
-// so the sums for dweight stand in shared memory, beside the weights.
+// so the sums for dweight stand in shared memory, beside the weights. Bound: shared memory and instructions
+// (bf16 32768 x 1001 68 us, 0.43 of the copy rate, fp32 77, 0.76; with a check of each column's place 83, 87).
 template <typename T, int E, int NV>
 __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p, int stages, int slot,
                                                                 int* err) {
@@ -767,7 +770,7 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
   const int64_t g = blockIdx.y;
   const int t = threadIdx.x, tpr = blockDim.x, dim = p.dim, bytes = dim * (int)sizeof(T);
   float* s_w = reinterpret_cast<float*>(smem + RING_BARS + stages * q.arrays * slot);
-  float* s_dw = s_w + padded(dim) + 1;
+  float* s_dw = s_w + padded<E>(dim + E);
   pdl_wait();
   auto load = [&](int64_t r, int stage) {
     const char* src[3] = {(const char*)row_of<const T>(p.dy, g, r), (const char*)row_of<const T>(p.s, g, r),
@@ -780,7 +783,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
       if (r < p.rows) load(r, s);
     }
   const float* weight = p.weight.data + g * p.weight.group;
-  for (int c = t; c < dim; c += tpr) s_w[padded(c)] = weight[c], s_dw[padded(c)] = 0.f;
+  for (int c = t - E; c < dim + E; c += tpr)
+    s_w[padded<E>(c)] = c >= 0 && c < dim ? weight[c] : 0.f, s_dw[padded<E>(c)] = 0.f;
   __syncthreads();
   int stage = 0;
   uint32_t turn = 0;
@@ -791,6 +795,9 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
     ring_wait(q, stage, turn & 1);
     Raw<T, E> dy[NV], s[NV], ds[NV];
     float along = 0.f;
+    // (bf16 rows keep the weights for the results; with them fp32 rows' registers leave room for fewer blocks:
+    // 16384 x 2049 104 us instead of 74)
+    float w[NV][E == 8 ? E : 1];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = t + i * tpr;
@@ -800,14 +807,20 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
       dy[i].load(reinterpret_cast<const T*>(rows) + c * E);
       s[i].load(reinterpret_cast<const T*>(rows + slot) + c * E);
       if (has_dsum) ds[i].load(reinterpret_cast<const T*>(rows + 2 * slot) + c * E);
+      if (!u.whole)  // (what lies beside the row adds nothing, whatever it is)
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (u.in(e, dim)) {
-          const float d = dy[i].get(e) * s[i].get(e);
-          const int at = padded(u.col + e);
-          s_dw[at] = fmaf(d, rstd, s_dw[at]);
-          along = fmaf(d, s_w[at], along);
-        }
+        for (int e = 0; e < E; ++e)
+          if (!u.in(e, dim)) dy[i].clear(e), s[i].clear(e);
+      const int at = c * (E + 1) + E - m;  // padded<E>(c E - m + e) = at + e, and from e = m on one more
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float d = dy[i].get(e) * s[i].get(e);
+        const int here = at + e + (e >= m);
+        const float we = s_w[here];
+        if constexpr (E == 8) w[i][e] = we;
+        s_dw[here] = fmaf(d, rstd, s_dw[here]);
+        along = fmaf(d, we, along);
+      }
     }
     // (the next row's sums for a column follow after this barrier)
     along = block_reduce<true, false>(Sums{along, 0u}, s_red[turn >> 1 & 1]).ss;
@@ -819,10 +832,11 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
       const Unit<E> u(t + i * tpr, m, dim);
       if (!u.live) continue;
       float v[E];
+      const float* ws = s_w + (t + i * tpr) * (E + 1) + E - m;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float w = u.in(e, dim) ? s_w[padded(u.col + e)] : 0.f;
-        v[e] = fmaf(rstd, fmaf(-s[i].get(e), c2, dy[i].get(e) * w), ds[i].get(e));
+        const float we = E == 8 ? w[i][E == 8 ? e : 0] : ws[e + (e >= m)];
+        v[e] = fmaf(rstd, fmaf(-s[i].get(e), c2, dy[i].get(e) * we), ds[i].get(e));
       }
       store_unit<T, E>(dx, u, dim, v);
     }
@@ -833,7 +847,7 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
     }
   }
   ring_done(q, err);
-  if (p.dweight.data) join_cluster(p, g, s_dw, [](int c) { return padded(c); });
+  if (p.dweight.data) join_cluster(p, g, s_dw, [](int c) { return padded<E>(c); });
 }
 
 // Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of
@@ -983,8 +997,7 @@ struct StreamShape {
 StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int params = 0, bool wide = false) {
   StreamShape s;
   const int nvec = params ? (int)ceil_div(dim + 2 * e - 2, e) : dim / e;
-  // (k_rows_shift: columns and E more on either side, one word in E + 1 left out)
-  const int fixed = params == 1 ? ((dim + 2 * e) / e + 1) * (e + 1) * 4 : params * (dim + dim / 32 + 2) * 4;
+  const int fixed = params * ((dim + 2 * e) / e + 1) * (e + 1) * 4;  // (padded)
   s.wide = row_threads(nvec, 16 / e) > 512 || wide;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
   s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;

@@ -46,6 +46,10 @@ struct Raw {
 #pragma unroll
     for (uint32_t& v : w) v = 0;
   }
+  __device__ __forceinline__ void clear(int e) {
+    if constexpr (sizeof(T) == 4) w[e] = 0;
+    else w[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+  }
   __device__ __forceinline__ float get(int e) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
     return e & 1 ? __uint_as_float(w[e >> 1] & 0xFFFF0000u) : __uint_as_float(w[e >> 1] << 16);
