@@ -59,22 +59,40 @@ __device__ __forceinline__ int64_t group_of(const RowArgs& p, int64_t r) {
   return p.total == p.rows ? 0 : (uint32_t)r / (uint32_t)p.rows;
 }
 
-// What a row's elements (times the weights) are multiplied by: f, and for 8 bits then by inv (one after the
-// other: their product may be infinite); else inv is 1. `first`: this thread writes rstd and scale.
+// A row's scale in 8 bits from its largest magnitude: top / 448 or 2^-126. 1/448 is the sum of two floats, and the
+// quotient comes out to nearest (sevenths are never near halfway between two) down to 2^-100, where the second
+// product begins to lose bits.
+__device__ __forceinline__ float scale_of(float top) {
+  return max_nan(fmaf(top, 0x1.249248p-9f, top * 0x1.24924ap-33f), SCALE_MIN);
+}
+// 1 / scale as hi + lo, good to 2^-46 (2^-30 where lo is subnormal), so that v hi + v lo rounds to v / scale: a
+// value halfway between two of e4m3's goes to the even one. (scale >= 2^-126 and, finite, below 2^120: hi is a
+// normal number. Of an infinite scale hi is 0, and so is lo, which the remainder would make NaN.)
+struct Reciprocal {
+  float hi, lo;
+};
+__device__ __forceinline__ Reciprocal reciprocal_of(float scale) {
+  const float hi = rcp_approx(scale);
+  return {hi, hi == 0.f ? 0.f : hi * fmaf(-hi, scale, 1.f)};
+}
+
+// What a row's elements (times the weights) are multiplied by, f, and for 8 bits then by 1 / scale (one after the
+// other: their product may be infinite). `first`: this thread writes rstd and scale.
 struct RowScale {
-  float f, inv;
+  float f;
+  Reciprocal inv;
 };
 template <bool QUANT>
 __device__ __forceinline__ RowScale row_scale(const RowArgs& p, int64_t g, int64_t gr, Sums red, bool first) {
-  RowScale s{1.f, 1.f};
+  RowScale s{1.f, {1.f, 0.f}};
   if (!QUANT) {
     s.f = rsqrtf(fmaf(red.ss, p.inv_dim, p.eps));
     if (first && p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = s.f;
   }
   if (QUANT || p.scale.data) {
-    const float top = __uint_as_float(red.top) * s.f;
-    if (first) p.scale.data[g * p.scale.group + gr] = max_nan(top / E4M3_MAX, SCALE_MIN);
-    s.inv = min_nan(E4M3_MAX * rcp_approx(top), 1.f / SCALE_MIN);
+    const float scale = scale_of(__uint_as_float(red.top) * s.f);
+    if (first) p.scale.data[g * p.scale.group + gr] = scale;
+    s.inv = reciprocal_of(scale);
   }
   return s;
 }
@@ -90,6 +108,19 @@ __device__ __forceinline__ void scale_by(float* v, float f) {
       v[e] = r.x, v[e + 1] = r.y;
     } else {
       v[e] *= f;
+    }
+  }
+}
+template <int E>
+__device__ __forceinline__ void scale_by(float* v, Reciprocal r) {
+#pragma unroll
+  for (int e = 0; e < E; e += E >= 4 ? 2 : 1) {
+    if constexpr (E >= 4) {
+      const uint64_t q = pack2(v[e], v[e + 1]);
+      const float2 u = unpack2(fma2(q, both(r.hi), mul2(q, both(r.lo))));
+      v[e] = u.x, v[e + 1] = u.y;
+    } else {
+      v[e] = fmaf(v[e], r.hi, v[e] * r.lo);
     }
   }
 }
@@ -126,17 +157,22 @@ template <typename T, int E, int NV, bool QUANT>
 __device__ __forceinline__ void row_results(const RowArgs& p, int64_t g, int64_t gr, Sums red,
                                             float (&v)[NV][E], int t, int tpr, int nvec) {
   const RowScale f = row_scale<QUANT>(p, g, gr, red, t == 0);
+  if (QUANT || p.scale.data) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (t + i * tpr < nvec) {
-      if (!QUANT) scale_by<E>(v[i], f.f);
-      if (QUANT || p.scale.data) {
+    for (int i = 0; i < NV; ++i)
+      if (t + i * tpr < nvec) {
+        if (!QUANT) scale_by<E>(v[i], f.f);
         scale_by<E>(v[i], f.inv);
         store_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
-      } else {
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (t + i * tpr < nvec) {
+        scale_by<E>(v[i], f.f);
         store_vec<T, E>(row_of<T>(p.y, g, gr) + (t + i * tpr) * E, v[i]);
       }
-    }
+  }
 }
 
 // The norm, or with QUANT only the rows' values to 8 bits.
@@ -424,6 +460,10 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
         for (int e = 0; e < E; ++e) v[i][e] = 0.f;
       }
     }
+    // (fp32 rows' squares here leave their weights' loads together: 16384 x 8192 to 8 bits 144 us below, 131 so)
+    if constexpr (!QUANT && E == 4 && NV == 4)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) add_squares<E>(v[i], ss);
     if (!QUANT && p.sum.data) {
       T* s = row_of<T>(p.sum, g, gr);
 #pragma unroll
@@ -433,7 +473,7 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if constexpr (!QUANT) {
-        add_squares<E>(v[i], ss);
+        if constexpr (E != 4 || NV != 4) add_squares<E>(v[i], ss);
         if (t + i * tpr < nvec) {
           float w[E];
           load_params<E>(weight + (t + i * tpr) * E, w);
@@ -582,10 +622,15 @@ __global__ void __launch_bounds__(512) k_rows_shift(const RowArgs p, int stages,
     for (int i = 0; i < NV; ++i) {
       const Unit<E> u(t + i * tpr, m, dim);
       if (!u.live) continue;
+      if (!QUANT)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[i][e] = v[i][e] * f.f * f.inv;
-      if (QUANT || p.scale.data) store_unit_e4m3<E>(row_of<e4m3>(p.y, g, gr), u, dim, v[i]);
-      else store_unit<T, E>(row_of<T>(p.y, g, gr), u, dim, v[i]);
+        for (int e = 0; e < E; ++e) v[i][e] *= f.f;
+      if (QUANT || p.scale.data) {
+        scale_by<E>(v[i], f.inv);
+        store_unit_e4m3<E>(row_of<e4m3>(p.y, g, gr), u, dim, v[i]);
+      } else {
+        store_unit<T, E>(row_of<T>(p.y, g, gr), u, dim, v[i]);
+      }
     }
     turn ^= 2;
     if (++stage == stages) {
@@ -616,14 +661,13 @@ __global__ void __launch_bounds__(1024) k_quantize_long(const RowArgs p, int64_t
   if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = red;
   __syncthreads();
   red = join<false, true>(s_red, 0, 32);
-  const float scale = max_nan(__uint_as_float(red.top) / E4M3_MAX, SCALE_MIN);
+  const float scale = scale_of(__uint_as_float(red.top));
   if (threadIdx.x == 0) p.scale.data[g * p.scale.group + gr] = scale;
-  const float f = 1.f / scale;
+  const Reciprocal inv = reciprocal_of(scale);
 #pragma unroll 4
   for (int64_t c = threadIdx.x; c < dim / E; c += 1024) {
     load_vec<T, E>(x + c * E, v);
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] *= f;
+    scale_by<E>(v, inv);
     store_e4m3<E>(y + c * E, v);
   }
 }

@@ -13,17 +13,12 @@ namespace ops {
 
 typedef unsigned char e4m3;
 
-constexpr float E4M3_MAX = 448.f, SCALE_MIN = 1.17549435082228751e-38f;  // 2^-126
+constexpr float SCALE_MIN = 1.17549435082228751e-38f;  // 2^-126
 
-// The larger and the smaller of two values, NaN if either is.
+// The larger of two values, NaN if either is.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float min_nan(float a, float b) {
-  float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
 
