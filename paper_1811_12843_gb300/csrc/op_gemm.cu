@@ -18,7 +18,6 @@
 
 #include <string.h>
 
-#include <atomic>
 #include <type_traits>
 
 #include "op_gemm.h"
@@ -977,18 +976,6 @@ bool encode(CUtensorMap* map, const Operand& o, const Extent& x, int64_t groups,
 
 uint64_t round256(int64_t v) { return (uint64_t)ceil_div(v, 256) * 256; }
 
-// Sets the kernel's shared memory once per device.
-template <typename K>
-cudaError_t prepare_kernel(K kernel, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 64 && done.load() >> dev & 1) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
-  if (e == cudaSuccess && dev < 64) done.fetch_or((uint64_t)1 << dev);
-  return e;
-}
-
 template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false,
           bool DIRECT = false>
 cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
@@ -1053,7 +1040,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   k.stages = S::stages(k.a_rows, turn);
   static std::atomic<uint64_t> done{0};
   auto kernel = k_gemm_op<TYPE, CG, BN, FORWARD, T, VIA, SPLIT, DIRECT>;
-  cudaError_t e = prepare_kernel(kernel, done);
+  cudaError_t e = allow_dynamic_smem(kernel, SMEM_MAX, done);
   if (e != cudaSuccess) return e;
   const int cluster = SPLIT ? k.p[0].parts : CG, slots = SPLIT ? k.units : sm_count() / CG;
   const int ctas = (k.units < slots ? k.units : slots) * cluster;

@@ -1024,6 +1024,8 @@ __global__ void __launch_bounds__(1024)
   out.data[g * out.group + c] = v;
 }
 
+constexpr int RING_SMEM = 216 * 1024;  // of an SM, for rings and parameters
+
 int row_threads(int nvec, int nv) { return (int)(ceil_div(ceil_div(nvec, nv), 32) * 32); }
 
 // A streaming kernel's block: 16 elements per thread, 32 where 512 threads of 16 do not reach the row's
@@ -1045,22 +1047,23 @@ StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int pa
   s.wide = row_threads(nvec, 16 / e) > 512 || wide;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
   s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;
-  const int budget = 216 * 1024, row = s.slot * arrays;
+  const int row = s.slot * arrays;
   if (s.wide) threads /= 2;
   s.per_sm = threads / s.tpr < 24 ? threads / s.tpr : 24;
   if (s.per_sm < 1) s.per_sm = 1;
-  auto stages = [&] { return (budget / s.per_sm - 1024 - RING_BARS - fixed) / row; };
+  auto stages = [&] { return (RING_SMEM / s.per_sm - 1024 - RING_BARS - fixed) / row; };
   while (s.per_sm > 1 && stages() < 2) --s.per_sm;
   s.stages = stages() > RING_MAX ? RING_MAX : stages();
   s.smem = RING_BARS + s.stages * row + fixed;
   return s;
 }
 
-template <typename K>
-cudaError_t allow_smem(K kernel, int smem) {
-  return smem <= 48 * 1024
-             ? cudaSuccess
-             : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+// Allows a kernel that much shared memory, once per device and whatever the call needs: the default limit counts a
+// kernel's own arrays too, and a limit that follows the calls would be lowered under another thread's launch.
+template <auto KERNEL>
+cudaError_t allow_smem() {
+  static std::atomic<uint64_t> done{0};
+  return allow_dynamic_smem(KERNEL, RING_SMEM, done);
 }
 
 // (512 threads of 32 elements, less the two units more)
@@ -1087,8 +1090,8 @@ int blocks_resident(int registers, int tpr, int most) {
 
 template <typename T, int E, int NV, bool QUANT>
 cudaError_t launch_stream(const RowArgs& p, const StreamShape& s, cudaStream_t st) {
-  auto kernel = k_rows_stream<T, E, NV, QUANT>;
-  const cudaError_t e = allow_smem(kernel, s.smem);
+  constexpr auto kernel = k_rows_stream<T, E, NV, QUANT>;
+  const cudaError_t e = allow_smem<kernel>();
   if (e != cudaSuccess) return e;
   static const int registers = registers_of((const void*)kernel);
   const int64_t blocks = (int64_t)blocks_resident(registers, s.tpr, s.per_sm) * sm_count();
@@ -1106,9 +1109,9 @@ bool same_shift(const lipz_mat& a, const lipz_mat& b, int64_t groups, int64_t ro
 
 template <typename T, int E, int NV, bool QUANT>
 cudaError_t launch_shift_of(const RowArgs& p, const StreamShape& s, cudaStream_t st) {
-  const auto kernel = k_rows_shift<T, E, NV, QUANT>;
+  constexpr auto kernel = k_rows_shift<T, E, NV, QUANT>;
   static const int registers = registers_of((const void*)kernel);
-  const cudaError_t e = allow_smem(kernel, s.smem);
+  const cudaError_t e = allow_smem<kernel>();
   const int64_t blocks = (int64_t)blocks_resident(registers, s.tpr, s.per_sm) * sm_count();
   return e != cudaSuccess ? e
                           : launch_pdl(kernel, dim3((unsigned)(blocks < p.total ? blocks : p.total)),
@@ -1216,10 +1219,10 @@ int back_cluster(const lipz_rmsnorm_backward_args& a, const StreamShape& s) {
 }
 
 // Launch in clusters of `cluster` blocks.
-template <typename K>
-cudaError_t launch_clusters(K kernel, const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
-                            int cluster, cudaStream_t st) {
-  const cudaError_t e = allow_smem(kernel, s.smem);
+template <auto KERNEL>
+cudaError_t launch_clusters(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks, int cluster,
+                            cudaStream_t st) {
+  const cudaError_t e = allow_smem<KERNEL>();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks, (unsigned)groups);
@@ -1239,15 +1242,15 @@ cudaError_t launch_clusters(K kernel, const BackArgs& p, const StreamShape& s, i
     c.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     c.val.programmaticStreamSerializationAllowed = 1;
   }
-  return cudaLaunchKernelEx(&cfg, kernel, p, s.stages, s.slot, timeout_word());
+  return cudaLaunchKernelEx(&cfg, KERNEL, p, s.stages, s.slot, timeout_word());
 }
 
 template <typename T>
 cudaError_t launch_back_shift(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks,
                               cudaStream_t st) {
   constexpr int E = 16 / sizeof(T);
-  auto go = [&](auto kernel) { return launch_clusters(kernel, p, s, groups, blocks, 1, st); };
-  return s.wide ? go(k_rmsnorm_backward_shift<T, E, 32 / E>) : go(k_rmsnorm_backward_shift<T, E, 16 / E>);
+  return s.wide ? launch_clusters<k_rmsnorm_backward_shift<T, E, 32 / E>>(p, s, groups, blocks, 1, st)
+                : launch_clusters<k_rmsnorm_backward_shift<T, E, 16 / E>>(p, s, groups, blocks, 1, st);
 }
 
 template <typename T>
@@ -1268,8 +1271,9 @@ cudaError_t launch_back_rows(const BackArgs& p, int64_t groups, int blocks, cuda
 template <typename T, int E>
 cudaError_t launch_back(const BackArgs& p, const StreamShape& s, int64_t groups, int blocks, int parts,
                         cudaStream_t st) {
-  auto go = [&](auto kernel) { return launch_clusters(kernel, p, s, groups, blocks, blocks / parts, st); };
-  return s.wide ? go(k_rmsnorm_backward<T, E, 32 / E>) : go(k_rmsnorm_backward<T, E, 16 / E>);
+  const int cluster = blocks / parts;
+  return s.wide ? launch_clusters<k_rmsnorm_backward<T, E, 32 / E>>(p, s, groups, blocks, cluster, st)
+                : launch_clusters<k_rmsnorm_backward<T, E, 16 / E>>(p, s, groups, blocks, cluster, st);
 }
 
 }  // namespace

@@ -3,6 +3,7 @@
 
 #include <cuda_fp8.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "common.cuh"
@@ -88,6 +89,19 @@ __device__ __forceinline__ void load_params(const float* p, float* v) {
       v[i] = r.x, v[i + 1] = r.y, v[i + 2] = r.z, v[i + 3] = r.w;
     }
   }
+}
+
+// Host: lets a kernel's launches ask for up to `bytes` of dynamic shared memory, once per device (`done`: the
+// devices where that is so).
+template <typename K>
+cudaError_t allow_dynamic_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && done.load() >> dev & 1) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or((uint64_t)1 << dev);
+  return e;
 }
 
 // Two values to e4m3, to nearest even; past 448 they saturate, NaN stays NaN.
