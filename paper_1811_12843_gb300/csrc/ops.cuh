@@ -168,7 +168,8 @@ __device__ __forceinline__ float act_slope(float u, float slope) {
     return 4.f * e * r * r;
   }
   if constexpr (ACT == LIPZ_ACT_GELU) {
-    const float u2 = u * u, g = logistic(u * fmaf(GELU_3, u2, GELU_1));
+    // (u^2 stays finite: beside 1 - g = 0 an infinite one would make the slope of a large finite u NaN)
+    const float u2 = fminf(u * u, 1e30f), g = logistic(u * fmaf(GELU_3, u2, GELU_1));
     return g + u * g * (1.f - g) * fmaf(3.f * GELU_3, u2, GELU_1);
   }
   if constexpr (ACT == LIPZ_ACT_SILU) {
