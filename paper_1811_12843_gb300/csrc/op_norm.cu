@@ -770,7 +770,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward(const BackArgs p, int 
     }
     along = block_reduce<true, false>(Sums{along, 0u}, s_red[turn >> 1 & 1]).ss;
     if (t == 0 && r + (int64_t)stages * gridDim.x < p.rows) load(r + (int64_t)stages * gridDim.x, stage);
-    const float c2 = rstd * rstd * (along * p.inv_dim);
+    // (rstd^2 by itself may be infinite where the gradient is not)
+    const float c2 = rstd * (rstd * (along * p.inv_dim));
     T* dx = row_of<T>(p.dx, g, r);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -869,7 +870,7 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
     // (the next row's sums for a column follow after this barrier)
     along = block_reduce<true, false>(Sums{along, 0u}, s_red[turn >> 1 & 1]).ss;
     if (t == 0 && r + (int64_t)stages * gridDim.x < p.rows) load(r + (int64_t)stages * gridDim.x, stage);
-    const float c2 = rstd * rstd * (along * p.inv_dim);
+    const float c2 = rstd * (rstd * (along * p.inv_dim));
     T* dx = row_of<T>(p.dx, g, r);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -961,7 +962,7 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_rmsnorm_backward_rows(c
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) along += __shfl_xor_sync(0xffffffffu, along, o);
     if (r >= p.rows) continue;
-    const float c2 = f * f * (along * p.inv_dim);
+    const float c2 = f * (f * (along * p.inv_dim));
     T* dx = row_of<T>(p.dx, g, r);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

@@ -8,6 +8,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     from paper_1811_12843_gb300 import operators as ops
+    from test_gpu_operators import within
 
 BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
 
@@ -32,3 +33,22 @@ def test_slopes_at_huge_pre_activations(act, n):
     slope = torch.zeros_like(pre) if act == "tanh" else (pre > 0).to(BF16)
     assert torch.equal(dx, slope)
     assert torch.equal(db, slope.float().sum(dim=0))
+
+
+@pytest.mark.parametrize("rows,dim", [(5, 64), (700, 256), (700, 2056), (700, 1001), (4, 16383)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_backward_of_tiny_rows(rows, dim, dtype):
+    """rstd of 1e22: its square is infinite, the gradient is not."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    s = (torch.randn((rows, dim), generator=gen, device="cuda") * 1e-22).to(dtype)
+    dy = (torch.randn((rows, dim), generator=gen, device="cuda") * 1e-3).to(dtype)
+    w = 1 + 0.1 * torch.randn(dim, generator=gen, device="cuda")
+    rstd = s.to(F64).square().mean(dim=1).rsqrt().float()
+    dx, dw = ops.rmsnorm_backward(dy, s, rstd, w)
+    g, r, s64 = dy.to(F64) * w.to(F64), rstd.to(F64)[:, None], s.to(F64)
+    ref = r * (g - (s64 * r) * (r * (g * s64).mean(dim=1, keepdim=True)))
+    size = r * (g.abs() + (s64 * r).abs() * (r * (g * s64).abs().mean(dim=1, keepdim=True)))
+    rounding = 2.0 ** -8 if dtype == BF16 else 2.0 ** -23
+    within(dx, ref, rounding * ref.abs() + ((dim + 16) * 2.0 ** -24 + 2.0 ** -20) * size, "dx")
+    within(dw, (dy.to(F64) * s64 * r).sum(dim=0),
+           (rows + 16) * 2.0 ** -23 * (dy.to(F64) * s64 * r).abs().sum(dim=0), "dweight")
