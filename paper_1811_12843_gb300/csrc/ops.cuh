@@ -295,9 +295,12 @@ __device__ __forceinline__ void copy_rows(const CopyJobs& jobs, int64_t b) {
 }
 // The epilogue of element (m, n) of group g, from its sum u.
 __device__ __forceinline__ void finish(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
+  const float b = e.bias.data ? e.bias.data[g * e.bias.group + n] : 0.f;
+  // (one scale after the other, as for many rows: their product may leave fp32's range where the result does not)
   if (e.w_scale.data)
-    u *= e.x_scale.data[g * e.x_scale.group + m] * e.w_scale.data[g * e.w_scale.group + n];
-  if (e.bias.data) u += e.bias.data[g * e.bias.group + n];
+    u = fmaf(u * e.x_scale.data[g * e.x_scale.group + m], e.w_scale.data[g * e.w_scale.group + n], b);
+  else
+    u += b;
   if (e.pre.data)
     ((bf16*)e.pre.data)[g * e.pre.group + m * e.pre.row + n] = __float2bfloat16_rn(u);
   with_act(e.act, [&](auto act) { u = act_value<decltype(act)::value>(u, e.slope); });

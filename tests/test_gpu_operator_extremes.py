@@ -35,6 +35,24 @@ def test_slopes_at_huge_pre_activations(act, n):
     assert torch.equal(db, slope.float().sum(dim=0))
 
 
+@pytest.mark.parametrize("rows", [1, 3, 20, 300])
+@pytest.mark.parametrize("scale", [2e19, 1e-22])
+def test_scales_multiply_one_after_the_other(rows, scale):
+    """Scales whose product leaves fp32's normal range, beside sums that bring the result back into it or are
+    zero: the same in the kernels for few, some and many rows."""
+    k, n = 256, 96
+    x, w = torch.ones(rows, k, device="cuda"), torch.zeros(n, k, device="cuda")
+    if scale > 1:
+        w[::2, 7] = 0.25
+    else:
+        w[::2] = torch.arange(k, device="cuda").remainder(15) + 1.0
+    xs, ws = torch.full((rows,), scale, device="cuda"), torch.full((n,), scale, device="cuda")
+    y, _ = ops.linear(x.to(torch.float8_e4m3fn), w.to(torch.float8_e4m3fn), x_scale=xs, w_scale=ws, out_dtype=F32)
+    ref = (x.to(F64) @ w.to(F64).T) * xs.to(F64)[:, None] * ws.to(F64)
+    assert ref.abs().max() < 3e38 and (ref[:, ::2] > 0).all()
+    within(y, ref, 2.0 ** -20 * ref.abs() + 2.0 ** -148)
+
+
 @pytest.mark.parametrize("rows,dim", [(5, 64), (700, 256), (700, 2056), (700, 1001), (4, 16383)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_norm_backward_of_tiny_rows(rows, dim, dtype):
