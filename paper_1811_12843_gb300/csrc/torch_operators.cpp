@@ -7,6 +7,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -74,13 +75,14 @@ struct Call {
   static bool adjacent(const Tensor& t) {
     return t.stride(-1) == 1 || t.size(-1) <= 1 || t.numel() == 0;
   }
-  lipz_mat view(const Tensor& t, const char* what, int types) const {
+  lipz_mat view(const Tensor& t, const char* what, int types, bool out = false) const {
     const int type = type_of(t.scalar_type());
     if (type < 0 || !(types >> type & 1))
       refuse(std::string(what) + " has dtype " + at::toString(t.scalar_type()) + ", which is not taken");
     if (!adjacent(t)) refuse(std::string(what) + ": columns must be adjacent");
     const auto st = t.strides();
-    return {const_cast<void*>(t.const_data_ptr()), st.size() == 3 ? st[0] : 0, st[st.size() - 2], type, 0};
+    void* const data = out ? t.mutable_data_ptr() : const_cast<void*>(t.const_data_ptr());
+    return {data, st.size() == 3 ? st[0] : 0, st[st.size() - 2], type, 0};
   }
   // The tensor that gives the call its device, groups, rows and columns.
   lipz_mat first(PyObject* o, const char* what, int types) {
@@ -105,6 +107,19 @@ struct Call {
   }
   Shape matrix(int64_t r, int64_t c) const { return grouped ? Shape(groups, r, c) : Shape(r, c); }
   Shape vector(int64_t n) const { return grouped ? Shape(groups, n) : Shape(n); }
+  // A tensor of the caller's that the call writes to; wrote() follows the call. (A copy-on-write clone gets memory
+  // of its own here, so an input that may be the same tensor is taken after it.)
+  lipz_mat target(PyObject* o, const char* what, int64_t r, int64_t c, int types) const {
+    const Tensor& t = like(o, what, matrix(r, c));
+    if (t.is_inference() && !c10::InferenceMode::is_enabled())
+      refuse(std::string(what) + " is an inference tensor, which is written in inference mode alone");
+    return view(t, what, types, true);
+  }
+  // What autograd has saved of the tensor is no longer what it holds.
+  static void wrote(PyObject* o) {
+    const Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
   // (None: null)
   lipz_mat mat(PyObject* o, const char* what, int64_t r, int64_t c, int types) const {
     if (o == Py_None) return {};
@@ -219,13 +234,19 @@ PyObject* rmsnorm(PyObject* const* o) {
   if (o[2] == Py_None) {
     if (own_sum) c.refuse("sum_out needs a residual");
   } else {
+    if (own_sum) {
+      a.sum = c.target(o[6], "sum_out", c.rows, c.cols, bit(a.x.type));
+      a.x = c.view(c.tensor(o[0], "x"), "x", WIDE);  // (x may be sum_out)
+    } else {
+      a.sum = c.fresh(sum, c.rows, c.cols, type);
+    }
     a.residual = c.mat(o[2], "residual", c.rows, c.cols, bit(a.x.type));
-    a.sum = own_sum ? c.mat(o[6], "sum_out", c.rows, c.cols, bit(a.x.type)) : c.fresh(sum, c.rows, c.cols, type);
   }
   a.y = c.fresh(y, c.rows, c.cols, e4m3 ? E4M3 : type);
   if (e4m3) a.scale = c.fresh(scale, c.rows);
   if (keep) a.rstd = c.fresh(rstd, c.rows);
   run(c, lipz_rmsnorm, a);
+  if (own_sum) c.wrote(o[6]);
   return results(give(y), sum.defined() ? give(sum) : given(own_sum ? o[6] : o[0]), give(scale), give(rstd));
 }
 
@@ -277,6 +298,8 @@ PyObject* linear(PyObject* const* o) {
   a.act = (int)PyLong_AsLong(o[3]);
   a.slope = number(o[4]);
   const ScalarType type = c.result_type(o[8], "out_dtype");
+  const bool own = o[10] != Py_None;
+  if (own) a.y = c.target(o[10], "out", c.rows, n, bit(type_of(type)));
   a.residual = c.mat(o[5], "residual", c.rows, n, bit(type_of(type)));
   const bool bytes = a.x.type == LIPZ_E4M3;
   if ((o[6] != Py_None) != bytes || (o[7] != Py_None) != bytes)
@@ -284,10 +307,11 @@ PyObject* linear(PyObject* const* o) {
   a.x_scale = c.vec(o[6], "x_scale", c.rows);
   a.w_scale = c.vec(o[7], "w_scale", n);
   Tensor y, pre;
-  a.y = o[10] != Py_None ? c.mat(o[10], "out", c.rows, n, bit(type_of(type))) : c.fresh(y, c.rows, n, type);
+  if (!own) a.y = c.fresh(y, c.rows, n, type);
   if (truth(o[9])) a.pre = c.fresh(pre, c.rows, n, BF16);
   run(c, lipz_linear_workspace, lipz_linear, a);
-  return results(y.defined() ? give(y) : given(o[10]), give(pre));
+  if (own) c.wrote(o[10]);
+  return results(own ? given(o[10]) : give(y), give(pre));
 }
 
 // dy, x, w, act's code, slope, pre, want_dx, want_dw, want_db, dx_dtype, dw_dtype -> dx, dw, db
