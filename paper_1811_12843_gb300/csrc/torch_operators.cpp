@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -70,6 +71,9 @@ struct Call {
     if (!THPVariable_Check(o)) refuse(std::string(what) + " must be a CUDA tensor");
     const Tensor& t = THPVariable_Unpack(o);
     if (!t.is_cuda() || t.layout() != at::kStrided) refuse(std::string(what) + " must be a CUDA tensor");
+    // (no call records a graph: its results would have no gradient, without a word)
+    if (t.requires_grad() && at::GradMode::is_enabled())
+      refuse(std::string(what) + " requires a gradient, and this call records none: use torch.no_grad() or detach()");
     return t;
   }
   static bool adjacent(const Tensor& t) {

@@ -9,7 +9,8 @@ input between the groups. An output may not overlap an input unless its call say
 runs the library's CUDA kernels on the current stream of the tensors' device, allocates its outputs
 as torch does, waits for nothing, and may be captured in a CUDA graph. What the library does not
 take raises ``LipzError`` with nothing launched. Nothing here records an autograd graph: the
-backward passes are calls of their own.
+backward passes are calls of their own, and a tensor that requires a gradient is taken under
+``torch.no_grad()`` or detached (else refused, since its gradient would be lost).
 """
 
 import importlib.util

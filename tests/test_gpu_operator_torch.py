@@ -73,3 +73,27 @@ def test_inference_tensors_are_written_in_inference_mode_alone():
         with pytest.raises(L.LipzError, match="inference"):
             call()
     assert torch.equal(t, before)
+
+
+def test_a_gradient_is_refused_where_it_would_be_lost():
+    x, w, g = randn(24, 64), randn(32, 64), torch.ones(64, device="cuda")
+    bias, rstd, q = torch.zeros(32, device="cuda"), torch.ones(24, device="cuda"), ops.quantize_rows
+
+    def grad(t):
+        return t.detach().clone().requires_grad_(True)
+
+    calls = [lambda f: ops.rmsnorm(f(x), g), lambda f: ops.rmsnorm(x, f(g)),
+             lambda f: ops.rmsnorm(x, g, residual=f(x)), lambda f: q(f(x)), lambda f: ops.linear(f(x), w),
+             lambda f: ops.linear(x, f(w)), lambda f: ops.linear(x, w, f(bias)),
+             lambda f: ops.linear(x, w, residual=f(randn(24, 32))),
+             lambda f: ops.rmsnorm_backward(f(x), x, rstd, g), lambda f: ops.linear_backward(randn(24, 32), x, f(w))]
+    for call in calls:
+        call(lambda t: t)
+        with pytest.raises(L.LipzError, match="gradient") as e:
+            call(grad)
+        assert e.value.code == L.LIPZ_ERR_INVALID
+        with torch.no_grad():
+            call(grad)
+        with torch.inference_mode():
+            call(grad)
+        call(lambda t: grad(t).detach())
