@@ -351,7 +351,9 @@ LIPZ_API int lipz_fitness_from_logits_noalloc(const float* logits, int32_t cells
  *     that needs scratch memory says how much (its _workspace form, 0 for many sizes); the workspace
  *     is 256-byte aligned, and free again when the call's work on the stream is done.
  *   - Bad arguments give LIPZ_ERR_INVALID with nothing launched; the message is
- *     lipz_operator_error(). The library cannot check device buffers.
+ *     lipz_operator_error(). That includes an output that overlaps another argument, where one of the
+ *     two has no gaps between its rows or both have the same strides (of others the library compares
+ *     the starts alone). It cannot check what lies at an address.
  *   - A bounded device-side wait that expires (the output is then not valid) is reported once, as
  *     LIPZ_ERR_TIMEOUT, by the next operator call or by lipz_operator_status().
  */

@@ -1,8 +1,10 @@
 // C ABI of the residual-block operators: every argument that the host can check is checked here, then
 // the kernels of op_norm.cu, op_linear.cu and op_gemm.cu are launched.
+#include <algorithm>
 #include <atomic>
 #include <cstdarg>
 #include <cstdio>
+#include <utility>
 
 #include "op_gemm.h"
 
@@ -237,12 +239,169 @@ int check(const lipz_linear_backward_args* a) {
   return c.rc;
 }
 
+// ---- outputs that share memory with other arguments: a kernel would read what it has already overwritten
+
+// `groups` times `rows` rows of `width` bytes, `group` and `row` bytes apart.
+struct Region {
+  uintptr_t at;
+  int64_t width, rows, row, groups, group;
+
+  // (strides of 0 repeat one row or group)
+  static Region of(const void* data, int64_t width, int64_t rows, int64_t row, int64_t groups, int64_t group) {
+    if (!data || rows <= 0 || groups <= 0) return {0, 0, 0, 0, 0, 0};
+    const bool many = rows > 1 && row, grouped = groups > 1 && group;
+    return {(uintptr_t)data, width, many ? rows : 1, many ? row : 0, grouped ? groups : 1, grouped ? group : 0};
+  }
+  bool same_place(const Region& o) const {
+    return at == o.at && width == o.width && rows == o.rows && row == o.row && groups == o.groups && group == o.group;
+  }
+  int64_t span() const { return (rows - 1) * row + (groups - 1) * group + width; }
+  // Rows or groups without gaps between them as one row.
+  Region joined() const {
+    Region r = *this;
+    for (int i = 0; i < 2; ++i) {
+      if (r.rows > 1 && r.row == r.width) r.width *= r.rows, r.rows = 1, r.row = 0;
+      if (r.groups > 1 && r.group == r.width) r.width *= r.groups, r.groups = 1, r.group = 0;
+    }
+    return r;
+  }
+};
+
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
+
+// Whether some byte certainly lies in both. Exact where the two have one row stride and one group stride (rows or
+// groups that lie without gaps count as one row, which goes with any stride); of others only their starts are
+// compared.
+bool meet(const Region& p, const Region& q) {
+  if (!p.width || !q.width) return false;
+  if (q.at >= p.at + p.span() || p.at >= q.at + q.span()) return false;
+  const Region a = p.joined(), b = q.joined();
+  if ((a.rows > 1 && b.rows > 1 && a.row != b.row) || (a.groups > 1 && b.groups > 1 && a.group != b.group))
+    return a.at == b.at;
+  // rows i apart and groups j apart meet if -b.width < d - i row - j group < a.width
+  struct Steps {
+    int64_t by, lo, hi;
+  } outer{a.groups > 1 ? a.group : b.group, 1 - b.groups, a.groups - 1},
+      inner{a.rows > 1 ? a.row : b.row, 1 - b.rows, a.rows - 1};
+  if (outer.by < inner.by) std::swap(outer, inner);
+  const int64_t d = (int64_t)(b.at - a.at);
+  // the steps (from lo to hi) whose multiple lies in [x0, x1]
+  auto within = [](Steps s, int64_t x0, int64_t x1) {
+    if (s.lo == s.hi) return x0 <= 0 && 0 <= x1 ? s : Steps{0, 1, 0};
+    return Steps{s.by, std::max(s.lo, -floor_div(-x0, s.by)), std::min(s.hi, floor_div(x1, s.by))};
+  };
+  const Steps o = within(outer, d - inner.hi * inner.by - a.width + 1, d - inner.lo * inner.by + b.width - 1);
+  // (a few, unless rows lie across one another as only an input's may)
+  for (int64_t j = o.lo; j <= o.hi && j - o.lo < 64; ++j) {
+    const int64_t rest = d - j * outer.by;
+    const Steps i = within(inner, rest - a.width + 1, rest + b.width - 1);
+    if (i.lo <= i.hi) return true;
+  }
+  return false;
+}
+
+// One call's outputs against its inputs and one another.
+struct Overlap {
+  const char* call;
+  int64_t groups;
+  struct Part {
+    const char* name;
+    Region r;
+    unsigned places;  // of an output: the inputs whose own place it may have
+  };
+  Part in[6], out[4];
+  int ins = 0, outs = 0;
+
+  Overlap(const char* call_, int64_t groups_) : call(call_), groups(groups_) {}
+  Region region(const lipz_mat& m, int64_t rows, int64_t cols) const {
+    const int64_t b = ops::type_bytes(m.type);
+    return Region::of(m.data, cols * b, rows, m.row * b, groups, m.group * b);
+  }
+  Region region(const lipz_vec& v, int64_t n) const { return Region::of(v.data, n * 4, 1, 0, groups, v.group * 4); }
+  unsigned input(const char* name, const lipz_mat& m, int64_t rows, int64_t cols) {
+    in[ins] = {name, region(m, rows, cols), 0u};
+    return 1u << ins++;
+  }
+  void input(const char* name, const lipz_vec& v, int64_t n) { in[ins++] = {name, region(v, n), 0u}; }
+  void output(const char* name, const lipz_mat& m, int64_t rows, int64_t cols, unsigned places = 0) {
+    out[outs++] = {name, region(m, rows, cols), places};
+  }
+  void output(const char* name, const lipz_vec& v, int64_t n) { out[outs++] = {name, region(v, n), 0u}; }
+
+  int result() const {
+    for (int i = 0; i < outs; ++i) {
+      for (int j = 0; j < ins; ++j)
+        if (meet(out[i].r, in[j].r) && !(out[i].places >> j & 1 && out[i].r.same_place(in[j].r)))
+          return fail(LIPZ_ERR_INVALID, "%s: %s overlaps %s", call, out[i].name, in[j].name);
+      for (int j = 0; j < i; ++j)
+        if (meet(out[i].r, out[j].r))
+          return fail(LIPZ_ERR_INVALID, "%s: %s overlaps %s", call, out[i].name, out[j].name);
+    }
+    return LIPZ_OK;
+  }
+};
+
+// (The row operators' threads have an element of every input in registers before they write one there.)
+int overlap(const lipz_rmsnorm_args& a) {
+  Overlap o{"lipz_rmsnorm", a.groups};
+  const unsigned own = o.input("x", a.x, a.rows, a.dim) | o.input("residual", a.residual, a.rows, a.dim);
+  o.input("weight", a.weight, a.dim);
+  o.output("sum", a.sum, a.rows, a.dim, own);
+  o.output("y", a.y, a.rows, a.dim, own);
+  if (a.y.type == LIPZ_E4M3) o.output("scale", a.scale, a.rows);
+  o.output("rstd", a.rstd, a.rows);
+  return o.result();
+}
+int overlap(const lipz_rmsnorm_backward_args& a) {
+  Overlap o{"lipz_rmsnorm_backward", a.groups};
+  const unsigned own = o.input("dy", a.dy, a.rows, a.dim) | o.input("s", a.s, a.rows, a.dim) |
+                       o.input("dsum", a.dsum, a.rows, a.dim);
+  o.input("weight", a.weight, a.dim);
+  o.input("rstd", a.rstd, a.rows);
+  o.output("dx", a.dx, a.rows, a.dim, own);
+  o.output("dweight", a.dweight, a.dim);
+  return o.result();
+}
+int overlap(const lipz_quantize_rows_args& a) {
+  Overlap o{"lipz_quantize_rows", a.groups};
+  o.input("x", a.x, a.rows, a.dim);
+  o.output("q", a.q, a.rows, a.dim);
+  o.output("scale", a.scale, a.rows);
+  return o.result();
+}
+int overlap(const lipz_linear_args& a) {
+  Overlap o{"lipz_linear", a.groups};
+  const unsigned own = o.input("residual", a.residual, a.rows, a.n);
+  o.input("x", a.x, a.rows, a.k);
+  o.input("w", a.w, a.n, a.k);
+  o.input("bias", a.bias, a.n);
+  if (a.x.type == LIPZ_E4M3) {
+    o.input("x_scale", a.x_scale, a.rows);
+    o.input("w_scale", a.w_scale, a.n);
+  }
+  o.output("y", a.y, a.rows, a.n, own);
+  o.output("pre", a.pre, a.rows, a.n);
+  return o.result();
+}
+int overlap(const lipz_linear_backward_args& a) {
+  Overlap o{"lipz_linear_backward", a.groups};
+  o.input("dy", a.dy, a.rows, a.n);
+  if (a.dw.data) o.input("x", a.x, a.rows, a.k);
+  if (a.dx.data) o.input("w", a.w, a.n, a.k);
+  if (a.act != LIPZ_ACT_NONE) o.input("pre", a.pre, a.rows, a.n);
+  o.output("dx", a.dx, a.rows, a.k);
+  o.output("dw", a.dw, a.n, a.k);
+  o.output("db", a.db, a.n);
+  return o.result();
+}
+
 }  // namespace
 
 extern "C" {
 
 int lipz_rmsnorm(const lipz_rmsnorm_args* a, void* stream) {
   if (int rc = check(a)) return rc;
+  if (int rc = overlap(*a)) return rc;
   if (int rc = take_timeout("lipz_rmsnorm")) return rc;
   return finish("lipz_rmsnorm", ops::rmsnorm(*a, (cudaStream_t)stream));
 }
@@ -258,12 +417,14 @@ int lipz_rmsnorm_backward(const lipz_rmsnorm_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_rmsnorm_backward", a->groups, a->rows};
   if (!c.space(a->workspace, a->workspace_bytes, space_of(*a))) return c.rc;
+  if (int rc = overlap(*a)) return rc;
   if (int rc = take_timeout(c.call)) return rc;
   return finish(c.call, ops::rmsnorm_backward(*a, (cudaStream_t)stream));
 }
 
 int lipz_quantize_rows(const lipz_quantize_rows_args* a, void* stream) {
   if (int rc = check(a)) return rc;
+  if (int rc = overlap(*a)) return rc;
   if (int rc = take_timeout("lipz_quantize_rows")) return rc;
   return finish("lipz_quantize_rows", ops::quantize_rows(*a, (cudaStream_t)stream));
 }
@@ -278,6 +439,8 @@ int lipz_linear_workspace(const lipz_linear_args* a, uint64_t* bytes) {
 int lipz_linear(const lipz_linear_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear", a->groups, a->rows};
+  if (int rc = overlap(*a))
+    return c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a)) ? rc : c.rc;
   if (int rc = take_timeout(c.call)) return rc;
   uint64_t need;
   const cudaError_t e = ops::linear(*a, (cudaStream_t)stream, &need);
@@ -295,6 +458,8 @@ int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t*
 int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear_backward", a->groups, a->rows};
+  if (int rc = overlap(*a))
+    return c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a)) ? rc : c.rc;
   if (int rc = take_timeout(c.call)) return rc;
   uint64_t need;
   const cudaError_t e = ops::linear_backward(*a, (cudaStream_t)stream, &need);

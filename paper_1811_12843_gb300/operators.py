@@ -5,12 +5,12 @@
 forward and backward in bf16, and forward over 8-bit operands, for one network or for a population
 of them: tensors are [rows, columns], or [groups, rows, columns] with weights per group. Columns
 must be adjacent; rows and groups may be strided, and a group stride of 0 (``expand``) shares an
-input between the groups. An output may not overlap an input unless its call says so. Every call
-runs the library's CUDA kernels on the current stream of the tensors' device, allocates its outputs
-as torch does, waits for nothing, and may be captured in a CUDA graph. What the library does not
-take raises ``LipzError`` with nothing launched. Nothing here records an autograd graph: the
-backward passes are calls of their own, and a tensor that requires a gradient is taken under
-``torch.no_grad()`` or detached (else refused, since its gradient would be lost).
+input between the groups. An output may not overlap an input unless its call says so (refused where
+the strides show it). Every call runs the library's CUDA kernels on the current stream of the
+tensors' device, allocates its outputs as torch does, waits for nothing, and may be captured in a
+CUDA graph. What the library does not take raises ``LipzError`` with nothing launched. Nothing here
+records an autograd graph: the backward passes are calls of their own, and a tensor that requires a
+gradient is taken under ``torch.no_grad()`` or detached (else refused, since its gradient would be lost).
 """
 
 import importlib.util
