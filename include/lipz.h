@@ -355,7 +355,8 @@ LIPZ_API int lipz_fitness_from_logits_noalloc(const float* logits, int32_t cells
  *     two has no gaps between its rows or both have the same strides (of others the library compares
  *     the starts alone). It cannot check what lies at an address.
  *   - A bounded device-side wait that expires (the output is then not valid) is reported once, as
- *     LIPZ_ERR_TIMEOUT, by the next operator call or by lipz_operator_status().
+ *     LIPZ_ERR_TIMEOUT, to the thread that made the call (a graph's replays: that captured it), by its next
+ *     operator call, which then launches nothing, or by its lipz_operator_status().
  */
 enum { LIPZ_E4M3 = 2 };  /* 8-bit floats: 3 fraction bits, largest value 448, no infinity */
 enum {
@@ -469,8 +470,8 @@ typedef struct lipz_linear_backward_args {
 LIPZ_API int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t* bytes);
 LIPZ_API int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream);
 
-/* LIPZ_ERR_TIMEOUT if an operator's kernel gave up on a wait since the last report, else LIPZ_OK (of
- * the work that has run by now: it does not wait). */
+/* LIPZ_ERR_TIMEOUT if a kernel of this thread's operator calls gave up on a wait since the last report,
+ * else LIPZ_OK (of the work that has run by now: it does not wait). */
 LIPZ_API int lipz_operator_status(void);
 
 /* Message of this thread's last failed operator call. */

@@ -85,7 +85,7 @@ cudaError_t run_copies(const CopyJobs& jobs, cudaStream_t st);
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
                          cudaStream_t st);
 
-// The device word that a kernel sets when one of its waits expires (null: none can be had).
+// The word that a kernel of this thread's calls sets when one of its waits expires (null: none can be had).
 int* timeout_word();
 
 }  // namespace ops

@@ -1,9 +1,10 @@
 // C ABI of the residual-block operators: every argument that the host can check is checked here, then
 // the kernels of op_norm.cu, op_linear.cu and op_gemm.cu are launched.
 #include <algorithm>
-#include <atomic>
 #include <cstdarg>
 #include <cstdio>
+#include <cstring>
+#include <mutex>
 #include <utility>
 
 #include "op_gemm.h"
@@ -23,24 +24,34 @@ int sm_count() {
   return n;
 }
 
-// One word of pinned memory, which every device reaches: kernels store to it, the host reads it without
-// waiting for them.
+// A word of pinned memory for each host thread, which every device reaches: the kernels of the thread's calls store
+// to it, and the thread reads it without waiting for them. Words stay with the process, since a kernel, or a graph
+// that was captured from a call, may outlive the thread.
+thread_local int* t_word = nullptr;
+
 int* timeout_word() {
-  static int* const word = [] {
-    int* p = nullptr;
+  if (t_word) return t_word;
+  constexpr int BLOCK = 1024;
+  static std::mutex mutex;
+  static int* block = nullptr;
+  static int used = BLOCK;
+  const std::lock_guard<std::mutex> lock(mutex);
+  if (used == BLOCK) {
     // (allocating host memory is not part of a graph that another thread's stream may be capturing)
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     cudaThreadExchangeStreamCaptureMode(&mode);
-    if (cudaHostAlloc((void**)&p, sizeof(int), cudaHostAllocPortable | cudaHostAllocMapped) != cudaSuccess) {
-      cudaGetLastError();
-      p = nullptr;
-    } else {
-      *p = 0;
-    }
+    int* p = nullptr;
+    const cudaError_t e = cudaHostAlloc((void**)&p, BLOCK * sizeof(int), cudaHostAllocPortable | cudaHostAllocMapped);
     cudaThreadExchangeStreamCaptureMode(&mode);
-    return p;
-  }();
-  return word;
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    memset(p, 0, BLOCK * sizeof(int));
+    block = p;
+    used = 0;
+  }
+  return t_word = block + used++;
 }
 
 }  // namespace ops
@@ -58,20 +69,15 @@ __attribute__((format(printf, 2, 3))) int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-// Set once a kernel may have been launched that stores to the timeout word.
-std::atomic<bool> g_word_in_use{false};
-
 int finish(const char* call, cudaError_t e) {
-  g_word_in_use.store(true, std::memory_order_relaxed);
   if (e == cudaSuccess) return LIPZ_OK;
   cudaGetLastError();
   return fail(LIPZ_ERR_CUDA, "%s: %s", call, cudaGetErrorString(e));
 }
 
-// Whether a kernel gave up on a wait since the last report.
+// Whether a kernel of this thread's calls gave up on a wait since the last report.
 int take_timeout(const char* call) {
-  if (!g_word_in_use.load()) return LIPZ_OK;
-  int* word = ops::timeout_word();
+  int* const word = ops::t_word;  // (null: no kernel has been given one)
   const int code = word ? __atomic_exchange_n(word, 0, __ATOMIC_ACQ_REL) : 0;
   if (!code) return LIPZ_OK;
   return fail(LIPZ_ERR_TIMEOUT,
