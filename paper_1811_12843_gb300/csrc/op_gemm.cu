@@ -34,7 +34,11 @@ constexpr int EPI_WARPS = 16, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WAR
 constexpr int TURN = 32 * 17 * 4;         // a warp's block for turning rows into columns
 constexpr int MN_BOX = 64 * ROW;          // 64 k by 64 m (or n) of an operand whose rows run along m (n)
 static_assert(EPI_WARPS == SUM_WAYS, "a result warp per way");
-constexpr int SUM_CHUNKS = 8;             // chunks of k whose sum stands in tensor memory, for fp32 results
+// Tensor-core additions truncate: a sum of terms of one sign loses up to 2^-23 of its value by each 16 bf16 (32
+// e4m3) of k. fp32 results therefore are sums, in registers, of tensor memory's sums over SUM_CHUNKS chunks of k.
+// bf16 results are such sums (of more chunks: 2^-15) from LONG_CHUNKS (16384 bf16) on, where a single sum has lost
+// 2^-13 and at 500000 bf16 of k 2.3e-3, more than half of their half unit.
+constexpr int SUM_CHUNKS = 8, BF16_SUM_CHUNKS = 64, LONG_CHUNKS = 256;
 constexpr int SMEM_MAX = 232448, STAGES_MAX = 20;
 constexpr int DIRECT_CHUNKS = 4;          // most chunks of k per CTA whose operands the result warps bring
 
@@ -110,6 +114,7 @@ struct GemmParams {
   Problem p[NP];
   PartSums sums;
   int units, stages, stage_bytes, a_rows;  // a_rows: of A in a stage
+  int sum_chunks;                          // of k per sum in tensor memory, where results are sums of such
   int* err;
 };
 
@@ -290,9 +295,8 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
   return {g, first + q - nt * (whole ? 8 : p.tiles_m - first), nt, unit - t * p.splits};
 }
 
-// T: the results' type; fp32 results are sums, in fp32 registers, of sums over SUM_CHUNKS chunks of k,
-// because the tensor cores' additions truncate. FORWARD: K-major operands and the forward's epilogue, one
-// product; else up to two plain products.
+// T: float where results (of either type) are sums of sums over sum_chunks, else bf16. FORWARD: K-major operands and the
+// forward's epilogue, one product; else up to two plain products.
 // VIA: the residual comes and the results leave by TMA, through shared memory. With row-per-lane accesses,
 // whose 64-byte pieces reach memory one by one, results cost 12 us and a residual 25 more at 144 x 512 x 256
 // -> 768 (tanh with residual 88 us in all; by TMA 62).
@@ -463,7 +467,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         int c0, c1;
         chunk_range(p, pl.split, c0, c1);
         for (int kc = c0; kc < c1 && ok;) {
-          const int end = SUMS ? min(c1, kc + SUM_CHUNKS) : c1, r = sums % ACCS;
+          const int end = SUMS ? min(c1, kc + prm.sum_chunks) : c1, r = sums % ACCS;
           if (sums >= ACCS &&
               !wait(bFree + 8 * r, (uint32_t)(sums / ACCS - 1) & 1, abort_flag, code, 2)) {
             ok = false;
@@ -660,15 +664,21 @@ __global__ void __launch_bounds__(THREADS, 1)
       // VIA: this lane's 64 bytes of the warp's 32 rows, 16-byte units in the 64-byte swizzle
       uint8_t* mine = tiles + r * S::TILE + (ew >> 2) * (S::TILE / (BN / 32)) + q * 2048 + lane * 64;
       const int swizzle = lane >> 1 & 3;
+      const bool as_bf16 = SUMS && e.y.type == LIPZ_BF16;
       auto residual = [&](uint32_t (&v)[VW], int c) {
         if (VIA || !has_res) return;
-        const T* src =
-            (const T*)e.residual.data + sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
+        const int64_t at = sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
 #pragma unroll
-        for (int h = 0; h < CW; h += 16)
-          if (columns_left(c + h) > 0)
-            load_row<T>(src + h, e.residual.row, rows, columns_left(c + h), p.res_align, turn,
+        for (int h = 0; h < CW; h += 16) {
+          const int cols = columns_left(c + h);
+          if (cols <= 0) continue;
+          if (as_bf16)
+            load_row<bf16>((const bf16*)e.residual.data + at + h, e.residual.row, rows, cols, p.res_align, turn,
+                           v + h / 16 * WORDS<bf16>);
+          else
+            load_row<T>((const T*)e.residual.data + at + h, e.residual.row, rows, cols, p.res_align, turn,
                         v + h / 16 * WORDS<T>);
+        }
       };
       auto results = [&](float (&u)[CW], const uint32_t (&v)[VW], int c) {
         if (rows <= 0 || columns_left(c) <= 0) return;
@@ -722,6 +732,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
               for (int i = 0; i < 8; ++i) u[j * 8 + i] += element<T>(ww, i);
             }
+          } else if (has_res && as_bf16) {
+#pragma unroll
+            for (int i = 0; i < CW; ++i) u[i] += element<bf16>(v + i / 16 * WORDS<bf16>, i % 16);
           } else if (has_res) {
 #pragma unroll
             for (int i = 0; i < CW; ++i) u[i] += element<T>(v + i / 16 * WORDS<T>, i % 16);
@@ -740,11 +753,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             tc::tma_store_3d(&prm.y, tc::smem_u32(mine), sl.n + col0, sl.m + q * 32, sl.g);
           return;
         }
-        T* dst = (T*)e.y.data + sl.y + (int64_t)(q * 32) * e.y.row + col0 + c;
+        const int64_t at = sl.y + (int64_t)(q * 32) * e.y.row + col0 + c;
 #pragma unroll
-        for (int h = 0; h < CW; h += 16)
-          if (columns_left(c + h) > 0)
-            store_row<T>(dst + h, e.y.row, rows, columns_left(c + h), p.y_align, turn, u + h);
+        for (int h = 0; h < CW; h += 16) {
+          const int cols = columns_left(c + h);
+          if (cols <= 0) continue;
+          if (as_bf16) store_row<bf16>((bf16*)e.y.data + at + h, e.y.row, rows, cols, p.y_align, turn, u + h);
+          else store_row<T>((T*)e.y.data + at + h, e.y.row, rows, cols, p.y_align, turn, u + h);
+        }
       };
       auto tmem_load = [&](uint32_t t, float (&u)[CW]) {
         uint32_t r[CW];
@@ -760,7 +776,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         float acc[CW];
 #pragma unroll
         for (int i = 0; i < CW; ++i) acc[i] = 0.f;
-        for (int kc = sl.c0; kc < sl.c1; kc += SUM_CHUNKS) {
+        for (int kc = sl.c0; kc < sl.c1; kc += prm.sum_chunks) {
           const uint32_t t = wait_sum();
           if (!ok) break;
           float u[CW];
@@ -1034,6 +1050,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   }
   if (sums) k.sums = *sums;
   k.err = timeout_word();
+  k.sum_chunks = q.g[0].e.y.type == LIPZ_FP32 ? SUM_CHUNKS : BF16_SUM_CHUNKS;
   const Gemm& first = q.g[0];
   k.a_rows = FORWARD && CG == 1 && first.m < 128 ? (int)ceil_div(first.m, 8) * 8 : 128;
   k.stage_bytes = S::stage(k.a_rows);
@@ -1074,15 +1091,15 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
                          cudaStream_t st) {
   if constexpr (FORWARD) {
     if (p.direct)
-      return q.g[0].e.y.type == LIPZ_FP32
+      return p.sums
                  ? launch<TYPE, 1, 64, true, float, false, true, true>(q, p, parts, sums, st)
                  : launch<TYPE, 1, 64, true, bf16, false, true, true>(q, p, parts, sums, st);
     if (p.p[0].splits > 1)
-      return q.g[0].e.y.type == LIPZ_FP32
+      return p.sums
                  ? launch<TYPE, 1, 64, true, float, false, true>(q, p, parts, sums, st)
                  : launch<TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
   }
-  if (q.g[0].e.y.type == LIPZ_FP32) {
+  if (p.sums) {
     if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, float>(q, p, parts, sums, st);
     if (p.bn == 128) return launch<TYPE, 1, 128, FORWARD, float>(q, p, parts, sums, st);
     return launch<TYPE, 1, 64, FORWARD, float>(q, p, parts, sums, st);
@@ -1103,7 +1120,7 @@ GemmPlan plan_products(const Products& q) {
   GemmPlan plan{};
   const Gemm& g0 = q.g[0];
   const int eb = type_bytes(g0.type);
-  const bool sums = g0.e.y.type == LIPZ_FP32, res = g0.e.residual.data, heavy = g0.e.act >= LIPZ_ACT_TANH;
+  const bool fp32 = g0.e.y.type == LIPZ_FP32, res = g0.e.residual.data, heavy = g0.e.act >= LIPZ_ACT_TANH;
   // The shape and the number of parts of k that take the fewest clocks by a model of a unit's time: its MMA
   // steps (of 32 bytes of k) beside the epilogue of the unit before; parts of k cost a cluster's exchange,
   // or another launch and their way through L2. Clocks measured (1.9 GHz): MMA steps at 8192 x 4096 -> 8192
@@ -1120,14 +1137,14 @@ GemmPlan plan_products(const Products& q) {
   const int sms = sm_count();
   double best = -1;
   for (const Shape& shape : shapes) {
-    if (sums && shape.bn > 128) continue;
+    if (fp32 && shape.bn > 128) continue;
     // a forward's parts of k are a cluster's CTAs, all clusters resident at once
     for (int s0 = 1; s0 <= (forward ? 8 : 64); s0 *= 2) {
       if (forward && s0 > 1 && shape.bn != 64) continue;
       const Shape& c = by_tma && s0 == 1 && shape.cg == 2 && shape.bn == 128 ? via : shape;
       const int64_t slots = sms / c.cg;
       GemmPlan t{};
-      t.cg = c.cg, t.bn = c.bn;
+      t.cg = c.cg, t.bn = c.bn, t.sums = fp32;
       double work = 0, top = 0, last = 0, extra = 0;
       bool fits = true, split = false;
       for (int i = 0; i < q.n; ++i) {
@@ -1138,6 +1155,7 @@ GemmPlan plan_products(const Products& q) {
         const int64_t want = s0 < o.chunks ? s0 : o.chunks, tiles = o.tiles_m * o.tiles_n * g.groups;
         o.chunks_per_split = ceil_div(o.chunks, want);
         o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);
+        t.sums = t.sums || o.chunks_per_split > LONG_CHUNKS;
         fits = fits && tiles * o.splits <= INT32_MAX / 2 &&
                (o.splits == 1 || tiles * o.splits <= (forward ? 1 : 2) * slots) &&
                (!forward || o.splits == s0);
@@ -1150,7 +1168,7 @@ GemmPlan plan_products(const Products& q) {
         if (o.splits > 1 && !forward) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000;
         split = split || o.splits > 1;
       }
-      if (!fits || (s0 > 1 && !split)) continue;
+      if (!fits || (s0 > 1 && !split) || (t.sums && c.bn > 128)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
       // (a cluster's CTA finishes 64 / s0 columns of up to 128 rows, an element per thread and turn)
@@ -1169,7 +1187,7 @@ GemmPlan plan_products(const Products& q) {
     o.tiles_m = ceil_div(g0.m, 128), o.tiles_n = ceil_div(g0.n, 64), o.chunks = ceil_div(g0.k * eb, ROW);
     const int64_t tiles = o.tiles_m * o.tiles_n * g0.groups;
     if ((!tma_takes(g0.a, xa, g0.groups, eb) || !tma_takes(g0.b, xb, g0.groups, eb)) && tiles <= sms) {
-      t.direct = true, t.cg = 1, t.bn = 64;
+      t.direct = true, t.sums = fp32, t.cg = 1, t.bn = 64;
       for (int s0 = 8; s0 >= 1; s0 /= 2) {
         o.chunks_per_split = ceil_div(o.chunks, s0 < o.chunks ? s0 : o.chunks);
         o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);

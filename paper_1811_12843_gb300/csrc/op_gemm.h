@@ -65,6 +65,7 @@ struct GemmPlan {
   } p[2];
   int cg, bn;
   bool direct;  // operands from rows that TMA does not take, without copies
+  bool sums;    // results that are sums, in fp32 registers, of sums over a few chunks of k
   uint64_t bytes;
 };
 GemmPlan plan_products(const Products& q);

@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constan
 }
 
 // The workspace of a backward call: du (where dy is not it), the parts of db, then the products' own. dx and
-// dw share a launch where their results have one type.
+// dw share a launch where their results are bf16 and neither's sums are long.
 struct BackPlan {
   bool vec, need_du;
   int64_t ldu, blocks, rows_per_block;
@@ -313,13 +313,14 @@ BackPlan back_plan(const lipz_linear_backward_args& a) {
   const Gemm dw{{d, dg, dr, false}, {a.x.data, a.x.group, a.x.row, false}, LIPZ_BF16, a.groups, a.n,
                 a.k, a.rows, {a.dw}};
   // bf16 results run as planned for both, whether or not both are asked for, so that one's values do not
-  // depend on the other; fp32 results are planned by themselves
+  // depend on the other; fp32 results are planned by themselves, and so are products of which one is so long
+  // that its shape would slow the other (16392 x 4096 -> 4096: 708 us in one launch, 662 in two)
   Products both{{dx, dw}, 2};
   both.g[0].e.y.type = both.g[1].e.y.type = LIPZ_BF16;
   const GemmPlan joint = plan_products(both);
   auto add = [&](const Gemm& g, int i) {
     if (!g.e.y.data) return;
-    if (g.e.y.type == LIPZ_FP32) {
+    if (g.e.y.type == LIPZ_FP32 || joint.sums) {
       b.q[b.launches] = {{g}, 1};
       b.plan[b.launches] = plan_products(b.q[b.launches]);
       ++b.launches;
