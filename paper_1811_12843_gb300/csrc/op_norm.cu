@@ -1335,12 +1335,16 @@ struct BackBlocks {
 BackBlocks backward_blocks(const lipz_rmsnorm_backward_args& a) {
   const int64_t groups = a.groups > 0 ? a.groups : 1;
   if (backward_short(a)) {
-    // sixteen warps per SM; one block per group, which needs no second launch, from half that many groups on
+    // Sixteen warps per SM. Where that is fewer than four blocks per group, one block per group, which needs no
+    // second launch, while its turns are few (bf16 40 groups of 100 x 256 10 us, by three blocks 13, but 6000 x 256
+    // 150 and 72; 60 of 1000 x 256 30 and 24) or more blocks would come one after the other (144 of 1000 x 1024
+    // 156, by two 162, but 90 130, by three 109).
     const int lanes = back_lanes(ceil_div(a.dim, 16 / type_bytes(a.dy.type)));
     const int warps = lanes > 32 ? BACK_WARPS<4> : BACK_WARPS<2>, set = warps * (lanes > 32 ? 1 : 32 / lanes);
     const int64_t fill = (int64_t)(16 / warps) * sm_count() / groups, most = ceil_div(a.rows, 2 * set);
-    const int64_t b = fill < 4 ? 1 : fill < most ? fill : most;
-    return {b < 1 ? 1 : (int)b, b < 1 ? 1 : (int)b};
+    const int64_t b = fill < most ? fill : most;
+    const bool one = fill < 4 && (ceil_div(a.rows, set) <= 16 || ceil_div(b * groups, sm_count()) >= b);
+    return one || b < 1 ? BackBlocks{1, 1} : BackBlocks{(int)b, (int)b};
   }
   // four rows or more per block, whole clusters where there are that many
   const StreamShape s = backward_shape(a);
