@@ -346,7 +346,9 @@ LIPZ_API int lipz_fitness_from_logits_noalloc(const float* logits, int32_t cells
  *   - groups or rows may be 0 (weight gradients over no rows are zeros); column counts are at least 1.
  *   - All arithmetic is in fp32 or more, with one rounding at the end of a chain that its call names;
  *     NaN and infinity pass through as IEEE arithmetic has them. No atomics: the same inputs give the
- *     same bits.
+ *     same bits. Activations take the hardware's exponential and reciprocal: relative errors up to
+ *     2^-20, and for silu and gelu 2^-23 and 2^-21 times the argument of their e^-v on top; tanh for
+ *     bf16 results 2^-16.
  *   - Calls are asynchronous, allocate nothing on the device and may be captured in a graph. A call
  *     that needs scratch memory says how much (its _workspace form, 0 for many sizes); the workspace
  *     is 256-byte aligned, and free again when the call's work on the stream is done.

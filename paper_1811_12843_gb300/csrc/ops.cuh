@@ -134,7 +134,8 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return y;
 }
 constexpr float LOG2E = 1.44269504088896341f;
-// 1 / (1 + e^-v): two hardware approximations of 2^-22 or better
+// 1 / (1 + e^-v): the hardware's exponential and reciprocal, 2^-22 and 2^-23 of the value, and the rounding of the
+// exponent LOG2E v, which weighs |v| 2^-23 where e^-v does (2^-17 at v = -80)
 __device__ __forceinline__ float logistic(float v) { return rcp_approx(1.f + ex2_approx(-LOG2E * v)); }
 // gelu in its tanh form is u logistic(u (GELU_1 + GELU_3 u^2)): no difference of near values
 constexpr float GELU_1 = 1.59576912160573071f, GELU_3 = 0.0713548162726009f;
