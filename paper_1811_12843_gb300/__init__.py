@@ -356,11 +356,6 @@ def lipz_fitness_from_logits_noalloc(logits, cells, batch, fit_g, fit_d, stream=
 
 
 # ---- operators of residual blocks (the `operators` module takes torch tensors) ---------------
-def _args(a):
-    """An argument structure, or its bytes."""
-    return a if isinstance(a, bytes) else ctypes.byref(a)
-
-
 def _check_op(rc):
     if rc != LIPZ_OK:
         raise LipzError(rc, lipz_operator_error())
@@ -369,12 +364,12 @@ def _check_op(rc):
 
 def _workspace_of(call, args):
     n = ctypes.c_uint64()
-    _check_op(call(_args(args), ctypes.byref(n)))
+    _check_op(call(ctypes.byref(args), ctypes.byref(n)))
     return n.value
 
 
 def lipz_rmsnorm(args, stream=0):
-    return _check_op(load().lipz_rmsnorm(_args(args), stream))
+    return _check_op(load().lipz_rmsnorm(ctypes.byref(args), stream))
 
 
 def lipz_rmsnorm_backward_workspace(args) -> int:
@@ -382,11 +377,11 @@ def lipz_rmsnorm_backward_workspace(args) -> int:
 
 
 def lipz_rmsnorm_backward(args, stream=0):
-    return _check_op(load().lipz_rmsnorm_backward(_args(args), stream))
+    return _check_op(load().lipz_rmsnorm_backward(ctypes.byref(args), stream))
 
 
 def lipz_quantize_rows(args, stream=0):
-    return _check_op(load().lipz_quantize_rows(_args(args), stream))
+    return _check_op(load().lipz_quantize_rows(ctypes.byref(args), stream))
 
 
 def lipz_linear_workspace(args) -> int:
@@ -394,7 +389,7 @@ def lipz_linear_workspace(args) -> int:
 
 
 def lipz_linear(args, stream=0):
-    return _check_op(load().lipz_linear(_args(args), stream))
+    return _check_op(load().lipz_linear(ctypes.byref(args), stream))
 
 
 def lipz_linear_backward_workspace(args) -> int:
@@ -402,7 +397,7 @@ def lipz_linear_backward_workspace(args) -> int:
 
 
 def lipz_linear_backward(args, stream=0):
-    return _check_op(load().lipz_linear_backward(_args(args), stream))
+    return _check_op(load().lipz_linear_backward(ctypes.byref(args), stream))
 
 
 def lipz_operator_status():
