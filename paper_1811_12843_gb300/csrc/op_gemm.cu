@@ -295,8 +295,8 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
   return {g, first + q - nt * (whole ? 8 : p.tiles_m - first), nt, unit - t * p.splits};
 }
 
-// T: float where results (of either type) are sums of sums over sum_chunks, else bf16. FORWARD: K-major operands and the
-// forward's epilogue, one product; else up to two plain products.
+// T: float where results (of either type) are sums of sums over sum_chunks, else bf16. FORWARD: K-major operands
+// and the forward's epilogue, one product; else up to two plain products.
 // VIA: the residual comes and the results leave by TMA, through shared memory. With row-per-lane accesses,
 // whose 64-byte pieces reach memory one by one, results cost 12 us and a residual 25 more at 144 x 512 x 256
 // -> 768 (tanh with residual 88 us in all; by TMA 62).

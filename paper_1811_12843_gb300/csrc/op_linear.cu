@@ -157,11 +157,12 @@ bool in_units(const lipz_linear_args& a) {
 // Few rows go to k_linear_rows while it is the faster. Beside w's bytes it pays for each row of x that meets
 // them, so the weights that it takes fall with the square of the rows, and for each block, so the outputs of
 // all groups are bounded; element by element (rows off the 16-byte grid) its rate is bounded by the loads,
-// and the tensor cores' product has such rows copied first. There and on the tensor cores, us, bf16:
-//   rows   1 x 4096 -> 4096 12.3, 16.5   2 x 4096 -> 4096 14.5, 16.5   4 x 4096 -> 4096 18.7, 16.4
-//          1 x 8192 -> 8192 29.0, 34.3   2 x 8192 -> 8192 41.5, 34.6   4 x 1024 -> 1024  8.3, 14.5
-//   blocks 1 x 512 -> 16384 11.1, 11.9   1 x 512 -> 32768 15.3, 14.3   1 x 256 -> 512, 256 groups 34.8, 18.5
-//   odd    2 x 1001 -> 8001 18.4, 22.7   2 x 4001 -> 8001 59.2, 52.4   1 x 777 -> 500, 16 groups 14.3, 19.4
+// and the tensor cores' product has such rows copied first. There and on the tensor cores, us, bf16 (between events,
+// a launch with them, after a flush of L2; among other calls 1 x 4096 -> 4096 takes 10.2):
+//   rows   1 x 4096 -> 4096 12.3, 16.8   2 x 4096 -> 4096 14.4, 16.6   4 x 4096 -> 4096 19.7, 16.4
+//          1 x 8192 -> 8192 29.1, 34.8   2 x 8192 -> 8192 42.0, 34.4   4 x 1024 -> 1024  8.2, 14.3
+//   blocks 1 x 512 -> 16384 11.1, 12.0   1 x 512 -> 32768 14.6, 14.3   1 x 256 -> 512, 256 groups 35.5, 18.8
+//   odd    2 x 1001 -> 8001 19.1, 23.4   2 x 4001 -> 8001 58.6, 52.2   1 x 777 -> 500, 16 groups 15.6, 19.6
 bool few_rows(const lipz_linear_args& a) {
   if (a.rows > 4) return false;
   const double work = (double)a.rows * a.rows * a.groups * a.n * a.k;

@@ -98,7 +98,8 @@ __device__ __forceinline__ RowScale row_scale(const RowArgs& p, int64_t g, int64
 }
 
 // Element by element: v f, v w, and the sums of squares; in bf16 rows, whose instructions bound them, two at a
-// time (16384 x 4096 quantiser 35 -> 32 us, norm 54 -> 51; fp32 rows lose by the registers that pairs need).
+// time (16384 x 4096 quantiser 35 -> 33 us between events, 38 among other calls, norm 54 -> 51; fp32 rows lose by the
+// registers that pairs need, but for the two products with 1 / scale).
 template <int E>
 __device__ __forceinline__ void scale_by(float* v, float f) {
 #pragma unroll
@@ -500,8 +501,10 @@ __global__ void __launch_bounds__(512) k_rows_stream(const RowArgs p, int stages
 
 // ---- rows that start off the 16-byte grid (odd widths), all of a call's matrices at the same place of a
 // 16-byte unit in each row: threads take the whole units that a row touches, and the first and the last of
-// them in part. Parameters stand in shared memory, one word in E + 1 left out, so that lanes E columns apart meet different banks. (Element by element, 16385 x 4097 with residual
-// to 8 bits took 262 us, and 332 backward.)
+// them in part. Parameters stand in shared memory, one word in E + 1 left out, so that lanes E columns apart
+// meet different banks. Bound: instructions (bf16 8192 x 8191 norm 64 us, floor 40, quantiser 39, floor 30). Element
+// by element, which matrices at different places of a unit and rows past SHIFT_MAX_DIM still are, 16385 x 4097 with
+// residual to 8 bits took 262 us, and 332 backward.
 // Where a column's parameter stands, E columns of zeros on either side.
 template <int E>
 __device__ __forceinline__ int padded(int c) {
@@ -898,8 +901,8 @@ __global__ void __launch_bounds__(512) k_rmsnorm_backward_shift(const BackArgs p
 // Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of
 // WARPS walks over rows of one group, and its warps' sums for dweight are added in shared memory. (With a
 // ring and a block per row, 144 x 100 x 256 took 20 us with the parts' sum, two thirds of it the blocks'
-// own set-up; 10 so. With 32 lanes to every row bf16 131072 x 256 took 54 us instead of 39, 262144 x 64 77
-// instead of 23.)
+// own set-up; 10 so, between events after a flush of L2, and 7.5 among other calls. With 32 lanes to every row bf16
+// 131072 x 256 took 54 us instead of 39, 262144 x 64 77 instead of 23.)
 template <int NV>
 constexpr int BACK_WARPS = NV <= 2 ? 16 : 8;  // (registers)
 

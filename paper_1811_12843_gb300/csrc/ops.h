@@ -48,7 +48,7 @@ inline bool space_given(const void* p, uint64_t have, uint64_t need) {
   return !need || (p && have >= need && (uintptr_t)p % 256 == 0);
 }
 // *need: the scratch memory; nothing is launched where the call does not have it. (The plan that tells is the
-// launch's own: a call plans once.)
+// launch's own. A caller that first asks for the size, as the torch binding does, has the plan made twice.)
 uint64_t linear_workspace(const lipz_linear_args& a);
 cudaError_t linear(const lipz_linear_args& a, cudaStream_t st, uint64_t* need);
 uint64_t linear_backward_workspace(const lipz_linear_backward_args& a);

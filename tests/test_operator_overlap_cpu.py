@@ -37,7 +37,8 @@ int main() {
     bool shared = false;
     for (uintptr_t x : a) shared = shared || b.count(x);
     const Region p = r[0].joined(), q = r[1].joined();
-    const bool exact = (p.rows < 2 || q.rows < 2 || p.row == q.row) && (p.groups < 2 || q.groups < 2 || p.group == q.group);
+    const bool exact =
+        (p.rows < 2 || q.rows < 2 || p.row == q.row) && (p.groups < 2 || q.groups < 2 || p.group == q.group);
     if (meet(r[0], r[1]) != meet(r[1], r[0]) || (meet(r[0], r[1]) ? !shared : exact && shared)) {
       for (const Region& x : r)
         printf("%d %d x %d rows %d apart, %d groups %d apart\n", (int)x.at, (int)x.width, (int)x.rows, (int)x.row,

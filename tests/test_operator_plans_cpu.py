@@ -16,8 +16,9 @@ def L():
 
 
 @pytest.mark.parametrize("groups,rows,dim,parts", [
-    (144, 100, 256, 1), (60, 100, 256, 1), (40, 300, 256, 1), (40, 6000, 256, 3), (60, 2000, 256, 2), (76, 6000, 64, 2),
-    (90, 6000, 256, 1), (90, 1000, 1024, 3), (144, 1000, 1024, 1), (90, 100, 1024, 1), (20, 6000, 256, 7), (1, 8, 64, 1)])
+    (144, 100, 256, 1), (60, 100, 256, 1), (40, 300, 256, 1), (40, 6000, 256, 3), (60, 2000, 256, 2),
+    (76, 6000, 64, 2), (90, 6000, 256, 1), (90, 1000, 1024, 3), (144, 1000, 1024, 1), (90, 100, 1024, 1),
+    (20, 6000, 256, 7), (1, 8, 64, 1)])
 def test_norm_backward_of_short_rows_fills_the_device(L, groups, rows, dim, parts):
     """Few turns, or no free SMs: one block per group, whose sums need no workspace."""
     def mat(at):
