@@ -38,9 +38,11 @@ def _nvcc():
 
 
 def _torch_dir():
-    """torch's installation, found without importing it; None without one (and then no binding)."""
+    """The installation of a torch with CUDA, found without importing it; None without one (and then no
+    binding: the library is complete without it)."""
     spec = importlib.util.find_spec("torch")
-    return os.path.dirname(spec.origin) if spec is not None and spec.origin else None
+    d = os.path.dirname(spec.origin) if spec is not None and spec.origin else None
+    return d if d and os.path.exists(os.path.join(d, "lib", "libc10_cuda.so")) else None
 
 
 def _cxx():
