@@ -380,6 +380,22 @@ typedef struct lipz_vec { /* fp32 */
 } lipz_vec;
 
 /*
+ * A checkpoint: a matrix of activations kept in 8 bits for a backward pass. Each 16 adjacent columns of a
+ * row (the last ones: what there is) share a power of two 2^e, the smallest with e >= -126 that brings
+ * their magnitudes below 127.5, and are rounded to its nearest multiples (ties to even): an element is off
+ * by at most 2^e / 2, which is less than 2^-7 of its block's largest magnitude (or 2^-127). data: the
+ * multiples, -127..127; scale: a byte e + 127 per 16 columns. The value q 2^e is a bf16 number. A block that
+ * holds an infinity or a NaN has the byte 255 and stands for NaN throughout.
+ */
+#define LIPZ_BLOCK 16
+typedef struct lipz_blocks {
+  int8_t* data;                     /* [groups][rows][cols] */
+  int64_t group, row;               /* element strides */
+  uint8_t* scale;                   /* [groups][rows][(cols + 15) / 16] */
+  int64_t scale_group, scale_row;
+} lipz_blocks;
+
+/*
  * Root-mean-square norm of x (+ residual):
  *     s = x + residual;  rstd = 1 / sqrt(mean(s^2) + eps);  y = s rstd weight
  * x, residual, sum: one type, LIPZ_FP32 or LIPZ_BF16. sum (nullable) receives s rounded to that type
@@ -471,6 +487,90 @@ typedef struct lipz_linear_backward_args {
 } lipz_linear_backward_args;
 LIPZ_API int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t* bytes);
 LIPZ_API int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream);
+
+/*
+ * Layer norm of x (+ residual):
+ *     s = x + residual;  mean = mean(s);  rstd = 1 / sqrt(mean((s - mean)^2) + eps);
+ *     y = (s - mean) rstd weight + bias
+ * with the types, results and buffers of lipz_rmsnorm; bias (nullable) [dim]; mean and rstd [rows]
+ * (nullable) are kept for the backward pass. kept (nullable) receives what sum holds (without a
+ * residual: x) as a checkpoint; with a residual it needs sum. Squares are summed in fp32, as they are.
+ */
+typedef struct lipz_layernorm_args {
+  uint32_t struct_size;
+  float eps;
+  int64_t groups, rows, dim;
+  lipz_mat x, residual, sum, y;              /* residual, sum: data null = none */
+  lipz_vec weight, bias, scale, mean, rstd;  /* scale: e4m3 only */
+  lipz_blocks kept;                          /* data null = none */
+} lipz_layernorm_args;
+LIPZ_API int lipz_layernorm(const lipz_layernorm_args* a, void* stream);
+
+/*
+ * Its backward pass, from s (the x that was normalised, or sum), mean and rstd:
+ *     h = (s - mean) rstd;  g = dy weight;  dx = rstd (g - mean(g) - h mean(g h)) + dsum;
+ *     dweight = sum over rows of dy h;  dbias = sum over rows of dy
+ * with the types and buffers of lipz_rmsnorm_backward; s is a matrix of dy's type, or (s null) the
+ * checkpoint kept. dweight, dbias (each nullable): fp32, one per group.
+ */
+typedef struct lipz_layernorm_backward_args {
+  uint32_t struct_size;
+  uint32_t reserved;
+  int64_t groups, rows, dim;
+  lipz_mat dy, s, dsum, dx;
+  lipz_vec weight, mean, rstd, dweight, dbias;
+  lipz_blocks kept;
+  void* workspace;
+  uint64_t workspace_bytes;
+} lipz_layernorm_backward_args;
+LIPZ_API int lipz_layernorm_backward_workspace(const lipz_layernorm_backward_args* a, uint64_t* bytes);
+LIPZ_API int lipz_layernorm_backward(const lipz_layernorm_backward_args* a, void* stream);
+
+/* Rows (LIPZ_FP32 or LIPZ_BF16, any dim) to a checkpoint. */
+typedef struct lipz_checkpoint_rows_args {
+  uint32_t struct_size;
+  uint32_t reserved;
+  int64_t groups, rows, dim;
+  lipz_mat x;
+  lipz_blocks c;
+} lipz_checkpoint_rows_args;
+LIPZ_API int lipz_checkpoint_rows(const lipz_checkpoint_rows_args* a, void* stream);
+
+/* And back: y = act(v), v the values that the checkpoint stands for; y: LIPZ_FP32 or LIPZ_BF16. */
+typedef struct lipz_restore_rows_args {
+  uint32_t struct_size;
+  int32_t act;
+  float slope;
+  uint32_t reserved;
+  int64_t groups, rows, dim;
+  lipz_blocks c;
+  lipz_mat y;
+} lipz_restore_rows_args;
+LIPZ_API int lipz_restore_rows(const lipz_restore_rows_args* a, void* stream);
+
+/* lipz_linear (call, whose pre is null) that keeps u, before any rounding, as the checkpoint pre. */
+typedef struct lipz_linear_checkpoint_args {
+  uint32_t struct_size;
+  uint32_t reserved;
+  lipz_linear_args call;
+  lipz_blocks pre;
+} lipz_linear_checkpoint_args;
+LIPZ_API int lipz_linear_checkpoint_workspace(const lipz_linear_checkpoint_args* a, uint64_t* bytes);
+LIPZ_API int lipz_linear_checkpoint(const lipz_linear_checkpoint_args* a, void* stream);
+
+/*
+ * lipz_linear_backward (call) with checkpoints in the place of x, of pre, or of both (whose matrix in
+ * call is then null): the same results, to the bit, as over the bf16 values that they stand for.
+ */
+typedef struct lipz_linear_backward_checkpoint_args {
+  uint32_t struct_size;
+  uint32_t reserved;
+  lipz_linear_backward_args call;
+  lipz_blocks x, pre; /* data null = call's matrix */
+} lipz_linear_backward_checkpoint_args;
+LIPZ_API int lipz_linear_backward_checkpoint_workspace(const lipz_linear_backward_checkpoint_args* a,
+                                                       uint64_t* bytes);
+LIPZ_API int lipz_linear_backward_checkpoint(const lipz_linear_backward_checkpoint_args* a, void* stream);
 
 /* LIPZ_ERR_TIMEOUT if a kernel of this thread's operator calls gave up on a wait since the last report,
  * else LIPZ_OK (of the work that has run by now: it does not wait). */

@@ -28,6 +28,12 @@ __all__ = [
     "lipz_rmsnorm", "lipz_rmsnorm_backward", "lipz_rmsnorm_backward_workspace",
     "lipz_quantize_rows", "lipz_linear", "lipz_linear_workspace", "lipz_linear_backward",
     "lipz_linear_backward_workspace", "lipz_operator_status", "lipz_operator_error",
+    "lipz_blocks", "lipz_layernorm_args", "lipz_layernorm_backward_args", "lipz_checkpoint_rows_args",
+    "lipz_restore_rows_args", "lipz_linear_checkpoint_args", "lipz_linear_backward_checkpoint_args",
+    "lipz_layernorm", "lipz_layernorm_backward", "lipz_layernorm_backward_workspace",
+    "lipz_checkpoint_rows", "lipz_restore_rows", "lipz_linear_checkpoint",
+    "lipz_linear_checkpoint_workspace", "lipz_linear_backward_checkpoint",
+    "lipz_linear_backward_checkpoint_workspace",
     "EXPORTED", "Grid", "param_counts",
 ]
 
@@ -76,6 +82,11 @@ class lipz_vec(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("group", ctypes.c_int64)]
 
 
+class lipz_blocks(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("group", ctypes.c_int64), ("row", ctypes.c_int64),
+                ("scale", ctypes.c_void_p), ("scale_group", ctypes.c_int64), ("scale_row", ctypes.c_int64)]
+
+
 def _fields(sizes, mats, vecs, head=(("reserved", ctypes.c_uint32),), workspace=True):
     f = [("struct_size", ctypes.c_uint32)] + list(head)
     f += [(n, ctypes.c_int64) for n in sizes] + [(n, lipz_mat) for n in mats]
@@ -110,6 +121,36 @@ class lipz_linear_args(ctypes.Structure):
 class lipz_linear_backward_args(ctypes.Structure):
     _fields_ = _fields(("groups", "rows", "k", "n"), ("dy", "x", "w", "pre", "dx", "dw"), ("db",),
                        _ACT_HEAD)
+
+
+class lipz_layernorm_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), ("x", "residual", "sum", "y"),
+                       ("weight", "bias", "scale", "mean", "rstd"), (("eps", ctypes.c_float),),
+                       workspace=False) + [("kept", lipz_blocks)]
+
+
+class lipz_layernorm_backward_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), ("dy", "s", "dsum", "dx"),
+                       ("weight", "mean", "rstd", "dweight", "dbias"), workspace=False) + [
+        ("kept", lipz_blocks), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64)]
+
+
+class lipz_checkpoint_rows_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), ("x",), (), workspace=False) + [("c", lipz_blocks)]
+
+
+class lipz_restore_rows_args(ctypes.Structure):
+    _fields_ = _fields(("groups", "rows", "dim"), (), (), _ACT_HEAD, workspace=False) + [
+        ("c", lipz_blocks), ("y", lipz_mat)]
+
+
+class lipz_linear_checkpoint_args(ctypes.Structure):
+    _fields_ = _fields((), (), (), workspace=False) + [("call", lipz_linear_args), ("pre", lipz_blocks)]
+
+
+class lipz_linear_backward_checkpoint_args(ctypes.Structure):
+    _fields_ = _fields((), (), (), workspace=False) + [
+        ("call", lipz_linear_backward_args), ("x", lipz_blocks), ("pre", lipz_blocks)]
 
 
 _P = ctypes.c_void_p
@@ -149,6 +190,15 @@ _SIGS = {
     "lipz_linear_workspace": (_I, [_P, _P]),
     "lipz_linear_backward": (_I, [_P, _P]),
     "lipz_linear_backward_workspace": (_I, [_P, _P]),
+    "lipz_layernorm": (_I, [_P, _P]),
+    "lipz_layernorm_backward": (_I, [_P, _P]),
+    "lipz_layernorm_backward_workspace": (_I, [_P, _P]),
+    "lipz_checkpoint_rows": (_I, [_P, _P]),
+    "lipz_restore_rows": (_I, [_P, _P]),
+    "lipz_linear_checkpoint": (_I, [_P, _P]),
+    "lipz_linear_checkpoint_workspace": (_I, [_P, _P]),
+    "lipz_linear_backward_checkpoint": (_I, [_P, _P]),
+    "lipz_linear_backward_checkpoint_workspace": (_I, [_P, _P]),
     "lipz_operator_status": (_I, []),
     "lipz_operator_error": (ctypes.c_char_p, []),
     "lipz_last_error": (ctypes.c_char_p, [_P]),
@@ -398,6 +448,42 @@ def lipz_linear_backward_workspace(args) -> int:
 
 def lipz_linear_backward(args, stream=0):
     return _check_op(load().lipz_linear_backward(ctypes.byref(args), stream))
+
+
+def lipz_layernorm(args, stream=0):
+    return _check_op(load().lipz_layernorm(ctypes.byref(args), stream))
+
+
+def lipz_layernorm_backward_workspace(args) -> int:
+    return _workspace_of(load().lipz_layernorm_backward_workspace, args)
+
+
+def lipz_layernorm_backward(args, stream=0):
+    return _check_op(load().lipz_layernorm_backward(ctypes.byref(args), stream))
+
+
+def lipz_checkpoint_rows(args, stream=0):
+    return _check_op(load().lipz_checkpoint_rows(ctypes.byref(args), stream))
+
+
+def lipz_restore_rows(args, stream=0):
+    return _check_op(load().lipz_restore_rows(ctypes.byref(args), stream))
+
+
+def lipz_linear_checkpoint_workspace(args) -> int:
+    return _workspace_of(load().lipz_linear_checkpoint_workspace, args)
+
+
+def lipz_linear_checkpoint(args, stream=0):
+    return _check_op(load().lipz_linear_checkpoint(ctypes.byref(args), stream))
+
+
+def lipz_linear_backward_checkpoint_workspace(args) -> int:
+    return _workspace_of(load().lipz_linear_backward_checkpoint_workspace, args)
+
+
+def lipz_linear_backward_checkpoint(args, stream=0):
+    return _check_op(load().lipz_linear_backward_checkpoint(ctypes.byref(args), stream))
 
 
 def lipz_operator_status():

@@ -280,6 +280,23 @@ __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int col
     if (r < rows && col < cols) base[r * ld + col] = from_f<T>(turn[r * 17 + col]);
 }
 
+// A block of a checkpoint by one thread; cols: what there is of its 16 (what lies beyond may be NaN).
+__device__ __forceinline__ void keep_block(int8_t* dst, uint8_t* scale, int cols, int align, const float* v) {
+  uint32_t top = 0, w[4];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, i < cols ? magnitude(v[i]) : 0u);
+  const BlockScale s = block_scale(top);
+  block_multiples<16>(v, s.inv, w);
+  *scale = (uint8_t)s.byte;
+  if (align && cols >= 16) {
+    *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < cols) dst[i] = (int8_t)(w[i / 4] >> i % 4 * 8);
+  }
+}
+
 __device__ __forceinline__ int64_t ceil_div_d(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // A unit's place: which part of k of which tile; groups outermost, then panels of 8 tile rows, along which
@@ -719,6 +736,13 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int h = 0; h < CW; h += 16)
               if (columns_left(c + h) > 0)
                 store_row<bf16>(dst + h, e.pre.row, rows, columns_left(c + h), p.pre_align, turn, u + h);
+          } else if (e.kept.data && lane < rows) {
+            const int64_t m = sl.m + q * 32 + lane, n = sl.n + col0 + c;
+            int8_t* dst = e.kept.data + sl.g * e.kept.group + m * e.kept.row + n;
+            uint8_t* scale = e.kept.scale + sl.g * e.kept.scale_group + m * e.kept.scale_row + (n >> 4);
+#pragma unroll
+            for (int h = 0; h < CW; h += 16)
+              if (columns_left(c + h) > 0) keep_block(dst + h, scale + h / 16, columns_left(c + h), p.pre_align, u + h);
           }
           with_act(e.act, [&](auto act) {
 #pragma unroll
@@ -824,11 +848,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc::cluster_sync_all();  // every CTA's sums stand in its shared memory
     const Problem& p = prm.p[0];
     const Place pl = place(p, first);
-    const int parts = p.parts, rows = min(128, p.m - pl.mt * 128), width = BN / parts;
-    const int c0 = (int)tc::cluster_ctarank() * width;
-    for (int i = threadIdx.x; i < rows * width; i += THREADS) {
+    // (a checkpoint's blocks stay whole: then CTAs past the tile's last block finish nothing)
+    const bool kept = p.e.kept.data;
+    const int parts = p.parts, rows = min(128, p.m - pl.mt * 128), width = kept ? max(BN / parts, 16) : BN / parts;
+    const int c0 = (int)tc::cluster_ctarank() * width, count = c0 < BN ? rows * width : 0;
+    for (int i = threadIdx.x; i < count; i += THREADS) {
       const int r = i / width, c = c0 + i - r * width, n = pl.nt * BN + c;
-      if (n >= p.n) continue;
+      if (n >= p.n && !kept) continue;
       const uint32_t at = tc::smem_u32(s_part + r * (BN + 1) + c);
       float u = 0.f;
       for (int j = 0; j < parts; ++j) {
@@ -836,7 +862,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_shared(at, j)) : "memory");
         u += v;
       }
-      finish(p.e, pl.g, pl.mt * 128 + r, n, u);
+      if (kept) finish_kept(p.e, pl.g, pl.mt * 128 + r, n, n < p.n, u);
+      else finish(p.e, pl.g, pl.mt * 128 + r, n, u);
     }
   }
   tc::tc_fence_before();
@@ -934,13 +961,13 @@ Extent extent(const Operand& o, int64_t mn, int64_t k) {
 
 // Whether TMA takes the matrices as they lie: rows and groups on 16-byte boundaries, rows not overlapping.
 bool tma_takes(const Operand& o, const Extent& x, int64_t groups, int eb) {
-  if ((uintptr_t)o.data % 16) return false;
+  if (o.scale || (uintptr_t)o.data % 16) return false;
   if (x.rows > 1 && (o.ld * eb % 16 || o.ld < x.cols || o.ld * eb >= (int64_t)1 << 40)) return false;
   return groups == 1 || (o.group * eb % 16 == 0 && o.group * eb < (int64_t)1 << 40);
 }
 
 // An operand that the groups share is copied once (144 groups of 100 x 777 -> 501: 76 -> 38 us).
-int64_t copied_groups(const Operand& o, int64_t groups) { return o.group ? groups : 1; }
+int64_t copied_groups(const Operand& o, int64_t groups) { return o.group || o.scale_group ? groups : 1; }
 
 // The map of results or a residual, {n, m, groups}, in boxes of 32 bf16 columns.
 bool encode_tile(CUtensorMap* map, const lipz_mat& m, int64_t rows, int64_t cols, int64_t groups,
@@ -1040,6 +1067,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
       return a;
     };
     p.y_align = align(g.e.y), p.res_align = align(g.e.residual), p.pre_align = align(g.e.pre);
+    if (g.e.kept.data) p.pre_align = rows_aligned(bytes_of(g.e.kept), g.groups, g.m, 16) ? 16 : 0;
     k.units += p.units;
     if (VIA) {
       p.rz = g.groups > 1 && g.e.residual.group != 0;
@@ -1229,9 +1257,10 @@ int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* cop
     const int eb = type_bytes(g.type);
     auto add = [&](Operand& t, const Extent& x, int64_t ld, uint64_t bytes) {
       const int64_t groups = copied_groups(t, g.groups);
-      copies[n++] = {(const uint8_t*)t.data, w, t.group * eb, t.ld * eb, x.rows, groups * x.rows, x.cols * eb,
-                     ld * eb / 16};
-      t.data = w, t.ld = ld, t.group = groups > 1 ? x.rows * ld : 0;
+      const int from = t.scale ? 1 : eb;  // bytes of an element
+      copies[n++] = {(const uint8_t*)t.data, w, t.group * from, t.ld * from, x.rows, groups * x.rows,
+                     x.cols * from, ld * eb / 16, t.scale, t.scale_group, t.scale_ld};
+      t.data = w, t.ld = ld, t.group = groups > 1 ? x.rows * ld : 0, t.scale = nullptr;
       w += bytes;
     };
     if (o.copy_a) add(g.a, extent(g.a, g.m, g.k), o.lda, o.a_bytes);

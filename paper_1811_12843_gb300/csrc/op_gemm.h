@@ -7,20 +7,24 @@
 namespace lipz {
 namespace ops {
 
-// y = act(u) + residual, u = C x_scale[m] w_scale[n] + bias[n], pre = u.
+// y = act(u) + residual, u = C x_scale[m] w_scale[n] + bias[n], pre = u, or kept = u's checkpoint.
 struct Epilogue {
   lipz_mat y, residual, pre;
   lipz_vec x_scale, w_scale, bias;
   int act;
   float slope;
+  lipz_blocks kept;
 };
 
 // An operand's matrix as it lies in memory: rows of adjacent elements, `ld` elements apart. k_major: a
-// row per m (or n), its elements along k; else a row per k, its elements along m (or n).
+// row per m (or n), its elements along k; else a row per k, its elements along m (or n). With scales it is a
+// checkpoint, whose values are copied out before the product.
 struct Operand {
   const void* data;
   int64_t group, ld;
   bool k_major;
+  const uint8_t* scale;
+  int64_t scale_group, scale_ld;
 };
 
 struct Gemm {
@@ -47,12 +51,14 @@ struct Products {
   int n;
 };
 
-// Copies of operands whose rows TMA does not take, to rows of whole 16-byte units.
+// Copies of operands whose rows TMA does not take, to rows of whole 16-byte units, and checkpoints' values.
 struct RowCopy {
   const uint8_t* src;
   void* dst;
   int64_t group, ld, rows, total;  // strides in bytes; rows of a group, of all
-  int64_t bytes, units;            // of a row: to copy; 16-byte units there
+  int64_t bytes, units;            // of a row: to read; 16-byte units there
+  const uint8_t* scale;            // of a checkpoint, or null
+  int64_t scale_group, scale_ld;
 };
 
 // How products will run: their scratch memory, and the copies that have to be made before them.

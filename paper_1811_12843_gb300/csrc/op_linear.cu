@@ -62,14 +62,16 @@ struct VecParams {
   int rows, parts;  // warps that share an output
 };
 
-template <int TYPE, int R, bool VEC>
-__global__ void __launch_bounds__(32 * VEC_WARPS) k_linear_rows(const VecParams p) {
+// KEPT: u is kept as a checkpoint: VEC_WARPS * parts warps, so that a block has 16 outputs.
+template <int TYPE, int R, bool VEC, bool KEPT>
+__global__ void __launch_bounds__(32 * VEC_WARPS * (KEPT ? VEC_WARPS : 1)) k_linear_rows(const VecParams p) {
   using L = Elem<TYPE>;
   using T = typename L::T;
   constexpr int E = VEC ? L::E : 1;
-  __shared__ float s[VEC_WARPS][R * W_ROWS];
+  __shared__ float s[VEC_WARPS * (KEPT ? VEC_WARPS : 1)][R * W_ROWS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % p.parts;
-  const int per_block = VEC_WARPS / p.parts * W_ROWS;
+  const int per_block = KEPT ? VEC_WARPS * W_ROWS : VEC_WARPS / p.parts * W_ROWS;
+  static_assert(VEC_WARPS * W_ROWS == LIPZ_BLOCK, "a block of a checkpoint");
   const int64_t g = blockIdx.y, n0 = (int64_t)blockIdx.x * per_block + warp / p.parts * W_ROWS;
   const T* x = (const T*)p.x.data + g * p.x.group;
   const T* w = (const T*)p.w.data + g * p.w.group;
@@ -138,13 +140,14 @@ __global__ void __launch_bounds__(32 * VEC_WARPS) k_linear_rows(const VecParams 
       if (lane == 0) s[warp][r * W_ROWS + j] = acc[j][r];
     }
   __syncthreads();
-  for (int i = threadIdx.x; i < per_block * p.rows; i += 32 * VEC_WARPS) {
+  for (int i = threadIdx.x; i < per_block * p.rows; i += blockDim.x) {
     const int c = i % per_block, r = i / per_block;
     const int64_t n = (int64_t)blockIdx.x * per_block + c;
-    if (n >= p.n) continue;
+    if (n >= p.n && !KEPT) continue;
     float u = 0.f;
     for (int q = 0; q < p.parts; ++q) u += s[c / W_ROWS * p.parts + q][r * W_ROWS + c % W_ROWS];
-    finish(p.e, g, r, n, u);
+    if constexpr (KEPT) finish_kept(p.e, g, r, n, n < p.n, u);
+    else finish(p.e, g, r, n, u);
   }
 }
 
@@ -170,12 +173,18 @@ bool few_rows(const lipz_linear_args& a) {
   return (a.rows == 1 || work <= 64 << 20) && a.groups * a.n <= 12 << 10;
 }
 
-template <int TYPE, bool VEC>
+template <int TYPE, bool VEC, bool KEPT>
 cudaError_t launch_rows(const VecParams& p, dim3 grid, cudaStream_t st) {
-  const dim3 block(32 * VEC_WARPS);
-  if (p.rows == 1) return launch_pdl(k_linear_rows<TYPE, 1, VEC>, grid, block, 0, st, p);
-  if (p.rows == 2) return launch_pdl(k_linear_rows<TYPE, 2, VEC>, grid, block, 0, st, p);
-  return launch_pdl(k_linear_rows<TYPE, 4, VEC>, grid, block, 0, st, p);
+  const dim3 block(32 * VEC_WARPS * (KEPT ? p.parts : 1));
+  if (p.rows == 1) return launch_pdl(k_linear_rows<TYPE, 1, VEC, KEPT>, grid, block, 0, st, p);
+  if (p.rows == 2) return launch_pdl(k_linear_rows<TYPE, 2, VEC, KEPT>, grid, block, 0, st, p);
+  return launch_pdl(k_linear_rows<TYPE, 4, VEC, KEPT>, grid, block, 0, st, p);
+}
+template <int TYPE>
+cudaError_t launch_rows(const VecParams& p, bool vec, dim3 grid, cudaStream_t st) {
+  if (p.e.kept.data)
+    return vec ? launch_rows<TYPE, true, true>(p, grid, st) : launch_rows<TYPE, false, true>(p, grid, st);
+  return vec ? launch_rows<TYPE, true, false>(p, grid, st) : launch_rows<TYPE, false, false>(p, grid, st);
 }
 
 cudaError_t linear_rows(const lipz_linear_args& a, const Epilogue& e, cudaStream_t st) {
@@ -187,20 +196,19 @@ cudaError_t linear_rows(const lipz_linear_args& a, const Epilogue& e, cudaStream
          a.k >= (vec ? per : 1) * 64 * parts)
     parts *= 2;
   const VecParams p{a.x, a.w, e, a.n, a.k, (int)a.rows, parts};
-  const dim3 grid((unsigned)ceil_div(a.n, VEC_WARPS / parts * W_ROWS), (unsigned)a.groups);
-  if (a.x.type == LIPZ_E4M3)
-    return vec ? launch_rows<LIPZ_E4M3, true>(p, grid, st) : launch_rows<LIPZ_E4M3, false>(p, grid, st);
-  return vec ? launch_rows<LIPZ_BF16, true>(p, grid, st) : launch_rows<LIPZ_BF16, false>(p, grid, st);
+  const int outputs = VEC_WARPS / (e.kept.data ? 1 : parts) * W_ROWS;
+  const dim3 grid((unsigned)ceil_div(a.n, outputs), (unsigned)a.groups);
+  return a.x.type == LIPZ_E4M3 ? launch_rows<LIPZ_E4M3>(p, vec, grid, st) : launch_rows<LIPZ_BF16>(p, vec, grid, st);
 }
 
-Epilogue epilogue_of(const lipz_linear_args& a) {
-  Epilogue e{a.y, a.residual, a.pre, a.x_scale, a.w_scale, a.bias, a.act, a.slope};
+Epilogue epilogue_of(const lipz_linear_args& a, const lipz_blocks& kept) {
+  Epilogue e{a.y, a.residual, a.pre, a.x_scale, a.w_scale, a.bias, a.act, a.slope, kept};
   if (a.x.type != LIPZ_E4M3) e.x_scale.data = e.w_scale.data = nullptr;
   return e;
 }
-Products product_of(const lipz_linear_args& a) {
+Products product_of(const lipz_linear_args& a, const lipz_blocks& kept) {
   return {{{{a.x.data, a.x.group, a.x.row, true}, {a.w.data, a.w.group, a.w.row, true}, a.x.type,
-            a.groups, a.rows, a.n, a.k, epilogue_of(a)}},
+            a.groups, a.rows, a.n, a.k, epilogue_of(a, kept)}},
           1};
 }
 
@@ -208,6 +216,7 @@ Products product_of(const lipz_linear_args& a) {
 // 32 vectors of columns by 8 rows at a time; the blocks after those copy operands' rows. Bound: HBM.
 struct DuArgs {
   lipz_mat dy, pre;
+  lipz_blocks kept;  // in pre's place, or data null
   bf16* du;     // [groups][rows][ldu], or null: the sums only
   float* part;  // [groups][row_blocks][n], or null: no sums
   int64_t rows, n, ldu, rows_per_block;
@@ -218,7 +227,7 @@ struct DuArgs {
 
 // ALIGNED: rows of whole 16-byte units; else 8 columns are brought from the aligned words that hold them
 // (777 x 1001 with the copies beside it: one at a time 8.6 us, so 7.9, most of it latency).
-template <bool ALIGNED>
+template <bool ALIGNED, bool KEPT>
 __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
   constexpr int E = 8;
   __shared__ float s[8][32 * E + 1];
@@ -241,6 +250,19 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constan
       for (int e = 0; e < E; ++e) v[e] = __uint_as_float(e & 1 ? ww[e >> 1] & 0xFFFF0000u : ww[e >> 1] << 16);
     }
   };
+  auto load_kept = [&](int64_t r, float* v) {
+    const int8_t* src = p.kept.data + g * p.kept.group + r * p.kept.row + c;
+    const float unit = block_unit(__ldg(p.kept.scale + g * p.kept.scale_group + r * p.kept.scale_row + (c >> 4)));
+    uint2 w;
+    if constexpr (ALIGNED) {
+      w = __ldg(reinterpret_cast<const uint2*>(src));
+    } else {
+      const uint4 b = bytes16((const uint8_t*)src, min(p.n - c, (int64_t)E));
+      w = make_uint2(b.x, b.y);
+    }
+    block_values(w.x, unit, v);
+    block_values(w.y, unit, v + 4);
+  };
   float sum[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] = 0.f;
@@ -253,7 +275,8 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constan
         load(p.dy, r, d);
         if constexpr (ACT != LIPZ_ACT_NONE) {
           float u[E];
-          load(p.pre, r, u);
+          if constexpr (KEPT) load_kept(r, u);
+          else load(p.pre, r, u);
 #pragma unroll
           for (int e = 0; e < E; ++e) d[e] *= act_slope<ACT>(u[e], p.slope);
         }
@@ -286,10 +309,12 @@ struct BackPlan {
   Products q[2];
   GemmPlan plan[2];
 };
-BackPlan back_plan(const lipz_linear_backward_args& a) {
+// kept_x, kept_pre: checkpoints in the places of x and pre, or data null.
+BackPlan back_plan(const lipz_linear_backward_args& a, const lipz_blocks& kept_x, const lipz_blocks& kept_pre) {
   BackPlan b{};
   b.vec = a.n % 8 == 0 && rows_aligned(a.dy, a.groups, a.rows, 16) &&
-          (!a.pre.data || rows_aligned(a.pre, a.groups, a.rows, 16));
+          (kept_pre.data ? rows_aligned(bytes_of(kept_pre), a.groups, a.rows, 8)
+                         : !a.pre.data || rows_aligned(a.pre, a.groups, a.rows, 16));
   // Without an activation du is dy: written where the products cannot read dy itself, unless one of them is
   // all that is wanted. (Instead of a copy for each: 8192 x 4096 -> 4097 401 -> 357 us, 144 groups of 100 x
   // 256 -> 501 55 -> 45.)
@@ -311,8 +336,10 @@ BackPlan back_plan(const lipz_linear_backward_args& a) {
   const int64_t dg = b.need_du ? a.rows * b.ldu : a.dy.group, dr = b.need_du ? b.ldu : a.dy.row;
   const Gemm dx{{d, dg, dr, true}, {a.w.data, a.w.group, a.w.row, false}, LIPZ_BF16, a.groups, a.rows,
                 a.k, a.n, {a.dx}};
-  const Gemm dw{{d, dg, dr, false}, {a.x.data, a.x.group, a.x.row, false}, LIPZ_BF16, a.groups, a.n,
-                a.k, a.rows, {a.dw}};
+  Operand x{a.x.data, a.x.group, a.x.row, false};
+  if (kept_x.data)
+    x = {kept_x.data, kept_x.group, kept_x.row, false, kept_x.scale, kept_x.scale_group, kept_x.scale_row};
+  const Gemm dw{{d, dg, dr, false}, x, LIPZ_BF16, a.groups, a.n, a.k, a.rows, {a.dw}};
   // bf16 results run as planned for both, whether or not both are asked for, so that one's values do not
   // depend on the other; fp32 results are planned by themselves, and so are products of which one is so long
   // that its shape would slow the other (16392 x 4096 -> 4096: 708 us in one launch, 662 in two)
@@ -344,15 +371,15 @@ BackPlan back_plan(const lipz_linear_backward_args& a) {
 
 }  // namespace
 
-uint64_t linear_workspace(const lipz_linear_args& a) {
-  return a.groups == 0 || a.rows == 0 || few_rows(a) ? 0 : plan_products(product_of(a)).bytes;
+uint64_t linear_workspace(const lipz_linear_args& a, const lipz_blocks& kept) {
+  return a.groups == 0 || a.rows == 0 || few_rows(a) ? 0 : plan_products(product_of(a, kept)).bytes;
 }
 
-cudaError_t linear(const lipz_linear_args& a, cudaStream_t st, uint64_t* need) {
+cudaError_t linear(const lipz_linear_args& a, const lipz_blocks& kept, cudaStream_t st, uint64_t* need) {
   *need = 0;
   if (a.groups == 0 || a.rows == 0) return cudaSuccess;
-  if (few_rows(a)) return linear_rows(a, epilogue_of(a), st);
-  Products q = product_of(a);
+  if (few_rows(a)) return linear_rows(a, epilogue_of(a, kept), st);
+  Products q = product_of(a, kept);
   const GemmPlan plan = plan_products(q);
   *need = plan.bytes;
   if (!space_given(a.workspace, a.workspace_bytes, *need)) return cudaSuccess;
@@ -362,9 +389,13 @@ cudaError_t linear(const lipz_linear_args& a, cudaStream_t st, uint64_t* need) {
   return e != cudaSuccess ? e : run_products(plan, q, a.workspace, nullptr, st);
 }
 
-uint64_t linear_backward_workspace(const lipz_linear_backward_args& a) { return back_plan(a).bytes; }
+uint64_t linear_backward_workspace(const lipz_linear_backward_args& a, const lipz_blocks& kept_x,
+                                   const lipz_blocks& kept_pre) {
+  return back_plan(a, kept_x, kept_pre).bytes;
+}
 
-cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st, uint64_t* need) {
+cudaError_t linear_backward(const lipz_linear_backward_args& a, const lipz_blocks& kept_x,
+                            const lipz_blocks& kept_pre, cudaStream_t st, uint64_t* need) {
   *need = 0;
   if (a.groups == 0) return cudaSuccess;
   if (a.rows == 0) {  // sums over no rows
@@ -380,7 +411,7 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st,
     }
     return e;
   }
-  BackPlan b = back_plan(a);
+  BackPlan b = back_plan(a, kept_x, kept_pre);
   *need = b.bytes;
   if (!space_given(a.workspace, a.workspace_bytes, *need)) return cudaSuccess;
   bf16* du = b.need_du ? (bf16*)a.workspace : nullptr;
@@ -394,11 +425,15 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st,
   cudaError_t e;
   if (du || part) {
     const int64_t cols = ceil_div(a.n, 256), blocks = cols * b.blocks * a.groups;
-    const DuArgs p{a.dy, a.pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope,
+    const DuArgs p{a.dy, a.pre, kept_pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope,
                    (int)cols, (int)b.blocks, (int)blocks};
     const dim3 grid((unsigned)(blocks + jobs.blocks));
-    e = b.vec ? launch_pdl(k_du<true>, grid, dim3(256), 0, st, p, jobs)
-              : launch_pdl(k_du<false>, grid, dim3(256), 0, st, p, jobs);
+    if (kept_pre.data)
+      e = b.vec ? launch_pdl(k_du<true, true>, grid, dim3(256), 0, st, p, jobs)
+                : launch_pdl(k_du<false, true>, grid, dim3(256), 0, st, p, jobs);
+    else
+      e = b.vec ? launch_pdl(k_du<true, false>, grid, dim3(256), 0, st, p, jobs)
+                : launch_pdl(k_du<false, false>, grid, dim3(256), 0, st, p, jobs);
   } else {
     e = run_copies(jobs, st);
   }

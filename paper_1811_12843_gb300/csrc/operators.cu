@@ -1,5 +1,5 @@
 // C ABI of the residual-block operators: every argument that the host can check is checked here, then
-// the kernels of op_norm.cu, op_linear.cu and op_gemm.cu are launched.
+// the kernels of op_norm.cu, op_layernorm.cu, op_checkpoint.cu, op_linear.cu and op_gemm.cu are launched.
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
@@ -138,6 +138,13 @@ struct Check {
     else if (groups > 1 && v.group < (out ? n : 0)) fail_mat(name, "has a group stride that is too small");
     return rc == LIPZ_OK;
   }
+  bool blocks(const lipz_blocks& b, const char* name, const char* scale, int64_t nrows, int64_t cols, bool out,
+              bool optional = false) {
+    if (rc != LIPZ_OK) return false;
+    if (!b.data && !b.scale && optional) return true;
+    return mat(ops::bytes_of(b), name, nrows, cols, 1 << LIPZ_E4M3, out) &&
+           mat(ops::scales_of(b), scale, nrows, ops::ceil_div(cols, LIPZ_BLOCK), 1 << LIPZ_E4M3, out);
+  }
   bool space(const void* p, uint64_t have, uint64_t need) {
     if (rc != LIPZ_OK || ops::space_given(p, have, need)) return rc == LIPZ_OK;
     if (!p || have < need)
@@ -245,6 +252,103 @@ int check(const lipz_linear_backward_args* a) {
   return c.rc;
 }
 
+int check(const lipz_layernorm_args* a) {
+  Check c{"lipz_layernorm"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, LIPZ_NORM_MAX_DIM, "dim")) return c.rc;
+  c.want(a->eps >= 0.f, "eps must not be negative");
+  c.mat(a->x, "x", a->rows, a->dim, F32 | B16, false);
+  const int t = 1 << a->x.type;
+  c.mat(a->residual, "residual", a->rows, a->dim, t, false, true);
+  c.mat(a->sum, "sum", a->rows, a->dim, t, true, true);
+  c.mat(a->y, "y", a->rows, a->dim, t | F8, true);
+  c.vec(a->weight, "weight", a->dim, false);
+  c.vec(a->bias, "bias", a->dim, false, true);
+  if (a->y.data && a->y.type == LIPZ_E4M3) c.vec(a->scale, "scale", a->rows, true);
+  c.vec(a->mean, "mean", a->rows, true, true);
+  c.vec(a->rstd, "rstd", a->rows, true, true);
+  c.blocks(a->kept, "kept", "kept's scale", a->rows, a->dim, true, true);
+  c.want(!a->kept.data || !a->residual.data || a->sum.data, "kept needs sum beside a residual");
+  return c.rc;
+}
+
+int check(const lipz_layernorm_backward_args* a) {
+  Check c{"lipz_layernorm_backward"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, LIPZ_NORM_MAX_DIM, "dim")) return c.rc;
+  c.mat(a->dy, "dy", a->rows, a->dim, F32 | B16, false);
+  const int t = 1 << a->dy.type;
+  c.want(!a->s.data || !a->kept.data, "s is given twice, as a matrix and as a checkpoint");
+  if (a->kept.data) c.blocks(a->kept, "kept", "kept's scale", a->rows, a->dim, false);
+  else c.mat(a->s, "s", a->rows, a->dim, t, false);
+  c.mat(a->dsum, "dsum", a->rows, a->dim, t, false, true);
+  c.mat(a->dx, "dx", a->rows, a->dim, t, true);
+  c.vec(a->weight, "weight", a->dim, false);
+  c.vec(a->mean, "mean", a->rows, false);
+  c.vec(a->rstd, "rstd", a->rows, false);
+  c.vec(a->dweight, "dweight", a->dim, true, true);
+  c.vec(a->dbias, "dbias", a->dim, true, true);
+  return c.rc;
+}
+
+int check(const lipz_checkpoint_rows_args* a) {
+  Check c{"lipz_checkpoint_rows"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, MAX_EXTENT, "dim")) return c.rc;
+  c.mat(a->x, "x", a->rows, a->dim, F32 | B16, false);
+  c.blocks(a->c, "c", "c's scale", a->rows, a->dim, true);
+  return c.rc;
+}
+
+int check(const lipz_restore_rows_args* a) {
+  Check c{"lipz_restore_rows"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->groups, c.rows = a->rows;
+  if (!c.extents() || !c.extent(a->dim, 1, MAX_EXTENT, "dim")) return c.rc;
+  c.extent(a->act, LIPZ_ACT_NONE, LIPZ_ACT_SILU, "act");
+  c.blocks(a->c, "c", "c's scale", a->rows, a->dim, false);
+  c.mat(a->y, "y", a->rows, a->dim, F32 | B16, true);
+  return c.rc;
+}
+
+int check(const lipz_linear_checkpoint_args* a) {
+  Check c{"lipz_linear_checkpoint"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  if (int rc = check(&a->call)) return rc;
+  c.groups = a->call.groups, c.rows = a->call.rows;
+  c.want(!a->call.pre.data, "pre is given twice, as a matrix and as a checkpoint");
+  c.blocks(a->pre, "pre", "pre's scale", a->call.rows, a->call.n, true);
+  return c.rc;
+}
+
+// The call with the matrices that its checkpoints stand in for: where those stand, for its checks.
+lipz_linear_backward_args with_places(const lipz_linear_backward_checkpoint_args& a) {
+  lipz_linear_backward_args b = a.call;
+  auto place = [](const lipz_blocks& c, int64_t cols) {
+    return lipz_mat{(void*)((uintptr_t)c.data & ~(uintptr_t)1), 0, cols, LIPZ_BF16, 0};
+  };
+  if (a.x.data) b.x = place(a.x, b.k);
+  if (a.pre.data) b.pre = place(a.pre, b.n);
+  return b;
+}
+
+int check(const lipz_linear_backward_checkpoint_args* a) {
+  Check c{"lipz_linear_backward_checkpoint"};
+  if (!struct_ok(a, c.call, &c.rc)) return c.rc;
+  c.groups = a->call.groups, c.rows = a->call.rows;
+  c.want(!a->x.data || !a->call.x.data, "x is given twice, as a matrix and as a checkpoint");
+  c.want(!a->pre.data || !a->call.pre.data, "pre is given twice, as a matrix and as a checkpoint");
+  if (c.rc) return c.rc;
+  const lipz_linear_backward_args b = with_places(*a);
+  if (int rc = check(&b)) return rc;
+  c.blocks(a->x, "x", "x's scale", b.rows, b.k, false, true);
+  c.blocks(a->pre, "pre", "pre's scale", b.rows, b.n, false, true);
+  return c.rc;
+}
+
 // ---- outputs that share memory with other arguments: a kernel would read what it has already overwritten
 
 // `groups` times `rows` rows of `width` bytes, `group` and `row` bytes apart.
@@ -315,7 +419,7 @@ struct Overlap {
     Region r;
     unsigned places;  // of an output: the inputs whose own place it may have
   };
-  Part in[6], out[4];
+  Part in[8], out[6];
   int ins = 0, outs = 0;
 
   Overlap(const char* call_, int64_t groups_) : call(call_), groups(groups_) {}
@@ -329,6 +433,14 @@ struct Overlap {
     return 1u << ins++;
   }
   void input(const char* name, const lipz_vec& v, int64_t n) { in[ins++] = {name, region(v, n), 0u}; }
+  void input(const char* name, const lipz_blocks& b, int64_t rows, int64_t cols) {
+    input(name, ops::bytes_of(b), rows, cols);
+    input(name, ops::scales_of(b), rows, ops::ceil_div(cols, LIPZ_BLOCK));
+  }
+  void output(const char* name, const lipz_blocks& b, int64_t rows, int64_t cols) {
+    output(name, ops::bytes_of(b), rows, cols);
+    output(name, ops::scales_of(b), rows, ops::ceil_div(cols, LIPZ_BLOCK));
+  }
   void output(const char* name, const lipz_mat& m, int64_t rows, int64_t cols, unsigned places = 0) {
     out[outs++] = {name, region(m, rows, cols), places};
   }
@@ -375,7 +487,53 @@ int overlap(const lipz_quantize_rows_args& a) {
   o.output("scale", a.scale, a.rows);
   return o.result();
 }
-int overlap(const lipz_linear_args& a) {
+int overlap(const lipz_layernorm_args& a) {
+  Overlap o{"lipz_layernorm", a.groups};
+  const unsigned own = o.input("x", a.x, a.rows, a.dim) | o.input("residual", a.residual, a.rows, a.dim);
+  o.input("weight", a.weight, a.dim);
+  o.input("bias", a.bias, a.dim);
+  o.output("sum", a.sum, a.rows, a.dim, own);
+  o.output("y", a.y, a.rows, a.dim, own);
+  if (a.y.type == LIPZ_E4M3) o.output("scale", a.scale, a.rows);
+  o.output("mean", a.mean, a.rows);
+  o.output("rstd", a.rstd, a.rows);
+  if (int rc = o.result()) return rc;
+  // the checkpoint against all of those
+  Overlap k{"lipz_layernorm", a.groups};
+  k.input("x", a.x, a.rows, a.dim), k.input("residual", a.residual, a.rows, a.dim);
+  k.input("weight", a.weight, a.dim), k.input("bias", a.bias, a.dim);
+  k.input("sum", a.sum, a.rows, a.dim), k.input("y", a.y, a.rows, a.dim);
+  k.input("mean", a.mean, a.rows), k.input("rstd", a.rstd, a.rows);
+  k.output("kept", a.kept, a.rows, a.dim);
+  if (a.y.type == LIPZ_E4M3) k.output("scale", a.scale, a.rows);
+  return k.result();
+}
+int overlap(const lipz_layernorm_backward_args& a) {
+  Overlap o{"lipz_layernorm_backward", a.groups};
+  const unsigned own = o.input("dy", a.dy, a.rows, a.dim) | o.input("s", a.s, a.rows, a.dim) |
+                       o.input("dsum", a.dsum, a.rows, a.dim);
+  o.input("weight", a.weight, a.dim);
+  o.input("mean", a.mean, a.rows);
+  o.input("rstd", a.rstd, a.rows);
+  if (a.kept.data) o.input("kept", a.kept, a.rows, a.dim);
+  o.output("dx", a.dx, a.rows, a.dim, own);
+  o.output("dweight", a.dweight, a.dim);
+  o.output("dbias", a.dbias, a.dim);
+  return o.result();
+}
+int overlap(const lipz_checkpoint_rows_args& a) {
+  Overlap o{"lipz_checkpoint_rows", a.groups};
+  o.input("x", a.x, a.rows, a.dim);
+  o.output("c", a.c, a.rows, a.dim);
+  return o.result();
+}
+int overlap(const lipz_restore_rows_args& a) {
+  Overlap o{"lipz_restore_rows", a.groups};
+  o.input("c", a.c, a.rows, a.dim);
+  o.output("y", a.y, a.rows, a.dim);
+  return o.result();
+}
+int overlap(const lipz_linear_args& a, const lipz_blocks* kept = nullptr) {
   Overlap o{"lipz_linear", a.groups};
   const unsigned own = o.input("residual", a.residual, a.rows, a.n);
   o.input("x", a.x, a.rows, a.k);
@@ -386,15 +544,18 @@ int overlap(const lipz_linear_args& a) {
     o.input("w_scale", a.w_scale, a.n);
   }
   o.output("y", a.y, a.rows, a.n, own);
-  o.output("pre", a.pre, a.rows, a.n);
+  if (kept) o.output("pre", *kept, a.rows, a.n);
+  else o.output("pre", a.pre, a.rows, a.n);
   return o.result();
 }
-int overlap(const lipz_linear_backward_args& a) {
+int overlap(const lipz_linear_backward_args& a, const lipz_blocks* x = nullptr, const lipz_blocks* pre = nullptr) {
   Overlap o{"lipz_linear_backward", a.groups};
   o.input("dy", a.dy, a.rows, a.n);
-  if (a.dw.data) o.input("x", a.x, a.rows, a.k);
+  if (a.dw.data && x && x->data) o.input("x", *x, a.rows, a.k);
+  else if (a.dw.data) o.input("x", a.x, a.rows, a.k);
   if (a.dx.data) o.input("w", a.w, a.n, a.k);
-  if (a.act != LIPZ_ACT_NONE) o.input("pre", a.pre, a.rows, a.n);
+  if (a.act != LIPZ_ACT_NONE && pre && pre->data) o.input("pre", *pre, a.rows, a.n);
+  else if (a.act != LIPZ_ACT_NONE) o.input("pre", a.pre, a.rows, a.n);
   o.output("dx", a.dx, a.rows, a.k);
   o.output("dw", a.dw, a.n, a.k);
   o.output("db", a.db, a.n);
@@ -438,7 +599,7 @@ int lipz_quantize_rows(const lipz_quantize_rows_args* a, void* stream) {
 int lipz_linear_workspace(const lipz_linear_args* a, uint64_t* bytes) {
   if (int rc = check(a)) return rc;
   if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_linear_workspace: bytes is null");
-  *bytes = ops::linear_workspace(*a);
+  *bytes = ops::linear_workspace(*a, {});
   return LIPZ_OK;
 }
 
@@ -446,10 +607,10 @@ int lipz_linear(const lipz_linear_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear", a->groups, a->rows};
   if (int rc = overlap(*a))
-    return c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a)) ? rc : c.rc;
+    return c.space(a->workspace, a->workspace_bytes, ops::linear_workspace(*a, {})) ? rc : c.rc;
   if (int rc = take_timeout(c.call)) return rc;
   uint64_t need;
-  const cudaError_t e = ops::linear(*a, (cudaStream_t)stream, &need);
+  const cudaError_t e = ops::linear(*a, {}, (cudaStream_t)stream, &need);
   if (!c.space(a->workspace, a->workspace_bytes, need)) return c.rc;
   return finish(c.call, e);
 }
@@ -457,7 +618,7 @@ int lipz_linear(const lipz_linear_args* a, void* stream) {
 int lipz_linear_backward_workspace(const lipz_linear_backward_args* a, uint64_t* bytes) {
   if (int rc = check(a)) return rc;
   if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_linear_backward_workspace: bytes is null");
-  *bytes = ops::linear_backward_workspace(*a);
+  *bytes = ops::linear_backward_workspace(*a, {}, {});
   return LIPZ_OK;
 }
 
@@ -465,11 +626,84 @@ int lipz_linear_backward(const lipz_linear_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_linear_backward", a->groups, a->rows};
   if (int rc = overlap(*a))
-    return c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a)) ? rc : c.rc;
+    return c.space(a->workspace, a->workspace_bytes, ops::linear_backward_workspace(*a, {}, {})) ? rc : c.rc;
   if (int rc = take_timeout(c.call)) return rc;
   uint64_t need;
-  const cudaError_t e = ops::linear_backward(*a, (cudaStream_t)stream, &need);
+  const cudaError_t e = ops::linear_backward(*a, {}, {}, (cudaStream_t)stream, &need);
   if (!c.space(a->workspace, a->workspace_bytes, need)) return c.rc;
+  return finish(c.call, e);
+}
+
+int lipz_layernorm(const lipz_layernorm_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  if (int rc = overlap(*a)) return rc;
+  if (int rc = take_timeout("lipz_layernorm")) return rc;
+  return finish("lipz_layernorm", ops::layernorm(*a, (cudaStream_t)stream));
+}
+
+int lipz_layernorm_backward_workspace(const lipz_layernorm_backward_args* a, uint64_t* bytes) {
+  if (int rc = check(a)) return rc;
+  if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_layernorm_backward_workspace: bytes is null");
+  *bytes = ops::layernorm_backward_workspace(*a);
+  return LIPZ_OK;
+}
+
+int lipz_layernorm_backward(const lipz_layernorm_backward_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  Check c{"lipz_layernorm_backward", a->groups, a->rows};
+  if (!c.space(a->workspace, a->workspace_bytes, ops::layernorm_backward_workspace(*a))) return c.rc;
+  if (int rc = overlap(*a)) return rc;
+  if (int rc = take_timeout(c.call)) return rc;
+  return finish(c.call, ops::layernorm_backward(*a, (cudaStream_t)stream));
+}
+
+int lipz_checkpoint_rows(const lipz_checkpoint_rows_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  if (int rc = overlap(*a)) return rc;
+  if (int rc = take_timeout("lipz_checkpoint_rows")) return rc;
+  return finish("lipz_checkpoint_rows", ops::checkpoint_rows(*a, (cudaStream_t)stream));
+}
+
+int lipz_restore_rows(const lipz_restore_rows_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  if (int rc = overlap(*a)) return rc;
+  if (int rc = take_timeout("lipz_restore_rows")) return rc;
+  return finish("lipz_restore_rows", ops::restore_rows(*a, (cudaStream_t)stream));
+}
+
+int lipz_linear_checkpoint_workspace(const lipz_linear_checkpoint_args* a, uint64_t* bytes) {
+  if (int rc = check(a)) return rc;
+  if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_linear_checkpoint_workspace: bytes is null");
+  *bytes = ops::linear_workspace(a->call, a->pre);
+  return LIPZ_OK;
+}
+
+int lipz_linear_checkpoint(const lipz_linear_checkpoint_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  Check c{"lipz_linear_checkpoint", a->call.groups, a->call.rows};
+  if (int rc = overlap(a->call, &a->pre)) return rc;
+  if (int rc = take_timeout(c.call)) return rc;
+  uint64_t need;
+  const cudaError_t e = ops::linear(a->call, a->pre, (cudaStream_t)stream, &need);
+  if (!c.space(a->call.workspace, a->call.workspace_bytes, need)) return c.rc;
+  return finish(c.call, e);
+}
+
+int lipz_linear_backward_checkpoint_workspace(const lipz_linear_backward_checkpoint_args* a, uint64_t* bytes) {
+  if (int rc = check(a)) return rc;
+  if (!bytes) return fail(LIPZ_ERR_INVALID, "lipz_linear_backward_checkpoint_workspace: bytes is null");
+  *bytes = ops::linear_backward_workspace(a->call, a->x, a->pre);
+  return LIPZ_OK;
+}
+
+int lipz_linear_backward_checkpoint(const lipz_linear_backward_checkpoint_args* a, void* stream) {
+  if (int rc = check(a)) return rc;
+  Check c{"lipz_linear_backward_checkpoint", a->call.groups, a->call.rows};
+  if (int rc = overlap(a->call, &a->x, &a->pre)) return rc;
+  if (int rc = take_timeout(c.call)) return rc;
+  uint64_t need;
+  const cudaError_t e = ops::linear_backward(a->call, a->x, a->pre, (cudaStream_t)stream, &need);
+  if (!c.space(a->call.workspace, a->call.workspace_bytes, need)) return c.rc;
   return finish(c.call, e);
 }
 

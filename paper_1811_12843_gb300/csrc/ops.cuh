@@ -208,6 +208,58 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 __device__ __forceinline__ uint64_t both(float a) { return pack2(a, a); }
 
+// ---- checkpoints: 16 columns share a power of two
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// A block's byte, and what its elements are multiplied by, from its largest magnitude's bits (as integers,
+// magnitudes keep their order, with infinity above every number and NaN above that). 127.5 is 2^6 times 1 + 127/128:
+// from there on 2^16, added to the bits, carries into the exponent. Of a block with an infinity or NaN the multiplier
+// is NaN.
+struct BlockScale {
+  float inv;
+  uint32_t byte;
+};
+__device__ __forceinline__ BlockScale block_scale(uint32_t top) {
+  const uint32_t byte = max((top + 0x10000u) >> 23, 7u) - 6u;
+  if (top >= 0x7F800000u) return {__uint_as_float(0x7FC00000u), 255u};
+  return {__uint_as_float((254u - byte) << 23), byte};
+}
+// A value's multiple of the power of two, to nearest even, in the low byte: 1.5 2^23 + v inv has no fraction bits.
+__device__ __forceinline__ uint32_t block_multiple(float v, float inv) {
+  return __float_as_uint(fmaf(v, inv, 12582912.f));
+}
+__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// E multiples of 4 or more, in words.
+template <int E>
+__device__ __forceinline__ void block_multiples(const float* v, float inv, uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < E; i += 4) {
+    const float2 a = unpack2(fma2(pack2(v[i], v[i + 1]), both(inv), both(12582912.f)));
+    const float2 b = unpack2(fma2(pack2(v[i + 2], v[i + 3]), both(inv), both(12582912.f)));
+    w[i / 4] = pack_bytes(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+  }
+}
+// And back: the power of two of a byte (NaN of 255), and a word's four values.
+__device__ __forceinline__ float block_unit(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);
+}
+// (q + 128 in the low byte of 2^23 is the number 2^23 + 128 + q)
+__device__ __forceinline__ void block_values(uint32_t w, float unit, float* v) {
+  const uint32_t u = w ^ 0x80808080u;
+  const uint64_t off = both(-8388736.f), by = both(unit);
+  const float2 a = unpack2(mul2(add2(pack2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440)),
+                                           __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7441))), off), by));
+  const float2 b = unpack2(mul2(add2(pack2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7442)),
+                                           __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7443))), off), by));
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+// Two such values as bf16, which holds them: the upper halves.
+__device__ __forceinline__ uint32_t block_pair(float lo, float hi) {
+  return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+}
+
 // act_value of two values, in place. Without EXACT the result is good to 2^-16, for results that are then
 // rounded to bf16: tanh takes x - x^3/3 below 1/64, where its other form has lost 2^-17.
 template <int ACT, bool EXACT>
@@ -274,11 +326,31 @@ __device__ __forceinline__ uint4 bytes16(const uint8_t* p, int64_t n) {
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a warp.
+// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a warp; of a
+// checkpoint's row (p.bytes: its columns) the bf16 values that it stands for, 16 at a time.
 __device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
-  const int64_t g = r / p.rows;
-  const uint8_t* s = p.src + g * p.group + (r - g * p.rows) * p.ld;
+  const int64_t g = r / p.rows, at = r - g * p.rows;
+  const uint8_t* s = p.src + g * p.group + at * p.ld;
   uint4* d = (uint4*)p.dst + r * p.units;
+  if (p.scale) {
+    const uint8_t* scale = p.scale + g * p.scale_group + at * p.scale_ld;
+#pragma unroll 2
+    for (int64_t u = threadIdx.x & 31; 2 * u < p.units; u += 32) {
+      const uint4 q = bytes16(s + u * 16, p.bytes - u * 16);
+      const float unit = block_unit(__ldg(scale + u));
+      const uint32_t qq[4] = {q.x, q.y, q.z, q.w};
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[4];
+        block_values(qq[i], unit, v);
+        w[2 * i] = block_pair(v[0], v[1]), w[2 * i + 1] = block_pair(v[2], v[3]);
+      }
+      d[2 * u] = make_uint4(w[0], w[1], w[2], w[3]);
+      if (2 * u + 1 < p.units) d[2 * u + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    return;
+  }
 #pragma unroll 2
   for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) d[u] = bytes16(s + u * 16, p.bytes - u * 16);
 }
@@ -294,14 +366,15 @@ __device__ __forceinline__ void copy_rows(const CopyJobs& jobs, int64_t b) {
     b -= blocks;
   }
 }
-// The epilogue of element (m, n) of group g, from its sum u.
-__device__ __forceinline__ void finish(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
+// The epilogue of element (m, n) of group g, from its sum: u, and the results from it.
+__device__ __forceinline__ float pre_activation(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
   const float b = e.bias.data ? e.bias.data[g * e.bias.group + n] : 0.f;
   // (one scale after the other, as for many rows: their product may leave fp32's range where the result does not)
   if (e.w_scale.data)
-    u = fmaf(u * e.x_scale.data[g * e.x_scale.group + m], e.w_scale.data[g * e.w_scale.group + n], b);
-  else
-    u += b;
+    return fmaf(u * e.x_scale.data[g * e.x_scale.group + m], e.w_scale.data[g * e.w_scale.group + n], b);
+  return u + b;
+}
+__device__ __forceinline__ void finish_from(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
   if (e.pre.data)
     ((bf16*)e.pre.data)[g * e.pre.group + m * e.pre.row + n] = __float2bfloat16_rn(u);
   with_act(e.act, [&](auto act) { u = act_value<decltype(act)::value>(u, e.slope); });
@@ -314,6 +387,22 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t g, int64_t m, 
     if (e.residual.data) u += __bfloat162float(((const bf16*)e.residual.data)[ro]);
     ((bf16*)e.y.data)[yo] = __float2bfloat16_rn(u);
   }
+}
+__device__ __forceinline__ void finish(const Epilogue& e, int64_t g, int64_t m, int64_t n, float u) {
+  finish_from(e, g, m, n, pre_activation(e, g, m, n, u));
+}
+// The same with u kept as a checkpoint, by the 16 lanes of a half-warp that hold a block's columns (live: n is one).
+__device__ __forceinline__ void finish_kept(const Epilogue& e, int64_t g, int64_t m, int64_t n, bool live, float u) {
+  const int lane = threadIdx.x & 31;
+  if (live) u = pre_activation(e, g, m, n, u);
+  uint32_t top = live ? magnitude(u) : 0u;
+#pragma unroll
+  for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFu << (lane & 16), top, o));
+  if (!live) return;
+  const BlockScale s = block_scale(top);
+  e.kept.data[g * e.kept.group + m * e.kept.row + n] = (int8_t)block_multiple(u, s.inv);
+  if (lane % 16 == 0) e.kept.scale[g * e.kept.scale_group + m * e.kept.scale_row + (n >> 4)] = (uint8_t)s.byte;
+  finish_from(e, g, m, n, u);
 }
 
 }  // namespace ops

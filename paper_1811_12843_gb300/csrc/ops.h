@@ -1,5 +1,6 @@
 // Internal interface of the residual-block operators (include/lipz.h): operators.cu checks a call's
-// arguments and launches the kernels of op_norm.cu, op_linear.cu and op_gemm.cu.
+// arguments and launches the kernels of op_norm.cu, op_layernorm.cu, op_checkpoint.cu, op_linear.cu and
+// op_gemm.cu.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -26,6 +27,10 @@ inline bool rows_aligned(const lipz_vec& v, int64_t groups, int bytes) {
   return bits % bytes == 0;
 }
 
+// A checkpoint's bytes and its scales as matrices (of any 8-bit type).
+inline lipz_mat bytes_of(const lipz_blocks& b) { return {b.data, b.group, b.row, LIPZ_E4M3, 0}; }
+inline lipz_mat scales_of(const lipz_blocks& b) { return {b.scale, b.scale_group, b.scale_row, LIPZ_E4M3, 0}; }
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // SMs of the current device.
@@ -49,10 +54,19 @@ inline bool space_given(const void* p, uint64_t have, uint64_t need) {
 }
 // *need: the scratch memory; nothing is launched where the call does not have it. (The plan that tells is the
 // launch's own. A caller that first asks for the size, as the torch binding does, has the plan made twice.)
-uint64_t linear_workspace(const lipz_linear_args& a);
-cudaError_t linear(const lipz_linear_args& a, cudaStream_t st, uint64_t* need);
-uint64_t linear_backward_workspace(const lipz_linear_backward_args& a);
-cudaError_t linear_backward(const lipz_linear_backward_args& a, cudaStream_t st, uint64_t* need);
+// kept: pre as a checkpoint; kept_x, kept_pre: checkpoints in the places of x and pre (data null: none)
+uint64_t linear_workspace(const lipz_linear_args& a, const lipz_blocks& kept);
+cudaError_t linear(const lipz_linear_args& a, const lipz_blocks& kept, cudaStream_t st, uint64_t* need);
+uint64_t linear_backward_workspace(const lipz_linear_backward_args& a, const lipz_blocks& kept_x,
+                                   const lipz_blocks& kept_pre);
+cudaError_t linear_backward(const lipz_linear_backward_args& a, const lipz_blocks& kept_x,
+                            const lipz_blocks& kept_pre, cudaStream_t st, uint64_t* need);
+
+cudaError_t layernorm(const lipz_layernorm_args& a, cudaStream_t st);
+uint64_t layernorm_backward_workspace(const lipz_layernorm_backward_args& a);
+cudaError_t layernorm_backward(const lipz_layernorm_backward_args& a, cudaStream_t st);
+cudaError_t checkpoint_rows(const lipz_checkpoint_rows_args& a, cudaStream_t st);
+cudaError_t restore_rows(const lipz_restore_rows_args& a, cudaStream_t st);
 
 }  // namespace ops
 }  // namespace lipz

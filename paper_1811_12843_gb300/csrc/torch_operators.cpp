@@ -9,6 +9,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <c10/core/InferenceMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -92,6 +93,10 @@ struct Call {
   // The tensor that gives the call its device, groups, rows and columns.
   lipz_mat first(PyObject* o, const char* what, int types) {
     const Tensor& t = tensor(o, what);
+    first(t, what);
+    return view(t, what, types);
+  }
+  void first(const Tensor& t, const char* what) {
     const auto s = t.sizes();
     if (s.size() != 2 && s.size() != 3)
       refuse(std::string(what) + " must be [rows, columns] or [groups, rows, columns]");
@@ -99,7 +104,6 @@ struct Call {
     if (grouped) groups = s[0];
     rows = s[s.size() - 2], cols = s[s.size() - 1];
     device = t.get_device();
-    return view(t, what, types);
   }
   const Tensor& like(PyObject* o, const char* what, const Shape& shape) const {
     const Tensor& t = tensor(o, what);
@@ -150,6 +154,33 @@ struct Call {
     t = empty(vector(n), F32);
     return {(float*)t.mutable_data_ptr(), n};
   }
+  // A checkpoint: a tuple of its data and its scales.
+  static bool is_checkpoint(PyObject* o) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 2; }
+  lipz_blocks blocks_of(const Tensor& q, const Tensor& s, const std::string& what) const {
+    if (q.scalar_type() != ScalarType::Char || s.scalar_type() != ScalarType::Byte)
+      refuse(what + ": a checkpoint is of torch.int8, and its scale of torch.uint8");
+    if (!adjacent(q) || !adjacent(s)) refuse(what + ": columns must be adjacent");
+    const auto a = q.strides(), b = s.strides();
+    return {(int8_t*)q.const_data_ptr(), a.size() == 3 ? a[0] : 0, a[a.size() - 2],
+            (uint8_t*)s.const_data_ptr(), b.size() == 3 ? b[0] : 0, b[b.size() - 2]};
+  }
+  lipz_blocks blocks(PyObject* o, const char* what, int64_t r, int64_t c) const {
+    const std::string scale = std::string(what) + "'s scale";
+    const Tensor& q = like(PyTuple_GET_ITEM(o, 0), what, matrix(r, c));
+    return blocks_of(q, like(PyTuple_GET_ITEM(o, 1), scale.c_str(), matrix(r, (c + LIPZ_BLOCK - 1) / LIPZ_BLOCK)),
+                     what);
+  }
+  // Rows begin whole blocks apart.
+  lipz_blocks fresh(Tensor& q, Tensor& s, int64_t r, int64_t c) const {
+    const int64_t n = (c + LIPZ_BLOCK - 1) / LIPZ_BLOCK, row = n * LIPZ_BLOCK;
+    const int64_t size[3] = {groups, r, c}, stride[3] = {r * row, row, 1};
+    const int skip = grouped ? 0 : 1;
+    q = at::empty_strided(at::IntArrayRef(size + skip, 3 - skip), at::IntArrayRef(stride + skip, 3 - skip),
+                          at::TensorOptions().dtype(ScalarType::Char).device(
+                              at::Device(at::kCUDA, (c10::DeviceIndex)device)));
+    s = empty(matrix(r, n), ScalarType::Byte);
+    return {(int8_t*)q.mutable_data_ptr(), r * row, row, (uint8_t*)s.mutable_data_ptr(), r * n, n};
+  }
   void require(PyObject* o, const char* what) const {
     if (o == Py_None) refuse(std::string(what) + " must be given");
   }
@@ -176,19 +207,23 @@ void run(const Call& c, int (*f)(const A*, void*), const A& a) {
   Py_END_ALLOW_THREADS
   done(rc);
 }
-// With the workspace that it asks for.
-template <typename A>
-void run(const Call& c, int (*query)(const A*, uint64_t*), int (*f)(const A*, void*), A& a) {
+// With the workspace that it asks for, which w takes.
+template <typename A, typename W>
+void run(const Call& c, int (*query)(const A*, uint64_t*), int (*f)(const A*, void*), A& a, W& w) {
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
   uint64_t need = 0;
   done(query(&a, &need));
   Tensor space;
   if (need) {
     space = c.empty(Shape((int64_t)need), ScalarType::Byte);
-    a.workspace = space.mutable_data_ptr();
-    a.workspace_bytes = need;
+    w.workspace = space.mutable_data_ptr();
+    w.workspace_bytes = need;
   }
   run(c, f, a);
+}
+template <typename A>
+void run(const Call& c, int (*query)(const A*, uint64_t*), int (*f)(const A*, void*), A& a) {
+  run(c, query, f, a, a);
 }
 
 PyObject* give(const Tensor& t) {
@@ -212,6 +247,12 @@ PyObject* results(P... p) {
   return r;
 }
 
+// A checkpoint's two tensors (undefined: None).
+PyObject* give(const Tensor& q, const Tensor& s) {
+  if (!q.defined()) Py_RETURN_NONE;
+  return results(give(q), give(s));
+}
+
 bool truth(PyObject* o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw python_error();
@@ -221,6 +262,13 @@ float number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw python_error();
   return (float)v;
+}
+
+// keep: false, true, or "int8" (2)
+int keep_of(const Call& c, PyObject* o) {
+  if (!PyUnicode_Check(o)) return truth(o);
+  if (PyUnicode_CompareWithASCIIString(o, "int8")) c.refuse("keep must be False, True or \"int8\"");
+  return 2;
 }
 
 // x, weight, residual, eps, e4m3, keep, sum_out -> y, sum, scale, rstd
@@ -274,6 +322,99 @@ PyObject* rmsnorm_backward(PyObject* const* o) {
   return results(give(dx), give(dweight));
 }
 
+// x, weight, bias, residual, eps, e4m3, keep, sum_out -> y, sum, scale, mean, rstd, kept
+PyObject* layernorm(PyObject* const* o) {
+  Call c{"layernorm"};
+  lipz_layernorm_args a{};
+  a.struct_size = sizeof a;
+  a.x = c.first(o[0], "x", WIDE);
+  c.require(o[1], "weight");
+  a.weight = c.vec(o[1], "weight", c.cols);
+  a.bias = c.vec(o[2], "bias", c.cols);
+  a.eps = number(o[4]);
+  a.groups = c.groups, a.rows = c.rows, a.dim = c.cols;
+  const bool e4m3 = truth(o[5]), own_sum = o[7] != Py_None;
+  const int keep = keep_of(c, o[6]);
+  const ScalarType type = a.x.type == LIPZ_FP32 ? F32 : BF16;
+  Tensor y, sum, scale, mean, rstd, q, blocks;
+  if (o[3] == Py_None) {
+    if (own_sum) c.refuse("sum_out needs a residual");
+  } else {
+    if (own_sum) {
+      a.sum = c.target(o[7], "sum_out", c.rows, c.cols, bit(a.x.type));
+      a.x = c.view(c.tensor(o[0], "x"), "x", WIDE);  // (x may be sum_out)
+    } else {
+      a.sum = c.fresh(sum, c.rows, c.cols, type);
+    }
+    a.residual = c.mat(o[3], "residual", c.rows, c.cols, bit(a.x.type));
+  }
+  a.y = c.fresh(y, c.rows, c.cols, e4m3 ? E4M3 : type);
+  if (e4m3) a.scale = c.fresh(scale, c.rows);
+  if (keep) a.mean = c.fresh(mean, c.rows), a.rstd = c.fresh(rstd, c.rows);
+  if (keep == 2) a.kept = c.fresh(q, blocks, c.rows, c.cols);
+  run(c, lipz_layernorm, a);
+  if (own_sum) c.wrote(o[7]);
+  return results(give(y), sum.defined() ? give(sum) : given(own_sum ? o[7] : o[0]), give(scale), give(mean),
+                 give(rstd), give(q, blocks));
+}
+
+// dy, s, mean, rstd, weight, dsum, want_dweight, want_dbias -> dx, dweight, dbias
+PyObject* layernorm_backward(PyObject* const* o) {
+  Call c{"layernorm_backward"};
+  lipz_layernorm_backward_args a{};
+  a.struct_size = sizeof a;
+  a.dy = c.first(o[0], "dy", WIDE);
+  c.require(o[2], "mean"), c.require(o[3], "rstd"), c.require(o[4], "weight");
+  a.groups = c.groups, a.rows = c.rows, a.dim = c.cols;
+  if (c.is_checkpoint(o[1])) {
+    a.kept = c.blocks(o[1], "s", c.rows, c.cols);
+  } else {
+    c.require(o[1], "s");
+    a.s = c.mat(o[1], "s", c.rows, c.cols, bit(a.dy.type));
+  }
+  a.mean = c.vec(o[2], "mean", c.rows);
+  a.rstd = c.vec(o[3], "rstd", c.rows);
+  a.weight = c.vec(o[4], "weight", c.cols);
+  a.dsum = c.mat(o[5], "dsum", c.rows, c.cols, bit(a.dy.type));
+  Tensor dx, dweight, dbias;
+  a.dx = c.fresh(dx, c.rows, c.cols, a.dy.type == LIPZ_FP32 ? F32 : BF16);
+  if (truth(o[6])) a.dweight = c.fresh(dweight, c.cols);
+  if (truth(o[7])) a.dbias = c.fresh(dbias, c.cols);
+  run(c, lipz_layernorm_backward_workspace, lipz_layernorm_backward, a);
+  return results(give(dx), give(dweight), give(dbias));
+}
+
+// x -> data, scale
+PyObject* checkpoint_rows(PyObject* const* o) {
+  Call c{"checkpoint_rows"};
+  lipz_checkpoint_rows_args a{};
+  a.struct_size = sizeof a;
+  a.x = c.first(o[0], "x", WIDE);
+  a.groups = c.groups, a.rows = c.rows, a.dim = c.cols;
+  Tensor q, blocks;
+  a.c = c.fresh(q, blocks, c.rows, c.cols);
+  run(c, lipz_checkpoint_rows, a);
+  return give(q, blocks);
+}
+
+// checkpoint, act's code, slope, out_dtype -> y
+PyObject* restore_rows(PyObject* const* o) {
+  Call c{"restore_rows"};
+  lipz_restore_rows_args a{};
+  a.struct_size = sizeof a;
+  if (!c.is_checkpoint(o[0])) c.refuse("a checkpoint is taken: its data and its scale");
+  const Tensor& q = c.tensor(PyTuple_GET_ITEM(o[0], 0), "the checkpoint");
+  c.first(q, "the checkpoint");
+  a.c = c.blocks(o[0], "the checkpoint", c.rows, c.cols);
+  a.groups = c.groups, a.rows = c.rows, a.dim = c.cols;
+  a.act = (int)PyLong_AsLong(o[1]);
+  a.slope = number(o[2]);
+  Tensor y;
+  a.y = c.fresh(y, c.rows, c.cols, c.result_type(o[3], "out_dtype"));
+  run(c, lipz_restore_rows, a);
+  return give(y);
+}
+
 // x -> q, scale
 PyObject* quantize_rows(PyObject* const* o) {
   Call c{"quantize_rows"};
@@ -291,7 +432,9 @@ PyObject* quantize_rows(PyObject* const* o) {
 // x, w, bias, act's code, slope, residual, x_scale, w_scale, out_dtype, keep, out -> y, pre
 PyObject* linear(PyObject* const* o) {
   Call c{"linear"};
-  lipz_linear_args a{};
+  lipz_linear_checkpoint_args kept{};
+  lipz_linear_args& a = kept.call;
+  kept.struct_size = sizeof kept;
   a.struct_size = sizeof a;
   a.x = c.first(o[0], "x", bit(LIPZ_BF16) | bit(LIPZ_E4M3));
   const Tensor& w = c.tensor(o[1], "w");
@@ -311,39 +454,53 @@ PyObject* linear(PyObject* const* o) {
     c.refuse("x_scale and w_scale go with 8-bit operands, and with them alone");
   a.x_scale = c.vec(o[6], "x_scale", c.rows);
   a.w_scale = c.vec(o[7], "w_scale", n);
-  Tensor y, pre;
+  const int keep = keep_of(c, o[9]);
+  Tensor y, pre, blocks;
   if (!own) a.y = c.fresh(y, c.rows, n, type);
-  if (truth(o[9])) a.pre = c.fresh(pre, c.rows, n, BF16);
-  run(c, lipz_linear_workspace, lipz_linear, a);
+  if (keep == 1) a.pre = c.fresh(pre, c.rows, n, BF16);
+  if (keep == 2) {
+    kept.pre = c.fresh(pre, blocks, c.rows, n);
+    run(c, lipz_linear_checkpoint_workspace, lipz_linear_checkpoint, kept, a);
+  } else {
+    run(c, lipz_linear_workspace, lipz_linear, a);
+  }
   if (own) c.wrote(o[10]);
-  return results(own ? given(o[10]) : give(y), give(pre));
+  return results(own ? given(o[10]) : give(y), keep == 2 ? give(pre, blocks) : give(pre));
 }
 
 // dy, x, w, act's code, slope, pre, want_dx, want_dw, want_db, dx_dtype, dw_dtype -> dx, dw, db
 PyObject* linear_backward(PyObject* const* o) {
   Call c{"linear_backward"};
-  lipz_linear_backward_args a{};
+  lipz_linear_backward_checkpoint_args kept{};
+  lipz_linear_backward_args& a = kept.call;
+  kept.struct_size = sizeof kept;
   a.struct_size = sizeof a;
   a.dy = c.first(o[0], "dy", HALF);
-  const Tensor& x = c.tensor(o[1], "x");
+  const bool x_kept = c.is_checkpoint(o[1]);
+  const Tensor& x = c.tensor(x_kept ? PyTuple_GET_ITEM(o[1], 0) : o[1], "x");
   if (x.dim() != (c.grouped ? 3 : 2)) c.refuse("x must be a CUDA tensor with dy's number of dimensions");
   c.require(o[2], "w");
   const int64_t n = c.cols, k = x.size(-1);
   a.groups = c.groups, a.rows = c.rows, a.k = k, a.n = n;
-  a.x = c.mat(o[1], "x", c.rows, k, HALF);
+  if (x_kept) kept.x = c.blocks(o[1], "x", c.rows, k);
+  else a.x = c.mat(o[1], "x", c.rows, k, HALF);
   a.w = c.mat(o[2], "w", n, k, HALF);
   a.act = (int)PyLong_AsLong(o[3]);
   a.slope = number(o[4]);
   if (a.act != LIPZ_ACT_NONE) {
     if (o[5] == Py_None) c.refuse("an activation needs pre");
-    a.pre = c.mat(o[5], "pre", c.rows, n, HALF);
+    if (c.is_checkpoint(o[5])) kept.pre = c.blocks(o[5], "pre", c.rows, n);
+    else a.pre = c.mat(o[5], "pre", c.rows, n, HALF);
   }
   const ScalarType dx_type = c.result_type(o[9], "dx_dtype"), dw_type = c.result_type(o[10], "dw_dtype");
   Tensor dx, dw, db;
   if (truth(o[6])) a.dx = c.fresh(dx, c.rows, k, dx_type);
   if (truth(o[7])) a.dw = c.fresh(dw, n, k, dw_type);
   if (truth(o[8])) a.db = c.fresh(db, n);
-  run(c, lipz_linear_backward_workspace, lipz_linear_backward, a);
+  if (kept.x.data || kept.pre.data)
+    run(c, lipz_linear_backward_checkpoint_workspace, lipz_linear_backward_checkpoint, kept, a);
+  else
+    run(c, lipz_linear_backward_workspace, lipz_linear_backward, a);
   return results(give(dx), give(dw), give(db));
 }
 
@@ -373,7 +530,8 @@ PyObject* entry(PyObject*, PyObject* const* o, Py_ssize_t n) {
 
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)())entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(rmsnorm, 7), ENTRY(rmsnorm_backward, 6), ENTRY(quantize_rows, 1),
-                         ENTRY(linear, 11), ENTRY(linear_backward, 11), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(linear, 11), ENTRY(linear_backward, 11), ENTRY(layernorm, 8),
+                         ENTRY(layernorm_backward, 8), ENTRY(checkpoint_rows, 1), ENTRY(restore_rows, 4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "torch_operators", nullptr, -1, methods};
 
 }  // namespace
@@ -384,9 +542,13 @@ PyMODINIT_FUNC PyInit_torch_operators() {
   g_error = package ? PyObject_GetAttrString(package, "LipzError") : nullptr;
   Py_XDECREF(package);
   // the sizes of the argument structures that this was compiled with
-  PyObject* sizes = g_error ? Py_BuildValue("nnnnn", sizeof(lipz_rmsnorm_args), sizeof(lipz_rmsnorm_backward_args),
-                                            sizeof(lipz_quantize_rows_args), sizeof(lipz_linear_args),
-                                            sizeof(lipz_linear_backward_args))
+  PyObject* sizes = g_error ? Py_BuildValue("nnnnnnnnnnn", sizeof(lipz_rmsnorm_args),
+                                            sizeof(lipz_rmsnorm_backward_args), sizeof(lipz_quantize_rows_args),
+                                            sizeof(lipz_linear_args), sizeof(lipz_linear_backward_args),
+                                            sizeof(lipz_layernorm_args), sizeof(lipz_layernorm_backward_args),
+                                            sizeof(lipz_checkpoint_rows_args), sizeof(lipz_restore_rows_args),
+                                            sizeof(lipz_linear_checkpoint_args),
+                                            sizeof(lipz_linear_backward_checkpoint_args))
                             : nullptr;
   if (!sizes || PyModule_AddObject(m, "SIZES", sizes) < 0) {
     Py_XDECREF(m);
