@@ -207,6 +207,18 @@ int row_threads(int nvec, int nv) { return (int)(ceil_div(ceil_div(nvec, nv), 32
 struct StreamShape {
   bool wide;
   int tpr, per_sm, stages, slot, smem;
+  int row, fixed;  // bytes of a stage, and of what stands beside the ring
+  void fit() {
+    stages = (RING_SMEM / per_sm - 1024 - RING_BARS - fixed) / row;
+    if (stages > RING_MAX) stages = RING_MAX;
+    smem = RING_BARS + stages * row + fixed;
+  }
+  // Blocks of `threads` per SM in all, as many as leave each two stages or more.
+  void share(int threads) {
+    per_sm = threads / tpr < 24 ? threads / tpr : 24;
+    if (per_sm < 1) per_sm = 1;
+    for (fit(); per_sm > 1 && stages < 2; fit()) --per_sm;
+  }
 };
 // `params`: fp32 parameters of a column that stand in shared memory (k_rows_shift and its backward, whose
 // rows touch up to two units more).
@@ -218,14 +230,8 @@ StreamShape stream_shape(int dim, int e, int eb, int arrays, int threads, int pa
   s.wide = row_threads(nvec, 16 / e) > 512 || wide;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
   s.slot = (int)ceil_div((int64_t)dim * eb, 16) * 16 + 16;
-  const int row = s.slot * arrays;
-  if (s.wide) threads /= 2;
-  s.per_sm = threads / s.tpr < 24 ? threads / s.tpr : 24;
-  if (s.per_sm < 1) s.per_sm = 1;
-  auto stages = [&] { return (RING_SMEM / s.per_sm - 1024 - RING_BARS - fixed) / row; };
-  while (s.per_sm > 1 && stages() < 2) --s.per_sm;
-  s.stages = stages() > RING_MAX ? RING_MAX : stages();
-  s.smem = RING_BARS + s.stages * row + fixed;
+  s.row = s.slot * arrays, s.fixed = fixed;
+  s.share(s.wide ? threads / 2 : threads);
   return s;
 }
 
