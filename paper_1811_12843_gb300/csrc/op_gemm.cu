@@ -39,6 +39,10 @@ static_assert(EPI_WARPS == SUM_WAYS, "a result warp per way");
 // bf16 results are such sums (of more chunks: 2^-15) from LONG_CHUNKS (16384 bf16) on, where a single sum has lost
 // 2^-13 and at 500000 bf16 of k 2.3e-3, more than half of their half unit.
 constexpr int SUM_CHUNKS = 8, BF16_SUM_CHUNKS = 64, LONG_CHUNKS = 256;
+// Results that are kept as a checkpoint too are sums of KEPT_SUM_CHUNKS where they have more: a rounding to a whole
+// multiple turns where the sum is off by as little as its distance from the middle between two, so an error of delta
+// units moves delta of the multiples by one (8192 x 4096 -> 8192: 3.1e-4 of the values' rms by single sums, KEPT_ERR so).
+constexpr int KEPT_SUM_CHUNKS = 16;
 constexpr int SMEM_MAX = 232448, STAGES_MAX = 20;
 constexpr int DIRECT_CHUNKS = 4;          // most chunks of k per CTA whose operands the result warps bring
 
@@ -74,21 +78,6 @@ struct Shape {
     return n;
   }
 };
-
-// n / d for 0 <= n < 2^31 as a multiplication: with s = ceil(log2 d) and m = ceil(2^(31 + s) / d), n m /
-// 2^(31 + s) is above n / d by less than n / (d 2^31) < 1 / d.
-struct Divisor {
-  uint32_t mul;
-  int shift;
-  __device__ __forceinline__ int operator()(int n) const {
-    return (int)((uint64_t)(uint32_t)n * mul >> shift);
-  }
-};
-Divisor divisor(int64_t d) {
-  int s = 0;
-  while (((int64_t)1 << s) < d) ++s;
-  return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
-}
 
 // One product's part of a launch.
 struct Problem {
@@ -329,7 +318,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   static_assert(!SPLIT || (FORWARD && CG == 1 && !VIA && 128 * (BN + 1) * 4 <= 5 * S::B_BYTES),
                 "sums of a tile");
   constexpr int BM = 128 * CG, COLSW = S::COLSW, ACCS = S::ACCS, SLOTS = S::SLOTS;
-  constexpr int CW = COLSW < 32 ? COLSW : 32;       // a result warp's columns at a time
+  constexpr int CW = SUMS && COLSW == 64 ? 16 : COLSW < 32 ? COLSW : 32;  // a result warp's columns at a time
   constexpr int KE = TYPE == LIPZ_BF16 ? 64 : 128;  // k of a stage
   extern __shared__ uint8_t smem_raw[];
   const int stages = prm.stages, stage_bytes = FORWARD ? prm.stage_bytes : S::STAGE;
@@ -796,22 +785,30 @@ __global__ void __launch_bounds__(THREADS, 1)
       };
       uint32_t v[VW];
       if constexpr (SUMS) {
-        static_assert(COLSW == CW, "the sums of a warp's columns stand in registers");
-        float acc[CW];
+        // the sums of a warp's columns stand in registers
+        float acc[COLSW / CW][CW];
 #pragma unroll
-        for (int i = 0; i < CW; ++i) acc[i] = 0.f;
+        for (int j = 0; j < COLSW / CW; ++j)
+#pragma unroll
+          for (int i = 0; i < CW; ++i) acc[j][i] = 0.f;
         for (int kc = sl.c0; kc < sl.c1; kc += prm.sum_chunks) {
           const uint32_t t = wait_sum();
           if (!ok) break;
-          float u[CW];
-          tmem_load(t, u);
-          free_sum();
 #pragma unroll
-          for (int i = 0; i < CW; ++i) acc[i] += u[i];
+          for (int j = 0; j < COLSW / CW; ++j) {
+            float u[CW];
+            tmem_load(t + j * CW, u);
+            if (j + 1 == COLSW / CW) free_sum();
+#pragma unroll
+            for (int i = 0; i < CW; ++i) acc[j][i] += u[i];
+          }
         }
         if (!ok) break;
-        residual(v, 0);
-        results(acc, v, 0);
+#pragma unroll
+        for (int j = 0; j < COLSW / CW; ++j) {
+          residual(v, j * CW);
+          results(acc[j], v, j * CW);
+        }
       } else {
         residual(v, 0);
         const uint32_t t = wait_sum();
@@ -1078,7 +1075,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   }
   if (sums) k.sums = *sums;
   k.err = timeout_word();
-  k.sum_chunks = q.g[0].e.y.type == LIPZ_FP32 ? SUM_CHUNKS : BF16_SUM_CHUNKS;
+  k.sum_chunks = q.g[0].e.y.type == LIPZ_FP32 ? SUM_CHUNKS : q.g[0].e.kept.data ? KEPT_SUM_CHUNKS : BF16_SUM_CHUNKS;
   const Gemm& first = q.g[0];
   k.a_rows = FORWARD && CG == 1 && first.m < 128 ? (int)ceil_div(first.m, 8) * 8 : 128;
   k.stage_bytes = S::stage(k.a_rows);
@@ -1128,6 +1125,9 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
                  : launch<TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
   }
   if (p.sums) {
+    if constexpr (FORWARD) {
+      if (p.bn == 256) return launch<TYPE, 2, 256, true, float>(q, p, parts, sums, st);
+    }
     if (p.cg == 2) return launch<TYPE, 2, 128, FORWARD, float>(q, p, parts, sums, st);
     if (p.bn == 128) return launch<TYPE, 1, 128, FORWARD, float>(q, p, parts, sums, st);
     return launch<TYPE, 1, 64, FORWARD, float>(q, p, parts, sums, st);
@@ -1161,7 +1161,9 @@ GemmPlan plan_products(const Products& q) {
   static const Shape shapes[] = {{2, 256, 158, 9000, 2500, 5500}, {2, 128, 88, 3900, 800, 2600},
                                  {1, 128, 108, 3900, 800, 2600}, {1, 64, 82, 2350, 250, 900}};
   const Shape via{2, 128, 100, 3500, 400, 1000};  // shape 1 with its results through shared memory
-  const bool by_tma = results_by_tma(g0), forward = g0.a.k_major && g0.b.k_major;
+  const int64_t long_chunks = g0.e.kept.data ? KEPT_SUM_CHUNKS : LONG_CHUNKS;
+  const bool by_tma = results_by_tma(g0) && ceil_div(g0.k * eb, ROW) <= long_chunks;
+  const bool forward = g0.a.k_major && g0.b.k_major;
   const int sms = sm_count();
   double best = -1;
   for (const Shape& shape : shapes) {
@@ -1183,7 +1185,7 @@ GemmPlan plan_products(const Products& q) {
         const int64_t want = s0 < o.chunks ? s0 : o.chunks, tiles = o.tiles_m * o.tiles_n * g.groups;
         o.chunks_per_split = ceil_div(o.chunks, want);
         o.splits = (int)ceil_div(o.chunks, o.chunks_per_split);
-        t.sums = t.sums || o.chunks_per_split > LONG_CHUNKS;
+        t.sums = t.sums || o.chunks_per_split > long_chunks;
         fits = fits && tiles * o.splits <= INT32_MAX / 2 &&
                (o.splits == 1 || tiles * o.splits <= (forward ? 1 : 2) * slots) &&
                (!forward || o.splits == s0);
@@ -1196,7 +1198,7 @@ GemmPlan plan_products(const Products& q) {
         if (o.splits > 1 && !forward) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000;
         split = split || o.splits > 1;
       }
-      if (!fits || (s0 > 1 && !split) || (t.sums && c.bn > 128)) continue;
+      if (!fits || (s0 > 1 && !split) || (t.sums && c.bn > 128 && !g0.e.kept.data)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
       // (a cluster's CTA finishes 64 / s0 columns of up to 128 rows, an element per thread and turn)
@@ -1259,7 +1261,9 @@ int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* cop
       const int64_t groups = copied_groups(t, g.groups);
       const int from = t.scale ? 1 : eb;  // bytes of an element
       copies[n++] = {(const uint8_t*)t.data, w, t.group * from, t.ld * from, x.rows, groups * x.rows,
-                     x.cols * from, ld * eb / 16, t.scale, t.scale_group, t.scale_ld};
+                     x.cols * from, ld * eb / 16, t.scale, t.scale_group, t.scale_ld, 32};
+      if (t.scale)
+        while (copies[n - 1].lanes > 1 && copies[n - 1].lanes >= copies[n - 1].units) copies[n - 1].lanes /= 2;
       t.data = w, t.ld = ld, t.group = groups > 1 ? x.rows * ld : 0, t.scale = nullptr;
       w += bytes;
     };
@@ -1274,7 +1278,7 @@ CopyJobs copy_jobs(const RowCopy* c, int n) {
   jobs.n = n;
   for (int i = 0; i < n; ++i) {
     jobs.c[i] = c[i];
-    jobs.blocks += ceil_div(c[i].total, COPY_ROWS);
+    jobs.blocks += ceil_div(c[i].total, COPY_ROWS * 32 / c[i].lanes);
   }
   return jobs;
 }

@@ -59,6 +59,7 @@ struct RowCopy {
   int64_t bytes, units;            // of a row: to read; 16-byte units there
   const uint8_t* scale;            // of a checkpoint, or null
   int64_t scale_group, scale_ld;
+  int lanes;                       // of a row: 32, fewer for a short row of a checkpoint
 };
 
 // How products will run: their scratch memory, and the copies that have to be made before them.
@@ -80,7 +81,7 @@ void plan_space(const Products& q, GemmPlan* plan);
 // The copies that the products of a plan need, into its workspace (copies[4]), and the operands that the
 // products then have.
 int plan_copies(const GemmPlan& plan, Products* q, void* workspace, RowCopy* copies);
-constexpr int COPY_ROWS = 8;  // rows of a block
+constexpr int COPY_ROWS = 8;  // rows of a block, of 32 lanes each
 struct CopyJobs {
   RowCopy c[4];
   int n;

@@ -36,16 +36,16 @@ __device__ __forceinline__ float warp_sum(float v) {
 struct Moments {
   float mean, rstd;
 };
+// (by the lanes of each warp, a share to each, up to 32; every warp has the sums in the same order)
 __device__ __forceinline__ Moments join_shares(const float4* s, int warps, float inv_dim, float eps) {
-  float sum = 0.f, m2 = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < warps; ++i) sum += s[i].y;
-  const float mean = sum * inv_dim;
-#pragma unroll 4
-  for (int i = 0; i < warps; ++i) {
-    const float off = s[i].z - mean;
-    if (s[i].x > 0.f) m2 += fmaf(s[i].x * off, off, s[i].w);
-  }
+  const int lane = threadIdx.x & 31;
+  const float4 q = lane < warps ? s[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+  float sum = q.y;
+  for (int o = 1; o < warps; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const float mean = __shfl_sync(0xffffffffu, sum, 0) * inv_dim, off = q.z - mean;
+  float m2 = q.x > 0.f ? fmaf(q.x * off, off, q.w) : 0.f;
+  for (int o = 1; o < warps; o <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+  m2 = __shfl_sync(0xffffffffu, m2, 0);
   return {mean, rsqrtf(fmaf(m2, inv_dim, eps))};
 }
 
@@ -130,6 +130,128 @@ __device__ __forceinline__ void keep_vec(int8_t* q, uint8_t* scale, int col, boo
     else *reinterpret_cast<uint32_t*>(q + col) = w[0];
   }
   if (col % LIPZ_BLOCK == 0) scale[col / LIPZ_BLOCK] = (uint8_t)s.byte;
+}
+
+// ---- elements two to a 64-bit register pair, as the instructions over two of them take them. (Arrays of single
+// elements cost as many moves as there are operations: 16384 x 8192 with a checkpoint PAIRS_BEFORE us, so PAIRS_NOW.)
+template <typename T, int E>
+__device__ __forceinline__ void pairs_of(const Raw<T, E>& r, uint64_t* v) {
+#pragma unroll
+  for (int j = 0; j < E / 2; ++j) v[j] = pack2(r.get(2 * j), r.get(2 * j + 1));
+}
+template <int E>
+__device__ __forceinline__ void load_pairs(const float* p, uint64_t* w) {
+#pragma unroll
+  for (int j = 0; j < E / 2; j += 2) {
+    const ulonglong2 r = __ldg(reinterpret_cast<const ulonglong2*>(p + 2 * j));
+    w[j] = r.x, w[j + 1] = r.y;
+  }
+}
+// As they are written: rounded to T.
+template <typename T, int E>
+__device__ __forceinline__ Raw<T, E> rounded(const uint64_t* v) {
+  Raw<T, E> r;
+#pragma unroll
+  for (int j = 0; j < E / 2; ++j) {
+    const float2 f = unpack2(v[j]);
+    if constexpr (sizeof(T) == 4) {
+      r.w[2 * j] = __float_as_uint(f.x), r.w[2 * j + 1] = __float_as_uint(f.y);
+    } else {
+      r.w[j] = tc::pack_bf16(f.x, f.y);
+    }
+  }
+  return r;
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_raw(T* p, const Raw<T, E>& r) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_pairs(T* p, const uint64_t* v) {
+  store_raw<T, E>(p, rounded<T, E>(v));
+}
+template <int E>
+__device__ __forceinline__ void store_pairs_e4m3(e4m3* p, const uint64_t* v, Reciprocal inv) {
+  uint32_t h[E / 2];
+#pragma unroll
+  for (int j = 0; j < E / 2; ++j) {
+    const float2 f = unpack2(fma2(v[j], both(inv.hi), mul2(v[j], both(inv.lo))));
+    h[j] = e4m3x2(f.x, f.y);
+  }
+  if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+  else *reinterpret_cast<uint32_t*>(p) = h[0] | h[1] << 16;
+}
+// The largest magnitude's bits of a vector as it is written.
+template <typename T, int E>
+__device__ __forceinline__ uint32_t top_of(const Raw<T, E>& r) {
+  if constexpr (sizeof(T) == 4) {
+    float m = fabsf(r.get(0));
+#pragma unroll
+    for (int e = 1; e < E; ++e) m = max_nan(m, fabsf(r.get(e)));
+    return __float_as_uint(m);
+  } else {
+    uint32_t m = r.w[0] & 0x7FFF7FFFu;
+#pragma unroll
+    for (int j = 1; j < E / 2; ++j)
+      asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(r.w[j] & 0x7FFF7FFFu));
+    return max(m << 16, m & 0xFFFF0000u);
+  }
+}
+// A vector, as it is written to sum, to its checkpoint: 16 / E lanes hold a block, and all of a warp's lanes call it
+// (live: this lane's elements are part of the row).
+template <typename T, int E>
+__device__ __forceinline__ void keep_raw(int8_t* q, uint8_t* scale, int col, bool live, const Raw<T, E>& r) {
+  uint32_t top = live ? top_of<T, E>(r) : 0u;
+#pragma unroll
+  for (int o = 1; o < LIPZ_BLOCK / E; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (!live) return;
+  const BlockScale s = block_scale(top);
+  uint32_t w[E / 4];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) {
+    const float2 a = unpack2(fma2(pack2(r.get(4 * i), r.get(4 * i + 1)), both(s.inv), both(12582912.f)));
+    const float2 b = unpack2(fma2(pack2(r.get(4 * i + 2), r.get(4 * i + 3)), both(s.inv), both(12582912.f)));
+    w[i] = pack_bytes(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+  }
+  if constexpr (E == 8) *reinterpret_cast<uint2*>(q + col) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(q + col) = w[0];
+  if (col % LIPZ_BLOCK == 0) scale[col / LIPZ_BLOCK] = (uint8_t)s.byte;
+}
+template <int N>
+__device__ __forceinline__ float pairs_sum(const uint64_t (&v)[N]) {
+  uint64_t a = v[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) a = add2(a, v[j]);
+  const float2 r = unpack2(a);
+  return r.x + r.y;
+}
+// Of the squares of distances from a mean, over the first `count` vectors.
+template <int E, int NV>
+__device__ __forceinline__ float pairs_squares(const uint64_t (&v)[NV * E / 2], float mean, int count) {
+  uint64_t a = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i < count)
+#pragma unroll
+      for (int j = 0; j < E / 2; ++j) {
+        const uint64_t d = add2(v[i * (E / 2) + j], both(-mean));
+        a = fma2(d, d, a);
+      }
+  const float2 r = unpack2(a);
+  return r.x + r.y;
+}
+// v = (v - mean) rstd w + b; returns the largest magnitude if it is wanted.
+template <int E, bool MAX>
+__device__ __forceinline__ float pairs_affine(uint64_t* v, Moments mo, const uint64_t* w, const uint64_t* b, float top) {
+#pragma unroll
+  for (int j = 0; j < E / 2; ++j) {
+    v[j] = fma2(mul2(add2(v[j], both(-mo.mean)), both(mo.rstd)), w[j], b[j]);
+    if constexpr (MAX) {
+      const float2 f = unpack2(v[j]);
+      top = max_nan(max_nan(top, fabsf(f.x)), fabsf(f.y));
+    }
+  }
+  return top;
 }
 
 // Results of a row that is in registers: statistics kept, y or its 8 bits.
@@ -266,41 +388,50 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k
       }
     }
   };
-  float w[HELD ? NV : 1][E], b[HELD ? NV : 1][E];
+  constexpr int P = E / 2;
+  uint64_t w[HELD ? NV * P : P], b[HELD ? NV * P : P];
   int64_t held_of = -1;  // the group whose parameters w and b are
   auto params = [&](int64_t g, int i, int at) {
     const int c = (t + i * L) * E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) b[at][e] = 0.f;
-    load_params<E>(p.weight.data + g * p.weight.group + c, w[at]);
-    if (p.bias.data) load_params<E>(p.bias.data + g * p.bias.group + c, b[at]);
+    for (int j = 0; j < P; ++j) b[at + j] = 0;
+    load_pairs<E>(p.weight.data + g * p.weight.group + c, w + at);
+    if (p.bias.data) load_pairs<E>(p.bias.data + g * p.bias.group + c, b + at);
   };
   int64_t r = ((int64_t)blockIdx.x * SHORT_WARPS + (threadIdx.x >> 5)) * R + sub;
   bring(r);
   for (; r - sub < p.total; r += step) {  // (the same turns for all lanes of a warp)
-    float v[NV][E];
+    uint64_t v[NV * P];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      pairs_of<T, E>(x[i], v + i * P);
+      if (has_res) {
+        uint64_t u[P];
+        pairs_of<T, E>(res[i], u);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[i][e] = x[i].get(e) + (has_res ? res[i].get(e) : 0.f);
+        for (int j = 0; j < P; ++j) v[i * P + j] = add2(v[i * P + j], u[j]);
+      }
+    }
     bring(r + step);
     const bool live = r < p.total;
     const int64_t g = live ? group_at(r, p.rows, p.total) : 0, gr = r - g * p.rows;
-    if (live && p.sum.data)
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i < count) store_vec<T, E>(row_of<T>(p.sum, g, gr) + (t + i * L) * E, v[i]);
-    if (p.kept.data) {
+    if (p.sum.data || p.kept.data) {
+      T* s = p.sum.data ? row_of<T>(p.sum, g, gr) : nullptr;
       int8_t* q = p.kept.data + g * p.kept.group + gr * p.kept.row;
       uint8_t* scale = p.kept.scale + g * p.kept.scale_group + gr * p.kept.scale_row;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) keep_vec<T, E>(q, scale, (t + i * L) * E, live && i < count, v[i]);
+      for (int i = 0; i < NV; ++i) {
+        const bool here = live && i < count;
+        const Raw<T, E> u = rounded<T, E>(v + i * P);
+        if (s && here) store_raw<T, E>(s + (t + i * L) * E, u);
+        if (p.kept.data) keep_raw<T, E>(q, scale, (t + i * L) * E, here, u);
+      }
     }
-    float sum = sum_of<E, NV>(v);
+    float sum = pairs_sum(v);
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float mean = sum * p.inv_dim;
-    float m2 = squares_of<E, NV>(v, mean, count);
+    float m2 = pairs_squares<E, NV>(v, mean, count);
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
     const Moments mo{mean, rsqrtf(fmaf(m2, p.inv_dim, p.eps))};
@@ -308,35 +439,46 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k
       held_of = g;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (i < count) params(g, i, HELD ? i : 0);
+        if (i < count) params(g, i, HELD ? i * P : 0);
     }
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (i < count) {
-        if (!HELD) params(g, i, 0);
-        affine<E>(v[i], mo, w[HELD ? i : 0], b[HELD ? i : 0]);
-        if (p.scale.data)
-#pragma unroll
-          for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
-      }
-    Reciprocal inv{1.f, 0.f};
+    if (t == 0 && live) {
+      if (p.mean.data) p.mean.data[g * p.mean.group + gr] = mo.mean;
+      if (p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = mo.rstd;
+    }
     if (p.scale.data) {
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) {
+          if (!HELD) params(g, i, 0);
+          top = pairs_affine<E, true>(v + i * P, mo, w + (HELD ? i * P : 0), b + (HELD ? i * P : 0), top);
+        }
       uint32_t most = __float_as_uint(top);
 #pragma unroll
       for (int o = L / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
       const float scale = scale_of(__uint_as_float(most));
-      inv = reciprocal_of(scale);
-      if (live && t == 0) p.scale.data[g * p.scale.group + gr] = scale;
+      const Reciprocal inv = reciprocal_of(scale);
+      if (!live) continue;
+      if (t == 0) p.scale.data[g * p.scale.group + gr] = scale;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) store_pairs_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * L) * E, v + i * P, inv);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (live && i < count) {
+          if (!HELD) params(g, i, 0);
+          pairs_affine<E, false>(v + i * P, mo, w + (HELD ? i * P : 0), b + (HELD ? i * P : 0), 0.f);
+          store_pairs<T, E>(row_of<T>(p.y, g, gr) + (t + i * L) * E, v + i * P);
+        }
     }
-    if (live) layer_results<T, E, NV>(p, g, gr, mo, inv, v, t, L, nvec);
   }
 }
 
 // ---- many rows: a block of one row's threads walks over rows that arrive in a ring of shared-memory stages by bulk
 // copies, so that loads stay in flight while rows are summed and written.
 template <typename T, int E, int NV>
-__global__ void __launch_bounds__(512) k_layer_stream(const LayerArgs p, int stages, int slot, int* err) {
+__global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_stream(const LayerArgs p, int stages, int slot, int* err) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float4 s_share[2][16];
   __shared__ uint32_t s_top[2][16];
@@ -369,70 +511,87 @@ __global__ void __launch_bounds__(512) k_layer_stream(const LayerArgs p, int sta
                                  ring_row(smem, q, stage, 1, row_of<const T>(p.residual, g, gr)))
                            : nullptr;
     ring_wait(q, stage, turn & 1);
-    float v[NV][E];
+    constexpr int P = E / 2;
+    uint64_t v[NV * P];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (i < count) {
-        load_vec<T, E>(x + (t + i * tpr) * E, v[i]);
+        Raw<T, E> a;
+        a.load(x + (t + i * tpr) * E);
+        pairs_of<T, E>(a, v + i * P);
         if (has_res) {
-          float w[E];
-          load_vec<T, E>(res + (t + i * tpr) * E, w);
+          uint64_t u[P];
+          a.load(res + (t + i * tpr) * E);
+          pairs_of<T, E>(a, u);
 #pragma unroll
-          for (int e = 0; e < E; ++e) v[i][e] += w[e];
+          for (int j = 0; j < P; ++j) v[i * P + j] = add2(v[i * P + j], u[j]);
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[i][e] = 0.f;
+        for (int j = 0; j < P; ++j) v[i * P + j] = 0;
       }
     }
-    const float sum = warp_sum(sum_of<E, NV>(v)), own = sum * inv_n;
-    const float m2 = warp_sum(squares_of<E, NV>(v, own, count));
+    const float sum = warp_sum(pairs_sum(v)), own = sum * inv_n;
+    const float m2 = warp_sum(pairs_squares<E, NV>(v, own, count));
     float4* shares = s_share[turn >> 1 & 1];
     if ((t & 31) == 0) shares[warp] = make_float4(n, sum, own, m2);
     __syncthreads();
     // (the row is in registers everywhere: its stage takes the row that comes `stages` later)
     if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
-    if (p.sum.data) {
-      T* s = row_of<T>(p.sum, g, gr);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i < count) store_vec<T, E>(s + (t + i * tpr) * E, v[i]);
-    }
-    if (p.kept.data) {
+    if (p.sum.data || p.kept.data) {
+      T* s = p.sum.data ? row_of<T>(p.sum, g, gr) : nullptr;
       int8_t* kq = p.kept.data + g * p.kept.group + gr * p.kept.row;
       uint8_t* scale = p.kept.scale + g * p.kept.scale_group + gr * p.kept.scale_row;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) keep_vec<T, E>(kq, scale, (t + i * tpr) * E, i < count, v[i]);
+      for (int i = 0; i < NV; ++i) {
+        const Raw<T, E> u = rounded<T, E>(v + i * P);
+        if (s && i < count) store_raw<T, E>(s + (t + i * tpr) * E, u);
+        if (p.kept.data) keep_raw<T, E>(kq, scale, (t + i * tpr) * E, i < count, u);
+      }
     }
     const Moments mo = join_shares(shares, warps, p.inv_dim, p.eps);
+    if (t == 0) {
+      if (p.mean.data) p.mean.data[g * p.mean.group + gr] = mo.mean;
+      if (p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = mo.rstd;
+    }
     const float* weight = p.weight.data + g * p.weight.group;
     const float* bias = p.bias.data ? p.bias.data + g * p.bias.group : nullptr;
-    float top = 0.f;
+    auto params = [&](int i, uint64_t* w, uint64_t* b) {
+      load_pairs<E>(weight + (t + i * tpr) * E, w);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (i < count) {
-        float w[E], b[E];
-        load_params<E>(weight + (t + i * tpr) * E, w);
-#pragma unroll
-        for (int e = 0; e < E; ++e) b[e] = 0.f;
-        if (bias) load_params<E>(bias + (t + i * tpr) * E, b);
-        affine<E>(v[i], mo, w, b);
-        if (p.scale.data)
-#pragma unroll
-          for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(v[i][e]));
-      }
-    Reciprocal inv{1.f, 0.f};
+      for (int j = 0; j < P; ++j) b[j] = 0;
+      if (bias) load_pairs<E>(bias + (t + i * tpr) * E, b);
+    };
     if (p.scale.data) {
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) {
+          uint64_t w[P], b[P];
+          params(i, w, b);
+          top = pairs_affine<E, true>(v + i * P, mo, w, b, top);
+        }
       uint32_t* tops = s_top[turn >> 1 & 1];
       uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
       if ((t & 31) == 0) tops[warp] = most;
       __syncthreads();
-      for (int i = 0; i < warps; ++i) most = max(most, tops[i]);
+      most = __reduce_max_sync(0xffffffffu, tops[min(t & 31, warps - 1)]);
       const float scale = scale_of(__uint_as_float(most));
-      inv = reciprocal_of(scale);
+      const Reciprocal inv = reciprocal_of(scale);
       if (t == 0) p.scale.data[g * p.scale.group + gr] = scale;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) store_pairs_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * tpr) * E, v + i * P, inv);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) {
+          uint64_t w[P], b[P];
+          params(i, w, b);
+          pairs_affine<E, false>(v + i * P, mo, w, b, 0.f);
+          store_pairs<T, E>(row_of<T>(p.y, g, gr) + (t + i * tpr) * E, v + i * P);
+        }
     }
-    layer_results<T, E, NV>(p, g, gr, mo, inv, v, t, tpr, nvec);
     turn ^= 2;
     if (++stage == stages) {
       stage = 0;
@@ -777,10 +936,7 @@ template <typename T, int E, bool KEPT>
 struct Source {
   Raw<T, E> raw;
   __device__ __forceinline__ void zero() { raw.zero(); }
-  __device__ __forceinline__ void get(float* v) const {
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = raw.get(e);
-  }
+  __device__ __forceinline__ void get(uint64_t* v) const { pairs_of<T, E>(raw, v); }
 };
 template <typename T, int E>
 struct Source<T, E, true> {
@@ -795,20 +951,26 @@ struct Source<T, E, true> {
   __device__ __forceinline__ void load(const int8_t* q, uint32_t byte) {
     if constexpr (E == 8) {
       const uint2 r = *reinterpret_cast<const uint2*>(q);
-      w[0] = r.x, w[1] = r.y;
+      w[0] = r.x ^ 0x80808080u, w[1] = r.y ^ 0x80808080u;
     } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(q);
+      w[0] = *reinterpret_cast<const uint32_t*>(q) ^ 0x80808080u;
     }
     unit = block_unit(byte);
   }
-  __device__ __forceinline__ void get(float* v) const {
+  __device__ __forceinline__ void get(uint64_t* v) const {
 #pragma unroll
-    for (int i = 0; i < E / 4; ++i) block_values(w[i], unit, v + 4 * i);
+    for (int i = 0; i < E / 4; ++i) {
+      const uint64_t a = pack2(__uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7440)),
+                               __uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7441)));
+      const uint64_t b = pack2(__uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7442)),
+                               __uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7443)));
+      v[2 * i] = mul2(add2(a, both(-8388736.f)), both(unit));
+      v[2 * i + 1] = mul2(add2(b, both(-8388736.f)), both(unit));
+    }
   }
 };
 
-// A vector's terms: of the two sums along the row (x: g, y: g (s - mean)) and of those down the columns.
-template <int E>
+// A vector's terms: of the two sums along the row (g, and g (s - mean)) and of those down the columns.
 struct Terms {
   uint64_t along_g = 0, along_x = 0;
   __device__ __forceinline__ float2 sums() const {
@@ -817,31 +979,32 @@ struct Terms {
   }
 };
 template <typename T, int E>
-__device__ __forceinline__ void add_terms(Terms<E>& t, const Raw<T, E>& dy, const float* s, const float* w, float mean,
-                                          float rstd, float* dw, float* db) {
+__device__ __forceinline__ void add_terms(Terms& t, const Raw<T, E>& dy, const uint64_t* s, const uint64_t* w,
+                                          float mean, float rstd, uint64_t* dw, uint64_t* db) {
+  uint64_t d[E / 2];
+  pairs_of<T, E>(dy, d);
 #pragma unroll
-  for (int e = 0; e < E; e += 2) {
-    const uint64_t d = pack2(dy.get(e), dy.get(e + 1)), ww = pack2(w[e], w[e + 1]);
-    const uint64_t m = mul2(d, add2(pack2(s[e], s[e + 1]), both(-mean)));
-    const float2 a = unpack2(fma2(m, both(rstd), pack2(dw[e], dw[e + 1])));
-    const float2 b = unpack2(add2(d, pack2(db[e], db[e + 1])));
-    dw[e] = a.x, dw[e + 1] = a.y, db[e] = b.x, db[e + 1] = b.y;
-    t.along_g = fma2(d, ww, t.along_g);
-    t.along_x = fma2(m, ww, t.along_x);
+  for (int j = 0; j < E / 2; ++j) {
+    const uint64_t m = mul2(d[j], add2(s[j], both(-mean)));
+    dw[j] = fma2(m, both(rstd), dw[j]);
+    db[j] = add2(d[j], db[j]);
+    t.along_g = fma2(d[j], w[j], t.along_g);
+    t.along_x = fma2(m, w[j], t.along_x);
   }
 }
 // dx = rstd (g - c1 - (s - mean) c2) + dsum
 template <typename T, int E>
-__device__ __forceinline__ void gradient(const Raw<T, E>& dy, const float* s, const float* w, const Raw<T, E>& ds,
-                                         float mean, float rstd, float c1, float c2, float* v) {
+__device__ __forceinline__ void store_gradient(T* dx, const Raw<T, E>& dy, const uint64_t* s, const uint64_t* w,
+                                               const Raw<T, E>& ds, float mean, float rstd, float c1, float c2) {
+  uint64_t d[E / 2], v[E / 2];
+  pairs_of<T, E>(dy, d);
+  pairs_of<T, E>(ds, v);
 #pragma unroll
-  for (int e = 0; e < E; e += 2) {
-    const uint64_t x = add2(pack2(s[e], s[e + 1]), both(-mean));
-    uint64_t a = fma2(pack2(dy.get(e), dy.get(e + 1)), pack2(w[e], w[e + 1]), both(-c1));
-    a = fma2(x, both(-c2), a);
-    const float2 r = unpack2(fma2(both(rstd), a, pack2(ds.get(e), ds.get(e + 1))));
-    v[e] = r.x, v[e + 1] = r.y;
+  for (int j = 0; j < E / 2; ++j) {
+    const uint64_t a = fma2(add2(s[j], both(-mean)), both(-c2), fma2(d[j], w[j], both(-c1)));
+    v[j] = fma2(both(rstd), a, v[j]);
   }
+  store_pairs<T, E>(dx, v);
 }
 
 // Where a stage's rows stand, and how many bytes one has: of dy, of what was normalised, of its scales, of dsum.
@@ -891,6 +1054,7 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
                                                            int* err) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float2 s_red[2][16];
+  constexpr int P = E / 2;
   const bool has_dsum = p.dsum.data;
   const Ring q = ring_init(smem, stages, slot, 1);
   const int64_t g = blockIdx.y;
@@ -910,11 +1074,11 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
       if (r < p.rows) load(r, s);
     }
   const float* weight = p.weight.data + g * p.weight.group;
-  float dw[NV][E], db[NV][E];
+  uint64_t dw[NV][P], db[NV][P];
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < E; ++e) dw[i][e] = db[i][e] = 0.f;
+    for (int j = 0; j < P; ++j) dw[i][j] = db[i][j] = 0;
   int stage = 0;
   uint32_t turn = 0;
   for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
@@ -927,7 +1091,7 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
     ring_wait(q, stage, turn & 1);
     Raw<T, E> dy[NV], ds[NV];
     Source<T, E, KEPT> x[NV];
-    Terms<E> terms;
+    Terms terms;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * tpr) * E;
@@ -937,8 +1101,8 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
         if constexpr (KEPT) x[i].load(reinterpret_cast<const int8_t*>(rows[1]) + c, rows[2][c / LIPZ_BLOCK]);
         else x[i].raw.load(reinterpret_cast<const T*>(rows[1]) + c);
         if (has_dsum) ds[i].load(reinterpret_cast<const T*>(rows[3]) + c);
-        float w[E], s[E];
-        load_params<E>(weight + c, w);
+        uint64_t w[P], s[P];
+        load_pairs<E>(weight + c, w);
         x[i].get(s);
         add_terms<T, E>(terms, dy[i], s, w, mean, rstd, dw[i], db[i]);
       }
@@ -952,11 +1116,10 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
     for (int i = 0; i < NV; ++i)
       if (i < count) {
         const int c = (t + i * tpr) * E;
-        float w[E], s[E], v[E];
-        load_params<E>(weight + c, w);
+        uint64_t w[P], s[P];
+        load_pairs<E>(weight + c, w);
         x[i].get(s);
-        gradient<T, E>(dy[i], s, w, ds[i], mean, rstd, c1, c2, v);
-        store_vec<T, E>(dx + c, v);
+        store_gradient<T, E>(dx + c, dy[i], s, w, ds[i], mean, rstd, c1, c2);
       }
     turn ^= 2;
     if (++stage == stages) {
@@ -970,10 +1133,11 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
   for (int i = 0; i < NV; ++i)
     if (i < count)
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int c = (t + i * tpr) * E + e;
-        if (out.dw) out.dw[c] = dw[i][e];
-        if (out.db) out.db[c] = db[i][e];
+      for (int j = 0; j < P; ++j) {
+        const int c = (t + i * tpr) * E + 2 * j;
+        const float2 a = unpack2(dw[i][j]), b = unpack2(db[i][j]);
+        if (out.dw) out.dw[c] = a.x, out.dw[c + 1] = a.y;
+        if (out.db) out.db[c] = b.x, out.db[c + 1] = b.y;
       }
 }
 
@@ -1111,13 +1275,14 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
 #pragma unroll
   for (int i = 0; i < NV; ++i) count += t + i * L < nvec;
   pdl_wait();
-  float w[NV][E], dw[NV][E], db[NV][E];
+  constexpr int P = E / 2;
+  uint64_t w[NV][P], dw[NV][P], db[NV][P];
   const float* weight = p.weight.data + g * p.weight.group;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) w[i][e] = dw[i][e] = db[i][e] = 0.f;
-    if (i < count) load_params<E>(weight + (t + i * L) * E, w[i]);
+    for (int j = 0; j < P; ++j) w[i][j] = dw[i][j] = db[i][j] = 0;
+    if (i < count) load_pairs<E>(weight + (t + i * L) * E, w[i]);
   }
   const bool has_dsum = p.dsum.data;
   Raw<T, E> dy[NV], ds[NV];
@@ -1155,11 +1320,11 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
 #pragma unroll
     for (int i = 0; i < NV; ++i) a[i] = dy[i], y[i] = x[i], c3[i] = ds[i];
     load(r + step);
-    Terms<E> terms;
+    Terms terms;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i < count) {
-        float s[E];
+        uint64_t s[P];
         y[i].get(s);
         add_terms<T, E>(terms, a[i], s, w[i], m, f, dw[i], db[i]);
       }
@@ -1175,25 +1340,25 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i < count) {
-        float s[E], v[E];
+        uint64_t s[P];
         y[i].get(s);
-        gradient<T, E>(a[i], s, w[i], c3[i], m, f, c1, c2, v);
-        store_vec<T, E>(dx + (t + i * L) * E, v);
+        store_gradient<T, E>(dx + (t + i * L) * E, a[i], s, w[i], c3[i], m, f, c1, c2);
       }
   }
   if (!p.dweight.data && !p.dbias.data) return;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int j = 0; j < P; ++j) {
 #pragma unroll
       for (int o = L; o < 32; o <<= 1) {
-        dw[i][e] += __shfl_xor_sync(0xffffffffu, dw[i][e], o);
-        db[i][e] += __shfl_xor_sync(0xffffffffu, db[i][e], o);
+        dw[i][j] = add2(dw[i][j], __shfl_xor_sync(0xffffffffu, dw[i][j], o));
+        db[i][j] = add2(db[i][j], __shfl_xor_sync(0xffffffffu, db[i][j], o));
       }
       if (sub == 0 && i < count) {
-        float* at = s_sums + warp * 2 * p.dim + (t + i * L) * E + e;
-        at[0] = dw[i][e], at[p.dim] = db[i][e];
+        float* at = s_sums + warp * 2 * p.dim + (t + i * L) * E + 2 * j;
+        const float2 a = unpack2(dw[i][j]), b = unpack2(db[i][j]);
+        at[0] = a.x, at[1] = a.y, at[p.dim] = b.x, at[p.dim + 1] = b.y;
       }
     }
   __syncthreads();

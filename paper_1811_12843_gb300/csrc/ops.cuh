@@ -23,6 +23,21 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// n / d for 0 <= n < 2^31 as a multiplication: with s = ceil(log2 d) and m = ceil(2^(31 + s) / d), n m /
+// 2^(31 + s) is above n / d by less than n / (d 2^31) < 1 / d.
+struct Divisor {
+  uint32_t mul;
+  int shift;
+  __device__ __forceinline__ int operator()(int n) const {
+    return (int)((uint64_t)(uint32_t)n * mul >> shift);
+  }
+};
+inline Divisor divisor(int64_t d) {
+  int s = 0;
+  while (((int64_t)1 << s) < d) ++s;
+  return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
+}
+
 // E elements of one access (1, or 16 bytes of the wider types), in registers as they lie in memory.
 template <typename T, int E>
 struct Raw {
@@ -326,7 +341,32 @@ __device__ __forceinline__ uint4 bytes16(const uint8_t* p, int64_t n) {
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a warp; of a
+// 32 bytes at a time where they lie on such a boundary.
+template <bool WIDE>
+__device__ __forceinline__ void load32(const void* p, uint32_t* w) {
+  if constexpr (WIDE) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
+  } else {
+    const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+  }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+  if constexpr (WIDE) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
+// A row's copy in whole 16-byte units (the bytes past its last element are zero), by `lanes` lanes of a warp; of a
 // checkpoint's row (p.bytes: its columns) the bf16 values that it stands for, 16 at a time.
 __device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
   const int64_t g = r / p.rows, at = r - g * p.rows;
@@ -334,9 +374,11 @@ __device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
   uint4* d = (uint4*)p.dst + r * p.units;
   if (p.scale) {
     const uint8_t* scale = p.scale + g * p.scale_group + at * p.scale_ld;
-#pragma unroll 2
-    for (int64_t u = threadIdx.x & 31; 2 * u < p.units; u += 32) {
-      const uint4 q = bytes16(s + u * 16, p.bytes - u * 16);
+    const bool whole = ((uint64_t)s & 15) == 0, wide = ((uint64_t)d & 31) == 0;
+#pragma unroll 4
+    for (int64_t u = threadIdx.x & (p.lanes - 1); 2 * u < p.units; u += p.lanes) {
+      const bool full = p.bytes - u * 16 >= 16;
+      const uint4 q = whole && full ? __ldg((const uint4*)s + u) : bytes16(s + u * 16, p.bytes - u * 16);
       const float unit = block_unit(__ldg(scale + u));
       const uint32_t qq[4] = {q.x, q.y, q.z, q.w};
       uint32_t w[8];
@@ -346,20 +388,30 @@ __device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
         block_values(qq[i], unit, v);
         w[2 * i] = block_pair(v[0], v[1]), w[2 * i + 1] = block_pair(v[2], v[3]);
       }
-      d[2 * u] = make_uint4(w[0], w[1], w[2], w[3]);
-      if (2 * u + 1 < p.units) d[2 * u + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+      if (!full) {  // (a NaN block's values end with the row)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (u * 16 + i >= p.bytes) w[i / 2] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      }
+      if (wide && 2 * u + 1 < p.units) {
+        store32<true>(d + 2 * u, w);
+      } else {
+        d[2 * u] = make_uint4(w[0], w[1], w[2], w[3]);
+        if (2 * u + 1 < p.units) d[2 * u + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
     }
     return;
   }
 #pragma unroll 2
   for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) d[u] = bytes16(s + u * 16, p.bytes - u * 16);
 }
-// Block `b` of 256 threads: 8 rows, of one copy after the other.
+// Block `b` of 256 threads: 8 rows per warp's worth of lanes, of one copy after the other.
 __device__ __forceinline__ void copy_rows(const CopyJobs& jobs, int64_t b) {
   for (int j = 0; j < jobs.n; ++j) {
-    const int64_t blocks = (jobs.c[j].total + COPY_ROWS - 1) / COPY_ROWS;
+    const int rows = COPY_ROWS * 32 / jobs.c[j].lanes;
+    const int64_t blocks = (jobs.c[j].total + rows - 1) / rows;
     if (b < blocks) {
-      const int64_t r = b * COPY_ROWS + (threadIdx.x >> 5);
+      const int64_t r = b * rows + threadIdx.x / jobs.c[j].lanes;
       if (r < jobs.c[j].total) copy_row(jobs.c[j], r);
       return;
     }
