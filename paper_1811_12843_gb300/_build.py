@@ -24,7 +24,7 @@ BINDING = os.path.join(OUT_DIR, "torch_operators.so")
 
 SOURCES = ["api.cu", "simt_kernels.cu", "gemm_tc.cu", "fwd_tc.cu", "bwd_tc.cu", "noalloc.cu",
            "conv_kernels.cu", "dcgan.cu", "conv_tc.cu", "operators.cu", "op_linear.cu", "op_gemm.cu",
-           "op_norm.cu", "op_layernorm.cu", "op_checkpoint.cu"]
+           "op_gemm_kept.cu", "op_norm.cu", "op_layernorm.cu", "op_checkpoint.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-I" + INCLUDE, "-I" + CSRC]

@@ -11,7 +11,7 @@ constexpr int B = LIPZ_BLOCK;
 struct BlocksArgs {
   lipz_mat m;  // x, or y
   lipz_blocks c;
-  int64_t rows, dim, blocks, total;  // of a group; of a row; of all rows
+  int64_t rows, dim, blocks, total;  // of a group; pieces of work of a row; of all rows
   int act;
   float slope;
   bool few;  // total below 2^31: the two divisors
@@ -21,6 +21,7 @@ struct At {
   int64_t g, r, b;
 };
 __device__ __forceinline__ At block_at(const BlocksArgs& p, int64_t i) {
+  if (p.total == p.blocks) return {0, 0, i};
   if (p.few) {
     const int row = p.by_row((int)i), g = p.by_group(row);
     return {g, row - g * p.rows, (int)i - (int64_t)row * p.blocks};
@@ -29,243 +30,167 @@ __device__ __forceinline__ At block_at(const BlocksArgs& p, int64_t i) {
   return {g, row - g * p.rows, i - row * p.blocks};
 }
 
-// A block per thread, AHEAD of them at a time, over whole 16-byte units on both sides; WIDE: and 32 bytes of x (y).
-template <typename T>
-constexpr int BLOCKS_AHEAD = sizeof(T) == 4 ? 2 : 4;
-
-template <typename T, bool WIDE>
+// A block per thread and turn, in few registers: what keeps enough loads in flight is threads. (16384 x 4096 in bf16,
+// 205 MB, to a checkpoint 32.8 us and back 34.6, 0.92 and 0.87 of the copy rate; two blocks at a time 32.1 and 39.3,
+// four 33.4 and 47.7.) WIDE: 32 bytes of x at a time; SHIFT: its rows begin anywhere, and a block's elements come from
+// the 16-byte units that hold them, moved by whole words and half words.
+template <typename T, bool WIDE, bool SHIFT>
 __global__ void __launch_bounds__(256) k_checkpoint(const BlocksArgs p) {
-  constexpr int W = B * sizeof(T) / 4, AHEAD = BLOCKS_AHEAD<T>;  // words of a block
+  constexpr int W = B * sizeof(T) / 4, U = 16 / sizeof(T);  // words of a block, elements of a unit
   pdl_wait();
-  const int64_t step = (int64_t)gridDim.x * 256;
-  for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < p.total; i0 += AHEAD * step) {
-    uint32_t x[AHEAD][W];
-    At at[AHEAD];
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * 256) {
+    const At at = block_at(p, i);
+    const T* src = (const T*)p.m.data + at.g * p.m.group + at.r * p.m.row + at.b * B;
+    const int64_t left = p.dim - at.b * B;
+    const int cols = left < B ? (int)left : B;
+    uint32_t x[W + (SHIFT ? 4 : 0)];
+    if constexpr (SHIFT) {
+      const int m = (int)((uint64_t)src & 15) / (int)sizeof(T);  // elements of the first unit before the block
+      const uint4* units = reinterpret_cast<const uint4*>((uint64_t)src & ~15ull);
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
+      for (int j = 0; j <= W / 4; ++j) {
+        const uint4 r = j * U < m + cols ? __ldg(units + j) : make_uint4(0, 0, 0, 0);
+        x[4 * j] = r.x, x[4 * j + 1] = r.y, x[4 * j + 2] = r.z, x[4 * j + 3] = r.w;
+      }
+      const int words = sizeof(T) == 4 ? m : m >> 1;
 #pragma unroll
-      for (int j = 0; j < W; ++j) x[a][j] = 0;
-      if (i0 + a * step >= p.total) continue;
-      at[a] = block_at(p, i0 + a * step);
-      const T* src = (const T*)p.m.data + at[a].g * p.m.group + at[a].r * p.m.row + at[a].b * B;
-      if (p.dim - at[a].b * B >= B) {
+      for (int j = 0; j < W + 2; ++j) x[j] = words & 2 ? x[j + 2] : x[j];
 #pragma unroll
-        for (int j = 0; j < W; j += 8) load32<WIDE>((const char*)src + 4 * j, x[a] + j);
-      } else {  // (a row's last block, in 16-byte units)
+      for (int j = 0; j < W + 1; ++j) x[j] = words & 1 ? x[j + 1] : x[j];
+      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int j = 0; j < W; j += 4)
-          if (at[a].b * B + j * 4 / (int)sizeof(T) < p.dim) {
-            const uint4 r = *reinterpret_cast<const uint4*>((const char*)src + 4 * j);
-            x[a][j] = r.x, x[a][j + 1] = r.y, x[a][j + 2] = r.z, x[a][j + 3] = r.w;
+        for (int j = 0; j < W; ++j) x[j] = __funnelshift_r(x[j], x[j + 1], (m & 1) * 16);
+      }
+      if (cols < B) {  // (what lies behind the row is nothing of it)
+#pragma unroll
+        for (int e = 0; e < B; ++e)
+          if (e >= cols) {
+            if constexpr (sizeof(T) == 4) x[e] = 0;
+            else x[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
           }
       }
+    } else if (cols == B) {
+#pragma unroll
+      for (int j = 0; j < W; j += 8) load32<WIDE>((const char*)src + 4 * j, x + j);
+    } else {  // (a row's last block, in 16-byte units)
+#pragma unroll
+      for (int j = 0; j < W; j += 4) {
+        const uint4 r = j / 4 * U < cols ? *reinterpret_cast<const uint4*>((const char*)src + 4 * j)
+                                         : make_uint4(0, 0, 0, 0);
+        x[j] = r.x, x[j + 1] = r.y, x[j + 2] = r.z, x[j + 3] = r.w;
+      }
     }
+    float v[B], most = 0.f;
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      if (i0 + a * step >= p.total) continue;
-      float v[B], most = 0.f;
+    for (int e = 0; e < B; ++e) {
+      if constexpr (sizeof(T) == 4) v[e] = __uint_as_float(x[e]);
+      else v[e] = __uint_as_float(e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16);
+      most = max_nan(most, fabsf(v[e]));
+    }
+    const BlockScale s = block_scale(__float_as_uint(most));
+    uint32_t w[4];
+    block_multiples<B>(v, s.inv, w);
+    int8_t* q = p.c.data + at.g * p.c.group + at.r * p.c.row + at.b * B;
+    if (cols == B && (!SHIFT || ((uint64_t)q & 15) == 0)) {
+      *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
 #pragma unroll
-      for (int j = 0; j < B; ++j) {
-        if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(x[a][j]);
-        else v[j] = __uint_as_float(j & 1 ? x[a][j >> 1] & 0xFFFF0000u : x[a][j >> 1] << 16);
-        most = max_nan(most, fabsf(v[j]));
-      }
-      const BlockScale s = block_scale(__float_as_uint(most));
-      uint32_t w[4];
-      block_multiples<B>(v, s.inv, w);
-      int8_t* q = p.c.data + at[a].g * p.c.group + at[a].r * p.c.row + at[a].b * B;
-      const int64_t cols = p.dim - at[a].b * B;
-      if (cols >= B) {
-        *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
+      for (int e = 0; e < B; ++e)
+        if (e < cols) q[e] = (int8_t)(w[e / 4] >> e % 4 * 8);
+    }
+    p.c.scale[at.g * p.c.scale_group + at.r * p.c.scale_row + at.b] = (uint8_t)s.byte;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void act_words(int act, float slope, float* v, uint32_t* w) {
+  with_act(act, [&](auto a) {
 #pragma unroll
-        for (int j = 0; j < B; j += 4)
-          if (j < cols) *reinterpret_cast<uint32_t*>(q + j) = w[j / 4];
-      }
-      p.c.scale[at[a].g * p.c.scale_group + at[a].r * p.c.scale_row + at[a].b] = (uint8_t)s.byte;
+    for (int j = 0; j < B; j += 2) act_pair<decltype(a)::value, sizeof(T) == 4>(v[j], v[j + 1], slope);
+  });
+#pragma unroll
+  for (int j = 0; j < B * (int)sizeof(T) / 4; ++j) {
+    if constexpr (sizeof(T) == 4) {
+      w[j] = __float_as_uint(v[j]);
+    } else {
+      const __nv_bfloat162 r = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+      w[j] = *reinterpret_cast<const uint32_t*>(&r);
     }
   }
 }
 
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) k_restore(const BlocksArgs p) {
-  constexpr int W = B * sizeof(T) / 4, AHEAD = BLOCKS_AHEAD<T>;
+  constexpr int W = B * sizeof(T) / 4, U = 16 / sizeof(T);
   pdl_wait();
-  const int64_t step = (int64_t)gridDim.x * 256;
-  for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < p.total; i0 += AHEAD * step) {
-    uint4 q[AHEAD];
-    uint32_t byte[AHEAD];
-    At at[AHEAD];
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * 256) {
+    const At at = block_at(p, i);
+    const int8_t* src = p.c.data + at.g * p.c.group + at.r * p.c.row + at.b * B;
+    const int64_t left = p.dim - at.b * B;
+    const uint4 q = left >= B ? __ldg(reinterpret_cast<const uint4*>(src)) : bytes16((const uint8_t*)src, left);
+    const float unit = block_unit(__ldg(p.c.scale + at.g * p.c.scale_group + at.r * p.c.scale_row + at.b));
+    float v[B];
+    block_values(q.x, unit, v), block_values(q.y, unit, v + 4);
+    block_values(q.z, unit, v + 8), block_values(q.w, unit, v + 12);
+    uint32_t w[W];
+    act_words<T>(p.act, p.slope, v, w);
+    T* y = (T*)p.m.data + at.g * p.m.group + at.r * p.m.row + at.b * B;
+    if (left >= B) {
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      q[a] = make_uint4(0, 0, 0, 0), byte[a] = 0;
-      if (i0 + a * step >= p.total) continue;
-      at[a] = block_at(p, i0 + a * step);
-      const int8_t* src = p.c.data + at[a].g * p.c.group + at[a].r * p.c.row + at[a].b * B;
-      if (p.dim - at[a].b * B >= B) q[a] = __ldg(reinterpret_cast<const uint4*>(src));
-      else q[a] = bytes16((const uint8_t*)src, p.dim - at[a].b * B);
-      byte[a] = __ldg(p.c.scale + at[a].g * p.c.scale_group + at[a].r * p.c.scale_row + at[a].b);
+      for (int j = 0; j < W; j += 8) store32<WIDE>((char*)y + 4 * j, w + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; j += 4)
+        if (j / 4 * U < left)
+          *reinterpret_cast<uint4*>((char*)y + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
     }
+  }
+}
+
+// The same where rows are off that grid: 16 columns from a 16-byte boundary of y on (a row's first and last in part),
+// which are of two blocks.
+template <typename T>
+__global__ void __launch_bounds__(256) k_restore_shift(const BlocksArgs p) {
+  constexpr int W = B * sizeof(T) / 4;
+  pdl_wait();
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.total; i += (int64_t)gridDim.x * 256) {
+    const At at = block_at(p, i);
+    T* row = (T*)p.m.data + at.g * p.m.group + at.r * p.m.row;
+    const int m = (int)((uint64_t)row & 15) / (int)sizeof(T);
+    const int64_t col = at.b * B - m;  // of the first of the 16; it lies m columns before a block's border
+    if (col >= p.dim) continue;
+    const uint8_t* src = (const uint8_t*)p.c.data + at.g * p.c.group + at.r * p.c.row;
+    const uint8_t* scale = p.c.scale + at.g * p.c.scale_group + at.r * p.c.scale_row;
+    const bool all = col >= 0 && col + B <= p.dim;
+    uint32_t q[4] = {0, 0, 0, 0};
+    if (all) {
+      const uint4 r = bytes16(src + col, B);
+      q[0] = r.x, q[1] = r.y, q[2] = r.z, q[3] = r.w;
+    } else {
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      if (i0 + a * step >= p.total) continue;
-      const float unit = block_unit(byte[a]);
-      float v[B];
-      block_values(q[a].x, unit, v), block_values(q[a].y, unit, v + 4);
-      block_values(q[a].z, unit, v + 8), block_values(q[a].w, unit, v + 12);
-      with_act(p.act, [&](auto act) {
+      for (int e = 0; e < B; ++e)
+        if (col + e >= 0 && col + e < p.dim) q[e / 4] |= (uint32_t)__ldg(src + col + e) << e % 4 * 8;
+    }
+    const float before = block_unit(at.b && m ? __ldg(scale + at.b - 1) : 0u);
+    const float behind = block_unit(at.b * B < p.dim ? __ldg(scale + at.b) : 0u);
+    float v[B];
 #pragma unroll
-        for (int j = 0; j < B; j += 2) act_pair<decltype(act)::value, sizeof(T) == 4>(v[j], v[j + 1], p.slope);
-      });
-      uint32_t w[W];
+    for (int j = 0; j < 4; ++j) block_values(q[j], 1.f, v + 4 * j);
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        if constexpr (sizeof(T) == 4) {
-          w[j] = __float_as_uint(v[j]);
-        } else {
-          const __nv_bfloat162 r = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-          w[j] = *reinterpret_cast<const uint32_t*>(&r);
+    for (int e = 0; e < B; ++e) v[e] *= e < m ? before : behind;
+    uint32_t w[W];
+    act_words<T>(p.act, p.slope, v, w);
+    if (all) {
+#pragma unroll
+      for (int j = 0; j < W; j += 4)
+        *reinterpret_cast<uint4*>((char*)(row + col) + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < B; ++e)
+        if (col + e >= 0 && col + e < p.dim) {
+          if constexpr (sizeof(T) == 4) row[col + e] = __uint_as_float(w[e]);
+          else reinterpret_cast<unsigned short*>(row)[col + e] = (unsigned short)(w[e >> 1] >> (e & 1) * 16);
         }
-      }
-      T* y = (T*)p.m.data + at[a].g * p.m.group + at[a].r * p.m.row + at[a].b * B;
-      if (p.dim - at[a].b * B >= B) {
-#pragma unroll
-        for (int j = 0; j < W; j += 8) store32<WIDE>((char*)y + 4 * j, w + j);
-      } else {
-#pragma unroll
-        for (int j = 0; j < W; j += 4)
-          if (at[a].b * B + j * 4 / (int)sizeof(T) < p.dim)
-            *reinterpret_cast<uint4*>((char*)y + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
-      }
-    }
-  }
-}
-
-// Rows off that grid: four lanes to a block, four columns to a lane, from the words that hold them.
-constexpr int QUADS_AHEAD = 4;
-
-template <typename T>
-__global__ void __launch_bounds__(256) k_checkpoint_quads(const BlocksArgs p) {
-  const int lane = threadIdx.x & 31, c = (lane & 3) * 4;
-  const uint32_t four = 0xFu << (lane & 28);
-  pdl_wait();
-  const int64_t step = (int64_t)gridDim.x * 64;
-  for (int64_t i0 = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 2); i0 < p.total; i0 += QUADS_AHEAD * step) {
-    uint32_t x[QUADS_AHEAD][sizeof(T)];
-    At at[QUADS_AHEAD];
-    int left[QUADS_AHEAD];  // columns of this lane
-#pragma unroll
-    for (int a = 0; a < QUADS_AHEAD; ++a) {
-#pragma unroll
-      for (int j = 0; j < (int)sizeof(T); ++j) x[a][j] = 0;
-      left[a] = 0;
-      if (i0 + a * step >= p.total) continue;
-      at[a] = block_at(p, i0 + a * step);
-      left[a] = (int)max((int64_t)0, min((int64_t)4, p.dim - at[a].b * B - c));
-      const T* src = (const T*)p.m.data + at[a].g * p.m.group + at[a].r * p.m.row + at[a].b * B + c;
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j < left[a]) x[a][j] = __ldg(reinterpret_cast<const uint32_t*>(src) + j);
-      } else if (left[a] == 4) {
-        const uint32_t off = (uint32_t)(uint64_t)src & 2u;
-        const uint32_t* w = reinterpret_cast<const uint32_t*>((const char*)src - off);
-        const uint32_t w0 = __ldg(w), w1 = __ldg(w + 1), w2 = off ? __ldg(w + 2) : 0u;
-        x[a][0] = __funnelshift_r(w0, w1, off * 8), x[a][1] = __funnelshift_r(w1, w2, off * 8);
-      } else {
-        const unsigned short* h = reinterpret_cast<const unsigned short*>(src);
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-          if (j < left[a]) x[a][j >> 1] |= (uint32_t)__ldg(h + j) << (j & 1) * 16;
-      }
-    }
-#pragma unroll
-    for (int a = 0; a < QUADS_AHEAD; ++a) {
-      float v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(x[a][j]);
-        else v[j] = __uint_as_float(j & 1 ? x[a][j >> 1] & 0xFFFF0000u : x[a][j >> 1] << 16);
-      }
-      uint32_t top = max(max(magnitude(v[0]), magnitude(v[1])), max(magnitude(v[2]), magnitude(v[3])));
-      top = max(top, __shfl_xor_sync(four, top, 1));
-      top = max(top, __shfl_xor_sync(four, top, 2));
-      if (i0 + a * step >= p.total) continue;
-      const BlockScale s = block_scale(top);
-      uint32_t w;
-      block_multiples<4>(v, s.inv, &w);
-      int8_t* q = p.c.data + at[a].g * p.c.group + at[a].r * p.c.row + at[a].b * B + c;
-      if (left[a] == 4 && ((uint64_t)q & 3) == 0) {
-        *reinterpret_cast<uint32_t*>(q) = w;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j < left[a]) q[j] = (int8_t)(w >> 8 * j);
-      }
-      if (c == 0) p.c.scale[at[a].g * p.c.scale_group + at[a].r * p.c.scale_row + at[a].b] = (uint8_t)s.byte;
-    }
-  }
-}
-
-// And back: a lane takes 16 bytes of y from such a boundary on (a row's first and last in part); their columns are of
-// two blocks at most. (p.blocks: units that a row touches at most)
-constexpr int UNITS_AHEAD = 4;
-
-template <typename T>
-__global__ void __launch_bounds__(256) k_restore_units(const BlocksArgs p) {
-  constexpr int E = 16 / sizeof(T);
-  pdl_wait();
-  const int64_t step = (int64_t)gridDim.x * 256;
-  for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < p.total; i0 += UNITS_AHEAD * step) {
-    uint32_t q[UNITS_AHEAD][E / 4], byte[UNITS_AHEAD][2];
-    T* y[UNITS_AHEAD];
-    int64_t col[UNITS_AHEAD];
-#pragma unroll
-    for (int a = 0; a < UNITS_AHEAD; ++a) {
-      col[a] = p.dim;
-      if (i0 + a * step >= p.total) continue;
-      const At at = block_at(p, i0 + a * step);
-      T* row = (T*)p.m.data + at.g * p.m.group + at.r * p.m.row;
-      const int64_t c = at.b * E - (int)((uint64_t)row & 15) / (int)sizeof(T);
-      if (c >= p.dim) continue;
-      col[a] = c, y[a] = row + c;
-      const uint8_t* src = (const uint8_t*)p.c.data + at.g * p.c.group + at.r * p.c.row;
-      const uint8_t* scale = p.c.scale + at.g * p.c.scale_group + at.r * p.c.scale_row;
-      byte[a][0] = __ldg(scale + max(c, (int64_t)0) / B);
-      byte[a][1] = __ldg(scale + (min(c + E, p.dim) - 1) / B);
-      if (c >= 0 && c + E <= p.dim) {
-        const uint4 w = bytes16(src + c, E);
-        q[a][0] = w.x;
-        if constexpr (E == 8) q[a][1] = w.y;
-      } else {
-#pragma unroll
-        for (int j = 0; j < E / 4; ++j) q[a][j] = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (c + e >= 0 && c + e < p.dim) q[a][e / 4] |= (uint32_t)__ldg(src + c + e) << e % 4 * 8;
-      }
-    }
-#pragma unroll
-    for (int a = 0; a < UNITS_AHEAD; ++a) {
-      if (col[a] >= p.dim) continue;
-      const float unit0 = block_unit(byte[a][0]), unit1 = block_unit(byte[a][1]);
-      const int border = B - (int)(max(col[a], (int64_t)0) & (B - 1)) + (col[a] < 0 ? (int)-col[a] : 0);
-      float v[E];
-#pragma unroll
-      for (int j = 0; j < E / 4; ++j) block_values(q[a][j], 1.f, v + 4 * j);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= e < border ? unit0 : unit1;
-      with_act(p.act, [&](auto act) {
-#pragma unroll
-        for (int e = 0; e < E; e += 2) act_pair<decltype(act)::value, sizeof(T) == 4>(v[e], v[e + 1], p.slope);
-      });
-      if (col[a] >= 0 && col[a] + E <= p.dim) {
-        store_vec<T, E>(y[a], v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (col[a] + e >= 0 && col[a] + e < p.dim) y[a][e] = from_f<T>(v[e]);
-      }
     }
   }
 }
@@ -290,9 +215,27 @@ BlocksArgs blocks_args(const lipz_mat& m, const lipz_blocks& c, int64_t groups, 
 bool starts_on(const BlocksArgs& p, int64_t groups, int64_t rows, int bytes) {
   return rows_aligned(p.m, groups, rows, bytes) && rows_aligned(bytes_of(p.c), groups, rows, 16);
 }
-dim3 grid_of(const BlocksArgs& p, int per_block) {
-  const int64_t want = ceil_div(p.total, per_block), most = 8 * (int64_t)sm_count();
+dim3 grid_of(const BlocksArgs& p) {
+  const int64_t want = ceil_div(p.total, 256), most = 16 * (int64_t)sm_count();
   return dim3((unsigned)(want < most ? want : most));
+}
+
+template <typename T>
+cudaError_t checkpoint_of(const BlocksArgs& p, const lipz_checkpoint_rows_args& a, cudaStream_t st) {
+  if (a.dim % (16 / sizeof(T)) || !starts_on(p, a.groups, a.rows, 16))
+    return launch_pdl(k_checkpoint<T, false, true>, grid_of(p), dim3(256), 0, st, p);
+  return starts_on(p, a.groups, a.rows, 32)
+             ? launch_pdl(k_checkpoint<T, true, false>, grid_of(p), dim3(256), 0, st, p)
+             : launch_pdl(k_checkpoint<T, false, false>, grid_of(p), dim3(256), 0, st, p);
+}
+template <typename T>
+cudaError_t restore_of(BlocksArgs& p, const lipz_restore_rows_args& a, cudaStream_t st) {
+  if (a.dim % (16 / sizeof(T)) || !starts_on(p, a.groups, a.rows, 16)) {
+    share_out(&p, p.dim == a.dim ? a.groups : 1, ceil_div(p.dim + 16 / sizeof(T) - 1, B));
+    return launch_pdl(k_restore_shift<T>, grid_of(p), dim3(256), 0, st, p);
+  }
+  return starts_on(p, a.groups, a.rows, 32) ? launch_pdl(k_restore<T, true>, grid_of(p), dim3(256), 0, st, p)
+                                            : launch_pdl(k_restore<T, false>, grid_of(p), dim3(256), 0, st, p);
 }
 
 }  // namespace
@@ -300,35 +243,14 @@ dim3 grid_of(const BlocksArgs& p, int per_block) {
 cudaError_t checkpoint_rows(const lipz_checkpoint_rows_args& a, cudaStream_t st) {
   const BlocksArgs p = blocks_args(a.x, a.c, a.groups, a.rows, a.dim);
   if (p.total == 0) return cudaSuccess;
-  const bool fp32 = a.x.type == LIPZ_FP32;
-  if (a.dim % (16 / type_bytes(a.x.type)) || !starts_on(p, a.groups, a.rows, 16))
-    return fp32 ? launch_pdl(k_checkpoint_quads<float>, grid_of(p, 64), dim3(256), 0, st, p)
-                : launch_pdl(k_checkpoint_quads<bf16>, grid_of(p, 64), dim3(256), 0, st, p);
-  const bool wide = starts_on(p, a.groups, a.rows, 32);
-  if (fp32)
-    return wide ? launch_pdl(k_checkpoint<float, true>, grid_of(p, 256), dim3(256), 0, st, p)
-                : launch_pdl(k_checkpoint<float, false>, grid_of(p, 256), dim3(256), 0, st, p);
-  return wide ? launch_pdl(k_checkpoint<bf16, true>, grid_of(p, 256), dim3(256), 0, st, p)
-              : launch_pdl(k_checkpoint<bf16, false>, grid_of(p, 256), dim3(256), 0, st, p);
+  return a.x.type == LIPZ_FP32 ? checkpoint_of<float>(p, a, st) : checkpoint_of<bf16>(p, a, st);
 }
 
 cudaError_t restore_rows(const lipz_restore_rows_args& a, cudaStream_t st) {
   BlocksArgs p = blocks_args(a.y, a.c, a.groups, a.rows, a.dim);
   if (p.total == 0) return cudaSuccess;
   p.act = a.act, p.slope = a.slope;
-  const bool fp32 = a.y.type == LIPZ_FP32;
-  const int e = 16 / type_bytes(a.y.type);
-  if (a.dim % e || !starts_on(p, a.groups, a.rows, 16)) {
-    share_out(&p, p.dim == a.dim ? a.groups : 1, ceil_div(p.dim + e - 1, e));
-    return fp32 ? launch_pdl(k_restore_units<float>, grid_of(p, 256), dim3(256), 0, st, p)
-                : launch_pdl(k_restore_units<bf16>, grid_of(p, 256), dim3(256), 0, st, p);
-  }
-  const bool wide = starts_on(p, a.groups, a.rows, 32);
-  if (fp32)
-    return wide ? launch_pdl(k_restore<float, true>, grid_of(p, 256), dim3(256), 0, st, p)
-                : launch_pdl(k_restore<float, false>, grid_of(p, 256), dim3(256), 0, st, p);
-  return wide ? launch_pdl(k_restore<bf16, true>, grid_of(p, 256), dim3(256), 0, st, p)
-              : launch_pdl(k_restore<bf16, false>, grid_of(p, 256), dim3(256), 0, st, p);
+  return a.y.type == LIPZ_FP32 ? restore_of<float>(p, a, st) : restore_of<bf16>(p, a, st);
 }
 
 }  // namespace ops

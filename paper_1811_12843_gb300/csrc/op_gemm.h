@@ -92,6 +92,8 @@ cudaError_t run_copies(const CopyJobs& jobs, cudaStream_t st);
 // The products themselves; sums: null, or formed beside them.
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,
                          cudaStream_t st);
+// A forward product that keeps a checkpoint.
+cudaError_t run_kept_product(const GemmPlan& plan, const Products& q, cudaStream_t st);
 
 // The word that a kernel of this thread's calls sets when one of its waits expires (null: none can be had).
 int* timeout_word();

@@ -186,7 +186,10 @@ def test_linear_keeps_a_checkpoint(groups, rows, k, n, e4m3):
     check_blocks(pre, y)
     for act, residual in (("gelu", None), ("silu", randn(14, u.shape, 1.0)), ("none", None)):
         y, pre = ops.linear(x, w, b, act=act, residual=residual, keep="int8", **kw)
-        assert torch.equal(y, ops.linear(x, w, b, act=act, residual=residual, keep=True, **kw)[0])
+        # (its sums are added up in other parts than without a checkpoint: gelu's and silu's slopes are below 1.13)
+        ref = act64(act, u) + (0 if residual is None else d(residual))
+        within(y, ref, 2.0 ** -8 * ref.abs() * (1 + 2.0 ** -7) + 1.13 * sum_error(k) * size * (1 + 2.0 ** -8) +
+               2.0 ** -17 * act64(act, u).abs() * (1 + u.abs()), act)
         top = torch.nn.functional.pad(u.abs() + sum_error(k) * size, (0, -n % 16))
         top = top.unflatten(-1, (-(-n // 16), 16)).amax(dim=-1).repeat_interleave(16, dim=-1)[..., :n]
         within(ops.restore_rows(pre), u, top / 127.5 + sum_error(k) * size, act)
