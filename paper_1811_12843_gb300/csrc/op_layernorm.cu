@@ -19,6 +19,9 @@ struct LayerArgs {
   float eps, inv_dim;
 };
 
+// Widest rows that are taken in units off the 16-byte grid: 512 threads of 16 elements, less the unit more.
+constexpr int SHIFT_DIM = 512 * 16 - 8;
+
 // (rows of all groups stay below 2^31)
 __device__ __forceinline__ int64_t group_at(int64_t r, int64_t rows, int64_t total) {
   return total == rows ? 0 : (uint32_t)r / (uint32_t)rows;
@@ -139,8 +142,15 @@ __device__ __forceinline__ void pairs_of(const Raw<T, E>& r, uint64_t* v) {
 #pragma unroll
   for (int j = 0; j < E / 2; ++j) v[j] = pack2(r.get(2 * j), r.get(2 * j + 1));
 }
+// (eight by one access where they lie on 32 bytes: lanes 32 bytes apart meet each line once)
 template <int E>
 __device__ __forceinline__ void load_pairs(const float* p, uint64_t* w) {
+  if constexpr (E == 8) {
+    if (((uint64_t)p & 31) == 0) {
+      asm("ld.global.nc.v4.b64 {%0,%1,%2,%3}, [%4];" : "=l"(w[0]), "=l"(w[1]), "=l"(w[2]), "=l"(w[3]) : "l"(p));
+      return;
+    }
+  }
 #pragma unroll
   for (int j = 0; j < E / 2; j += 2) {
     const ulonglong2 r = __ldg(reinterpret_cast<const ulonglong2*>(p + 2 * j));
@@ -225,13 +235,13 @@ __device__ __forceinline__ float pairs_sum(const uint64_t (&v)[N]) {
   const float2 r = unpack2(a);
   return r.x + r.y;
 }
-// Of the squares of distances from a mean, over the first `count` vectors.
+// Of the squares of distances from a mean, over the vectors of a set.
 template <int E, int NV>
-__device__ __forceinline__ float pairs_squares(const uint64_t (&v)[NV * E / 2], float mean, int count) {
+__device__ __forceinline__ float pairs_squares(const uint64_t (&v)[NV * E / 2], float mean, uint32_t set) {
   uint64_t a = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (i < count)
+    if (set >> i & 1)
 #pragma unroll
       for (int j = 0; j < E / 2; ++j) {
         const uint64_t d = add2(v[i * (E / 2) + j], both(-mean));
@@ -431,7 +441,7 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float mean = sum * p.inv_dim;
-    float m2 = pairs_squares<E, NV>(v, mean, count);
+    float m2 = pairs_squares<E, NV>(v, mean, (1u << count) - 1u);
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
     const Moments mo{mean, rsqrtf(fmaf(m2, p.inv_dim, p.eps))};
@@ -477,22 +487,74 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k
 
 // ---- many rows: a block of one row's threads walks over rows that arrive in a ring of shared-memory stages by bulk
 // copies, so that loads stay in flight while rows are summed and written.
-template <typename T, int E, int NV>
-__global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_stream(const LayerArgs p, int stages, int slot, int* err) {
+//
+// SHIFT: rows off the 16-byte grid (odd widths), all of a call's matrices at the same place of a unit in each row. A
+// thread takes whole units, the row's first and last in part. A block's rows lie a multiple of 16 rows' bytes apart, so
+// that all of them begin at the same place of a unit: weights and biases stand in shared memory in those units. (For
+// rows at any place, a word to each column, bf16 16385 x 4097 took 128 us; in registers, which leave room for fewer
+// blocks, 194; so SHIFT_NOW.)
+template <int E>
+struct Units {
+  int m, dim;  // elements of the first unit before the row
+  __device__ __forceinline__ int col(int c) const { return c * E - m; }
+  __device__ __forceinline__ bool live(int c) const { return c * E - m < dim; }
+  __device__ __forceinline__ bool whole(int c) const { return c * E >= m && c * E - m + E <= dim; }
+  __device__ __forceinline__ bool in(int c, int e) const { return c * E - m + e >= 0 && c * E - m + e < dim; }
+  __device__ __forceinline__ int count(int c) const { return min(c * E - m + E, dim) - max(c * E - m, 0); }
+  // a unit's parameters, zeros beside the row
+  __device__ __forceinline__ void params(const float* p, int c, uint64_t* w) const {
+#pragma unroll
+    for (int e = 0; e < E; e += 2)
+      w[e / 2] = pack2(in(c, e) ? __ldg(p + col(c) + e) : 0.f, in(c, e + 1) ? __ldg(p + col(c) + e + 1) : 0.f);
+  }
+};
+template <typename T, int E>
+__device__ __forceinline__ void store_edge(T* row, const Units<E>& u, int c, const Raw<T, E>& r) {
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (u.in(c, e)) row[u.col(c) + e] = from_f<T>(r.get(e));
+}
+
+template <typename T, int E, int NV, bool SHIFT>
+__global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1)
+    k_layer_stream(const LayerArgs p, int stages, int slot, int* err) {
+  constexpr int P = E / 2;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float4 s_share[2][16];
   __shared__ uint32_t s_top[2][16];
   const bool has_res = p.residual.data;
   const Ring q = ring_init(smem, stages, slot, has_res ? 2 : 1);
-  const int t = threadIdx.x, tpr = blockDim.x, nvec = p.dim / E, bytes = p.dim * (int)sizeof(T);
+  const int t = threadIdx.x, tpr = blockDim.x, bytes = p.dim * (int)sizeof(T);
   const int warp = t >> 5, warps = tpr >> 5;
-  int count = 0;
+  const int64_t rows = SHIFT ? p.rows : p.total, g0 = SHIFT ? blockIdx.y : 0;  // (SHIFT: of one group)
+  auto place = [&](int64_t r, int64_t& g, int64_t& gr) {
+    g = SHIFT ? g0 : group_at(r, p.rows, p.total);
+    gr = SHIFT ? r : r - g * p.rows;
+  };
+  const Units<E> units{SHIFT ? (int)((uint64_t)row_of<const T>(p.x, g0, blockIdx.x) & 15) / (int)sizeof(T) : 0, p.dim};
+  int count = 0, held = 0;
+  uint32_t edge = 0;  // vectors that the row has in part
 #pragma unroll
-  for (int i = 0; i < NV; ++i) count += t + i * tpr < nvec;
-  const float n = (float)__reduce_add_sync(0xffffffffu, count * E), inv_n = n > 0.f ? 1.f / n : 0.f;
+  for (int i = 0; i < NV; ++i) {
+    const int c = t + i * tpr;
+    if (!units.live(c)) continue;
+    ++count;
+    held += SHIFT ? units.count(c) : E;
+    if (SHIFT && !units.whole(c)) edge |= 1u << i;
+  }
+  const uint32_t whole = ((1u << count) - 1u) & ~edge;
+  // (few threads have any: apart from the others' code, whose instructions bound bf16 rows)
+  auto edges = [&](auto f) {
+    if (!SHIFT || !edge) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (edge >> i & 1) f(i);
+  };
+  const float n = (float)__reduce_add_sync(0xffffffffu, held), inv_n = n > 0.f ? 1.f / n : 0.f;
   pdl_wait();
   auto load = [&](int64_t r, int stage) {
-    const int64_t g = group_at(r, p.rows, p.total), gr = r - g * p.rows;
+    int64_t g, gr;
+    place(r, g, gr);
     const char* src[3] = {(const char*)row_of<const T>(p.x, g, gr),
                           has_res ? (const char*)row_of<const T>(p.residual, g, gr) : nullptr, nullptr};
     ring_load(q, stage, src, bytes);
@@ -500,18 +562,32 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_s
   if (t == 0)
     for (int s = 0; s < stages; ++s) {
       const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
-      if (r < p.total) load(r, s);
+      if (r < rows) load(r, s);
     }
+  // [quarters of a unit][weights, biases][units of the row][4], zeros beside the row (so that lanes read adjacent 16 bytes)
+  float* s_par = reinterpret_cast<float*>(smem + RING_BARS + stages * q.arrays * slot);
+  const int width = (int)(units.m + p.dim + E - 1) / E * E, plane = width / E * 4;
+  if constexpr (SHIFT) {
+    const float* w = p.weight.data + g0 * p.weight.group;
+    const float* b = p.bias.data ? p.bias.data + g0 * p.bias.group : nullptr;
+    for (int i = t; i < width; i += tpr) {
+      const int c = i - units.m;
+      const bool in = c >= 0 && c < p.dim;
+      float* to = s_par + i % E / 4 * 2 * plane + i / E * 4 + i % 4;
+      to[0] = in ? __ldg(w + c) : 0.f, to[plane] = in && b ? __ldg(b + c) : 0.f;
+    }
+    __syncthreads();
+  }
   int stage = 0;
   uint32_t turn = 0;
-  for (int64_t r = blockIdx.x; r < p.total; r += gridDim.x) {
-    const int64_t g = group_at(r, p.rows, p.total), gr = r - g * p.rows;
-    const T* x = reinterpret_cast<const T*>(ring_row(smem, q, stage, 0, row_of<const T>(p.x, g, gr)));
-    const T* res = has_res ? reinterpret_cast<const T*>(
-                                 ring_row(smem, q, stage, 1, row_of<const T>(p.residual, g, gr)))
-                           : nullptr;
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    int64_t g, gr;
+    place(r, g, gr);
+    const char* at = reinterpret_cast<const char*>(smem) + RING_BARS + stage * q.arrays * slot;
+    const T* x = reinterpret_cast<const T*>(at + (SHIFT ? 0 : (uint64_t)row_of<const T>(p.x, g, gr) & 15));
+    const T* res = reinterpret_cast<const T*>(
+        at + slot + (SHIFT ? 0 : has_res ? (uint64_t)row_of<const T>(p.residual, g, gr) & 15 : 0));
     ring_wait(q, stage, turn & 1);
-    constexpr int P = E / 2;
     uint64_t v[NV * P];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -531,23 +607,41 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_s
         for (int j = 0; j < P; ++j) v[i * P + j] = 0;
       }
     }
+    edges([&](int i) {
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const float2 f = unpack2(v[i * P + j]);
+        v[i * P + j] = pack2(units.in(t + i * tpr, 2 * j) ? f.x : 0.f, units.in(t + i * tpr, 2 * j + 1) ? f.y : 0.f);
+      }
+    });
     const float sum = warp_sum(pairs_sum(v)), own = sum * inv_n;
-    const float m2 = warp_sum(pairs_squares<E, NV>(v, own, count));
+    float m2 = pairs_squares<E, NV>(v, own, whole);
+    edges([&](int i) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float2 f = unpack2(v[i * P + e / 2]);
+        const float off = (e & 1 ? f.y : f.x) - own;
+        if (units.in(t + i * tpr, e)) m2 = fmaf(off, off, m2);
+      }
+    });
+    m2 = warp_sum(m2);
     float4* shares = s_share[turn >> 1 & 1];
     if ((t & 31) == 0) shares[warp] = make_float4(n, sum, own, m2);
     __syncthreads();
     // (the row is in registers everywhere: its stage takes the row that comes `stages` later)
-    if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
-    if (p.sum.data || p.kept.data) {
+    if (t == 0 && r + (int64_t)stages * gridDim.x < rows) load(r + (int64_t)stages * gridDim.x, stage);
+    if (p.sum.data || (!SHIFT && p.kept.data)) {
       T* s = p.sum.data ? row_of<T>(p.sum, g, gr) : nullptr;
       int8_t* kq = p.kept.data + g * p.kept.group + gr * p.kept.row;
       uint8_t* scale = p.kept.scale + g * p.kept.scale_group + gr * p.kept.scale_row;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const Raw<T, E> u = rounded<T, E>(v + i * P);
-        if (s && i < count) store_raw<T, E>(s + (t + i * tpr) * E, u);
-        if (p.kept.data) keep_raw<T, E>(kq, scale, (t + i * tpr) * E, i < count, u);
+        const int c = t + i * tpr;
+        if (s && whole >> i & 1) store_raw<T, E>(s + units.col(c), u);
+        if (!SHIFT && p.kept.data) keep_raw<T, E>(kq, scale, c * E, i < count, u);
       }
+      edges([&](int i) { store_edge<T, E>(s, units, t + i * tpr, rounded<T, E>(v + i * P)); });
     }
     const Moments mo = join_shares(shares, warps, p.inv_dim, p.eps);
     if (t == 0) {
@@ -557,10 +651,20 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_s
     const float* weight = p.weight.data + g * p.weight.group;
     const float* bias = p.bias.data ? p.bias.data + g * p.bias.group : nullptr;
     auto params = [&](int i, uint64_t* w, uint64_t* b) {
-      load_pairs<E>(weight + (t + i * tpr) * E, w);
+      if constexpr (SHIFT) {
 #pragma unroll
-      for (int j = 0; j < P; ++j) b[j] = 0;
-      if (bias) load_pairs<E>(bias + (t + i * tpr) * E, b);
+        for (int j = 0; j < P; j += 2) {
+          const float* from = s_par + j / 2 * 2 * plane + (t + i * tpr) * 4;
+          const ulonglong2 x2 = *reinterpret_cast<const ulonglong2*>(from);
+          const ulonglong2 y2 = *reinterpret_cast<const ulonglong2*>(from + plane);
+          w[j] = x2.x, w[j + 1] = x2.y, b[j] = y2.x, b[j + 1] = y2.y;
+        }
+      } else {
+        load_pairs<E>(weight + (t + i * tpr) * E, w);
+#pragma unroll
+        for (int j = 0; j < P; ++j) b[j] = 0;
+        if (bias) load_pairs<E>(bias + (t + i * tpr) * E, b);
+      }
     };
     if (p.scale.data) {
       float top = 0.f;
@@ -569,8 +673,16 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_s
         if (i < count) {
           uint64_t w[P], b[P];
           params(i, w, b);
-          top = pairs_affine<E, true>(v + i * P, mo, w, b, top);
+          const float here = pairs_affine<E, true>(v + i * P, mo, w, b, top);
+          if (whole >> i & 1) top = here;
         }
+      edges([&](int i) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float2 f = unpack2(v[i * P + e / 2]);
+          if (units.in(t + i * tpr, e)) top = max_nan(top, fabsf(e & 1 ? f.y : f.x));
+        }
+      });
       uint32_t* tops = s_top[turn >> 1 & 1];
       uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
       if ((t & 31) == 0) tops[warp] = most;
@@ -579,154 +691,30 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1) k_layer_s
       const float scale = scale_of(__uint_as_float(most));
       const Reciprocal inv = reciprocal_of(scale);
       if (t == 0) p.scale.data[g * p.scale.group + gr] = scale;
+      e4m3* y = row_of<e4m3>(p.y, g, gr);
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (i < count) store_pairs_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * tpr) * E, v + i * P, inv);
+        if (whole >> i & 1) store_pairs_e4m3<E>(y + units.col(t + i * tpr), v + i * P, inv);
+      edges([&](int i) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float2 f = unpack2(v[i * P + e / 2]);
+          float one = e & 1 ? f.y : f.x;
+          scale_by<1>(&one, inv);
+          if (units.in(t + i * tpr, e)) store_e4m3<1>(y + units.col(t + i * tpr) + e, &one);
+        }
+      });
     } else {
+      T* y = row_of<T>(p.y, g, gr);
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (i < count) {
           uint64_t w[P], b[P];
           params(i, w, b);
           pairs_affine<E, false>(v + i * P, mo, w, b, 0.f);
-          store_pairs<T, E>(row_of<T>(p.y, g, gr) + (t + i * tpr) * E, v + i * P);
+          if (whole >> i & 1) store_pairs<T, E>(y + units.col(t + i * tpr), v + i * P);
         }
-    }
-    turn ^= 2;
-    if (++stage == stages) {
-      stage = 0;
-      turn ^= 1;
-    }
-  }
-  ring_done(q, err);
-}
-
-// ---- rows that start off the 16-byte grid (odd widths), all of a call's matrices at the same place of a 16-byte unit
-// in each row: threads take the whole units that a row touches. Weights and biases stand in shared memory.
-template <typename T, int E, int NV>
-__global__ void __launch_bounds__(512) k_layer_shift(const LayerArgs p, int stages, int slot, int* err) {
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float4 s_share[2][16];
-  __shared__ uint32_t s_top[2][16];
-  const bool has_res = p.residual.data;
-  const Ring q = ring_init(smem, stages, slot, has_res ? 2 : 1);
-  float* s_w = reinterpret_cast<float*>(smem + RING_BARS + stages * q.arrays * slot);
-  const int t = threadIdx.x, tpr = blockDim.x, dim = p.dim, bytes = dim * (int)sizeof(T);
-  float* s_b = s_w + padded<E>(dim + E);
-  const int warp = t >> 5, warps = tpr >> 5;
-  pdl_wait();
-  auto load = [&](int64_t r, int stage) {
-    const int64_t g = group_at(r, p.rows, p.total), gr = r - g * p.rows;
-    const char* src[3] = {(const char*)row_of<const T>(p.x, g, gr),
-                          has_res ? (const char*)row_of<const T>(p.residual, g, gr) : nullptr, nullptr};
-    ring_load(q, stage, src, bytes);
-  };
-  if (t == 0)
-    for (int s = 0; s < stages; ++s) {
-      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
-      if (r < p.total) load(r, s);
-    }
-  int64_t held_of = -1;  // the group whose parameters stand in shared memory
-  int stage = 0;
-  uint32_t turn = 0;
-  for (int64_t r = blockIdx.x; r < p.total; r += gridDim.x) {
-    const int64_t g = group_at(r, p.rows, p.total), gr = r - g * p.rows;
-    if (g != held_of) {
-      held_of = g;
-      const float* weight = p.weight.data + g * p.weight.group;
-      const float* bias = p.bias.data ? p.bias.data + g * p.bias.group : nullptr;
-      __syncthreads();
-      for (int c = t - E; c < dim + E; c += tpr) {
-        const bool in = c >= 0 && c < dim;
-        s_w[padded<E>(c)] = in ? weight[c] : 0.f, s_b[padded<E>(c)] = in && bias ? bias[c] : 0.f;
-      }
-      __syncthreads();
-    }
-    const int m = (int)((uint64_t)row_of<const T>(p.x, g, gr) & 15) / (int)sizeof(T);
-    const uint8_t* x = smem + RING_BARS + stage * q.arrays * slot;
-    ring_wait(q, stage, turn & 1);
-    float v[NV][E];
-    int held = 0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = t + i * tpr;
-      const Unit<E> u(c, m, dim);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[i][e] = 0.f;
-      if (u.live) {
-        load_vec<T, E>(reinterpret_cast<const T*>(x) + c * E, v[i]);
-        if (has_res) {
-          float w[E];
-          load_vec<T, E>(reinterpret_cast<const T*>(x + slot) + c * E, w);
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[i][e] += w[e];
-        }
-        if (!u.whole)
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (!u.in(e, dim)) v[i][e] = 0.f;
-        held += u.whole ? E : min(u.col + E, dim) - max(u.col, 0);
-        if (p.sum.data) store_unit<T, E>(row_of<T>(p.sum, g, gr), u, dim, v[i]);
-      }
-    }
-    const float sum = warp_sum(sum_of<E, NV>(v));
-    const float n = (float)__reduce_add_sync(0xffffffffu, held), own = n > 0.f ? sum / n : 0.f;
-    float m2 = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const Unit<E> u(t + i * tpr, m, dim);
-      if (u.live)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float off = u.in(e, dim) ? v[i][e] - own : 0.f;
-          m2 = fmaf(off, off, m2);
-        }
-    }
-    m2 = warp_sum(m2);
-    float4* shares = s_share[turn >> 1 & 1];
-    if ((t & 31) == 0) shares[warp] = make_float4(n, sum, own, m2);
-    __syncthreads();
-    if (t == 0 && r + (int64_t)stages * gridDim.x < p.total) load(r + (int64_t)stages * gridDim.x, stage);
-    const Moments mo = join_shares(shares, warps, p.inv_dim, p.eps);
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = t + i * tpr, at = c * (E + 1) + E - m;
-      const Unit<E> u(c, m, dim);
-      if (!u.live) continue;
-      // (beside the row weight and bias are zero, and so is what a non-finite mean does not make NaN)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int here = at + e + (e >= m);
-        v[i][e] = fmaf((v[i][e] - mo.mean) * mo.rstd, s_w[here], s_b[here]);
-        if (p.scale.data && u.in(e, dim)) top = max_nan(top, fabsf(v[i][e]));
-      }
-    }
-    Reciprocal inv{1.f, 0.f};
-    if (p.scale.data) {
-      uint32_t* tops = s_top[turn >> 1 & 1];
-      uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-      if ((t & 31) == 0) tops[warp] = most;
-      __syncthreads();
-      for (int i = 0; i < warps; ++i) most = max(most, tops[i]);
-      const float scale = scale_of(__uint_as_float(most));
-      inv = reciprocal_of(scale);
-      if (t == 0) p.scale.data[g * p.scale.group + gr] = scale;
-    }
-    if (t == 0) {
-      if (p.mean.data) p.mean.data[g * p.mean.group + gr] = mo.mean;
-      if (p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = mo.rstd;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const Unit<E> u(t + i * tpr, m, dim);
-      if (!u.live) continue;
-      if (p.scale.data) {
-        scale_by<E>(v[i], inv);
-        store_unit_e4m3<E>(row_of<e4m3>(p.y, g, gr), u, dim, v[i]);
-      } else {
-        store_unit<T, E>(row_of<T>(p.y, g, gr), u, dim, v[i]);
-      }
+      edges([&](int i) { store_edge<T, E>(y, units, t + i * tpr, rounded<T, E>(v + i * P)); });
     }
     turn ^= 2;
     if (++stage == stages) {
@@ -752,23 +740,30 @@ cudaError_t launch_short(const LayerArgs& p, cudaStream_t st) {
                     0, st, p);
 }
 
+// Blocks of a group (shift: whose rows must begin at the same place of a unit, 16 bytes' rows apart or alone).
+int64_t shift_blocks(int64_t blocks, int64_t rows, int u) {
+  if (blocks >= rows) return rows;
+  return blocks < u ? (rows < u ? rows : u) : blocks - blocks % u;
+}
+
 template <auto KERNEL>
-cudaError_t launch_rings(const LayerArgs& p, StreamShape s, cudaStream_t st) {
+cudaError_t launch_rings(const LayerArgs& p, StreamShape s, int shift, cudaStream_t st) {
   const cudaError_t e = allow_smem<KERNEL>();
   if (e != cudaSuccess) return e;
   static const int registers = registers_of((const void*)KERNEL);
   s.per_sm = blocks_resident(registers, s.tpr, s.per_sm);
   s.fit();
-  const int64_t blocks = (int64_t)s.per_sm * sm_count();
-  return launch_pdl(KERNEL, dim3((unsigned)(blocks < p.total ? blocks : p.total)), dim3(s.tpr), s.smem, st, p,
-                    s.stages, s.slot, timeout_word());
+  const int64_t groups = p.total / p.rows, fill = (int64_t)s.per_sm * sm_count();
+  const dim3 grid = shift ? dim3((unsigned)shift_blocks(ceil_div(fill, groups), p.rows, shift), (unsigned)groups)
+                          : dim3((unsigned)(fill < p.total ? fill : p.total));
+  return launch_pdl(KERNEL, grid, dim3(s.tpr), s.smem, st, p, s.stages, s.slot, timeout_word());
 }
 
-// Whether rows go to k_layer_shift: off the 16-byte grid, at the same place of a unit in all of the matrices.
+// Whether rows go by units: off the 16-byte grid, at the same place of a unit in all of the matrices.
 bool layer_shift(const LayerArgs& p) {
   const int e = 16 / type_bytes(p.x.type);
   const int64_t groups = p.total / p.rows;
-  return p.total > STREAM_ROWS * sm_count() && p.dim <= SHIFT_MAX_DIM && same_shift(p.x, p.y, groups, p.rows, e) &&
+  return p.total > STREAM_ROWS * sm_count() && p.dim <= SHIFT_DIM && same_shift(p.x, p.y, groups, p.rows, e) &&
          same_shift(p.x, p.residual, groups, p.rows, e) && same_shift(p.x, p.sum, groups, p.rows, e);
 }
 
@@ -788,14 +783,17 @@ cudaError_t launch_layer(LayerArgs& p, cudaStream_t st) {
     }
     if (many) {
       const StreamShape s = stream_shape(p.dim, E, sizeof(T), arrays, 2048, 0, E == 8);
-      return s.wide ? launch_rings<k_layer_stream<T, E, 32 / E>>(p, s, st)
-                    : launch_rings<k_layer_stream<T, E, 16 / E>>(p, s, st);
+      return s.wide ? launch_rings<k_layer_stream<T, E, 32 / E, false>>(p, s, 0, st)
+                    : launch_rings<k_layer_stream<T, E, 16 / E, false>>(p, s, 0, st);
     }
   } else if (layer_shift(p)) {
-    const StreamShape s = stream_shape(p.dim, U, sizeof(T), arrays, 2048, 2);
-    if (s.stages >= 1)
-      return s.wide ? launch_rings<k_layer_shift<T, U, 32 / U>>(p, s, st)
-                    : launch_rings<k_layer_shift<T, U, 16 / U>>(p, s, st);
+    // (a row touches a unit more than it fills)
+    // (of 32 elements per thread bf16 rows have no registers left: 16385 x 4097 172 us)
+    const int wide = (int)ceil_div(p.dim + U - 1, U) * U;
+    StreamShape s = stream_shape(wide, U, sizeof(T), arrays, 2048);
+    s.fixed = 2 * wide * 4;
+    s.share(2048);
+    return launch_rings<k_layer_stream<T, U, 16 / U, true>>(p, s, U, st);
   }
   // as many threads as vectors (of 4 single elements), so that a row takes one load latency
   constexpr int few = E == 1 ? 4 : 1;
@@ -916,12 +914,12 @@ __device__ __forceinline__ float warp_pair(float a, float b) {
   for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// The block's two sums, with one barrier; s: [2][16], by turns.
-__device__ __forceinline__ float2 block_pair_sum(float2 v, float2* s) {
-  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+// A team's two sums, with one barrier (its own, `id`); s: a place per warp, by turns.
+__device__ __forceinline__ float2 team_sum(float2 v, float2* s, int warp, int warps, int id) {
   const float w = warp_pair(v.x, v.y);
+  if (warps == 1) return make_float2(__shfl_sync(0xffffffffu, w, 0), __shfl_sync(0xffffffffu, w, 16));
   if ((threadIdx.x & 15) == 0) (&s[warp].x)[threadIdx.x >> 4 & 1] = w;
-  __syncthreads();
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory");
   float2 r = s[0];
 #pragma unroll 4
   for (int i = 1; i < warps; ++i) {
@@ -931,23 +929,28 @@ __device__ __forceinline__ float2 block_pair_sum(float2 v, float2* s) {
   return r;
 }
 
-// A vector of what was normalised, as it lies in memory: of dy's type, or a checkpoint's multiples and their unit.
-template <typename T, int E, bool KEPT>
+// A vector of what was normalised, as it lies in memory: of dy's type, or a checkpoint's multiples and their unit (SHIFT:
+// from a column that need not be a block's, so that the last `behind` elements may have another).
+template <typename T, int E, bool KEPT, bool SHIFT = false>
 struct Source {
   Raw<T, E> raw;
   __device__ __forceinline__ void zero() { raw.zero(); }
+  __device__ __forceinline__ void clear(int e) { raw.clear(e); }
   __device__ __forceinline__ void get(uint64_t* v) const { pairs_of<T, E>(raw, v); }
 };
-template <typename T, int E>
-struct Source<T, E, true> {
+template <typename T, int E, bool SHIFT>
+struct Source<T, E, true, SHIFT> {
   static_assert(E >= 4, "words");
-  uint32_t w[E / 4];
-  float unit;
+  uint32_t w[E / 4];  // multiples + 128
+  float unit, unit2;
+  int border;  // SHIFT: elements before it have the first unit
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (uint32_t& v : w) v = 0;
-    unit = 0.f;
+    unit = unit2 = 0.f;
+    border = E;
   }
+  __device__ __forceinline__ void clear(int e) { w[e / 4] = (w[e / 4] & ~(255u << e % 4 * 8)) | 128u << e % 4 * 8; }
   __device__ __forceinline__ void load(const int8_t* q, uint32_t byte) {
     if constexpr (E == 8) {
       const uint2 r = *reinterpret_cast<const uint2*>(q);
@@ -957,15 +960,27 @@ struct Source<T, E, true> {
     }
     unit = block_unit(byte);
   }
+  // From shared memory, at any byte, up to E - 1 of them before the row.
+  __device__ __forceinline__ void load(const uint8_t* q, const uint8_t* scale, int col, int dim) {
+    const uint8_t* from = q + col;
+    const uint32_t off = (uint32_t)(uint64_t)from & 3u;
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(from - off);
+    uint32_t r[E / 4 + 1];
+#pragma unroll
+    for (int j = 0; j <= E / 4; ++j) r[j] = words[j];
+#pragma unroll
+    for (int j = 0; j < E / 4; ++j) w[j] = __funnelshift_r(r[j], r[j + 1], off * 8) ^ 0x80808080u;
+    const int first = max(col, 0), last = min(col + E, dim) - 1;
+    unit = block_unit(scale[first / LIPZ_BLOCK]), unit2 = block_unit(scale[last / LIPZ_BLOCK]);
+    border = (first | (LIPZ_BLOCK - 1)) + 1 - col;
+  }
   __device__ __forceinline__ void get(uint64_t* v) const {
 #pragma unroll
-    for (int i = 0; i < E / 4; ++i) {
-      const uint64_t a = pack2(__uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7440)),
-                               __uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7441)));
-      const uint64_t b = pack2(__uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7442)),
-                               __uint_as_float(__byte_perm(w[i], 0x4B000000u, 0x7443)));
-      v[2 * i] = mul2(add2(a, both(-8388736.f)), both(unit));
-      v[2 * i + 1] = mul2(add2(b, both(-8388736.f)), both(unit));
+    for (int i = 0; i < E / 2; ++i) {
+      const uint64_t a = pack2(__uint_as_float(__byte_perm(w[i / 2], 0x4B000000u, i & 1 ? 0x7442 : 0x7440)),
+                               __uint_as_float(__byte_perm(w[i / 2], 0x4B000000u, i & 1 ? 0x7443 : 0x7441)));
+      const uint64_t by = SHIFT ? pack2(2 * i < border ? unit : unit2, 2 * i + 1 < border ? unit : unit2) : both(unit);
+      v[i] = mul2(add2(a, both(-8388736.f)), by);
     }
   }
 };
@@ -994,9 +1009,9 @@ __device__ __forceinline__ void add_terms(Terms& t, const Raw<T, E>& dy, const u
 }
 // dx = rstd (g - c1 - (s - mean) c2) + dsum
 template <typename T, int E>
-__device__ __forceinline__ void store_gradient(T* dx, const Raw<T, E>& dy, const uint64_t* s, const uint64_t* w,
-                                               const Raw<T, E>& ds, float mean, float rstd, float c1, float c2) {
-  uint64_t d[E / 2], v[E / 2];
+__device__ __forceinline__ void gradient(uint64_t* v, const Raw<T, E>& dy, const uint64_t* s, const uint64_t* w,
+                                         const Raw<T, E>& ds, float mean, float rstd, float c1, float c2) {
+  uint64_t d[E / 2];
   pairs_of<T, E>(dy, d);
   pairs_of<T, E>(ds, v);
 #pragma unroll
@@ -1004,7 +1019,6 @@ __device__ __forceinline__ void store_gradient(T* dx, const Raw<T, E>& dy, const
     const uint64_t a = fma2(add2(s[j], both(-mean)), both(-c2), fma2(d[j], w[j], both(-c1)));
     v[j] = fma2(both(rstd), a, v[j]);
   }
-  store_pairs<T, E>(dx, v);
 }
 
 // Where a stage's rows stand, and how many bytes one has: of dy, of what was normalised, of its scales, of dsum.
@@ -1047,21 +1061,38 @@ __device__ __forceinline__ void back_rows(const LayerBack& p, int64_t g, int64_t
   src[3] = p.dsum.data ? row_of<const T>(p.dsum, g, r) : nullptr;
 }
 
-// A block of one row's threads walks over rows of one group (blockIdx.y), which arrive in a ring; its sums for dweight
-// and dbias stay in registers.
-template <typename T, int E, int NV, bool KEPT>
-__global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, const BackStage b, int stages, int slot,
-                                                           int* err) {
+// Teams of one row's threads, several to a block, walk over rows of one group (blockIdx.y), which arrive in a ring of
+// each; their sums for dweight and dbias stay in registers, and of 16 elements the weights. At the end the teams' sums are
+// added in shared memory: one part per SM is left for the launch that adds those (16384 x 2048 over a checkpoint: with a
+// part per team 65 us, 7 of them that launch; so BACK_NOW). SHIFT: rows off the 16-byte grid, as in k_layer_stream; a
+// checkpoint's row lies at any byte: its multiples come from the words that hold them, and a unit's columns from two
+// blocks at most.
+template <typename T, int E, int NV, bool KEPT, bool SHIFT>
+__global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, const BackStage b, int tpr, int stages,
+                                                           int slot, int* err) {
+  constexpr int P = E / 2;
+  constexpr bool HELD = NV * E == 16;
+  static_assert(!SHIFT || HELD, "weights in registers");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float2 s_red[2][16];
-  constexpr int P = E / 2;
   const bool has_dsum = p.dsum.data;
-  const Ring q = ring_init(smem, stages, slot, 1);
-  const int64_t g = blockIdx.y;
-  const int t = threadIdx.x, tpr = blockDim.x, nvec = p.dim / E;
+  const int teams = blockDim.x / tpr, team = threadIdx.x / tpr, t = threadIdx.x - team * tpr, warps = tpr >> 5;
+  const int ring_bytes = RING_BARS + stages * slot;
+  uint8_t* ring = smem + team * ring_bytes;
+  const Ring q = ring_of(ring, stages, slot, 1);
+  if (t == 0) ring_set_up(q);
+  __syncthreads();
+  const int64_t g = blockIdx.y, first = (int64_t)blockIdx.x * teams + team, step = (int64_t)gridDim.x * teams;
+  const Units<E> units{SHIFT ? (int)((uint64_t)row_of<const T>(p.dy, g, first) & 15) / (int)sizeof(T) : 0, p.dim};
   int count = 0;
+  bool edge = false;  // the row has some of this thread's vectors in part
 #pragma unroll
-  for (int i = 0; i < NV; ++i) count += t + i * tpr < nvec;
+  for (int i = 0; i < NV; ++i) {
+    const int c = t + i * tpr;
+    if (!units.live(c)) continue;
+    ++count;
+    if (SHIFT && !units.whole(c)) edge = true;
+  }
   pdl_wait();
   auto load = [&](int64_t r, int stage) {
     const void* src[4];
@@ -1070,193 +1101,128 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
   };
   if (t == 0)
     for (int s = 0; s < stages; ++s) {
-      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
+      const int64_t r = first + s * step;
       if (r < p.rows) load(r, s);
     }
   const float* weight = p.weight.data + g * p.weight.group;
-  uint64_t dw[NV][P], db[NV][P];
+  uint64_t dw[NV][P], db[NV][P], hw[HELD ? NV : 1][P];
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < P; ++j) dw[i][j] = db[i][j] = 0;
+    if constexpr (HELD) {
+      if (SHIFT) units.params(weight, t + i * tpr, hw[i]);
+      else if (i < count) load_pairs<E>(weight + (t + i * tpr) * E, hw[i]);
+    }
+  }
+  const float *means = p.mean.data + g * p.mean.group, *rstds = p.rstd.data + g * p.rstd.group;
+  float next_mean = 0.f, next_rstd = 0.f;  // (of the row after this one: in flight while this one is worked on)
+  if (first < p.rows) next_mean = __ldg(means + first), next_rstd = __ldg(rstds + first);
+  // a checkpoint's rows begin anywhere in their 16-byte units
+  uint32_t low_q = 0, low_scale = 0, step_q = 0, step_scale = 0;
+  if constexpr (KEPT) {
+    low_q = (uint32_t)(uint64_t)(p.kept.data + g * p.kept.group + first * p.kept.row);
+    low_scale = (uint32_t)(uint64_t)(p.kept.scale + g * p.kept.scale_group + first * p.kept.scale_row);
+    step_q = (uint32_t)(step * p.kept.row), step_scale = (uint32_t)(step * p.kept.scale_row);
+  }
+  T* dx = row_of<T>(p.dx, g, first);
+  const int64_t dx_step = step * p.dx.row;
   int stage = 0;
   uint32_t turn = 0;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-    const float mean = p.mean.data[g * p.mean.group + r], rstd = p.rstd.data[g * p.rstd.group + r];
-    const void* src[4];
-    back_rows<T, KEPT>(p, g, r, src);
-    const uint8_t* rows[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) rows[i] = smem + RING_BARS + stage * slot + b.at[i] + ((uint64_t)src[i] & 15);
+  for (int64_t r = first; r < p.rows; r += step) {
+    const float mean = next_mean, rstd = next_rstd;
+    if (r + step < p.rows) next_mean = __ldg(means + r + step), next_rstd = __ldg(rstds + r + step);
+    const uint8_t* at = ring + RING_BARS + stage * slot;
+    const uint8_t *at_q = at + b.at[1] + (low_q & 15), *at_scale = at + b.at[2] + (low_scale & 15);
     ring_wait(q, stage, turn & 1);
     Raw<T, E> dy[NV], ds[NV];
-    Source<T, E, KEPT> x[NV];
+    Source<T, E, KEPT, SHIFT> x[NV];
     Terms terms;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * tpr) * E;
+      const int c = t + i * tpr;
       dy[i].zero(), x[i].zero(), ds[i].zero();
       if (i < count) {
-        dy[i].load(reinterpret_cast<const T*>(rows[0]) + c);
-        if constexpr (KEPT) x[i].load(reinterpret_cast<const int8_t*>(rows[1]) + c, rows[2][c / LIPZ_BLOCK]);
-        else x[i].raw.load(reinterpret_cast<const T*>(rows[1]) + c);
-        if (has_dsum) ds[i].load(reinterpret_cast<const T*>(rows[3]) + c);
+        dy[i].load(reinterpret_cast<const T*>(at + b.at[0]) + c * E);
+        if constexpr (KEPT && SHIFT)
+          x[i].load(at_q, at_scale, units.col(c), p.dim);
+        else if constexpr (KEPT)
+          x[i].load(reinterpret_cast<const int8_t*>(at_q) + c * E, at_scale[c * E / LIPZ_BLOCK]);
+        else
+          x[i].raw.load(reinterpret_cast<const T*>(at + b.at[1]) + c * E);
+        if (has_dsum) ds[i].load(reinterpret_cast<const T*>(at + b.at[3]) + c * E);
+        if (SHIFT && edge) {  // (what lies beside the row adds nothing, whatever it is)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (!units.in(c, e)) dy[i].clear(e), x[i].clear(e);
+        }
         uint64_t w[P], s[P];
-        load_pairs<E>(weight + c, w);
+        if constexpr (!HELD) load_pairs<E>(weight + c * E, w);
         x[i].get(s);
-        add_terms<T, E>(terms, dy[i], s, w, mean, rstd, dw[i], db[i]);
+        add_terms<T, E>(terms, dy[i], s, HELD ? hw[HELD ? i : 0] : w, mean, rstd, dw[i], db[i]);
       }
     }
-    const float2 along = block_pair_sum(terms.sums(), s_red[turn >> 1 & 1]);
-    if (t == 0 && r + (int64_t)stages * gridDim.x < p.rows) load(r + (int64_t)stages * gridDim.x, stage);
+    const float2 along = team_sum(terms.sums(), s_red[turn >> 1 & 1] + team * warps, t >> 5, warps, team + 1);
+    if (t == 0 && r + stages * step < p.rows) load(r + stages * step, stage);
     // (rstd^2 by itself may be infinite where the gradient is not)
     const float c1 = along.x * p.inv_dim, c2 = rstd * (rstd * (along.y * p.inv_dim));
-    T* dx = row_of<T>(p.dx, g, r);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i < count) {
-        const int c = (t + i * tpr) * E;
-        uint64_t w[P], s[P];
-        load_pairs<E>(weight + c, w);
+        const int c = t + i * tpr;
+        uint64_t w[P], s[P], v[P];
+        if constexpr (!HELD) load_pairs<E>(weight + c * E, w);
         x[i].get(s);
-        store_gradient<T, E>(dx + c, dy[i], s, w, ds[i], mean, rstd, c1, c2);
+        gradient<T, E>(v, dy[i], s, HELD ? hw[HELD ? i : 0] : w, ds[i], mean, rstd, c1, c2);
+        if (SHIFT && edge && !units.whole(c)) store_edge<T, E>(dx, units, c, rounded<T, E>(v));
+        else store_pairs<T, E>(dx + units.col(c), v);
       }
+    dx += dx_step;
+    low_q += step_q, low_scale += step_scale;
     turn ^= 2;
     if (++stage == stages) {
       stage = 0;
       turn ^= 1;
     }
   }
-  ring_done(q, err);
+  __syncthreads();
+  int code = 0;  // a wait that expired: copies in flight land before the block leaves, or its rings are written over
+  for (int k = 0; k < teams; ++k)
+    if (*reinterpret_cast<volatile int*>(smem + k * ring_bytes + 8 * RING_MAX))
+      code = *reinterpret_cast<volatile int*>(smem + k * ring_bytes + 8 * RING_MAX + 4);
+  if (code) {
+    const unsigned long long t0 = tc::globaltimer();
+    while (tc::globaltimer() - t0 < 200000ull) {
+    }
+    if (threadIdx.x == 0 && err) *reinterpret_cast<volatile int*>(err) = code;
+  }
+  if (!p.dweight.data && !p.dbias.data) return;
   const SumsOut out = sums_out(p, g);
+  float* s_sums = reinterpret_cast<float*>(smem);  // [teams][2][dim], over the rings
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < NV; ++i)
     if (i < count)
 #pragma unroll
-      for (int j = 0; j < P; ++j) {
-        const int c = (t + i * tpr) * E + 2 * j;
-        const float2 a = unpack2(dw[i][j]), b = unpack2(db[i][j]);
-        if (out.dw) out.dw[c] = a.x, out.dw[c + 1] = a.y;
-        if (out.db) out.db[c] = b.x, out.db[c + 1] = b.y;
-      }
-}
-
-// Rows off the 16-byte grid, in the units of dy: a column is another thread's in every row, so its sums stand in
-// shared memory, beside the weights. A checkpoint's row lies at any byte: its multiples come from the words that hold
-// them, and a unit's columns from two blocks at most.
-template <typename T, int E, int NV, bool KEPT>
-__global__ void __launch_bounds__(512) k_layer_back_shift(const LayerBack p, const BackStage b, int stages, int slot,
-                                                          int* err) {
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float2 s_red[2][16];
-  const bool has_dsum = p.dsum.data;
-  const Ring q = ring_init(smem, stages, slot, 1);
-  const int64_t g = blockIdx.y;
-  const int t = threadIdx.x, tpr = blockDim.x, dim = p.dim;
-  float* s_w = reinterpret_cast<float*>(smem + RING_BARS + stages * slot);
-  float *s_dw = s_w + padded<E>(dim + E), *s_db = s_dw + padded<E>(dim + E);
-  pdl_wait();
-  auto load = [&](int64_t r, int stage) {
-    const void* src[4];
-    back_rows<T, KEPT>(p, g, r, src);
-    load_stage(q, b, stage, src);
-  };
-  if (t == 0)
-    for (int s = 0; s < stages; ++s) {
-      const int64_t r = blockIdx.x + (int64_t)s * gridDim.x;
-      if (r < p.rows) load(r, s);
-    }
-  const float* weight = p.weight.data + g * p.weight.group;
-  for (int c = t - E; c < dim + E; c += tpr) {
-    const int at = padded<E>(c);
-    s_w[at] = c >= 0 && c < dim ? weight[c] : 0.f, s_dw[at] = s_db[at] = 0.f;
-  }
-  __syncthreads();
-  int stage = 0;
-  uint32_t turn = 0;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-    const float mean = p.mean.data[g * p.mean.group + r], rstd = p.rstd.data[g * p.rstd.group + r];
-    const void* src[4];
-    back_rows<T, KEPT>(p, g, r, src);
-    const int m = (int)((uint64_t)src[0] & 15) / (int)sizeof(T);
-    const uint8_t* rows = smem + RING_BARS + stage * slot;
-    const uint8_t* scales = rows + b.at[2] + ((uint64_t)src[2] & 15);
-    ring_wait(q, stage, turn & 1);
-    Raw<T, E> dy[NV], ds[NV];
-    float x[NV][E];  // s - mean
-    float2 along = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = t + i * tpr;
-      const Unit<E> u(c, m, dim);
-      dy[i].zero(), ds[i].zero();
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[i][e] = 0.f;
-      if (!u.live) continue;
-      dy[i].load(reinterpret_cast<const T*>(rows + b.at[0]) + c * E);
-      if (has_dsum) ds[i].load(reinterpret_cast<const T*>(rows + b.at[3]) + c * E);
-      if constexpr (KEPT) {
-        // (before the row's first column there are up to E - 1 bytes; its slot leaves room for them)
-        const int from = b.at[1] + (int)((uint64_t)src[1] & 15) + u.col, off = from & 3;
-        const uint32_t* words = reinterpret_cast<const uint32_t*>(rows + (from - off));
-        uint32_t w[E / 4 + 1];
-#pragma unroll
-        for (int j = 0; j <= E / 4; ++j) w[j] = words[j];
-        const int first = max(u.col, 0) / LIPZ_BLOCK, last = min(u.col + E - 1, dim - 1) / LIPZ_BLOCK;
-        const float unit0 = block_unit(scales[first]), unit1 = block_unit(scales[last]);
-        float one[E];
-#pragma unroll
-        for (int j = 0; j < E / 4; ++j) block_values(__funnelshift_r(w[j], w[j + 1], off * 8), 1.f, one + 4 * j);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          x[i][e] = one[e] * ((u.col + e) / LIPZ_BLOCK == first || u.col + e < 0 ? unit0 : unit1);
-      } else {
-        load_vec<T, E>(reinterpret_cast<const T*>(rows + b.at[1]) + c * E, x[i]);
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[i][e] -= mean;
-      if (!u.whole)  // (what lies beside the row adds nothing, whatever it is)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (!u.in(e, dim)) dy[i].clear(e), x[i][e] = 0.f;
-      const int at = c * (E + 1) + E - m;  // padded<E>(c E - m + e) = at + e, and from e = m on one more
-#pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int here = at + e + (e >= m);
-        const float d = dy[i].get(e), xd = d * x[i][e], we = s_w[here];
-        s_dw[here] = fmaf(xd, rstd, s_dw[here]);
-        s_db[here] += d;
-        along.x = fmaf(d, we, along.x);
-        along.y = fmaf(xd, we, along.y);
+        const int c = units.col(t + i * tpr) + e;
+        const float2 a = unpack2(dw[i][e / 2]), d = unpack2(db[i][e / 2]);
+        if (SHIFT && !units.in(t + i * tpr, e)) continue;
+        if (teams > 1) {
+          s_sums[team * 2 * p.dim + c] = e & 1 ? a.y : a.x, s_sums[(team * 2 + 1) * p.dim + c] = e & 1 ? d.y : d.x;
+          continue;
+        }
+        if (out.dw) out.dw[c] = e & 1 ? a.y : a.x;
+        if (out.db) out.db[c] = e & 1 ? d.y : d.x;
       }
-    }
-    // (the next row's sums for a column follow after this barrier)
-    along = block_pair_sum(along, s_red[turn >> 1 & 1]);
-    if (t == 0 && r + (int64_t)stages * gridDim.x < p.rows) load(r + (int64_t)stages * gridDim.x, stage);
-    const float c1 = along.x * p.inv_dim, c2 = rstd * (rstd * (along.y * p.inv_dim));
-    T* dx = row_of<T>(p.dx, g, r);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = t + i * tpr, at = c * (E + 1) + E - m;
-      const Unit<E> u(c, m, dim);
-      if (!u.live) continue;
-      float v[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        v[e] = fmaf(rstd, fmaf(-x[i][e], c2, fmaf(dy[i].get(e), s_w[at + e + (e >= m)], -c1)), ds[i].get(e));
-      store_unit<T, E>(dx, u, dim, v);
-    }
-    turn ^= 2;
-    if (++stage == stages) {
-      stage = 0;
-      turn ^= 1;
-    }
-  }
-  ring_done(q, err);
-  const SumsOut out = sums_out(p, g);
-  for (int c = t; c < dim; c += tpr) {
-    if (out.dw) out.dw[c] = s_dw[padded<E>(c)];
-    if (out.db) out.db[c] = s_db[padded<E>(c)];
+  if (teams == 1) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * p.dim; c += blockDim.x) {
+    float v = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < teams; ++k) v += s_sums[k * 2 * p.dim + c];
+    if (c < p.dim && out.dw) out.dw[c] = v;
+    if (c >= p.dim && out.db) out.db[c - p.dim] = v;
   }
 }
 
@@ -1340,9 +1306,10 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i < count) {
-        uint64_t s[P];
+        uint64_t s[P], v[P];
         y[i].get(s);
-        store_gradient<T, E>(dx + (t + i * L) * E, a[i], s, w[i], c3[i], m, f, c1, c2);
+        gradient<T, E>(v, a[i], s, w[i], c3[i], m, f, c1, c2);
+        store_pairs<T, E>(dx + (t + i * L) * E, v);
       }
   }
   if (!p.dweight.data && !p.dbias.data) return;
@@ -1414,9 +1381,10 @@ bool back_vec(const lipz_layernorm_backward_args& a) {
 // element by element; its blocks per group, whose sums are parts where there are several.
 struct BackPlan {
   enum { SHORT, STREAM, SHIFT, SINGLE } kind;
-  StreamShape s;
+  StreamShape s;  // (per_sm: teams of a block, one to an SM)
   BackStage stage;
   int blocks;
+  int teams() const { return s.per_sm; }
 };
 // Lanes of a row in k_layer_back_short, two vectors to each (past 32: four to each of 32).
 int back_lanes(int64_t nvec) {
@@ -1425,13 +1393,12 @@ int back_lanes(int64_t nvec) {
   return lanes;
 }
 // A block of 16 elements per thread (32 where 512 threads do not reach a row's end), and its ring.
-StreamShape back_shape(const lipz_layernorm_backward_args& a, int params, BackStage* b) {
+StreamShape back_shape(const lipz_layernorm_backward_args& a, BackStage* b) {
   const int eb = type_bytes(a.dy.type), e = 16 / eb, dim = (int)a.dim;
-  const int nvec = params ? (int)ceil_div(dim + 2 * e - 2, e) : dim / e;
+  const int nvec = (int)ceil_div(dim + (back_vec(a) ? 0 : e - 1), e);
   StreamShape s{};
   s.wide = row_threads(nvec, 16 / e) > 512;
   s.tpr = row_threads(nvec, (s.wide ? 32 : 16) / e);
-  s.fixed = params * ((dim + 2 * e) / e + 1) * (e + 1) * 4;  // (padded)
   const int bytes[4] = {dim * eb, a.kept.data ? dim : dim * eb,
                         a.kept.data ? (int)ceil_div(dim, LIPZ_BLOCK) : 0, a.dsum.data ? dim * eb : 0};
   int at = 0;
@@ -1440,6 +1407,7 @@ StreamShape back_shape(const lipz_layernorm_backward_args& a, int params, BackSt
     if (bytes[i]) at += (int)ceil_div(bytes[i], 16) * 16 + 32;  // (a unit before the row, and one after)
   }
   s.row = s.slot = at;
+  s.share(512);
   return s;
 }
 
@@ -1454,7 +1422,7 @@ BackPlan back_plan(const lipz_layernorm_backward_args& a) {
   };
   if (back_vec(a)) {
     const int64_t nvec = a.dim / e;
-    if (nvec <= 128) {
+    if (nvec <= 64) {
       b.kind = BackPlan::SHORT;
       const int lanes = back_lanes(nvec);
       const int warps = lanes > 32 ? BACK_WARPS<4> : BACK_WARPS<2>, set = warps * (lanes > 32 ? 1 : 32 / lanes);
@@ -1465,20 +1433,17 @@ BackPlan back_plan(const lipz_layernorm_backward_args& a) {
       return b;
     }
     b.kind = BackPlan::STREAM;
-    b.s = back_shape(a, 0, &b.stage);
-    b.s.share(b.s.wide ? 512 : 640);
-    b.blocks = blocks(b.s.per_sm, 4);
+    b.s = back_shape(a, &b.stage);
+    b.blocks = blocks(1, 4 * b.teams());
     return b;
   }
   auto same = [&](const lipz_mat& m) { return same_shift(a.dy, m, a.groups, a.rows, e); };
-  if (same(a.dx) && same(a.dsum) && (a.kept.data || same(a.s))) {
-    b.s = back_shape(a, 3, &b.stage);
-    b.s.share(1024);
-    if (b.s.stages >= 1) {
-      b.kind = BackPlan::SHIFT;
-      b.blocks = blocks(b.s.per_sm, 4);
-      return b;
-    }
+  if (a.dim <= SHIFT_DIM && same(a.dx) && same(a.dsum) && (a.kept.data || same(a.s))) {
+    b.kind = BackPlan::SHIFT;
+    b.s = back_shape(a, &b.stage);
+    b.blocks = (int)shift_blocks(blocks(1, 4 * b.teams()), ceil_div(a.rows, b.teams()), e);
+    if (b.blocks < 1) b.blocks = 1;
+    return b;
   }
   b.kind = BackPlan::SINGLE;
   b.blocks = blocks(2, 4);
@@ -1488,9 +1453,10 @@ BackPlan back_plan(const lipz_layernorm_backward_args& a) {
 template <auto KERNEL>
 cudaError_t launch_back_rings(const LayerBack& p, const BackPlan& b, int64_t groups, cudaStream_t st) {
   const cudaError_t e = allow_smem<KERNEL>();
-  return e != cudaSuccess ? e
-                          : launch_pdl(KERNEL, dim3(b.blocks, (unsigned)groups), dim3(b.s.tpr), b.s.smem, st, p,
-                                       b.stage, b.s.stages, b.s.slot, timeout_word());
+  if (e != cudaSuccess) return e;
+  const int sums = b.teams() > 1 ? b.teams() * 2 * p.dim * 4 : 0, rings = b.teams() * b.s.smem;
+  return launch_pdl(KERNEL, dim3(b.blocks, (unsigned)groups), dim3(b.s.tpr * b.teams()), rings > sums ? rings : sums, st,
+                    p, b.stage, b.s.tpr, b.s.stages, b.s.slot, timeout_word());
 }
 template <typename T, int E, int NV, int L, bool KEPT>
 cudaError_t launch_back_short(const LayerBack& p, int64_t groups, int blocks, cudaStream_t st) {
@@ -1512,11 +1478,9 @@ cudaError_t launch_back(const LayerBack& p, const BackPlan& b, int64_t groups, c
     return launch_back_short<T, E, 2, 4, KEPT>(p, groups, b.blocks, st);
   }
   if (b.kind == BackPlan::STREAM)
-    return b.s.wide ? launch_back_rings<k_layer_back_stream<T, E, 32 / E, KEPT>>(p, b, groups, st)
-                    : launch_back_rings<k_layer_back_stream<T, E, 16 / E, KEPT>>(p, b, groups, st);
-  if (b.kind == BackPlan::SHIFT)
-    return b.s.wide ? launch_back_rings<k_layer_back_shift<T, E, 32 / E, KEPT>>(p, b, groups, st)
-                    : launch_back_rings<k_layer_back_shift<T, E, 16 / E, KEPT>>(p, b, groups, st);
+    return b.s.wide ? launch_back_rings<k_layer_back_stream<T, E, 32 / E, KEPT, false>>(p, b, groups, st)
+                    : launch_back_rings<k_layer_back_stream<T, E, 16 / E, KEPT, false>>(p, b, groups, st);
+  if (b.kind == BackPlan::SHIFT) return launch_back_rings<k_layer_back_stream<T, E, 16 / E, KEPT, true>>(p, b, groups, st);
   const int nv = row_threads(p.dim, 16) <= 512 ? 16 : 32;
   const dim3 grid(b.blocks, (unsigned)groups), block(row_threads(p.dim, nv));
   return nv == 16 ? launch_pdl(k_layer_backward<T, 16, KEPT>, grid, block, 0, st, p)

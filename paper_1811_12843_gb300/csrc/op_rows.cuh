@@ -83,20 +83,26 @@ struct Ring {
   int* code;
 };
 
-__device__ __forceinline__ Ring ring_init(uint8_t* smem, int stages, int slot, int arrays) {
+__device__ __forceinline__ Ring ring_of(uint8_t* smem, int stages, int slot, int arrays) {
   Ring q;
   q.bars = tc::smem_u32(smem);
   q.data = q.bars + RING_BARS;
   q.stages = stages, q.slot = slot, q.arrays = arrays;
   q.abort_flag = reinterpret_cast<volatile int*>(smem + 8 * RING_MAX);
   q.code = reinterpret_cast<int*>(smem + 8 * RING_MAX + 4);
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < stages; ++s) tc::mbar_init(q.bars + 8 * s, 1);
-    *q.abort_flag = 0;
-    *q.code = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
+  return q;
+}
+// One thread, before a barrier of those that use the ring.
+__device__ __forceinline__ void ring_set_up(const Ring& q) {
+  for (int s = 0; s < q.stages; ++s) tc::mbar_init(q.bars + 8 * s, 1);
+  *q.abort_flag = 0;
+  *q.code = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+__device__ __forceinline__ Ring ring_init(uint8_t* smem, int stages, int slot, int arrays) {
+  const Ring q = ring_of(smem, stages, slot, arrays);
+  if (threadIdx.x == 0) ring_set_up(q);
   __syncthreads();
   return q;
 }

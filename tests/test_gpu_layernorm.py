@@ -402,11 +402,13 @@ def block_inputs(groups, rows, dim, hidden, seed=91):
 
 @pytest.mark.parametrize("groups,rows,dim,hidden", [(1, 37, 100, 333), (5, 100, 256, 512), (1, 700, 784, 1001)])
 def test_a_block_in_8_bits(groups, rows, dim, hidden):
-    """The results are the same; gradients are off by what half a step of each block, 2^-7 of its largest at most and
-    as good as random, does to them: below 2^-5 of a gradient's rms, as are bf16's own roundings."""
+    """The sum is the same, and y but for the order of its sums, which may move a rounding to bf16 (2^-8 of an element at
+    most) of h or of y; gradients are off by what half a step of each block, 2^-7 of its largest at most and as good as
+    random, does to them: below 2^-5 of a gradient's rms, as are bf16's own roundings."""
     x, stream, p = block_inputs(groups, rows, dim, hidden)
     whole, kept = block(x, stream, p, False), block(x, stream, p, True)
-    assert torch.equal(whole[0], kept[0]) and torch.equal(whole[1], kept[1])
+    assert torch.equal(whole[1], kept[1])
+    assert (d(whole[0]) - d(kept[0])).square().mean().sqrt() <= 2.0 ** -8 * d(whole[0]).square().mean().sqrt()
     for a, b in zip(whole[2:], kept[2:]):
         assert a.shape == b.shape and a.dtype == b.dtype
         assert ((d(a) - d(b)).square().mean().sqrt() <= 2.0 ** -5 * d(a).square().mean().sqrt())
