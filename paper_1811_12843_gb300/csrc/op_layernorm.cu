@@ -985,7 +985,7 @@ struct Source<T, E, true, SHIFT> {
   }
 };
 
-// A vector's terms: of the two sums along the row (g, and g (s - mean)) and of those down the columns.
+// A vector's terms (x: s - mean): of the two sums along the row (g, and g x) and of those down the columns.
 struct Terms {
   uint64_t along_g = 0, along_x = 0;
   __device__ __forceinline__ float2 sums() const {
@@ -993,14 +993,19 @@ struct Terms {
     return make_float2(a.x + a.y, b.x + b.y);
   }
 };
+template <int E>
+__device__ __forceinline__ void take_mean(uint64_t* s, float mean) {
+#pragma unroll
+  for (int j = 0; j < E / 2; ++j) s[j] = add2(s[j], both(-mean));
+}
 template <typename T, int E>
-__device__ __forceinline__ void add_terms(Terms& t, const Raw<T, E>& dy, const uint64_t* s, const uint64_t* w,
-                                          float mean, float rstd, uint64_t* dw, uint64_t* db) {
+__device__ __forceinline__ void add_terms(Terms& t, const Raw<T, E>& dy, const uint64_t* x, const uint64_t* w,
+                                          float rstd, uint64_t* dw, uint64_t* db) {
   uint64_t d[E / 2];
   pairs_of<T, E>(dy, d);
 #pragma unroll
   for (int j = 0; j < E / 2; ++j) {
-    const uint64_t m = mul2(d[j], add2(s[j], both(-mean)));
+    const uint64_t m = mul2(d[j], x[j]);
     dw[j] = fma2(m, both(rstd), dw[j]);
     db[j] = add2(d[j], db[j]);
     t.along_g = fma2(d[j], w[j], t.along_g);
@@ -1009,14 +1014,14 @@ __device__ __forceinline__ void add_terms(Terms& t, const Raw<T, E>& dy, const u
 }
 // dx = rstd (g - c1 - (s - mean) c2) + dsum
 template <typename T, int E>
-__device__ __forceinline__ void gradient(uint64_t* v, const Raw<T, E>& dy, const uint64_t* s, const uint64_t* w,
-                                         const Raw<T, E>& ds, float mean, float rstd, float c1, float c2) {
+__device__ __forceinline__ void gradient(uint64_t* v, const Raw<T, E>& dy, const uint64_t* x, const uint64_t* w,
+                                         const Raw<T, E>& ds, float rstd, float c1, float c2) {
   uint64_t d[E / 2];
   pairs_of<T, E>(dy, d);
   pairs_of<T, E>(ds, v);
 #pragma unroll
   for (int j = 0; j < E / 2; ++j) {
-    const uint64_t a = fma2(add2(s[j], both(-mean)), both(-c2), fma2(d[j], w[j], both(-c1)));
+    const uint64_t a = fma2(x[j], both(-c2), fma2(d[j], w[j], both(-c1)));
     v[j] = fma2(both(rstd), a, v[j]);
   }
 }
@@ -1067,14 +1072,16 @@ __device__ __forceinline__ void back_rows(const LayerBack& p, int64_t g, int64_t
 // part per team 65 us, 7 of them that launch; so BACK_NOW). SHIFT: rows off the 16-byte grid, as in k_layer_stream; a
 // checkpoint's row lies at any byte: its multiples come from the words that hold them, and a unit's columns from two
 // blocks at most.
+constexpr int TEAM_THREADS = 512;  // of a block (registers)
+
 template <typename T, int E, int NV, bool KEPT, bool SHIFT>
-__global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, const BackStage b, int tpr, int stages,
+__global__ void __launch_bounds__(TEAM_THREADS) k_layer_back_stream(const LayerBack p, const BackStage b, int tpr, int stages,
                                                            int slot, int* err) {
   constexpr int P = E / 2;
   constexpr bool HELD = NV * E == 16;
   static_assert(!SHIFT || HELD, "weights in registers");
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float2 s_red[2][16];
+  __shared__ float2 s_red[2][TEAM_THREADS / 32];
   const bool has_dsum = p.dsum.data;
   const int teams = blockDim.x / tpr, team = threadIdx.x / tpr, t = threadIdx.x - team * tpr, warps = tpr >> 5;
   const int ring_bytes = RING_BARS + stages * slot;
@@ -1135,48 +1142,65 @@ __global__ void __launch_bounds__(512) k_layer_back_stream(const LayerBack p, co
     const uint8_t* at = ring + RING_BARS + stage * slot;
     const uint8_t *at_q = at + b.at[1] + (low_q & 15), *at_scale = at + b.at[2] + (low_scale & 15);
     ring_wait(q, stage, turn & 1);
-    Raw<T, E> dy[NV], ds[NV];
-    Source<T, E, KEPT, SHIFT> x[NV];
-    Terms terms;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    // A vector of dy and of what was normalised; zeros where neither is the row's (what lies beside it adds nothing).
+    auto take = [&](int i, Raw<T, E>& dy, uint64_t* v) {
       const int c = t + i * tpr;
-      dy[i].zero(), x[i].zero(), ds[i].zero();
-      if (i < count) {
-        dy[i].load(reinterpret_cast<const T*>(at + b.at[0]) + c * E);
-        if constexpr (KEPT && SHIFT)
-          x[i].load(at_q, at_scale, units.col(c), p.dim);
-        else if constexpr (KEPT)
-          x[i].load(reinterpret_cast<const int8_t*>(at_q) + c * E, at_scale[c * E / LIPZ_BLOCK]);
-        else
-          x[i].raw.load(reinterpret_cast<const T*>(at + b.at[1]) + c * E);
-        if (has_dsum) ds[i].load(reinterpret_cast<const T*>(at + b.at[3]) + c * E);
-        if (SHIFT && edge) {  // (what lies beside the row adds nothing, whatever it is)
+      Source<T, E, KEPT, SHIFT> x;
+      dy.load(reinterpret_cast<const T*>(at + b.at[0]) + c * E);
+      if constexpr (KEPT && SHIFT)
+        x.load(at_q, at_scale, units.col(c), p.dim);
+      else if constexpr (KEPT)
+        x.load(reinterpret_cast<const int8_t*>(at_q) + c * E, at_scale[c * E / LIPZ_BLOCK]);
+      else
+        x.raw.load(reinterpret_cast<const T*>(at + b.at[1]) + c * E);
+      if (SHIFT && edge) {
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (!units.in(c, e)) dy[i].clear(e), x[i].clear(e);
-        }
-        uint64_t w[P], s[P];
-        if constexpr (!HELD) load_pairs<E>(weight + c * E, w);
-        x[i].get(s);
-        add_terms<T, E>(terms, dy[i], s, HELD ? hw[HELD ? i : 0] : w, mean, rstd, dw[i], db[i]);
+        for (int e = 0; e < E; ++e)
+          if (!units.in(c, e)) dy.clear(e), x.clear(e);
       }
-    }
+      x.get(v);
+      take_mean<E>(v, mean);
+    };
+    Terms terms;
+    Raw<T, E> dy[HELD ? NV : 1];
+    uint64_t x[HELD ? NV : 1][P];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i < count) {
+        const int h = HELD ? i : 0;
+        take(i, dy[h], x[h]);
+        uint64_t w[P];
+        if constexpr (!HELD) load_pairs<E>(weight + (t + i * tpr) * E, w);
+        add_terms<T, E>(terms, dy[h], x[h], HELD ? hw[h] : w, rstd, dw[i], db[i]);
+      }
     const float2 along = team_sum(terms.sums(), s_red[turn >> 1 & 1] + team * warps, t >> 5, warps, team + 1);
-    if (t == 0 && r + stages * step < p.rows) load(r + stages * step, stage);
+    // (every thread is done with the row before this one, whose stage takes the row that comes stages - 1 later: until
+    // then dsum is read from there, and of 32 elements all, which registers do not hold over the barrier)
+    if (t == 0 && stages > 1 && r != first && r + (stages - 1) * step < p.rows)
+      load(r + (stages - 1) * step, stage ? stage - 1 : stages - 1);
     // (rstd^2 by itself may be infinite where the gradient is not)
     const float c1 = along.x * p.inv_dim, c2 = rstd * (rstd * (along.y * p.inv_dim));
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i < count) {
         const int c = t + i * tpr;
-        uint64_t w[P], s[P], v[P];
-        if constexpr (!HELD) load_pairs<E>(weight + c * E, w);
-        x[i].get(s);
-        gradient<T, E>(v, dy[i], s, HELD ? hw[HELD ? i : 0] : w, ds[i], mean, rstd, c1, c2);
+        const int h = HELD ? i : 0;
+        Raw<T, E> ds;
+        uint64_t w[P], v[P];
+        ds.zero();
+        if (has_dsum) ds.load(reinterpret_cast<const T*>(at + b.at[3]) + c * E);
+        if constexpr (!HELD) {
+          take(i, dy[0], x[0]);
+          load_pairs<E>(weight + c * E, w);
+        }
+        gradient<T, E>(v, dy[h], x[h], HELD ? hw[h] : w, ds, rstd, c1, c2);
         if (SHIFT && edge && !units.whole(c)) store_edge<T, E>(dx, units, c, rounded<T, E>(v));
         else store_pairs<T, E>(dx + units.col(c), v);
       }
+    if (stages == 1) {  // (rows of which shared memory holds one)
+      asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(tpr) : "memory");
+      if (t == 0 && r + step < p.rows) load(r + step, 0);
+    }
     dx += dx_step;
     low_q += step_q, low_scale += step_scale;
     turn ^= 2;
@@ -1292,7 +1316,8 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
       if (i < count) {
         uint64_t s[P];
         y[i].get(s);
-        add_terms<T, E>(terms, a[i], s, w[i], m, f, dw[i], db[i]);
+        take_mean<E>(s, m);
+        add_terms<T, E>(terms, a[i], s, w[i], f, dw[i], db[i]);
       }
     float2 along = terms.sums();
 #pragma unroll
@@ -1308,7 +1333,8 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
       if (i < count) {
         uint64_t s[P], v[P];
         y[i].get(s);
-        gradient<T, E>(v, a[i], s, w[i], c3[i], m, f, c1, c2);
+        take_mean<E>(s, m);
+        gradient<T, E>(v, a[i], s, w[i], c3[i], f, c1, c2);
         store_pairs<T, E>(dx + (t + i * L) * E, v);
       }
   }
@@ -1407,7 +1433,7 @@ StreamShape back_shape(const lipz_layernorm_backward_args& a, BackStage* b) {
     if (bytes[i]) at += (int)ceil_div(bytes[i], 16) * 16 + 32;  // (a unit before the row, and one after)
   }
   s.row = s.slot = at;
-  s.share(512);
+  s.share(TEAM_THREADS);
   return s;
 }
 

@@ -228,7 +228,7 @@ struct DuArgs {
 // ALIGNED: rows of whole 16-byte units; else 8 columns are brought from the aligned words that hold them
 // (777 x 1001 with the copies beside it: one at a time 8.6 us, so 7.9, most of it latency).
 template <bool ALIGNED, bool KEPT>
-__global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
+__global__ void __launch_bounds__(256, KEPT ? 4 : 0) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
   constexpr int E = 8;
   __shared__ float s[8][32 * E + 1];
   pdl_wait();
@@ -275,10 +275,18 @@ __global__ void __launch_bounds__(256) k_du(const DuArgs p, const __grid_constan
         load(p.dy, r, d);
         if constexpr (ACT != LIPZ_ACT_NONE) {
           float u[E];
-          if constexpr (KEPT) load_kept(r, u);
-          else load(p.pre, r, u);
+          if constexpr (KEPT) {
+            load_kept(r, u);
 #pragma unroll
-          for (int e = 0; e < E; ++e) d[e] *= act_slope<ACT>(u[e], p.slope);
+            for (int e = 0; e < E; e += 2) {
+              const float2 both = unpack2(mul2(pack2(d[e], d[e + 1]), act_slope_pair<ACT>(pack2(u[e], u[e + 1]), p.slope)));
+              d[e] = both.x, d[e + 1] = both.y;
+            }
+          } else {
+            load(p.pre, r, u);
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] *= act_slope<ACT>(u[e], p.slope);
+          }
         }
         if (p.du) store_vec<bf16, E>(p.du + (g * p.rows + r) * p.ldu + c, d);
 #pragma unroll

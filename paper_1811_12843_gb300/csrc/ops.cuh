@@ -311,6 +311,35 @@ __device__ __forceinline__ void act_pair(float& a, float& b, float slope) {
   }
 }
 
+// act_slope of two values, operation by operation as there.
+template <int ACT>
+__device__ __forceinline__ uint64_t act_slope_pair(uint64_t u, float slope) {
+  const float2 f = unpack2(u);
+  const uint64_t one = both(1.f);
+  auto logistic2 = [&](uint64_t v) {
+    const float2 arg = unpack2(mul2(both(-LOG2E), v));
+    const float2 y = unpack2(add2(one, pack2(ex2_approx(arg.x), ex2_approx(arg.y))));
+    return pack2(rcp_approx(y.x), rcp_approx(y.y));
+  };
+  if constexpr (ACT == LIPZ_ACT_TANH) {
+    const float2 arg = unpack2(mul2(both(-2.f * LOG2E), pack2(fabsf(f.x), fabsf(f.y))));
+    const uint64_t e = pack2(ex2_approx(arg.x), ex2_approx(arg.y));
+    const float2 y = unpack2(add2(one, e));
+    const uint64_t r = pack2(rcp_approx(y.x), rcp_approx(y.y));
+    return mul2(mul2(mul2(both(4.f), e), r), r);
+  } else if constexpr (ACT == LIPZ_ACT_GELU) {
+    const float2 sq = unpack2(mul2(u, u));
+    const uint64_t u2 = pack2(fminf(sq.x, 1e30f), fminf(sq.y, 1e30f));
+    const uint64_t g = logistic2(mul2(u, fma2(both(GELU_3), u2, both(GELU_1))));
+    return fma2(mul2(mul2(u, g), fma2(g, both(-1.f), one)), fma2(both(3.f * GELU_3), u2, both(GELU_1)), g);
+  } else if constexpr (ACT == LIPZ_ACT_SILU) {
+    const uint64_t g = logistic2(u);
+    return mul2(g, fma2(u, fma2(g, both(-1.f), one), one));
+  } else {
+    return pack2(act_slope<ACT>(f.x, slope), act_slope<ACT>(f.y, slope));
+  }
+}
+
 // Calls f with the activation as a constant.
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F&& f) {

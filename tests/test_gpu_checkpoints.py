@@ -211,7 +211,7 @@ BACKWARDS = [(1, 1, 64, 32), (1, 37, 500, 1000), (1, 777, 500, 1001), (3, 100, 2
 
 
 @pytest.mark.parametrize("groups,rows,k,n", BACKWARDS)
-@pytest.mark.parametrize("act", ["none", "relu", "gelu", "tanh"])
+@pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("whole", [True, False])
 def test_linear_backward_over_checkpoints(groups, rows, k, n, act, whole):
     """The bits of the same call over the bf16 values, whatever of x and pre is a checkpoint."""
@@ -232,6 +232,19 @@ def test_linear_backward_over_checkpoints(groups, rows, k, n, act, whole):
         want = ops.linear_backward(dy, xv, w, act=act, slope=SLOPE, pre=prev if act != "none" else None, **wants)
         for a, b in zip(got, want):
             assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_slopes_at_the_ends(act):
+    """Pre-activations from nothing to the largest: the bits of the same call over the bf16 values."""
+    exps = torch.arange(-126, 122, device="cuda", dtype=F32)
+    u = torch.cat([torch.exp2(exps) * s * 1.5 for s in (1, -1)] + [torch.linspace(-100, 100, 1008, device="cuda")])
+    pre = ops.checkpoint_rows(u.reshape(-1, 1).expand(-1, 16).contiguous())
+    dy, x, w = randn(28, (u.numel(), 16), 1.0), randn(29, (u.numel(), 8)), randn(30, (16, 8))
+    ref = ops.linear_backward(dy, x, w, act=act, slope=SLOPE, pre=ops.restore_rows(pre) if act != "none" else None)
+    got = ops.linear_backward(dy, x, w, act=act, slope=SLOPE, pre=pre if act != "none" else None)
+    for a, b in zip(got, ref):
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(0.0), b.nan_to_num(0.0))
 
 
 def test_linear_backward_over_a_shared_checkpoint():
