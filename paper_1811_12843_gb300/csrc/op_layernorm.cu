@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k
 // thread takes whole units, the row's first and last in part. A block's rows lie a multiple of 16 rows' bytes apart, so
 // that all of them begin at the same place of a unit: weights and biases stand in shared memory in those units. (For
 // rows at any place, a word to each column, bf16 16385 x 4097 took 128 us; in registers, which leave room for fewer
-// blocks, 194; so SHIFT_NOW.)
+// blocks, 194; so 97.)
 template <int E>
 struct Units {
   int m, dim;  // elements of the first unit before the row
@@ -1069,7 +1069,7 @@ __device__ __forceinline__ void back_rows(const LayerBack& p, int64_t g, int64_t
 // Teams of one row's threads, several to a block, walk over rows of one group (blockIdx.y), which arrive in a ring of
 // each; their sums for dweight and dbias stay in registers, and of 16 elements the weights. At the end the teams' sums are
 // added in shared memory: one part per SM is left for the launch that adds those (16384 x 2048 over a checkpoint: with a
-// part per team 65 us, 7 of them that launch; so BACK_NOW). SHIFT: rows off the 16-byte grid, as in k_layer_stream; a
+// part per team 65 us, 7 of them that launch; so 62). SHIFT: rows off the 16-byte grid, as in k_layer_stream; a
 // checkpoint's row lies at any byte: its multiples come from the words that hold them, and a unit's columns from two
 // blocks at most.
 constexpr int TEAM_THREADS = 512;  // of a block (registers)
@@ -1541,16 +1541,23 @@ cudaError_t layernorm(const lipz_layernorm_args& a, cudaStream_t st) {
   return a.residual.data ? checkpoint_rows(c, st) : go();
 }
 
+namespace {
+uint64_t back_space(const lipz_layernorm_backward_args& a, const BackPlan& b) {
+  return b.blocks > 1 && (a.dweight.data || a.dbias.data) ? (uint64_t)a.groups * b.blocks * 2 * a.dim * 4 : 0;
+}
+}  // namespace
+
 uint64_t layernorm_backward_workspace(const lipz_layernorm_backward_args& a) {
-  if (!a.dweight.data && !a.dbias.data) return 0;
-  const int blocks = back_plan(a).blocks;
-  return blocks > 1 ? (uint64_t)a.groups * blocks * 2 * a.dim * 4 : 0;
+  return a.dweight.data || a.dbias.data ? back_space(a, back_plan(a)) : 0;
 }
 
-cudaError_t layernorm_backward(const lipz_layernorm_backward_args& a, cudaStream_t st) {
+cudaError_t layernorm_backward(const lipz_layernorm_backward_args& a, cudaStream_t st, uint64_t* need) {
+  *need = 0;
   if (a.groups == 0) return cudaSuccess;
   const BackPlan b = back_plan(a);
-  const bool parts = b.blocks > 1 && (a.dweight.data || a.dbias.data), kept = a.kept.data;
+  *need = back_space(a, b);
+  if (!space_given(a.workspace, a.workspace_bytes, *need)) return cudaSuccess;
+  const bool parts = *need, kept = a.kept.data;
   const LayerBack p{a.dy, a.s, a.dsum, a.dx, a.kept, a.weight, a.mean, a.rstd, a.dweight, a.dbias,
                     parts ? (float*)a.workspace : nullptr, a.rows, (int)a.dim, 1.f / (float)a.dim};
   cudaError_t e;

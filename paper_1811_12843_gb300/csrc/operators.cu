@@ -1,6 +1,7 @@
 // C ABI of the residual-block operators: every argument that the host can check is checked here, then
 // the kernels of op_norm.cu, op_layernorm.cu, op_checkpoint.cu, op_linear.cu and op_gemm.cu are launched.
 #include <algorithm>
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -15,12 +16,18 @@ namespace lipz {
 namespace ops {
 
 int sm_count() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) {
     cudaGetLastError();
     return 152;
   }
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed))) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return 152;
+  }
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 
@@ -651,10 +658,13 @@ int lipz_layernorm_backward_workspace(const lipz_layernorm_backward_args* a, uin
 int lipz_layernorm_backward(const lipz_layernorm_backward_args* a, void* stream) {
   if (int rc = check(a)) return rc;
   Check c{"lipz_layernorm_backward", a->groups, a->rows};
-  if (!c.space(a->workspace, a->workspace_bytes, ops::layernorm_backward_workspace(*a))) return c.rc;
-  if (int rc = overlap(*a)) return rc;
+  if (int rc = overlap(*a))
+    return c.space(a->workspace, a->workspace_bytes, ops::layernorm_backward_workspace(*a)) ? rc : c.rc;
   if (int rc = take_timeout(c.call)) return rc;
-  return finish(c.call, ops::layernorm_backward(*a, (cudaStream_t)stream));
+  uint64_t need;
+  const cudaError_t e = ops::layernorm_backward(*a, (cudaStream_t)stream, &need);
+  if (!c.space(a->workspace, a->workspace_bytes, need)) return c.rc;
+  return finish(c.call, e);
 }
 
 int lipz_checkpoint_rows(const lipz_checkpoint_rows_args* a, void* stream) {

@@ -64,7 +64,7 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, const lipz_block
 
 cudaError_t layernorm(const lipz_layernorm_args& a, cudaStream_t st);
 uint64_t layernorm_backward_workspace(const lipz_layernorm_backward_args& a);
-cudaError_t layernorm_backward(const lipz_layernorm_backward_args& a, cudaStream_t st);
+cudaError_t layernorm_backward(const lipz_layernorm_backward_args& a, cudaStream_t st, uint64_t* need);
 cudaError_t checkpoint_rows(const lipz_checkpoint_rows_args& a, cudaStream_t st);
 cudaError_t restore_rows(const lipz_restore_rows_args& a, cudaStream_t st);
 
