@@ -80,7 +80,13 @@ GemmPlan plan_products(const Products& q) {
   static const Shape shapes[] = {{2, 256, 158, 9000, 2500, 5500}, {2, 128, 88, 3900, 800, 2600},
                                  {1, 128, 108, 3900, 800, 2600}, {1, 64, 82, 2350, 250, 900}};
   const Shape via{2, 128, 100, 3500, 400, 1000};  // shape 1 with its results through shared memory
-  const int64_t long_chunks = g0.e.kept.data ? KEPT_MIN : LONG_CHUNKS;
+  const bool kept = g0.e.kept.data;
+  const int64_t long_chunks = kept ? KEPT_MIN : LONG_CHUNKS;
+  auto kept_sums = [&](int64_t chunks) {
+    const int64_t quarter = ceil_div(chunks, 4), most = fp32 ? SUM_CHUNKS : KEPT_MAX;
+    const int64_t n = quarter < KEPT_MIN ? KEPT_MIN : quarter < most ? quarter : most;
+    return (double)ceil_div(chunks, n);
+  };
   const bool by_tma = results_by_tma(g0);
   const bool forward = g0.a.k_major && g0.b.k_major;
   const int sms = sm_count();
@@ -109,7 +115,12 @@ GemmPlan plan_products(const Products& q) {
                (o.splits == 1 || tiles * o.splits <= (forward ? 1 : 2) * slots) &&
                (!forward || o.splits == s0);
         const double mma = o.chunks_per_split * 4 * c.step * (eb == 1 ? 1.16 : 1);
-        const double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0);
+        double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0);
+        // A checkpoint beside them: its own stores, and each sum's way into registers. In 256-wide tiles the MMAs are
+        // ahead by no more than the first two sums, five eighths of k. (8192 x 1024 -> 4096 66 us by 256 x 128, 92 by
+        // 256 x 256; 8192 x 4096 -> 8192 394 and 322.)
+        if (kept) epi += c.bn * (c.bn == 256 ? 10 : 3) + kept_sums(o.chunks_per_split) * (c.bn == 256 ? 2700. : 1300.);
+        if (kept && c.bn == 256) epi += 0.375 * mma;
         const double unit = mma > epi ? mma : epi;
         work += unit * tiles * o.splits;
         if (unit > top) top = unit;
@@ -118,7 +129,7 @@ GemmPlan plan_products(const Products& q) {
         split = split || o.splits > 1;
       }
       // (sums in 256-wide tiles: bf16 results of a checkpoint's product alone)
-      if (!fits || (s0 > 1 && !split) || (t.sums && c.bn > 128 && !g0.e.kept.data)) continue;
+      if (!fits || (s0 > 1 && !split) || (t.sums && c.bn > 128 && !kept)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
       // (a cluster's CTA finishes 64 / s0 columns of up to 128 rows, an element per thread and turn)
@@ -221,9 +232,9 @@ cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspac
   const Gemm& g0 = q.g[0];
   cudaError_t e;
   if (g0.e.kept.data) e = run_kept_product(plan, q, st);
-  else if (g0.type == LIPZ_E4M3) e = launch_shape<LIPZ_E4M3, true, false>(q, plan, parts, sums, st);
-  else if (g0.a.k_major && g0.b.k_major) e = launch_shape<LIPZ_BF16, true, false>(q, plan, parts, sums, st);
-  else e = launch_shape<LIPZ_BF16, false, false>(q, plan, parts, sums, st);
+  else if (g0.type == LIPZ_E4M3) e = launch_shape<LIPZ_E4M3, true, 0>(q, plan, parts, sums, st);
+  else if (g0.a.k_major && g0.b.k_major) e = launch_shape<LIPZ_BF16, true, 0>(q, plan, parts, sums, st);
+  else e = launch_shape<LIPZ_BF16, false, 0>(q, plan, parts, sums, st);
   if (e != cudaSuccess || (!parts[0] && !parts[1])) return e;
   FinishPair f{};
   int n = 0;

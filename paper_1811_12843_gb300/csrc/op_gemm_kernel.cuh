@@ -319,8 +319,8 @@ __device__ __forceinline__ Place place(const Problem& p, int unit) {
 // SPLIT: a cluster of CTAs shares a tile, each with a part of k; their sums are added over the cluster's
 // shared memory, each CTA finishing a part of the columns. One tile per cluster.
 // DIRECT: the result warps bring the operands first, from rows that TMA does not take.
-// KEPT: pre is kept as a checkpoint.
-template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA, bool SPLIT, bool DIRECT, bool KEPT>
+// KEPT: pre is kept as a checkpoint, beside bf16 results (1) or, of sums, fp32 results (2).
+template <int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA, bool SPLIT, bool DIRECT, int KEPT>
 __global__ void __launch_bounds__(THREADS, 1)
     k_gemm_op(const __grid_constant__ GemmParams<FORWARD ? 1 : 2> prm) {
   using S = Shape<CG, BN, VIA>;
@@ -682,8 +682,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       // VIA: this lane's 64 bytes of the warp's 32 rows, 16-byte units in the 64-byte swizzle
       uint8_t* mine = tiles + r * S::TILE + (ew >> 2) * (S::TILE / (BN / 32)) + q * 2048 + lane * 64;
       const int swizzle = lane >> 1 & 3;
-      // (256-wide tiles of sums have bf16 results: plan_products)
-      const bool as_bf16 = SUMS && (VIA || BN == 256 || e.y.type == LIPZ_BF16);
+      const bool as_bf16 = SUMS && (KEPT ? KEPT == 1 : e.y.type == LIPZ_BF16);
       auto residual = [&](uint32_t (&v)[VW], int c) {
         if (VIA || !has_res) return;
         const int64_t at = sl.residual + (int64_t)(q * 32) * e.residual.row + col0 + c;
@@ -1009,7 +1008,7 @@ bool encode(CUtensorMap* map, const Operand& o, const Extent& x, int64_t groups,
 
 uint64_t round256(int64_t v) { return (uint64_t)ceil_div(v, 256) * 256; }
 
-template <bool KEPT, int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false,
+template <int KEPT, int TYPE, int CG, int BN, bool FORWARD, typename T, bool VIA = false, bool SPLIT = false,
           bool DIRECT = false>
 cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts, const PartSums* sums,
                    cudaStream_t st) {
@@ -1113,7 +1112,7 @@ bool results_by_tma(const Gemm& g) {
   return g.e.y.type == LIPZ_BF16 && g.a.k_major && g.b.k_major && takes(g.e.y) && takes(g.e.residual);
 }
 
-template <int TYPE, bool FORWARD, bool KEPT>
+template <int TYPE, bool FORWARD, int KEPT>
 cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* parts, const PartSums* sums,
                          cudaStream_t st) {
   if constexpr (FORWARD) {
@@ -1127,7 +1126,12 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
                  : launch<KEPT, TYPE, 1, 64, true, bf16, false, true>(q, p, parts, sums, st);
   }
   if (p.sums) {
-    if constexpr (KEPT) {
+    if constexpr (KEPT == 1) {
+      if (q.g[0].e.y.type == LIPZ_FP32) {
+        if (p.cg == 2) return launch<2, TYPE, 2, 128, FORWARD, float>(q, p, parts, sums, st);
+        if (p.bn == 128) return launch<2, TYPE, 1, 128, FORWARD, float>(q, p, parts, sums, st);
+        return launch<2, TYPE, 1, 64, FORWARD, float>(q, p, parts, sums, st);
+      }
       if (p.cg == 2 && p.bn == 128 && results_by_tma(q.g[0]))
         return launch<KEPT, TYPE, 2, 128, true, float, true>(q, p, parts, sums, st);
       if (p.bn == 256) return launch<KEPT, TYPE, 2, 256, true, float>(q, p, parts, sums, st);
