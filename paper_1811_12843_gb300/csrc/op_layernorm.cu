@@ -369,130 +369,7 @@ __global__ void __launch_bounds__(E * NV <= 8 ? 1024 : 512) k_layer_rows(const L
   if (live) layer_results<T, E, NV>(p, g, gr, mo, inv, v, t, p.tpr, nvec);
 }
 
-// ---- many short rows: a warp walks over sets of 32 / L rows, L lanes to a row of NV vectors each. The next set's
-// loads are in flight while this one is summed and written; weights and biases stay in a lane's registers where a
-// lane has 16 elements. No barrier.
-constexpr int SHORT_WARPS = 4;  // of a block
-
-template <typename T, int E, int NV, int L>
-__global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k_layer_short(const LayerArgs p) {
-  constexpr int R = 32 / L;
-  constexpr bool HELD = NV * E <= 16;
-  const int lane = threadIdx.x & 31, t = lane % L, sub = lane / L, nvec = p.dim / E;
-  const int64_t step = (int64_t)gridDim.x * SHORT_WARPS * R;
-  const bool has_res = p.residual.data;
-  int count = 0;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) count += t + i * L < nvec;
-  pdl_wait();
-  Raw<T, E> x[NV], res[NV];
-  auto bring = [&](int64_t r) {
-    const bool live = r < p.total;
-    const int64_t g = live ? group_at(r, p.rows, p.total) : 0, gr = r - g * p.rows;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      x[i].zero(), res[i].zero();
-      if (live && i < count) {
-        x[i].load(row_of<const T>(p.x, g, gr) + (t + i * L) * E);
-        if (has_res) res[i].load(row_of<const T>(p.residual, g, gr) + (t + i * L) * E);
-      }
-    }
-  };
-  constexpr int P = E / 2;
-  uint64_t w[HELD ? NV * P : P], b[HELD ? NV * P : P];
-  int64_t held_of = -1;  // the group whose parameters w and b are
-  auto params = [&](int64_t g, int i, int at) {
-    const int c = (t + i * L) * E;
-#pragma unroll
-    for (int j = 0; j < P; ++j) b[at + j] = 0;
-    load_pairs<E>(p.weight.data + g * p.weight.group + c, w + at);
-    if (p.bias.data) load_pairs<E>(p.bias.data + g * p.bias.group + c, b + at);
-  };
-  int64_t r = ((int64_t)blockIdx.x * SHORT_WARPS + (threadIdx.x >> 5)) * R + sub;
-  bring(r);
-  for (; r - sub < p.total; r += step) {  // (the same turns for all lanes of a warp)
-    uint64_t v[NV * P];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      pairs_of<T, E>(x[i], v + i * P);
-      if (has_res) {
-        uint64_t u[P];
-        pairs_of<T, E>(res[i], u);
-#pragma unroll
-        for (int j = 0; j < P; ++j) v[i * P + j] = add2(v[i * P + j], u[j]);
-      }
-    }
-    bring(r + step);
-    const bool live = r < p.total;
-    const int64_t g = live ? group_at(r, p.rows, p.total) : 0, gr = r - g * p.rows;
-    if (p.sum.data || p.kept.data) {
-      T* s = p.sum.data ? row_of<T>(p.sum, g, gr) : nullptr;
-      int8_t* q = p.kept.data + g * p.kept.group + gr * p.kept.row;
-      uint8_t* scale = p.kept.scale + g * p.kept.scale_group + gr * p.kept.scale_row;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const bool here = live && i < count;
-        const Raw<T, E> u = rounded<T, E>(v + i * P);
-        if (s && here) store_raw<T, E>(s + (t + i * L) * E, u);
-        if (p.kept.data) keep_raw<T, E>(q, scale, (t + i * L) * E, here, u);
-      }
-    }
-    float sum = pairs_sum(v);
-#pragma unroll
-    for (int o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float mean = sum * p.inv_dim;
-    float m2 = pairs_squares<E, NV>(v, mean, (1u << count) - 1u);
-#pragma unroll
-    for (int o = L / 2; o; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-    const Moments mo{mean, rsqrtf(fmaf(m2, p.inv_dim, p.eps))};
-    if (HELD && g != held_of) {
-      held_of = g;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i < count) params(g, i, HELD ? i * P : 0);
-    }
-    if (t == 0 && live) {
-      if (p.mean.data) p.mean.data[g * p.mean.group + gr] = mo.mean;
-      if (p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = mo.rstd;
-    }
-    if (p.scale.data) {
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i < count) {
-          if (!HELD) params(g, i, 0);
-          top = pairs_affine<E, true>(v + i * P, mo, w + (HELD ? i * P : 0), b + (HELD ? i * P : 0), top);
-        }
-      uint32_t most = __float_as_uint(top);
-#pragma unroll
-      for (int o = L / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-      const float scale = scale_of(__uint_as_float(most));
-      const Reciprocal inv = reciprocal_of(scale);
-      if (!live) continue;
-      if (t == 0) p.scale.data[g * p.scale.group + gr] = scale;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i < count) store_pairs_e4m3<E>(row_of<e4m3>(p.y, g, gr) + (t + i * L) * E, v + i * P, inv);
-    } else {
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (live && i < count) {
-          if (!HELD) params(g, i, 0);
-          pairs_affine<E, false>(v + i * P, mo, w + (HELD ? i * P : 0), b + (HELD ? i * P : 0), 0.f);
-          store_pairs<T, E>(row_of<T>(p.y, g, gr) + (t + i * L) * E, v + i * P);
-        }
-    }
-  }
-}
-
-// ---- many rows: a block of one row's threads walks over rows that arrive in a ring of shared-memory stages by bulk
-// copies, so that loads stay in flight while rows are summed and written.
-//
-// SHIFT: rows off the 16-byte grid (odd widths), all of a call's matrices at the same place of a unit in each row. A
-// thread takes whole units, the row's first and last in part. A block's rows lie a multiple of 16 rows' bytes apart, so
-// that all of them begin at the same place of a unit: weights and biases stand in shared memory in those units. (For
-// rows at any place, a word to each column, bf16 16385 x 4097 took 128 us; in registers, which leave room for fewer
-// blocks, 194; so 97.)
+// The units of a row off the 16-byte grid: a thread's columns are c E - m + e, the row's first and last unit in part.
 template <int E>
 struct Units {
   int m, dim;  // elements of the first unit before the row
@@ -515,6 +392,188 @@ __device__ __forceinline__ void store_edge(T* row, const Units<E>& u, int c, con
     if (u.in(c, e)) row[u.col(c) + e] = from_f<T>(r.get(e));
 }
 
+template <int E>
+__device__ __forceinline__ void store_edge_e4m3(e4m3* row, const Units<E>& u, int c, const uint64_t* v, Reciprocal inv) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float2 f = unpack2(v[e / 2]);
+    float one = e & 1 ? f.y : f.x;
+    scale_by<1>(&one, inv);
+    if (u.in(c, e)) store_e4m3<1>(row + u.col(c) + e, &one);
+  }
+}
+
+// ---- many short rows: a warp walks over sets of 32 / L rows, L lanes to a row of NV vectors each. The next set's
+// loads are in flight while this one is summed and written; weights and biases stay in a lane's registers where a
+// lane has 16 elements. No barrier.
+constexpr int SHORT_WARPS = 4;  // of a block
+
+// SHIFT: rows off the 16-byte grid, which all begin at the same place of a unit for a lane: the rows that it takes lie a
+// multiple of 16 rows' bytes apart. (Through rings, a row per warp, 65536 x 301 took 66 us and 131072 x 77 88; so 66 and 35.)
+template <typename T, int E, int NV, int L, bool SHIFT>
+__global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k_layer_short(const LayerArgs p) {
+  constexpr int R = 32 / L, P = E / 2;
+  constexpr bool HELD = NV * E <= 16;
+  static_assert(!SHIFT || HELD, "parameters in registers");
+  const int lane = threadIdx.x & 31, t = lane % L, sub = lane / L;
+  const int64_t step = (int64_t)gridDim.x * SHORT_WARPS * R;
+  int64_t r = ((int64_t)blockIdx.x * SHORT_WARPS + (threadIdx.x >> 5)) * R + sub;
+  const bool has_res = p.residual.data;
+  auto group = [&](int64_t at) { return at < p.total ? group_at(at, p.rows, p.total) : 0; };
+  const Units<E> units{
+      SHIFT ? (int)((uint64_t)row_of<const T>(p.x, group(r), r - group(r) * p.rows) & 15) / (int)sizeof(T) : 0, p.dim};
+  int count = 0;
+  uint32_t edge = 0;  // vectors that the row has in part
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (!units.live(t + i * L)) continue;
+    ++count;
+    if (SHIFT && !units.whole(t + i * L)) edge |= 1u << i;
+  }
+  const uint32_t whole = ((1u << count) - 1u) & ~edge;
+  auto edges = [&](auto f) {
+    if (!SHIFT || !edge) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (edge >> i & 1) f(i, t + i * L);
+  };
+  pdl_wait();
+  Raw<T, E> x[NV], res[NV];
+  auto bring = [&](int64_t at) {
+    const bool live = at < p.total;
+    const int64_t g = group(at), gr = at - g * p.rows;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      x[i].zero(), res[i].zero();
+      if (live && i < count) {
+        x[i].load(row_of<const T>(p.x, g, gr) + units.col(t + i * L));
+        if (has_res) res[i].load(row_of<const T>(p.residual, g, gr) + units.col(t + i * L));
+      }
+    }
+  };
+  uint64_t w[HELD ? NV * P : P], b[HELD ? NV * P : P];
+  int64_t held_of = -1;  // the group whose parameters w and b are
+  auto params = [&](int64_t g, int i, int at) {
+    const int c = t + i * L;
+#pragma unroll
+    for (int j = 0; j < P; ++j) b[at + j] = 0;
+    if constexpr (SHIFT) {
+      units.params(p.weight.data + g * p.weight.group, c, w + at);
+      if (p.bias.data) units.params(p.bias.data + g * p.bias.group, c, b + at);
+    } else {
+      load_pairs<E>(p.weight.data + g * p.weight.group + c * E, w + at);
+      if (p.bias.data) load_pairs<E>(p.bias.data + g * p.bias.group + c * E, b + at);
+    }
+  };
+  bring(r);
+  for (; r - sub < p.total; r += step) {  // (the same turns for all lanes of a warp)
+    uint64_t v[NV * P];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      pairs_of<T, E>(x[i], v + i * P);
+      if (has_res) {
+        uint64_t u[P];
+        pairs_of<T, E>(res[i], u);
+#pragma unroll
+        for (int j = 0; j < P; ++j) v[i * P + j] = add2(v[i * P + j], u[j]);
+      }
+    }
+    edges([&](int i, int c) {
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const float2 f = unpack2(v[i * P + j]);
+        v[i * P + j] = pack2(units.in(c, 2 * j) ? f.x : 0.f, units.in(c, 2 * j + 1) ? f.y : 0.f);
+      }
+    });
+    bring(r + step);
+    const bool live = r < p.total;
+    const int64_t g = group(r), gr = r - g * p.rows;
+    if (p.sum.data || (!SHIFT && p.kept.data)) {
+      T* s = p.sum.data ? row_of<T>(p.sum, g, gr) : nullptr;
+      int8_t* q = p.kept.data + g * p.kept.group + gr * p.kept.row;
+      uint8_t* scale = p.kept.scale + g * p.kept.scale_group + gr * p.kept.scale_row;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const Raw<T, E> u = rounded<T, E>(v + i * P);
+        if (s && live && whole >> i & 1) store_raw<T, E>(s + units.col(t + i * L), u);
+        if (!SHIFT && p.kept.data) keep_raw<T, E>(q, scale, (t + i * L) * E, live && i < count, u);
+      }
+      if (s && live) edges([&](int i, int c) { store_edge<T, E>(s, units, c, rounded<T, E>(v + i * P)); });
+    }
+    float sum = pairs_sum(v);
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float mean = sum * p.inv_dim;
+    float m2 = pairs_squares<E, NV>(v, mean, whole);
+    edges([&](int i, int c) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float2 f = unpack2(v[i * P + e / 2]);
+        const float off = (e & 1 ? f.y : f.x) - mean;
+        if (units.in(c, e)) m2 = fmaf(off, off, m2);
+      }
+    });
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+    const Moments mo{mean, rsqrtf(fmaf(m2, p.inv_dim, p.eps))};
+    if (HELD && g != held_of) {
+      held_of = g;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) params(g, i, HELD ? i * P : 0);
+    }
+    if (t == 0 && live) {
+      if (p.mean.data) p.mean.data[g * p.mean.group + gr] = mo.mean;
+      if (p.rstd.data) p.rstd.data[g * p.rstd.group + gr] = mo.rstd;
+    }
+    if (p.scale.data) {
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < count) {
+          if (!HELD) params(g, i, 0);
+          const float here = pairs_affine<E, true>(v + i * P, mo, w + (HELD ? i * P : 0), b + (HELD ? i * P : 0), top);
+          if (whole >> i & 1) top = here;
+        }
+      edges([&](int i, int c) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float2 f = unpack2(v[i * P + e / 2]);
+          if (units.in(c, e)) top = max_nan(top, fabsf(e & 1 ? f.y : f.x));
+        }
+      });
+      uint32_t most = __float_as_uint(top);
+#pragma unroll
+      for (int o = L / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+      const float scale = scale_of(__uint_as_float(most));
+      const Reciprocal inv = reciprocal_of(scale);
+      if (!live) continue;
+      if (t == 0) p.scale.data[g * p.scale.group + gr] = scale;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (whole >> i & 1) store_pairs_e4m3<E>(row_of<e4m3>(p.y, g, gr) + units.col(t + i * L), v + i * P, inv);
+      edges([&](int i, int c) { store_edge_e4m3<E>(row_of<e4m3>(p.y, g, gr), units, c, v + i * P, inv); });
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (live && i < count) {
+          if (!HELD) params(g, i, 0);
+          pairs_affine<E, false>(v + i * P, mo, w + (HELD ? i * P : 0), b + (HELD ? i * P : 0), 0.f);
+          if (whole >> i & 1) store_pairs<T, E>(row_of<T>(p.y, g, gr) + units.col(t + i * L), v + i * P);
+        }
+      if (live) edges([&](int i, int c) { store_edge<T, E>(row_of<T>(p.y, g, gr), units, c, rounded<T, E>(v + i * P)); });
+    }
+  }
+}
+
+// ---- many rows: a block of one row's threads walks over rows that arrive in a ring of shared-memory stages by bulk
+// copies, so that loads stay in flight while rows are summed and written.
+//
+// SHIFT: rows off the 16-byte grid (odd widths), all of a call's matrices at the same place of a unit in each row. A
+// thread takes whole units, the row's first and last in part. A block's rows lie a multiple of 16 rows' bytes apart, so
+// that all of them begin at the same place of a unit: weights and biases stand in shared memory in those units. (For
+// rows at any place, a word to each column, bf16 16385 x 4097 took 128 us; in registers, which leave room for fewer
+// blocks, 194; so 97.)
 template <typename T, int E, int NV, bool SHIFT>
 __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1)
     k_layer_stream(const LayerArgs p, int stages, int slot, int* err) {
@@ -695,15 +754,7 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1)
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (whole >> i & 1) store_pairs_e4m3<E>(y + units.col(t + i * tpr), v + i * P, inv);
-      edges([&](int i) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float2 f = unpack2(v[i * P + e / 2]);
-          float one = e & 1 ? f.y : f.x;
-          scale_by<1>(&one, inv);
-          if (units.in(t + i * tpr, e)) store_e4m3<1>(y + units.col(t + i * tpr) + e, &one);
-        }
-      });
+      edges([&](int i) { store_edge_e4m3<E>(y, units, t + i * tpr, v + i * P, inv); });
     } else {
       T* y = row_of<T>(p.y, g, gr);
 #pragma unroll
@@ -725,19 +776,26 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1)
   ring_done(q, err);
 }
 
-// One wave of blocks.
-template <typename T, int E, int NV, int L>
+// One wave of blocks, whose turns are a multiple of 8 rows.
+template <typename T, int E, int NV, int L, bool SHIFT>
 cudaError_t launch_short(const LayerArgs& p, cudaStream_t st) {
+  constexpr auto kernel = k_layer_short<T, E, NV, L, SHIFT>;
   static const int resident = [] {
     int n = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_layer_short<T, E, NV, L>,
-                                                                        32 * SHORT_WARPS, 0);
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, 32 * SHORT_WARPS, 0);
     if (e != cudaSuccess) cudaGetLastError();
     return e == cudaSuccess && n > 0 ? n : 4;
   }();
   const int64_t most = (int64_t)sm_count() * resident, want = ceil_div(p.total, SHORT_WARPS * (32 / L));
-  return launch_pdl(k_layer_short<T, E, NV, L>, dim3((unsigned)(want < most ? want : most)), dim3(32 * SHORT_WARPS),
-                    0, st, p);
+  const int64_t blocks = want < most ? want : (most + 1) / 2 * 2;
+  return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * SHORT_WARPS), 0, st, p);
+}
+template <typename T, int E, bool SHIFT>
+cudaError_t launch_short(const LayerArgs& p, int lanes, cudaStream_t st) {
+  if (lanes <= 4) return launch_short<T, E, 16 / E, 4, SHIFT>(p, st);
+  if (lanes <= 8) return launch_short<T, E, 16 / E, 8, SHIFT>(p, st);
+  if (lanes <= 16) return launch_short<T, E, 16 / E, 16, SHIFT>(p, st);
+  return launch_short<T, E, 16 / E, 32, SHIFT>(p, st);
 }
 
 // Blocks of a group (shift: whose rows must begin at the same place of a unit, 16 bytes' rows apart or alone).
@@ -774,13 +832,8 @@ cudaError_t launch_layer(LayerArgs& p, cudaStream_t st) {
   const int arrays = p.residual.data ? 2 : 1;
   if constexpr (E > 1) {
     const int lanes = (int)ceil_div(p.dim, 16);
-    if (many && lanes <= 64) {
-      if (lanes <= 4) return launch_short<T, E, 16 / E, 4>(p, st);
-      if (lanes <= 8) return launch_short<T, E, 16 / E, 8>(p, st);
-      if (lanes <= 16) return launch_short<T, E, 16 / E, 16>(p, st);
-      if (lanes <= 32) return launch_short<T, E, 16 / E, 32>(p, st);
-      return launch_short<T, E, 32 / E, 32>(p, st);
-    }
+    if (many && lanes <= 32) return launch_short<T, E, false>(p, lanes, st);
+    if (many && lanes <= 64) return launch_short<T, E, 32 / E, 32, false>(p, st);
     if (many) {
       const StreamShape s = stream_shape(p.dim, E, sizeof(T), arrays, 2048, 0, E == 8);
       return s.wide ? launch_rings<k_layer_stream<T, E, 32 / E, false>>(p, s, 0, st)
@@ -788,6 +841,10 @@ cudaError_t launch_layer(LayerArgs& p, cudaStream_t st) {
     }
   } else if (layer_shift(p)) {
     // (a row touches a unit more than it fills)
+    // (rows of several groups are one sequence to k_layer_short, which must begin as one group's do)
+    const int lanes = (int)ceil_div(p.dim + U - 1, 16);
+    if (lanes <= 32 && (p.total == p.rows || (p.x.group - p.rows * p.x.row) % U == 0))
+      return launch_short<T, U, true>(p, lanes, st);
     // (of 32 elements per thread bf16 rows have no registers left: 16385 x 4097 172 us)
     const int wide = (int)ceil_div(p.dim + U - 1, U) * U;
     StreamShape s = stream_shape(wide, U, sizeof(T), arrays, 2048);
@@ -972,6 +1029,24 @@ struct Source<T, E, true, SHIFT> {
     for (int j = 0; j < E / 4; ++j) w[j] = __funnelshift_r(r[j], r[j + 1], off * 8) ^ 0x80808080u;
     const int first = max(col, 0), last = min(col + E, dim) - 1;
     unit = block_unit(scale[first / LIPZ_BLOCK]), unit2 = block_unit(scale[last / LIPZ_BLOCK]);
+    border = (first | (LIPZ_BLOCK - 1)) + 1 - col;
+  }
+  // From global memory, at any byte.
+  __device__ __forceinline__ void gather(const int8_t* q, const uint8_t* scale, int col, int dim) {
+    if (col >= 0 && col + E <= dim) {
+      const uint4 r = bytes16(reinterpret_cast<const uint8_t*>(q) + col, E);
+      const uint32_t two[2] = {r.x, r.y};
+#pragma unroll
+      for (int j = 0; j < E / 4; ++j) w[j] = two[j] ^ 0x80808080u;
+    } else {
+#pragma unroll
+      for (int j = 0; j < E / 4; ++j) w[j] = 0x80808080u;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (col + e >= 0 && col + e < dim) w[e / 4] ^= (uint32_t)(uint8_t)__ldg(q + col + e) << e % 4 * 8;
+    }
+    const int first = max(col, 0), last = min(col + E, dim) - 1;
+    unit = block_unit(__ldg(scale + first / LIPZ_BLOCK)), unit2 = block_unit(__ldg(scale + last / LIPZ_BLOCK));
     border = (first | (LIPZ_BLOCK - 1)) + 1 - col;
   }
   __device__ __forceinline__ void get(uint64_t* v) const {
@@ -1252,18 +1327,27 @@ __global__ void __launch_bounds__(TEAM_THREADS) k_layer_back_stream(const LayerB
 
 // Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of WARPS walks over
 // rows of one group, and its warps' sums are added in shared memory.
-template <int NV>
-constexpr int BACK_WARPS = NV <= 2 ? 16 : 8;  // (registers)
+constexpr int BACK_WARPS = 16;  // (registers)
 
-template <typename T, int E, int NV, int L, bool KEPT>
-__global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const LayerBack p) {
-  constexpr int WARPS = BACK_WARPS<NV>, R = 32 / L;
-  extern __shared__ float s_sums[];  // [WARPS][2][dim]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane % L, sub = lane / L, nvec = p.dim / E;
+// SHIFT: rows off the 16-byte grid, as in k_layer_short: the columns of a warp's rows are different lanes', so that the
+// sums of each of them meet in shared memory.
+template <typename T, int E, int NV, int L, bool KEPT, bool SHIFT>
+__global__ void __launch_bounds__(32 * BACK_WARPS) k_layer_back_short(const LayerBack p) {
+  constexpr int WARPS = BACK_WARPS, R = 32 / L;
+  constexpr int SETS = SHIFT ? WARPS * R : WARPS;
+  extern __shared__ float s_sums[];  // [SETS][2][dim]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane % L, sub = lane / L;
   const int64_t g = blockIdx.y, step = (int64_t)gridDim.x * WARPS * R;
+  int64_t r = ((int64_t)blockIdx.x * WARPS + warp) * R + sub;
+  const Units<E> units{SHIFT ? (int)((uint64_t)row_of<const T>(p.dy, g, r) & 15) / (int)sizeof(T) : 0, p.dim};
   int count = 0;
+  bool edge = false;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) count += t + i * L < nvec;
+  for (int i = 0; i < NV; ++i) {
+    if (!units.live(t + i * L)) continue;
+    ++count;
+    if (SHIFT && !units.whole(t + i * L)) edge = true;
+  }
   pdl_wait();
   constexpr int P = E / 2;
   uint64_t w[NV][P], dw[NV][P], db[NV][P];
@@ -1272,11 +1356,12 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
     for (int j = 0; j < P; ++j) w[i][j] = dw[i][j] = db[i][j] = 0;
-    if (i < count) load_pairs<E>(weight + (t + i * L) * E, w[i]);
+    if (SHIFT) units.params(weight, t + i * L, w[i]);
+    else if (i < count) load_pairs<E>(weight + (t + i * L) * E, w[i]);
   }
   const bool has_dsum = p.dsum.data;
   Raw<T, E> dy[NV], ds[NV];
-  Source<T, E, KEPT> x[NV];
+  Source<T, E, KEPT, SHIFT> x[NV];
   float mean = 0.f, rstd = 0.f;
   auto load = [&](int64_t r) {
     if (r >= p.rows) {  // (a row of zeros adds nothing to the sums)
@@ -1289,23 +1374,30 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (i < count) {
-        const int c = (t + i * L) * E;
+        const int c = units.col(t + i * L);
         dy[i].load(row_of<const T>(p.dy, g, r) + c);
-        if constexpr (KEPT)
+        if constexpr (KEPT && SHIFT)
+          x[i].gather(p.kept.data + g * p.kept.group + r * p.kept.row,
+                      p.kept.scale + g * p.kept.scale_group + r * p.kept.scale_row, c, p.dim);
+        else if constexpr (KEPT)
           x[i].load(p.kept.data + g * p.kept.group + r * p.kept.row + c,
                     p.kept.scale[g * p.kept.scale_group + r * p.kept.scale_row + c / LIPZ_BLOCK]);
         else
           x[i].raw.load(row_of<const T>(p.s, g, r) + c);
         if (has_dsum) ds[i].load(row_of<const T>(p.dsum, g, r) + c);
+        if (SHIFT && edge) {  // (what lies beside the row adds nothing, whatever it is)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (!units.in(t + i * L, e)) dy[i].clear(e), x[i].clear(e);
+        }
       }
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) dy[i].zero(), x[i].zero(), ds[i].zero();
-  int64_t r = ((int64_t)blockIdx.x * WARPS + warp) * R + sub;
   load(r);
   for (; r - sub < p.rows; r += step) {  // (the same turns for all lanes of a warp)
     Raw<T, E> a[NV], c3[NV];
-    Source<T, E, KEPT> y[NV];
+    Source<T, E, KEPT, SHIFT> y[NV];
     const float m = mean, f = rstd;
 #pragma unroll
     for (int i = 0; i < NV; ++i) a[i] = dy[i], y[i] = x[i], c3[i] = ds[i];
@@ -1335,7 +1427,8 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
         y[i].get(s);
         take_mean<E>(s, m);
         gradient<T, E>(v, a[i], s, w[i], c3[i], f, c1, c2);
-        store_pairs<T, E>(dx + (t + i * L) * E, v);
+        if (SHIFT && edge && !units.whole(t + i * L)) store_edge<T, E>(dx, units, t + i * L, rounded<T, E>(v));
+        else store_pairs<T, E>(dx + units.col(t + i * L), v);
       }
   }
   if (!p.dweight.data && !p.dbias.data) return;
@@ -1343,15 +1436,18 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int j = 0; j < P; ++j) {
+      if (!SHIFT)
 #pragma unroll
-      for (int o = L; o < 32; o <<= 1) {
-        dw[i][j] = add2(dw[i][j], __shfl_xor_sync(0xffffffffu, dw[i][j], o));
-        db[i][j] = add2(db[i][j], __shfl_xor_sync(0xffffffffu, db[i][j], o));
-      }
-      if (sub == 0 && i < count) {
-        float* at = s_sums + warp * 2 * p.dim + (t + i * L) * E + 2 * j;
+        for (int o = L; o < 32; o <<= 1) {
+          dw[i][j] = add2(dw[i][j], __shfl_xor_sync(0xffffffffu, dw[i][j], o));
+          db[i][j] = add2(db[i][j], __shfl_xor_sync(0xffffffffu, db[i][j], o));
+        }
+      if ((SHIFT || sub == 0) && i < count) {
+        const int c = units.col(t + i * L) + 2 * j;
+        float* at = s_sums + (SHIFT ? warp * R + sub : warp) * 2 * p.dim + c;
         const float2 a = unpack2(dw[i][j]), b = unpack2(db[i][j]);
-        at[0] = a.x, at[1] = a.y, at[p.dim] = b.x, at[p.dim + 1] = b.y;
+        if (!SHIFT || units.in(t + i * L, 2 * j)) at[0] = a.x, at[p.dim] = b.x;
+        if (!SHIFT || units.in(t + i * L, 2 * j + 1)) at[1] = a.y, at[p.dim + 1] = b.y;
       }
     }
   __syncthreads();
@@ -1359,7 +1455,7 @@ __global__ void __launch_bounds__(32 * BACK_WARPS<NV>) k_layer_back_short(const 
   for (int c = threadIdx.x; c < 2 * p.dim; c += blockDim.x) {
     float v = 0.f;
 #pragma unroll
-    for (int q = 0; q < WARPS; ++q) v += s_sums[q * 2 * p.dim + c];
+    for (int q = 0; q < SETS; ++q) v += s_sums[q * 2 * p.dim + c];
     if (c < p.dim && out.dw) out.dw[c] = v;
     if (c >= p.dim && out.db) out.db[c - p.dim] = v;
   }
@@ -1411,11 +1507,12 @@ struct BackPlan {
   BackStage stage;
   int blocks;
   int teams() const { return s.per_sm; }
+  bool shift;  // SHORT: off the 16-byte grid
 };
-// Lanes of a row in k_layer_back_short, two vectors to each (past 32: four to each of 32).
+// Lanes of a row in k_layer_back_short, two vectors to each.
 int back_lanes(int64_t nvec) {
   int lanes = 4;
-  while (lanes < 64 && lanes * 2 < nvec) lanes *= 2;
+  while (lanes < 32 && lanes * 2 < nvec) lanes *= 2;
   return lanes;
 }
 // A block of 16 elements per thread (32 where 512 threads do not reach a row's end), and its ring.
@@ -1446,18 +1543,18 @@ BackPlan back_plan(const lipz_layernorm_backward_args& a) {
     const int64_t n = fill < most ? fill : most;
     return n < 1 ? 1 : (int)n;
   };
+  auto by_warps = [&](int64_t nvec) {
+    b.kind = BackPlan::SHORT;
+    const int lanes = back_lanes(nvec);
+    const int warps = BACK_WARPS, set = warps * 32 / lanes;
+    b.blocks = blocks(16 / warps, 2 * set);
+    // one block per group needs no second launch: where its turns are few, or more would come one after the other
+    const int64_t fill = (int64_t)(16 / warps) * sm_count() / groups;
+    if (fill < 4 && (ceil_div(a.rows, set) <= 16 || ceil_div(b.blocks * groups, sm_count()) >= b.blocks)) b.blocks = 1;
+    return b;
+  };
   if (back_vec(a)) {
-    const int64_t nvec = a.dim / e;
-    if (nvec <= 64) {
-      b.kind = BackPlan::SHORT;
-      const int lanes = back_lanes(nvec);
-      const int warps = lanes > 32 ? BACK_WARPS<4> : BACK_WARPS<2>, set = warps * (lanes > 32 ? 1 : 32 / lanes);
-      b.blocks = blocks(16 / warps, 2 * set);
-      // one block per group needs no second launch: where its turns are few, or more would come one after the other
-      const int64_t fill = (int64_t)(16 / warps) * sm_count() / groups;
-      if (fill < 4 && (ceil_div(a.rows, set) <= 16 || ceil_div(b.blocks * groups, sm_count()) >= b.blocks)) b.blocks = 1;
-      return b;
-    }
+    if (a.dim / e <= 64) return by_warps(a.dim / e);
     b.kind = BackPlan::STREAM;
     b.s = back_shape(a, &b.stage);
     b.blocks = blocks(1, 4 * b.teams());
@@ -1465,6 +1562,11 @@ BackPlan back_plan(const lipz_layernorm_backward_args& a) {
   }
   auto same = [&](const lipz_mat& m) { return same_shift(a.dy, m, a.groups, a.rows, e); };
   if (a.dim <= SHIFT_DIM && same(a.dx) && same(a.dsum) && (a.kept.data || same(a.s))) {
+    const int64_t units = ceil_div(a.dim + e - 1, e);
+    b.shift = true;
+    // (a warp's work on a row's ends weighs the more, the fewer rows share it, but rings of many groups leave each few
+    // blocks: 131072 x 77 53 us by warps, 95 through rings, 65536 x 301 89 and 71, 144 groups of 100 x 257 21 and 52)
+    if (units <= 16 || (units <= 64 && groups >= 8)) return by_warps(units);
     b.kind = BackPlan::SHIFT;
     b.s = back_shape(a, &b.stage);
     b.blocks = (int)shift_blocks(blocks(1, 4 * b.teams()), ceil_div(a.rows, b.teams()), e);
@@ -1484,25 +1586,29 @@ cudaError_t launch_back_rings(const LayerBack& p, const BackPlan& b, int64_t gro
   return launch_pdl(KERNEL, dim3(b.blocks, (unsigned)groups), dim3(b.s.tpr * b.teams()), rings > sums ? rings : sums, st,
                     p, b.stage, b.s.tpr, b.s.stages, b.s.slot, timeout_word());
 }
-template <typename T, int E, int NV, int L, bool KEPT>
+template <typename T, int L, bool KEPT, bool SHIFT>
 cudaError_t launch_back_short(const LayerBack& p, int64_t groups, int blocks, cudaStream_t st) {
-  constexpr auto kernel = k_layer_back_short<T, E, NV, L, KEPT>;
+  constexpr auto kernel = k_layer_back_short<T, 16 / sizeof(T), 2, L, KEPT, SHIFT>;
   const cudaError_t e = allow_smem<kernel>();
   return e != cudaSuccess ? e
-                          : launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(32 * BACK_WARPS<NV>),
-                                       (size_t)BACK_WARPS<NV> * 2 * p.dim * 4, st, p);
+                          : launch_pdl(kernel, dim3(blocks, (unsigned)groups), dim3(32 * BACK_WARPS),
+                                       (size_t)BACK_WARPS * (SHIFT ? 32 / L : 1) * 2 * p.dim * 4, st, p);
+}
+template <typename T, bool KEPT, bool SHIFT>
+cudaError_t launch_back_short(const LayerBack& p, int64_t groups, int blocks, cudaStream_t st) {
+  constexpr int E = 16 / sizeof(T);
+  const int lanes = back_lanes(ceil_div(p.dim + (SHIFT ? E - 1 : 0), E));
+  if (lanes == 32) return launch_back_short<T, 32, KEPT, SHIFT>(p, groups, blocks, st);
+  if (lanes == 16) return launch_back_short<T, 16, KEPT, SHIFT>(p, groups, blocks, st);
+  if (lanes == 8) return launch_back_short<T, 8, KEPT, SHIFT>(p, groups, blocks, st);
+  return launch_back_short<T, 4, KEPT, SHIFT>(p, groups, blocks, st);
 }
 template <typename T, bool KEPT>
 cudaError_t launch_back(const LayerBack& p, const BackPlan& b, int64_t groups, cudaStream_t st) {
   constexpr int E = 16 / sizeof(T);
-  if (b.kind == BackPlan::SHORT) {
-    const int lanes = back_lanes(p.dim / E);
-    if (lanes > 32) return launch_back_short<T, E, 4, 32, KEPT>(p, groups, b.blocks, st);
-    if (lanes == 32) return launch_back_short<T, E, 2, 32, KEPT>(p, groups, b.blocks, st);
-    if (lanes == 16) return launch_back_short<T, E, 2, 16, KEPT>(p, groups, b.blocks, st);
-    if (lanes == 8) return launch_back_short<T, E, 2, 8, KEPT>(p, groups, b.blocks, st);
-    return launch_back_short<T, E, 2, 4, KEPT>(p, groups, b.blocks, st);
-  }
+  if (b.kind == BackPlan::SHORT)
+    return b.shift ? launch_back_short<T, KEPT, true>(p, groups, b.blocks, st)
+                   : launch_back_short<T, KEPT, false>(p, groups, b.blocks, st);
   if (b.kind == BackPlan::STREAM)
     return b.s.wide ? launch_back_rings<k_layer_back_stream<T, E, 32 / E, KEPT, false>>(p, b, groups, st)
                     : launch_back_rings<k_layer_back_stream<T, E, 16 / E, KEPT, false>>(p, b, groups, st);
