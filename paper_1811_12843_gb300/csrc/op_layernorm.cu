@@ -835,7 +835,11 @@ cudaError_t launch_layer(LayerArgs& p, cudaStream_t st) {
     if (many && lanes <= 32) return launch_short<T, E, false>(p, lanes, st);
     if (many && lanes <= 64) return launch_short<T, E, 32 / E, 32, false>(p, st);
     if (many) {
-      const StreamShape s = stream_shape(p.dim, E, sizeof(T), arrays, 2048, 0, E == 8);
+      // bf16 rows in 32 elements per thread where one matrix alone keeps the loads going, and to 8 bits, whose second
+      // barrier costs a block of many warps more: 16384 x 4096 without residual 60 us (of 16 elements 71), with it 114
+      // (101, kept in 8 bits), 16384 x 8192 to 8 bits 188 (208), kept in 8 bits 221 (204).
+      const bool wide = E == 8 && (!p.residual.data || (p.scale.data && p.dim > 4096));
+      const StreamShape s = stream_shape(p.dim, E, sizeof(T), arrays, 2048, 0, wide);
       return s.wide ? launch_rings<k_layer_stream<T, E, 32 / E, false>>(p, s, 0, st)
                     : launch_rings<k_layer_stream<T, E, 16 / E, false>>(p, s, 0, st);
     }
