@@ -11,7 +11,12 @@ All individuals train at once, each with weights of its own (the operators' grou
 kept in fp32 with Adam's moments; the products read bf16 copies. Afterwards the weights are quantised
 row by row, and the same rows are scored over 8-bit operands.
 
-    python examples/residual_discriminators.py [--cells 12] [--steps 60]
+With --norm layer the norms have a mean and a bias (layernorm in the place of rmsnorm), and with --keep int8
+what a step keeps of its blocks for the backward pass takes 8 bits an element instead of 16: a block's sum
+and its pre-activations, written so by the calls that work them out, and its norm's result; the activations
+are worked out from the pre-activations again.
+
+    python examples/residual_discriminators.py [--cells 12] [--steps 60] [--norm layer [--keep int8]]
 """
 
 import argparse
@@ -30,20 +35,27 @@ BF16, F32 = torch.bfloat16, torch.float32
 class ResidualNets:
     """`cells` networks; parameters are fp32 tensors [cells, ...] by name."""
 
-    def __init__(self, cells, x_dim=784, width=256, hidden=512, depth=3, seed=0):
+    def __init__(self, cells, x_dim=784, width=256, hidden=512, depth=3, seed=0, norm="rms", keep8=False):
+        if keep8 and norm != "layer":
+            raise ValueError("the layer norm keeps its sum in 8 bits")
         gen = torch.Generator(device="cuda").manual_seed(seed)
-        self.depth, self.p = depth, {}
+        self.depth, self.p, self.layer, self.keep8 = depth, {}, norm == "layer", keep8
 
         def weight(name, n, k):
             self.p[name + ".w"] = torch.randn((cells, n, k), generator=gen, device="cuda") * k ** -0.5
             self.p[name + ".b"] = torch.zeros((cells, n), device="cuda")
 
+        def norm_weight(name):
+            self.p[name] = torch.ones((cells, width), device="cuda")
+            if self.layer:
+                self.p[name + ".b"] = torch.zeros((cells, width), device="cuda")
+
         weight("stem", width, x_dim)
         for i in range(depth):
-            self.p["%d.norm" % i] = torch.ones((cells, width), device="cuda")
+            norm_weight("%d.norm" % i)
             weight("%d.up" % i, hidden, width)
             weight("%d.down" % i, width, hidden)
-        self.p["norm"] = torch.ones((cells, width), device="cuda")
+        norm_weight("norm")
         weight("head", 1, width)
         self.refresh()
 
@@ -51,17 +63,35 @@ class ResidualNets:
         """The bf16 copies that the products read."""
         self.w = {k: v.to(BF16) for k, v in self.p.items() if k.endswith(".w")}
 
+    def norm(self, name, x, keep=True, **kw):
+        p = self.p
+        if not self.layer:
+            return ops.rmsnorm(x, p[name], keep=keep, **kw)
+        return ops.layernorm(x, p[name], p[name + ".b"], keep="int8" if keep and self.keep8 else keep, **kw)
+
+    def norm_backward(self, name, dy, n, g, dsum=None):
+        """The gradient of the norm's inputs; its parameters' go to g."""
+        if not self.layer:
+            dx, g[name] = ops.rmsnorm_backward(dy, n.sum, n.rstd, self.p[name], dsum=dsum)
+            return dx
+        dx, g[name], g[name + ".b"] = ops.layernorm_backward(dy, n.kept or n.sum, n.mean, n.rstd, self.p[name],
+                                                             dsum=dsum)
+        return dx
+
     def forward(self, x):
         """Logits [cells, rows] of x [cells, rows, x_dim], and what the backward pass reads. A block's
         result joins the stream in the norm of the block after it."""
         p, w = self.p, self.w
         delta, stream, kept = ops.linear(x, w["stem.w"], p["stem.b"])[0], None, []
         for i in range(self.depth):
-            n = ops.rmsnorm(delta, p["%d.norm" % i], residual=stream, keep=True)
-            a, pre = ops.linear(n.y, w["%d.up.w" % i], p["%d.up.b" % i], act="gelu", keep=True)
+            n = self.norm("%d.norm" % i, delta, residual=stream)
+            a, pre = ops.linear(n.y, w["%d.up.w" % i], p["%d.up.b" % i], act="gelu",
+                                keep="int8" if self.keep8 else True)
             delta, stream = ops.linear(a, w["%d.down.w" % i], p["%d.down.b" % i])[0], n.sum
-            kept.append((n, a, pre))
-        n = ops.rmsnorm(delta, p["norm"], residual=stream, keep=True)
+            if self.keep8:  # (the sum's own memory is free when the block after this one has read it)
+                n = n._replace(y=ops.checkpoint_rows(n.y), sum=None)
+            kept.append((n, None if self.keep8 else a, pre))
+        n = self.norm("norm", delta, residual=stream)
         logits = ops.linear(n.y, w["head.w"], p["head.b"], out_dtype=F32)[0]
         return logits[..., 0], (x, kept, n)
 
@@ -76,14 +106,15 @@ class ResidualNets:
             return dx
 
         dy = product("head", dlogits[..., None].to(BF16), n.y)
-        dstream, g["norm"] = ops.rmsnorm_backward(dy, n.sum, n.rstd, p["norm"])
+        dstream = self.norm_backward("norm", dy, n, g)
         for i in reversed(range(self.depth)):
             n, a, pre = kept[i]
+            if a is None:
+                a = ops.restore_rows(pre, act="gelu")
             # (dstream reaches both the block's result and the stream beside it)
             da = product("%d.down" % i, dstream, a)
             dh = product("%d.up" % i, da, n.y, act="gelu", pre=pre)
-            dstream, g["%d.norm" % i] = ops.rmsnorm_backward(dh, n.sum, n.rstd, p["%d.norm" % i],
-                                                             dsum=dstream)
+            dstream = self.norm_backward("%d.norm" % i, dh, n, g, dsum=dstream)
         product("stem", dstream, x, want_dx=False)
         return g
 
@@ -101,10 +132,10 @@ class ResidualNets:
 
         s = product("stem", ops.quantize_rows(x))
         for i in range(self.depth):
-            n = ops.rmsnorm(s, p["%d.norm" % i], e4m3=True)
+            n = self.norm("%d.norm" % i, s, keep=False, e4m3=True)
             a = product("%d.up" % i, (n.y, n.scale), act="gelu")
             product("%d.down" % i, ops.quantize_rows(a), residual=s, out=s)
-        n = ops.rmsnorm(s, p["norm"], e4m3=True)
+        n = self.norm("norm", s, keep=False, e4m3=True)
         return product("head", (n.y, n.scale), out_dtype=F32)[..., 0]
 
 
@@ -144,10 +175,12 @@ def main():
     ap.add_argument("--cells", type=int, default=12)
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--rows", type=int, default=100)
+    ap.add_argument("--norm", choices=("rms", "layer"), default="rms")
+    ap.add_argument("--keep", choices=("bf16", "int8"), default="bf16")
     a = ap.parse_args()
     pool = torch.from_numpy(lipz_synth.blob_pool(1811, n=4000, dim=784)).cuda()
     gen = torch.Generator(device="cuda").manual_seed(7)
-    nets = ResidualNets(a.cells)
+    nets = ResidualNets(a.cells, norm=a.norm, keep8=a.keep == "int8")
     opt = Adam(nets.p)
     for step in range(a.steps):
         x, labels = batch(pool, a.cells, a.rows, gen)
