@@ -384,8 +384,10 @@ typedef struct lipz_vec { /* fp32 */
  * row (the last ones: what there is) share a power of two 2^e, the smallest with e >= -126 that brings
  * their magnitudes below 127.5, and are rounded to its nearest multiples (ties to even): an element is off
  * by at most 2^e / 2, which is less than 2^-7 of its block's largest magnitude (or 2^-127). data: the
- * multiples, -127..127; scale: a byte e + 127 per 16 columns. The value q 2^e is a bf16 number. A block that
- * holds an infinity or a NaN has the byte 255 and stands for NaN throughout.
+ * multiples, -127..127; scale: a byte e + 127 per 16 columns. The value q 2^e is a bf16 number (an infinity
+ * where it passes bf16's range: of magnitudes from 127.5 2^121 on). A block that holds an infinity or a NaN
+ * has the byte 255 and stands for NaN throughout, whatever its data is; of the byte 0 all values are 0.
+ * Rows of data 16 bytes or a multiple apart, from 16-byte boundaries, are the fast case.
  */
 #define LIPZ_BLOCK 16
 typedef struct lipz_blocks {
@@ -494,7 +496,8 @@ LIPZ_API int lipz_linear_backward(const lipz_linear_backward_args* a, void* stre
  *     y = (s - mean) rstd weight + bias
  * with the types, results and buffers of lipz_rmsnorm; bias (nullable) [dim]; mean and rstd [rows]
  * (nullable) are kept for the backward pass. kept (nullable) receives what sum holds (without a
- * residual: x) as a checkpoint; with a residual it needs sum. Squares are summed in fp32, as they are.
+ * residual: x, as it was) as a checkpoint; with a residual it needs sum. The squares are of distances from
+ * the mean (or, in parts of a row, from their own means, and joined), so that a far mean costs no bits.
  */
 typedef struct lipz_layernorm_args {
   uint32_t struct_size;
@@ -510,8 +513,8 @@ LIPZ_API int lipz_layernorm(const lipz_layernorm_args* a, void* stream);
  * Its backward pass, from s (the x that was normalised, or sum), mean and rstd:
  *     h = (s - mean) rstd;  g = dy weight;  dx = rstd (g - mean(g) - h mean(g h)) + dsum;
  *     dweight = sum over rows of dy h;  dbias = sum over rows of dy
- * with the types and buffers of lipz_rmsnorm_backward; s is a matrix of dy's type, or (s null) the
- * checkpoint kept. dweight, dbias (each nullable): fp32, one per group.
+ * with the types of lipz_rmsnorm_backward; dx may be dy's, s's or dsum's own buffer. s is a matrix of dy's
+ * type, or (s null) the checkpoint kept. dweight, dbias (each nullable): fp32, one per group.
  */
 typedef struct lipz_layernorm_backward_args {
   uint32_t struct_size;
@@ -548,7 +551,9 @@ typedef struct lipz_restore_rows_args {
 } lipz_restore_rows_args;
 LIPZ_API int lipz_restore_rows(const lipz_restore_rows_args* a, void* stream);
 
-/* lipz_linear (call, whose pre is null) that keeps u, before any rounding, as the checkpoint pre. */
+/* lipz_linear (call, whose pre is null) that keeps u, before any rounding, as the checkpoint pre. Its sums over k
+ * are joined from more parts than lipz_linear's, since a multiple turns where u is off by as little as its distance
+ * from the middle between two: y is the same but for the order of its sums. */
 typedef struct lipz_linear_checkpoint_args {
   uint32_t struct_size;
   uint32_t reserved;

@@ -541,7 +541,7 @@ int overlap(const lipz_restore_rows_args& a) {
   return o.result();
 }
 int overlap(const lipz_linear_args& a, const lipz_blocks* kept = nullptr) {
-  Overlap o{"lipz_linear", a.groups};
+  Overlap o{kept ? "lipz_linear_checkpoint" : "lipz_linear", a.groups};
   const unsigned own = o.input("residual", a.residual, a.rows, a.n);
   o.input("x", a.x, a.rows, a.k);
   o.input("w", a.w, a.n, a.k);
@@ -556,7 +556,7 @@ int overlap(const lipz_linear_args& a, const lipz_blocks* kept = nullptr) {
   return o.result();
 }
 int overlap(const lipz_linear_backward_args& a, const lipz_blocks* x = nullptr, const lipz_blocks* pre = nullptr) {
-  Overlap o{"lipz_linear_backward", a.groups};
+  Overlap o{x ? "lipz_linear_backward_checkpoint" : "lipz_linear_backward", a.groups};
   o.input("dy", a.dy, a.rows, a.n);
   if (a.dw.data && x && x->data) o.input("x", *x, a.rows, a.k);
   else if (a.dw.data) o.input("x", a.x, a.rows, a.k);

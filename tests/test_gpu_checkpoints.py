@@ -206,6 +206,33 @@ def test_a_checkpoint_of_nan_and_infinity_stays_in_its_row():
         assert (pre.scale[1:3] == 255).all() and (pre.scale[0] != 255).all()
 
 
+@pytest.mark.parametrize("rows,k,n", [(3, 256, 37), (40, 256, 300), (130, 512, 1001), (700, 256, 264)])
+@pytest.mark.parametrize("gap", [0, 5, 48])
+def test_nothing_beside_a_checkpoints_rows(rows, k, n, gap):
+    """The C call with rows of its own: what lies between them, and the bytes behind the last block's, stay as they are."""
+    x, w = randn(17, (rows, k), 1.0), randn(18, (n, k), 0.1)
+    nb, row = -(-n // 16), n + gap
+    data = torch.full((rows + 1, row), 99, device="cuda", dtype=torch.int8)
+    scale = torch.full((rows + 1, nb + 3), 7, device="cuda", dtype=torch.uint8)
+    y = torch.empty(rows, n, device="cuda", dtype=BF16)
+    a = L.lipz_linear_checkpoint_args()
+    a.struct_size, a.call.struct_size = L.ctypes.sizeof(a), L.ctypes.sizeof(a.call)
+    a.call.groups, a.call.rows, a.call.k, a.call.n = 1, rows, k, n
+    a.call.x, a.call.w = L.lipz_mat(x.data_ptr(), 0, k, L.LIPZ_BF16, 0), L.lipz_mat(w.data_ptr(), 0, k, L.LIPZ_BF16, 0)
+    a.call.y = L.lipz_mat(y.data_ptr(), 0, n, L.LIPZ_BF16, 0)
+    a.pre = L.lipz_blocks(data.data_ptr(), 0, row, scale.data_ptr(), 0, nb + 3)
+    need = L.lipz_linear_checkpoint_workspace(a)
+    space = torch.empty(need + 256, device="cuda", dtype=torch.uint8)
+    a.call.workspace, a.call.workspace_bytes = (space.data_ptr() + 255) // 256 * 256, need
+    L.lipz_linear_checkpoint(a, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    ref = ops.linear(x, w, keep="int8")
+    assert torch.equal(y, ref[0])
+    assert torch.equal(data[:rows, :n], ref[1].data) and torch.equal(scale[:rows, :nb], ref[1].scale)
+    assert (data[:rows, n:] == 99).all() and (data[rows] == 99).all()
+    assert (scale[:rows, nb:] == 7).all() and (scale[rows] == 7).all()
+
+
 BACKWARDS = [(1, 1, 64, 32), (1, 37, 500, 1000), (1, 777, 500, 1001), (3, 100, 256, 512), (2, 65, 513, 77),
              (1, 1500, 784, 264), (1, 3000, 40, 24), (1, 0, 64, 32), (1, 9, 17, 1)]
 

@@ -35,7 +35,8 @@ NORM_SHAPES = [(1, 1, 1), (1, 1, 4096), (1, 3, 7), (1, 5, 64), (1, 37, 256), (3,
                (1, 4, 16383), (144, 100, 256), (1, 1, 16384), (1, 0, 64), (0, 4, 64)]
 # rows that start anywhere in a 16-byte unit, many of them; a dimension past the widest that is taken in units
 OFF_GRID = [(1, 1300, 257), (3, 300, 1001), (1, 650, 8191), (2, 700, 7), (1, 640, 1), (1, 700, 16383),
-            (5, 200, 12), (1, 900, 4100), (1, 1000, 16378), (1, 1300, 33)]
+            (5, 200, 12), (1, 900, 4100), (1, 1000, 16378), (1, 1300, 33), (1, 700, 8183), (1, 620, 8185), (3, 333, 505),
+            (2, 900, 506), (144, 9, 77), (700, 1, 129), (1, 3001, 1537), (90, 8, 300)]
 
 
 def norm64(x, residual, weight, bias, eps):
@@ -170,6 +171,54 @@ def test_y_over_x_keeps_x():
         assert torch.equal(own, ops.layernorm(x, w, b).y)
         check_blocks(ops.Checkpoint(data[:, :dim], scale), x)
         assert (data[:, dim:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [7, 900])
+@pytest.mark.parametrize("dim,cut", [(77, 3), (256, 8), (301, 1), (509, 5), (1001, 7), (4099, 2), (2000, 16)])
+def test_nan_beside_the_rows_stays_there(dtype, rows, dim, cut):
+    """Rows cut from wider ones whose other columns are NaN: the bits of the same rows by themselves."""
+    def cut_from(t):
+        wide = torch.full((rows, dim + 32), float("nan"), device="cuda", dtype=dtype)
+        wide[:, cut:cut + dim] = t
+        return wide[:, cut:cut + dim], wide
+
+    x, res, w, b = inputs(1, rows, dim, dtype, True, True, seed=31)
+    dy = randn(36, (rows, dim), 0.1, dtype)
+    (xc, _), (rc, _), (dc, _) = cut_from(x), cut_from(res), cut_from(dy)
+    for e4m3 in (False, True):
+        r = ops.layernorm(xc, w, b, residual=rc, e4m3=e4m3, keep="int8")
+        check(r, x, res, w, b, 1e-5, e4m3, "int8")
+    own, wide = cut_from(res)
+    got = ops.layernorm(xc, w, b, residual=own, sum_out=own, keep=True)
+    assert torch.equal(own, r.sum)
+    assert wide[:, :cut].isnan().all() and wide[:, cut + dim:].isnan().all()
+    back = ops.layernorm_backward(dc, own, got.mean, got.rstd, w, dsum=rc)
+    check_backward(back, dy, r.sum, got.mean, got.rstd, w, res)
+    back = ops.layernorm_backward(dc, r.kept, got.mean, got.rstd, w, dsum=rc)
+    check_backward(back, dy, ops.restore_rows(r.kept, out_dtype=F32), got.mean, got.rstd, w, res)
+    check_blocks(ops.checkpoint_rows(xc), x)
+
+
+def test_rows_behind_two_gigaelements():
+    """Offsets past 2^31: the last rows as by themselves."""
+    rows, dim, last = 270000, 8192, 700
+    x = torch.zeros(rows, dim, device="cuda", dtype=BF16)
+    x[-last:] = randn(45, (last, dim), 1.0)
+    w, b = 1 + randn(46, (dim,), 0.1, F32), randn(47, (dim,), 0.1, F32)
+    tail = x[-last:].clone()
+    few = ops.layernorm(tail, w, b, keep="int8")
+    r = ops.layernorm(x, w, b, keep="int8")
+    assert torch.equal(r.y[-last:], few.y) and torch.equal(r.mean[-last:], few.mean)
+    assert torch.equal(r.kept.data[-last:], few.kept.data) and torch.equal(r.kept.scale[-last:], few.kept.scale)
+    assert torch.equal(ops.restore_rows(r.kept)[-last:], ops.restore_rows(few.kept))
+    c = ops.checkpoint_rows(x)
+    assert torch.equal(c.data[-last:], few.kept.data)
+    dx, dw, db = ops.layernorm_backward(x, r.kept, r.mean, r.rstd, w)  # (dy is zero but for the last rows)
+    ref = ops.layernorm_backward(tail, few.kept, few.mean, few.rstd, w)
+    assert torch.equal(dx[-last:], ref[0]) and (dx[:-last] == 0).all()
+    for a, b2 in ((dw, ref[1]), (db, ref[2])):  # (summed in another order: 700 terms of order 1)
+        assert (a - b2).abs().max() <= 2 * 800 * 2.0 ** -24 * 700
 
 
 @pytest.mark.parametrize("rows", [9, 700])
