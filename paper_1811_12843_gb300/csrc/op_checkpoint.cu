@@ -1,4 +1,10 @@
-// Rows to checkpoints (8 bits, a power of two per 16 columns) and back. Bound: HBM.
+// Rows to checkpoints (8 bits, a power of two per 16 columns) and back.
+//
+//     e = max(-126, the smallest with max |v| < 127.5 2^e over 16 columns),  data = v 2^-e to the nearest whole number
+//
+// The power comes from the largest magnitude's bits, so that dividing by it is exact, and multiples are found by one
+// addition whose last bit is 1. A multiple of 8 bits times a power of two is a bf16 number: nothing is rounded on the
+// way back. Bound: HBM; with an activation its exponential beside it (16384 x 4096, gelu, back: 41 us, without 35).
 #include "ops.cuh"
 
 namespace lipz {

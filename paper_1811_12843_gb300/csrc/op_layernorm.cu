@@ -1,8 +1,21 @@
 // Layer norm with the residual's addition, forward (with the sum kept in 8 bits) and backward.
 //
+//     s = x + residual,  y = (s - mean) rstd w + b,  rstd = 1 / sqrt(mean((s - mean)^2) + eps)
+//     g = dy w,  dx = rstd (g - mean(g) - (s - mean) rstd^2 mean(g (s - mean))) + dsum
+//     dw = sum over rows of dy (s - mean) rstd,  db = sum over rows of dy
+//
 // A row's elements are read once and stay in the registers of its threads (multiples of 32 of them, NV
-// vectors of E elements each) between the row's sums and its results. Bound: HBM; a launch and two memory
-// latencies for a few rows.
+// vectors of E elements each) between the row's sums and its results, all in fp32, in an order that only sizes
+// decide. The sum of squares is of distances from means (join_shares), so that a row far from zero loses nothing.
+//
+// Bound: HBM, and what a row's two sums make it wait for; a launch and two memory latencies for a few rows.
+// Measured (a copy runs at 6784 GB/s; inputs larger than L2, a call's time among others):
+//   to bf16 and a checkpoint, with a residual, 16384 x 8192   204 us  0.88 of the copy rate (k_layer_stream)
+//   fp32, 8193 x 1001, with a residual                        27 us   0.72 (k_layer_stream, SHIFT)
+//   backward with dsum, 8192 x 4096                           57 us   0.69 (k_layer_back_stream, k_sum_pairs)
+//   backward over a checkpoint with dsum, 16384 x 2048        59 us   0.59 (the same)
+//   backward with dsum, 144 groups of 100 x 256               8.2 us  latency (k_layer_back_short)
+//   one row of 4096 to 8 bits                                 2.9 us  in a graph (k_layer_rows)
 #include "op_rows.cuh"
 
 namespace lipz {
@@ -409,7 +422,7 @@ __device__ __forceinline__ void store_edge_e4m3(e4m3* row, const Units<E>& u, in
 constexpr int SHORT_WARPS = 4;  // of a block
 
 // SHIFT: rows off the 16-byte grid, which all begin at the same place of a unit for a lane: the rows that it takes lie a
-// multiple of 16 rows' bytes apart. (Through rings, a row per warp, 65536 x 301 took 66 us and 131072 x 77 88; so 66 and 35.)
+// multiple of 16 rows' bytes apart. (131072 x 77 through rings, a row per warp, 88 us, so 35; 65536 x 301 66 both ways.)
 template <typename T, int E, int NV, int L, bool SHIFT>
 __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k_layer_short(const LayerArgs p) {
   constexpr int R = 32 / L, P = E / 2;
@@ -1146,11 +1159,16 @@ __device__ __forceinline__ void back_rows(const LayerBack& p, int64_t g, int64_t
 }
 
 // Teams of one row's threads, several to a block, walk over rows of one group (blockIdx.y), which arrive in a ring of
-// each; their sums for dweight and dbias stay in registers, and of 16 elements the weights. At the end the teams' sums are
-// added in shared memory: one part per SM is left for the launch that adds those (16384 x 2048 over a checkpoint: with a
-// part per team 65 us, 7 of them that launch; so 62). SHIFT: rows off the 16-byte grid, as in k_layer_stream; a
+// each; their sums for dweight and dbias stay in registers, and of 16 elements the weights. At the end the teams' sums
+// are added in shared memory: one part per SM is left for the launch that adds those (16384 x 2048 over a checkpoint:
+// with a part per team 65 us, 7 of them that launch; so 62). SHIFT: rows off the 16-byte grid, as in k_layer_stream; a
 // checkpoint's row lies at any byte: its multiples come from the words that hold them, and a unit's columns from two
 // blocks at most.
+//
+// Bound: instructions as much as HBM: about 26 for an element (two sums along the row, two down the columns, the
+// result, conversions), two elements at a time where the instruction exists, at two issued a clock by 16 warps of 128
+// registers (8192 x 4096 with dsum 51 us by itself, 61 % of HBM's time). Two rows of a team at once took 74, rows read
+// again in the place of registers 62 (640 threads), 8 elements per thread 79.
 constexpr int TEAM_THREADS = 512;  // of a block (registers)
 
 template <typename T, int E, int NV, bool KEPT, bool SHIFT>
@@ -1330,7 +1348,8 @@ __global__ void __launch_bounds__(TEAM_THREADS) k_layer_back_stream(const LayerB
 }
 
 // Short rows: L lanes to a row, 32 / L rows to a warp, loaded into registers one set ahead; a block of WARPS walks over
-// rows of one group, and its warps' sums are added in shared memory.
+// rows of one group, and its warps' sums are added in shared memory; where a block takes a whole group these are the
+// results, without a second launch (144 groups of 100 x 256, 30 MB: 6.2 us in a graph).
 constexpr int BACK_WARPS = 16;  // (registers)
 
 // SHIFT: rows off the 16-byte grid, as in k_layer_short: the columns of a warp's rows are different lanes', so that the
@@ -1465,7 +1484,8 @@ __global__ void __launch_bounds__(32 * BACK_WARPS) k_layer_back_short(const Laye
   }
 }
 
-// 32 columns per block, blockDim.y parts at a time, of dweight's sums (blockIdx.z = 0) or dbias's.
+// 32 columns per block, blockDim.y parts at a time, of dweight's sums (blockIdx.z = 0) or dbias's. Bound: latency (152
+// parts of 4096 columns, 5 MB, 6 us).
 __global__ void __launch_bounds__(1024)
     k_sum_pairs(const float* __restrict__ part, int parts, int64_t cols, lipz_vec dweight, lipz_vec dbias) {
   __shared__ float s[32][33];

@@ -227,6 +227,8 @@ struct DuArgs {
 
 // ALIGNED: rows of whole 16-byte units; else 8 columns are brought from the aligned words that hold them
 // (777 x 1001 with the copies beside it: one at a time 8.6 us, so 7.9, most of it latency).
+// KEPT: pre is a checkpoint, whose multiples are widened and multiplied by their power two at a time; four blocks to an SM,
+// so that 8192 x 4096 -> 4096 takes 370 us in all (by the registers that it would take, 390).
 template <bool ALIGNED, bool KEPT>
 __global__ void __launch_bounds__(256, KEPT ? 4 : 0) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
   constexpr int E = 8;
