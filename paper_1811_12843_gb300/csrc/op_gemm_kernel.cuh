@@ -41,12 +41,12 @@ static_assert(EPI_WARPS == SUM_WAYS, "a result warp per way");
 // bf16 results are such sums (of more chunks: 2^-15) from LONG_CHUNKS (16384 bf16) on, where a single sum has lost
 // 2^-13 and at 500000 bf16 of k 2.3e-3, more than half of their half unit.
 constexpr int SUM_CHUNKS = 8, BF16_SUM_CHUNKS = 64, LONG_CHUNKS = 256;
-// Results that are kept as a checkpoint are sums of about a quarter of k each (KEPT_MIN to KEPT_MAX chunks): a multiple turns
-// where the sum is off by as little as its distance from the middle between two, so an error of delta units moves delta
-// of the multiples by one, and their rms error grows with sqrt(delta). A sum over n chunks loses about n^2 of what one
-// over a single chunk does: 8192 x 4096 -> 8192 by single sums has 2.9e-4 of the values' rms, 1.1e-4 so, and 1.0e-4 by
-// fp32 additions to nearest. (A tile's first two sums are formed while the result warps are at the tile before, and so
-// are the longer ones.)
+// Results that are kept as a checkpoint are sums of about a quarter of k each (KEPT_MIN to KEPT_MAX chunks): a multiple
+// turns where the sum is off by as little as its distance from the middle between two, so an error of delta units moves
+// delta of the multiples by one, and their rms error grows with sqrt(delta). A sum over n chunks loses about n^2 of what
+// one over a single chunk does: 8192 x 4096 -> 8192 by single sums has 2.9e-4 of the values' rms, 1.1e-4 so, and 1.0e-4
+// by fp32 additions to nearest. (A tile's first two sums are formed while the result warps are at the tile before, and
+// so are the longer ones.)
 constexpr int KEPT_MIN = 2, KEPT_MAX = 16;
 struct SumChunks {
   int first, rest;  // of the first two sums, of the others
@@ -1075,7 +1075,8 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   if (KEPT) {
     const int64_t quarter = ceil_div(ceil_div(q.g[0].k * type_bytes(TYPE), ROW), 4);
     const int n = quarter < KEPT_MIN ? KEPT_MIN : quarter < most ? (int)quarter : most;
-    k.sum_chunks = {n + n / 4, n - n / 4};
+    const int first = most == SUM_CHUNKS && n + n / 4 > most ? most : n + n / 4;  // (fp32 results: none longer)
+    k.sum_chunks = {first, n - n / 4};
   }
   const Gemm& first = q.g[0];
   k.a_rows = FORWARD && CG == 1 && first.m < 128 ? (int)ceil_div(first.m, 8) * 8 : 128;
