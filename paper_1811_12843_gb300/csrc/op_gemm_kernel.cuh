@@ -242,6 +242,29 @@ __device__ __forceinline__ void load_row(const T* base, int64_t ld, int rows, in
     else w[i] = tc::pack_bf16(turn[lane * 17 + 2 * i], turn[lane * 17 + 2 * i + 1]);
   }
 }
+// W words at a 16-byte boundary, 32 bytes at a time where they lie on one of those: memory takes half of a sector as long
+// as a whole one. (Rows 16 bytes off, as every second one of 8 columns more than a multiple of 16 is: the weights'
+// gradients of 13 groups of 276 x 6728 -> 1424 218 us by 16 bytes, so 177; of 6736 columns 153.)
+template <int W>
+__device__ __forceinline__ void store_words(char* p, const uint32_t* w) {
+  const bool off = (uint64_t)p & 31;
+  auto one = [&](int i) {
+    *reinterpret_cast<uint4*>(p + 4 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  };
+  auto two = [&](int i) {
+    tc::st_global_v8(p + 4 * i, make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]),
+                     make_uint4(w[i + 4], w[i + 5], w[i + 6], w[i + 7]));
+  };
+  if (off) {
+    one(0);
+#pragma unroll
+    for (int i = 4; i + 8 < W; i += 8) two(i);
+    one(W - 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; i += 8) two(i);
+  }
+}
 template <typename T>
 __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int cols, int align,
                                           float* turn, const float* v) {
@@ -262,9 +285,7 @@ __device__ __forceinline__ void store_row(T* base, int64_t ld, int rows, int col
         tc::st_global_v8(p + 4 * i, make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]),
                          make_uint4(w[i + 4], w[i + 5], w[i + 6], w[i + 7]));
     } else {
-#pragma unroll
-      for (int i = 0; i < W; i += 4)
-        *reinterpret_cast<uint4*>(p + 4 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+      store_words<W>(p, w);
     }
     return;
   }
@@ -811,6 +832,17 @@ __global__ void __launch_bounds__(THREADS, 1)
           return;
         }
         const int64_t at = sl.y + (int64_t)(q * 32) * e.y.row + col0 + c;
+        if constexpr (CW == 32 && !FORWARD && !SUMS) {
+          if (p.y_align == 16 && columns_left(c) >= 32) {
+            if (lane < rows) {
+              uint32_t w[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w[i] = tc::pack_bf16(u[2 * i], u[2 * i + 1]);
+              store_words<16>(reinterpret_cast<char*>((bf16*)e.y.data + at + lane * e.y.row), w);
+            }
+            return;
+          }
+        }
 #pragma unroll
         for (int h = 0; h < CW; h += 16) {
           const int cols = columns_left(c + h);
@@ -1072,7 +1104,7 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   k.err = timeout_word();
   const int most = q.g[0].e.y.type == LIPZ_FP32 ? SUM_CHUNKS : KEPT ? KEPT_MAX : BF16_SUM_CHUNKS;
   k.sum_chunks = {most, most};
-  if (KEPT) {
+  if constexpr (KEPT != 0) {
     const int64_t quarter = ceil_div(ceil_div(q.g[0].k * type_bytes(TYPE), ROW), 4);
     const int n = quarter < KEPT_MIN ? KEPT_MIN : quarter < most ? (int)quarter : most;
     const int first = most == SUM_CHUNKS && n + n / 4 > most ? most : n + n / 4;  // (fp32 results: none longer)

@@ -15,7 +15,7 @@ torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     import paper_1811_12843_gb300 as L
     from paper_1811_12843_gb300 import operators as ops
-    from test_gpu_operators import SLOPE, act64, d, norm_shape, randn, sum_error, within
+    from test_gpu_operators import SLOPE, act64, backward_ref, d, norm_shape, randn, sum_error, within
 
 ACTS = ["none", "relu", "lrelu", "tanh", "gelu", "silu"]
 BF16, F32, F64, E4M3 = torch.bfloat16, torch.float32, torch.float64, torch.float8_e4m3fn
@@ -259,6 +259,22 @@ def test_linear_backward_over_checkpoints(groups, rows, k, n, act, whole):
         want = ops.linear_backward(dy, xv, w, act=act, slope=SLOPE, pre=prev if act != "none" else None, **wants)
         for a, b in zip(got, want):
             assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("groups,rows,k,n", [(1, 2100, 2056, 1992), (1, 300, 4104, 1000), (9, 270, 712, 360)])
+def test_gradients_in_rows_16_bytes_off(groups, rows, k, n, dtype):
+    """Widths of odd eights, whose rows begin on 16 bytes and on 32 by turns: against the formula in 64 bits over the
+    values of the checkpoints (the errors of test_gpu_operators.py's test_linear_backward)."""
+    shape = (lambda *s: norm_shape(groups, *s))
+    x, w = ops.checkpoint_rows(randn(61, shape(rows, k))), randn(62, shape(n, k), k ** -0.5)
+    pre, dy = ops.checkpoint_rows(randn(63, shape(rows, n), 1.5)), randn(64, shape(rows, n), 0.1)
+    dx, dw, _ = ops.linear_backward(dy, x, w, act="silu", pre=pre, dx_dtype=dtype, dw_dtype=dtype)
+    xv = ops.restore_rows(x)
+    _, rx, rw, _ = backward_ref(dy, xv, w, "silu", ops.restore_rows(pre))
+    size, delta, half = 1.2 * d(dy).abs(), 2.0 ** -8 + 2.0 ** -17, 2.0 ** -8 if dtype is BF16 else 2.0 ** -24
+    within(dx, rx, half * rx.abs() + (delta + sum_error(n)) * (size @ d(w).abs()) + 1e-30, "dx")
+    within(dw, rw, half * rw.abs() + (delta + sum_error(rows)) * (size.transpose(-1, -2) @ d(xv).abs()) + 1e-30, "dw")
 
 
 @pytest.mark.parametrize("act", ACTS)
