@@ -732,12 +732,13 @@ __global__ void __launch_bounds__(THREADS, 1)
           uint32_t w[4];
           bytes |= keep_block(cols, u + h, w) << (c + h) / 2;
           const bool second = (c + h) & 16;
-          if (COLSW >= 32 && p.pre_align == 32 && columns_left((c + h) & ~16) >= 32) {
-            if (second)
-              tc::st_global_v8(dst + h - 16, make_uint4(held[0], held[1], held[2], held[3]),
-                               make_uint4(w[0], w[1], w[2], w[3]));
-            else
+          if (COLSW >= 32 && p.pre_align && columns_left((c + h) & ~16) >= 32) {
+            if (!second) {
               held[0] = w[0], held[1] = w[1], held[2] = w[2], held[3] = w[3];
+            } else {
+              const uint32_t both[8] = {held[0], held[1], held[2], held[3], w[0], w[1], w[2], w[3]};
+              store_words<8>(reinterpret_cast<char*>(dst + h - 16), both);
+            }
           } else if (p.pre_align && cols >= 16) {
             *reinterpret_cast<uint4*>(dst + h) = make_uint4(w[0], w[1], w[2], w[3]);
           } else {
