@@ -12,7 +12,7 @@
 // Measured (a copy runs at 6784 GB/s; inputs larger than L2, a call's time among others):
 //   to bf16 and a checkpoint, with a residual, 16384 x 8192   204 us  0.88 of the copy rate (k_layer_stream)
 //   fp32, 8193 x 1001, with a residual                        27 us   0.72 (k_layer_stream, SHIFT)
-//   backward with dsum, 8192 x 4096                           57 us   0.69 (k_layer_back_stream, k_sum_pairs)
+//   backward with dsum, 8192 x 4096                           56 us   0.70 (k_layer_back_stream, k_sum_pairs)
 //   backward over a checkpoint with dsum, 16384 x 2048        59 us   0.59 (the same)
 //   backward with dsum, 144 groups of 100 x 256               8.2 us  latency (k_layer_back_short)
 //   one row of 4096 to 8 bits                                 2.9 us  in a graph (k_layer_rows)
@@ -988,19 +988,34 @@ __device__ __forceinline__ float warp_pair(float a, float b) {
   for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+// N pairs of sums as a tree, all loads in flight at once (one after the other 16384 x 8192 with dsum 190 us, so 184).
+template <int N>
+__device__ __forceinline__ uint64_t sum_places(const float2* s) {
+  uint64_t v[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const ulonglong2 q = reinterpret_cast<const ulonglong2*>(s)[i];
+    v[i] = add2(q.x, q.y);
+  }
+#pragma unroll
+  for (int o = N / 4; o; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < o; ++i) v[i] = add2(v[i], v[i + o]);
+  return v[0];
+}
 // A team's two sums, with one barrier (its own, `id`); s: a place per warp, by turns.
 __device__ __forceinline__ float2 team_sum(float2 v, float2* s, int warp, int warps, int id) {
   const float w = warp_pair(v.x, v.y);
   if (warps == 1) return make_float2(__shfl_sync(0xffffffffu, w, 0), __shfl_sync(0xffffffffu, w, 16));
   if ((threadIdx.x & 15) == 0) (&s[warp].x)[threadIdx.x >> 4 & 1] = w;
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(warps * 32) : "memory");
-  float2 r = s[0];
+  if (warps == 8) return unpack2(sum_places<8>(s));
+  if (warps == 16) return unpack2(sum_places<16>(s));
+  const uint64_t* pairs = reinterpret_cast<const uint64_t*>(s);
+  uint64_t r = pairs[0];
 #pragma unroll 4
-  for (int i = 1; i < warps; ++i) {
-    const float2 q = s[i];
-    r.x += q.x, r.y += q.y;
-  }
-  return r;
+  for (int i = 1; i < warps; ++i) r = add2(r, pairs[i]);
+  return unpack2(r);
 }
 
 // A vector of what was normalised, as it lies in memory: of dy's type, or a checkpoint's multiples and their unit (SHIFT:
@@ -1178,7 +1193,7 @@ __global__ void __launch_bounds__(TEAM_THREADS) k_layer_back_stream(const LayerB
   constexpr bool HELD = NV * E == 16;
   static_assert(!SHIFT || HELD, "weights in registers");
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float2 s_red[2][TEAM_THREADS / 32];
+  __shared__ __align__(16) float2 s_red[2][TEAM_THREADS / 32];
   const bool has_dsum = p.dsum.data;
   const int teams = blockDim.x / tpr, team = threadIdx.x / tpr, t = threadIdx.x - team * tpr, warps = tpr >> 5;
   const int ring_bytes = RING_BARS + stages * slot;
