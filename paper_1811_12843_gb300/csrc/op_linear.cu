@@ -228,7 +228,8 @@ struct DuArgs {
 // ALIGNED: rows of whole 16-byte units; else 8 columns are brought from the aligned words that hold them
 // (777 x 1001 with the copies beside it: one at a time 8.6 us, so 7.9, most of it latency).
 // KEPT: pre is a checkpoint, whose multiples are widened and multiplied by their power two at a time; four blocks to an SM,
-// so that 8192 x 4096 -> 4096 takes 370 us in all (by the registers that it would take, 390).
+// a row at a time, which needs no more registers than those have (8192 x 4096, gelu, the sums alone: 36.0 us; four rows
+// at a time 37.5 with spills, 37.6 with three blocks; of five or six blocks, which are no whole waves, 46).
 template <bool ALIGNED, bool KEPT>
 __global__ void __launch_bounds__(256, KEPT ? 4 : 0) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
   constexpr int E = 8;
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(256, KEPT ? 4 : 0) k_du(const DuArgs p, const 
   with_act(p.act, [&](auto act) {
     constexpr int ACT = decltype(act)::value;
     if (c < p.n) {
-#pragma unroll 4
+#pragma unroll (KEPT ? 1 : 4)
       for (int64_t r = r0 + ty; r < r1; r += 8) {
         float d[E];
         load(p.dy, r, d);
