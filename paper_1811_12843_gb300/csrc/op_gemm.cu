@@ -118,7 +118,7 @@ GemmPlan plan_products(const Products& q) {
         double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0);
         // A checkpoint beside them: its own stores, and each sum's way into registers. In 256-wide tiles the MMAs are
         // ahead by no more than the first two sums, five eighths of k. (8192 x 1024 -> 4096 66 us by 256 x 128, 92 by
-        // 256 x 256; 8192 x 4096 -> 8192 394 and 322.)
+        // 256 x 256; 8192 x 4096 -> 8192 394 and, by four sums, 322.)
         if (kept) epi += c.bn * (c.bn == 256 ? 10 : 3) + kept_sums(o.chunks_per_split) * (c.bn == 256 ? 2700. : 1300.);
         if (kept && c.bn == 256) epi += 0.375 * mma;
         const double unit = mma > epi ? mma : epi;

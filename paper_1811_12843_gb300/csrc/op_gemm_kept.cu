@@ -1,6 +1,6 @@
 // The products that keep their pre-activations as a checkpoint (op_gemm_kernel.cuh): kernels of their own, since
-// beside the other results these cost registers. Measured: 8192 x 4096 -> 8192 with SiLU 321 to 349 us (0.91 to 0.84
-// of cuBLAS's rate; the power limit), 144 x 100 x 256 -> 512 with gelu 22 by itself (68 MB, 10 us; four chunks of k to
+// beside the other results these cost registers. Measured: 8192 x 4096 -> 8192 with SiLU 338 to 365 us (0.86 to 0.80
+// of cuBLAS's rate; the power limit, and six sums to a tile), 144 x 100 x 256 -> 512 with gelu 22 by itself (68 MB, 10 us; four chunks of k to
 // a tile, whose results take longer than its operands).
 #include "op_gemm_kernel.cuh"
 

@@ -44,10 +44,10 @@ constexpr int SUM_CHUNKS = 8, BF16_SUM_CHUNKS = 64, LONG_CHUNKS = 256;
 // Results that are kept as a checkpoint are sums of about a quarter of k each (KEPT_MIN to KEPT_MAX chunks): a multiple
 // turns where the sum is off by as little as its distance from the middle between two, so an error of delta units moves
 // delta of the multiples by one, and their rms error grows with sqrt(delta). A sum over n chunks loses about n^2 of what
-// one over a single chunk does: 8192 x 4096 -> 8192 by single sums has 2.9e-4 of the values' rms, 1.1e-4 so, and 1.0e-4
-// by fp32 additions to nearest. (A tile's first two sums are formed while the result warps are at the tile before, and
+// one over a single chunk does: 8192 x 4096 -> 8192 by single sums has 2.9e-4 of the values' rms, by sums of up to 16
+// chunks 1.45e-4 (321 us), of 12 so 1.2e-4 (338), of 8 0.9e-4 (395), and 1.0e-4 by fp32 additions to nearest. (A tile's first two sums are formed while the result warps are at the tile before, and
 // so are the longer ones.)
-constexpr int KEPT_MIN = 2, KEPT_MAX = 16;
+constexpr int KEPT_MIN = 2, KEPT_MAX = 12;
 struct SumChunks {
   int first, rest;  // of the first two sums, of the others
   __host__ __device__ __forceinline__ int end(int c0, int kc) const { return kc + (kc - c0 < 2 * first ? first : rest); }
@@ -1103,12 +1103,13 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   }
   if (sums) k.sums = *sums;
   k.err = timeout_word();
-  const int most = q.g[0].e.y.type == LIPZ_FP32 ? SUM_CHUNKS : KEPT ? KEPT_MAX : BF16_SUM_CHUNKS;
+  const bool fp32_results = q.g[0].e.y.type == LIPZ_FP32;
+  const int most = fp32_results ? SUM_CHUNKS : KEPT ? KEPT_MAX : BF16_SUM_CHUNKS;
   k.sum_chunks = {most, most};
   if constexpr (KEPT != 0) {
     const int64_t quarter = ceil_div(ceil_div(q.g[0].k * type_bytes(TYPE), ROW), 4);
     const int n = quarter < KEPT_MIN ? KEPT_MIN : quarter < most ? (int)quarter : most;
-    const int first = most == SUM_CHUNKS && n + n / 4 > most ? most : n + n / 4;  // (fp32 results: none longer)
+    const int first = fp32_results && n + n / 4 > most ? most : n + n / 4;  // (fp32 results: none longer)
     k.sum_chunks = {first, n - n / 4};
   }
   const Gemm& first = q.g[0];
