@@ -13,7 +13,7 @@
 //   to bf16 and a checkpoint, with a residual, 16384 x 8192   204 us  0.88 of the copy rate (k_layer_stream)
 //   fp32, 8193 x 1001, with a residual                        27 us   0.72 (k_layer_stream, SHIFT)
 //   backward with dsum, 8192 x 4096                           56 us   0.70 (k_layer_back_stream, k_sum_pairs)
-//   backward over a checkpoint with dsum, 16384 x 2048        59 us   0.59 (the same)
+//   backward over a checkpoint with dsum, 16384 x 2048        60 us   0.58 (the same)
 //   backward with dsum, 144 groups of 100 x 256               8.2 us  latency (k_layer_back_short)
 //   one row of 4096 to 8 bits                                 2.9 us  in a graph (k_layer_rows)
 #include "op_rows.cuh"
