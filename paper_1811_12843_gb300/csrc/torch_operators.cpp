@@ -275,10 +275,16 @@ int keep_of(const Call& c, PyObject* o) {
   if (PyUnicode_CompareWithASCIIString(o, "int8")) c.refuse("keep must be False, True or \"int8\"");
   return 2;
 }
+// Of a call that keeps nothing in 8 bits: a word would be taken for True, and what it asks for left out.
+bool keep_plain(const Call& c, PyObject* o) {
+  if (PyUnicode_Check(o)) c.refuse("keep must be False or True: nothing is kept in 8 bits here");
+  return truth(o);
+}
 
 // x, weight, residual, eps, e4m3, keep, sum_out -> y, sum, scale, rstd
 PyObject* rmsnorm(PyObject* const* o) {
   Call c{"rmsnorm"};
+  const bool keep = keep_plain(c, o[5]);
   lipz_rmsnorm_args a{};
   a.struct_size = sizeof a;
   a.x = c.first(o[0], "x", WIDE);
@@ -286,7 +292,7 @@ PyObject* rmsnorm(PyObject* const* o) {
   a.weight = c.vec(o[1], "weight", c.cols);
   a.eps = number(o[3]);
   a.groups = c.groups, a.rows = c.rows, a.dim = c.cols;
-  const bool e4m3 = truth(o[4]), keep = truth(o[5]), own_sum = o[6] != Py_None;
+  const bool e4m3 = truth(o[4]), own_sum = o[6] != Py_None;
   const ScalarType type = a.x.type == LIPZ_FP32 ? F32 : BF16;
   Tensor y, sum, scale, rstd;
   if (o[2] == Py_None) {

@@ -94,7 +94,8 @@ def rmsnorm(x, weight, residual=None, eps=1e-6, e4m3=False, keep=False, sum_out=
     x, residual: bf16 or fp32; weight [columns] (or [groups, columns]) fp32. ``sum`` is s in x's type
     (x itself without a residual), written to ``sum_out`` if given (it may be x or residual: the
     residual stream updated in place). y has x's type; with ``e4m3`` it is float8_e4m3fn and
-    y scale[row] the values. ``keep``: return rstd, which the backward pass reads."""
+    y scale[row] the values. ``keep`` (False or True; the layer norm alone keeps its sum in 8 bits):
+    return rstd, which the backward pass reads."""
     return Norm._make((_module or _load()).rmsnorm(x, weight, residual, eps, e4m3, keep, sum_out))
 
 
