@@ -7,10 +7,15 @@
 // checkpoint and makes six results 14.5 us, now 9.2.)
 #include <Python.h>
 
+#include <ATen/Context.h>
 #include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
+#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
+#include <ATen/record_function.h>
 #include <c10/core/InferenceMode.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -147,10 +152,22 @@ struct Call {
     if (!adjacent(t)) refuse(std::string(what) + ": columns must be adjacent");
     return {(float*)t.const_data_ptr(), grouped ? t.stride(0) : 0};
   }
-  // (from torch's allocator, as at::empty but for its way through the dispatcher: norm with a checkpoint, seven results,
-  // 14.5 us of the host, so 9.2)
+  // Whether an allocation goes through torch's dispatcher: a dispatch mode or a transform of this thread's, or the
+  // profiler, is to see it, or memory is to be filled. Else the same tensor comes from the allocator itself (norm with a
+  // checkpoint, seven results: 14.5 us of the host by the dispatcher, so 9.2).
+  static bool dispatched() {
+    const auto keys = c10::impl::tls_local_dispatch_key_set().included_ - c10::default_included_set;
+    const auto& context = at::globalContext();
+    return !keys.empty() || at::getStepCallbacksUnlessEmpty(at::RecordScope::FUNCTION).has_value() ||
+           (context.deterministicAlgorithms() && context.deterministicFillUninitializedMemory());
+  }
+  at::TensorOptions options(ScalarType t) const {
+    return at::TensorOptions().dtype(t).device(c10::kCUDA, (c10::DeviceIndex)device);
+  }
   Tensor empty(const Shape& s, ScalarType t) const {
-    return Tensor(at::detail::empty_generic(at::IntArrayRef(s.d, s.dims), c10::cuda::CUDACachingAllocator::get(),
+    const at::IntArrayRef size(s.d, s.dims);
+    if (dispatched()) return at::empty(size, options(t));
+    return Tensor(at::detail::empty_generic(size, c10::cuda::CUDACachingAllocator::get(),
                                             c10::DispatchKeySet(c10::DispatchKey::CUDA), t, std::nullopt));
   }
   lipz_mat fresh(Tensor& t, int64_t r, int64_t c, ScalarType type) const {
@@ -182,9 +199,11 @@ struct Call {
     const int64_t n = (c + LIPZ_BLOCK - 1) / LIPZ_BLOCK, row = n * LIPZ_BLOCK;
     const int64_t size[3] = {groups, r, c}, stride[3] = {r * row, row, 1};
     const int skip = grouped ? 0 : 1;
-    q = Tensor(at::detail::empty_strided_generic(
-        at::IntArrayRef(size + skip, 3 - skip), at::IntArrayRef(stride + skip, 3 - skip),
-        c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), ScalarType::Char));
+    const at::IntArrayRef sizes(size + skip, 3 - skip), strides(stride + skip, 3 - skip);
+    q = dispatched() ? at::empty_strided(sizes, strides, options(ScalarType::Char))
+                     : Tensor(at::detail::empty_strided_generic(sizes, strides, c10::cuda::CUDACachingAllocator::get(),
+                                                                c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                                ScalarType::Char));
     s = empty(matrix(r, n), ScalarType::Byte);
     return {(int8_t*)q.mutable_data_ptr(), r * row, row, (uint8_t*)s.mutable_data_ptr(), r * n, n};
   }
