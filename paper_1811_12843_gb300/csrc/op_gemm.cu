@@ -50,9 +50,10 @@ __global__ void __launch_bounds__(256) k_finish(const __grid_constant__ FinishPa
   }
 }
 
+template <bool KEPT>
 __global__ void __launch_bounds__(256) k_copy_rows(const __grid_constant__ CopyJobs jobs) {
   pdl_wait();
-  copy_rows(jobs, blockIdx.x);
+  copy_rows<KEPT>(jobs, blockIdx.x);
 }
 
 // Blocks of 8 rows by 32 columns' threads; columns past 65535 blocks are looped over.
@@ -209,6 +210,7 @@ CopyJobs copy_jobs(const RowCopy* c, int n) {
   jobs.n = n;
   for (int i = 0; i < n; ++i) {
     jobs.c[i] = c[i];
+    jobs.kept = jobs.kept || c[i].scale;
     jobs.blocks += ceil_div(c[i].total, COPY_ROWS * 32 / c[i].lanes);
   }
   return jobs;
@@ -216,7 +218,8 @@ CopyJobs copy_jobs(const RowCopy* c, int n) {
 
 cudaError_t run_copies(const CopyJobs& jobs, cudaStream_t st) {
   if (jobs.blocks == 0) return cudaSuccess;
-  return launch_pdl(k_copy_rows, dim3((unsigned)jobs.blocks), dim3(256), 0, st, jobs);
+  return launch_pdl(jobs.kept ? k_copy_rows<true> : k_copy_rows<false>, dim3((unsigned)jobs.blocks), dim3(256), 0, st,
+                    jobs);
 }
 
 cudaError_t run_products(const GemmPlan& plan, const Products& q, void* workspace, const PartSums* sums,

@@ -85,6 +85,7 @@ constexpr int COPY_ROWS = 8;  // rows of a block, of 32 lanes each
 struct CopyJobs {
   RowCopy c[4];
   int n;
+  bool kept;  // some of them are of checkpoints
   int64_t blocks;
 };
 CopyJobs copy_jobs(const RowCopy* c, int n);

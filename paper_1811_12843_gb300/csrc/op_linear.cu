@@ -230,12 +230,13 @@ struct DuArgs {
 // KEPT: pre is a checkpoint, whose multiples are widened and multiplied by their power two at a time; four blocks to an SM,
 // a row at a time, which needs no more registers than those have (8192 x 4096, gelu, the sums alone: 36.0 us; four rows
 // at a time 37.5 with spills, 37.6 with three blocks; of five or six blocks, which are no whole waves, 46).
-template <bool ALIGNED, bool KEPT>
+// COPIES: rows of checkpoints may be among those copied.
+template <bool ALIGNED, bool KEPT, bool COPIES>
 __global__ void __launch_bounds__(256, KEPT ? 4 : 0) k_du(const DuArgs p, const __grid_constant__ CopyJobs jobs) {
   constexpr int E = 8;
   __shared__ float s[8][32 * E + 1];
   pdl_wait();
-  if ((int)blockIdx.x >= p.blocks) return copy_rows(jobs, (int)blockIdx.x - p.blocks);
+  if ((int)blockIdx.x >= p.blocks) return copy_rows<COPIES>(jobs, (int)blockIdx.x - p.blocks);
   const int per = p.col_blocks * p.row_blocks, in_group = blockIdx.x % per;
   const int row_block = in_group / p.col_blocks, col_block = in_group - row_block * p.col_blocks;
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
@@ -439,12 +440,10 @@ cudaError_t linear_backward(const lipz_linear_backward_args& a, const lipz_block
     const DuArgs p{a.dy, a.pre, kept_pre, du, part, a.rows, a.n, b.ldu, b.rows_per_block, a.act, a.slope,
                    (int)cols, (int)b.blocks, (int)blocks};
     const dim3 grid((unsigned)(blocks + jobs.blocks));
-    if (kept_pre.data)
-      e = b.vec ? launch_pdl(k_du<true, true>, grid, dim3(256), 0, st, p, jobs)
-                : launch_pdl(k_du<false, true>, grid, dim3(256), 0, st, p, jobs);
-    else
-      e = b.vec ? launch_pdl(k_du<true, false>, grid, dim3(256), 0, st, p, jobs)
-                : launch_pdl(k_du<false, false>, grid, dim3(256), 0, st, p, jobs);
+    auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(256), 0, st, p, jobs); };
+    if (kept_pre.data) e = b.vec ? run(k_du<true, true, true>) : run(k_du<false, true, true>);
+    else if (jobs.kept) e = b.vec ? run(k_du<true, false, true>) : run(k_du<false, false, true>);
+    else e = b.vec ? run(k_du<true, false, false>) : run(k_du<false, false, false>);
   } else {
     e = run_copies(jobs, st);
   }

@@ -395,13 +395,16 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w) {
   }
 }
 
-// A row's copy in whole 16-byte units (the bytes past its last element are zero), by `lanes` lanes of a warp; of a
-// checkpoint's row (p.bytes: its columns) the bf16 values that it stands for, 16 at a time.
+// A row's copy in whole 16-byte units (the bytes past its last element are zero), by the 32 lanes of a warp; of a
+// checkpoint's row (p.bytes: its columns) the bf16 values that it stands for, 16 at a time, by p.lanes lanes. KEPT: there
+// may be such rows. (Kernels that know of none are shorter: over 8-bit operands 1459 x 88 -> 3947 with both in one kernel
+// took 26.9 us, so 25.0, 1137 x 3304 -> 2048 24.8 and 22.9.)
+template <bool KEPT>
 __device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
   const int64_t g = r / p.rows, at = r - g * p.rows;
   const uint8_t* s = p.src + g * p.group + at * p.ld;
   uint4* d = (uint4*)p.dst + r * p.units;
-  if (p.scale) {
+  if (KEPT && p.scale) {
     const uint8_t* scale = p.scale + g * p.scale_group + at * p.scale_ld;
     const bool whole = ((uint64_t)s & 15) == 0, wide = ((uint64_t)d & 31) == 0;
 #pragma unroll 4
@@ -435,13 +438,14 @@ __device__ __forceinline__ void copy_row(const RowCopy& p, int64_t r) {
   for (int64_t u = threadIdx.x & 31; u < p.units; u += 32) d[u] = bytes16(s + u * 16, p.bytes - u * 16);
 }
 // Block `b` of 256 threads: 8 rows per warp's worth of lanes, of one copy after the other.
+template <bool KEPT>
 __device__ __forceinline__ void copy_rows(const CopyJobs& jobs, int64_t b) {
   for (int j = 0; j < jobs.n; ++j) {
-    const int rows = COPY_ROWS * 32 / jobs.c[j].lanes;
+    const int lanes = KEPT ? jobs.c[j].lanes : 32, rows = COPY_ROWS * 32 / lanes;
     const int64_t blocks = (jobs.c[j].total + rows - 1) / rows;
     if (b < blocks) {
-      const int64_t r = b * rows + threadIdx.x / jobs.c[j].lanes;
-      if (r < jobs.c[j].total) copy_row(jobs.c[j], r);
+      const int64_t r = b * rows + threadIdx.x / lanes;
+      if (r < jobs.c[j].total) copy_row<KEPT>(jobs.c[j], r);
       return;
     }
     b -= blocks;
