@@ -129,8 +129,8 @@ GemmPlan plan_products(const Products& q) {
         if (o.splits > 1 && !forward) extra += (double)g.groups * g.m * g.n * 4 * o.splits * 2 / 3000;
         split = split || o.splits > 1;
       }
-      // (sums in 256-wide tiles: bf16 results of a checkpoint's product alone)
-      if (!fits || (s0 > 1 && !split) || (t.sums && c.bn > 128 && !kept)) continue;
+      // (sums in 256-wide tiles: bf16 results of a checkpoint's product, and of those no others)
+      if (!fits || (s0 > 1 && !split) || (c.bn > 128 && t.sums != kept)) continue;
       double waves = work / (slots * top);
       waves = waves < 1 ? 0 : (double)(int64_t)(waves + 0.999) - 1;
       // (a cluster's CTA finishes 64 / s0 columns of up to 128 rows, an element per thread and turn)

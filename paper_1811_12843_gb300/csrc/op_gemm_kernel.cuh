@@ -1175,7 +1175,9 @@ cudaError_t launch_shape(const Products& q, const GemmPlan& p, float* const* par
     if (p.bn == 128) return launch<KEPT, TYPE, 1, 128, FORWARD, float>(q, p, parts, sums, st);
     return launch<KEPT, TYPE, 1, 64, FORWARD, float>(q, p, parts, sums, st);
   }
-  if (p.cg == 2 && p.bn == 256) return launch<KEPT, TYPE, 2, 256, FORWARD, bf16>(q, p, parts, sums, st);
+  if constexpr (KEPT == 0) {  // (of a kept one results take longer than so few chunks' MMAs: never planned in 256-wide tiles)
+    if (p.cg == 2 && p.bn == 256) return launch<KEPT, TYPE, 2, 256, FORWARD, bf16>(q, p, parts, sums, st);
+  }
   if constexpr (FORWARD) {
     if (p.cg == 2 && results_by_tma(q.g[0]))
       return launch<KEPT, TYPE, 2, 128, true, bf16, true>(q, p, parts, sums, st);
