@@ -383,7 +383,7 @@ typedef struct lipz_vec { /* fp32 */
  * A checkpoint: a matrix of activations kept in 8 bits for a backward pass. Each 16 adjacent columns of a
  * row (the last ones: what there is) share a power of two 2^e, the smallest with e >= -126 that brings
  * their magnitudes below 127.5, and are rounded to its nearest multiples (ties to even): an element is off
- * by at most 2^e / 2, which is less than 2^-7 of its block's largest magnitude (or 2^-127). data: the
+ * by at most 2^e / 2, which is 1 / 127.5 of its block's largest magnitude or less (or 2^-127). data: the
  * multiples, -127..127; scale: a byte e + 127 per 16 columns. The value q 2^e is a bf16 number (an infinity
  * where it passes bf16's range: of magnitudes from 127.5 2^121 on). A block that holds an infinity or a NaN
  * has the byte 255 and stands for NaN throughout, whatever its data is; of the byte 0 all values are 0.

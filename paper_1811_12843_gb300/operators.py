@@ -115,8 +115,8 @@ class Checkpoint(NamedTuple):
     """Activations kept in 8 bits. Each 16 adjacent columns (the last ones: what there is) share a power of
     two 2^e, the smallest with e >= -126 that brings their magnitudes below 127.5: ``data`` holds its nearest
     multiples, int8 [.., rows, columns], ``scale`` the bytes e + 127, uint8 [.., rows, ceil(columns / 16)].
-    The values data 2^e are bf16 numbers, off by less than 2^-7 of their block's largest; a block with an
-    infinity or NaN (byte 255) stands for NaN. Rows may be strided; those that a call here allocates begin
+    The values data 2^e are bf16 numbers, off by at most 1 / 127.5 of their block's largest (or 2^-127); a block
+    with an infinity or NaN (byte 255) stands for NaN. Rows may be strided; those that a call here allocates begin
     16 bytes or a multiple apart."""
     data: torch.Tensor
     scale: torch.Tensor
