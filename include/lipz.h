@@ -497,7 +497,9 @@ LIPZ_API int lipz_linear_backward(const lipz_linear_backward_args* a, void* stre
  * with the types, results and buffers of lipz_rmsnorm; bias (nullable) [dim]; mean and rstd [rows]
  * (nullable) are kept for the backward pass. kept (nullable) receives what sum holds (without a
  * residual: x, as it was) as a checkpoint; with a residual it needs sum. The squares are of distances from
- * the mean (or, in parts of a row, from their own means, and joined), so that a far mean costs no bits.
+ * the mean (or, in parts of a row, from their own means, and joined), so that those of a far mean do not
+ * cancel. What a far mean costs is the rounding of s and of the mean: with q = |mean| rstd 2^-24, errors of
+ * the order of q in (s - mean) rstd, and of q rstd in rstd.
  */
 typedef struct lipz_layernorm_args {
   uint32_t struct_size;
