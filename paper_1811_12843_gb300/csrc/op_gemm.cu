@@ -117,9 +117,11 @@ GemmPlan plan_products(const Products& q) {
                (!forward || o.splits == s0);
         const double mma = o.chunks_per_split * 4 * c.step * (eb == 1 ? 1.16 : 1);
         double epi = c.epi + (heavy ? c.act : 0) + (res ? c.residual : 0);
-        // A checkpoint beside them: its own stores, and each sum's way into registers. In 256-wide tiles the MMAs are
-        // ahead by no more than the first two sums, five eighths of k. (8192 x 1024 -> 4096 66 us by 256 x 128, 92 by
-        // 256 x 256; 8192 x 4096 -> 8192 394 and, by four sums, 322.)
+        // A checkpoint beside them: its own stores, and its sums' way into registers, priced as sums of a quarter of the
+        // part; in 256-wide tiles, where the MMAs are ahead by two sums, three eighths of their time. (8192 x 1024 ->
+        // 4096 66 us by 256 x 128, 92 by 256 x 256; 8192 x 4096 -> 8192 398 and 323, 4100 x 8192 -> 4096 228 and 178.)
+        // Prices fitted to such times, not counts of the sums that run (SumChunks): by those all of the latter went to
+        // 256 x 128, and small products to parts of k (519 x 1408 -> 128 over 8-bit operands 6.8 us, so 9.5).
         if (kept) epi += c.bn * (c.bn == 256 ? 10 : 3) + kept_sums(o.chunks_per_split) * (c.bn == 256 ? 2700. : 1300.);
         if (kept && c.bn == 256) epi += 0.375 * mma;
         const double unit = mma > epi ? mma : epi;

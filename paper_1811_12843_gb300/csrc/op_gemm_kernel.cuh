@@ -41,12 +41,14 @@ static_assert(EPI_WARPS == SUM_WAYS, "a result warp per way");
 // bf16 results are such sums (of more chunks: 2^-15) from LONG_CHUNKS (16384 bf16) on, where a single sum has lost
 // 2^-13 and at 500000 bf16 of k 2.3e-3, more than half of their half unit.
 constexpr int SUM_CHUNKS = 8, BF16_SUM_CHUNKS = 64, LONG_CHUNKS = 256;
-// Results that are kept as a checkpoint are sums of about a quarter of k each (KEPT_MIN to KEPT_MAX chunks): a multiple
-// turns where the sum is off by as little as its distance from the middle between two, so an error of delta units moves
-// delta of the multiples by one, and their rms error grows with sqrt(delta). A sum over n chunks loses about n^2 of what
-// one over a single chunk does: 8192 x 4096 -> 8192 by single sums has 2.9e-4 of the values' rms, by sums of up to 16
-// chunks 1.45e-4 (321 us), of 12 so 1.2e-4 (338), of 8 0.9e-4 (395), and 1.0e-4 by fp32 additions to nearest. (A tile's first two sums are formed while the result warps are at the tile before, and
-// so are the longer ones.)
+// Results that are kept as a checkpoint are sums of n chunks by and large, about a quarter of k, from KEPT_MIN to
+// KEPT_MAX (or SUM_CHUNKS): the first two, which are formed while the result warps are at the tile before, of 5 n / 4,
+// the others of 3 n / 4. So no sum is over more than 15 chunks (960 of k in bf16, 1920 in 8 bits), beside fp32 results
+// over more than 8. A multiple turns where the sum is off by as little as its distance from the middle between two, so an
+// error of delta units moves delta of the multiples by one, and their rms error grows with sqrt(delta). A sum over n
+// chunks loses about n^2 of what one over a single chunk does. Of the values' rms, 8192 x 4096 -> 8192 has 2.8e-4 by
+// single sums, 1.45e-4 with KEPT_MAX at 16 (321 us), 1.2e-4 at 12, as it is (338), 0.9e-4 at 8 (395), and 1.0e-4 by fp32
+// additions to nearest.
 constexpr int KEPT_MIN = 2, KEPT_MAX = 12;
 struct SumChunks {
   int first, rest;  // of the first two sums, of the others
@@ -1106,11 +1108,10 @@ cudaError_t launch(const Products& q, const GemmPlan& plan, float* const* parts,
   const bool fp32_results = q.g[0].e.y.type == LIPZ_FP32;
   const int most = fp32_results ? SUM_CHUNKS : KEPT ? KEPT_MAX : BF16_SUM_CHUNKS;
   k.sum_chunks = {most, most};
-  if constexpr (KEPT != 0) {
+  if (KEPT) {
     const int64_t quarter = ceil_div(ceil_div(q.g[0].k * type_bytes(TYPE), ROW), 4);
-    const int n = quarter < KEPT_MIN ? KEPT_MIN : quarter < most ? (int)quarter : most;
-    const int first = fp32_results && n + n / 4 > most ? most : n + n / 4;  // (fp32 results: none longer)
-    k.sum_chunks = {first, n - n / 4};
+    const int n = quarter < KEPT_MIN ? KEPT_MIN : quarter < most ? (int)quarter : most, longer = n + n / 4;
+    k.sum_chunks = {fp32_results && longer > most ? most : longer, n - n / 4};  // (fp32 results: none longer)
   }
   const Gemm& first = q.g[0];
   k.a_rows = FORWARD && CG == 1 && first.m < 128 ? (int)ceil_div(first.m, 8) * 8 : 128;

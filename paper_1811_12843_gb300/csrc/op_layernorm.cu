@@ -446,10 +446,12 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS, E == 4 && NV == 8 ? 3 : 4) k
   }
   const uint32_t whole = ((1u << count) - 1u) & ~edge;
   auto edges = [&](auto f) {
-    if (!SHIFT || !edge) return;
+    if constexpr (SHIFT) {
+      if (!edge) return;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (edge >> i & 1) f(i, t + i * L);
+      for (int i = 0; i < NV; ++i)
+        if (edge >> i & 1) f(i, t + i * L);
+    }
   };
   pdl_wait();
   Raw<T, E> x[NV], res[NV];
@@ -618,10 +620,12 @@ __global__ void __launch_bounds__(512, E * NV == 16 || E == 8 ? 2 : 1)
   const uint32_t whole = ((1u << count) - 1u) & ~edge;
   // (few threads have any: apart from the others' code, whose instructions bound bf16 rows)
   auto edges = [&](auto f) {
-    if (!SHIFT || !edge) return;
+    if constexpr (SHIFT) {
+      if (!edge) return;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (edge >> i & 1) f(i);
+      for (int i = 0; i < NV; ++i)
+        if (edge >> i & 1) f(i);
+    }
   };
   const float n = (float)__reduce_add_sync(0xffffffffu, held), inv_n = n > 0.f ? 1.f / n : 0.f;
   pdl_wait();
@@ -1181,10 +1185,11 @@ __device__ __forceinline__ void back_rows(const LayerBack& p, int64_t g, int64_t
 // checkpoint's row lies at any byte: its multiples come from the words that hold them, and a unit's columns from two
 // blocks at most.
 //
-// Bound: instructions as much as HBM: about 26 for an element (two sums along the row, two down the columns, the
-// result, conversions), two elements at a time where the instruction exists, at two issued a clock by 16 warps of 128
-// registers (8192 x 4096 with dsum 51 us by itself, 61 % of HBM's time). Two rows of a team at once took 74, rows read
-// again in the place of registers 62 (640 threads), 8 elements per thread 79.
+// Bound: latency at 16 warps of 128 registers. 8192 x 4096 with dsum takes 51 us by itself, with DRAM in use for 61 % of
+// them and half of the issue slots: between two instructions a warp waits for the one before (1.7 clocks), at the row's
+// barrier (1.5) and for shared memory (1.5). An element takes 26 instructions, of which about nine are its arithmetic and
+// conversions (two elements at a time where the instruction exists); the rest is a row's: reduction, barrier, ring, moves.
+// Two rows of a team at once took 74, rows read again in the place of registers 62 (640 threads), 8 elements per thread 79.
 constexpr int TEAM_THREADS = 512;  // of a block (registers)
 
 template <typename T, int E, int NV, bool KEPT, bool SHIFT>

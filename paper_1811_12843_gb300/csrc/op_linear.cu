@@ -62,7 +62,8 @@ struct VecParams {
   int rows, parts;  // warps that share an output
 };
 
-// KEPT: u is kept as a checkpoint: VEC_WARPS * parts warps, so that a block has 16 outputs.
+// KEPT: u is kept as a checkpoint: VEC_WARPS * parts warps, so that a block has 16 outputs. (Up to 512 threads have 128
+// registers each; four rows in whole vectors spill 56 bytes there, over 8 bits 160.)
 template <int TYPE, int R, bool VEC, bool KEPT>
 __global__ void __launch_bounds__(32 * VEC_WARPS * (KEPT ? VEC_WARPS : 1)) k_linear_rows(const VecParams p) {
   using L = Elem<TYPE>;
