@@ -3,8 +3,8 @@
 // documentation (operators.py). Written against torch's C++ interface because next to kernels of a few
 // microseconds the same steps in Python took most of a call: the norm of one row of 4096 to 8 bits 17 us, now 6.5 to
 // 8 with two microseconds of kernel, 37 x 1000 -> 500 over 8-bit operands 18.5, now 7.6, the backward of 777 x 500 ->
-// 1001 38, now 16. (One guard to a call, results made without torch's dispatcher: the layer norm that keeps a
-// checkpoint and makes six results 14.5 us, now 9.2.)
+// 1001 38, now 16. (One guard to a call, results made without torch's dispatcher where nothing listens to it: the
+// layer norm that keeps a checkpoint and makes six results 14.5 us, now 9.2.)
 #include <Python.h>
 
 #include <ATen/Context.h>
@@ -153,8 +153,8 @@ struct Call {
     return {(float*)t.const_data_ptr(), grouped ? t.stride(0) : 0};
   }
   // Whether an allocation goes through torch's dispatcher: a dispatch mode or a transform of this thread's, or the
-  // profiler, is to see it, or memory is to be filled. Else the same tensor comes from the allocator itself (norm with a
-  // checkpoint, seven results: 14.5 us of the host by the dispatcher, so 9.2).
+  // profiler, is to see it, or memory is to be filled. Else the same tensor comes from the allocator itself (the layer
+  // norm with a checkpoint: 14.5 us of the host by the dispatcher, so 9.2).
   static bool dispatched() {
     const auto keys = c10::impl::tls_local_dispatch_key_set().included_ - c10::default_included_set;
     const auto& context = at::globalContext();
